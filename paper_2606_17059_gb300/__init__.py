@@ -16,18 +16,21 @@ import numpy as np
 from . import build as _build
 
 __all__ = [
-    "P2PError", "Router", "build", "library_path",
+    "P2PError", "Router", "KvCache", "build", "library_path",
     "p2p_router_create", "p2p_router_destroy", "p2p_router_set_stream", "p2p_router_sync", "p2p_last_error",
     "p2p_router_num_trees", "p2p_router_launch_count", "p2p_snapshot_build", "p2p_snapshot_view", "p2p_snapshot_free",
     "p2p_flat_tree_validate", "p2p_tree_upload", "p2p_tree_build", "p2p_tree_download", "p2p_tree_apply_delta",
     "p2p_tree_apply_delta_static", "p2p_tree_stats", "p2p_route_batch", "p2p_route_batch_host", "p2p_route_decide",
     "p2p_router_kernel_clock", "p2p_router_kernel_time", "p2p_update_estimates", "p2p_route_batch_decide",
     "p2p_lru_enable", "p2p_lru_insert", "p2p_lru_access", "p2p_lru_evict", "p2p_hit_rate", "p2p_route_prepare",
+    "p2p_kv_create", "p2p_kv_destroy", "p2p_kv_set_stream", "p2p_kv_sync", "p2p_kv_last_error", "p2p_kv_launch_count",
+    "p2p_kv_stats", "p2p_kv_extend", "p2p_kv_write", "p2p_kv_fork", "p2p_kv_trim", "p2p_kv_compact", "p2p_kv_attend",
 ]
 
 P2P_OK, P2P_E_INVAL, P2P_E_NOMEM, P2P_E_FORMAT, P2P_E_CUDA, P2P_E_DEVICE = 0, -1, -2, -3, -4, -5
 P2P_OP_INSERT, P2P_OP_DELETE = 0, 1
 P2P_MEM_HOST, P2P_MEM_DEVICE = 0, 1
+P2P_KV_BF16, P2P_KV_F16, P2P_KV_E4M3 = 0, 1, 2
 ERROR_NAMES = {-1: "P2P_E_INVAL", -2: "P2P_E_NOMEM", -3: "P2P_E_FORMAT", -4: "P2P_E_CUDA", -5: "P2P_E_DEVICE"}
 FLAT_FIELDS = ("label_off", "label_len", "child_begin", "child_count", "term_count",
                "child_first_tok", "child_idx", "labels")
@@ -60,6 +63,12 @@ class Seqs(ctypes.Structure):
 
 class Delta(ctypes.Structure):
     _fields_ = [("op", _vp), ("seqs", Seqs), ("peer_begin", _vp), ("mem", _i32)]
+
+
+class KvLayout(ctypes.Structure):
+    _fields_ = ([(f, _i32) for f in ("type", "n_layers", "n_pages", "page_tokens", "n_heads", "head_dim", "n_seqs", "max_pages")]
+                + [(f, _i64) for f in ("layer_stride", "page_stride", "token_stride", "head_stride")]
+                + [(f, _vp) for f in ("k", "v", "k_scale", "v_scale", "table", "length", "refs")])
 
 
 _lib = None
@@ -104,6 +113,20 @@ def _load():
             "p2p_lru_evict": (ctypes.c_int, [_vp, _i32, _i64, P(_i64)]),
             "p2p_hit_rate": (ctypes.c_int, [_vp, _vp, _vp, _i64, _vp, _vp]),
             "p2p_route_prepare": (ctypes.c_int, [_vp, _vp, _i64, _vp, _i64]),
+            "p2p_kv_create": (ctypes.c_int, [P(KvLayout), P(_vp)]),
+            "p2p_kv_destroy": (None, [_vp]),
+            "p2p_kv_set_stream": (ctypes.c_int, [_vp, _vp]),
+            "p2p_kv_sync": (ctypes.c_int, [_vp]),
+            "p2p_kv_last_error": (ctypes.c_char_p, [_vp]),
+            "p2p_kv_launch_count": (_i64, [_vp]),
+            "p2p_kv_stats": (ctypes.c_int, [_vp, P(_i64 * 4)]),
+            "p2p_kv_extend": (ctypes.c_int, [_vp, _i32, _vp, _vp]),
+            "p2p_kv_write": (ctypes.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i32]),
+            "p2p_kv_fork": (ctypes.c_int, [_vp, _i32, _vp, _vp, _vp]),
+            "p2p_kv_trim": (ctypes.c_int, [_vp, _i32, _vp, _vp]),
+            "p2p_kv_compact": (ctypes.c_int, [_vp]),
+            "p2p_kv_attend": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _i64, _i64, _i32, _i32, ctypes.c_float, _i32, _vp, _i64,
+                                             _i64, _vp]),
             "p2p_router_kernel_time": (ctypes.c_int, [_vp, _i32, P(ctypes.c_char_p), P(_i64), P(ctypes.c_double)]),
         }
         for name, (res, args) in sig.items():
@@ -418,7 +441,233 @@ def p2p_route_batch_host(r, tokens: np.ndarray, offsets: np.ndarray, B: int, loa
                                         _addr(out_match), _addr(out_peer)), r)
 
 
-# ---- convenience wrapper ----------------------------------------------------------------------------------
+# ---- the paged key-value cache ----------------------------------------------------------------------------
+
+def _kv_check(rc: int, kv=None):
+    if rc != P2P_OK:
+        msg = _load().p2p_kv_last_error(kv)
+        raise P2PError(rc, msg.decode() if msg else "")
+
+
+def p2p_kv_create(layout: KvLayout):
+    """Handle on the cache that `layout` describes (its device arrays must outlive the handle)."""
+    h = _vp()
+    _kv_check(_load().p2p_kv_create(ctypes.byref(layout), ctypes.byref(h)))
+    return h
+
+
+def p2p_kv_destroy(kv) -> None:
+    _load().p2p_kv_destroy(kv)
+
+
+def p2p_kv_set_stream(kv, stream=None) -> None:
+    s = None
+    if stream is not None:
+        s = stream if isinstance(stream, int) else stream.cuda_stream
+    _kv_check(_load().p2p_kv_set_stream(kv, s), kv)
+
+
+def p2p_kv_sync(kv) -> None:
+    _kv_check(_load().p2p_kv_sync(kv), kv)
+
+
+def p2p_kv_last_error(kv=None) -> str:
+    m = _load().p2p_kv_last_error(kv)
+    return m.decode() if m else ""
+
+
+def p2p_kv_launch_count(kv) -> int:
+    return int(_load().p2p_kv_launch_count(kv))
+
+
+KV_STAT_NAMES = ("pages_used", "pages_shared", "pages_end", "tokens")
+
+
+def p2p_kv_stats(kv) -> dict:
+    out = (_i64 * 4)()
+    _kv_check(_load().p2p_kv_stats(kv, ctypes.byref(out)), kv)
+    return dict(zip(KV_STAT_NAMES, [int(x) for x in out]))
+
+
+def p2p_kv_extend(kv, n: int, seq, count) -> None:
+    """Room for count[i] more tokens of sequence seq[i] (CUDA int32 tensors or addresses, as below)."""
+    _kv_check(_load().p2p_kv_extend(kv, n, _addr(seq), _addr(count)), kv)
+
+
+def p2p_kv_write(kv, layer: int, n_layers: int, n: int, seq, offsets, n_tokens: int, k, v, layer_stride: int, token_stride: int,
+                 head_stride: int, dtype: int) -> None:
+    """Keys and values of the sequences' last tokens; k and v are addresses (their strides are arguments)."""
+    _kv_check(_load().p2p_kv_write(kv, layer, n_layers, n, _addr(seq), _addr(offsets), n_tokens, k, v, layer_stride, token_stride,
+                                   head_stride, dtype), kv)
+
+
+def p2p_kv_fork(kv, n: int, src, dst, n_tokens) -> None:
+    _kv_check(_load().p2p_kv_fork(kv, n, _addr(src), _addr(dst), _addr(n_tokens)), kv)
+
+
+def p2p_kv_trim(kv, n: int, seq, n_tokens) -> None:
+    _kv_check(_load().p2p_kv_trim(kv, n, _addr(seq), _addr(n_tokens)), kv)
+
+
+def p2p_kv_compact(kv) -> None:
+    _kv_check(_load().p2p_kv_compact(kv), kv)
+
+
+def p2p_kv_attend(kv, layer: int, n: int, seq, q, q_row_stride: int, q_head_stride: int, dtype: int, n_heads: int, scale: float,
+                  window: int, out, out_row_stride: int, out_head_stride: int, lse=None) -> None:
+    """One new token of each sequence; q and out are addresses (their strides are arguments)."""
+    _kv_check(_load().p2p_kv_attend(kv, layer, n, _addr(seq), q, q_row_stride, q_head_stride, dtype, n_heads, scale, window, out,
+                                    out_row_stride, out_head_stride, _addr(lse)), kv)
+
+
+# ---- convenience wrappers ---------------------------------------------------------------------------------
+
+class KvCache:
+    """A paged key-value cache (p2p_kv) over the caller's CUDA tensors.
+
+    k, v      [layers, pages, tokens a page, heads, head dim] of bfloat16, float16 or float8_e4m3fn, strided alike; the
+              order of the dimensions in memory is free (see p2p_kv_layout), the last is contiguous
+    table     int32 [sequences, pages a sequence]; length int32 [sequences]; refs int32 [pages]
+    k_scale, v_scale   float32 [layers, heads], with float8_e4m3fn only
+
+    ``KvCache.empty`` allocates them.  Calls run on `stream` (torch's current one at construction) and return before their
+    work is done; tensors made or used on another stream are the caller's to order.  What the device finds wrong is
+    raised by ``sync``."""
+
+    def __init__(self, k, v, table, length, refs, k_scale=None, v_scale=None, stream=None):
+        import torch
+        self._types = {torch.bfloat16: P2P_KV_BF16, torch.float16: P2P_KV_F16, torch.float8_e4m3fn: P2P_KV_E4M3}
+        if k.dim() != 5 or k.dtype not in self._types or v.dtype != k.dtype or v.shape != k.shape or v.stride() != k.stride():
+            raise ValueError("k and v must be [layers, pages, page tokens, heads, head dim] of one type and of the same strides")
+        if k.shape[4] > 1 and k.stride(4) != 1:
+            raise ValueError("the last dimension of k and v must be contiguous")
+        layers, pages, page, heads, dim = k.shape
+        if table.dim() != 2 or tuple(length.shape) != (table.shape[0],) or tuple(refs.shape) != (pages,):
+            raise ValueError("table must be [sequences, entries], length [sequences], refs [pages]")
+        scales = (k_scale, v_scale)
+        for t in scales:
+            if t is not None and tuple(t.shape) != (layers, heads):
+                raise ValueError("scales must be [layers, heads]")
+        for t, dtype in ((table, torch.int32), (length, torch.int32), (refs, torch.int32), (k_scale, torch.float32),
+                         (v_scale, torch.float32)):
+            if t is not None and (t.dtype != dtype or not t.is_contiguous()):
+                raise ValueError(f"table, length, refs (int32) and scales (float32) must be contiguous: got {t.dtype}")
+        if any(t is not None and t.device != k.device for t in (v, table, length, refs, *scales)) or not k.is_cuda:
+            raise ValueError("the cache's tensors must be on one CUDA device")
+        self.k, self.v, self.table, self.length, self.refs = k, v, table, length, refs
+        self.k_scale, self.v_scale = scales
+        self.layers, self.heads, self.dim, self.n_seqs = layers, heads, dim, table.shape[0]
+        a = KvLayout(self._types[k.dtype], layers, pages, page, heads, dim, table.shape[0], table.shape[1], *k.stride()[:4],
+                     k.data_ptr(), v.data_ptr(), _addr(k_scale), _addr(v_scale), table.data_ptr(), length.data_ptr(), refs.data_ptr())
+        self.device = k.device
+        with torch.cuda.device(k.device):
+            self._h = p2p_kv_create(a)
+            self.stream = stream if stream is not None else torch.cuda.current_stream()
+        p2p_kv_set_stream(self._h, self.stream)
+
+    @classmethod
+    def empty(cls, layers: int, pages: int, page: int, heads: int, dim: int, n_seqs: int, max_pages: int, dtype=None, k_scale=None,
+              v_scale=None, device="cuda", stream=None):
+        """An empty cache whose pages keep each head's tokens together (dtype: bfloat16 unless given)."""
+        import torch
+        k, v = (torch.zeros((layers, pages, heads, page, dim), dtype=dtype or torch.bfloat16, device=device).transpose(2, 3)
+                for _ in "kv")
+        table, length, refs = (torch.zeros(s, dtype=torch.int32, device=device) for s in ((n_seqs, max_pages), n_seqs, pages))
+        return cls(k, v, table, length, refs, k_scale, v_scale, stream)
+
+    @property
+    def handle(self):
+        return self._h
+
+    def close(self):
+        if getattr(self, "_h", None) is not None:
+            p2p_kv_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        self.close()
+
+    def _list(self, first, *others):
+        """The length of a call's lists (int32 CUDA tensors, one entry an item)."""
+        n = first.numel()
+        for t in (first, *others):
+            if t.numel() != n or t.element_size() != 4 or t.is_floating_point() or t.device != self.device:
+                raise ValueError("lists must be int32 tensors of one length on the cache's device")
+        return n
+
+    def extend(self, seq, count) -> None:
+        """Room for count[i] more tokens of sequence seq[i]; shared last pages are copied first."""
+        p2p_kv_extend(self._h, self._list(seq, count), seq, count)
+
+    def trim(self, seq, n_tokens) -> None:
+        """Sequence seq[i] keeps its first n_tokens[i] tokens."""
+        p2p_kv_trim(self._h, self._list(seq, n_tokens), seq, n_tokens)
+
+    def fork(self, src, dst, n_tokens) -> None:
+        """The empty sequence dst[i] becomes the first n_tokens[i] tokens of src[i], whose pages it shares."""
+        p2p_kv_fork(self._h, self._list(src, dst, n_tokens), src, dst, n_tokens)
+
+    def compact(self) -> None:
+        """Moves the pages in use to the front of the pool."""
+        p2p_kv_compact(self._h)
+
+    def write(self, layer: int, seq, offsets, k, v) -> None:
+        """Keys and values of the last offsets[i+1] - offsets[i] tokens of sequence seq[i]: k and v [layers, tokens, heads,
+        head dim] for layers layer, layer + 1, ... (or [tokens, heads, head dim] for one); offsets int64 [n + 1]."""
+        n = self._list(seq)
+        s = k.stride()
+        if k.dim() == 3:
+            layers, s = 1, (0, *s)
+        elif k.dim() == 4:
+            layers = k.shape[0]
+        else:
+            layers = -1
+        if layers < 0 or v.shape != k.shape or v.stride() != k.stride() or tuple(k.shape[-2:]) != (self.heads, self.dim) \
+                or v.dtype != k.dtype or k.dtype not in self._types or (self.dim > 1 and s[3] != 1):
+            raise ValueError("k and v must be [layers, tokens, heads, head dim] or [tokens, heads, head dim], strided alike, "
+                             "the last dimension contiguous")
+        if offsets.numel() != n + 1 or offsets.element_size() != 8 or offsets.is_floating_point():
+            raise ValueError("offsets must be int64 [n + 1]")
+        if k.device != self.device or v.device != self.device or offsets.device != self.device:
+            raise ValueError("tensors must be on the cache's device")
+        p2p_kv_write(self._h, layer, layers, n, seq, offsets, k.shape[-3], k.data_ptr(), v.data_ptr(), s[0], s[1], s[2],
+                     self._types[k.dtype])
+
+    def attend(self, layer: int, q, scale=None, seq=None, window: int = 0, out=None, lse=None):
+        """One new token of each sequence (of seq, int32, or sequences 0, 1, ...): q [n, query heads, head dim]; scale: head
+        dim ** -0.5 unless given.  Returns (out like q, lse float32 [n, query heads])."""
+        import torch
+        n, heads, dim = q.shape
+        if dim != self.dim or q.dtype not in self._types or (dim > 1 and q.stride(2) != 1):
+            raise ValueError("q must be [n, query heads, head dim], the last dimension contiguous")
+        if seq is not None and self._list(seq) != n:
+            raise ValueError("seq must have one entry per row of q")
+        if out is None:
+            out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype != q.dtype or (dim > 1 and out.stride(2) != 1):
+            raise ValueError("out must be like q, the last dimension contiguous")
+        if lse is None:
+            lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+        elif tuple(lse.shape) != (n, heads) or lse.dtype != torch.float32:
+            raise ValueError("lse must be float32 [n, query heads]")
+        if q.device != self.device or out.device != self.device or lse.device != self.device:
+            raise ValueError("tensors must be on the cache's device")
+        qs, os_ = q.stride(), out.stride()
+        p2p_kv_attend(self._h, layer, n, seq, q.data_ptr(), qs[0], qs[1], self._types[q.dtype], heads,
+                      dim ** -0.5 if scale is None else scale, window, out.data_ptr(), os_[0], os_[1], lse)
+        return out, lse
+
+    def stats(self) -> dict:
+        """Pages in use, shared pages, the highest page in use + 1, tokens held (waits for queued work)."""
+        return p2p_kv_stats(self._h)
+
+    def launch_count(self) -> int:
+        return p2p_kv_launch_count(self._h)
+
+    def sync(self) -> None:
+        """Waits for queued work; raises what the device found wrong since the last call."""
+        p2p_kv_sync(self._h)
+
 
 class Router:
     """Owns one p2p_router.  Device work runs on torch's current CUDA stream at construction."""

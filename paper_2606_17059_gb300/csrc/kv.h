@@ -1,0 +1,87 @@
+// kv.h -- the paged key-value cache (p2p_kv_* of p2p_router.h): what its host code and its kernels share.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "p2p_router.h"
+
+namespace p2p {
+
+// Division of x < 2^31 by a fixed 1 <= d < 2^31: floor(x / d) = (x * mul) >> shift with shift = 31 + ceil(log2 d) and
+// mul = ceil(2^shift / d) = (2^shift + e) / d, 0 <= e < d.  The product over 2^shift is x / d + (x * e / 2^shift) / d; as
+// x * e < 2^shift, that is less than 1 / d above x / d, which does not reach the next whole number.
+struct FastDiv {
+  uint32_t d = 1, shift = 31;
+  uint64_t mul = 1ull << 31;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t n) : d(n) {
+    uint32_t l = 0;
+    while ((1ull << l) < n) ++l;
+    shift = 31 + l;
+    mul = ((1ull << shift) + n - 1) / n;
+  }
+  __host__ __device__ __forceinline__ uint32_t div(uint32_t x) const { return (uint32_t)((x * mul) >> shift); }
+  __host__ __device__ __forceinline__ uint32_t ceil(uint32_t x) const { return x ? div(x - 1) + 1 : 0; }
+};
+
+// The cache as the kernels see it; strides in bytes.
+struct KvView {
+  char *k, *v;
+  const float *k_scale, *v_scale;
+  int32_t *table, *length, *refs;
+  int32_t n_layers, n_pages, page, heads, dim, type, n_seqs, max_pages;
+  int64_t layer_stride, page_stride, token_stride, head_stride;
+  FastDiv by_page;
+  int32_t row16;  // 16-byte pieces of a head's values of one token
+};
+
+// Bits of the device error word.
+enum { KV_BAD_SEQ = 1, KV_BAD_COUNT = 2, KV_NO_PAGES = 4, KV_BAD_PAGE = 8, KV_SHARED = 16, KV_BAD_OFFSETS = 32 };
+
+struct KvJob {  // copy the first `tokens` tokens of page `from` to page `to`, in every layer
+  int32_t from, to, tokens;
+};
+
+// Device words and scratch of the calls that change the page tables.
+struct KvScratch {
+  int32_t* err;    // error bits since the last p2p_kv_sync
+  int32_t* halt;   // 1 since a call on the tables failed: later ones, and writes, change nothing until p2p_kv_sync
+  int32_t* njobs;
+  int32_t* claim;  // [n_seqs], zero between calls: a sequence named twice in one call
+  int32_t* start;  // [n_seqs + 1]: where a sequence's page entries start among the call's
+  int32_t* first;  // [n_seqs]: its first entry concerned
+  int32_t* cut;    // [n_seqs]: > 0: the tokens of its shared last page that it takes along into a page of its own
+  int32_t* list;   // [n_pages]: free pages in ascending order; compaction: a page's new number
+  KvJob* jobs;     // [max(n_seqs, n_pages)]
+};
+
+cudaError_t launch_kv_extend(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* count,
+                             int num_sms, cudaStream_t st);
+cudaError_t launch_kv_trim(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* to, cudaStream_t st);
+cudaError_t launch_kv_fork(const KvView& c, const KvScratch& s, int32_t n, const int32_t* src, const int32_t* dst,
+                           const int32_t* tokens, cudaStream_t st);
+cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, cudaStream_t st);
+// Keys and values to write; strides in elements.
+struct KvRows {
+  const void *k, *v;
+  int64_t layer_stride, token_stride, head_stride;
+  int32_t type;
+};
+cudaError_t launch_kv_write(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq,
+                            const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms, cudaStream_t st);
+// out (zeroed by the launch): pages in use, pages shared, the highest page in use + 1, tokens held.
+cudaError_t launch_kv_stats(const KvView& c, unsigned long long* out, int num_sms, cudaStream_t st);
+
+// One token of each of n sequences (kv_attend.cu).
+struct KvQuery {
+  const void* q;
+  void* out;
+  float* lse;
+  const int32_t* seq;  // NULL: sequences 0 .. n-1
+  int64_t q_row, q_head, out_row, out_head;  // strides in elements
+  int32_t n, heads, type, window, layer;
+  float scale;
+};
+cudaError_t launch_kv_attend(const KvView& c, const KvQuery& q, int32_t* err, int num_sms, cudaStream_t st);
+
+}  // namespace p2p
