@@ -1,7 +1,10 @@
 // kv.h -- the paged key-value cache (p2p_kv_* of p2p_router.h): what its host code and its kernels share.
 #pragma once
 #include <cuda_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "p2p_router.h"
 
@@ -82,6 +85,15 @@ struct KvQuery {
   int32_t n, heads, type, window, layer;
   float scale;
 };
-cudaError_t launch_kv_attend(const KvView& c, const KvQuery& q, int32_t* err, int num_sms, cudaStream_t st);
+// Parts of rows that several CTAs share, and how many of a row's have arrived (by its first CTA; zero between launches).
+struct KvAttendScratch {
+  static constexpr int kCtasPerSm = 3;
+  float* parts;      // [kv_attend_parts()]
+  int32_t* arrived;  // [kCtasPerSm * SMs]
+  int32_t* err;
+};
+size_t kv_attend_parts(int32_t dim, int num_sms);
+// With q = NULL it launches nothing, but makes the cache's kernels ready for launches (at creation).
+cudaError_t launch_kv_attend(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
 
 }  // namespace p2p

@@ -2,6 +2,21 @@
 //
 // For a query head and the tokens t that it sees: x_t = scale * q . k_t, m = max x_t, z = sum exp(x_t - m), out = sum
 // exp(x_t - m) v_t / z, lse = m + ln z; without a token, out = 0 and lse = -inf.
+//
+// Keys and values are read once, and that is what bounds it: with g query heads a kv head, 4 g dim operations go with
+// 4 dim bytes, g a byte (2 g with 8 bits), where the GPU has 277 operations of its tensor cores for a byte of memory.
+//
+// The work is cut into units of kTile tokens of a (sequence, kv head, block of its query heads), numbered in that order,
+// and every CTA takes an equal, contiguous range of them: one sequence of 131,071 tokens fills the GPU as a batch does.
+// A range's parts of a unit row that it shares with other CTAs go to scratch (maximum, sum, unnormalised out), and the
+// CTA that finishes such a row last joins its parts, in their order: results do not depend on timing.
+//
+// Inside a unit each warp streams 16 tokens at a time through shared memory of its own, several tiles ahead
+// (cp.async, 16 bytes a lane, 16-byte pieces swizzled so that ldmatrix meets no bank twice), with no barrier between
+// warps.  A 16-token tile is multiplied transposed: S^T [tokens, heads] = K Q^T and O^T [dim, heads] += V^T P^T, so that
+// eight query heads fill a product's n and the 16 tokens its m.  P^T goes from the first product's layout to the
+// second's by two 8 x 8 transposes of registers.  exp(x - m) takes for m not the running maximum but one that lags
+// it by at most a factor of 2^8, so that a tile's maximum is only reduced, and O rescaled, where it goes past that.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -11,86 +26,572 @@
 namespace p2p {
 namespace {
 
-constexpr int kWarps = 8, kPer = 8;  // values of a head's row that a lane holds (head_dim <= 256)
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kRows = 16;               // tokens a warp takes at a time
+constexpr int kTile = kWarps * kRows;   // tokens of a unit
+constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
+constexpr float kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ float value(const char* row, int32_t i, int32_t type) {
-  if (type == P2P_KV_BF16) return __bfloat162float(((const __nv_bfloat16*)row)[i]);
-  if (type == P2P_KV_F16) return __half2float(((const __half*)row)[i]);
-  __nv_fp8_e4m3 x;
-  x.__x = ((const uint8_t*)row)[i];
-  return float(x);
+template <int KIND>
+struct Type;
+template <>
+struct Type<P2P_KV_BF16> {
+  static constexpr int kSize = 2;
+};
+template <>
+struct Type<P2P_KV_F16> {
+  static constexpr int kSize = 2;
+};
+template <>
+struct Type<P2P_KV_E4M3> {
+  static constexpr int kSize = 1;
+};
+
+// Sizes of the kernel for values of KIND, head_dim padded to DP, NB blocks of eight query heads.
+template <int KIND, int DP, int NB>
+struct Shape {
+  static constexpr int kRowBytes = DP * Type<KIND>::kSize;
+  static constexpr int kPieces = kRowBytes / 16;               // 16-byte pieces of a row
+  static constexpr int kArray = kRows * kRowBytes;             // keys (or values) of a warp's tile
+  static constexpr int kStage = 2 * kArray;
+  static constexpr int kStages = 98304 / (kWarps * kStage) < 3 ? 3 : 98304 / (kWarps * kStage) > 8 ? 8 : 98304 / (kWarps * kStage);
+  static constexpr int kBytes = kStages * kStage * kWarps;     // of a CTA
+  static constexpr int kHeads = 8 * NB;
+  static constexpr int kPitch = DP + 4;                        // of a head's sums in shared memory
+  // What a part leaves in scratch: kHeads rows of DP sums, then the maxima, then the sums of exp.
+  static constexpr int kPart = kHeads * (DP + 2);
+  static_assert(kHeads * kPitch * 4 <= kStages * kStage, "a warp's sums fit its tiles' room");
+};
+
+__device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void load4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void load4t(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// c [16, 8] += a [16, 16] b [16, 8]
+template <int KIND>
+__device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+  if (KIND == P2P_KV_BF16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <int KIND>
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+  if (KIND == P2P_KV_BF16) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+    return *(const uint32_t*)&x;
+  }
+  const __half2 x = __floats2half2_rn(a, b);
+  return *(const uint32_t*)&x;
+}
+// Two 8-bit values (the low half of x) as two of 16.
+__device__ __forceinline__ uint32_t widen(uint32_t x) {
+  uint32_t y;
+  asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, lo; }" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t widen_high(uint32_t x) {
+  uint32_t y;
+  asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, hi; }" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ float half_value(const void* p, int64_t i, int32_t type) {
+  return type == P2P_KV_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i]) : __half2float(((const __half*)p)[i]);
+}
+__device__ __forceinline__ void store_half(void* p, int64_t i, int32_t type, float x) {
+  if (type == P2P_KV_BF16)
+    ((__nv_bfloat16*)p)[i] = __float2bfloat16(x);
+  else
+    ((__half*)p)[i] = __float2half(x);
 }
 
-// A CTA takes a (sequence, query head); its warps take tokens in turn, a running maximum and sum each.
-__global__ void __launch_bounds__(kWarps * 32) attend_kernel(KvView c, KvQuery a, int32_t* err) {
-  const int32_t i = blockIdx.x / a.heads, head = blockIdx.x % a.heads, h = head / (a.heads / c.heads);
+// Byte offset in a warp's tile of piece `piece` of row `row`: the pieces of eight rows that ldmatrix reads together lie
+// in different banks.
+template <int PIECES>
+__device__ __forceinline__ uint32_t place(int row, int piece) {
+  const int turn = PIECES >= 8 ? row & 7 : (row >> 1) & 3;
+  return (uint32_t)(row * PIECES + (piece ^ turn)) * 16;
+}
+
+// A row of the batch: which tokens it sees.
+struct Row {
+  int32_t seq, begin, end;
+  __device__ __forceinline__ int32_t tiles() const { return end > begin ? (end - begin - 1) / kTile + 1 : 1; }
+};
+__device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t i, int32_t* err) {
+  Row r = {i < a.n ? (a.seq ? __ldg(a.seq + i) : i) : 0, 0, 0};
+  if (i >= a.n) return r;
+  if ((uint32_t)r.seq >= (uint32_t)c.n_seqs) {
+    if (err) atomicOr(err, KV_BAD_SEQ);
+    r.seq = 0;
+    return r;
+  }
+  const int32_t len = __ldg(c.length + r.seq);
+  if (len < 0 || len > c.max_pages * c.page) {
+    if (err) atomicOr(err, KV_BAD_COUNT);
+    return r;
+  }
+  r.end = len;
+  r.begin = a.window && len > a.window ? len - a.window : 0;
+  return r;
+}
+
+struct Shared {
+  int64_t sums[kWarps];
+  int64_t before;  // units of the rows before `row` (over the kv heads and blocks of one)
+  int32_t row, last;
+  float top[kWarps][16], sum[kWarps][16];  // of the warps' parts, by head
+  float base[16], total[16];
+};
+
+template <int KIND, int DP, int NB>
+__global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
+  using S = Shape<KIND, DP, NB>;
+  constexpr int PIECES = S::kPieces, KSTEPS = DP / 16;
+  constexpr int LANES = PIECES < 32 ? PIECES : 32, PER = 32 / LANES;  // lanes of a row, rows of a copy instruction
+  extern __shared__ __align__(1024) char room[];
+  __shared__ Shared sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int32_t s = a.seq ? a.seq[i] : i;
-  int32_t len = 0;
-  if ((uint32_t)s >= (uint32_t)c.n_seqs) {
-    if (threadIdx.x == 0) atomicOr(err, KV_BAD_SEQ);
-  } else {
-    len = c.length[s];
-    if (len < 0 || len > c.max_pages * c.page) {
-      if (threadIdx.x == 0) atomicOr(err, KV_BAD_COUNT);
-      len = 0;
-    }
+  char* const tiles = room + warp * S::kStages * S::kStage;
+  const uint32_t tiles_at = smem_of(tiles);
+  const int32_t group = a.heads / c.heads, blocks = (group + S::kHeads - 1) / S::kHeads;
+  const int32_t per_row = c.heads * blocks;  // (kv head, block) pairs of a row
+
+  // ---- this CTA's range of the units: a thread sums the tiles of consecutive rows, the CTA scans the threads' sums.
+  const int32_t each = (a.n + kThreads - 1) / kThreads, r0 = threadIdx.x * each;
+  int64_t mine = 0;
+  for (int32_t i = r0; i < r0 + each && i < a.n; ++i) mine += row_at(c, a, i, blockIdx.x == 0 ? w.err : nullptr).tiles();
+  int64_t scan = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t y = __shfl_up_sync(~0u, scan, d);
+    if (lane >= d) scan += y;
   }
-  const int32_t begin = a.window && len > a.window ? len - a.window : 0;
-  const int64_t layer = (int64_t)a.layer * c.layer_stride + h * c.head_stride;
-  const float k_scale = (c.k_scale ? c.k_scale[a.layer * c.heads + h] : 1.f) * a.scale;
-  const float v_scale = c.v_scale ? c.v_scale[a.layer * c.heads + h] : 1.f;
-  float q[kPer], o[kPer] = {}, m = -INFINITY, z = 0.f;
-  for (int j = 0; j < kPer; ++j) {
-    const int32_t x = lane + 32 * j;
-    q[j] = x < c.dim ? value((const char*)a.q + (i * a.q_row + head * a.q_head) * 2, x, a.type) : 0.f;
-  }
-  for (int32_t t = begin + warp; t < len; t += kWarps) {
-    const int32_t e = (int32_t)c.by_page.div(t), page = c.table[(int64_t)s * c.max_pages + e];
-    if ((uint32_t)page >= (uint32_t)c.n_pages) {
-      if (lane == 0) atomicOr(err, KV_BAD_PAGE);
-      continue;
-    }
-    const int64_t at = layer + page * c.page_stride + (t - e * c.page) * c.token_stride;
-    float x = 0.f;
-    for (int j = 0; j < kPer; ++j)
-      if (lane + 32 * j < c.dim) x += q[j] * value(c.k + at, lane + 32 * j, c.type);
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
-    x *= k_scale;
-    const float top = fmaxf(m, x), base = top == -INFINITY ? 0.f : top, fade = __expf(m - base), p = __expf(x - base);
-    z = z * fade + p;
-    for (int j = 0; j < kPer; ++j)
-      if (lane + 32 * j < c.dim) o[j] = o[j] * fade + p * value(c.v + at, lane + 32 * j, c.type);
-    m = top;
-  }
-  __shared__ float sm[kWarps], sz[kWarps], so[kWarps][kPer * 32];
-  if (lane == 0) sm[warp] = m, sz[warp] = z;
-  for (int j = 0; j < kPer; ++j) so[warp][lane + 32 * j] = o[j];
+  if (lane == 31) sh.sums[warp] = scan;
   __syncthreads();
-  float top = -INFINITY, sum = 0.f, w[kWarps];
-  for (int k = 0; k < kWarps; ++k) top = fmaxf(top, sm[k]);
-  const float base = top == -INFINITY ? 0.f : top;
-  for (int k = 0; k < kWarps; ++k) sum += sz[k] * (w[k] = __expf(sm[k] - base));
-  for (int32_t x = threadIdx.x; x < c.dim; x += kWarps * 32) {
-    float y = 0.f;
-    for (int k = 0; k < kWarps; ++k) y += w[k] * so[k][x];
-    y = len > begin ? y / sum * v_scale : 0.f;
-    const int64_t to = i * a.out_row + head * a.out_head + x;
-    if (a.type == P2P_KV_BF16)
-      ((__nv_bfloat16*)a.out)[to] = __float2bfloat16(y);
-    else
-      ((__half*)a.out)[to] = __float2half(y);
+  int64_t before = 0, all = 0;
+#pragma unroll
+  for (int k = 0; k < kWarps; ++k) {
+    before += k < warp ? sh.sums[k] : 0;
+    all += sh.sums[k];
   }
-  if (threadIdx.x == 0 && a.lse) a.lse[(int64_t)i * a.heads + head] = len > begin ? top + logf(sum) : -INFINITY;
+  const int64_t total = all * per_row;
+  const int64_t ctas = total < gridDim.x ? total : gridDim.x;
+  if (blockIdx.x >= ctas) return;
+  int64_t x = total * blockIdx.x / ctas;
+  const int64_t x_end = total * (blockIdx.x + 1) / ctas;
+  before += scan - mine;
+  const int64_t at = x / per_row;
+  if (at >= before && at < before + mine) {
+    int32_t i = r0;
+    for (;; ++i) {
+      const int32_t t = row_at(c, a, i, nullptr).tiles();
+      if (at < before + t) break;
+      before += t;
+    }
+    sh.row = i;
+    sh.before = before;
+  }
+  __syncthreads();
+  int32_t i = sh.row;
+  Row row = row_at(c, a, i, nullptr);
+  int64_t row_x = sh.before * per_row;  // the row's first unit
+
+  while (x < x_end) {
+    const Row next = row_at(c, a, i + 1, nullptr);  // (on its way while this row is worked on)
+    const int32_t nt = row.tiles();
+    const int32_t pair = (int32_t)((x - row_x) / nt), t0 = (int32_t)((x - row_x) % nt);
+    const int32_t t1 = (int32_t)(nt - t0 < x_end - x ? nt : t0 + (x_end - x));
+    const int32_t h = pair / blocks, head0 = h * group + pair % blocks * S::kHeads;
+    const int32_t heads = group - pair % blocks * S::kHeads < S::kHeads ? group - pair % blocks * S::kHeads : S::kHeads;
+    const int64_t base = (int64_t)a.layer * c.layer_stride + h * c.head_stride;
+    const int32_t* table = c.table + (int64_t)row.seq * c.max_pages;
+
+    // ---- the warp's tiles of the unit row: tile j is tokens first + j * kTile .. + 15.
+    const uint32_t first = (uint32_t)row.begin + (uint32_t)(t0 * kTile + warp * kRows);
+    const int32_t count = t1 - t0;
+    int64_t offset;  // of the row that this lane looks up (lanes 0 .. 15), for the tile to be copied next; -1: none
+    const auto look_up = [&](int32_t j) {
+      const int64_t t = (int64_t)first + (int64_t)j * kTile + (lane & 15);
+      offset = -1;
+      if (j < count && t < row.end) {
+        const uint32_t e = c.by_page.div((uint32_t)t);
+        const int32_t page = __ldg(table + e);
+        if ((uint32_t)page < (uint32_t)c.n_pages)
+          offset = page * c.page_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
+        else
+          atomicOr(w.err, KV_BAD_PAGE);
+      }
+    };
+    const auto copy = [&](int32_t j) {  // tile j, which look_up has looked up
+      if (j < count) {
+        const uint32_t to = tiles_at + j % S::kStages * S::kStage;
+#pragma unroll
+        for (int y = 0; y < kRows / PER; ++y) {
+          const int r = y * PER + lane / LANES;
+          const int64_t o = __shfl_sync(~0u, offset, r);
+#pragma unroll
+          for (int p0 = 0; p0 < PIECES; p0 += LANES) {
+            const int piece = p0 + lane % LANES;
+            const bool in = o >= 0 && piece < c.row16;
+            const int64_t from = in ? base + o + piece * 16 : 0;
+            const uint32_t d = to + place<PIECES>(r, piece);
+            copy16(d, c.k + from, in);
+            copy16(d + S::kArray, c.v + from, in);
+          }
+        }
+      }
+      commit();
+    };
+    look_up(0);
+    for (int j = 0; j < S::kStages - 1; ++j) {
+      copy(j);
+      look_up(j + 1);
+    }
+
+    // ---- the queries, as the second operand of the first product: lane holds head lane / 4 of each block of eight.
+    // (With 8-bit values a piece of 16 is 16 of the product's k, in the order that their bytes come to a lane.)
+    uint32_t q[KSTEPS][NB][2];
+    float mul[NB][2];  // logit (in log2) of a sum, for the heads 2 * (lane % 4) + {0, 1} of a block
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int32_t head = b * 8 + lane / 4;
+      const int64_t from = i * a.q_row + (head0 + head) * a.q_head;
+      float unit = a.scale * kLog2e * (KIND == P2P_KV_E4M3 ? __ldg(c.k_scale + a.layer * c.heads + h) : 1.f);
+      if (KIND == P2P_KV_E4M3) {
+        // The queries in f16, scaled by a power of two so that a row's largest is in [1, 2): exact but for what is
+        // below 2^-14 of it.
+        float largest = 0.f;
+        for (int d = lane % 4; d < c.dim; d += 4)
+          if (head < heads) largest = fmaxf(largest, fabsf(half_value(a.q, from + d, a.type)));
+        largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 1));
+        largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 2));
+        const int e = largest > 0.f && largest < INFINITY ? ilogbf(largest) : 0;
+        unit = ldexpf(unit, e);
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float v[2];
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              const int d = 16 * k + 4 * (lane % 4) + 2 * y + z;
+              v[z] = head < heads && d < c.dim ? ldexpf(half_value(a.q, from + d, a.type), -e) : 0.f;
+            }
+            q[k][b][y] = pack<KIND>(v[0], v[1]);
+          }
+      } else {
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            uint32_t v[2];
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              const int d = 16 * k + 8 * y + 2 * (lane % 4) + z;
+              v[z] = head < heads && d < c.dim ? __ldg((const uint16_t*)a.q + from + d) : 0;
+            }
+            q[k][b][y] = v[0] | v[1] << 16;
+          }
+      }
+#pragma unroll
+      for (int y = 0; y < 2; ++y) mul[b][y] = __shfl_sync(~0u, unit, 4 * (2 * (lane % 4) + y));
+    }
+
+    float o[KSTEPS][NB][4], top[NB][2], sum[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      top[b][0] = top[b][1] = -INFINITY;
+      sum[b][0] = sum[b][1] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KSTEPS; ++k) o[k][b][0] = o[k][b][1] = o[k][b][2] = o[k][b][3] = 0.f;
+    }
+
+    for (int32_t j = 0; j < count; ++j) {
+      wait<S::kStages - 2>();
+      __syncwarp();  // every lane's pieces of tile j are there, and every lane is done with tile j - 1
+      copy(j + S::kStages - 1);
+      look_up(j + S::kStages);
+      const uint32_t keys = tiles_at + j % S::kStages * S::kStage, values = keys + S::kArray;
+
+      float s[NB][4] = {};  // tokens lane / 4 (+ 8 in 2, 3), heads 2 * (lane % 4) + {0, 1}
+      if (KIND == P2P_KV_E4M3) {
+#pragma unroll
+        for (int k = 0; k < KSTEPS; k += 2) {
+          uint32_t r[4];  // tokens 0-7 and 8-15 of piece k, then of piece k + 1
+          load4(r, keys + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, k + (lane >> 4)));
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const uint32_t f[4] = {widen(r[2 * y]), widen(r[2 * y + 1]), widen_high(r[2 * y]), widen_high(r[2 * y + 1])};
+#pragma unroll
+            for (int b = 0; b < NB; ++b) multiply<KIND>(s[b], f, q[k + y][b]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k) {
+          uint32_t f[4];
+          load4(f, keys + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, 2 * k + (lane >> 4)));
+#pragma unroll
+          for (int b = 0; b < NB; ++b) multiply<KIND>(s[b], f, q[k][b]);
+        }
+      }
+      const int32_t left = (int32_t)((uint32_t)row.end - (first + (uint32_t)j * kTile));  // tokens of the tile that are seen, if that is below 16
+      bool past = false;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          s[b][y] = lane / 4 + (y >> 1) * 8 < left ? s[b][y] * mul[b][y & 1] : -INFINITY;
+          past |= s[b][y] > top[b][y & 1] + kLag;
+        }
+      if (__any_sync(~0u, past)) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float t = fmaxf(s[b][y], s[b][y + 2]);
+            t = fmaxf(t, __shfl_xor_sync(~0u, t, 4));
+            t = fmaxf(t, __shfl_xor_sync(~0u, t, 8));
+            t = fmaxf(t, __shfl_xor_sync(~0u, t, 16));
+            t = fmaxf(t, top[b][y]);
+            const float fade = t == -INFINITY ? 1.f : exp2_fast(top[b][y] - t);
+            top[b][y] = t;
+            sum[b][y] *= fade;
+#pragma unroll
+            for (int k = 0; k < KSTEPS; ++k) {
+              o[k][b][y] *= fade;
+              o[k][b][y + 2] *= fade;
+            }
+          }
+      }
+      uint32_t p[NB][2];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float from = top[b][y & 1];
+          s[b][y] = exp2_fast(s[b][y] - (from == -INFINITY ? 0.f : from));
+          sum[b][y & 1] += s[b][y];
+        }
+        p[b][0] = transpose8(pack<KIND>(s[b][0], s[b][1]));
+        p[b][1] = transpose8(pack<KIND>(s[b][2], s[b][3]));
+      }
+      if (KIND == P2P_KV_E4M3) {
+#pragma unroll
+        for (int k = 0; k < KSTEPS; k += 2) {
+          uint32_t r[4];  // tokens 0-7 and 8-15 of piece k, then of piece k + 1
+          load4t(r, values + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, k + (lane >> 4)));
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            // A lane's register: values 2 * (lane / 4) + {0, 1} of one token, then of the next; the product's rows 0-7 are
+            // the even values, 8-15 the odd ones.
+            const uint32_t lo = __byte_perm(r[2 * y], 0, 0x3120), hi = __byte_perm(r[2 * y + 1], 0, 0x3120);
+            const uint32_t f[4] = {widen(lo), widen_high(lo), widen(hi), widen_high(hi)};
+#pragma unroll
+            for (int b = 0; b < NB; ++b) multiply<KIND>(o[k + y][b], f, p[b]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k) {
+          uint32_t f[4];
+          load4t(f, values + place<PIECES>((lane & 7) + (lane >> 4) * 8, 2 * k + (lane >> 3 & 1)));
+#pragma unroll
+          for (int b = 0; b < NB; ++b) multiply<KIND>(o[k][b], f, p[b]);
+        }
+      }
+    }
+    wait<0>();
+    __syncwarp();
+
+    // ---- the four warps' parts.  Their sums go to the tiles' room, [head][dim].
+    float* const sums = (float*)tiles;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int head = b * 8 + 2 * (lane % 4) + y;
+        float z = sum[b][y];
+        z += __shfl_xor_sync(~0u, z, 4);
+        z += __shfl_xor_sync(~0u, z, 8);
+        z += __shfl_xor_sync(~0u, z, 16);
+        if (lane < 4) sh.top[warp][head] = top[b][y], sh.sum[warp][head] = z;
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k) {
+          const int d = KIND == P2P_KV_E4M3 ? 16 * k + 2 * (lane / 4) : 16 * k + lane / 4;
+          sums[head * S::kPitch + d] = o[k][b][y];
+          sums[head * S::kPitch + d + (KIND == P2P_KV_E4M3 ? 1 : 8)] = o[k][b][y + 2];
+        }
+      }
+    }
+    __syncthreads();
+    const bool whole = t0 == 0 && t1 == nt;
+    const int64_t x0 = x - t0;  // the unit row's first unit
+    const int32_t slot = blockIdx.x * 2 + (t0 == 0);
+    float* const part = w.parts + (int64_t)slot * S::kPart;
+    const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + h) : 1.f;
+    const bool empty = row.end <= row.begin;
+    for (int y = threadIdx.x; y < S::kHeads * DP / 4; y += kThreads) {
+      const int head = y / (DP / 4), d = y % (DP / 4) * 4;
+      float t = -INFINITY, z = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) t = fmaxf(t, sh.top[k][head]);
+      const float ref = t == -INFINITY ? 0.f : t;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) {
+        const float fade = exp2_fast(sh.top[k][head] - ref);
+        const float4 u = *(const float4*)((const float*)(room + k * S::kStages * S::kStage) + head * S::kPitch + d);
+        z += fade * sh.sum[k][head];
+        v.x += fade * u.x, v.y += fade * u.y, v.z += fade * u.z, v.w += fade * u.w;
+      }
+      if (!whole) {
+        *(float4*)(part + head * DP + d) = v;
+        if (d == 0) part[S::kHeads * DP + head] = t, part[S::kHeads * (DP + 1) + head] = z;
+      } else if (head < heads) {
+        const float f = v_scale / z;
+        const int64_t to = i * a.out_row + (head0 + head) * a.out_head + d;
+        const float r[4] = {v.x * f, v.y * f, v.z * f, v.w * f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (d + k < c.dim) store_half(a.out, to + k, a.type, empty ? 0.f : r[k]);
+        if (d == 0 && a.lse) a.lse[(int64_t)i * a.heads + head0 + head] = empty ? -INFINITY : (t + log2f(z)) / kLog2e;
+      }
+    }
+    if (!whole) {
+      // The CTA that brings the last part of the unit row joins them.
+      __threadfence();
+      __syncthreads();
+      const int32_t c0 = (int32_t)(((x0 + 1) * ctas - 1) / total), c1 = (int32_t)(((x0 + nt) * ctas - 1) / total);
+      if (threadIdx.x == 0) {
+        sh.last = atomicAdd(w.arrived + c0, 1) == c1 - c0;
+        if (sh.last) w.arrived[c0] = 0;  // for the next launch
+      }
+      __syncthreads();
+      if (sh.last) {
+        __threadfence();
+        const int32_t parts = c1 - c0 + 1;
+        const auto part_of = [&](int32_t k) {  // the first CTA's is its range's last unit row, the others' their first
+          return w.parts + (int64_t)((c0 + k) * 2 + (k == 0)) * S::kPart;
+        };
+        for (int head = warp; head < heads; head += kWarps) {
+          float t = -INFINITY, z = 0.f;
+          for (int32_t k = lane; k < parts; k += 32) t = fmaxf(t, __ldcg(part_of(k) + S::kHeads * DP + head));
+#pragma unroll
+          for (int d = 16; d; d >>= 1) t = fmaxf(t, __shfl_xor_sync(~0u, t, d));
+          const float ref = t == -INFINITY ? 0.f : t;
+          for (int32_t k = lane; k < parts; k += 32)
+            z += exp2_fast(__ldcg(part_of(k) + S::kHeads * DP + head) - ref) * __ldcg(part_of(k) + S::kHeads * (DP + 1) + head);
+#pragma unroll
+          for (int d = 16; d; d >>= 1) z += __shfl_xor_sync(~0u, z, d);
+          if (lane == 0) {
+            sh.base[head] = ref;
+            sh.total[head] = z;
+            if (a.lse) a.lse[(int64_t)i * a.heads + head0 + head] = (t + log2f(z)) / kLog2e;
+          }
+        }
+        __syncthreads();
+        for (int y = threadIdx.x; y < heads * (DP / 4); y += kThreads) {
+          const int head = y / (DP / 4), d = y % (DP / 4) * 4;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int32_t k = 0; k < parts; ++k) {
+            const float* p = part_of(k);
+            const float fade = exp2_fast(__ldcg(p + S::kHeads * DP + head) - sh.base[head]);
+            const float4 u = __ldcg((const float4*)(p + head * DP + d));
+            v.x += fade * u.x, v.y += fade * u.y, v.z += fade * u.z, v.w += fade * u.w;
+          }
+          const float f = v_scale / sh.total[head];
+          const int64_t to = i * a.out_row + (head0 + head) * a.out_head + d;
+          const float r[4] = {v.x * f, v.y * f, v.z * f, v.w * f};
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (d + k < c.dim) store_half(a.out, to + k, a.type, r[k]);
+        }
+      }
+    }
+    __syncthreads();  // the tiles' room and sh are free again
+
+    x += t1 - t0;
+    if (x - row_x == (int64_t)nt * per_row) {
+      row_x = x;
+      row = next;
+      ++i;
+    }
+  }
+}
+
+// With q = NULL the kernel is only made ready for launches.
+template <int KIND, int DP, int NB>
+cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+  using S = Shape<KIND, DP, NB>;
+  const auto kernel = attend_kernel<KIND, DP, NB>;
+  if (!q) return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+  // As many CTAs as are resident together (by shared memory: 227 KB an SM, 1 KB of it the system's for each CTA).
+  const int per_sm = std::max(1, std::min(KvAttendScratch::kCtasPerSm, 232448 / (S::kBytes + 2048)));
+  kernel<<<per_sm * num_sms, kThreads, S::kBytes, st>>>(c, *q, w);
+  return cudaGetLastError();
+}
+
+template <int KIND, int DP>
+cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+  if (!q) {
+    const cudaError_t e = launch<KIND, DP, 1>(c, q, w, num_sms, st);
+    return e == cudaSuccess ? launch<KIND, DP, 2>(c, q, w, num_sms, st) : e;
+  }
+  return q->heads / c.heads <= 8 ? launch<KIND, DP, 1>(c, q, w, num_sms, st) : launch<KIND, DP, 2>(c, q, w, num_sms, st);
+}
+
+template <int KIND>
+cudaError_t launch_dim(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+  return c.dim <= 64    ? launch_heads<KIND, 64>(c, q, w, num_sms, st)
+         : c.dim <= 128 ? launch_heads<KIND, 128>(c, q, w, num_sms, st)
+                        : launch_heads<KIND, 256>(c, q, w, num_sms, st);
 }
 
 }  // namespace
 
-cudaError_t launch_kv_attend(const KvView& c, const KvQuery& q, int32_t* err, int num_sms, cudaStream_t st) {
-  (void)num_sms;
-  if ((int64_t)q.n * q.heads > INT32_MAX) return cudaErrorInvalidValue;
-  attend_kernel<<<q.n * q.heads, kWarps * 32, 0, st>>>(c, q, err);
-  return cudaGetLastError();
+size_t kv_attend_parts(int32_t dim, int num_sms) {
+  const int32_t dp = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
+  return (size_t)2 * KvAttendScratch::kCtasPerSm * num_sms * 16 * (dp + 2);
+}
+
+cudaError_t launch_kv_attend(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+  return c.type == P2P_KV_BF16  ? launch_dim<P2P_KV_BF16>(c, q, w, num_sms, st)
+         : c.type == P2P_KV_F16 ? launch_dim<P2P_KV_F16>(c, q, w, num_sms, st)
+                                : launch_dim<P2P_KV_E4M3>(c, q, w, num_sms, st);
 }
 
 }  // namespace p2p

@@ -15,6 +15,7 @@
 struct p2p_kv {
   p2p::KvView c = {};
   p2p::KvScratch s = {};
+  p2p::KvAttendScratch w = {};
   void* scratch = nullptr;             // one allocation: s's arrays and d_stats
   unsigned long long* d_stats = nullptr;
   int device = 0, num_sms = 0;
@@ -138,10 +139,13 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
     return here;
   };
   const size_t S = (size_t)a.n_seqs, N = (size_t)a.n_pages;
-  const size_t words = part(256), claim = part(4 * S), zero = at, start = part(4 * (S + 1)), first = part(4 * S), cut = part(4 * S),
-               list = part(4 * N), jobs = part(sizeof(p2p::KvJob) * std::max(S, N));
+  const size_t words = part(256), claim = part(4 * S),
+               arrived = part(sizeof(int32_t) * p2p::KvAttendScratch::kCtasPerSm * sms), zero = at, start = part(4 * (S + 1)), first = part(4 * S), cut = part(4 * S),
+               list = part(4 * N), jobs = part(sizeof(p2p::KvJob) * std::max(S, N)),
+               parts = part(sizeof(float) * p2p::kv_attend_parts(a.head_dim, sms));
   cudaError_t e = cudaMalloc(&n->scratch, at);
   if (e == cudaSuccess) e = cudaMemset(n->scratch, 0, zero);
+  if (e == cudaSuccess) e = p2p::launch_kv_attend(c, nullptr, n->w, sms, nullptr);
   if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);  // (calls may go to a stream that does not wait for this one)
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
@@ -160,6 +164,9 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   n->s.cut = (int32_t*)(p + cut);
   n->s.list = (int32_t*)(p + list);
   n->s.jobs = (p2p::KvJob*)(p + jobs);
+  n->w.parts = (float*)(p + parts);
+  n->w.arrived = (int32_t*)(p + arrived);
+  n->w.err = n->s.err;
   *out = n;
   return P2P_OK;
 }
@@ -296,7 +303,7 @@ int p2p_kv_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const
   DeviceGuard g(h->device);
   const p2p::KvQuery a = {q, out, lse, seq, q_row_stride, q_head_stride, out_row_stride, out_head_stride,
                           n, n_heads, type, window, layer, scale};
-  CK(p2p::launch_kv_attend(h->c, a, h->s.err, h->num_sms, h->stream));
+  CK(p2p::launch_kv_attend(h->c, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;
 }
