@@ -84,10 +84,12 @@ struct KvQuery {
   int64_t q_row, q_head, out_row, out_head;  // strides in elements
   int32_t n, heads, type, window, layer;
   float scale;
+  // Whether rows of q may be read by twos, and those of out written by fours, of their values.
+  bool q_pairs, out_fours;
 };
 // Parts of rows that several CTAs share, and how many of a row's have arrived (by its first CTA; zero between launches).
 struct KvAttendScratch {
-  static constexpr int kCtasPerSm = 3;
+  static constexpr int kCtasPerSm = 2;
   float* parts;      // [kv_attend_parts()]
   int32_t* arrived;  // [kCtasPerSm * SMs]
   int32_t* err;

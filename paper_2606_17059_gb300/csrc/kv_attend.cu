@@ -9,12 +9,14 @@
 // The work is cut into units of kTile tokens of a (sequence, kv head, block of its query heads), numbered in that order,
 // and every CTA takes an equal, contiguous range of them: one sequence of 131,071 tokens fills the GPU as a batch does.
 // A range's parts of a unit row that it shares with other CTAs go to scratch (maximum, sum, unnormalised out), and the
-// CTA that finishes such a row last joins its parts, in their order: results do not depend on timing.
+// CTA that finishes such a row last joins its parts, in their order: results do not depend on timing.  (The start of a
+// unit row counts as kOver units more, for the joining of its warps' parts.)
 //
-// Inside a unit each warp streams 16 tokens at a time through shared memory of its own, several tiles ahead
-// (cp.async, 16 bytes a lane, 16-byte pieces swizzled so that ldmatrix meets no bank twice), with no barrier between
-// warps.  A 16-token tile is multiplied transposed: S^T [tokens, heads] = K Q^T and O^T [dim, heads] += V^T P^T, so that
-// eight query heads fill a product's n and the 16 tokens its m.  P^T goes from the first product's layout to the
+// Each warp streams 16 tokens at a time through shared memory of its own, several tiles ahead (cp.async, 16 bytes a
+// lane, 16-byte pieces swizzled so that ldmatrix meets no bank twice), with no barrier between warps inside a unit row;
+// the copies run on into the next unit row while this one's parts are joined, and page numbers are read two tiles ahead
+// of the copies.  A 16-token tile is multiplied transposed: S^T [tokens, heads] = K Q^T and O^T [dim, heads] += V^T P^T,
+// so that eight query heads fill a product's n and the 16 tokens its m.  P^T goes from the first product's layout to the
 // second's by two 8 x 8 transposes of registers.  exp(x - m) takes for m not the running maximum but one that lags
 // it by at most a factor of 2^8, so that a tile's maximum is only reduced, and O rescaled, where it goes past that.
 #include <cuda_bf16.h>
@@ -29,6 +31,7 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kRows = 16;               // tokens a warp takes at a time
 constexpr int kTile = kWarps * kRows;   // tokens of a unit
+constexpr int kOver = 1;                // units that a unit row counts for beyond its own
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -54,13 +57,16 @@ struct Shape {
   static constexpr int kPieces = kRowBytes / 16;               // 16-byte pieces of a row
   static constexpr int kArray = kRows * kRowBytes;             // keys (or values) of a warp's tile
   static constexpr int kStage = 2 * kArray;
-  static constexpr int kStages = 98304 / (kWarps * kStage) < 3 ? 3 : 98304 / (kWarps * kStage) > 8 ? 8 : 98304 / (kWarps * kStage);
-  static constexpr int kBytes = kStages * kStage * kWarps;     // of a CTA
+  static constexpr int kCtas = DP == 256 ? 1 : 2;  // resident on an SM
+  static constexpr int kSums = 8 * DP * 4;                     // of a warp, for eight heads
+  static constexpr int kFit = ((232448 / kCtas - 1024 - 512) / kWarps - kSums) / kStage;
+  static constexpr int kStages = kFit < 8 ? kFit : 8;
+  static constexpr int kRoom = kStages * kStage;               // a warp's tiles
+  static constexpr int kBytes = (kRoom + kSums) * kWarps;      // of a CTA
   static constexpr int kHeads = 8 * NB;
-  static constexpr int kPitch = DP + 4;                        // of a head's sums in shared memory
   // What a part leaves in scratch: kHeads rows of DP sums, then the maxima, then the sums of exp.
   static constexpr int kPart = kHeads * (DP + 2);
-  static_assert(kHeads * kPitch * 4 <= kStages * kStage, "a warp's sums fit its tiles' room");
+  static_assert(kStages >= 3, "two tiles on their way");
 };
 
 __device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -126,14 +132,23 @@ __device__ __forceinline__ uint32_t widen_high(uint32_t x) {
   asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, hi; }" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ float half_value(const void* p, int64_t i, int32_t type) {
-  return type == P2P_KV_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i]) : __half2float(((const __half*)p)[i]);
+__device__ __forceinline__ float2 two_halves(uint32_t x, int32_t type) {
+  return type == P2P_KV_BF16 ? __bfloat1622float2(*(const __nv_bfloat162*)&x) : __half22float2(*(const __half2*)&x);
 }
-__device__ __forceinline__ void store_half(void* p, int64_t i, int32_t type, float x) {
-  if (type == P2P_KV_BF16)
-    ((__nv_bfloat16*)p)[i] = __float2bfloat16(x);
-  else
-    ((__half*)p)[i] = __float2half(x);
+// Values d .. d + 3 of a head's result, times f; zero: 0 in their place.
+__device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_t i, int32_t head, int32_t d, float4 v, float f,
+                                       bool zero) {
+  if (d >= c.dim) return;  // (dim is a multiple of 8)
+  if (zero) v = make_float4(0.f, 0.f, 0.f, 0.f), f = 0.f;
+  const uint32_t x = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.x * f, v.y * f) : pack<P2P_KV_F16>(v.x * f, v.y * f);
+  const uint32_t y = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.z * f, v.w * f) : pack<P2P_KV_F16>(v.z * f, v.w * f);
+  uint16_t* to = (uint16_t*)a.out + i * a.out_row + head * a.out_head + d;
+  if (a.out_fours) {
+    *(uint2*)to = make_uint2(x, y);
+  } else {
+    to[0] = (uint16_t)x, to[1] = (uint16_t)(x >> 16);
+    to[2] = (uint16_t)y, to[3] = (uint16_t)(y >> 16);
+  }
 }
 
 // Byte offset in a warp's tile of piece `piece` of row `row`: the pieces of eight rows that ldmatrix reads together lie
@@ -171,27 +186,52 @@ struct Shared {
   int64_t sums[kWarps];
   int64_t before;  // units of the rows before `row` (over the kv heads and blocks of one)
   int32_t row, last;
-  float top[kWarps][16], sum[kWarps][16];  // of the warps' parts, by head
+  float top[kWarps][8], sum[kWarps][8];  // of the warps' parts, by head of a block
   float base[16], total[16];
+};
+
+static_assert(sizeof(Shared) <= 512, "Shape counts on it");
+
+// A place in a CTA's range: tile t of nt of the unit row (row i, kv head h, block of its query heads).
+struct Cursor {
+  Row row, next;
+  int32_t i, h, block, t, nt;
+  int64_t left;  // units of the range from here on; none: at its end
+  // k tiles on, none past the unit row's end.
+  __device__ __forceinline__ void advance(int32_t k, const KvView& c, const KvQuery& a, int32_t blocks) {
+    t += k;
+    left -= k;
+    if (t < nt) return;
+    t = 0;
+    left -= kOver;
+    if (++block < blocks) return;
+    block = 0;
+    if (++h < c.heads) return;
+    h = 0;
+    ++i;
+    row = next;
+    nt = row.tiles();
+    next = row_at(c, a, i + 1, nullptr);
+  }
 };
 
 template <int KIND, int DP, int NB>
 __global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
   using S = Shape<KIND, DP, NB>;
   constexpr int PIECES = S::kPieces, KSTEPS = DP / 16;
-  constexpr int LANES = PIECES < 32 ? PIECES : 32, PER = 32 / LANES;  // lanes of a row, rows of a copy instruction
-  extern __shared__ __align__(1024) char room[];
+  constexpr int LANES = PIECES, PER = 32 / LANES;  // lanes of a row, rows of a copy instruction
+  extern __shared__ __align__(128) char room[];
   __shared__ Shared sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  char* const tiles = room + warp * S::kStages * S::kStage;
-  const uint32_t tiles_at = smem_of(tiles);
+  const uint32_t tiles_at = smem_of(room + warp * S::kRoom);
+  float* const sums = (float*)(room + kWarps * S::kRoom) + warp * 8 * DP;
   const int32_t group = a.heads / c.heads, blocks = (group + S::kHeads - 1) / S::kHeads;
   const int32_t per_row = c.heads * blocks;  // (kv head, block) pairs of a row
 
-  // ---- this CTA's range of the units: a thread sums the tiles of consecutive rows, the CTA scans the threads' sums.
+  // ---- this CTA's range of the units: a thread sums those of consecutive rows, the CTA scans the threads' sums.
   const int32_t each = (a.n + kThreads - 1) / kThreads, r0 = threadIdx.x * each;
   int64_t mine = 0;
-  for (int32_t i = r0; i < r0 + each && i < a.n; ++i) mine += row_at(c, a, i, blockIdx.x == 0 ? w.err : nullptr).tiles();
+  for (int32_t i = r0; i < r0 + each && i < a.n; ++i) mine += row_at(c, a, i, blockIdx.x == 0 ? w.err : nullptr).tiles() + kOver;
   int64_t scan = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -209,14 +249,13 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, K
   const int64_t total = all * per_row;
   const int64_t ctas = total < gridDim.x ? total : gridDim.x;
   if (blockIdx.x >= ctas) return;
-  int64_t x = total * blockIdx.x / ctas;
-  const int64_t x_end = total * (blockIdx.x + 1) / ctas;
+  const int64_t x0 = total * blockIdx.x / ctas, x_end = total * (blockIdx.x + 1) / ctas;
   before += scan - mine;
-  const int64_t at = x / per_row;
+  const int64_t at = x0 / per_row;
   if (at >= before && at < before + mine) {
     int32_t i = r0;
     for (;; ++i) {
-      const int32_t t = row_at(c, a, i, nullptr).tiles();
+      const int32_t t = row_at(c, a, i, nullptr).tiles() + kOver;
       if (at < before + t) break;
       before += t;
     }
@@ -224,111 +263,137 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, K
     sh.before = before;
   }
   __syncthreads();
-  int32_t i = sh.row;
-  Row row = row_at(c, a, i, nullptr);
-  int64_t row_x = sh.before * per_row;  // the row's first unit
+  Cursor here;  // what is computed
+  here.i = sh.row;
+  here.row = row_at(c, a, here.i, nullptr);
+  here.next = row_at(c, a, here.i + 1, nullptr);
+  here.nt = here.row.tiles();
+  {
+    const int64_t in = x0 - sh.before * per_row;
+    const int32_t units = here.nt + kOver, pair = (int32_t)(in / units), u = (int32_t)(in % units);
+    here.h = pair / blocks;
+    here.block = pair % blocks;
+    here.t = u > kOver ? u - kOver : 0;
+    here.left = x_end - x0 - (u < kOver ? kOver - u : 0);
+  }
 
-  while (x < x_end) {
-    const Row next = row_at(c, a, i + 1, nullptr);  // (on its way while this row is worked on)
-    const int32_t nt = row.tiles();
-    const int32_t pair = (int32_t)((x - row_x) / nt), t0 = (int32_t)((x - row_x) % nt);
-    const int32_t t1 = (int32_t)(nt - t0 < x_end - x ? nt : t0 + (x_end - x));
-    const int32_t h = pair / blocks, head0 = h * group + pair % blocks * S::kHeads;
-    const int32_t heads = group - pair % blocks * S::kHeads < S::kHeads ? group - pair % blocks * S::kHeads : S::kHeads;
-    const int64_t base = (int64_t)a.layer * c.layer_stride + h * c.head_stride;
-    const int32_t* table = c.table + (int64_t)row.seq * c.max_pages;
-
-    // ---- the warp's tiles of the unit row: tile j is tokens first + j * kTile .. + 15.
-    const uint32_t first = (uint32_t)row.begin + (uint32_t)(t0 * kTile + warp * kRows);
-    const int32_t count = t1 - t0;
-    int64_t offset;  // of the row that this lane looks up (lanes 0 .. 15), for the tile to be copied next; -1: none
-    const auto look_up = [&](int32_t j) {
-      const int64_t t = (int64_t)first + (int64_t)j * kTile + (lane & 15);
-      offset = -1;
-      if (j < count && t < row.end) {
+  // ---- copies of the warp's tiles, in the order of the range.  Lanes 0 .. 15 look up a token each: its page, and where
+  // it lies but for that (page < 0: no token).
+  Cursor ahead = here;  // what is looked up
+  struct Token {
+    int32_t page;
+    int64_t at;
+  };
+  const auto look_up = [&]() {
+    Token k = {-1, 0};
+    if (ahead.left > 0) {
+      const int64_t t = (int64_t)ahead.row.begin + (int64_t)ahead.t * kTile + warp * kRows + (lane & 15);
+      if (t < ahead.row.end) {
         const uint32_t e = c.by_page.div((uint32_t)t);
-        const int32_t page = __ldg(table + e);
-        if ((uint32_t)page < (uint32_t)c.n_pages)
-          offset = page * c.page_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
-        else
-          atomicOr(w.err, KV_BAD_PAGE);
+        k.page = __ldg(c.table + (int64_t)ahead.row.seq * c.max_pages + e);
+        k.at = (int64_t)a.layer * c.layer_stride + ahead.h * c.head_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
+        if (k.page < 0) k.page = INT32_MAX;
       }
-    };
-    const auto copy = [&](int32_t j) {  // tile j, which look_up has looked up
-      if (j < count) {
-        const uint32_t to = tiles_at + j % S::kStages * S::kStage;
-#pragma unroll
-        for (int y = 0; y < kRows / PER; ++y) {
-          const int r = y * PER + lane / LANES;
-          const int64_t o = __shfl_sync(~0u, offset, r);
-#pragma unroll
-          for (int p0 = 0; p0 < PIECES; p0 += LANES) {
-            const int piece = p0 + lane % LANES;
-            const bool in = o >= 0 && piece < c.row16;
-            const int64_t from = in ? base + o + piece * 16 : 0;
-            const uint32_t d = to + place<PIECES>(r, piece);
-            copy16(d, c.k + from, in);
-            copy16(d + S::kArray, c.v + from, in);
-          }
-        }
-      }
-      commit();
-    };
-    look_up(0);
-    for (int j = 0; j < S::kStages - 1; ++j) {
-      copy(j);
-      look_up(j + 1);
+      ahead.advance(1, c, a, blocks);
     }
+    return k;
+  };
+  int32_t to_slot = 0;
+  const auto copy = [&](const Token& k) {
+    int64_t offset = -1;
+    if (k.page >= 0) {
+      if (k.page < c.n_pages)
+        offset = k.at + k.page * c.page_stride;
+      else
+        atomicOr(w.err, KV_BAD_PAGE);
+    }
+    const uint32_t to = tiles_at + to_slot * S::kStage;
+    to_slot = to_slot + 1 < S::kStages ? to_slot + 1 : 0;
+#pragma unroll
+    for (int y = 0; y < kRows / PER; ++y) {
+      const int r = y * PER + lane / LANES;
+      const int64_t o = __shfl_sync(~0u, offset, r);
+      const int piece = lane % LANES;
+      const bool in = o >= 0 && piece < c.row16;
+      const int64_t from = in ? o + piece * 16 : 0;
+      const uint32_t d = to + place<PIECES>(r, piece);
+      copy16(d, c.k + from, in);
+      copy16(d + S::kArray, c.v + from, in);
+    }
+    commit();
+  };
+  Token soon = look_up(), later = look_up();
+  const auto step = [&]() {
+    copy(soon);
+    soon = later;
+    later = look_up();
+  };
 
-    // ---- the queries, as the second operand of the first product: lane holds head lane / 4 of each block of eight.
-    // (With 8-bit values a piece of 16 is 16 of the product's k, in the order that their bytes come to a lane.)
-    uint32_t q[KSTEPS][NB][2];
-    float mul[NB][2];  // logit (in log2) of a sum, for the heads 2 * (lane % 4) + {0, 1} of a block
+  // ---- the queries, as the second operand of the first product: lane holds head lane / 4 of each block of eight.
+  // (With 8-bit values a piece of 16 is 16 of the product's k, in the order that their bytes come to a lane.)
+  uint32_t q[KSTEPS][NB][2];
+  float mul[NB][2];  // logit (in log2) of a sum, for the heads 2 * (lane % 4) + {0, 1} of a block
+  const auto load_queries = [&](const Cursor& u) {
+    const int32_t head0 = u.h * group + u.block * S::kHeads, heads = min(group - u.block * S::kHeads, S::kHeads);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int32_t head = b * 8 + lane / 4;
-      const int64_t from = i * a.q_row + (head0 + head) * a.q_head;
-      float unit = a.scale * kLog2e * (KIND == P2P_KV_E4M3 ? __ldg(c.k_scale + a.layer * c.heads + h) : 1.f);
+      const uint16_t* from = (const uint16_t*)a.q + u.i * a.q_row + (head0 + head) * a.q_head;
+#pragma unroll
+      for (int k = 0; k < KSTEPS; ++k)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int d = KIND == P2P_KV_E4M3 ? 16 * k + 4 * (lane % 4) + 2 * y : 16 * k + 8 * y + 2 * (lane % 4);
+          uint32_t v = 0;
+          if (head < heads && d < c.dim) v = a.q_pairs ? __ldg((const uint32_t*)(from + d)) : __ldg(from + d) | (uint32_t)__ldg(from + d + 1) << 16;
+          q[k][b][y] = v;
+        }
+    }
+  };
+  const auto use_queries = [&](const Cursor& u) {
+    float unit = a.scale * kLog2e * (KIND == P2P_KV_E4M3 ? __ldg(c.k_scale + a.layer * c.heads + u.h) : 1.f);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      float mine = unit;
       if (KIND == P2P_KV_E4M3) {
         // The queries in f16, scaled by a power of two so that a row's largest is in [1, 2): exact but for what is
         // below 2^-14 of it.
         float largest = 0.f;
-        for (int d = lane % 4; d < c.dim; d += 4)
-          if (head < heads) largest = fmaxf(largest, fabsf(half_value(a.q, from + d, a.type)));
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float2 v = two_halves(q[k][b][y], a.type);
+            largest = fmaxf(largest, fmaxf(fabsf(v.x), fabsf(v.y)));
+          }
         largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 1));
         largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 2));
-        const int e = largest > 0.f && largest < INFINITY ? ilogbf(largest) : 0;
-        unit = ldexpf(unit, e);
+        const int e = largest > 0.f && largest < INFINITY ? max(ilogbf(largest), -126) : 0;
+        const float down = ldexpf(1.f, -e);
+        mine = ldexpf(unit, e);
 #pragma unroll
         for (int k = 0; k < KSTEPS; ++k)
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            float v[2];
-#pragma unroll
-            for (int z = 0; z < 2; ++z) {
-              const int d = 16 * k + 4 * (lane % 4) + 2 * y + z;
-              v[z] = head < heads && d < c.dim ? ldexpf(half_value(a.q, from + d, a.type), -e) : 0.f;
-            }
-            q[k][b][y] = pack<KIND>(v[0], v[1]);
-          }
-      } else {
-#pragma unroll
-        for (int k = 0; k < KSTEPS; ++k)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            uint32_t v[2];
-#pragma unroll
-            for (int z = 0; z < 2; ++z) {
-              const int d = 16 * k + 8 * y + 2 * (lane % 4) + z;
-              v[z] = head < heads && d < c.dim ? __ldg((const uint16_t*)a.q + from + d) : 0;
-            }
-            q[k][b][y] = v[0] | v[1] << 16;
+            const float2 v = two_halves(q[k][b][y], a.type);
+            q[k][b][y] = pack<KIND>(v.x * down, v.y * down);
           }
       }
 #pragma unroll
-      for (int y = 0; y < 2; ++y) mul[b][y] = __shfl_sync(~0u, unit, 4 * (2 * (lane % 4) + y));
+      for (int y = 0; y < 2; ++y) mul[b][y] = __shfl_sync(~0u, mine, 4 * (2 * (lane % 4) + y));
     }
+  };
 
+  load_queries(here);
+#pragma unroll 1
+  for (int j = 0; j < S::kStages - 1; ++j) step();
+  int32_t slot = 0;
+
+  while (here.left > 0) {
+    use_queries(here);
+    const Cursor u = here;  // the unit row, from its tile u.t on
+    const int32_t count = (int32_t)(u.nt - u.t < u.left ? u.nt - u.t : u.left);
+    const uint32_t first = (uint32_t)u.row.begin + (uint32_t)(u.t * kTile + warp * kRows);
     float o[KSTEPS][NB][4], top[NB][2], sum[NB][2];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -338,12 +403,13 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, K
       for (int k = 0; k < KSTEPS; ++k) o[k][b][0] = o[k][b][1] = o[k][b][2] = o[k][b][3] = 0.f;
     }
 
+#pragma unroll 1
     for (int32_t j = 0; j < count; ++j) {
       wait<S::kStages - 2>();
       __syncwarp();  // every lane's pieces of tile j are there, and every lane is done with tile j - 1
-      copy(j + S::kStages - 1);
-      look_up(j + S::kStages);
-      const uint32_t keys = tiles_at + j % S::kStages * S::kStage, values = keys + S::kArray;
+      step();
+      const uint32_t keys = tiles_at + slot * S::kStage, values = keys + S::kArray;
+      slot = slot + 1 < S::kStages ? slot + 1 : 0;
 
       float s[NB][4] = {};  // tokens lane / 4 (+ 8 in 2, 3), heads 2 * (lane % 4) + {0, 1}
       if (KIND == P2P_KV_E4M3) {
@@ -367,7 +433,7 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, K
           for (int b = 0; b < NB; ++b) multiply<KIND>(s[b], f, q[k][b]);
         }
       }
-      const int32_t left = (int32_t)((uint32_t)row.end - (first + (uint32_t)j * kTile));  // tokens of the tile that are seen, if that is below 16
+      const int32_t left = (int32_t)((uint32_t)u.row.end - (first + (uint32_t)j * kTile));  // tokens of the tile that are seen, if that is below 16
       bool past = false;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -433,16 +499,22 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, K
         }
       }
     }
-    wait<0>();
-    __syncwarp();
+    here.advance(count, c, a, blocks);
+    if (here.left > 0) load_queries(here);  // (on their way while this unit row's parts are joined)
 
-    // ---- the four warps' parts.  Their sums go to the tiles' room, [head][dim].
-    float* const sums = (float*)tiles;
+    // ---- the four warps' parts, eight heads at a time through shared memory: [head][dim], turned by the head so that
+    // neither side's accesses meet a bank twice.
+    const int32_t head0 = u.h * group + u.block * S::kHeads, heads = min(group - u.block * S::kHeads, S::kHeads);
+    const bool whole = u.t == 0 && count == u.nt, empty = u.row.end <= u.row.begin;
+    const int64_t unit0 = x_end - u.left - u.t;  // where the unit row's first tile stands among all units
+    float* const part = w.parts + (int64_t)(blockIdx.x * 2 + (u.t == 0)) * S::kPart;
+    const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + u.h) : 1.f;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
+      if (b * 8 >= heads) break;
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const int head = b * 8 + 2 * (lane % 4) + y;
+        const int head = 2 * (lane % 4) + y;
         float z = sum[b][y];
         z += __shfl_xor_sync(~0u, z, 4);
         z += __shfl_xor_sync(~0u, z, 8);
@@ -451,105 +523,83 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, K
 #pragma unroll
         for (int k = 0; k < KSTEPS; ++k) {
           const int d = KIND == P2P_KV_E4M3 ? 16 * k + 2 * (lane / 4) : 16 * k + lane / 4;
-          sums[head * S::kPitch + d] = o[k][b][y];
-          sums[head * S::kPitch + d + (KIND == P2P_KV_E4M3 ? 1 : 8)] = o[k][b][y + 2];
+          sums[head * DP + (d ^ head * 4)] = o[k][b][y];
+          sums[head * DP + ((d + (KIND == P2P_KV_E4M3 ? 1 : 8)) ^ head * 4)] = o[k][b][y + 2];
         }
+      }
+      __syncthreads();
+      for (int y = threadIdx.x; y < 8 * DP / 4; y += kThreads) {
+        const int head = y / (DP / 4), d = y % (DP / 4) * 4, h8 = b * 8 + head;
+        float t = -INFINITY, z = 0.f;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) t = fmaxf(t, sh.top[k][head]);
+        const float ref = t == -INFINITY ? 0.f : t;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) {
+          const float fade = exp2_fast(sh.top[k][head] - ref);
+          const float4 f = *(const float4*)((const float*)(room + kWarps * S::kRoom) + k * 8 * DP + head * DP + (d ^ head * 4));
+          z += fade * sh.sum[k][head];
+          v.x += fade * f.x, v.y += fade * f.y, v.z += fade * f.z, v.w += fade * f.w;
+        }
+        if (!whole) {
+          *(float4*)(part + h8 * DP + d) = v;
+          if (d == 0) part[S::kHeads * DP + h8] = t, part[S::kHeads * (DP + 1) + h8] = z;
+        } else if (h8 < heads) {
+          const float f = v_scale / z;
+          store4(c, a, u.i, head0 + h8, d, v, f, empty);
+          if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + head0 + h8] = empty ? -INFINITY : (t + log2f(z)) / kLog2e;
+        }
+      }
+      if (whole || b + 1 < NB) __syncthreads();  // the sums' room is free again
+    }
+    if (whole) continue;
+
+    // The CTA that brings the last part of the unit row joins them.
+    __threadfence();
+    __syncthreads();
+    const int32_t c0 = (int32_t)(((unit0 + 1) * ctas - 1) / total), c1 = (int32_t)(((unit0 + u.nt) * ctas - 1) / total);
+    if (threadIdx.x == 0) {
+      sh.last = atomicAdd(w.arrived + c0, 1) == c1 - c0;
+      if (sh.last) w.arrived[c0] = 0;  // for the next launch
+    }
+    __syncthreads();
+    if (!sh.last) continue;
+    __threadfence();
+    const int32_t parts = c1 - c0 + 1;
+    const auto part_of = [&](int32_t k) {  // the first CTA's is its range's last unit row, the others' their first
+      return w.parts + (int64_t)((c0 + k) * 2 + (k == 0)) * S::kPart;
+    };
+    for (int head = warp; head < heads; head += kWarps) {
+      float t = -INFINITY, z = 0.f;
+      for (int32_t k = lane; k < parts; k += 32) t = fmaxf(t, __ldcg(part_of(k) + S::kHeads * DP + head));
+#pragma unroll
+      for (int d = 16; d; d >>= 1) t = fmaxf(t, __shfl_xor_sync(~0u, t, d));
+      const float ref = t == -INFINITY ? 0.f : t;
+      for (int32_t k = lane; k < parts; k += 32)
+        z += exp2_fast(__ldcg(part_of(k) + S::kHeads * DP + head) - ref) * __ldcg(part_of(k) + S::kHeads * (DP + 1) + head);
+#pragma unroll
+      for (int d = 16; d; d >>= 1) z += __shfl_xor_sync(~0u, z, d);
+      if (lane == 0) {
+        sh.base[head] = ref;
+        sh.total[head] = z;
+        if (a.lse) a.lse[(int64_t)u.i * a.heads + head0 + head] = (t + log2f(z)) / kLog2e;
       }
     }
     __syncthreads();
-    const bool whole = t0 == 0 && t1 == nt;
-    const int64_t x0 = x - t0;  // the unit row's first unit
-    const int32_t slot = blockIdx.x * 2 + (t0 == 0);
-    float* const part = w.parts + (int64_t)slot * S::kPart;
-    const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + h) : 1.f;
-    const bool empty = row.end <= row.begin;
-    for (int y = threadIdx.x; y < S::kHeads * DP / 4; y += kThreads) {
+    for (int y = threadIdx.x; y < heads * (DP / 4); y += kThreads) {
       const int head = y / (DP / 4), d = y % (DP / 4) * 4;
-      float t = -INFINITY, z = 0.f;
-#pragma unroll
-      for (int k = 0; k < kWarps; ++k) t = fmaxf(t, sh.top[k][head]);
-      const float ref = t == -INFINITY ? 0.f : t;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < kWarps; ++k) {
-        const float fade = exp2_fast(sh.top[k][head] - ref);
-        const float4 u = *(const float4*)((const float*)(room + k * S::kStages * S::kStage) + head * S::kPitch + d);
-        z += fade * sh.sum[k][head];
-        v.x += fade * u.x, v.y += fade * u.y, v.z += fade * u.z, v.w += fade * u.w;
-      }
-      if (!whole) {
-        *(float4*)(part + head * DP + d) = v;
-        if (d == 0) part[S::kHeads * DP + head] = t, part[S::kHeads * (DP + 1) + head] = z;
-      } else if (head < heads) {
-        const float f = v_scale / z;
-        const int64_t to = i * a.out_row + (head0 + head) * a.out_head + d;
-        const float r[4] = {v.x * f, v.y * f, v.z * f, v.w * f};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (d + k < c.dim) store_half(a.out, to + k, a.type, empty ? 0.f : r[k]);
-        if (d == 0 && a.lse) a.lse[(int64_t)i * a.heads + head0 + head] = empty ? -INFINITY : (t + log2f(z)) / kLog2e;
-      }
-    }
-    if (!whole) {
-      // The CTA that brings the last part of the unit row joins them.
-      __threadfence();
-      __syncthreads();
-      const int32_t c0 = (int32_t)(((x0 + 1) * ctas - 1) / total), c1 = (int32_t)(((x0 + nt) * ctas - 1) / total);
-      if (threadIdx.x == 0) {
-        sh.last = atomicAdd(w.arrived + c0, 1) == c1 - c0;
-        if (sh.last) w.arrived[c0] = 0;  // for the next launch
-      }
-      __syncthreads();
-      if (sh.last) {
-        __threadfence();
-        const int32_t parts = c1 - c0 + 1;
-        const auto part_of = [&](int32_t k) {  // the first CTA's is its range's last unit row, the others' their first
-          return w.parts + (int64_t)((c0 + k) * 2 + (k == 0)) * S::kPart;
-        };
-        for (int head = warp; head < heads; head += kWarps) {
-          float t = -INFINITY, z = 0.f;
-          for (int32_t k = lane; k < parts; k += 32) t = fmaxf(t, __ldcg(part_of(k) + S::kHeads * DP + head));
-#pragma unroll
-          for (int d = 16; d; d >>= 1) t = fmaxf(t, __shfl_xor_sync(~0u, t, d));
-          const float ref = t == -INFINITY ? 0.f : t;
-          for (int32_t k = lane; k < parts; k += 32)
-            z += exp2_fast(__ldcg(part_of(k) + S::kHeads * DP + head) - ref) * __ldcg(part_of(k) + S::kHeads * (DP + 1) + head);
-#pragma unroll
-          for (int d = 16; d; d >>= 1) z += __shfl_xor_sync(~0u, z, d);
-          if (lane == 0) {
-            sh.base[head] = ref;
-            sh.total[head] = z;
-            if (a.lse) a.lse[(int64_t)i * a.heads + head0 + head] = (t + log2f(z)) / kLog2e;
-          }
-        }
-        __syncthreads();
-        for (int y = threadIdx.x; y < heads * (DP / 4); y += kThreads) {
-          const int head = y / (DP / 4), d = y % (DP / 4) * 4;
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-          for (int32_t k = 0; k < parts; ++k) {
-            const float* p = part_of(k);
-            const float fade = exp2_fast(__ldcg(p + S::kHeads * DP + head) - sh.base[head]);
-            const float4 u = __ldcg((const float4*)(p + head * DP + d));
-            v.x += fade * u.x, v.y += fade * u.y, v.z += fade * u.z, v.w += fade * u.w;
-          }
-          const float f = v_scale / sh.total[head];
-          const int64_t to = i * a.out_row + (head0 + head) * a.out_head + d;
-          const float r[4] = {v.x * f, v.y * f, v.z * f, v.w * f};
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (d + k < c.dim) store_half(a.out, to + k, a.type, r[k]);
-        }
+      for (int32_t k = 0; k < parts; ++k) {
+        const float* p = part_of(k);
+        const float fade = exp2_fast(__ldcg(p + S::kHeads * DP + head) - sh.base[head]);
+        const float4 f = __ldcg((const float4*)(p + head * DP + d));
+        v.x += fade * f.x, v.y += fade * f.y, v.z += fade * f.z, v.w += fade * f.w;
       }
+      store4(c, a, u.i, head0 + head, d, v, v_scale / sh.total[head], false);
     }
-    __syncthreads();  // the tiles' room and sh are free again
-
-    x += t1 - t0;
-    if (x - row_x == (int64_t)nt * per_row) {
-      row_x = x;
-      row = next;
-      ++i;
-    }
+    __syncthreads();
   }
 }
 
@@ -559,19 +609,24 @@ cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, 
   using S = Shape<KIND, DP, NB>;
   const auto kernel = attend_kernel<KIND, DP, NB>;
   if (!q) return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
-  // As many CTAs as are resident together (by shared memory: 227 KB an SM, 1 KB of it the system's for each CTA).
-  const int per_sm = std::max(1, std::min(KvAttendScratch::kCtasPerSm, 232448 / (S::kBytes + 2048)));
-  kernel<<<per_sm * num_sms, kThreads, S::kBytes, st>>>(c, *q, w);
+  // As many CTAs as are resident together (by shared memory: 227 KB an SM, of which each CTA takes 1 KB for the system).
+  static_assert(S::kCtas <= KvAttendScratch::kCtasPerSm, "the scratch is for so many");
+  kernel<<<S::kCtas * num_sms, kThreads, S::kBytes, st>>>(c, *q, w);
   return cudaGetLastError();
 }
 
+// (Blocks of 16 query heads take 192 registers at DP = 256: blocks of eight, whose keys and values the second finds in L2.)
 template <int KIND, int DP>
 cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  if (!q) {
-    const cudaError_t e = launch<KIND, DP, 1>(c, q, w, num_sms, st);
-    return e == cudaSuccess ? launch<KIND, DP, 2>(c, q, w, num_sms, st) : e;
+  if constexpr (DP == 256) {
+    return launch<KIND, DP, 1>(c, q, w, num_sms, st);
+  } else {
+    if (!q) {
+      const cudaError_t e = launch<KIND, DP, 1>(c, q, w, num_sms, st);
+      return e == cudaSuccess ? launch<KIND, DP, 2>(c, q, w, num_sms, st) : e;
+    }
+    return q->heads / c.heads <= 8 ? launch<KIND, DP, 1>(c, q, w, num_sms, st) : launch<KIND, DP, 2>(c, q, w, num_sms, st);
   }
-  return q->heads / c.heads <= 8 ? launch<KIND, DP, 1>(c, q, w, num_sms, st) : launch<KIND, DP, 2>(c, q, w, num_sms, st);
 }
 
 template <int KIND>

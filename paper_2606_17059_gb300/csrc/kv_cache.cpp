@@ -302,7 +302,9 @@ int p2p_kv_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const
   if ((uintptr_t)q % 2 || (uintptr_t)out % 2 || (uintptr_t)lse % 4) return fail(h, P2P_E_INVAL, "a pointer is not aligned to its type");
   DeviceGuard g(h->device);
   const p2p::KvQuery a = {q, out, lse, seq, q_row_stride, q_head_stride, out_row_stride, out_head_stride,
-                          n, n_heads, type, window, layer, scale};
+                          n, n_heads, type, window, layer, scale,
+                          (uintptr_t)q % 4 == 0 && q_row_stride % 2 == 0 && q_head_stride % 2 == 0,
+                          (uintptr_t)out % 8 == 0 && out_row_stride % 4 == 0 && out_head_stride % 4 == 0};
   CK(p2p::launch_kv_attend(h->c, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;
