@@ -41,8 +41,8 @@ struct KvView {
 // Bits of the device error word.
 enum { KV_BAD_SEQ = 1, KV_BAD_COUNT = 2, KV_NO_PAGES = 4, KV_BAD_PAGE = 8, KV_SHARED = 16, KV_BAD_OFFSETS = 32 };
 
-struct KvJob {  // copy the first `tokens` tokens of page `from` to page `to`, in every layer
-  int32_t from, to, tokens;
+struct __align__(16) KvJob {  // copy the first `tokens` tokens of page `from` to page `to`, in every layer
+  int32_t from, to, tokens, pad_;
 };
 
 // Device words and scratch of the calls that change the page tables.
@@ -50,14 +50,16 @@ struct KvScratch {
   int32_t* err;    // error bits since the last p2p_kv_sync
   int32_t* halt;   // 1 since a call on the tables failed: later ones, and writes, change nothing until p2p_kv_sync
   int32_t* njobs;
+  int32_t* live;   // pages in use, as a compaction found them
   int32_t* claim;  // [n_seqs], zero between calls: a sequence named twice in one call
   int32_t* start;  // [n_seqs + 1]: where a sequence's page entries start among the call's
   int32_t* first;  // [n_seqs]: its first entry concerned
   int32_t* cut;    // [n_seqs]: > 0: the tokens of its shared last page that it takes along into a page of its own
-  int32_t* list;   // [n_pages]: free pages in ascending order; compaction: a page's new number
+  int32_t* list;   // [n_pages]: compaction: a moved page's new number
   KvJob* jobs;     // [max(n_seqs, n_pages)]
 };
 
+cudaError_t prepare_kv_pages();  // makes the kernels ready for launches (at creation)
 cudaError_t launch_kv_extend(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* count,
                              int num_sms, cudaStream_t st);
 cudaError_t launch_kv_trim(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* to, cudaStream_t st);

@@ -145,6 +145,7 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
                parts = part(sizeof(float) * p2p::kv_attend_parts(a.head_dim, sms));
   cudaError_t e = cudaMalloc(&n->scratch, at);
   if (e == cudaSuccess) e = cudaMemset(n->scratch, 0, zero);
+  if (e == cudaSuccess) e = p2p::prepare_kv_pages();
   if (e == cudaSuccess) e = p2p::launch_kv_attend(c, nullptr, n->w, sms, nullptr);
   if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);  // (calls may go to a stream that does not wait for this one)
   if (e != cudaSuccess) {
@@ -157,6 +158,7 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   n->s.err = (int32_t*)(p + words);
   n->s.halt = n->s.err + 1;
   n->s.njobs = n->s.err + 2;
+  n->s.live = n->s.err + 3;
   n->d_stats = (unsigned long long*)(p + words + 64);
   n->s.claim = (int32_t*)(p + claim);
   n->s.start = (int32_t*)(p + start);

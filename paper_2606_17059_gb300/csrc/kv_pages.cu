@@ -1,9 +1,15 @@
 // kv_pages.cu -- the page tables of the paged key-value cache: extend, trim, fork, compact, write (p2p_kv_*).
 //
-// A call over a list of sequences is planned by one CTA: every item is checked, the page entries it concerns are
-// counted and scanned, and the entries are then worked off as one flat range, so that one long sequence and many short
-// ones take the same time.  Nothing is changed before every item has been found good.  Pages are copied by a second
-// launch over the whole GPU from the list of copies that the plan leaves.
+// A call on the tables is one cluster of eight CTAs.  Each of them checks every item, counts the page entries that it
+// concerns and scans the counts in its own shared memory (for long lists the first CTA does, in scratch); the pool's
+// reference counts are scanned in eight parts.  The CTAs tell each other what they found through shared memory and
+// meet once; then, if every item was good, the entries are worked off as one flat range, so that one long sequence and
+// many short ones take the same time.  Nothing is changed before that.  What bounds these calls is the chain of loads
+// behind an item (its sequence, the length, the last page, its count) and of the launch itself.
+//
+// Pages are copied by a second launch over the whole GPU, from the list of copies that the plan leaves; it is started
+// early and waits for the plan.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -13,34 +19,59 @@
 namespace p2p {
 namespace {
 
-constexpr int kThreads = 1024;
+namespace cg = cooperative_groups;
 
-// Exclusive scan of one value a thread over the CTA; total: the sum.  (warp_sum: one word a warp.)
-__device__ int64_t block_scan(int64_t v, int64_t* warp_sum, int64_t& total) {
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kCluster = 8;
+constexpr int kItems = 8192;  // items of a call whose plan fits shared memory
+
+// What a CTA of the cluster tells the others.
+struct Found {
+  int64_t count, count2;
+  int32_t err;
+};
+struct Plan {
+  Found found[kCluster];
+  int64_t warp_sum[kWarps];
+  int32_t warp_count[kWarps];
+  int32_t err, cuts;
+};
+// The items of a call: their first entry among the call's (start[n]: all), the first page entry they concern, and, for
+// extend, the tokens of a shared last page that move to a page of their own (0: none).
+struct Items {
+  int32_t *start, *first, *cut;
+};
+extern __shared__ int32_t item_room[];
+__device__ __forceinline__ Items items_of(const KvScratch& s, int32_t n) {
+  if (n > kItems) return {s.start, s.first, s.cut};
+  return {item_room, item_room + n + 1, item_room + 2 * n + 1};
+}
+size_t item_bytes(int32_t n) { return n > kItems ? 0 : (size_t)(3 * n + 1) * sizeof(int32_t); }
+
+// Exclusive scan of one value a thread over the CTA; total: the sum.
+__device__ int64_t block_scan(int64_t v, Plan& p, int64_t& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int64_t x = v;
+#pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const int64_t y = __shfl_up_sync(~0u, x, d);
     if (lane >= d) x += y;
   }
   __syncthreads();  // the words of an earlier scan have been read
-  if (lane == 31) warp_sum[warp] = x;
+  if (lane == 31) p.warp_sum[warp] = x;
   __syncthreads();
-  int64_t before = 0, all = 0;
-  for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) before += warp_sum[w];
-    all += warp_sum[w];
+  int64_t w = p.warp_sum[lane], sum = w;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t y = __shfl_up_sync(~0u, sum, d);
+    if (lane >= d) sum += y;
   }
-  total = all;
-  return before + x - v;
+  total = __shfl_sync(~0u, sum, 31);
+  return __shfl_sync(~0u, sum - w, warp) + x - v;
 }
+static_assert(kWarps == 32, "a lane a warp");
 
-struct Plan {  // shared memory of a planning CTA
-  int32_t err;
-  int64_t warp_sum[kThreads / 32];
-};
-
-// The item (index into start[0 .. n], start[n] = total) that entry r belongs to.
+// The item that entry r belongs to.
 __device__ __forceinline__ int32_t item_of(const int32_t* start, int32_t n, int32_t r) {
   int32_t lo = 0, hi = n;  // start[lo] <= r < start[hi]
   while (hi - lo > 1) {
@@ -53,37 +84,95 @@ __device__ __forceinline__ int32_t item_of(const int32_t* start, int32_t n, int3
   return lo;
 }
 
-// Counts of the items (in start[]) -> their exclusive scan in place; returns the total, or -1 (and an error bit) where it
-// does not fit the table's entries.
-__device__ int64_t scan_items(int32_t* start, int32_t n, Plan& p) {
+// Fills in the items: item(i, need, first, cut) gives the entries that item i concerns, and its error bits.
+template <class F>
+__device__ void plan_items(Plan& p, const Items& it, int32_t n, F item) {
   int64_t carry = 0;
   for (int32_t i0 = 0; i0 < n; i0 += kThreads) {
     const int32_t i = i0 + threadIdx.x;
+    int32_t need = 0, first = 0, cut = 0;
+    if (i < n)
+      if (const int32_t bad = item(i, need, first, cut)) atomicOr(&p.err, bad), need = 0;
     int64_t total;
-    const int64_t at = carry + block_scan(i < n ? start[i] : 0, p.warp_sum, total);
-    if (i < n) start[i] = (int32_t)at;
+    const int64_t at = carry + block_scan(need, p, total);
+    if (i < n) it.start[i] = (int32_t)at, it.first[i] = first, it.cut[i] = cut;
     carry += total;
-    if (carry > INT32_MAX) return -1;
   }
-  if (threadIdx.x == 0) start[n] = (int32_t)carry;
+  if (threadIdx.x == 0) {
+    if (carry > INT32_MAX) p.err |= KV_BAD_COUNT;
+    it.start[n] = (int32_t)carry;
+  }
   __syncthreads();
-  return carry;
 }
 
-// Gives up the claims of a call's sequences and reports its errors; true if there are any.
-__device__ bool settle(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, int32_t err) {
+// Tells the cluster what this CTA found and waits for the others; returns all their error bits.
+__device__ int32_t meet(Plan& p, int64_t count, int64_t count2) {
+  cg::cluster_group cluster = cg::this_cluster();
+  __syncthreads();
+  if (threadIdx.x < kCluster)
+    *cluster.map_shared_rank(&p.found[cluster.block_rank()], threadIdx.x) = Found{count, count2, p.err};
+  cluster.sync();
+  int32_t err = 0;
+#pragma unroll
+  for (int k = 0; k < kCluster; ++k) err |= p.found[k].err;
+  return err;
+}
+
+// This thread block's part of the pool, by warps: pages begin .. end of this warp.
+struct Part {
+  int32_t begin, end;
+};
+__device__ __forceinline__ Part part_of(const KvView& c, int rank) {
+  const int32_t each = ((c.n_pages + kCluster * kWarps - 1) / (kCluster * kWarps) + 31) / 32 * 32;
+  const int64_t begin = (int64_t)(rank * kWarps + (threadIdx.x >> 5)) * each;
+  return {(int32_t)(begin < c.n_pages ? begin : c.n_pages), (int32_t)(begin + each < c.n_pages ? begin + each : c.n_pages)};
+}
+// How many of the warp's pages hold for `what`; every lane gets the sum.
+template <class F>
+__device__ __forceinline__ int32_t count_pages(const KvView& c, const Part& r, F what) {
+  const int lane = threadIdx.x & 31;
+  int32_t n = 0;
+#pragma unroll 8
+  for (int32_t page = r.begin + lane; page < r.end; page += 32) n += what(page, __ldcg(c.refs + page));
+  return __reduce_add_sync(~0u, n);
+}
+// The warps' counts: this warp's place among the CTA's, and the CTA's sum.
+__device__ int32_t scan_warps(Plan& p, int32_t mine, int32_t& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __syncthreads();
+  if (lane == 0) p.warp_count[warp] = mine;
+  __syncthreads();
+  const int32_t v = p.warp_count[lane];
+  total = __reduce_add_sync(~0u, v);
+  return __reduce_add_sync(~0u, lane < warp ? v : 0);
+}
+// f(page, k) for the warp's pages that hold for `what`, k counting on from `at`; ends when k passes `most`.
+template <class F, class G>
+__device__ __forceinline__ void each_page(const KvView& c, const Part& r, int64_t at, int64_t most, F what, G f) {
+  const int lane = threadIdx.x & 31;
+  for (int32_t p0 = r.begin; p0 < r.end && at < most; p0 += 32) {
+    const int32_t page = p0 + lane;
+    const bool is = page < r.end && what(page, __ldcg(c.refs + page));
+    const uint32_t m = __ballot_sync(~0u, is);
+    const int64_t k = at + __popc(m & ((1u << lane) - 1));
+    if (is && k < most) f(page, k);
+    at += __popc(m);
+  }
+}
+
+// Gives up the claims of a call's sequences; reports its errors and returns whether there are any.  (The first CTA.)
+__device__ void settle(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, int32_t err) {
   for (int32_t i = threadIdx.x; i < n; i += kThreads)
     if ((uint32_t)seq[i] < (uint32_t)c.n_seqs) s.claim[seq[i]] = 0;
   if (err && threadIdx.x == 0) {
     atomicOr(s.err, err);
     *s.halt = 1;
   }
-  return err != 0;
 }
-
-__device__ __forceinline__ int32_t claim(const KvView& c, const KvScratch& s, int32_t seq) {
+// (The first CTA alone marks the sequences: what it meets a second time was named twice.)
+__device__ __forceinline__ int32_t claim(const KvView& c, const KvScratch& s, int32_t seq, bool first) {
   if ((uint32_t)seq >= (uint32_t)c.n_seqs) return KV_BAD_SEQ;
-  return atomicExch(&s.claim[seq], 1) ? KV_BAD_SEQ : 0;
+  return first && atomicExch(&s.claim[seq], 1) ? KV_BAD_SEQ : 0;
 }
 
 // A length as the table can hold it, or -1.
@@ -93,275 +182,382 @@ __device__ __forceinline__ int32_t length_of(const KvView& c, int32_t seq) {
 }
 __device__ __forceinline__ int32_t* row_of(const KvView& c, int32_t seq) { return c.table + (int64_t)seq * c.max_pages; }
 
-__global__ void __launch_bounds__(kThreads) extend_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ seq,
-                                                          const int32_t* __restrict__ count) {
+__device__ __forceinline__ void start_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_plan() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+    extend_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ seq, const int32_t* __restrict__ count) {
   __shared__ Plan p;
-  if (threadIdx.x == 0) p.err = 0, *s.njobs = 0;
-  __syncthreads();
+  const int rank = (int)cg::this_cluster().block_rank();
+  start_dependents();
+  if (threadIdx.x == 0) {
+    p.err = p.cuts = 0;
+    if (rank == 0) *s.njobs = 0;
+  }
   if (*s.halt) return;
-  for (int32_t i = threadIdx.x; i < n; i += kThreads) {
-    int32_t need = 0, first = 0, cut = 0;
-    int32_t bad = claim(c, s, seq[i]);
-    if (!bad) {
+  __syncthreads();
+  const Part mine = part_of(c, rank);
+  const auto is_free = [](int32_t, int32_t refs) { return refs == 0; };
+  int32_t free_here;
+  const int32_t free_before = scan_warps(p, count_pages(c, mine, is_free), free_here);
+  const Items it = items_of(s, n);
+  if (rank == 0 || n <= kItems)
+    plan_items(p, it, n, [&](int32_t i, int32_t& need, int32_t& first, int32_t& cut) -> int32_t {
+      if (const int32_t bad = claim(c, s, seq[i], rank == 0)) return bad;
       const int32_t len = length_of(c, seq[i]), add = count[i];
-      if (len < 0 || add < 0 || add > c.max_pages * c.page - len) {
-        bad = KV_BAD_COUNT;
-      } else {
-        const int32_t have = (int32_t)c.by_page.ceil(len);
-        need = (int32_t)c.by_page.ceil(len + add) - have;
-        first = have;
-        const int32_t used = len - (int32_t)c.by_page.div(len) * c.page;
-        if (add > 0 && used > 0) {
-          const int32_t last = row_of(c, seq[i])[have - 1];
-          if ((uint32_t)last >= (uint32_t)c.n_pages || c.refs[last] < 1)
-            bad = KV_BAD_PAGE;
-          else if (c.refs[last] > 1)
-            cut = used, first = have - 1, need += 1;
-        }
+      if (len < 0 || add < 0 || add > c.max_pages * c.page - len) return KV_BAD_COUNT;
+      const int32_t have = (int32_t)c.by_page.ceil(len);
+      need = (int32_t)c.by_page.ceil(len + add) - have;
+      first = have;
+      const int32_t used = len - (int32_t)c.by_page.div(len) * c.page;
+      if (add > 0 && used > 0) {
+        const int32_t last = row_of(c, seq[i])[have - 1];
+        const int32_t refs = (uint32_t)last < (uint32_t)c.n_pages ? __ldcg(c.refs + last) : 0;
+        if (refs < 1) return KV_BAD_PAGE;
+        if (refs > 1) cut = used, first = have - 1, need += 1, p.cuts = 1;
       }
-    }
-    if (bad) atomicOr(&p.err, bad);
-    s.start[i] = need;
-    s.first[i] = first;
-    s.cut[i] = cut;
+      return 0;
+    });
+  int32_t err = meet(p, free_here, p.cuts);
+  const int32_t total = it.start[n];
+  int64_t at = free_before, all = 0;
+#pragma unroll
+  for (int k = 0; k < kCluster; ++k) {
+    all += p.found[k].count;
+    at += k < rank ? p.found[k].count : 0;
   }
-  __syncthreads();
-  int64_t total = p.err ? 0 : scan_items(s.start, n, p);
-  // The lowest free pages, as many as are needed.
-  int64_t found = 0;
-  if (!p.err && total > c.n_pages) total = -1;
-  if (!p.err && total > 0) {
-    for (int32_t p0 = 0; p0 < c.n_pages && found < total; p0 += kThreads) {
-      const int32_t page = p0 + threadIdx.x;
-      const bool free = page < c.n_pages && c.refs[page] == 0;
-      int64_t here;
-      const int64_t at = found + block_scan(free, p.warp_sum, here);
-      if (free && at < total) s.list[at] = page;
-      found += here;
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x == 0 && !p.err && (total < 0 || found < total)) p.err = KV_NO_PAGES;
-  __syncthreads();
-  if (settle(c, s, n, seq, p.err)) return;
-  for (int32_t r = threadIdx.x; r < total; r += kThreads) {
-    const int32_t i = item_of(s.start, n, r), e = s.first[i] + r - s.start[i], page = s.list[r];
+  if (!err && total > all) err = KV_NO_PAGES;
+  if (rank == 0) settle(c, s, n, seq, err);
+  if (err) return;
+  // The free pages, from the lowest on, go to the entries in their order.
+  each_page(c, mine, at, total, is_free, [&](int32_t page, int64_t k) {
+    const int32_t r = (int32_t)k, i = item_of(it.start, n, r), e = it.first[i] + r - it.start[i];
     int32_t* row = row_of(c, seq[i]);
-    if (s.cut[i] && r == s.start[i]) {
-      const int32_t old = row[e];
-      atomicSub(&c.refs[old], 1);
-      s.jobs[atomicAdd(s.njobs, 1)] = KvJob{old, page, s.cut[i]};
-    }
+    if (it.cut[i] && r == it.start[i]) s.jobs[atomicAdd(s.njobs, 1)] = KvJob{row[e], page, it.cut[i], 0};
     row[e] = page;
     c.refs[page] = 1;
+  });
+  if (p.found[0].count2) {
+    cg::this_cluster().sync();  // (a page that all its sharers leave is free from here on, not for this call's entries)
+    const int32_t jobs = __ldcg(s.njobs);
+    for (int32_t k = rank * kThreads + threadIdx.x; k < jobs; k += kCluster * kThreads) atomicSub(&c.refs[__ldcg(&s.jobs[k].from)], 1);
   }
-  for (int32_t i = threadIdx.x; i < n; i += kThreads) c.length[seq[i]] += count[i];
+  if (rank == 0)
+    for (int32_t i = threadIdx.x; i < n; i += kThreads) c.length[seq[i]] += count[i];
 }
 
-__global__ void __launch_bounds__(kThreads) trim_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ seq,
-                                                        const int32_t* __restrict__ to) {
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+    trim_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ seq, const int32_t* __restrict__ to) {
   __shared__ Plan p;
+  const int rank = (int)cg::this_cluster().block_rank();
   if (threadIdx.x == 0) p.err = 0;
-  __syncthreads();
   if (*s.halt) return;
-  for (int32_t i = threadIdx.x; i < n; i += kThreads) {
-    int32_t need = 0, keep = 0;
-    int32_t bad = claim(c, s, seq[i]);
-    if (!bad) {
+  __syncthreads();
+  const Items it = items_of(s, n);
+  if (rank == 0 || n <= kItems)
+    plan_items(p, it, n, [&](int32_t i, int32_t& need, int32_t& first, int32_t&) -> int32_t {
+      if (const int32_t bad = claim(c, s, seq[i], rank == 0)) return bad;
       const int32_t len = length_of(c, seq[i]);
-      if (len < 0 || to[i] < 0 || to[i] > len) {
-        bad = KV_BAD_COUNT;
-      } else {
-        keep = (int32_t)c.by_page.ceil(to[i]);
-        need = (int32_t)c.by_page.ceil(len) - keep;
-      }
-    }
-    if (bad) atomicOr(&p.err, bad);
-    s.start[i] = need;
-    s.first[i] = keep;
-  }
-  __syncthreads();
-  int64_t total = p.err ? 0 : scan_items(s.start, n, p);
-  __syncthreads();
-  if (threadIdx.x == 0 && total < 0) p.err = KV_BAD_COUNT;
-  __syncthreads();
-  if (settle(c, s, n, seq, p.err)) return;
-  for (int32_t r = threadIdx.x; r < total; r += kThreads) {
-    const int32_t i = item_of(s.start, n, r), page = row_of(c, seq[i])[s.first[i] + r - s.start[i]];
+      if (len < 0 || to[i] < 0 || to[i] > len) return KV_BAD_COUNT;
+      first = (int32_t)c.by_page.ceil(to[i]);
+      need = (int32_t)c.by_page.ceil(len) - first;
+      return 0;
+    });
+  const int32_t err = meet(p, 0, 0);
+  if (rank == 0) settle(c, s, n, seq, err);
+  if (err) return;
+  const int32_t total = it.start[n];
+  for (int64_t r = rank * kThreads + threadIdx.x; r < total; r += kCluster * kThreads) {
+    const int32_t i = item_of(it.start, n, (int32_t)r), page = row_of(c, seq[i])[it.first[i] + (int32_t)r - it.start[i]];
     if ((uint32_t)page >= (uint32_t)c.n_pages)
       atomicOr(s.err, KV_BAD_PAGE);
     else if (atomicSub(&c.refs[page], 1) < 1)
       atomicAdd(&c.refs[page], 1), atomicOr(s.err, KV_BAD_PAGE);
   }
-  for (int32_t i = threadIdx.x; i < n; i += kThreads) c.length[seq[i]] = to[i];
+  if (rank == 0)
+    for (int32_t i = threadIdx.x; i < n; i += kThreads) c.length[seq[i]] = to[i];
 }
 
-__global__ void __launch_bounds__(kThreads) fork_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ src,
-                                                        const int32_t* __restrict__ dst, const int32_t* __restrict__ tokens) {
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+    fork_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                const int32_t* __restrict__ tokens) {
   __shared__ Plan p;
+  const int rank = (int)cg::this_cluster().block_rank();
   if (threadIdx.x == 0) p.err = 0;
-  __syncthreads();
   if (*s.halt) return;
-  for (int32_t i = threadIdx.x; i < n; i += kThreads) {
-    int32_t need = 0;
-    int32_t bad = claim(c, s, dst[i]);
-    if (!bad && (uint32_t)src[i] >= (uint32_t)c.n_seqs) bad = KV_BAD_SEQ;
-    if (!bad) {
+  __syncthreads();
+  const Items it = items_of(s, n);
+  if (rank == 0 || n <= kItems)
+    plan_items(p, it, n, [&](int32_t i, int32_t& need, int32_t&, int32_t&) -> int32_t {
+      if (const int32_t bad = claim(c, s, dst[i], rank == 0)) return bad;
+      if ((uint32_t)src[i] >= (uint32_t)c.n_seqs) return KV_BAD_SEQ;
       const int32_t len = length_of(c, src[i]);
-      if (len < 0 || tokens[i] < 0 || tokens[i] > len || c.length[dst[i]] != 0)
-        bad = KV_BAD_COUNT;
-      else
-        need = (int32_t)c.by_page.ceil(tokens[i]);
-    }
-    if (bad) atomicOr(&p.err, bad);
-    s.start[i] = need;
-  }
-  __syncthreads();
-  int64_t total = p.err ? 0 : scan_items(s.start, n, p);
-  __syncthreads();
-  if (threadIdx.x == 0 && total < 0) p.err = KV_BAD_COUNT;
-  __syncthreads();
-  if (settle(c, s, n, dst, p.err)) return;
-  for (int32_t r = threadIdx.x; r < total; r += kThreads) {
-    const int32_t i = item_of(s.start, n, r), e = r - s.start[i], page = row_of(c, src[i])[e];
+      if (len < 0 || tokens[i] < 0 || tokens[i] > len || c.length[dst[i]] != 0) return KV_BAD_COUNT;
+      need = (int32_t)c.by_page.ceil(tokens[i]);
+      return 0;
+    });
+  const int32_t err = meet(p, 0, 0);
+  if (rank == 0) settle(c, s, n, dst, err);
+  if (err) return;
+  const int32_t total = it.start[n];
+  for (int64_t r = rank * kThreads + threadIdx.x; r < total; r += kCluster * kThreads) {
+    const int32_t i = item_of(it.start, n, (int32_t)r), e = (int32_t)r - it.start[i], page = row_of(c, src[i])[e];
     row_of(c, dst[i])[e] = page;
     if ((uint32_t)page >= (uint32_t)c.n_pages)
       atomicOr(s.err, KV_BAD_PAGE);
     else
       atomicAdd(&c.refs[page], 1);
   }
-  for (int32_t i = threadIdx.x; i < n; i += kThreads) c.length[dst[i]] = tokens[i];
+  if (rank == 0)
+    for (int32_t i = threadIdx.x; i < n; i += kThreads) c.length[dst[i]] = tokens[i];
 }
 
-// n_live pages are in use: those at n_live and beyond go to the free ones below, both in ascending order.  list[page] =
-// where a page goes; the copies become jobs.
-__global__ void __launch_bounds__(kThreads) compact_kernel(KvView c, KvScratch s) {
+// `live` pages are in use: those numbered live and up go to the free ones below, both in ascending order.  The k-th of
+// either kind is job k's; list[page]: where a page goes (the tables follow in copy_pages_kernel).
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) compact_kernel(KvView c, KvScratch s) {
   __shared__ Plan p;
-  if (threadIdx.x == 0) *s.njobs = 0;
-  __syncthreads();
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank();
+  start_dependents();
+  if (threadIdx.x == 0) {
+    p.err = 0;
+    if (rank == 0) *s.njobs = 0, *s.live = c.n_pages;
+  }
   if (*s.halt) return;
+  __syncthreads();
+  const Part mine = part_of(c, rank);
+  int32_t used;
+  scan_warps(p, count_pages(c, mine, [](int32_t, int32_t refs) { return refs > 0; }), used);
+  meet(p, used, 0);
   int64_t live = 0;
-  for (int32_t p0 = 0; p0 < c.n_pages; p0 += kThreads) {
-    const int32_t page = p0 + threadIdx.x;
-    int64_t here;
-    block_scan(page < c.n_pages && c.refs[page] > 0, p.warp_sum, here);
-    live += here;
+#pragma unroll
+  for (int k = 0; k < kCluster; ++k) live += p.found[k].count;
+  cluster.sync();  // p.found is written again
+  const auto hole = [live](int32_t page, int32_t refs) { return page < live && refs <= 0; };
+  const auto mover = [live](int32_t page, int32_t refs) { return page >= live && refs > 0; };
+  int32_t holes, movers;
+  int64_t h = scan_warps(p, count_pages(c, mine, hole), holes);
+  int64_t m = scan_warps(p, count_pages(c, mine, mover), movers);
+  meet(p, holes, movers);
+  int64_t jobs = 0;
+#pragma unroll
+  for (int k = 0; k < kCluster; ++k) {
+    jobs += p.found[k].count2;
+    h += k < rank ? p.found[k].count : 0;
+    m += k < rank ? p.found[k].count2 : 0;
   }
-  int64_t holes = 0, movers = 0;
-  for (int32_t p0 = 0; p0 < c.n_pages; p0 += kThreads) {
-    const int32_t page = p0 + threadIdx.x;
-    const bool in = page < c.n_pages, used = in && c.refs[page] > 0, hole = in && page < live && !used, mover = used && page >= live;
-    int64_t nh, nm;
-    const int64_t h = holes + block_scan(hole, p.warp_sum, nh), m = movers + block_scan(mover, p.warp_sum, nm);
-    if (hole) s.jobs[h].to = page;
-    if (mover) s.jobs[m].from = page, s.jobs[m].tokens = c.page;
-    holes += nh;
-    movers += nm;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) *s.njobs = (int32_t)movers;
-  for (int32_t m = threadIdx.x; m < movers; m += kThreads) {
-    const KvJob j = s.jobs[m];
-    s.list[j.from] = j.to;
-    c.refs[j.to] = c.refs[j.from];
-    c.refs[j.from] = 0;
-  }
-  __syncthreads();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int32_t q = warp; q < c.n_seqs; q += kThreads / 32) {
-    const int32_t len = length_of(c, q), used = len < 0 ? 0 : (int32_t)c.by_page.ceil(len);
-    if (len < 0 && lane == 0) atomicOr(s.err, KV_BAD_COUNT);
-    int32_t* row = row_of(c, q);
-    for (int32_t e = lane; e < used; e += 32) {
-      const int32_t page = row[e];
-      if ((uint32_t)page >= (uint32_t)c.n_pages)
-        atomicOr(s.err, KV_BAD_PAGE);
-      else if (page >= live)
-        row[e] = s.list[page];
-    }
+  each_page(c, mine, h, jobs, hole, [&](int32_t page, int64_t k) { s.jobs[k].to = page; });
+  each_page(c, mine, m, jobs, mover, [&](int32_t page, int64_t k) { s.jobs[k].from = page, s.jobs[k].tokens = c.page; });
+  cluster.sync();
+  if (rank == 0 && threadIdx.x == 0) *s.njobs = (int32_t)jobs, *s.live = (int32_t)live;
+  for (int64_t k = rank * kThreads + threadIdx.x; k < jobs; k += kCluster * kThreads) {
+    const int4 j = __ldcg((const int4*)(s.jobs + k));  // from, to
+    s.list[j.x] = j.y;
+    c.refs[j.y] = c.refs[j.x];
+    c.refs[j.x] = 0;
   }
 }
 
-// The copies of the plan before it: one CTA a page, layer and array (keys or values) at a time.
-__global__ void __launch_bounds__(256) copy_pages_kernel(KvView c, KvScratch s) {
-  const int64_t items = (int64_t)*s.njobs * c.n_layers * 2;
-  for (int64_t x = blockIdx.x; x < items; x += gridDim.x) {
-    const int32_t what = (int32_t)(x % (2 * c.n_layers));
-    const KvJob j = s.jobs[x / (2 * c.n_layers)];
-    char* base = (what & 1 ? c.v : c.k) + (what >> 1) * c.layer_stride;
-    for (int32_t y = threadIdx.x; y < j.tokens * c.heads * c.row16; y += blockDim.x) {
-      const int32_t piece = y % c.row16, t = y / c.row16 / c.heads, h = y / c.row16 % c.heads;
-      const int64_t at = t * c.token_stride + h * c.head_stride + piece * 16;
-      *(uint4*)(base + j.to * c.page_stride + at) = *(const uint4*)(base + j.from * c.page_stride + at);
+// The copies of the plan before it, in 16-byte pieces.  A warp takes 32 pieces of a page, one a lane, in `planes` of the
+// 2 * n_layers arrays (keys and values of each layer) and, where those are fewer than kCopies, further 32 pieces, so that
+// a lane has kCopies loads in flight whose places differ by strides alone.
+constexpr int kCopies = 8, kCopyThreads = 256, kCopyCtas = 4;
+struct PageShape {
+  FastDiv by_row, by_token;  // pieces of a head's values of a token, and of a token
+  int32_t planes_log;        // planes = 1 << planes_log <= kCopies
+};
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvView c, KvScratch s, PageShape g, int32_t moved) {
+  wait_for_plan();
+  // (Loads past the first cache: this launch may have shared its SM with the plan's.)
+  const int32_t njobs = __ldcg(s.njobs);
+  if (moved && !__ldcg(s.halt)) {  // the tables of a compaction
+    const int32_t live = __ldcg(s.live);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int32_t q = blockIdx.x * (kCopyThreads / 32) + warp; q < c.n_seqs; q += gridDim.x * (kCopyThreads / 32)) {
+      const int32_t len = length_of(c, q), used = len < 0 ? 0 : (int32_t)c.by_page.ceil(len);
+      if (len < 0 && lane == 0) atomicOr(s.err, KV_BAD_COUNT);
+      int32_t* row = row_of(c, q);
+      for (int32_t e = lane; e < used; e += 32) {
+        const int32_t page = __ldcg(row + e);
+        if ((uint32_t)page >= (uint32_t)c.n_pages)
+          atomicOr(s.err, KV_BAD_PAGE);
+        else if (page >= live)
+          row[e] = __ldcg(s.list + page);
+      }
     }
+  }
+  if (njobs == 0) return;
+  const int lane = threadIdx.x & 31;
+  const int32_t planes = 1 << g.planes_log, per_warp = 32 * (kCopies >> g.planes_log);
+  const int32_t chunks = (c.page * (int32_t)g.by_token.d + per_warp - 1) / per_warp, groups = (2 * c.n_layers + planes - 1) / planes;
+  const int64_t items = (int64_t)njobs * groups * chunks;
+  for (int64_t x = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); x < items; x += (int64_t)gridDim.x * (kCopyThreads / 32)) {
+    const int64_t job = x / ((int64_t)groups * chunks);
+    const int32_t rest = (int32_t)(x - job * groups * chunks), group = rest / chunks;
+    // (Turned from job to job: where pages are copied in part, no warp has their used beginnings alone.)
+    const int32_t chunk = (int32_t)((rest - group * chunks + job) % chunks);
+    const int4 j = __ldcg((const int4*)(s.jobs + job));  // from, to, tokens
+    const int64_t move = (int64_t)(j.y - j.x) * c.page_stride;
+    const int32_t pieces = j.z * (int32_t)g.by_token.d, plane0 = group << g.planes_log;
+    uint4 v[kCopies];
+    const auto at = [&](int k) -> char* {  // the k-th of the lane's pieces; NULL: none
+      const int32_t plane = plane0 + (k & (planes - 1)), z = chunk * per_warp + (k >> g.planes_log) * 32 + lane;
+      if (z >= pieces || plane >= 2 * c.n_layers) return nullptr;
+      const uint32_t t = g.by_token.div(z), in = z - t * g.by_token.d, h = g.by_row.div(in);
+      return (plane & 1 ? c.v : c.k) + (plane >> 1) * c.layer_stride + j.x * c.page_stride + t * c.token_stride + h * c.head_stride +
+             (in - h * g.by_row.d) * 16;
+    };
+#pragma unroll
+    for (int k = 0; k < kCopies; ++k)
+      if (const char* p = at(k)) v[k] = __ldcg((const uint4*)p);
+#pragma unroll
+    for (int k = 0; k < kCopies; ++k)
+      if (char* p = at(k)) __stcg((uint4*)(p + move), v[k]);
   }
 }
 
 // ---- write ------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float load_half(const void* p, int64_t i, int32_t type) {
-  return type == P2P_KV_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i]) : __half2float(((const __half*)p)[i]);
+// Where the tokens of a block go is found once, a lane a token, and serves all their heads in the layers and arrays that
+// the CTA writes.  Bound by the bytes read and written.
+constexpr int kBlock = 32, kWriteThreads = 256;
+
+// The last item that starts at or before token t (items without tokens share a start): every lane gets it.
+__device__ __forceinline__ int32_t find_item(const int64_t* offsets, int32_t n, int64_t t) {
+  const int lane = threadIdx.x & 31;
+  int32_t lo = 0, hi = n;
+  while (hi - lo > 1) {  // 32 probes a round
+    const int32_t step = (hi - lo + 31) / 32, at = lo + step * lane;
+    const uint32_t m = __ballot_sync(~0u, at < hi && __ldg(offsets + at) <= t);
+    if (!m) return lo;
+    const int32_t k = 31 - __clz(m);
+    lo = lo + step * k;
+    hi = min(hi, lo + step);
+  }
+  return lo;
 }
 
-// One 16-byte piece of a head's values of a token a thread.
-__global__ void __launch_bounds__(256) write_kernel(KvView c, KvScratch s, int32_t layer, int32_t n, const int32_t* __restrict__ seq,
-                                                    const int64_t* __restrict__ offsets, int64_t n_tokens, KvRows in) {
+// x / scale rounded to the nearest 32-bit value: the quotient by the rounded reciprocal, put right by its exact remainder
+// (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990), for scales of ordinary size; a
+// quotient that is above 448 by far stays as it is.
+__device__ __forceinline__ float divide(float x, float scale, float inverse) {
+  const float y = x * inverse, z = fmaf(fmaf(-y, scale, x), inverse, y);
+  return fabsf(y) < 65536.f ? z : y;
+}
+template <bool BF16>
+__device__ __forceinline__ float2 two_values(uint32_t x) {
+  return BF16 ? __bfloat1622float2(*(const __nv_bfloat162*)&x) : __half22float2(*(const __half2*)&x);
+}
+// Two values to 8 bits each, the first in the low ones.
+__device__ __forceinline__ uint32_t narrow(float2 v) {
+  return __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3);
+}
+template <bool BF16>
+__device__ __forceinline__ uint4 narrow16(const uint4& a, const uint4& b, float scale, float inverse, bool plain) {
+  const uint32_t in[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  uint32_t out[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float2 v = two_values<BF16>(in[2 * i]), w = two_values<BF16>(in[2 * i + 1]);
+    if (plain) {
+      v.x = divide(v.x, scale, inverse), v.y = divide(v.y, scale, inverse);
+      w.x = divide(w.x, scale, inverse), w.y = divide(w.y, scale, inverse);
+    } else {
+      v.x = __fdiv_rn(v.x, scale), v.y = __fdiv_rn(v.y, scale), w.x = __fdiv_rn(w.x, scale), w.y = __fdiv_rn(w.y, scale);
+    }
+    out[i] = narrow(v) | narrow(w) << 16;
+  }
+  return make_uint4(out[0], out[1], out[2], out[3]);
+}
+// Eight values from where they may lie on no 16-byte boundary.
+template <bool WIDE>
+__device__ __forceinline__ uint4 read8(const uint16_t* p) {
+  if constexpr (WIDE) {
+    return __ldcs((const uint4*)p);
+  } else {
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __ldg(p + 2 * i) | (uint32_t)__ldg(p + 2 * i + 1) << 16;
+    return make_uint4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+// KIND: the cache's type, BF16: that of the values given.  A CTA takes a block of tokens and `share` of the 2 * n_layers
+// arrays (keys and values of each layer).  by_token: 16-byte pieces of a token in one array, by_row: of a head.
+template <int KIND, bool BF16, bool WIDE>
+__global__ void __launch_bounds__(kWriteThreads)
+    write_kernel(KvView c, KvScratch s, int32_t layer, int32_t n_layers, int32_t share, int32_t n, const int32_t* __restrict__ seq,
+                 const int64_t* __restrict__ offsets, int64_t n_tokens, KvRows in, FastDiv by_token, FastDiv by_row) {
+  __shared__ int64_t place[kBlock];  // of a token, within its layer; -1: it is not written
   if (*s.halt) return;
-  const int32_t which = blockIdx.y & 1, l = blockIdx.y >> 1;
-  const void* src = which ? in.v : in.k;
-  char* dst = (which ? c.v : c.k) + (int64_t)(layer + l) * c.layer_stride;
-  const int64_t items = n_tokens * c.heads * c.row16;
-  for (int64_t x = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; x < items; x += (int64_t)gridDim.x * blockDim.x) {
-    const int32_t piece = (int32_t)(x % c.row16), h = (int32_t)(x / c.row16 % c.heads);
-    const int64_t t = x / c.row16 / c.heads;
-    // The last item that starts at or before t (items without tokens share a start).
-    int32_t lo = 0, hi = n;
+  const int64_t t0 = (int64_t)blockIdx.x * kBlock;
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int32_t i = threadIdx.x; i < n; i += kWriteThreads)
+      if (offsets[i] < 0 || offsets[i + 1] < offsets[i] || offsets[i + 1] > n_tokens) atomicOr(s.err, KV_BAD_OFFSETS);
+  if (threadIdx.x < kBlock) {
+    const int64_t t = t0 + threadIdx.x;
+    int32_t lo = find_item(offsets, n, t0), hi = min(n, find_item(offsets, n, t0 + kBlock - 1) + 1);
     while (hi - lo > 1) {
       const int32_t mid = (lo + hi) >> 1;
-      if (offsets[mid] <= t)
+      if (__ldg(offsets + mid) <= t)
         lo = mid;
       else
         hi = mid;
     }
+    int64_t at = -1;
     const int64_t o0 = offsets[lo], o1 = offsets[lo + 1];
-    if (o0 > t || o1 <= t) {
-      // Tokens outside [offsets[0], offsets[n]) belong to no sequence.
-      if (o0 < 0 || o1 > n_tokens || o1 < o0) atomicOr(s.err, KV_BAD_OFFSETS);
-      continue;
+    if (o0 >= 0 && o0 <= t && t < o1 && o1 <= n_tokens) {  // (else it belongs to no sequence)
+      const int32_t q = seq[lo], len = (uint32_t)q < (uint32_t)c.n_seqs ? length_of(c, q) : 0;
+      int32_t bad = 0;
+      if ((uint32_t)q >= (uint32_t)c.n_seqs) {
+        bad = KV_BAD_SEQ;
+      } else if (o1 - o0 > len) {
+        bad = KV_BAD_COUNT;
+      } else {
+        const int32_t pos = len - (int32_t)(o1 - t), e = (int32_t)c.by_page.div(pos), page = row_of(c, q)[e];
+        const int32_t refs = (uint32_t)page < (uint32_t)c.n_pages ? c.refs[page] : 0;
+        if (refs != 1)
+          bad = refs > 1 ? KV_SHARED : KV_BAD_PAGE;
+        else
+          at = page * c.page_stride + (pos - e * c.page) * c.token_stride;
+      }
+      if (bad) atomicOr(s.err, bad);
     }
-    const int32_t q = seq[lo];
-    if ((uint32_t)q >= (uint32_t)c.n_seqs) {
-      atomicOr(s.err, KV_BAD_SEQ);
-      continue;
+    place[threadIdx.x] = at;
+  }
+  __syncthreads();
+  const int32_t tokens = (int32_t)min((int64_t)kBlock, n_tokens - t0), a0 = blockIdx.y * share, a1 = min(a0 + share, 2 * n_layers);
+  const uint32_t all = tokens * by_token.d * (uint32_t)(a1 - a0);
+  constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8, kLoads = kValues / 8, kAhead = 4;  // pieces of a thread in flight
+  for (uint32_t y0 = threadIdx.x; y0 < all; y0 += kAhead * kWriteThreads) {
+    uint4 v[kAhead][kLoads];
+    char* to[kAhead];
+    float scale[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const uint32_t y = y0 + k * kWriteThreads, token_of = by_token.div(y), over = tokens == kBlock ? token_of / kBlock : token_of / tokens;
+      const uint32_t t = token_of - over * tokens, array = a0 + over, z = y - token_of * by_token.d, h = by_row.div(z), piece = z - h * by_row.d;
+      to[k] = nullptr;
+      const int64_t at = y < all ? place[t] : -1;
+      if (at >= 0) {
+        const int32_t l = array >> 1;
+        const uint16_t* from = (const uint16_t*)(array & 1 ? in.v : in.k) + l * in.layer_stride + (t0 + t) * in.token_stride + h * in.head_stride + piece * kValues;
+        to[k] = (array & 1 ? c.v : c.k) + (int64_t)(layer + l) * c.layer_stride + at + h * c.head_stride + piece * 16;
+#pragma unroll
+        for (int x = 0; x < kLoads; ++x) v[k][x] = read8<WIDE>(from + 8 * x);
+        if (KIND == P2P_KV_E4M3) scale[k] = __ldg((array & 1 ? c.v_scale : c.k_scale) + (layer + l) * c.heads + h);
+      }
     }
-    const int32_t len = length_of(c, q);
-    if (len < 0 || o0 < 0 || o1 > n_tokens || o1 - o0 > len) {
-      atomicOr(s.err, len < 0 || o1 - o0 > len ? KV_BAD_COUNT : KV_BAD_OFFSETS);
-      continue;
-    }
-    const int32_t pos = len - (int32_t)(o1 - t), e = (int32_t)c.by_page.div(pos), page = row_of(c, q)[e];
-    if ((uint32_t)page >= (uint32_t)c.n_pages) {
-      atomicOr(s.err, KV_BAD_PAGE);
-      continue;
-    }
-    if (c.refs[page] != 1) {
-      atomicOr(s.err, c.refs[page] > 1 ? KV_SHARED : KV_BAD_PAGE);
-      continue;
-    }
-    const int32_t per = c.type == P2P_KV_E4M3 ? 16 : 8;
-    const int64_t from = l * in.layer_stride + t * in.token_stride + h * in.head_stride + piece * per;
-    char* to = dst + page * c.page_stride + (pos - e * c.page) * c.token_stride + h * c.head_stride + piece * 16;
-    uint4 w;
-    if (c.type == P2P_KV_E4M3) {
-      const float scale = (which ? c.v_scale : c.k_scale)[(layer + l) * c.heads + h];
-      uint8_t* b = (uint8_t*)&w;
-      for (int i = 0; i < 16; ++i)
-        b[i] = __nv_cvt_float_to_fp8(__fdiv_rn(load_half(src, from + i, in.type), scale), __NV_SATFINITE, __NV_E4M3);
-    } else {
-      uint16_t* b = (uint16_t*)&w;
-      for (int i = 0; i < 8; ++i) b[i] = ((const uint16_t*)src)[from + i];
-    }
-    *(uint4*)to = w;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (to[k]) {
+        if (KIND == P2P_KV_E4M3) {
+          const bool plain = fabsf(scale[k]) > 0x1p-60f && fabsf(scale[k]) < 0x1p60f;
+          __stcs((uint4*)to[k], narrow16<BF16>(v[k][0], v[k][kLoads - 1], scale[k], __frcp_rn(scale[k]), plain));
+        } else {
+          __stcs((uint4*)to[k], v[k][0]);
+        }
+      }
   }
 }
 
@@ -384,50 +580,88 @@ __global__ void __launch_bounds__(256) stats_kernel(KvView c, unsigned long long
   if (tokens) atomicAdd(&out[3], tokens);
 }
 
-cudaError_t launch_copies(const KvView& c, const KvScratch& s, int num_sms, cudaStream_t st) {
-  copy_pages_kernel<<<8 * num_sms, 256, 0, st>>>(c, s);
+cudaError_t launch_copies(const KvView& c, const KvScratch& s, bool moved, int num_sms, cudaStream_t st) {
+  PageShape g;
+  g.by_row = FastDiv((uint32_t)c.row16);
+  g.by_token = FastDiv((uint32_t)(c.heads * c.row16));
+  g.planes_log = c.n_layers == 1 ? 1 : c.n_layers == 2 ? 2 : 3;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kCopyCtas * num_sms);
+  cfg.blockDim = dim3(kCopyThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, copy_pages_kernel, c, s, g, (int32_t)moved);
+}
+
+template <int KIND, bool BF16, bool WIDE>
+cudaError_t write_launch(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq,
+                         const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms, cudaStream_t st) {
+  const int64_t blocks = (n_tokens + kBlock - 1) / kBlock;
+  // All arrays of a block of tokens in one CTA where there are many blocks, else as few as fill the GPU.
+  const int64_t want = (8LL * num_sms + blocks - 1) / blocks;
+  // (A CTA's pieces are counted in 32 bits.)
+  const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / (kBlock * c.heads * c.row16));
+  const int32_t share = (int32_t)std::min(most, std::max<int64_t>(1, 2 * n_layers / std::min<int64_t>(want, 2 * n_layers)));
+  const dim3 grid((unsigned)blocks, (unsigned)((2 * n_layers + share - 1) / share));
+  write_kernel<KIND, BF16, WIDE><<<grid, kWriteThreads, 0, st>>>(c, s, layer, n_layers, share, n, seq, offsets, n_tokens, rows,
+                                                                 FastDiv((uint32_t)(c.heads * c.row16)), FastDiv((uint32_t)c.row16));
   return cudaGetLastError();
+}
+
+template <int KIND, bool BF16>
+cudaError_t write_wide(bool wide, const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq,
+                       const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms, cudaStream_t st) {
+  return wide ? write_launch<KIND, BF16, true>(c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st)
+              : write_launch<KIND, BF16, false>(c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st);
 }
 
 }  // namespace
 
+cudaError_t prepare_kv_pages() {
+  const int bytes = (int)item_bytes(kItems);
+  cudaError_t e = cudaFuncSetAttribute(extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(trim_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  return e;
+}
+
 cudaError_t launch_kv_extend(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* count, int num_sms,
                              cudaStream_t st) {
-  extend_kernel<<<1, kThreads, 0, st>>>(c, s, n, seq, count);
+  extend_kernel<<<kCluster, kThreads, item_bytes(n), st>>>(c, s, n, seq, count);
   const cudaError_t e = cudaGetLastError();
-  return e == cudaSuccess ? launch_copies(c, s, num_sms, st) : e;
+  return e == cudaSuccess ? launch_copies(c, s, false, num_sms, st) : e;
 }
 
 cudaError_t launch_kv_trim(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* to, cudaStream_t st) {
-  trim_kernel<<<1, kThreads, 0, st>>>(c, s, n, seq, to);
+  trim_kernel<<<kCluster, kThreads, item_bytes(n), st>>>(c, s, n, seq, to);
   return cudaGetLastError();
 }
 
 cudaError_t launch_kv_fork(const KvView& c, const KvScratch& s, int32_t n, const int32_t* src, const int32_t* dst,
                            const int32_t* tokens, cudaStream_t st) {
-  fork_kernel<<<1, kThreads, 0, st>>>(c, s, n, src, dst, tokens);
+  fork_kernel<<<kCluster, kThreads, item_bytes(n), st>>>(c, s, n, src, dst, tokens);
   return cudaGetLastError();
 }
 
 cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, cudaStream_t st) {
-  compact_kernel<<<1, kThreads, 0, st>>>(c, s);
+  compact_kernel<<<kCluster, kThreads, 0, st>>>(c, s);
   const cudaError_t e = cudaGetLastError();
-  return e == cudaSuccess ? launch_copies(c, s, num_sms, st) : e;
+  return e == cudaSuccess ? launch_copies(c, s, true, num_sms, st) : e;
 }
 
 cudaError_t launch_kv_write(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq,
                             const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms, cudaStream_t st) {
-  const int64_t items = n_tokens * c.heads * c.row16;
-  for (int32_t l = 0; l < n_layers; l += 16384) {  // (a grid has at most 65,535 blocks in y)
-    const int32_t m = n_layers - l < 16384 ? n_layers - l : 16384;
-    const int64_t blocks = (items + 255) / 256, most = (16LL * num_sms + 2 * m - 1) / (2 * m);
-    KvRows r = rows;
-    r.k = (const char*)rows.k + l * rows.layer_stride * 2;
-    r.v = (const char*)rows.v + l * rows.layer_stride * 2;
-    write_kernel<<<dim3((unsigned)(blocks < most ? blocks : most), 2 * m), 256, 0, st>>>(c, s, layer + l, n, seq, offsets, n_tokens, r);
-    if (const cudaError_t e = cudaGetLastError()) return e;
-  }
-  return cudaSuccess;
+  const bool wide = (uintptr_t)rows.k % 16 == 0 && (uintptr_t)rows.v % 16 == 0 && rows.layer_stride % 8 == 0 &&
+                    rows.token_stride % 8 == 0 && rows.head_stride % 8 == 0;
+  if (c.type != P2P_KV_E4M3)  // (16-bit values are stored as they are)
+    return write_wide<P2P_KV_BF16, true>(wide, c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st);
+  return rows.type == P2P_KV_BF16
+             ? write_wide<P2P_KV_E4M3, true>(wide, c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st)
+             : write_wide<P2P_KV_E4M3, false>(wide, c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st);
 }
 
 cudaError_t launch_kv_stats(const KvView& c, unsigned long long* out, int num_sms, cudaStream_t st) {
