@@ -91,7 +91,7 @@ struct KvQuery {
 };
 // Parts of rows that several CTAs share, and how many of a row's have arrived (by its first CTA; zero between launches).
 struct KvAttendScratch {
-  static constexpr int kCtasPerSm = 2;
+  static constexpr int kCtasPerSm = 3;
   float* parts;      // [kv_attend_parts()]
   int32_t* arrived;  // [kCtasPerSm * SMs]
   int32_t* err;

@@ -31,7 +31,7 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kRows = 16;               // tokens a warp takes at a time
 constexpr int kTile = kWarps * kRows;   // tokens of a unit
-constexpr int kOver = 1;                // units that a unit row counts for beyond its own
+constexpr int kOver = 4;                // units that a unit row counts for beyond its own
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -50,14 +50,17 @@ struct Type<P2P_KV_E4M3> {
   static constexpr int kSize = 1;
 };
 
-// Sizes of the kernel for values of KIND, head_dim padded to DP, NB blocks of eight query heads.
+// Sizes of the kernel for values of KIND, head_dim padded to DP (a multiple of 32), NB blocks of eight query heads.
 template <int KIND, int DP, int NB>
 struct Shape {
-  static constexpr int kRowBytes = DP * Type<KIND>::kSize;
+  static constexpr int kLaid = DP <= 64 ? 64 : DP <= 128 ? 128 : 256;  // values that a row in shared memory has room for
+  static constexpr int kRowBytes = kLaid * Type<KIND>::kSize;
   static constexpr int kPieces = kRowBytes / 16;               // 16-byte pieces of a row
   static constexpr int kArray = kRows * kRowBytes;             // keys (or values) of a warp's tile
   static constexpr int kStage = 2 * kArray;
-  static constexpr int kCtas = DP == 256 ? 1 : 2;  // resident on an SM
+  // Resident on an SM: by the room for two tiles or more a warp on their way, and where the tiles are small, so that a
+  // tile's products and softmax weigh more, by registers.
+  static constexpr int kCtas = DP > 128 ? 1 : kRowBytes <= 128 ? 3 : 2;
   static constexpr int kSums = 8 * DP * 4;                     // of a warp, for eight heads
   static constexpr int kFit = ((232448 / kCtas - 1024 - 512) / kWarps - kSums) / kStage;
   static constexpr int kStages = kFit < 8 ? kFit : 8;
@@ -216,7 +219,7 @@ struct Cursor {
 };
 
 template <int KIND, int DP, int NB>
-__global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
+__global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
   using S = Shape<KIND, DP, NB>;
   constexpr int PIECES = S::kPieces, KSTEPS = DP / 16;
   constexpr int LANES = PIECES, PER = 32 / LANES;  // lanes of a row, rows of a copy instruction
@@ -309,16 +312,32 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, K
     }
     const uint32_t to = tiles_at + to_slot * S::kStage;
     to_slot = to_slot + 1 < S::kStages ? to_slot + 1 : 0;
+    const int piece = lane % LANES, r0 = lane / LANES;
+    const int64_t o0 = __shfl_sync(~0u, offset, 0), o15 = __shfl_sync(~0u, offset, 15);
+    if (o0 >= 0 && o15 - o0 == 15 * c.token_stride && __shfl_sync(~0u, k.page, 0) == __shfl_sync(~0u, k.page, 15)) {
+      // All 16 tokens in one page: evenly apart.
+      const char* from = c.k + (o0 + r0 * c.token_stride + piece * 16);
+      const int64_t across = c.v - c.k, down = PER * c.token_stride;
+      const bool in = piece < c.row16;
+      if (!in) from = c.k;
 #pragma unroll
-    for (int y = 0; y < kRows / PER; ++y) {
-      const int r = y * PER + lane / LANES;
-      const int64_t o = __shfl_sync(~0u, offset, r);
-      const int piece = lane % LANES;
-      const bool in = o >= 0 && piece < c.row16;
-      const int64_t from = in ? o + piece * 16 : 0;
-      const uint32_t d = to + place<PIECES>(r, piece);
-      copy16(d, c.k + from, in);
-      copy16(d + S::kArray, c.v + from, in);
+      for (int y = 0; y < kRows / PER; ++y) {
+        const uint32_t d = to + place<PIECES>(y * PER + r0, piece);
+        copy16(d, from, in);
+        copy16(d + S::kArray, from + across, in);
+        if (in) from += down;
+      }
+    } else {
+#pragma unroll
+      for (int y = 0; y < kRows / PER; ++y) {
+        const int r = y * PER + r0;
+        const int64_t o = __shfl_sync(~0u, offset, r);
+        const bool in = o >= 0 && piece < c.row16;
+        const int64_t from = in ? o + piece * 16 : 0;
+        const uint32_t d = to + place<PIECES>(r, piece);
+        copy16(d, c.k + from, in);
+        copy16(d + S::kArray, c.v + from, in);
+      }
     }
     commit();
   };
@@ -438,10 +457,18 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(KvView c, KvQuery a, K
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          s[b][y] = lane / 4 + (y >> 1) * 8 < left ? s[b][y] * mul[b][y & 1] : -INFINITY;
-          past |= s[b][y] > top[b][y & 1] + kLag;
-        }
+        for (int y = 0; y < 4; ++y) s[b][y] *= mul[b][y & 1];
+      if (left < kRows) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            if (lane / 4 + (y >> 1) * 8 >= left) s[b][y] = -INFINITY;
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) past |= s[b][y] > top[b][y & 1] + kLag;
       if (__any_sync(~0u, past)) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -615,10 +642,10 @@ cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, 
   return cudaGetLastError();
 }
 
-// (Blocks of 16 query heads take 192 registers at DP = 256: blocks of eight, whose keys and values the second finds in L2.)
+// (Blocks of 16 query heads take 160 registers and more beyond DP = 128: blocks of eight, whose keys and values the second finds in L2.)
 template <int KIND, int DP>
 cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  if constexpr (DP == 256) {
+  if constexpr (DP > 128) {
     return launch<KIND, DP, 1>(c, q, w, num_sms, st);
   } else {
     if (!q) {
@@ -632,14 +659,16 @@ cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratc
 template <int KIND>
 cudaError_t launch_dim(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   return c.dim <= 64    ? launch_heads<KIND, 64>(c, q, w, num_sms, st)
+         : c.dim <= 96  ? launch_heads<KIND, 96>(c, q, w, num_sms, st)
          : c.dim <= 128 ? launch_heads<KIND, 128>(c, q, w, num_sms, st)
+         : c.dim <= 192 ? launch_heads<KIND, 192>(c, q, w, num_sms, st)
                         : launch_heads<KIND, 256>(c, q, w, num_sms, st);
 }
 
 }  // namespace
 
 size_t kv_attend_parts(int32_t dim, int num_sms) {
-  const int32_t dp = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
+  const int32_t dp = dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256;  // (as launch_dim)
   return (size_t)2 * KvAttendScratch::kCtasPerSm * num_sms * 16 * (dp + 2);
 }
 
