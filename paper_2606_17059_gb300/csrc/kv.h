@@ -36,6 +36,7 @@ struct KvView {
   int64_t layer_stride, page_stride, token_stride, head_stride;
   FastDiv by_page;
   int32_t row16;  // 16-byte pieces of a head's values of one token
+  int32_t side;   // log2 of the kv heads that a unit of the attention takes side by side
 };
 
 // Bits of the device error word.
@@ -96,7 +97,8 @@ struct KvAttendScratch {
   int32_t* arrived;  // [kCtasPerSm * SMs]
   int32_t* err;
 };
-size_t kv_attend_parts(int32_t dim, int num_sms);
+size_t kv_attend_parts(const KvView& c, int num_sms);
+int32_t kv_attend_side(const KvView& c);
 // With q = NULL it launches nothing, but makes the cache's kernels ready for launches (at creation).
 cudaError_t launch_kv_attend(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
 

@@ -30,7 +30,7 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kRows = 16;               // tokens a warp takes at a time
-constexpr int kTile = kWarps * kRows;   // tokens of a unit
+constexpr int kTile = kWarps * kRows;   // tokens that a CTA takes at a time, of one head
 constexpr int kOver = 4;                // units that a unit row counts for beyond its own
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
 constexpr float kLog2e = 1.4426950408889634f;
@@ -50,25 +50,24 @@ struct Type<P2P_KV_E4M3> {
   static constexpr int kSize = 1;
 };
 
-// Sizes of the kernel for values of KIND, head_dim padded to DP (a multiple of 32), NB blocks of eight query heads.
+// Sizes of the kernel for values of KIND, head_dim padded to DP, NB blocks of eight query heads.
 template <int KIND, int DP, int NB>
 struct Shape {
-  static constexpr int kLaid = DP <= 64 ? 64 : DP <= 128 ? 128 : 256;  // values that a row in shared memory has room for
-  static constexpr int kRowBytes = kLaid * Type<KIND>::kSize;
+  static constexpr int kRowBytes = DP * Type<KIND>::kSize;
   static constexpr int kPieces = kRowBytes / 16;               // 16-byte pieces of a row
+  static_assert(kPieces % 2 == 0, "a tile's pieces are whole turns of the warp");
   static constexpr int kArray = kRows * kRowBytes;             // keys (or values) of a warp's tile
   static constexpr int kStage = 2 * kArray;
   // Resident on an SM: by the room for two tiles or more a warp on their way, and where the tiles are small, so that a
   // tile's products and softmax weigh more, by registers.
-  static constexpr int kCtas = DP > 128 ? 1 : kRowBytes <= 128 ? 3 : 2;
-  static constexpr int kSums = 8 * DP * 4;                     // of a warp, for eight heads
+  static constexpr int kCtas = DP > 128 ? 1 : kRowBytes <= 160 ? 3 : 2;
+  static constexpr int kSumPitch = (DP + 31) / 32 * 32;
+  static constexpr int kSums = 8 * kSumPitch * 4;              // of a warp, for eight heads
   static constexpr int kFit = ((232448 / kCtas - 1024 - 512) / kWarps - kSums) / kStage;
   static constexpr int kStages = kFit < 8 ? kFit : 8;
   static constexpr int kRoom = kStages * kStage;               // a warp's tiles
   static constexpr int kBytes = (kRoom + kSums) * kWarps;      // of a CTA
   static constexpr int kHeads = 8 * NB;
-  // What a part leaves in scratch: kHeads rows of DP sums, then the maxima, then the sums of exp.
-  static constexpr int kPart = kHeads * (DP + 2);
   static_assert(kStages >= 3, "two tiles on their way");
 };
 
@@ -155,17 +154,20 @@ __device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_
 }
 
 // Byte offset in a warp's tile of piece `piece` of row `row`: the pieces of eight rows that ldmatrix reads together lie
-// in different banks.
+// in different banks (a turn by 1, 2 or all 3 low bits, as the rows' distance leaves them together).
 template <int PIECES>
 __device__ __forceinline__ uint32_t place(int row, int piece) {
-  const int turn = PIECES >= 8 ? row & 7 : (row >> 1) & 3;
+  const int turn = PIECES % 8 == 0 ? row & 7 : PIECES % 4 == 0 ? (row >> 1) & 3 : (row >> 2) & 1;
   return (uint32_t)(row * PIECES + (piece ^ turn)) * 16;
 }
 
+static_assert(kTile == 1 << 6, "Row::tiles");
 // A row of the batch: which tokens it sees.
 struct Row {
   int32_t seq, begin, end;
-  __device__ __forceinline__ int32_t tiles() const { return end > begin ? (end - begin - 1) / kTile + 1 : 1; }
+  __device__ __forceinline__ int32_t tiles(int32_t side) const {
+    return end > begin ? ((end - begin - 1) / kTile << side) + (((end - begin - 1) % kTile) >> (6 - side)) + 1 : 1;
+  }
 };
 __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t i, int32_t* err) {
   Row r = {i < a.n ? (a.seq ? __ldg(a.seq + i) : i) : 0, 0, 0};
@@ -190,7 +192,6 @@ struct Shared {
   int64_t before;  // units of the rows before `row` (over the kv heads and blocks of one)
   int32_t row, last;
   float top[kWarps][8], sum[kWarps][8];  // of the warps' parts, by head of a block
-  float base[16], total[16];
 };
 
 static_assert(sizeof(Shared) <= 512, "Shape counts on it");
@@ -198,7 +199,7 @@ static_assert(sizeof(Shared) <= 512, "Shape counts on it");
 // A place in a CTA's range: tile t of nt of the unit row (row i, kv head h, block of its query heads).
 struct Cursor {
   Row row, next;
-  int32_t i, h, block, t, nt;
+  int32_t i, h, block, t, nt;  // (h: the first of the unit's kv heads)
   int64_t left;  // units of the range from here on; none: at its end
   // k tiles on, none past the unit row's end.
   __device__ __forceinline__ void advance(int32_t k, const KvView& c, const KvQuery& a, int32_t blocks) {
@@ -209,11 +210,12 @@ struct Cursor {
     left -= kOver;
     if (++block < blocks) return;
     block = 0;
-    if (++h < c.heads) return;
+    h += 1 << c.side;
+    if (h < c.heads) return;
     h = 0;
     ++i;
     row = next;
-    nt = row.tiles();
+    nt = row.tiles(c.side);
     next = row_at(c, a, i + 1, nullptr);
   }
 };
@@ -222,19 +224,20 @@ template <int KIND, int DP, int NB>
 __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
   using S = Shape<KIND, DP, NB>;
   constexpr int PIECES = S::kPieces, KSTEPS = DP / 16;
-  constexpr int LANES = PIECES, PER = 32 / LANES;  // lanes of a row, rows of a copy instruction
   extern __shared__ __align__(128) char room[];
   __shared__ Shared sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t tiles_at = smem_of(room + warp * S::kRoom);
-  float* const sums = (float*)(room + kWarps * S::kRoom) + warp * 8 * DP;
+  float* const sums = (float*)(room + kWarps * S::kRoom) + warp * 8 * S::kSumPitch;
   const int32_t group = a.heads / c.heads, blocks = (group + S::kHeads - 1) / S::kHeads;
-  const int32_t per_row = c.heads * blocks;  // (kv head, block) pairs of a row
+  const int32_t per_row = (c.heads >> c.side) * blocks;  // unit rows of a row
+  const int32_t part_of_side = warp & ((1 << c.side) - 1), rank = warp >> c.side;  // the warp's kv head and tokens of a unit
+  const int32_t tile_log = 6 - c.side;
 
   // ---- this CTA's range of the units: a thread sums those of consecutive rows, the CTA scans the threads' sums.
   const int32_t each = (a.n + kThreads - 1) / kThreads, r0 = threadIdx.x * each;
   int64_t mine = 0;
-  for (int32_t i = r0; i < r0 + each && i < a.n; ++i) mine += row_at(c, a, i, blockIdx.x == 0 ? w.err : nullptr).tiles() + kOver;
+  for (int32_t i = r0; i < r0 + each && i < a.n; ++i) mine += row_at(c, a, i, blockIdx.x == 0 ? w.err : nullptr).tiles(c.side) + kOver;
   int64_t scan = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -258,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   if (at >= before && at < before + mine) {
     int32_t i = r0;
     for (;; ++i) {
-      const int32_t t = row_at(c, a, i, nullptr).tiles() + kOver;
+      const int32_t t = row_at(c, a, i, nullptr).tiles(c.side) + kOver;
       if (at < before + t) break;
       before += t;
     }
@@ -270,11 +273,11 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   here.i = sh.row;
   here.row = row_at(c, a, here.i, nullptr);
   here.next = row_at(c, a, here.i + 1, nullptr);
-  here.nt = here.row.tiles();
+  here.nt = here.row.tiles(c.side);
   {
     const int64_t in = x0 - sh.before * per_row;
     const int32_t units = here.nt + kOver, pair = (int32_t)(in / units), u = (int32_t)(in % units);
-    here.h = pair / blocks;
+    here.h = pair / blocks << c.side;
     here.block = pair % blocks;
     here.t = u > kOver ? u - kOver : 0;
     here.left = x_end - x0 - (u < kOver ? kOver - u : 0);
@@ -290,11 +293,11 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   const auto look_up = [&]() {
     Token k = {-1, 0};
     if (ahead.left > 0) {
-      const int64_t t = (int64_t)ahead.row.begin + (int64_t)ahead.t * kTile + warp * kRows + (lane & 15);
+      const int64_t t = (int64_t)ahead.row.begin + ((int64_t)ahead.t << tile_log) + rank * kRows + (lane & 15);
       if (t < ahead.row.end) {
         const uint32_t e = c.by_page.div((uint32_t)t);
         k.page = __ldg(c.table + (int64_t)ahead.row.seq * c.max_pages + e);
-        k.at = (int64_t)a.layer * c.layer_stride + ahead.h * c.head_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
+        k.at = (int64_t)a.layer * c.layer_stride + (ahead.h + part_of_side) * c.head_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
         if (k.page < 0) k.page = INT32_MAX;
       }
       ahead.advance(1, c, a, blocks);
@@ -312,25 +315,25 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     }
     const uint32_t to = tiles_at + to_slot * S::kStage;
     to_slot = to_slot + 1 < S::kStages ? to_slot + 1 : 0;
-    const int piece = lane % LANES, r0 = lane / LANES;
+    // The lane's y-th piece is the (lane + 32 y)-th of the tile.
     const int64_t o0 = __shfl_sync(~0u, offset, 0), o15 = __shfl_sync(~0u, offset, 15);
-    if (o0 >= 0 && o15 - o0 == 15 * c.token_stride && __shfl_sync(~0u, k.page, 0) == __shfl_sync(~0u, k.page, 15)) {
-      // All 16 tokens in one page: evenly apart.
-      const char* from = c.k + (o0 + r0 * c.token_stride + piece * 16);
-      const int64_t across = c.v - c.k, down = PER * c.token_stride;
-      const bool in = piece < c.row16;
-      if (!in) from = c.k;
+    const bool one_page = o0 >= 0 && o15 - o0 == 15 * c.token_stride && __shfl_sync(~0u, k.page, 0) == __shfl_sync(~0u, k.page, 15);
+    if (one_page) {  // all 16 tokens: evenly apart
+      const char* const base = c.k + o0;
+      const int64_t across = c.v - c.k;
 #pragma unroll
-      for (int y = 0; y < kRows / PER; ++y) {
-        const uint32_t d = to + place<PIECES>(y * PER + r0, piece);
+      for (int y = 0; y < PIECES / 2; ++y) {
+        const int z = lane + 32 * y, r = z / PIECES, piece = z % PIECES;
+        const bool in = piece < c.row16;
+        const char* from = in ? base + (r * c.token_stride + piece * 16) : c.k;
+        const uint32_t d = to + place<PIECES>(r, piece);
         copy16(d, from, in);
         copy16(d + S::kArray, from + across, in);
-        if (in) from += down;
       }
     } else {
 #pragma unroll
-      for (int y = 0; y < kRows / PER; ++y) {
-        const int r = y * PER + r0;
+      for (int y = 0; y < PIECES / 2; ++y) {
+        const int z = lane + 32 * y, r = z / PIECES, piece = z % PIECES;
         const int64_t o = __shfl_sync(~0u, offset, r);
         const bool in = o >= 0 && piece < c.row16;
         const int64_t from = in ? o + piece * 16 : 0;
@@ -353,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   uint32_t q[KSTEPS][NB][2];
   float mul[NB][2];  // logit (in log2) of a sum, for the heads 2 * (lane % 4) + {0, 1} of a block
   const auto load_queries = [&](const Cursor& u) {
-    const int32_t head0 = u.h * group + u.block * S::kHeads, heads = min(group - u.block * S::kHeads, S::kHeads);
+    const int32_t head0 = (u.h + part_of_side) * group + u.block * S::kHeads, heads = min(group - u.block * S::kHeads, S::kHeads);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int32_t head = b * 8 + lane / 4;
@@ -370,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     }
   };
   const auto use_queries = [&](const Cursor& u) {
-    float unit = a.scale * kLog2e * (KIND == P2P_KV_E4M3 ? __ldg(c.k_scale + a.layer * c.heads + u.h) : 1.f);
+    float unit = a.scale * kLog2e * (KIND == P2P_KV_E4M3 ? __ldg(c.k_scale + a.layer * c.heads + u.h + part_of_side) : 1.f);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       float mine = unit;
@@ -412,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     use_queries(here);
     const Cursor u = here;  // the unit row, from its tile u.t on
     const int32_t count = (int32_t)(u.nt - u.t < u.left ? u.nt - u.t : u.left);
-    const uint32_t first = (uint32_t)u.row.begin + (uint32_t)(u.t * kTile + warp * kRows);
+    const uint32_t first = (uint32_t)u.row.begin + ((uint32_t)u.t << tile_log) + rank * kRows;
     float o[KSTEPS][NB][4], top[NB][2], sum[NB][2];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -452,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
           for (int b = 0; b < NB; ++b) multiply<KIND>(s[b], f, q[k][b]);
         }
       }
-      const int32_t left = (int32_t)((uint32_t)u.row.end - (first + (uint32_t)j * kTile));  // tokens of the tile that are seen, if that is below 16
+      const int32_t left = (int32_t)((uint32_t)u.row.end - (first + ((uint32_t)j << tile_log)));  // tokens of the tile that are seen, if that is below 16
       bool past = false;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -530,12 +533,14 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     if (here.left > 0) load_queries(here);  // (on their way while this unit row's parts are joined)
 
     // ---- the four warps' parts, eight heads at a time through shared memory: [head][dim], turned by the head so that
-    // neither side's accesses meet a bank twice.
+    // neither side's accesses meet a bank twice (within 32 values, which the pitch is a multiple of).
     const int32_t head0 = u.h * group + u.block * S::kHeads, heads = min(group - u.block * S::kHeads, S::kHeads);
     const bool whole = u.t == 0 && count == u.nt, empty = u.row.end <= u.row.begin;
     const int64_t unit0 = x_end - u.left - u.t;  // where the unit row's first tile stands among all units
-    float* const part = w.parts + (int64_t)(blockIdx.x * 2 + (u.t == 0)) * S::kPart;
-    const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + u.h) : 1.f;
+    // A part: the sums [kv head of the unit][query head][dim], then the maxima, then the sums of exp.
+    const int32_t part_heads = S::kHeads << c.side;
+    const int64_t part_size = (int64_t)part_heads * (DP + 2);
+    float* const part = w.parts + (blockIdx.x * 2 + (u.t == 0)) * part_size;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       if (b * 8 >= heads) break;
@@ -550,32 +555,36 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
 #pragma unroll
         for (int k = 0; k < KSTEPS; ++k) {
           const int d = KIND == P2P_KV_E4M3 ? 16 * k + 2 * (lane / 4) : 16 * k + lane / 4;
-          sums[head * DP + (d ^ head * 4)] = o[k][b][y];
-          sums[head * DP + ((d + (KIND == P2P_KV_E4M3 ? 1 : 8)) ^ head * 4)] = o[k][b][y + 2];
+          sums[head * S::kSumPitch + (d ^ head * 4)] = o[k][b][y];
+          sums[head * S::kSumPitch + ((d + (KIND == P2P_KV_E4M3 ? 1 : 8)) ^ head * 4)] = o[k][b][y + 2];
         }
       }
       __syncthreads();
-      for (int y = threadIdx.x; y < 8 * DP / 4; y += kThreads) {
-        const int head = y / (DP / 4), d = y % (DP / 4) * 4, h8 = b * 8 + head;
+      for (int y = threadIdx.x; y < 8 * DP / 4 << c.side; y += kThreads) {
+        const int beside = y / (8 * DP / 4), head = y / (DP / 4) % 8, d = y % (DP / 4) * 4, h8 = b * 8 + head;
         float t = -INFINITY, z = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWarps; ++k) t = fmaxf(t, sh.top[k][head]);
+        for (int k = 0; k < kWarps; ++k)  // the warps that had this kv head
+          if ((k & ((1 << c.side) - 1)) == beside) t = fmaxf(t, sh.top[k][head]);
         const float ref = t == -INFINITY ? 0.f : t;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < kWarps; ++k) {
-          const float fade = exp2_fast(sh.top[k][head] - ref);
-          const float4 f = *(const float4*)((const float*)(room + kWarps * S::kRoom) + k * 8 * DP + head * DP + (d ^ head * 4));
-          z += fade * sh.sum[k][head];
-          v.x += fade * f.x, v.y += fade * f.y, v.z += fade * f.z, v.w += fade * f.w;
-        }
+        for (int k = 0; k < kWarps; ++k)
+          if ((k & ((1 << c.side) - 1)) == beside) {
+            const float fade = exp2_fast(sh.top[k][head] - ref);
+            const float4 f = *(const float4*)((const float*)(room + kWarps * S::kRoom) + (k * 8 + head) * S::kSumPitch + (d ^ head * 4));
+            z += fade * sh.sum[k][head];
+            v.x += fade * f.x, v.y += fade * f.y, v.z += fade * f.z, v.w += fade * f.w;
+          }
         if (!whole) {
-          *(float4*)(part + h8 * DP + d) = v;
-          if (d == 0) part[S::kHeads * DP + h8] = t, part[S::kHeads * (DP + 1) + h8] = z;
+          const int at = beside * S::kHeads + h8;
+          *(float4*)(part + at * DP + d) = v;
+          if (d == 0) part[part_heads * DP + at] = t, part[part_heads * (DP + 1) + at] = z;
         } else if (h8 < heads) {
-          const float f = v_scale / z;
-          store4(c, a, u.i, head0 + h8, d, v, f, empty);
-          if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + head0 + h8] = empty ? -INFINITY : (t + log2f(z)) / kLog2e;
+          const int32_t q_head = head0 + beside * group + h8;
+          const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + u.h + beside) : 1.f;
+          store4(c, a, u.i, q_head, d, v, v_scale / z, empty);
+          if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = empty ? -INFINITY : (t + log2f(z)) / kLog2e;
         }
       }
       if (whole || b + 1 < NB) __syncthreads();  // the sums' room is free again
@@ -595,36 +604,41 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     __threadfence();
     const int32_t parts = c1 - c0 + 1;
     const auto part_of = [&](int32_t k) {  // the first CTA's is its range's last unit row, the others' their first
-      return w.parts + (int64_t)((c0 + k) * 2 + (k == 0)) * S::kPart;
+      return w.parts + ((c0 + k) * 2 + (k == 0)) * part_size;
     };
-    for (int head = warp; head < heads; head += kWarps) {
+    float *const base = (float*)(room + kWarps * S::kRoom), *const sum_of = base + 64;  // (the sums' room, by head)
+    for (int y = warp; y < part_heads; y += kWarps) {
+      const int beside = y / S::kHeads, head = y % S::kHeads;
+      if (head >= heads) continue;
       float t = -INFINITY, z = 0.f;
-      for (int32_t k = lane; k < parts; k += 32) t = fmaxf(t, __ldcg(part_of(k) + S::kHeads * DP + head));
+      for (int32_t k = lane; k < parts; k += 32) t = fmaxf(t, __ldcg(part_of(k) + part_heads * DP + y));
 #pragma unroll
       for (int d = 16; d; d >>= 1) t = fmaxf(t, __shfl_xor_sync(~0u, t, d));
       const float ref = t == -INFINITY ? 0.f : t;
       for (int32_t k = lane; k < parts; k += 32)
-        z += exp2_fast(__ldcg(part_of(k) + S::kHeads * DP + head) - ref) * __ldcg(part_of(k) + S::kHeads * (DP + 1) + head);
+        z += exp2_fast(__ldcg(part_of(k) + part_heads * DP + y) - ref) * __ldcg(part_of(k) + part_heads * (DP + 1) + y);
 #pragma unroll
       for (int d = 16; d; d >>= 1) z += __shfl_xor_sync(~0u, z, d);
       if (lane == 0) {
-        sh.base[head] = ref;
-        sh.total[head] = z;
-        if (a.lse) a.lse[(int64_t)u.i * a.heads + head0 + head] = (t + log2f(z)) / kLog2e;
+        base[y] = ref;
+        sum_of[y] = z;
+        if (a.lse) a.lse[(int64_t)u.i * a.heads + head0 + beside * group + head] = (t + log2f(z)) / kLog2e;
       }
     }
     __syncthreads();
-    for (int y = threadIdx.x; y < heads * (DP / 4); y += kThreads) {
-      const int head = y / (DP / 4), d = y % (DP / 4) * 4;
+    for (int y = threadIdx.x; y < part_heads * (DP / 4); y += kThreads) {
+      const int at = y / (DP / 4), beside = at / S::kHeads, head = at % S::kHeads, d = y % (DP / 4) * 4;
+      if (head >= heads) continue;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
       for (int32_t k = 0; k < parts; ++k) {
         const float* p = part_of(k);
-        const float fade = exp2_fast(__ldcg(p + S::kHeads * DP + head) - sh.base[head]);
-        const float4 f = __ldcg((const float4*)(p + head * DP + d));
+        const float fade = exp2_fast(__ldcg(p + part_heads * DP + at) - base[at]);
+        const float4 f = __ldcg((const float4*)(p + at * DP + d));
         v.x += fade * f.x, v.y += fade * f.y, v.z += fade * f.z, v.w += fade * f.w;
       }
-      store4(c, a, u.i, head0 + head, d, v, v_scale / sh.total[head], false);
+      const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + u.h + beside) : 1.f;
+      store4(c, a, u.i, head0 + beside * group + head, d, v, v_scale / sum_of[at], false);
     }
     __syncthreads();
   }
@@ -658,7 +672,9 @@ cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratc
 
 template <int KIND>
 cudaError_t launch_dim(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+  constexpr int k80 = KIND == P2P_KV_E4M3 ? 96 : 80;  // (80 values of 8 bits are five pieces, not whole turns)
   return c.dim <= 64    ? launch_heads<KIND, 64>(c, q, w, num_sms, st)
+         : c.dim <= k80 ? launch_heads<KIND, k80>(c, q, w, num_sms, st)
          : c.dim <= 96  ? launch_heads<KIND, 96>(c, q, w, num_sms, st)
          : c.dim <= 128 ? launch_heads<KIND, 128>(c, q, w, num_sms, st)
          : c.dim <= 192 ? launch_heads<KIND, 192>(c, q, w, num_sms, st)
@@ -667,9 +683,18 @@ cudaError_t launch_dim(const KvView& c, const KvQuery* q, const KvAttendScratch&
 
 }  // namespace
 
-size_t kv_attend_parts(int32_t dim, int num_sms) {
-  const int32_t dp = dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256;  // (as launch_dim)
-  return (size_t)2 * KvAttendScratch::kCtasPerSm * num_sms * 16 * (dp + 2);
+size_t kv_attend_parts(const KvView& c, int num_sms) {
+  const int32_t dp = c.dim <= 64 ? 64 : c.dim <= 96 ? 96 : c.dim <= 128 ? 128 : c.dim <= 192 ? 192 : 256;  // (as launch_dim, or more)
+  const int32_t heads = dp > 128 ? 8 : 16;
+  return (size_t)2 * KvAttendScratch::kCtasPerSm * num_sms * (heads << c.side) * (dp + 2);
+}
+
+// Where a token's heads lie together, the rows of one head are pieces of lines and of pages of memory that other heads share (256 bytes and more
+// are read as fast alone):
+// the warps of a CTA take up to four neighbouring heads of the same tokens instead of four times the tokens.
+int32_t kv_attend_side(const KvView& c) {
+  if (c.head_stride > c.token_stride || c.row16 % 16 == 0) return 0;
+  return c.heads % 4 == 0 ? 2 : c.heads % 2 == 0 ? 1 : 0;
 }
 
 cudaError_t launch_kv_attend(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {

@@ -131,6 +131,7 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   c.head_stride = a.head_stride * es;
   c.by_page = p2p::FastDiv((uint32_t)a.page_tokens);
   c.row16 = (int32_t)(a.head_dim * es / 16);
+  c.side = p2p::kv_attend_side(c);
   // Scratch, each part on a 256-byte boundary.
   size_t at = 0;
   const auto part = [&at](size_t bytes) {
@@ -142,7 +143,7 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   const size_t words = part(256), claim = part(4 * S),
                arrived = part(sizeof(int32_t) * p2p::KvAttendScratch::kCtasPerSm * sms), zero = at, start = part(4 * (S + 1)), first = part(4 * S), cut = part(4 * S),
                list = part(4 * N), jobs = part(sizeof(p2p::KvJob) * std::max(S, N)),
-               parts = part(sizeof(float) * p2p::kv_attend_parts(a.head_dim, sms));
+               parts = part(sizeof(float) * p2p::kv_attend_parts(c, sms));
   cudaError_t e = cudaMalloc(&n->scratch, at);
   if (e == cudaSuccess) e = cudaMemset(n->scratch, 0, zero);
   if (e == cudaSuccess) e = p2p::prepare_kv_pages();
