@@ -90,11 +90,11 @@ struct KvQuery {
   // Whether rows of q may be read by twos, and those of out written by fours, of their values.
   bool q_pairs, out_fours;
 };
-// Parts of rows that several CTAs share, and how many of a row's have arrived (by its first CTA; zero between launches).
+// Parts of rows that several CTAs share, four a CTA (see the kernel), and how many have arrived (zero between launches).
 struct KvAttendScratch {
   static constexpr int kCtasPerSm = 3;
   float* parts;      // [kv_attend_parts()]
-  int32_t* arrived;  // [kCtasPerSm * SMs]
+  int32_t* arrived;  // [4 * kCtasPerSm * SMs]
   int32_t* err;
 };
 size_t kv_attend_parts(const KvView& c, int num_sms);

@@ -32,6 +32,7 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kRows = 16;               // tokens a warp takes at a time
 constexpr int kTile = kWarps * kRows;   // tokens that a CTA takes at a time, of one head
 constexpr int kOver = 4;                // units that a unit row counts for beyond its own
+constexpr int kJoin = 16;               // parts of a unit row that are read together
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -108,6 +109,11 @@ __device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ int32_t add_acq_rel(int32_t* p, int32_t x) {
+  int32_t y;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(y) : "l"(p), "r"(x) : "memory");
+  return y;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -540,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     // A part: the sums [kv head of the unit][query head][dim], then the maxima, then the sums of exp.
     const int32_t part_heads = S::kHeads << c.side;
     const int64_t part_size = (int64_t)part_heads * (DP + 2);
-    float* const part = w.parts + (blockIdx.x * 2 + (u.t == 0)) * part_size;
+    float* const part = w.parts + (blockIdx.x * 4 + (u.t == 0)) * part_size;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       if (b * 8 >= heads) break;
@@ -591,54 +597,102 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     }
     if (whole) continue;
 
-    // The CTA that brings the last part of the unit row joins them.
-    __threadfence();
-    __syncthreads();
+    // The CTA that brings the last part of the unit row joins them; where there are many, that of each `near` of them joins
+    // those, and the one that brings the last of the results joins these.  Each thread has four values of a head, over the
+    // parts in their order, kJoin of which are on their way at a time; with few values, groups of threads take every so
+    // many parts, and the first group puts theirs together.
     const int32_t c0 = (int32_t)(((unit0 + 1) * ctas - 1) / total), c1 = (int32_t)(((unit0 + u.nt) * ctas - 1) / total);
-    if (threadIdx.x == 0) {
-      sh.last = atomicAdd(w.arrived + c0, 1) == c1 - c0;
-      if (sh.last) w.arrived[c0] = 0;  // for the next launch
+    const int32_t parts = c1 - c0 + 1, all4 = (heads << c.side) * (DP / 4), turns = (all4 + kThreads - 1) / kThreads;
+    const int32_t teams = max(1, kThreads / all4);
+    int32_t near = parts;
+    if (parts * turns > 4 * kJoin * teams) {
+      near = kJoin * teams;
+      while (near * near < parts) near += kJoin * teams;
     }
-    __syncthreads();
-    if (!sh.last) continue;
-    __threadfence();
-    const int32_t parts = c1 - c0 + 1;
-    const auto part_of = [&](int32_t k) {  // the first CTA's is its range's last unit row, the others' their first
-      return w.parts + ((c0 + k) * 2 + (k == 0)) * part_size;
-    };
-    float *const base = (float*)(room + kWarps * S::kRoom), *const sum_of = base + 64;  // (the sums' room, by head)
-    for (int y = warp; y < part_heads; y += kWarps) {
-      const int beside = y / S::kHeads, head = y % S::kHeads;
-      if (head >= heads) continue;
-      float t = -INFINITY, z = 0.f;
-      for (int32_t k = lane; k < parts; k += 32) t = fmaxf(t, __ldcg(part_of(k) + part_heads * DP + y));
-#pragma unroll
-      for (int d = 16; d; d >>= 1) t = fmaxf(t, __shfl_xor_sync(~0u, t, d));
-      const float ref = t == -INFINITY ? 0.f : t;
-      for (int32_t k = lane; k < parts; k += 32)
-        z += exp2_fast(__ldcg(part_of(k) + part_heads * DP + y) - ref) * __ldcg(part_of(k) + part_heads * (DP + 1) + y);
-#pragma unroll
-      for (int d = 16; d; d >>= 1) z += __shfl_xor_sync(~0u, z, d);
-      if (lane == 0) {
-        base[y] = ref;
-        sum_of[y] = z;
-        if (a.lse) a.lse[(int64_t)u.i * a.heads + head0 + beside * group + head] = (t + log2f(z)) / kLog2e;
+    int32_t first_part = (blockIdx.x - c0) / near * near, members = min(near, parts - first_part);
+    for (int32_t level = 0;; ++level) {
+      // Part k lies with its CTA: the first CTA's is its range's last unit row, the others' their first.
+      const auto part_of = [&](int32_t k) { return w.parts + ((c0 + k) * 4 + (k == 0) + 2 * level) * part_size; };
+      const int32_t apart = level ? near : 1;
+      // (The count is read and raised after the barrier, in acquire and release order for all of the CTA's accesses.)
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        int32_t* const arrived = w.arrived + (c0 + first_part) * 4 + (first_part == 0) + 2 * level;
+        sh.last = add_acq_rel(arrived, 1) == members - 1;
+        if (sh.last) *arrived = 0;  // for the next launch
       }
-    }
-    __syncthreads();
-    for (int y = threadIdx.x; y < part_heads * (DP / 4); y += kThreads) {
-      const int at = y / (DP / 4), beside = at / S::kHeads, head = at % S::kHeads, d = y % (DP / 4) * 4;
-      if (head >= heads) continue;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (int32_t k = 0; k < parts; ++k) {
-        const float* p = part_of(k);
-        const float fade = exp2_fast(__ldcg(p + part_heads * DP + at) - base[at]);
-        const float4 f = __ldcg((const float4*)(p + at * DP + d));
-        v.x += fade * f.x, v.y += fade * f.y, v.z += fade * f.z, v.w += fade * f.w;
+      __syncthreads();
+      if (!sh.last) break;
+      const bool done = level == 1 || members == parts;
+      float* const joined = w.parts + ((c0 + first_part) * 4 + (first_part == 0) + 2) * part_size;
+      for (int y0 = 0; y0 < all4; y0 += kThreads) {
+        const int y = teams > 1 ? (int)threadIdx.x % all4 : y0 + (int)threadIdx.x, team = teams > 1 ? threadIdx.x / all4 : 0;
+        const int own = y / (DP / 4), beside = own / heads, head = own % heads, at = beside * S::kHeads + head, d = y % (DP / 4) * 4;
+        float t = -INFINITY, z = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (y < all4 && team < teams) {
+          for (int32_t k0 = team; k0 < members; k0 += teams * kJoin) {
+            float pt[kJoin], pz[kJoin];
+            float4 pv[kJoin];
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) {
+              const int32_t k = k0 + j * teams;
+              pt[j] = -INFINITY, pz[j] = 0.f, pv[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (k < members) {
+                const float* p = part_of(first_part + k * apart);
+                pt[j] = __ldcg(p + part_heads * DP + at);
+                pz[j] = __ldcg(p + part_heads * (DP + 1) + at);
+                pv[j] = __ldcg((const float4*)(p + at * DP + d));
+              }
+            }
+            float top1 = t;
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) top1 = fmaxf(top1, pt[j]);
+            const float ref = top1 == -INFINITY ? 0.f : top1;
+            const float fade = exp2_fast(t - ref);
+            t = top1;
+            z *= fade, v.x *= fade, v.y *= fade, v.z *= fade, v.w *= fade;
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) {
+              const float f = exp2_fast(pt[j] - ref);
+              z += f * pz[j], v.x += f * pv[j].x, v.y += f * pv[j].y, v.z += f * pv[j].z, v.w += f * pv[j].w;
+            }
+          }
+        }
+        if (teams > 1) {
+          float* const mine = (float*)(room + kWarps * S::kRoom) + threadIdx.x * 8;  // (the sums' room)
+          mine[0] = t, mine[1] = z;
+          *(float4*)(mine + 4) = v;
+          __syncthreads();
+          if (team == 0) {
+            float top1 = t;
+            for (int k = 1; k < teams; ++k) top1 = fmaxf(top1, mine[8 * k * all4]);
+            const float ref = top1 == -INFINITY ? 0.f : top1;
+            float fade = exp2_fast(t - ref);
+            t = top1;
+            z *= fade, v.x *= fade, v.y *= fade, v.z *= fade, v.w *= fade;
+            for (int k = 1; k < teams; ++k) {
+              const float* p = mine + 8 * k * all4;
+              fade = exp2_fast(p[0] - ref);
+              z += fade * p[1], v.x += fade * p[4], v.y += fade * p[5], v.z += fade * p[6], v.w += fade * p[7];
+            }
+          }
+        }
+        if (y < all4 && team == 0) {
+          if (done) {
+            const int32_t q_head = head0 + beside * group + head;
+            const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + u.h + beside) : 1.f;
+            store4(c, a, u.i, q_head, d, v, v_scale / z, false);
+            if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = (t + log2f(z)) / kLog2e;
+          } else {
+            *(float4*)(joined + at * DP + d) = v;
+            if (d == 0) joined[part_heads * DP + at] = t, joined[part_heads * (DP + 1) + at] = z;
+          }
+        }
       }
-      const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + u.h + beside) : 1.f;
-      store4(c, a, u.i, head0 + beside * group + head, d, v, v_scale / sum_of[at], false);
+      if (done) break;
+      first_part = 0;
+      members = (parts + near - 1) / near;
     }
     __syncthreads();
   }
@@ -686,7 +740,7 @@ cudaError_t launch_dim(const KvView& c, const KvQuery* q, const KvAttendScratch&
 size_t kv_attend_parts(const KvView& c, int num_sms) {
   const int32_t dp = c.dim <= 64 ? 64 : c.dim <= 96 ? 96 : c.dim <= 128 ? 128 : c.dim <= 192 ? 192 : 256;  // (as launch_dim, or more)
   const int32_t heads = dp > 128 ? 8 : 16;
-  return (size_t)2 * KvAttendScratch::kCtasPerSm * num_sms * (heads << c.side) * (dp + 2);
+  return (size_t)4 * KvAttendScratch::kCtasPerSm * num_sms * (heads << c.side) * (dp + 2);
 }
 
 // Where a token's heads lie together, the rows of one head are pieces of lines and of pages of memory that other heads share (256 bytes and more

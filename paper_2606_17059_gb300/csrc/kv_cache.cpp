@@ -141,7 +141,7 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   };
   const size_t S = (size_t)a.n_seqs, N = (size_t)a.n_pages;
   const size_t words = part(256), claim = part(4 * S),
-               arrived = part(sizeof(int32_t) * p2p::KvAttendScratch::kCtasPerSm * sms), zero = at, start = part(4 * (S + 1)), first = part(4 * S), cut = part(4 * S),
+               arrived = part(sizeof(int32_t) * 4 * p2p::KvAttendScratch::kCtasPerSm * sms), zero = at, start = part(4 * (S + 1)), first = part(4 * S), cut = part(4 * S),
                list = part(4 * N), jobs = part(sizeof(p2p::KvJob) * std::max(S, N)),
                parts = part(sizeof(float) * p2p::kv_attend_parts(c, sms));
   cudaError_t e = cudaMalloc(&n->scratch, at);
