@@ -97,9 +97,14 @@ struct KvAttendScratch {
   int32_t* arrived;  // [4 * kCtasPerSm * SMs]
   int32_t* err;
 };
-size_t kv_attend_parts(const KvView& c, int num_sms);
-int32_t kv_attend_side(const KvView& c);
-// With q = NULL it launches nothing, but makes the cache's kernels ready for launches (at creation).
-cudaError_t launch_kv_attend(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
+// Floats of `parts`: head_dim as the kernels pad it, at most, and blocks of 8 or 16 query heads of up to 4 kv heads.
+inline size_t kv_attend_parts(const KvView& c, int num_sms) {
+  const int32_t dp = c.dim <= 64 ? 64 : c.dim <= 96 ? 96 : c.dim <= 128 ? 128 : c.dim <= 192 ? 192 : 256, heads = dp > 128 ? 8 : 16;
+  return (size_t)4 * KvAttendScratch::kCtasPerSm * num_sms * (heads << c.side) * (dp + 2);
+}
+// With q = NULL they launch nothing, but make the cache's kernels ready for launches (at creation).
+cudaError_t launch_kv_attend_bf16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_attend_f16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_attend_e4m3(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
 
 }  // namespace p2p

@@ -1,4 +1,4 @@
-// kv_attend.cu -- attention of one new token a sequence over the paged key-value cache (p2p_kv_attend).
+// kv_attend.cuh -- attention of one new token a sequence over the paged key-value cache (p2p_kv_attend).
 //
 // For a query head and the tokens t that it sees: x_t = scale * q . k_t, m = max x_t, z = sum exp(x_t - m), out = sum
 // exp(x_t - m) v_t / z, lse = m + ln z; without a token, out = 0 and lse = -inf.
@@ -19,6 +19,7 @@
 // so that eight query heads fill a product's n and the 16 tokens its m.  P^T goes from the first product's layout to the
 // second's by two 8 x 8 transposes of registers.  exp(x - m) takes for m not the running maximum but one that lags
 // it by at most a factor of 2^8, so that a tile's maximum is only reduced, and O rescaled, where it goes past that.
+#pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -29,8 +30,6 @@ namespace p2p {
 namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kRows = 16;               // tokens a warp takes at a time
-constexpr int kTile = kWarps * kRows;   // tokens that a CTA takes at a time, of one head
 constexpr int kOver = 4;                // units that a unit row counts for beyond its own
 constexpr int kJoin = 16;               // parts of a unit row that are read together
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
@@ -57,19 +56,23 @@ struct Shape {
   static constexpr int kRowBytes = DP * Type<KIND>::kSize;
   static constexpr int kPieces = kRowBytes / 16;               // 16-byte pieces of a row
   static_assert(kPieces % 2 == 0, "a tile's pieces are whole turns of the warp");
+  // Tokens that a warp takes at a time: 32 of small rows, whose products weigh little beside what a turn of the loop costs
+  // (256 sequences of 8-bit values of 64: 83 us with 16, 65 with 32).
+  static constexpr int kRows = kRowBytes <= 128 ? 32 : 16;
+  static constexpr int kTileLog = kRows == 32 ? 7 : 6;         // (log2) that a CTA takes at a time, of one head
+  static_assert(kWarps * kRows == 1 << kTileLog);
   static constexpr int kArray = kRows * kRowBytes;             // keys (or values) of a warp's tile
   static constexpr int kStage = 2 * kArray;
-  // Resident on an SM: by the room for two tiles or more a warp on their way, and where the tiles are small, so that a
-  // tile's products and softmax weigh more, by registers.
-  static constexpr int kCtas = DP > 128 ? 1 : kRowBytes <= 160 ? 3 : 2;
-  static constexpr int kSumPitch = (DP + 31) / 32 * 32;
-  static constexpr int kSums = 8 * kSumPitch * 4;              // of a warp, for eight heads
-  static constexpr int kFit = ((232448 / kCtas - 1024 - 512) / kWarps - kSums) / kStage;
+  // Resident on an SM: three where three have room for more than two tiles a warp, one where two have not.
+  static constexpr int kCtas = kRows * kRowBytes <= 3072 ? 3 : kRowBytes <= 256 ? 2 : 1;
+  static constexpr int kSumPitch = (DP + 31) / 32 * 32;        // of a head's sums, which lie in the room of a tile
+  static_assert(8 * kSumPitch * 4 <= kStage);
+  static constexpr int kFit = (232448 / kCtas - 1024 - 512) / kWarps / kStage;
   static constexpr int kStages = kFit < 8 ? kFit : 8;
   static constexpr int kRoom = kStages * kStage;               // a warp's tiles
-  static constexpr int kBytes = (kRoom + kSums) * kWarps;      // of a CTA
+  static constexpr int kBytes = kRoom * kWarps;                // of a CTA
   static constexpr int kHeads = 8 * NB;
-  static_assert(kStages >= 3, "two tiles on their way");
+  static_assert(kStages >= 2, "a tile on its way");
 };
 
 __device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -167,16 +170,15 @@ __device__ __forceinline__ uint32_t place(int row, int piece) {
   return (uint32_t)(row * PIECES + (piece ^ turn)) * 16;
 }
 
-static_assert(kTile == 1 << 6, "Row::tiles");
-// A row of the batch: which tokens it sees.
+// A row of the batch: it sees tokens begin .. end of its sequence; tiles are counted from `from`.
 struct Row {
-  int32_t seq, begin, end;
-  __device__ __forceinline__ int32_t tiles(int32_t side) const {
-    return end > begin ? ((end - begin - 1) / kTile << side) + (((end - begin - 1) % kTile) >> (6 - side)) + 1 : 1;
-  }
+  int32_t seq, from, begin, end;
+  // Units of 1 << tile_log tokens (one without any).
+  __device__ __forceinline__ int32_t tiles(int32_t tile_log) const { return end > begin ? ((end - from - 1) >> tile_log) + 1 : 1; }
 };
+template <bool WHOLE>
 __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t i, int32_t* err) {
-  Row r = {i < a.n ? (a.seq ? __ldg(a.seq + i) : i) : 0, 0, 0};
+  Row r = {i < a.n ? (a.seq ? __ldg(a.seq + i) : i) : 0, 0, 0, 0};
   if (i >= a.n) return r;
   if ((uint32_t)r.seq >= (uint32_t)c.n_seqs) {
     if (err) atomicOr(err, KV_BAD_SEQ);
@@ -190,6 +192,7 @@ __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t
   }
   r.end = len;
   r.begin = a.window && len > a.window ? len - a.window : 0;
+  r.from = WHOLE ? r.begin / 16 * 16 : r.begin;
   return r;
 }
 
@@ -208,7 +211,8 @@ struct Cursor {
   int32_t i, h, block, t, nt;  // (h: the first of the unit's kv heads)
   int64_t left;  // units of the range from here on; none: at its end
   // k tiles on, none past the unit row's end.
-  __device__ __forceinline__ void advance(int32_t k, const KvView& c, const KvQuery& a, int32_t blocks) {
+  template <bool WHOLE>
+  __device__ __forceinline__ void advance(int32_t k, const KvView& c, const KvQuery& a, int32_t blocks, int32_t tile_log) {
     t += k;
     left -= k;
     if (t < nt) return;
@@ -221,12 +225,13 @@ struct Cursor {
     h = 0;
     ++i;
     row = next;
-    nt = row.tiles(c.side);
-    next = row_at(c, a, i + 1, nullptr);
+    nt = row.tiles(tile_log);
+    next = row_at<WHOLE>(c, a, i + 1, nullptr);
   }
 };
 
-template <int KIND, int DP, int NB>
+// WHOLE: pages are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly apart.
+template <int KIND, int DP, int NB, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
   using S = Shape<KIND, DP, NB>;
   constexpr int PIECES = S::kPieces, KSTEPS = DP / 16;
@@ -234,16 +239,15 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   __shared__ Shared sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t tiles_at = smem_of(room + warp * S::kRoom);
-  float* const sums = (float*)(room + kWarps * S::kRoom) + warp * 8 * S::kSumPitch;
   const int32_t group = a.heads / c.heads, blocks = (group + S::kHeads - 1) / S::kHeads;
   const int32_t per_row = (c.heads >> c.side) * blocks;  // unit rows of a row
   const int32_t part_of_side = warp & ((1 << c.side) - 1), rank = warp >> c.side;  // the warp's kv head and tokens of a unit
-  const int32_t tile_log = 6 - c.side;
+  const int32_t tile_log = S::kTileLog - c.side;
 
   // ---- this CTA's range of the units: a thread sums those of consecutive rows, the CTA scans the threads' sums.
   const int32_t each = (a.n + kThreads - 1) / kThreads, r0 = threadIdx.x * each;
   int64_t mine = 0;
-  for (int32_t i = r0; i < r0 + each && i < a.n; ++i) mine += row_at(c, a, i, blockIdx.x == 0 ? w.err : nullptr).tiles(c.side) + kOver;
+  for (int32_t i = r0; i < r0 + each && i < a.n; ++i) mine += row_at<WHOLE>(c, a, i, blockIdx.x == 0 ? w.err : nullptr).tiles(tile_log) + kOver;
   int64_t scan = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -267,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   if (at >= before && at < before + mine) {
     int32_t i = r0;
     for (;; ++i) {
-      const int32_t t = row_at(c, a, i, nullptr).tiles(c.side) + kOver;
+      const int32_t t = row_at<WHOLE>(c, a, i, nullptr).tiles(tile_log) + kOver;
       if (at < before + t) break;
       before += t;
     }
@@ -277,9 +281,9 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   __syncthreads();
   Cursor here;  // what is computed
   here.i = sh.row;
-  here.row = row_at(c, a, here.i, nullptr);
-  here.next = row_at(c, a, here.i + 1, nullptr);
-  here.nt = here.row.tiles(c.side);
+  here.row = row_at<WHOLE>(c, a, here.i, nullptr);
+  here.next = row_at<WHOLE>(c, a, here.i + 1, nullptr);
+  here.nt = here.row.tiles(tile_log);
   {
     const int64_t in = x0 - sh.before * per_row;
     const int32_t units = here.nt + kOver, pair = (int32_t)(in / units), u = (int32_t)(in % units);
@@ -289,9 +293,59 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     here.left = x_end - x0 - (u < kOver ? kOver - u : 0);
   }
 
-  // ---- copies of the warp's tiles, in the order of the range.  Lanes 0 .. 15 look up a token each: its page, and where
-  // it lies but for that (page < 0: no token).
-  Cursor ahead = here;  // what is looked up
+  // ---- copies of the warp's tiles, in the order of the range.
+  Cursor ahead = here;  // what is copied next, or, token by token, looked up next
+  int32_t to_slot = 0;
+  const auto next_slot = [&]() {
+    const uint32_t to = tiles_at + to_slot * S::kStage;
+    to_slot = to_slot + 1 < S::kStages ? to_slot + 1 : 0;
+    return to;
+  };
+  const int64_t across = c.v - c.k, layer_at = (int64_t)a.layer * c.layer_stride + part_of_side * c.head_stride;
+  // WHOLE: lane l has where the sixteens of tile near_t + l of row near_i lie (< 0: none); the kv heads of a row share them.
+  constexpr int SIXTEENS = S::kRows / 16;
+  int64_t near[SIXTEENS];
+  int32_t near_i = -1, near_t = 0;
+  const auto step_whole = [&]() {
+    if (ahead.left > 0) {
+      if (ahead.i != near_i || (uint32_t)(ahead.t - near_t) >= 32u) {
+        near_i = ahead.i, near_t = ahead.t;
+#pragma unroll
+        for (int m = 0; m < SIXTEENS; ++m) {
+          const int64_t t = (int64_t)ahead.row.from + ((int64_t)(near_t + lane) << tile_log) + rank * S::kRows + 16 * m;
+          near[m] = -1;
+          if (t < ahead.row.end) {
+            const uint32_t e = c.by_page.div((uint32_t)t);
+            const int32_t page = __ldg(c.table + (int64_t)ahead.row.seq * c.max_pages + e);
+            if ((uint32_t)page < (uint32_t)c.n_pages)
+              near[m] = page * c.page_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
+            else
+              atomicOr(w.err, KV_BAD_PAGE);
+          }
+        }
+      }
+      const uint32_t to = next_slot();
+      const int64_t t0 = (int64_t)ahead.row.from + ((int64_t)ahead.t << tile_log) + rank * S::kRows;
+      const int32_t lo = (int32_t)max(ahead.row.begin - t0, (int64_t)0), n = (int32_t)(min(ahead.row.end - t0, (int64_t)S::kRows) - lo);  // rows lo .. lo + n - 1
+#pragma unroll
+      for (int m = 0; m < SIXTEENS; ++m) {
+        const int64_t o = __shfl_sync(~0u, near[m], ahead.t - near_t);
+        const char* const base = c.k + (layer_at + ahead.h * c.head_stride + o);
+#pragma unroll
+        for (int y = 0; y < PIECES / 2; ++y) {  // the lane's y-th piece is the (lane + 32 y)-th of sixteen tokens'
+          const int z = lane + 32 * y, r = z / PIECES, piece = z % PIECES;
+          const bool in = o >= 0 && piece < c.row16 && 16 * m + r >= lo && 16 * m + r < lo + n;
+          const char* from = in ? base + (r * c.token_stride + piece * 16) : c.k;
+          const uint32_t d = to + m * 16 * S::kRowBytes + place<PIECES>(r, piece);
+          copy16(d, from, in);
+          copy16(d + S::kArray, from + across, in);
+        }
+      }
+      ahead.advance<WHOLE>(1, c, a, blocks, tile_log);
+    }
+    commit();
+  };
+  // Otherwise a lane looks up a token: its page, and where it lies but for that (page < 0: no token), two tiles ahead.
   struct Token {
     int32_t page;
     int64_t at;
@@ -299,63 +353,49 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   const auto look_up = [&]() {
     Token k = {-1, 0};
     if (ahead.left > 0) {
-      const int64_t t = (int64_t)ahead.row.begin + ((int64_t)ahead.t << tile_log) + rank * kRows + (lane & 15);
+      const int64_t t = (int64_t)ahead.row.from + ((int64_t)ahead.t << tile_log) + rank * S::kRows + (lane & (S::kRows - 1));
       if (t < ahead.row.end) {
         const uint32_t e = c.by_page.div((uint32_t)t);
         k.page = __ldg(c.table + (int64_t)ahead.row.seq * c.max_pages + e);
-        k.at = (int64_t)a.layer * c.layer_stride + (ahead.h + part_of_side) * c.head_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
+        k.at = layer_at + ahead.h * c.head_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
         if (k.page < 0) k.page = INT32_MAX;
       }
-      ahead.advance(1, c, a, blocks);
+      ahead.advance<WHOLE>(1, c, a, blocks, tile_log);
     }
     return k;
   };
-  int32_t to_slot = 0;
-  const auto copy = [&](const Token& k) {
-    int64_t offset = -1;
-    if (k.page >= 0) {
-      if (k.page < c.n_pages)
-        offset = k.at + k.page * c.page_stride;
-      else
-        atomicOr(w.err, KV_BAD_PAGE);
-    }
-    const uint32_t to = tiles_at + to_slot * S::kStage;
-    to_slot = to_slot + 1 < S::kStages ? to_slot + 1 : 0;
-    // The lane's y-th piece is the (lane + 32 y)-th of the tile.
-    const int64_t o0 = __shfl_sync(~0u, offset, 0), o15 = __shfl_sync(~0u, offset, 15);
-    const bool one_page = o0 >= 0 && o15 - o0 == 15 * c.token_stride && __shfl_sync(~0u, k.page, 0) == __shfl_sync(~0u, k.page, 15);
-    if (one_page) {  // all 16 tokens: evenly apart
-      const char* const base = c.k + o0;
-      const int64_t across = c.v - c.k;
+  Token soon = {-1, 0}, later = {-1, 0};
+  const auto step = [&]() {
+    if constexpr (WHOLE) {
+      step_whole();
+    } else {
+      int64_t offset = -1;
+      if (soon.page >= 0) {
+        if (soon.page < c.n_pages)
+          offset = soon.at + soon.page * c.page_stride;
+        else
+          atomicOr(w.err, KV_BAD_PAGE);
+      }
+      const uint32_t to = next_slot();
 #pragma unroll
-      for (int y = 0; y < PIECES / 2; ++y) {
+      for (int y = 0; y < S::kRows * PIECES / 32; ++y) {
         const int z = lane + 32 * y, r = z / PIECES, piece = z % PIECES;
-        const bool in = piece < c.row16;
-        const char* from = in ? base + (r * c.token_stride + piece * 16) : c.k;
+        const int64_t o = __shfl_sync(~0u, offset, r);
+        const bool in = o >= 0 && piece < c.row16;
+        const char* from = c.k + (in ? o + piece * 16 : 0);
         const uint32_t d = to + place<PIECES>(r, piece);
         copy16(d, from, in);
         copy16(d + S::kArray, from + across, in);
       }
-    } else {
-#pragma unroll
-      for (int y = 0; y < PIECES / 2; ++y) {
-        const int z = lane + 32 * y, r = z / PIECES, piece = z % PIECES;
-        const int64_t o = __shfl_sync(~0u, offset, r);
-        const bool in = o >= 0 && piece < c.row16;
-        const int64_t from = in ? o + piece * 16 : 0;
-        const uint32_t d = to + place<PIECES>(r, piece);
-        copy16(d, c.k + from, in);
-        copy16(d + S::kArray, c.v + from, in);
-      }
+      commit();
+      soon = later;
+      later = look_up();
     }
-    commit();
   };
-  Token soon = look_up(), later = look_up();
-  const auto step = [&]() {
-    copy(soon);
-    soon = later;
+  if constexpr (!WHOLE) {
+    soon = look_up();
     later = look_up();
-  };
+  }
 
   // ---- the queries, as the second operand of the first product: lane holds head lane / 4 of each block of eight.
   // (With 8-bit values a piece of 16 is 16 of the product's k, in the order that their bytes come to a lane.)
@@ -421,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     use_queries(here);
     const Cursor u = here;  // the unit row, from its tile u.t on
     const int32_t count = (int32_t)(u.nt - u.t < u.left ? u.nt - u.t : u.left);
-    const uint32_t first = (uint32_t)u.row.begin + ((uint32_t)u.t << tile_log) + rank * kRows;
+    const uint32_t first = (uint32_t)u.row.from + ((uint32_t)u.t << tile_log) + rank * S::kRows;
     float o[KSTEPS][NB][4], top[NB][2], sum[NB][2];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -439,51 +479,65 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
       const uint32_t keys = tiles_at + slot * S::kStage, values = keys + S::kArray;
       slot = slot + 1 < S::kStages ? slot + 1 : 0;
 
-      float s[NB][4] = {};  // tokens lane / 4 (+ 8 in 2, 3), heads 2 * (lane % 4) + {0, 1}
-      if (KIND == P2P_KV_E4M3) {
+      constexpr int MB = S::kRows / 16;
+      float s[MB][NB][4] = {};  // of each sixteen: tokens lane / 4 (+ 8 in 2, 3), heads 2 * (lane % 4) + {0, 1}
 #pragma unroll
-        for (int k = 0; k < KSTEPS; k += 2) {
-          uint32_t r[4];  // tokens 0-7 and 8-15 of piece k, then of piece k + 1
-          load4(r, keys + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, k + (lane >> 4)));
+      for (int m = 0; m < MB; ++m) {
+        const uint32_t keys16 = keys + m * 16 * S::kRowBytes;
+        if (KIND == P2P_KV_E4M3) {
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const uint32_t f[4] = {widen(r[2 * y]), widen(r[2 * y + 1]), widen_high(r[2 * y]), widen_high(r[2 * y + 1])};
+          for (int k = 0; k < KSTEPS; k += 2) {
+            uint32_t r[4];  // tokens 0-7 and 8-15 of piece k, then of piece k + 1
+            load4(r, keys16 + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, k + (lane >> 4)));
 #pragma unroll
-            for (int b = 0; b < NB; ++b) multiply<KIND>(s[b], f, q[k + y][b]);
+            for (int y = 0; y < 2; ++y) {
+              const uint32_t f[4] = {widen(r[2 * y]), widen(r[2 * y + 1]), widen_high(r[2 * y]), widen_high(r[2 * y + 1])};
+#pragma unroll
+              for (int b = 0; b < NB; ++b) multiply<KIND>(s[m][b], f, q[k + y][b]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < KSTEPS; ++k) {
+            uint32_t f[4];
+            load4(f, keys16 + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, 2 * k + (lane >> 4)));
+#pragma unroll
+            for (int b = 0; b < NB; ++b) multiply<KIND>(s[m][b], f, q[k][b]);
           }
         }
-      } else {
-#pragma unroll
-        for (int k = 0; k < KSTEPS; ++k) {
-          uint32_t f[4];
-          load4(f, keys + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, 2 * k + (lane >> 4)));
-#pragma unroll
-          for (int b = 0; b < NB; ++b) multiply<KIND>(s[b], f, q[k][b]);
-        }
       }
-      const int32_t left = (int32_t)((uint32_t)u.row.end - (first + ((uint32_t)j << tile_log)));  // tokens of the tile that are seen, if that is below 16
+      const int32_t left = (int32_t)((uint32_t)u.row.end - (first + ((uint32_t)j << tile_log)));  // tokens that are seen, if not all
       bool past = false;
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) s[b][y] *= mul[b][y & 1];
-      if (left < kRows) {
+      for (int m = 0; m < MB; ++m)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int y = 0; y < 4; ++y)
-            if (lane / 4 + (y >> 1) * 8 >= left) s[b][y] = -INFINITY;
+          for (int y = 0; y < 4; ++y) s[m][b][y] *= mul[b][y & 1];
+      const int32_t lead = WHOLE ? u.row.begin - (int32_t)(first + ((uint32_t)j << tile_log)) : 0;  // and that are not, before them
+      if (left < S::kRows || lead > 0) {
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              if (const int r = 16 * m + lane / 4 + (y >> 1) * 8; r >= left || r < lead) s[m][b][y] = -INFINITY;
       }
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int m = 0; m < MB; ++m)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) past |= s[b][y] > top[b][y & 1] + kLag;
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) past |= s[m][b][y] > top[b][y & 1] + kLag;
       if (__any_sync(~0u, past)) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            float t = fmaxf(s[b][y], s[b][y + 2]);
+            float t = fmaxf(s[0][b][y], s[0][b][y + 2]);
+#pragma unroll
+            for (int m = 1; m < MB; ++m) t = fmaxf(t, fmaxf(s[m][b][y], s[m][b][y + 2]));
             t = fmaxf(t, __shfl_xor_sync(~0u, t, 4));
             t = fmaxf(t, __shfl_xor_sync(~0u, t, 8));
             t = fmaxf(t, __shfl_xor_sync(~0u, t, 16));
@@ -498,45 +552,54 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
             }
           }
       }
-      uint32_t p[NB][2];
+      uint32_t p[MB][NB][2];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
+      for (int m = 0; m < MB; ++m)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const float from = top[b][y & 1];
-          s[b][y] = exp2_fast(s[b][y] - (from == -INFINITY ? 0.f : from));
-          sum[b][y & 1] += s[b][y];
-        }
-        p[b][0] = transpose8(pack<KIND>(s[b][0], s[b][1]));
-        p[b][1] = transpose8(pack<KIND>(s[b][2], s[b][3]));
-      }
-      if (KIND == P2P_KV_E4M3) {
+        for (int b = 0; b < NB; ++b) {
 #pragma unroll
-        for (int k = 0; k < KSTEPS; k += 2) {
-          uint32_t r[4];  // tokens 0-7 and 8-15 of piece k, then of piece k + 1
-          load4t(r, values + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, k + (lane >> 4)));
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            // A lane's register: values 2 * (lane / 4) + {0, 1} of one token, then of the next; the product's rows 0-7 are
-            // the even values, 8-15 the odd ones.
-            const uint32_t lo = __byte_perm(r[2 * y], 0, 0x3120), hi = __byte_perm(r[2 * y + 1], 0, 0x3120);
-            const uint32_t f[4] = {widen(lo), widen_high(lo), widen(hi), widen_high(hi)};
-#pragma unroll
-            for (int b = 0; b < NB; ++b) multiply<KIND>(o[k + y][b], f, p[b]);
+          for (int y = 0; y < 4; ++y) {
+            const float from = top[b][y & 1];
+            s[m][b][y] = exp2_fast(s[m][b][y] - (from == -INFINITY ? 0.f : from));
+            sum[b][y & 1] += s[m][b][y];
           }
+          p[m][b][0] = transpose8(pack<KIND>(s[m][b][0], s[m][b][1]));
+          p[m][b][1] = transpose8(pack<KIND>(s[m][b][2], s[m][b][3]));
         }
-      } else {
 #pragma unroll
-        for (int k = 0; k < KSTEPS; ++k) {
-          uint32_t f[4];
-          load4t(f, values + place<PIECES>((lane & 7) + (lane >> 4) * 8, 2 * k + (lane >> 3 & 1)));
+      for (int m = 0; m < MB; ++m) {
+        const uint32_t values16 = values + m * 16 * S::kRowBytes;
+        if (KIND == P2P_KV_E4M3) {
 #pragma unroll
-          for (int b = 0; b < NB; ++b) multiply<KIND>(o[k][b], f, p[b]);
+          for (int k = 0; k < KSTEPS; k += 2) {
+            uint32_t r[4];  // tokens 0-7 and 8-15 of piece k, then of piece k + 1
+            load4t(r, values16 + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, k + (lane >> 4)));
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              // A lane's register: values 2 * (lane / 4) + {0, 1} of one token, then of the next; the product's rows 0-7
+              // are the even values, 8-15 the odd ones.
+              const uint32_t lo = __byte_perm(r[2 * y], 0, 0x3120), hi = __byte_perm(r[2 * y + 1], 0, 0x3120);
+              const uint32_t f[4] = {widen(lo), widen_high(lo), widen(hi), widen_high(hi)};
+#pragma unroll
+              for (int b = 0; b < NB; ++b) multiply<KIND>(o[k + y][b], f, p[m][b]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < KSTEPS; ++k) {
+            uint32_t f[4];
+            load4t(f, values16 + place<PIECES>((lane & 7) + (lane >> 4) * 8, 2 * k + (lane >> 3 & 1)));
+#pragma unroll
+            for (int b = 0; b < NB; ++b) multiply<KIND>(o[k][b], f, p[m][b]);
+          }
         }
       }
     }
-    here.advance(count, c, a, blocks);
+    float* const sums = (float*)(room + warp * S::kRoom + (slot ? slot - 1 : S::kStages - 1) * S::kStage);  // (the last tile's room: it is not filled before the next step)
+    here.advance<WHOLE>(count, c, a, blocks, tile_log);
     if (here.left > 0) load_queries(here);  // (on their way while this unit row's parts are joined)
+
+    __syncwarp();  // every lane is done with the last tile
 
     // ---- the four warps' parts, eight heads at a time through shared memory: [head][dim], turned by the head so that
     // neither side's accesses meet a bank twice (within 32 values, which the pitch is a multiple of).
@@ -578,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         for (int k = 0; k < kWarps; ++k)
           if ((k & ((1 << c.side) - 1)) == beside) {
             const float fade = exp2_fast(sh.top[k][head] - ref);
-            const float4 f = *(const float4*)((const float*)(room + kWarps * S::kRoom) + (k * 8 + head) * S::kSumPitch + (d ^ head * 4));
+            const float4 f = *(const float4*)(sums + (k - warp) * (S::kRoom / 4) + head * S::kSumPitch + (d ^ head * 4));
             z += fade * sh.sum[k][head];
             v.x += fade * f.x, v.y += fade * f.y, v.z += fade * f.z, v.w += fade * f.w;
           }
@@ -660,19 +723,20 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
           }
         }
         if (teams > 1) {
-          float* const mine = (float*)(room + kWarps * S::kRoom) + threadIdx.x * 8;  // (the sums' room)
+          const auto of_thread = [&](int x) { return sums + ((x >> 5) - warp) * (S::kRoom / 4) + (x & 31) * 8; };
+          float* const mine = of_thread(threadIdx.x);
           mine[0] = t, mine[1] = z;
           *(float4*)(mine + 4) = v;
           __syncthreads();
           if (team == 0) {
             float top1 = t;
-            for (int k = 1; k < teams; ++k) top1 = fmaxf(top1, mine[8 * k * all4]);
+            for (int k = 1; k < teams; ++k) top1 = fmaxf(top1, of_thread(threadIdx.x + k * all4)[0]);
             const float ref = top1 == -INFINITY ? 0.f : top1;
             float fade = exp2_fast(t - ref);
             t = top1;
             z *= fade, v.x *= fade, v.y *= fade, v.z *= fade, v.w *= fade;
             for (int k = 1; k < teams; ++k) {
-              const float* p = mine + 8 * k * all4;
+              const float* p = of_thread(threadIdx.x + k * all4);
               fade = exp2_fast(p[0] - ref);
               z += fade * p[1], v.x += fade * p[4], v.y += fade * p[5], v.z += fade * p[6], v.w += fade * p[7];
             }
@@ -699,10 +763,10 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
 }
 
 // With q = NULL the kernel is only made ready for launches.
-template <int KIND, int DP, int NB>
+template <int KIND, int DP, int NB, bool WHOLE>
 cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   using S = Shape<KIND, DP, NB>;
-  const auto kernel = attend_kernel<KIND, DP, NB>;
+  const auto kernel = attend_kernel<KIND, DP, NB, WHOLE>;
   if (!q) return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
   // As many CTAs as are resident together (by shared memory: 227 KB an SM, of which each CTA takes 1 KB for the system).
   static_assert(S::kCtas <= KvAttendScratch::kCtasPerSm, "the scratch is for so many");
@@ -710,17 +774,22 @@ cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, 
   return cudaGetLastError();
 }
 
+template <int KIND, int DP, int NB>
+cudaError_t launch_pages(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+  return c.page % 16 == 0 ? launch<KIND, DP, NB, true>(c, q, w, num_sms, st) : launch<KIND, DP, NB, false>(c, q, w, num_sms, st);
+}
+
 // (Blocks of 16 query heads take 160 registers and more beyond DP = 128: blocks of eight, whose keys and values the second finds in L2.)
 template <int KIND, int DP>
 cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   if constexpr (DP > 128) {
-    return launch<KIND, DP, 1>(c, q, w, num_sms, st);
+    return launch_pages<KIND, DP, 1>(c, q, w, num_sms, st);
   } else {
     if (!q) {
-      const cudaError_t e = launch<KIND, DP, 1>(c, q, w, num_sms, st);
-      return e == cudaSuccess ? launch<KIND, DP, 2>(c, q, w, num_sms, st) : e;
+      const cudaError_t e = launch_pages<KIND, DP, 1>(c, q, w, num_sms, st);
+      return e == cudaSuccess ? launch_pages<KIND, DP, 2>(c, q, w, num_sms, st) : e;
     }
-    return q->heads / c.heads <= 8 ? launch<KIND, DP, 1>(c, q, w, num_sms, st) : launch<KIND, DP, 2>(c, q, w, num_sms, st);
+    return q->heads / c.heads <= 8 ? launch_pages<KIND, DP, 1>(c, q, w, num_sms, st) : launch_pages<KIND, DP, 2>(c, q, w, num_sms, st);
   }
 }
 
@@ -736,25 +805,4 @@ cudaError_t launch_dim(const KvView& c, const KvQuery* q, const KvAttendScratch&
 }
 
 }  // namespace
-
-size_t kv_attend_parts(const KvView& c, int num_sms) {
-  const int32_t dp = c.dim <= 64 ? 64 : c.dim <= 96 ? 96 : c.dim <= 128 ? 128 : c.dim <= 192 ? 192 : 256;  // (as launch_dim, or more)
-  const int32_t heads = dp > 128 ? 8 : 16;
-  return (size_t)4 * KvAttendScratch::kCtasPerSm * num_sms * (heads << c.side) * (dp + 2);
-}
-
-// Where a token's heads lie together, the rows of one head are pieces of lines and of pages of memory that other heads share (256 bytes and more
-// are read as fast alone):
-// the warps of a CTA take up to four neighbouring heads of the same tokens instead of four times the tokens.
-int32_t kv_attend_side(const KvView& c) {
-  if (c.head_stride > c.token_stride || c.row16 % 16 == 0) return 0;
-  return c.heads % 4 == 0 ? 2 : c.heads % 2 == 0 ? 1 : 0;
-}
-
-cudaError_t launch_kv_attend(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  return c.type == P2P_KV_BF16  ? launch_dim<P2P_KV_BF16>(c, q, w, num_sms, st)
-         : c.type == P2P_KV_F16 ? launch_dim<P2P_KV_F16>(c, q, w, num_sms, st)
-                                : launch_dim<P2P_KV_E4M3>(c, q, w, num_sms, st);
-}
-
 }  // namespace p2p
