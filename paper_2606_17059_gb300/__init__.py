@@ -557,6 +557,10 @@ class KvCache:
         self.k, self.v, self.table, self.length, self.refs = k, v, table, length, refs
         self.k_scale, self.v_scale = scales
         self.layers, self.heads, self.dim, self.n_seqs = layers, heads, dim, table.shape[0]
+        self._int32, self._int64, self._float32, self._empty = torch.int32, torch.int64, torch.float32, torch.empty
+        lib = _load()  # (the calls of a decode step go to the library's functions directly)
+        self._extend, self._trim, self._fork, self._write, self._attend = (
+            lib.p2p_kv_extend, lib.p2p_kv_trim, lib.p2p_kv_fork, lib.p2p_kv_write, lib.p2p_kv_attend)
         a = KvLayout(self._types[k.dtype], layers, pages, page, heads, dim, table.shape[0], table.shape[1], *k.stride()[:4],
                      k.data_ptr(), v.data_ptr(), _addr(k_scale), _addr(v_scale), table.data_ptr(), length.data_ptr(), refs.data_ptr())
         self.device = k.device
@@ -587,25 +591,32 @@ class KvCache:
     def __del__(self):
         self.close()
 
-    def _list(self, first, *others):
-        """The length of a call's lists (int32 CUDA tensors, one entry an item)."""
-        n = first.numel()
-        for t in (first, *others):
-            if t.numel() != n or t.element_size() != 4 or t.is_floating_point() or t.device != self.device:
-                raise ValueError("lists must be int32 tensors of one length on the cache's device")
-        return n
+    def _list(self, t, n: int, dtype) -> int:
+        """Address of a list of n entries."""
+        if t.dtype is not dtype or t.numel() != n or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"lists must be contiguous {dtype} tensors on the cache's device, here of {n} entries")
+        return t.data_ptr()
 
     def extend(self, seq, count) -> None:
         """Room for count[i] more tokens of sequence seq[i]; shared last pages are copied first."""
-        p2p_kv_extend(self._h, self._list(seq, count), seq, count)
+        n, i32 = seq.numel(), self._int32
+        rc = self._extend(self._h, n, self._list(seq, n, i32), self._list(count, n, i32))
+        if rc:
+            _kv_check(rc, self._h)
 
     def trim(self, seq, n_tokens) -> None:
         """Sequence seq[i] keeps its first n_tokens[i] tokens."""
-        p2p_kv_trim(self._h, self._list(seq, n_tokens), seq, n_tokens)
+        n, i32 = seq.numel(), self._int32
+        rc = self._trim(self._h, n, self._list(seq, n, i32), self._list(n_tokens, n, i32))
+        if rc:
+            _kv_check(rc, self._h)
 
     def fork(self, src, dst, n_tokens) -> None:
         """The empty sequence dst[i] becomes the first n_tokens[i] tokens of src[i], whose pages it shares."""
-        p2p_kv_fork(self._h, self._list(src, dst, n_tokens), src, dst, n_tokens)
+        n, i32 = src.numel(), self._int32
+        rc = self._fork(self._h, n, self._list(src, n, i32), self._list(dst, n, i32), self._list(n_tokens, n, i32))
+        if rc:
+            _kv_check(rc, self._h)
 
     def compact(self) -> None:
         """Moves the pages in use to the front of the pool."""
@@ -614,47 +625,45 @@ class KvCache:
     def write(self, layer: int, seq, offsets, k, v) -> None:
         """Keys and values of the last offsets[i+1] - offsets[i] tokens of sequence seq[i]: k and v [layers, tokens, heads,
         head dim] for layers layer, layer + 1, ... (or [tokens, heads, head dim] for one); offsets int64 [n + 1]."""
-        n = self._list(seq)
-        s = k.stride()
-        if k.dim() == 3:
-            layers, s = 1, (0, *s)
-        elif k.dim() == 4:
-            layers = k.shape[0]
-        else:
-            layers = -1
-        if layers < 0 or v.shape != k.shape or v.stride() != k.stride() or tuple(k.shape[-2:]) != (self.heads, self.dim) \
-                or v.dtype != k.dtype or k.dtype not in self._types or (self.dim > 1 and s[3] != 1):
+        n, shape, strides, kind = seq.numel(), k.shape, k.stride(), self._types.get(k.dtype)
+        if len(shape) == 3:
+            shape, strides = (1, *shape), (0, *strides)
+        if (len(shape) != 4 or shape[2] != self.heads or shape[3] != self.dim or kind is None or v.dtype is not k.dtype
+                or v.shape != k.shape or v.stride() != k.stride() or (self.dim > 1 and strides[3] != 1)):
             raise ValueError("k and v must be [layers, tokens, heads, head dim] or [tokens, heads, head dim], strided alike, "
                              "the last dimension contiguous")
-        if offsets.numel() != n + 1 or offsets.element_size() != 8 or offsets.is_floating_point():
-            raise ValueError("offsets must be int64 [n + 1]")
-        if k.device != self.device or v.device != self.device or offsets.device != self.device:
+        if k.device != self.device or v.device != self.device:
             raise ValueError("tensors must be on the cache's device")
-        p2p_kv_write(self._h, layer, layers, n, seq, offsets, k.shape[-3], k.data_ptr(), v.data_ptr(), s[0], s[1], s[2],
-                     self._types[k.dtype])
+        rc = self._write(self._h, layer, shape[0], n, self._list(seq, n, self._int32), self._list(offsets, n + 1, self._int64),
+                         shape[1], k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2], kind)
+        if rc:
+            _kv_check(rc, self._h)
 
     def attend(self, layer: int, q, scale=None, seq=None, window: int = 0, out=None, lse=None):
         """One new token of each sequence (of seq, int32, or sequences 0, 1, ...): q [n, query heads, head dim]; scale: head
         dim ** -0.5 unless given.  Returns (out like q, lse float32 [n, query heads])."""
-        import torch
-        n, heads, dim = q.shape
-        if dim != self.dim or q.dtype not in self._types or (dim > 1 and q.stride(2) != 1):
-            raise ValueError("q must be [n, query heads, head dim], the last dimension contiguous")
-        if seq is not None and self._list(seq) != n:
-            raise ValueError("seq must have one entry per row of q")
+        shape, dtype = q.shape, q.dtype
+        n, heads, dim = shape
+        row, head, inner = q.stride()
+        kind = self._types.get(dtype)
+        if dim != self.dim or kind is None or inner != 1 and dim > 1 or q.device != self.device:
+            raise ValueError("q must be [n, query heads, head dim] on the cache's device, the last dimension contiguous")
         if out is None:
-            out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
-        elif out.shape != q.shape or out.dtype != q.dtype or (dim > 1 and out.stride(2) != 1):
-            raise ValueError("out must be like q, the last dimension contiguous")
+            out = self._empty(shape, dtype=dtype, device=self.device)
+            out_row, out_head = heads * dim, dim
+        else:
+            if out.shape != shape or out.dtype is not dtype or out.device != self.device or out.stride(2) != 1 and dim > 1:
+                raise ValueError("out must be like q, the last dimension contiguous")
+            out_row, out_head, _ = out.stride()
         if lse is None:
-            lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
-        elif tuple(lse.shape) != (n, heads) or lse.dtype != torch.float32:
-            raise ValueError("lse must be float32 [n, query heads]")
-        if q.device != self.device or out.device != self.device or lse.device != self.device:
-            raise ValueError("tensors must be on the cache's device")
-        qs, os_ = q.stride(), out.stride()
-        p2p_kv_attend(self._h, layer, n, seq, q.data_ptr(), qs[0], qs[1], self._types[q.dtype], heads,
-                      dim ** -0.5 if scale is None else scale, window, out.data_ptr(), os_[0], os_[1], lse)
+            lse = self._empty((n, heads), dtype=self._float32, device=self.device)
+        elif (tuple(lse.shape) != (n, heads) or lse.dtype is not self._float32 or lse.device != self.device
+              or not lse.is_contiguous()):
+            raise ValueError("lse must be contiguous float32 [n, query heads]")
+        rc = self._attend(self._h, layer, n, None if seq is None else self._list(seq, n, self._int32), q.data_ptr(), row, head, kind,
+                          heads, dim ** -0.5 if scale is None else scale, window, out.data_ptr(), out_row, out_head, lse.data_ptr())
+        if rc:
+            _kv_check(rc, self._h)
         return out, lse
 
     def stats(self) -> dict:

@@ -27,6 +27,29 @@ struct FastDiv {
   __host__ __device__ __forceinline__ uint32_t ceil(uint32_t x) const { return x ? div(x - 1) + 1 : 0; }
 };
 
+// The cache's kernels are launched so that one may start while the one before it on the stream still runs; each waits for
+// that one's end before its first access to memory (begin_kernel) and lets the next start at once.  A short call's launch is
+// hidden that way.
+template <class... P, class... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t shared, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = shared;
+  cfg.stream = st;
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void begin_kernel() {
+  asm volatile("griddepcontrol.launch_dependents;\n griddepcontrol.wait;" ::: "memory");
+}
+#endif
+
 // The cache as the kernels see it; strides in bytes.
 struct KvView {
   char *k, *v;

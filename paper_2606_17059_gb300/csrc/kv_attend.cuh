@@ -237,6 +237,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   constexpr int PIECES = S::kPieces, KSTEPS = DP / 16;
   extern __shared__ __align__(128) char room[];
   __shared__ Shared sh;
+  begin_kernel();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t tiles_at = smem_of(room + warp * S::kRoom);
   const int32_t group = a.heads / c.heads, blocks = (group + S::kHeads - 1) / S::kHeads;
@@ -770,8 +771,7 @@ cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, 
   if (!q) return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
   // As many CTAs as are resident together (by shared memory: 227 KB an SM, of which each CTA takes 1 KB for the system).
   static_assert(S::kCtas <= KvAttendScratch::kCtasPerSm, "the scratch is for so many");
-  kernel<<<S::kCtas * num_sms, kThreads, S::kBytes, st>>>(c, *q, w);
-  return cudaGetLastError();
+  return launch_early(kernel, dim3(S::kCtas * num_sms), kThreads, S::kBytes, st, c, *q, w);
 }
 
 template <int KIND, int DP, int NB>

@@ -7,8 +7,7 @@
 // many short ones take the same time.  Nothing is changed before that.  What bounds these calls is the chain of loads
 // behind an item (its sequence, the length, the last page, its count) and of the launch itself.
 //
-// Pages are copied by a second launch over the whole GPU, from the list of copies that the plan leaves; it is started
-// early and waits for the plan.
+// Pages are copied by a second launch over the whole GPU, from the list of copies that the plan leaves.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -182,14 +181,11 @@ __device__ __forceinline__ int32_t length_of(const KvView& c, int32_t seq) {
 }
 __device__ __forceinline__ int32_t* row_of(const KvView& c, int32_t seq) { return c.table + (int64_t)seq * c.max_pages; }
 
-__device__ __forceinline__ void start_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_plan() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     extend_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ seq, const int32_t* __restrict__ count) {
   __shared__ Plan p;
+  begin_kernel();
   const int rank = (int)cg::this_cluster().block_rank();
-  start_dependents();
   if (threadIdx.x == 0) {
     p.err = p.cuts = 0;
     if (rank == 0) *s.njobs = 0;
@@ -249,6 +245,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     trim_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ seq, const int32_t* __restrict__ to) {
   __shared__ Plan p;
+  begin_kernel();
   const int rank = (int)cg::this_cluster().block_rank();
   if (threadIdx.x == 0) p.err = 0;
   if (*s.halt) return;
@@ -282,6 +279,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     fork_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                 const int32_t* __restrict__ tokens) {
   __shared__ Plan p;
+  begin_kernel();
   const int rank = (int)cg::this_cluster().block_rank();
   if (threadIdx.x == 0) p.err = 0;
   if (*s.halt) return;
@@ -316,9 +314,9 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
 // either kind is job k's; list[page]: where a page goes (the tables follow in copy_pages_kernel).
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) compact_kernel(KvView c, KvScratch s) {
   __shared__ Plan p;
+  begin_kernel();
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank();
-  start_dependents();
   if (threadIdx.x == 0) {
     p.err = 0;
     if (rank == 0) *s.njobs = 0, *s.live = c.n_pages;
@@ -367,7 +365,7 @@ struct PageShape {
   int32_t planes_log;        // planes = 1 << planes_log <= kCopies
 };
 __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvView c, KvScratch s, PageShape g, int32_t moved) {
-  wait_for_plan();
+  begin_kernel();
   // (Loads past the first cache: this launch may have shared its SM with the plan's.)
   const int32_t njobs = __ldcg(s.njobs);
   if (moved && !__ldcg(s.halt)) {  // the tables of a compaction
@@ -489,6 +487,7 @@ __global__ void __launch_bounds__(kWriteThreads)
     write_kernel(KvView c, KvScratch s, int32_t layer, int32_t n_layers, int32_t share, int32_t n, const int32_t* __restrict__ seq,
                  const int64_t* __restrict__ offsets, int64_t n_tokens, KvRows in, FastDiv by_token, FastDiv by_row) {
   __shared__ int64_t place[kBlock];  // of a token, within its layer; -1: it is not written
+  begin_kernel();
   if (*s.halt) return;
   const int64_t t0 = (int64_t)blockIdx.x * kBlock;
   if (blockIdx.x == 0 && blockIdx.y == 0)
@@ -585,16 +584,7 @@ cudaError_t launch_copies(const KvView& c, const KvScratch& s, bool moved, int n
   g.by_row = FastDiv((uint32_t)c.row16);
   g.by_token = FastDiv((uint32_t)(c.heads * c.row16));
   g.planes_log = c.n_layers == 1 ? 1 : c.n_layers == 2 ? 2 : 3;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(kCopyCtas * num_sms);
-  cfg.blockDim = dim3(kCopyThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute early;
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &early;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, copy_pages_kernel, c, s, g, (int32_t)moved);
+  return launch_early(copy_pages_kernel, dim3(kCopyCtas * num_sms), kCopyThreads, 0, st, c, s, g, (int32_t)moved);
 }
 
 template <int KIND, bool BF16, bool WIDE>
@@ -607,9 +597,8 @@ cudaError_t write_launch(const KvView& c, const KvScratch& s, int32_t layer, int
   const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / (kBlock * c.heads * c.row16));
   const int32_t share = (int32_t)std::min(most, std::max<int64_t>(1, 2 * n_layers / std::min<int64_t>(want, 2 * n_layers)));
   const dim3 grid((unsigned)blocks, (unsigned)((2 * n_layers + share - 1) / share));
-  write_kernel<KIND, BF16, WIDE><<<grid, kWriteThreads, 0, st>>>(c, s, layer, n_layers, share, n, seq, offsets, n_tokens, rows,
-                                                                 FastDiv((uint32_t)(c.heads * c.row16)), FastDiv((uint32_t)c.row16));
-  return cudaGetLastError();
+  return launch_early(write_kernel<KIND, BF16, WIDE>, grid, kWriteThreads, 0, st, c, s, layer, n_layers, share, n, seq, offsets, n_tokens,
+                      rows, FastDiv((uint32_t)(c.heads * c.row16)), FastDiv((uint32_t)c.row16));
 }
 
 template <int KIND, bool BF16>
@@ -631,25 +620,21 @@ cudaError_t prepare_kv_pages() {
 
 cudaError_t launch_kv_extend(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* count, int num_sms,
                              cudaStream_t st) {
-  extend_kernel<<<kCluster, kThreads, item_bytes(n), st>>>(c, s, n, seq, count);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_early(extend_kernel, dim3(kCluster), kThreads, item_bytes(n), st, c, s, n, seq, count);
   return e == cudaSuccess ? launch_copies(c, s, false, num_sms, st) : e;
 }
 
 cudaError_t launch_kv_trim(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* to, cudaStream_t st) {
-  trim_kernel<<<kCluster, kThreads, item_bytes(n), st>>>(c, s, n, seq, to);
-  return cudaGetLastError();
+  return launch_early(trim_kernel, dim3(kCluster), kThreads, item_bytes(n), st, c, s, n, seq, to);
 }
 
 cudaError_t launch_kv_fork(const KvView& c, const KvScratch& s, int32_t n, const int32_t* src, const int32_t* dst,
                            const int32_t* tokens, cudaStream_t st) {
-  fork_kernel<<<kCluster, kThreads, item_bytes(n), st>>>(c, s, n, src, dst, tokens);
-  return cudaGetLastError();
+  return launch_early(fork_kernel, dim3(kCluster), kThreads, item_bytes(n), st, c, s, n, src, dst, tokens);
 }
 
 cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, cudaStream_t st) {
-  compact_kernel<<<kCluster, kThreads, 0, st>>>(c, s);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_early(compact_kernel, dim3(kCluster), kThreads, 0, st, c, s);
   return e == cudaSuccess ? launch_copies(c, s, true, num_sms, st) : e;
 }
 
