@@ -26,6 +26,9 @@
 
 #include "kv.h"
 
+// (No load here goes past the coherent path, as __ldg or const __restrict__ would have it: the kernel before may still be writing
+// when this one starts, see launch_early.)
+
 namespace p2p {
 namespace {
 
@@ -178,14 +181,14 @@ struct Row {
 };
 template <bool WHOLE>
 __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t i, int32_t* err) {
-  Row r = {i < a.n ? (a.seq ? __ldg(a.seq + i) : i) : 0, 0, 0, 0};
+  Row r = {i < a.n ? (a.seq ? a.seq[i] : i) : 0, 0, 0, 0};
   if (i >= a.n) return r;
   if ((uint32_t)r.seq >= (uint32_t)c.n_seqs) {
     if (err) atomicOr(err, KV_BAD_SEQ);
     r.seq = 0;
     return r;
   }
-  const int32_t len = __ldg(c.length + r.seq);
+  const int32_t len = c.length[r.seq];
   if (len < 0 || len > c.max_pages * c.page) {
     if (err) atomicOr(err, KV_BAD_COUNT);
     return r;
@@ -317,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
           near[m] = -1;
           if (t < ahead.row.end) {
             const uint32_t e = c.by_page.div((uint32_t)t);
-            const int32_t page = __ldg(c.table + (int64_t)ahead.row.seq * c.max_pages + e);
+            const int32_t page = c.table[(int64_t)ahead.row.seq * c.max_pages + e];
             if ((uint32_t)page < (uint32_t)c.n_pages)
               near[m] = page * c.page_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
             else
@@ -357,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
       const int64_t t = (int64_t)ahead.row.from + ((int64_t)ahead.t << tile_log) + rank * S::kRows + (lane & (S::kRows - 1));
       if (t < ahead.row.end) {
         const uint32_t e = c.by_page.div((uint32_t)t);
-        k.page = __ldg(c.table + (int64_t)ahead.row.seq * c.max_pages + e);
+        k.page = c.table[(int64_t)ahead.row.seq * c.max_pages + e];
         k.at = layer_at + ahead.h * c.head_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
         if (k.page < 0) k.page = INT32_MAX;
       }
@@ -414,13 +417,13 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         for (int y = 0; y < 2; ++y) {
           const int d = KIND == P2P_KV_E4M3 ? 16 * k + 4 * (lane % 4) + 2 * y : 16 * k + 8 * y + 2 * (lane % 4);
           uint32_t v = 0;
-          if (head < heads && d < c.dim) v = a.q_pairs ? __ldg((const uint32_t*)(from + d)) : __ldg(from + d) | (uint32_t)__ldg(from + d + 1) << 16;
+          if (head < heads && d < c.dim) v = a.q_pairs ? *(const uint32_t*)(from + d) : from[d] | (uint32_t)from[d + 1] << 16;
           q[k][b][y] = v;
         }
     }
   };
   const auto use_queries = [&](const Cursor& u) {
-    float unit = a.scale * kLog2e * (KIND == P2P_KV_E4M3 ? __ldg(c.k_scale + a.layer * c.heads + u.h + part_of_side) : 1.f);
+    float unit = a.scale * kLog2e * (KIND == P2P_KV_E4M3 ? c.k_scale[a.layer * c.heads + u.h + part_of_side] : 1.f);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       float mine = unit;
@@ -652,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
           if (d == 0) part[part_heads * DP + at] = t, part[part_heads * (DP + 1) + at] = z;
         } else if (h8 < heads) {
           const int32_t q_head = head0 + beside * group + h8;
-          const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + u.h + beside) : 1.f;
+          const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
           store4(c, a, u.i, q_head, d, v, v_scale / z, empty);
           if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = empty ? -INFINITY : (t + log2f(z)) / kLog2e;
         }
@@ -746,7 +749,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         if (y < all4 && team == 0) {
           if (done) {
             const int32_t q_head = head0 + beside * group + head;
-            const float v_scale = KIND == P2P_KV_E4M3 ? __ldg(c.v_scale + a.layer * c.heads + u.h + beside) : 1.f;
+            const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
             store4(c, a, u.i, q_head, d, v, v_scale / z, false);
             if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = (t + log2f(z)) / kLog2e;
           } else {

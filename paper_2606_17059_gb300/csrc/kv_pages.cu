@@ -15,6 +15,8 @@
 
 #include "kv.h"
 
+// (No load here goes past the coherent path, as __ldg or const __restrict__ would have it: the kernel before may still be
+// writing when this one starts, see launch_early.)
 namespace p2p {
 namespace {
 
@@ -126,6 +128,32 @@ __device__ __forceinline__ Part part_of(const KvView& c, int rank) {
   const int64_t begin = (int64_t)(rank * kWarps + (threadIdx.x >> 5)) * each;
   return {(int32_t)(begin < c.n_pages ? begin : c.n_pages), (int32_t)(begin + each < c.n_pages ? begin + each : c.n_pages)};
 }
+// The reference counts of the warp's pages, the first of them read at construction.
+struct Counting {
+  static constexpr int kFirst = 8;
+  Part r;
+  int32_t v[kFirst];
+  __device__ __forceinline__ Counting(const KvView& c, const Part& part) : r(part) {
+#pragma unroll
+    for (int k = 0; k < kFirst; ++k) {
+      const int32_t page = r.begin + (threadIdx.x & 31) + 32 * k;
+      v[k] = page < r.end ? __ldcg(c.refs + page) : -1;
+    }
+  }
+  // How many hold for `what`; every lane gets the sum.
+  template <class F>
+  __device__ __forceinline__ int32_t count(const KvView& c, F what) const {
+    int32_t n = 0;
+#pragma unroll
+    for (int k = 0; k < kFirst; ++k) {
+      const int32_t page = r.begin + (threadIdx.x & 31) + 32 * k;
+      n += page < r.end && what(page, v[k]);
+    }
+#pragma unroll 8
+    for (int32_t page = r.begin + (threadIdx.x & 31) + 32 * kFirst; page < r.end; page += 32) n += what(page, __ldcg(c.refs + page));
+    return __reduce_add_sync(~0u, n);
+  }
+};
 // How many of the warp's pages hold for `what`; every lane gets the sum.
 template <class F>
 __device__ __forceinline__ int32_t count_pages(const KvView& c, const Part& r, F what) {
@@ -168,11 +196,9 @@ __device__ void settle(const KvView& c, const KvScratch& s, int32_t n, const int
     *s.halt = 1;
   }
 }
-// (The first CTA alone marks the sequences: what it meets a second time was named twice.)
-__device__ __forceinline__ int32_t claim(const KvView& c, const KvScratch& s, int32_t seq, bool first) {
-  if ((uint32_t)seq >= (uint32_t)c.n_seqs) return KV_BAD_SEQ;
-  return first && atomicExch(&s.claim[seq], 1) ? KV_BAD_SEQ : 0;
-}
+// (The first CTA alone marks the sequences: what it meets a second time was named twice.  The mark's old value is looked at
+// after the item's other loads are on their way.)
+__device__ __forceinline__ int32_t claim(const KvScratch& s, int32_t seq, bool first) { return first ? atomicExch(&s.claim[seq], 1) : 0; }
 
 // A length as the table can hold it, or -1.
 __device__ __forceinline__ int32_t length_of(const KvView& c, int32_t seq) {
@@ -182,39 +208,45 @@ __device__ __forceinline__ int32_t length_of(const KvView& c, int32_t seq) {
 __device__ __forceinline__ int32_t* row_of(const KvView& c, int32_t seq) { return c.table + (int64_t)seq * c.max_pages; }
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
-    extend_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ seq, const int32_t* __restrict__ count) {
+    extend_kernel(KvView c, KvScratch s, int32_t n, const int32_t* seq, const int32_t* count) {
   __shared__ Plan p;
   begin_kernel();
   const int rank = (int)cg::this_cluster().block_rank();
+  const int32_t halt = *s.halt;
   if (threadIdx.x == 0) {
     p.err = p.cuts = 0;
     if (rank == 0) *s.njobs = 0;
   }
-  if (*s.halt) return;
   __syncthreads();
   const Part mine = part_of(c, rank);
   const auto is_free = [](int32_t, int32_t refs) { return refs == 0; };
-  int32_t free_here;
-  const int32_t free_before = scan_warps(p, count_pages(c, mine, is_free), free_here);
+  const Counting counting(c, mine);  // (the first pages' counts, on their way while the items are planned)
   const Items it = items_of(s, n);
   if (rank == 0 || n <= kItems)
     plan_items(p, it, n, [&](int32_t i, int32_t& need, int32_t& first, int32_t& cut) -> int32_t {
-      if (const int32_t bad = claim(c, s, seq[i], rank == 0)) return bad;
-      const int32_t len = length_of(c, seq[i]), add = count[i];
+      const int32_t q = seq[i], add = count[i];
+      if ((uint32_t)q >= (uint32_t)c.n_seqs) return KV_BAD_SEQ;
+      const int32_t twice = claim(s, q, rank == 0), len = length_of(c, q);
       if (len < 0 || add < 0 || add > c.max_pages * c.page - len) return KV_BAD_COUNT;
       const int32_t have = (int32_t)c.by_page.ceil(len);
       need = (int32_t)c.by_page.ceil(len + add) - have;
       first = have;
       const int32_t used = len - (int32_t)c.by_page.div(len) * c.page;
       if (add > 0 && used > 0) {
-        const int32_t last = row_of(c, seq[i])[have - 1];
+        const int32_t last = row_of(c, q)[have - 1];
         const int32_t refs = (uint32_t)last < (uint32_t)c.n_pages ? __ldcg(c.refs + last) : 0;
         if (refs < 1) return KV_BAD_PAGE;
         if (refs > 1) cut = used, first = have - 1, need += 1, p.cuts = 1;
       }
-      return 0;
+      return twice ? KV_BAD_SEQ : 0;
     });
+  int32_t free_here;
+  const int32_t free_before = scan_warps(p, counting.count(c, is_free), free_here);
   int32_t err = meet(p, free_here, p.cuts);
+  if (halt) {
+    if (rank == 0) settle(c, s, n, seq, 0);
+    return;
+  }
   const int32_t total = it.start[n];
   int64_t at = free_before, all = 0;
 #pragma unroll
@@ -243,24 +275,29 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
 }
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
-    trim_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ seq, const int32_t* __restrict__ to) {
+    trim_kernel(KvView c, KvScratch s, int32_t n, const int32_t* seq, const int32_t* to) {
   __shared__ Plan p;
   begin_kernel();
   const int rank = (int)cg::this_cluster().block_rank();
+  const int32_t halt = *s.halt;
   if (threadIdx.x == 0) p.err = 0;
-  if (*s.halt) return;
   __syncthreads();
   const Items it = items_of(s, n);
   if (rank == 0 || n <= kItems)
     plan_items(p, it, n, [&](int32_t i, int32_t& need, int32_t& first, int32_t&) -> int32_t {
-      if (const int32_t bad = claim(c, s, seq[i], rank == 0)) return bad;
-      const int32_t len = length_of(c, seq[i]);
-      if (len < 0 || to[i] < 0 || to[i] > len) return KV_BAD_COUNT;
-      first = (int32_t)c.by_page.ceil(to[i]);
+      const int32_t q = seq[i], keep = to[i];
+      if ((uint32_t)q >= (uint32_t)c.n_seqs) return KV_BAD_SEQ;
+      const int32_t twice = claim(s, q, rank == 0), len = length_of(c, q);
+      if (len < 0 || keep < 0 || keep > len) return KV_BAD_COUNT;
+      first = (int32_t)c.by_page.ceil(keep);
       need = (int32_t)c.by_page.ceil(len) - first;
-      return 0;
+      return twice ? KV_BAD_SEQ : 0;
     });
   const int32_t err = meet(p, 0, 0);
+  if (halt) {
+    if (rank == 0) settle(c, s, n, seq, 0);
+    return;
+  }
   if (rank == 0) settle(c, s, n, seq, err);
   if (err) return;
   const int32_t total = it.start[n];
@@ -276,25 +313,29 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
 }
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
-    fork_kernel(KvView c, KvScratch s, int32_t n, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
-                const int32_t* __restrict__ tokens) {
+    fork_kernel(KvView c, KvScratch s, int32_t n, const int32_t* src, const int32_t* dst,
+                const int32_t* tokens) {
   __shared__ Plan p;
   begin_kernel();
   const int rank = (int)cg::this_cluster().block_rank();
+  const int32_t halt = *s.halt;
   if (threadIdx.x == 0) p.err = 0;
-  if (*s.halt) return;
   __syncthreads();
   const Items it = items_of(s, n);
   if (rank == 0 || n <= kItems)
     plan_items(p, it, n, [&](int32_t i, int32_t& need, int32_t&, int32_t&) -> int32_t {
-      if (const int32_t bad = claim(c, s, dst[i], rank == 0)) return bad;
-      if ((uint32_t)src[i] >= (uint32_t)c.n_seqs) return KV_BAD_SEQ;
-      const int32_t len = length_of(c, src[i]);
-      if (len < 0 || tokens[i] < 0 || tokens[i] > len || c.length[dst[i]] != 0) return KV_BAD_COUNT;
-      need = (int32_t)c.by_page.ceil(tokens[i]);
-      return 0;
+      const int32_t from = src[i], q = dst[i], take = tokens[i];
+      if ((uint32_t)q >= (uint32_t)c.n_seqs || (uint32_t)from >= (uint32_t)c.n_seqs) return KV_BAD_SEQ;
+      const int32_t twice = claim(s, q, rank == 0), len = length_of(c, from), held = c.length[q];
+      if (len < 0 || take < 0 || take > len || held != 0) return KV_BAD_COUNT;
+      need = (int32_t)c.by_page.ceil(take);
+      return twice ? KV_BAD_SEQ : 0;
     });
   const int32_t err = meet(p, 0, 0);
+  if (halt) {
+    if (rank == 0) settle(c, s, n, dst, 0);
+    return;
+  }
   if (rank == 0) settle(c, s, n, dst, err);
   if (err) return;
   const int32_t total = it.start[n];
@@ -356,14 +397,14 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) com
   }
 }
 
-// The copies of the plan before it, in 16-byte pieces.  A warp takes 32 pieces of a page, one a lane, in `planes` of the
+// The copies of the plan before it, in 16-byte pieces.  A warp takes 32 pieces of a page, one a lane, in 1 << PLANES_LOG of the
 // 2 * n_layers arrays (keys and values of each layer) and, where those are fewer than kCopies, further 32 pieces, so that
 // a lane has kCopies loads in flight whose places differ by strides alone.
 constexpr int kCopies = 8, kCopyThreads = 256, kCopyCtas = 4;
 struct PageShape {
   FastDiv by_row, by_token;  // pieces of a head's values of a token, and of a token
-  int32_t planes_log;        // planes = 1 << planes_log <= kCopies
 };
+template <int PLANES_LOG>
 __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvView c, KvScratch s, PageShape g, int32_t moved) {
   begin_kernel();
   // (Loads past the first cache: this launch may have shared its SM with the plan's.)
@@ -385,9 +426,9 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvV
     }
   }
   if (njobs == 0) return;
+  constexpr int kPlanes = 1 << PLANES_LOG, kPieces = kCopies / kPlanes;
   const int lane = threadIdx.x & 31;
-  const int32_t planes = 1 << g.planes_log, per_warp = 32 * (kCopies >> g.planes_log);
-  const int32_t chunks = (c.page * (int32_t)g.by_token.d + per_warp - 1) / per_warp, groups = (2 * c.n_layers + planes - 1) / planes;
+  const int32_t chunks = (c.page * (int32_t)g.by_token.d + 32 * kPieces - 1) / (32 * kPieces), groups = (2 * c.n_layers + kPlanes - 1) / kPlanes;
   const int64_t items = (int64_t)njobs * groups * chunks;
   for (int64_t x = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); x < items; x += (int64_t)gridDim.x * (kCopyThreads / 32)) {
     const int64_t job = x / ((int64_t)groups * chunks);
@@ -396,21 +437,26 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvV
     const int32_t chunk = (int32_t)((rest - group * chunks + job) % chunks);
     const int4 j = __ldcg((const int4*)(s.jobs + job));  // from, to, tokens
     const int64_t move = (int64_t)(j.y - j.x) * c.page_stride;
-    const int32_t pieces = j.z * (int32_t)g.by_token.d, plane0 = group << g.planes_log;
-    uint4 v[kCopies];
-    const auto at = [&](int k) -> char* {  // the k-th of the lane's pieces; NULL: none
-      const int32_t plane = plane0 + (k & (planes - 1)), z = chunk * per_warp + (k >> g.planes_log) * 32 + lane;
-      if (z >= pieces || plane >= 2 * c.n_layers) return nullptr;
+    int64_t at[kPieces];  // of the lane's pieces within their layer; -1: none
+#pragma unroll
+    for (int y = 0; y < kPieces; ++y) {
+      const int32_t z = (chunk * kPieces + y) * 32 + lane;
       const uint32_t t = g.by_token.div(z), in = z - t * g.by_token.d, h = g.by_row.div(in);
-      return (plane & 1 ? c.v : c.k) + (plane >> 1) * c.layer_stride + j.x * c.page_stride + t * c.token_stride + h * c.head_stride +
-             (in - h * g.by_row.d) * 16;
-    };
+      at[y] = (int32_t)t < j.z ? j.x * c.page_stride + t * c.token_stride + h * c.head_stride + (in - h * g.by_row.d) * 16 : -1;
+    }
+    const int32_t layer0 = group * (kPlanes / 2), layers = min(kPlanes / 2, c.n_layers - layer0);
+    char *const k0 = c.k + layer0 * c.layer_stride, *const v0 = c.v + layer0 * c.layer_stride;
+    uint4 v[kPieces][kPlanes];
 #pragma unroll
-    for (int k = 0; k < kCopies; ++k)
-      if (const char* p = at(k)) v[k] = __ldcg((const uint4*)p);
+    for (int y = 0; y < kPieces; ++y)
 #pragma unroll
-    for (int k = 0; k < kCopies; ++k)
-      if (char* p = at(k)) __stcg((uint4*)(p + move), v[k]);
+      for (int p = 0; p < kPlanes; ++p)
+        if (at[y] >= 0 && p / 2 < layers) v[y][p] = __ldcg((const uint4*)((p & 1 ? v0 : k0) + p / 2 * c.layer_stride + at[y]));
+#pragma unroll
+    for (int y = 0; y < kPieces; ++y)
+#pragma unroll
+      for (int p = 0; p < kPlanes; ++p)
+        if (at[y] >= 0 && p / 2 < layers) __stcg((uint4*)((p & 1 ? v0 : k0) + p / 2 * c.layer_stride + at[y] + move), v[y][p]);
   }
 }
 
@@ -419,6 +465,7 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvV
 // Where the tokens of a block go is found once, a lane a token, and serves all their heads in the layers and arrays that
 // the CTA writes.  Bound by the bytes read and written.
 constexpr int kBlock = 32, kWriteThreads = 256;
+static_assert(kBlock == 32, "a warp finds the places, all its lanes together");
 
 // The last item that starts at or before token t (items without tokens share a start): every lane gets it.
 __device__ __forceinline__ int32_t find_item(const int64_t* offsets, int32_t n, int64_t t) {
@@ -426,7 +473,7 @@ __device__ __forceinline__ int32_t find_item(const int64_t* offsets, int32_t n, 
   int32_t lo = 0, hi = n;
   while (hi - lo > 1) {  // 32 probes a round
     const int32_t step = (hi - lo + 31) / 32, at = lo + step * lane;
-    const uint32_t m = __ballot_sync(~0u, at < hi && __ldg(offsets + at) <= t);
+    const uint32_t m = __ballot_sync(~0u, at < hi && offsets[at] <= t);
     if (!m) return lo;
     const int32_t k = 31 - __clz(m);
     lo = lo + step * k;
@@ -467,16 +514,25 @@ __device__ __forceinline__ uint4 narrow16(const uint4& a, const uint4& b, float 
   }
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
-// Eight values from where they may lie on no 16-byte boundary.
-template <bool WIDE>
-__device__ __forceinline__ uint4 read8(const uint16_t* p) {
-  if constexpr (WIDE) {
-    return __ldcs((const uint4*)p);
+// 8 * N values, with WIDE from a 16 * N-byte boundary.  (One load for 16: as two, each
+// 32-byte sector is asked for twice, and 61 prompts in 8 bits take 760 us, not 575.)
+template <bool WIDE, int N>
+__device__ __forceinline__ void read_values(uint4 (&v)[N], const uint16_t* p) {
+  if constexpr (WIDE && N == 2) {
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y), "=r"(v[1].z), "=r"(v[1].w)
+                 : "l"(p)
+                 : "memory");
+  } else if constexpr (WIDE) {
+    v[0] = __ldcs((const uint4*)p);
   } else {
-    uint32_t v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __ldg(p + 2 * i) | (uint32_t)__ldg(p + 2 * i + 1) << 16;
-    return make_uint4(v[0], v[1], v[2], v[3]);
+    for (int k = 0; k < N; ++k) {
+      uint32_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = p[8 * k + 2 * i] | (uint32_t)p[8 * k + 2 * i + 1] << 16;
+      v[k] = make_uint4(x[0], x[1], x[2], x[3]);
+    }
   }
 }
 
@@ -484,12 +540,36 @@ __device__ __forceinline__ uint4 read8(const uint16_t* p) {
 // arrays (keys and values of each layer).  by_token: 16-byte pieces of a token in one array, by_row: of a head.
 template <int KIND, bool BF16, bool WIDE>
 __global__ void __launch_bounds__(kWriteThreads)
-    write_kernel(KvView c, KvScratch s, int32_t layer, int32_t n_layers, int32_t share, int32_t n, const int32_t* __restrict__ seq,
-                 const int64_t* __restrict__ offsets, int64_t n_tokens, KvRows in, FastDiv by_token, FastDiv by_row) {
+    write_kernel(KvView c, KvScratch s, int32_t layer, int32_t n_layers, int32_t share, int32_t n, const int32_t* seq,
+                 const int64_t* offsets, int64_t n_tokens, KvRows in, FastDiv by_token, FastDiv by_row) {
   __shared__ int64_t place[kBlock];  // of a token, within its layer; -1: it is not written
   begin_kernel();
-  if (*s.halt) return;
+  const int32_t halt = *s.halt;
   const int64_t t0 = (int64_t)blockIdx.x * kBlock;
+  const int32_t tokens = (int32_t)min((int64_t)kBlock, n_tokens - t0), a0 = blockIdx.y * share, a1 = min(a0 + share, 2 * n_layers);
+  const uint32_t all = tokens * by_token.d * (uint32_t)(a1 - a0);
+  constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8, kLoads = kValues / 8, kAhead = 4 / kLoads;  // pieces of a thread in flight
+  uint4 v[kAhead][kLoads];
+  float scale[kAhead];
+  char* to[kAhead];      // but for the token's place
+  int32_t token[kAhead];  // of the block; -1: no piece
+  const auto read = [&](uint32_t y0) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const uint32_t y = y0 + k * kWriteThreads;
+      token[k] = -1;
+      if (y >= all) continue;
+      const uint32_t token_of = by_token.div(y), over = tokens == kBlock ? token_of / kBlock : token_of / tokens;
+      const uint32_t t = token_of - over * tokens, array = a0 + over, z = y - token_of * by_token.d, h = by_row.div(z), piece = z - h * by_row.d;
+      const int32_t l = array >> 1;
+      const uint16_t* from = (const uint16_t*)(array & 1 ? in.v : in.k) + l * in.layer_stride + (t0 + t) * in.token_stride + h * in.head_stride + piece * kValues;
+      read_values<WIDE>(v[k], from);
+      if (KIND == P2P_KV_E4M3) scale[k] = (array & 1 ? c.v_scale : c.k_scale)[(layer + l) * c.heads + h];
+      to[k] = (array & 1 ? c.v : c.k) + (int64_t)(layer + l) * c.layer_stride + h * c.head_stride + piece * 16;
+      token[k] = t;
+    }
+  };
+  read(threadIdx.x);  // (on their way while it is found where they go)
   if (blockIdx.x == 0 && blockIdx.y == 0)
     for (int32_t i = threadIdx.x; i < n; i += kWriteThreads)
       if (offsets[i] < 0 || offsets[i + 1] < offsets[i] || offsets[i + 1] > n_tokens) atomicOr(s.err, KV_BAD_OFFSETS);
@@ -498,14 +578,14 @@ __global__ void __launch_bounds__(kWriteThreads)
     int32_t lo = find_item(offsets, n, t0), hi = min(n, find_item(offsets, n, t0 + kBlock - 1) + 1);
     while (hi - lo > 1) {
       const int32_t mid = (lo + hi) >> 1;
-      if (__ldg(offsets + mid) <= t)
+      if (offsets[mid] <= t)
         lo = mid;
       else
         hi = mid;
     }
     int64_t at = -1;
     const int64_t o0 = offsets[lo], o1 = offsets[lo + 1];
-    if (o0 >= 0 && o0 <= t && t < o1 && o1 <= n_tokens) {  // (else it belongs to no sequence)
+    if (!halt && o0 >= 0 && o0 <= t && t < o1 && o1 <= n_tokens) {  // (else it belongs to no sequence)
       const int32_t q = seq[lo], len = (uint32_t)q < (uint32_t)c.n_seqs ? length_of(c, q) : 0;
       int32_t bad = 0;
       if ((uint32_t)q >= (uint32_t)c.n_seqs) {
@@ -525,38 +605,23 @@ __global__ void __launch_bounds__(kWriteThreads)
     place[threadIdx.x] = at;
   }
   __syncthreads();
-  const int32_t tokens = (int32_t)min((int64_t)kBlock, n_tokens - t0), a0 = blockIdx.y * share, a1 = min(a0 + share, 2 * n_layers);
-  const uint32_t all = tokens * by_token.d * (uint32_t)(a1 - a0);
-  constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8, kLoads = kValues / 8, kAhead = 4;  // pieces of a thread in flight
-  for (uint32_t y0 = threadIdx.x; y0 < all; y0 += kAhead * kWriteThreads) {
-    uint4 v[kAhead][kLoads];
-    char* to[kAhead];
-    float scale[kAhead];
+  const auto write = [&]() {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const uint32_t y = y0 + k * kWriteThreads, token_of = by_token.div(y), over = tokens == kBlock ? token_of / kBlock : token_of / tokens;
-      const uint32_t t = token_of - over * tokens, array = a0 + over, z = y - token_of * by_token.d, h = by_row.div(z), piece = z - h * by_row.d;
-      to[k] = nullptr;
-      const int64_t at = y < all ? place[t] : -1;
-      if (at >= 0) {
-        const int32_t l = array >> 1;
-        const uint16_t* from = (const uint16_t*)(array & 1 ? in.v : in.k) + l * in.layer_stride + (t0 + t) * in.token_stride + h * in.head_stride + piece * kValues;
-        to[k] = (array & 1 ? c.v : c.k) + (int64_t)(layer + l) * c.layer_stride + at + h * c.head_stride + piece * 16;
-#pragma unroll
-        for (int x = 0; x < kLoads; ++x) v[k][x] = read8<WIDE>(from + 8 * x);
-        if (KIND == P2P_KV_E4M3) scale[k] = __ldg((array & 1 ? c.v_scale : c.k_scale) + (layer + l) * c.heads + h);
+      const int64_t at = token[k] < 0 ? -1 : place[token[k]];
+      if (at < 0) continue;
+      if (KIND == P2P_KV_E4M3) {
+        const bool plain = fabsf(scale[k]) > 0x1p-60f && fabsf(scale[k]) < 0x1p60f;
+        __stcs((uint4*)(to[k] + at), narrow16<BF16>(v[k][0], v[k][kLoads - 1], scale[k], __frcp_rn(scale[k]), plain));
+      } else {
+        __stcs((uint4*)(to[k] + at), v[k][0]);
       }
     }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (to[k]) {
-        if (KIND == P2P_KV_E4M3) {
-          const bool plain = fabsf(scale[k]) > 0x1p-60f && fabsf(scale[k]) < 0x1p60f;
-          __stcs((uint4*)to[k], narrow16<BF16>(v[k][0], v[k][kLoads - 1], scale[k], __frcp_rn(scale[k]), plain));
-        } else {
-          __stcs((uint4*)to[k], v[k][0]);
-        }
-      }
+  };
+  write();
+  for (uint32_t y0 = threadIdx.x + kAhead * kWriteThreads; y0 < all; y0 += kAhead * kWriteThreads) {
+    read(y0);
+    write();
   }
 }
 
@@ -583,8 +648,8 @@ cudaError_t launch_copies(const KvView& c, const KvScratch& s, bool moved, int n
   PageShape g;
   g.by_row = FastDiv((uint32_t)c.row16);
   g.by_token = FastDiv((uint32_t)(c.heads * c.row16));
-  g.planes_log = c.n_layers == 1 ? 1 : c.n_layers == 2 ? 2 : 3;
-  return launch_early(copy_pages_kernel, dim3(kCopyCtas * num_sms), kCopyThreads, 0, st, c, s, g, (int32_t)moved);
+  const auto kernel = c.n_layers == 1 ? copy_pages_kernel<1> : c.n_layers == 2 ? copy_pages_kernel<2> : copy_pages_kernel<3>;
+  return launch_early(kernel, dim3(kCopyCtas * num_sms), kCopyThreads, 0, st, c, s, g, (int32_t)moved);
 }
 
 template <int KIND, bool BF16, bool WIDE>
@@ -640,8 +705,9 @@ cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, 
 
 cudaError_t launch_kv_write(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq,
                             const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms, cudaStream_t st) {
-  const bool wide = (uintptr_t)rows.k % 16 == 0 && (uintptr_t)rows.v % 16 == 0 && rows.layer_stride % 8 == 0 &&
-                    rows.token_stride % 8 == 0 && rows.head_stride % 8 == 0;
+  const int64_t values = c.type == P2P_KV_E4M3 ? 16 : 8;  // that are read together
+  const bool wide = (uintptr_t)rows.k % (2 * values) == 0 && (uintptr_t)rows.v % (2 * values) == 0 && rows.layer_stride % values == 0 &&
+                    rows.token_stride % values == 0 && rows.head_stride % values == 0;
   if (c.type != P2P_KV_E4M3)  // (16-bit values are stored as they are)
     return write_wide<P2P_KV_BF16, true>(wide, c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st);
   return rows.type == P2P_KV_BF16
