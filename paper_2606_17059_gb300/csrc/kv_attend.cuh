@@ -33,7 +33,7 @@ namespace p2p {
 namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kOver = 4;                // units that a unit row counts for beyond its own
+constexpr int kOver = 3;                // units that a unit row counts for beyond its own
 constexpr int kJoin = 16;               // parts of a unit row that are read together
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
 constexpr float kLog2e = 1.4426950408889634f;
@@ -181,20 +181,14 @@ struct Row {
 };
 template <bool WHOLE>
 __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t i, int32_t* err) {
-  Row r = {i < a.n ? (a.seq ? a.seq[i] : i) : 0, 0, 0, 0};
-  if (i >= a.n) return r;
-  if ((uint32_t)r.seq >= (uint32_t)c.n_seqs) {
-    if (err) atomicOr(err, KV_BAD_SEQ);
-    r.seq = 0;
-    return r;
-  }
-  const int32_t len = c.length[r.seq];
-  if (len < 0 || len > c.max_pages * c.page) {
-    if (err) atomicOr(err, KV_BAD_COUNT);
-    return r;
-  }
-  r.end = len;
-  r.begin = a.window && len > a.window ? len - a.window : 0;
+  const bool there = i < a.n;
+  const int32_t seq = there && a.seq ? a.seq[i] : there ? i : 0;
+  const bool known = (uint32_t)seq < (uint32_t)c.n_seqs;
+  const int32_t len = there && known ? c.length[seq] : 0;
+  const bool fits = len >= 0 && len <= c.max_pages * c.page;
+  if (err && !(known && fits)) atomicOr(err, known ? KV_BAD_COUNT : KV_BAD_SEQ);
+  Row r = {known ? seq : 0, 0, 0, fits ? len : 0};
+  r.begin = a.window && r.end > a.window ? r.end - a.window : 0;
   r.from = WHOLE ? r.begin / 16 * 16 : r.begin;
   return r;
 }
@@ -251,7 +245,13 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   // ---- this CTA's range of the units: a thread sums those of consecutive rows, the CTA scans the threads' sums.
   const int32_t each = (a.n + kThreads - 1) / kThreads, r0 = threadIdx.x * each;
   int64_t mine = 0;
-  for (int32_t i = r0; i < r0 + each && i < a.n; ++i) mine += row_at<WHOLE>(c, a, i, blockIdx.x == 0 ? w.err : nullptr).tiles(tile_log) + kOver;
+  for (int32_t i0 = r0; i0 < r0 + each && i0 < a.n; i0 += 4) {
+    Row r[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[k] = row_at<WHOLE>(c, a, i0 + k < r0 + each ? i0 + k : a.n, blockIdx.x == 0 ? w.err : nullptr);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mine += i0 + k < r0 + each && i0 + k < a.n ? r[k].tiles(tile_log) + kOver : 0;
+  }
   int64_t scan = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
