@@ -364,7 +364,9 @@ int p2p_route_decide(p2p_router* r, const int32_t* match, int64_t B, const int32
  *   - Table entries past a sequence's length mean nothing.  A sequence is named once in a call's list.
  *   - A call whose items do not hold (see each call) changes nothing, and neither does any later call on the tables or
  *     p2p_kv_write, until p2p_kv_sync has reported it.
- *   - Page numbers out of range are never followed: they are reported, and what they would have given is left out.
+ *   - Page numbers out of range are never followed: they are reported, and what they would have given is left out
+ *     (p2p_kv_attend takes zeros in its place).
+ *   - The page entries that a call concerns are at most 2^31 - 1.
  */
 enum { P2P_KV_BF16 = 0, P2P_KV_F16 = 1, P2P_KV_E4M3 = 2 };
 
@@ -391,9 +393,9 @@ typedef struct p2p_kv_layout {
   int32_t *refs;        /* int32[n_pages] */
 } p2p_kv_layout;
 
-/* A handle on the cache `layout` describes, on the current CUDA device; its scratch is allocated here.  The arrays stay
- * the caller's and must outlive the handle.  Errors: P2P_E_INVAL (message of p2p_kv_last_error(NULL)), P2P_E_NOMEM,
- * P2P_E_CUDA. */
+/* A handle on the cache `layout` describes, on the current CUDA device; its scratch (8 to 61 MB by head_dim and order, and
+ * up to 20 bytes a page and 32 a sequence) is allocated here.  The arrays stay the caller's and must outlive the handle.
+ * Errors: P2P_E_INVAL (message of p2p_kv_last_error(NULL)), P2P_E_NOMEM, P2P_E_CUDA. */
 int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out);
 
 /* Frees the handle and its scratch (after finishing its queued work).  NULL is a no-op. */

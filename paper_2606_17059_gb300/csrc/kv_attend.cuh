@@ -5,20 +5,30 @@
 //
 // Keys and values are read once, and that is what bounds it: with g query heads a kv head, 4 g dim operations go with
 // 4 dim bytes, g a byte (2 g with 8 bits), where the GPU has 277 operations of its tensor cores for a byte of memory.
+// Measured (one GB300, copy bandwidth 6.8 TB/s): 32 sequences of 4,352 to 33,792 tokens, 40 / 8 heads of 128 f16 values,
+// 1.88 GB in 277 us (the copy bandwidth); one sequence of 131,071 tokens, 32 / 8 heads, 0.54 GB in 85 us (93%); 256
+// sequences of 128 to 4,224 tokens in 8 bits, 64 / 8 heads, 0.61 GB in 105 us (87%: there the widening of the values
+// and the ends of the rows weigh); one of 540 tokens 7.5 us, a chain of a launch, four loads, a tile and the join.
 //
-// The work is cut into units of kTile tokens of a (sequence, kv head, block of its query heads), numbered in that order,
-// and every CTA takes an equal, contiguous range of them: one sequence of 131,071 tokens fills the GPU as a batch does.
-// A range's parts of a unit row that it shares with other CTAs go to scratch (maximum, sum, unnormalised out), and the
-// CTA that finishes such a row last joins its parts, in their order: results do not depend on timing.  (The start of a
-// unit row counts as kOver units more, for the joining of its warps' parts.)
+// The work is cut into units of 64 or 128 tokens of a (sequence, kv head, block of its query heads), numbered in that
+// order, and every CTA takes an equal, contiguous range of them: one long sequence fills the GPU as a batch does.  A
+// range's parts of a unit row that it shares with other CTAs go to scratch (maximum, sum, unnormalised out), and the CTA
+// that finishes such a row last joins its parts, in their order: results do not depend on timing.  (The start of a unit
+// row counts as kOver units more, for what its end costs: with 1 instead of 3, the 256 sequences in 8 bits take 115 us.)
 //
-// Each warp streams 16 tokens at a time through shared memory of its own, several tiles ahead (cp.async, 16 bytes a
-// lane, 16-byte pieces swizzled so that ldmatrix meets no bank twice), with no barrier between warps inside a unit row;
-// the copies run on into the next unit row while this one's parts are joined, and page numbers are read two tiles ahead
-// of the copies.  A 16-token tile is multiplied transposed: S^T [tokens, heads] = K Q^T and O^T [dim, heads] += V^T P^T,
-// so that eight query heads fill a product's n and the 16 tokens its m.  P^T goes from the first product's layout to the
-// second's by two 8 x 8 transposes of registers.  exp(x - m) takes for m not the running maximum but one that lags
-// it by at most a factor of 2^8, so that a tile's maximum is only reduced, and O rescaled, where it goes past that.
+// Each warp streams 16 or 32 tokens at a time through shared memory of its own, up to seven tiles ahead (cp.async, 16
+// bytes a lane, 16-byte pieces turned so that ldmatrix meets no bank twice), with no barrier between warps inside a
+// unit row; the copies run on into the next unit row while this one's parts are joined.  Where pages are whole sixteens
+// of tokens, a lane looks up the page of a whole tile ahead, for 32 tiles at once; else each token's is looked up two
+// tiles ahead.  Sixteen tokens are multiplied transposed: S^T [tokens, heads] = K Q^T and O^T [dim, heads] += V^T P^T,
+// so that eight query heads fill a product's n and the tokens (or values) its m of 16.  P^T goes from the first product's
+// layout to the second's by two 8 x 8 transposes of registers.  exp(x - m) takes for m not the running maximum but one
+// that lags it by at most a factor of 2^8, so that a tile's maximum is only reduced, and O rescaled, where it goes past
+// that.  P is rounded to the values' type (f16 for 8 bits) for its product; sums, maxima and O are held in 32 bits.
+//
+// The products are warp-wide ones (mma): 9% of the tensor cores' time at the copy bandwidth (8 bits: 17%), and their operands come
+// out of shared memory by ldmatrix in any row size.  The tensor memory path (tcgen05) would free issue slots that 16-bit
+// values do not need and that 8-bit values, which have to be widened beside 16-bit queries, could not use it for.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
