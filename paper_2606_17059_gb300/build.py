@@ -19,8 +19,8 @@ LIB = os.path.join(PKG, "libp2prouter.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc" if os.path.exists("/usr/local/cuda/bin/nvcc") else "nvcc")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["route_kernel.cu", "group_kernel.cu", "delta_kernel.cu", "delta_bulk.cu", "delta_static.cu", "update_kernel.cu",
-           "lru_kernel.cu", "router.cu", "snapshot.cpp", "kv_pages.cu", "kv_attend_bf16.cu", "kv_attend_f16.cu",
-           "kv_attend_e4m3.cu", "kv_cache.cpp"]
+           "lru_kernel.cu", "router.cu", "snapshot.cpp", "kv_pages.cu", "kv_cache.cpp",
+           *(f"kv_attend_{t}{w}.cu" for t in ("bf16", "f16", "e4m3") for w in ("", "_side"))]
 
 
 def _flags(extra=()):

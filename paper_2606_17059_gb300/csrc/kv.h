@@ -127,7 +127,10 @@ inline size_t kv_attend_parts(const KvView& c, int num_sms) {
 }
 // With q = NULL they launch nothing, but make the cache's kernels ready for launches (at creation).
 cudaError_t launch_kv_attend_bf16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_attend_bf16_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
 cudaError_t launch_kv_attend_f16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_attend_f16_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
 cudaError_t launch_kv_attend_e4m3(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_attend_e4m3_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
 
 }  // namespace p2p

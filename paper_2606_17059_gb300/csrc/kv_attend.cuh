@@ -46,7 +46,7 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kOver = 3;                // units that a unit row counts for beyond its own
 constexpr int kJoin = 16;               // parts of a unit row that are read together
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <int KIND>
 struct Type;
@@ -219,7 +219,7 @@ struct Cursor {
   int64_t left;  // units of the range from here on; none: at its end
   // k tiles on, none past the unit row's end.
   template <bool WHOLE>
-  __device__ __forceinline__ void advance(int32_t k, const KvView& c, const KvQuery& a, int32_t blocks, int32_t tile_log) {
+  __device__ __forceinline__ void advance(int32_t k, const KvView& c, const KvQuery& a, int32_t blocks, int32_t side, int32_t tile_log) {
     t += k;
     left -= k;
     if (t < nt) return;
@@ -227,7 +227,7 @@ struct Cursor {
     left -= kOver;
     if (++block < blocks) return;
     block = 0;
-    h += 1 << c.side;
+    h += 1 << side;
     if (h < c.heads) return;
     h = 0;
     ++i;
@@ -237,20 +237,22 @@ struct Cursor {
   }
 };
 
-// WHOLE: pages are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly apart.
-template <int KIND, int DP, int NB, bool WHOLE>
+// SIDE: the warps of a CTA take 1 << c.side neighbouring kv heads (see heads_side_by_side in kv_cache.cpp), else one.  WHOLE: pages
+// are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly apart.
+template <int KIND, int DP, int NB, bool SIDE, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
   using S = Shape<KIND, DP, NB>;
   constexpr int PIECES = S::kPieces, KSTEPS = DP / 16;
+  const int32_t side = SIDE ? c.side : 0;
   extern __shared__ __align__(128) char room[];
   __shared__ Shared sh;
   begin_kernel();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t tiles_at = smem_of(room + warp * S::kRoom);
   const int32_t group = a.heads / c.heads, blocks = (group + S::kHeads - 1) / S::kHeads;
-  const int32_t per_row = (c.heads >> c.side) * blocks;  // unit rows of a row
-  const int32_t part_of_side = warp & ((1 << c.side) - 1), rank = warp >> c.side;  // the warp's kv head and tokens of a unit
-  const int32_t tile_log = S::kTileLog - c.side;
+  const int32_t per_row = (c.heads >> side) * blocks;  // unit rows of a row
+  const int32_t part_of_side = warp & ((1 << side) - 1), rank = warp >> side;  // the warp's kv head and tokens of a unit
+  const int32_t tile_log = S::kTileLog - side;
 
   // ---- this CTA's range of the units: a thread sums those of consecutive rows, the CTA scans the threads' sums.
   const int32_t each = (a.n + kThreads - 1) / kThreads, r0 = threadIdx.x * each;
@@ -301,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   {
     const int64_t in = x0 - sh.before * per_row;
     const int32_t units = here.nt + kOver, pair = (int32_t)(in / units), u = (int32_t)(in % units);
-    here.h = pair / blocks << c.side;
+    here.h = pair / blocks << side;
     here.block = pair % blocks;
     here.t = u > kOver ? u - kOver : 0;
     here.left = x_end - x0 - (u < kOver ? kOver - u : 0);
@@ -355,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
           copy16(d + S::kArray, from + across, in);
         }
       }
-      ahead.advance<WHOLE>(1, c, a, blocks, tile_log);
+      ahead.advance<WHOLE>(1, c, a, blocks, side, tile_log);
     }
     commit();
   };
@@ -374,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         k.at = layer_at + ahead.h * c.head_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
         if (k.page < 0) k.page = INT32_MAX;
       }
-      ahead.advance<WHOLE>(1, c, a, blocks, tile_log);
+      ahead.advance<WHOLE>(1, c, a, blocks, side, tile_log);
     }
     return k;
   };
@@ -610,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
       }
     }
     float* const sums = (float*)(room + warp * S::kRoom + (slot ? slot - 1 : S::kStages - 1) * S::kStage);  // (the last tile's room: it is not filled before the next step)
-    here.advance<WHOLE>(count, c, a, blocks, tile_log);
+    here.advance<WHOLE>(count, c, a, blocks, side, tile_log);
     if (here.left > 0) load_queries(here);  // (on their way while this unit row's parts are joined)
 
     __syncwarp();  // every lane is done with the last tile
@@ -621,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     const bool whole = u.t == 0 && count == u.nt, empty = u.row.end <= u.row.begin;
     const int64_t unit0 = x_end - u.left - u.t;  // where the unit row's first tile stands among all units
     // A part: the sums [kv head of the unit][query head][dim], then the maxima, then the sums of exp.
-    const int32_t part_heads = S::kHeads << c.side;
+    const int32_t part_heads = S::kHeads << side;
     const int64_t part_size = (int64_t)part_heads * (DP + 2);
     float* const part = w.parts + (blockIdx.x * 4 + (u.t == 0)) * part_size;
 #pragma unroll
@@ -643,17 +645,17 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         }
       }
       __syncthreads();
-      for (int y = threadIdx.x; y < 8 * DP / 4 << c.side; y += kThreads) {
+      for (int y = threadIdx.x; y < 8 * DP / 4 << side; y += kThreads) {
         const int beside = y / (8 * DP / 4), head = y / (DP / 4) % 8, d = y % (DP / 4) * 4, h8 = b * 8 + head;
         float t = -INFINITY, z = 0.f;
 #pragma unroll
         for (int k = 0; k < kWarps; ++k)  // the warps that had this kv head
-          if ((k & ((1 << c.side) - 1)) == beside) t = fmaxf(t, sh.top[k][head]);
+          if ((k & ((1 << side) - 1)) == beside) t = fmaxf(t, sh.top[k][head]);
         const float ref = t == -INFINITY ? 0.f : t;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < kWarps; ++k)
-          if ((k & ((1 << c.side) - 1)) == beside) {
+          if ((k & ((1 << side) - 1)) == beside) {
             const float fade = exp2_fast(sh.top[k][head] - ref);
             const float4 f = *(const float4*)(sums + (k - warp) * (S::kRoom / 4) + head * S::kSumPitch + (d ^ head * 4));
             z += fade * sh.sum[k][head];
@@ -666,8 +668,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         } else if (h8 < heads) {
           const int32_t q_head = head0 + beside * group + h8;
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
-          store4(c, a, u.i, q_head, d, v, v_scale / z, empty);
-          if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = empty ? -INFINITY : (t + log2f(z)) / kLog2e;
+          store4(c, a, u.i, q_head, d, v, __fdividef(v_scale, z), empty);
+          if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = empty ? -INFINITY : (t + __log2f(z)) * kLn2;
         }
       }
       if (whole || b + 1 < NB) __syncthreads();  // the sums' room is free again
@@ -679,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     // parts in their order, kJoin of which are on their way at a time; with few values, groups of threads take every so
     // many parts, and the first group puts theirs together.
     const int32_t c0 = (int32_t)(((unit0 + 1) * ctas - 1) / total), c1 = (int32_t)(((unit0 + u.nt) * ctas - 1) / total);
-    const int32_t parts = c1 - c0 + 1, all4 = (heads << c.side) * (DP / 4), turns = (all4 + kThreads - 1) / kThreads;
+    const int32_t parts = c1 - c0 + 1, all4 = (heads << side) * (DP / 4), turns = (all4 + kThreads - 1) / kThreads;
     const int32_t teams = max(1, kThreads / all4);
     int32_t near = parts;
     if (parts * turns > 4 * kJoin * teams) {
@@ -760,8 +762,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
           if (done) {
             const int32_t q_head = head0 + beside * group + head;
             const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
-            store4(c, a, u.i, q_head, d, v, v_scale / z, false);
-            if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = (t + log2f(z)) / kLog2e;
+            store4(c, a, u.i, q_head, d, v, __fdividef(v_scale, z), false);
+            if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = (t + __log2f(z)) * kLn2;
           } else {
             *(float4*)(joined + at * DP + d) = v;
             if (d == 0) joined[part_heads * DP + at] = t, joined[part_heads * (DP + 1) + at] = z;
@@ -777,44 +779,44 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
 }
 
 // With q = NULL the kernel is only made ready for launches.
-template <int KIND, int DP, int NB, bool WHOLE>
+template <int KIND, int DP, int NB, bool SIDE, bool WHOLE>
 cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   using S = Shape<KIND, DP, NB>;
-  const auto kernel = attend_kernel<KIND, DP, NB, WHOLE>;
+  const auto kernel = attend_kernel<KIND, DP, NB, SIDE, WHOLE>;
   if (!q) return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
   // As many CTAs as are resident together (by shared memory: 227 KB an SM, of which each CTA takes 1 KB for the system).
   static_assert(S::kCtas <= KvAttendScratch::kCtasPerSm, "the scratch is for so many");
   return launch_early(kernel, dim3(S::kCtas * num_sms), kThreads, S::kBytes, st, c, *q, w);
 }
 
-template <int KIND, int DP, int NB>
+template <int KIND, int DP, int NB, bool SIDE>
 cudaError_t launch_pages(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  return c.page % 16 == 0 ? launch<KIND, DP, NB, true>(c, q, w, num_sms, st) : launch<KIND, DP, NB, false>(c, q, w, num_sms, st);
+  return c.page % 16 == 0 ? launch<KIND, DP, NB, SIDE, true>(c, q, w, num_sms, st) : launch<KIND, DP, NB, SIDE, false>(c, q, w, num_sms, st);
 }
 
 // (Blocks of 16 query heads take 160 registers and more beyond DP = 128: blocks of eight, whose keys and values the second finds in L2.)
-template <int KIND, int DP>
+template <int KIND, int DP, bool SIDE>
 cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   if constexpr (DP > 128) {
-    return launch_pages<KIND, DP, 1>(c, q, w, num_sms, st);
+    return launch_pages<KIND, DP, 1, SIDE>(c, q, w, num_sms, st);
   } else {
     if (!q) {
-      const cudaError_t e = launch_pages<KIND, DP, 1>(c, q, w, num_sms, st);
-      return e == cudaSuccess ? launch_pages<KIND, DP, 2>(c, q, w, num_sms, st) : e;
+      const cudaError_t e = launch_pages<KIND, DP, 1, SIDE>(c, q, w, num_sms, st);
+      return e == cudaSuccess ? launch_pages<KIND, DP, 2, SIDE>(c, q, w, num_sms, st) : e;
     }
-    return q->heads / c.heads <= 8 ? launch_pages<KIND, DP, 1>(c, q, w, num_sms, st) : launch_pages<KIND, DP, 2>(c, q, w, num_sms, st);
+    return q->heads / c.heads <= 8 ? launch_pages<KIND, DP, 1, SIDE>(c, q, w, num_sms, st) : launch_pages<KIND, DP, 2, SIDE>(c, q, w, num_sms, st);
   }
 }
 
-template <int KIND>
+template <int KIND, bool SIDE>
 cudaError_t launch_dim(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   constexpr int k80 = KIND == P2P_KV_E4M3 ? 96 : 80;  // (80 values of 8 bits are five pieces, not whole turns)
-  return c.dim <= 64    ? launch_heads<KIND, 64>(c, q, w, num_sms, st)
-         : c.dim <= k80 ? launch_heads<KIND, k80>(c, q, w, num_sms, st)
-         : c.dim <= 96  ? launch_heads<KIND, 96>(c, q, w, num_sms, st)
-         : c.dim <= 128 ? launch_heads<KIND, 128>(c, q, w, num_sms, st)
-         : c.dim <= 192 ? launch_heads<KIND, 192>(c, q, w, num_sms, st)
-                        : launch_heads<KIND, 256>(c, q, w, num_sms, st);
+  return c.dim <= 64    ? launch_heads<KIND, 64, SIDE>(c, q, w, num_sms, st)
+         : c.dim <= k80 ? launch_heads<KIND, k80, SIDE>(c, q, w, num_sms, st)
+         : c.dim <= 96  ? launch_heads<KIND, 96, SIDE>(c, q, w, num_sms, st)
+         : c.dim <= 128 ? launch_heads<KIND, 128, SIDE>(c, q, w, num_sms, st)
+         : c.dim <= 192 ? launch_heads<KIND, 192, SIDE>(c, q, w, num_sms, st)
+                        : launch_heads<KIND, 256, SIDE>(c, q, w, num_sms, st);
 }
 
 }  // namespace

@@ -101,7 +101,11 @@ int32_t heads_side_by_side(const p2p::KvView& c) {
 }
 
 cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p::KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  const auto launch = c.type == P2P_KV_BF16 ? p2p::launch_kv_attend_bf16 : c.type == P2P_KV_F16 ? p2p::launch_kv_attend_f16 : p2p::launch_kv_attend_e4m3;
+  using namespace p2p;
+  const auto launch = c.side == 0 ? (c.type == P2P_KV_BF16 ? launch_kv_attend_bf16 : c.type == P2P_KV_F16 ? launch_kv_attend_f16 : launch_kv_attend_e4m3)
+                                  : (c.type == P2P_KV_BF16  ? launch_kv_attend_bf16_side
+                                     : c.type == P2P_KV_F16 ? launch_kv_attend_f16_side
+                                                            : launch_kv_attend_e4m3_side);
   return launch(c, q, w, num_sms, st);
 }
 
