@@ -69,9 +69,10 @@ struct Shape {
   static constexpr int kRowBytes = DP * Type<KIND>::kSize;
   static constexpr int kPieces = kRowBytes / 16;               // 16-byte pieces of a row
   static_assert(kPieces % 2 == 0, "a tile's pieces are whole turns of the warp");
-  // Tokens that a warp takes at a time: 32 of small rows, whose products weigh little beside what a turn of the loop costs
-  // (256 sequences of 8-bit values of 64: 83 us with 16, 65 with 32).
-  static constexpr int kRows = kRowBytes <= 128 ? 32 : 16;
+  // Tokens that a warp takes at a time: 32 of small 8-bit rows, where a turn of the loop costs much beside the bytes it takes
+  // (256 sequences of 8-bit values of 64: 83 us with 16, 65 with 32).  Of 16-bit values of 64, 131,071 tokens take 49.3 and
+  // 47.9 us, but 512 sequences of 10 to 300 tokens 13.6 and 14.8: there smaller tiles fit rows better.
+  static constexpr int kRows = KIND == P2P_KV_E4M3 && kRowBytes <= 128 ? 32 : 16;
   static constexpr int kTileLog = kRows == 32 ? 7 : 6;         // (log2) that a CTA takes at a time, of one head
   static_assert(kWarps * kRows == 1 << kTileLog);
   static constexpr int kArray = kRows * kRowBytes;             // keys (or values) of a warp's tile
