@@ -280,7 +280,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     all += sh.sums[k];
   }
   const int64_t total = all * per_row;
-  const int64_t ctas = total < gridDim.x ? total : gridDim.x;
+  // Two units a CTA at least: fewer parts to join (one sequence of 3,000 tokens with 8 kv heads: 11.0 us with one, 10.0 with two).
+  const int64_t ctas = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
   if (blockIdx.x >= ctas) return;
   const int64_t x0 = total * blockIdx.x / ctas, x_end = total * (blockIdx.x + 1) / ctas;
   before += scan - mine;
