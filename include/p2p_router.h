@@ -345,22 +345,22 @@ int p2p_route_decide(p2p_router* r, const int32_t* match, int64_t B, const int32
 
 /* ---- paged key-value cache (UpdateKVCache, EvictKVCache and the cache's part of RunInfer, Algorithm 1) --------
  *
- * The node's own trie says which prefixes its KV cache holds; these calls keep that cache.  Keys and values lie in pages
- * of page_tokens tokens; table[s * max_pages + e] is the page of tokens e * page_tokens .. of sequence s, length[s] how
- * many tokens it holds, refs[p] how many table entries within their sequences' lengths name page p (0: free).  A hit
- * forks the matched tokens of a cached sequence (p2p_kv_fork: pages are shared), the rest of the prompt is appended
- * (p2p_kv_extend finds pages, p2p_kv_write fills them, layer by layer or all at once), every new token attends over its
- * sequence (p2p_kv_attend), evicted tokens are cut off (p2p_kv_trim, as EvictLRUTrie removes them from the end), and the
- * pages in use are moved together when a part of the pool is wanted back (p2p_kv_compact).
+ * The node's own trie says which prefixes its KV cache holds; these calls keep that cache.  Keys and values lie in
+ * pages of page_tokens tokens; table[s * max_pages + e] is the page of tokens e * page_tokens .. of sequence s,
+ * length[s] how many tokens it holds, refs[p] how many table entries within their sequences' lengths name page p (0:
+ * free).  A hit forks the matched tokens of a cached sequence (p2p_kv_fork: pages are shared), the rest of the prompt
+ * is appended (p2p_kv_extend finds pages, p2p_kv_write fills them, layer by layer or all at once), every new token
+ * attends over its sequence (p2p_kv_attend), evicted tokens are cut off (p2p_kv_trim, as EvictLRUTrie removes them from
+ * the end), and the pages in use are moved together when a part of the pool is wanted back (p2p_kv_compact).
  *
  * Conventions
  *   - Every array, the pages, table, length and refs among them, is the caller's and in DEVICE memory.  The caller sets
  *     them up (all of length and refs zero: an empty cache) and may read them in stream order; between calls it changes
  *     the contents of pages at will, table, length and refs only so that they hold together.
  *   - Calls return before their work is done and neither allocate nor wait, but p2p_kv_create, _destroy, _set_stream,
- *     _sync and _stats; they may be captured in a CUDA graph.  Work goes to the handle's stream (NULL, the legacy default
- *     stream, at first); arrays used on other streams are the caller's to order.  Calls of one handle share its scratch:
- *     they may not overlap, replays of captured graphs included.
+ *     _sync and _stats; they may be captured in a CUDA graph.  Work goes to the handle's stream (NULL, the legacy
+ *     default stream, at first); arrays used on other streams are the caller's to order.  Calls of one handle share its
+ *     scratch: they may not overlap, replays of captured graphs included.
  *   - Table entries past a sequence's length mean nothing.  A sequence is named once in a call's list.
  *   - A call whose items do not hold (see each call) changes nothing, and neither does any later call on the tables or
  *     p2p_kv_write, until p2p_kv_sync has reported it.
@@ -393,9 +393,9 @@ typedef struct p2p_kv_layout {
   int32_t *refs;        /* int32[n_pages] */
 } p2p_kv_layout;
 
-/* A handle on the cache `layout` describes, on the current CUDA device; its scratch (8 to 61 MB by head_dim and order, and
- * up to 20 bytes a page and 32 a sequence) is allocated here.  The arrays stay the caller's and must outlive the handle.
- * Errors: P2P_E_INVAL (message of p2p_kv_last_error(NULL)), P2P_E_NOMEM, P2P_E_CUDA. */
+/* A handle on the cache `layout` describes, on the current CUDA device; its scratch (8 to 61 MB by head_dim and order,
+ * and up to 20 bytes a page and 32 a sequence) is allocated here.  The arrays stay the caller's and must outlive the
+ * handle. Errors: P2P_E_INVAL (message of p2p_kv_last_error(NULL)), P2P_E_NOMEM, P2P_E_CUDA. */
 int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out);
 
 /* Frees the handle and its scratch (after finishing its queued work).  NULL is a no-op. */
@@ -414,40 +414,40 @@ const char* p2p_kv_last_error(const p2p_kv* kv);
 /* Number of CUDA kernels the handle has launched. */
 int64_t p2p_kv_launch_count(const p2p_kv* kv);
 
-/* out[0] pages in use, out[1] pages shared by several sequences, out[2] the highest page in use + 1, out[3] tokens held by
- * all sequences (shared ones counted for each).  Waits for queued work. */
+/* out[0] pages in use, out[1] pages shared by several sequences, out[2] the highest page in use + 1, out[3] tokens held
+ * by all sequences (shared ones counted for each).  Waits for queued work. */
 int p2p_kv_stats(p2p_kv* kv, int64_t out[4]);
 
-/* Room for count[i] more tokens in each of the n sequences seq[i] (int32[n]; n <= n_seqs): lengths grow, and new pages are
- * the free ones with the lowest numbers, handed out in the order of the list and of the tokens.  A last page that is
- * partly used and shared (refs above 1 when the call begins) is first copied, as far as it is used and in all layers, to a
- * page of its own, which is the first the sequence takes; the one it shared loses a reference and is not handed out by
- * the same call.  The new tokens' keys and values are p2p_kv_write's.  Device-side errors: a sequence out of range or
- * named twice, a negative count, more tokens than table entries hold, too few free pages. */
+/* Room for count[i] more tokens in each of the n sequences seq[i] (int32[n]; n <= n_seqs): lengths grow, and new pages
+ * are the free ones with the lowest numbers, handed out in the order of the list and of the tokens.  A last page that
+ * is partly used and shared (refs above 1 when the call begins) is first copied, as far as it is used and in all
+ * layers, to a page of its own, which is the first the sequence takes; the one it shared loses a reference and is not
+ * handed out by the same call.  The new tokens' keys and values are p2p_kv_write's.  Device-side errors: a sequence out
+ * of range or named twice, a negative count, more tokens than table entries hold, too few free pages. */
 int p2p_kv_extend(p2p_kv* kv, int32_t n, const int32_t* seq, const int32_t* count);
 
-/* Keys and values of layers layer .. layer + n_layers - 1 for the last offsets[i+1] - offsets[i] tokens of each sequence
- * seq[i], i < n <= n_seqs (int64 offsets[n+1], non-decreasing, within [0, n_tokens]); row t of k and v is token t of the
- * batch: (k or v)[l * layer_stride + t * token_stride + h * head_stride + x], strides in values, l from 0.  type: the
- * cache's, stored as it is; for P2P_KV_E4M3 P2P_KV_BF16 or P2P_KV_F16, stored as value / scale rounded to the nearest
- * (ties to even) and at most 448 in magnitude.  Rows in no sequence's range are left out.  A page that
- * is shared is not written (p2p_kv_extend gives a sequence pages of its own): a device-side error, as are offsets or
+/* Keys and values of layers layer .. layer + n_layers - 1 for the last offsets[i+1] - offsets[i] tokens of each
+ * sequence seq[i], i < n <= n_seqs (int64 offsets[n+1], non-decreasing, within [0, n_tokens]); row t of k and v is
+ * token t of the batch: (k or v)[l * layer_stride + t * token_stride + h * head_stride + x], strides in values, l from
+ * 0.  type: the cache's, stored as it is; for P2P_KV_E4M3 P2P_KV_BF16 or P2P_KV_F16, stored as value / scale rounded to
+ * the nearest (ties to even) and at most 448 in magnitude.  Rows in no sequence's range are left out.  A page that is
+ * shared is not written (p2p_kv_extend gives a sequence pages of its own): a device-side error, as are offsets or
  * counts out of range; what is wrong is left out, the rest is written. */
 int p2p_kv_write(p2p_kv* kv, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq, const int64_t* offsets,
                  int64_t n_tokens, const void* k, const void* v, int64_t layer_stride, int64_t token_stride,
                  int64_t head_stride, int32_t type);
 
-/* Each sequence dst[i], which must be empty, becomes the first n_tokens[i] tokens of sequence src[i] (int32[n] each; n <=
- * n_seqs) by sharing their pages.  Device-side errors: a sequence out of range, a dst named twice or not empty, more
+/* Each sequence dst[i], which must be empty, becomes the first n_tokens[i] tokens of sequence src[i] (int32[n] each; n
+ * <= n_seqs) by sharing their pages.  Device-side errors: a sequence out of range, a dst named twice or not empty, more
  * tokens than src holds when the call begins. */
 int p2p_kv_fork(p2p_kv* kv, int32_t n, const int32_t* src, const int32_t* dst, const int32_t* n_tokens);
 
-/* Cuts each of the n sequences seq[i] down to its first n_tokens[i] tokens (0: frees it); pages that no sequence names any
- * more are free.  Device-side errors: a sequence out of range or named twice, more tokens than it holds. */
+/* Cuts each of the n sequences seq[i] down to its first n_tokens[i] tokens (0: frees it); pages that no sequence names
+ * any more are free.  Device-side errors: a sequence out of range or named twice, more tokens than it holds. */
 int p2p_kv_trim(p2p_kv* kv, int32_t n, const int32_t* seq, const int32_t* n_tokens);
 
-/* Moves the pages in use to the front of the pool: with n of them, those numbered n and up go, in ascending order, to the
- * free ones below n, in ascending order; contents, table and refs follow. */
+/* Moves the pages in use to the front of the pool: with n of them, those numbered n and up go, in ascending order, to
+ * the free ones below n, in ascending order; contents, table and refs follow. */
 int p2p_kv_compact(p2p_kv* kv);
 
 /* Attention of one new token of each of n sequences seq[i] (NULL: sequences 0 .. n-1; one may be named again) over the
@@ -455,9 +455,9 @@ int p2p_kv_compact(p2p_kv* kv);
  * key-value head h / (n_heads / the cache's heads), and tokens t of the last `window` (0: all),
  *   out[i * out_row_stride + h * out_head_stride + x] = sum_t p_t v_t[x],   p = softmax over t of scale * (q . k_t),
  *   lse[i * n_heads + h] (float, nullable) = ln sum_t exp(scale * (q . k_t)),
- * q[i * q_row_stride + h * q_head_stride + x] of `type` like out: the cache's, for P2P_KV_E4M3 P2P_KV_BF16 or P2P_KV_F16.
- * Sums are held in 32 bits.  A sequence without tokens gives 0 and -infinity.  Device-side errors: a sequence or a page
- * out of range. */
+ * q[i * q_row_stride + h * q_head_stride + x] of `type` like out: the cache's, for P2P_KV_E4M3 P2P_KV_BF16 or
+ * P2P_KV_F16.  Sums are held in 32 bits.  A sequence without tokens gives 0 and -infinity.  Device-side errors: a
+ * sequence or a page out of range. */
 int p2p_kv_attend(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, const void* q, int64_t q_row_stride,
                   int64_t q_head_stride, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
                   int64_t out_row_stride, int64_t out_head_stride, float* lse);

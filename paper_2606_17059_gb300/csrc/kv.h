@@ -11,8 +11,8 @@
 namespace p2p {
 
 // Division of x < 2^31 by a fixed 1 <= d < 2^31: floor(x / d) = (x * mul) >> shift with shift = 31 + ceil(log2 d) and
-// mul = ceil(2^shift / d) = (2^shift + e) / d, 0 <= e < d.  The product over 2^shift is x / d + (x * e / 2^shift) / d; as
-// x * e < 2^shift, that is less than 1 / d above x / d, which does not reach the next whole number.
+// mul = ceil(2^shift / d) = (2^shift + e) / d, 0 <= e < d.  The product over 2^shift is x / d + (x * e / 2^shift) /
+// d; as x * e < 2^shift, that is less than 1 / d above x / d, which does not reach the next whole number.
 struct FastDiv {
   uint32_t d = 1, shift = 31;
   uint64_t mul = 1ull << 31;
@@ -27,11 +27,12 @@ struct FastDiv {
   __host__ __device__ __forceinline__ uint32_t ceil(uint32_t x) const { return x ? div(x - 1) + 1 : 0; }
 };
 
-// The cache's kernels are launched so that one may start while the one before it on the stream still runs; each waits for
-// that one's end before its first access to memory (begin_kernel) and lets the next start at once.  A short call's launch is
-// hidden that way.
+// The cache's kernels are launched so that one may start while the one before it on the stream still runs; each waits
+// for that one's end before its first access to memory (begin_kernel) and lets the next start at once.  A short
+// call's launch is hidden that way.
 template <class... P, class... A>
-cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t shared, cudaStream_t st, const A&... args) {
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t shared, cudaStream_t st,
+                         const A&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads);
@@ -86,7 +87,8 @@ struct KvScratch {
 cudaError_t prepare_kv_pages();  // makes the kernels ready for launches (at creation)
 cudaError_t launch_kv_extend(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* count,
                              int num_sms, cudaStream_t st);
-cudaError_t launch_kv_trim(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* to, cudaStream_t st);
+cudaError_t launch_kv_trim(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* to,
+                           cudaStream_t st);
 cudaError_t launch_kv_fork(const KvView& c, const KvScratch& s, int32_t n, const int32_t* src, const int32_t* dst,
                            const int32_t* tokens, cudaStream_t st);
 cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, cudaStream_t st);
@@ -96,8 +98,9 @@ struct KvRows {
   int64_t layer_stride, token_stride, head_stride;
   int32_t type;
 };
-cudaError_t launch_kv_write(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq,
-                            const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_write(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n,
+                            const int32_t* seq, const int64_t* offsets, int64_t n_tokens, const KvRows& rows,
+                            int num_sms, cudaStream_t st);
 // out (zeroed by the launch): pages in use, pages shared, the highest page in use + 1, tokens held.
 cudaError_t launch_kv_stats(const KvView& c, unsigned long long* out, int num_sms, cudaStream_t st);
 
@@ -113,7 +116,8 @@ struct KvQuery {
   // Whether rows of q may be read by twos, and those of out written by fours, of their values.
   bool q_pairs, out_fours;
 };
-// Parts of rows that several CTAs share, four a CTA (see the kernel), and how many have arrived (zero between launches).
+// Parts of rows that several CTAs share, four a CTA (see the kernel), and how many have arrived (zero between
+// launches).
 struct KvAttendScratch {
   static constexpr int kCtasPerSm = 3;
   float* parts;      // [kv_attend_parts()]
@@ -122,15 +126,22 @@ struct KvAttendScratch {
 };
 // Floats of `parts`: head_dim as the kernels pad it, at most, and blocks of 8 or 16 query heads of up to 4 kv heads.
 inline size_t kv_attend_parts(const KvView& c, int num_sms) {
-  const int32_t dp = c.dim <= 64 ? 64 : c.dim <= 96 ? 96 : c.dim <= 128 ? 128 : c.dim <= 192 ? 192 : 256, heads = dp > 128 ? 8 : 16;
+  const int32_t dp = c.dim <= 64 ? 64 : c.dim <= 96 ? 96 : c.dim <= 128 ? 128 : c.dim <= 192 ? 192 : 256,
+      heads = dp > 128 ? 8 : 16;
   return (size_t)4 * KvAttendScratch::kCtasPerSm * num_sms * (heads << c.side) * (dp + 2);
 }
 // With q = NULL they launch nothing, but make the cache's kernels ready for launches (at creation).
-cudaError_t launch_kv_attend_bf16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
-cudaError_t launch_kv_attend_bf16_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
-cudaError_t launch_kv_attend_f16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
-cudaError_t launch_kv_attend_f16_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
-cudaError_t launch_kv_attend_e4m3(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
-cudaError_t launch_kv_attend_e4m3_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_attend_bf16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                  cudaStream_t st);
+cudaError_t launch_kv_attend_bf16_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                       cudaStream_t st);
+cudaError_t launch_kv_attend_f16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                 cudaStream_t st);
+cudaError_t launch_kv_attend_f16_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                      cudaStream_t st);
+cudaError_t launch_kv_attend_e4m3(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                  cudaStream_t st);
+cudaError_t launch_kv_attend_e4m3_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                       cudaStream_t st);
 
 }  // namespace p2p

@@ -5,30 +5,34 @@
 //
 // Keys and values are read once, and that is what bounds it: with g query heads a kv head, 4 g dim operations go with
 // 4 dim bytes, g a byte (2 g with 8 bits), where the GPU has 277 operations of its tensor cores for a byte of memory.
-// Measured (one GB300, copy bandwidth 6.8 TB/s): 32 sequences of 4,352 to 33,792 tokens, 40 / 8 heads of 128 f16 values,
-// 1.88 GB in 277 us (the copy bandwidth); one sequence of 131,071 tokens, 32 / 8 heads, 0.54 GB in 85 us (93%); 256
-// sequences of 128 to 4,224 tokens in 8 bits, 64 / 8 heads, 0.61 GB in 105 us (87%: there the widening of the values
-// and the ends of the rows weigh); one of 540 tokens 7.5 us, a chain of a launch, four loads, a tile and the join.
+// Measured (one GB300, copy bandwidth 6.8 TB/s): 32 sequences of 4,352 to 33,792 tokens, 40 / 8 heads of 128 f16
+// values, 1.88 GB in 277 us (the copy bandwidth); one sequence of 131,071 tokens, 32 / 8 heads, 0.54 GB in 85 us
+// (93%); 256 sequences of 128 to 4,224 tokens in 8 bits, 64 / 8 heads, 0.61 GB in 105 us (87%: there the widening of
+// the values and the ends of the rows weigh); one of 540 tokens 7.0 us, a chain of a launch, four loads, a tile and
+// the join.
 //
 // The work is cut into units of 64 or 128 tokens of a (sequence, kv head, block of its query heads), numbered in that
 // order, and every CTA takes an equal, contiguous range of them: one long sequence fills the GPU as a batch does.  A
-// range's parts of a unit row that it shares with other CTAs go to scratch (maximum, sum, unnormalised out), and the CTA
-// that finishes such a row last joins its parts, in their order: results do not depend on timing.  (The start of a unit
-// row counts as kOver units more, for what its end costs: with 1 instead of 3, the 256 sequences in 8 bits take 115 us.)
+// range's parts of a unit row that it shares with other CTAs go to scratch (maximum, sum, unnormalised out), and the
+// CTA that finishes such a row last joins its parts, in their order: results do not depend on timing.  (The start of
+// a unit row counts as kOver units more, for what its end costs: with 1 instead of 3, the 256 sequences in 8 bits
+// take 115 us.)
 //
 // Each warp streams 16 or 32 tokens at a time through shared memory of its own, up to seven tiles ahead (cp.async, 16
 // bytes a lane, 16-byte pieces turned so that ldmatrix meets no bank twice), with no barrier between warps inside a
-// unit row; the copies run on into the next unit row while this one's parts are joined.  Where pages are whole sixteens
-// of tokens, a lane looks up the page of a whole tile ahead, for 32 tiles at once; else each token's is looked up two
-// tiles ahead.  Sixteen tokens are multiplied transposed: S^T [tokens, heads] = K Q^T and O^T [dim, heads] += V^T P^T,
-// so that eight query heads fill a product's n and the tokens (or values) its m of 16.  P^T goes from the first product's
-// layout to the second's by two 8 x 8 transposes of registers.  exp(x - m) takes for m not the running maximum but one
-// that lags it by at most a factor of 2^8, so that a tile's maximum is only reduced, and O rescaled, where it goes past
-// that.  P is rounded to the values' type (f16 for 8 bits) for its product; sums, maxima and O are held in 32 bits.
+// unit row; the copies run on into the next unit row while this one's parts are joined.  Where pages are whole
+// sixteens of tokens, a lane looks up the page of a whole tile ahead, for 32 tiles at once; else each token's is
+// looked up two tiles ahead.  Sixteen tokens are multiplied transposed: S^T [tokens, heads] = K Q^T and O^T [dim,
+// heads] += V^T P^T, so that eight query heads fill a product's n and the tokens (or values) its m of 16.  P^T goes
+// from the first product's layout to the second's by two 8 x 8 transposes of registers.  exp(x - m) takes for m not
+// the running maximum but one that lags it by at most a factor of 2^8, so that a tile's maximum is only reduced, and
+// O rescaled, where it goes past that.  P is rounded to the values' type (f16 for 8 bits) for its product; sums,
+// maxima and O are held in 32 bits.
 //
-// The products are warp-wide ones (mma): 9% of the tensor cores' time at the copy bandwidth (8 bits: 17%), and their operands come
-// out of shared memory by ldmatrix in any row size.  The tensor memory path (tcgen05) would free issue slots that 16-bit
-// values do not need and that 8-bit values, which have to be widened beside 16-bit queries, could not use it for.
+// The products are warp-wide ones (mma): 9% of the tensor cores' time at the copy bandwidth (8 bits: 17%), and their
+// operands come out of shared memory by ldmatrix in any row size.  The tensor memory path (tcgen05) would free issue
+// slots that 16-bit values do not need and that 8-bit values, which have to be widened beside 16-bit queries, could
+// not use it for.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -36,8 +40,8 @@
 
 #include "kv.h"
 
-// (No load here goes past the coherent path, as __ldg or const __restrict__ would have it: the kernel before may still be writing
-// when this one starts, see launch_early.)
+// (No load here goes past the coherent path, as __ldg or const __restrict__ would have it: the kernel before may
+// still be writing when this one starts, see launch_early.)
 
 namespace p2p {
 namespace {
@@ -69,9 +73,10 @@ struct Shape {
   static constexpr int kRowBytes = DP * Type<KIND>::kSize;
   static constexpr int kPieces = kRowBytes / 16;               // 16-byte pieces of a row
   static_assert(kPieces % 2 == 0, "a tile's pieces are whole turns of the warp");
-  // Tokens that a warp takes at a time: 32 of small 8-bit rows, where a turn of the loop costs much beside the bytes it takes
-  // (256 sequences of 8-bit values of 64: 83 us with 16, 65 with 32).  Of 16-bit values of 64, 131,071 tokens take 49.3 and
-  // 47.9 us, but 512 sequences of 10 to 300 tokens 13.6 and 14.8: there smaller tiles fit rows better.
+  // Tokens that a warp takes at a time: 32 of small 8-bit rows, where a turn of the loop costs much beside the bytes
+  // it takes (256 sequences of 8-bit values of 64: 83 us with 16, 65 with 32).  Of 16-bit values of 64, 131,071
+  // tokens take 49.3 and 47.9 us, but 512 sequences of 10 to 300 tokens 13.6 and 14.8: there smaller tiles fit rows
+  // better.
   static constexpr int kRows = KIND == P2P_KV_E4M3 && kRowBytes <= 128 ? 32 : 16;
   static constexpr int kTileLog = kRows == 32 ? 7 : 6;         // (log2) that a CTA takes at a time, of one head
   static_assert(kWarps * kRows == 1 << kTileLog);
@@ -119,11 +124,13 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 template <int KIND>
 __device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
   if (KIND == P2P_KV_BF16)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+                 "{%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+                 "{%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
@@ -161,8 +168,8 @@ __device__ __forceinline__ float2 two_halves(uint32_t x, int32_t type) {
   return type == P2P_KV_BF16 ? __bfloat1622float2(*(const __nv_bfloat162*)&x) : __half22float2(*(const __half2*)&x);
 }
 // Values d .. d + 3 of a head's result, times f; zero: 0 in their place.
-__device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_t i, int32_t head, int32_t d, float4 v, float f,
-                                       bool zero) {
+__device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_t i, int32_t head, int32_t d, float4 v,
+                                       float f, bool zero) {
   if (d >= c.dim) return;  // (dim is a multiple of 8)
   if (zero) v = make_float4(0.f, 0.f, 0.f, 0.f), f = 0.f;
   const uint32_t x = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.x * f, v.y * f) : pack<P2P_KV_F16>(v.x * f, v.y * f);
@@ -188,7 +195,9 @@ __device__ __forceinline__ uint32_t place(int row, int piece) {
 struct Row {
   int32_t seq, from, begin, end;
   // Units of 1 << tile_log tokens (one without any).
-  __device__ __forceinline__ int32_t tiles(int32_t tile_log) const { return end > begin ? ((end - from - 1) >> tile_log) + 1 : 1; }
+  __device__ __forceinline__ int32_t tiles(int32_t tile_log) const {
+    return end > begin ? ((end - from - 1) >> tile_log) + 1 : 1;
+  }
 };
 template <bool WHOLE>
 __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t i, int32_t* err) {
@@ -220,7 +229,8 @@ struct Cursor {
   int64_t left;  // units of the range from here on; none: at its end
   // k tiles on, none past the unit row's end.
   template <bool WHOLE>
-  __device__ __forceinline__ void advance(int32_t k, const KvView& c, const KvQuery& a, int32_t blocks, int32_t side, int32_t tile_log) {
+  __device__ __forceinline__ void advance(int32_t k, const KvView& c, const KvQuery& a, int32_t blocks, int32_t side,
+                                          int32_t tile_log) {
     t += k;
     left -= k;
     if (t < nt) return;
@@ -238,10 +248,12 @@ struct Cursor {
   }
 };
 
-// SIDE: the warps of a CTA take 1 << c.side neighbouring kv heads (see heads_side_by_side in kv_cache.cpp), else one.  WHOLE: pages
-// are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly apart.
+// SIDE: the warps of a CTA take 1 << c.side neighbouring kv heads (see heads_side_by_side in kv_cache.cpp), else
+// one.  WHOLE: pages are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly
+// apart.
 template <int KIND, int DP, int NB, bool SIDE, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
+__global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
+    attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
   using S = Shape<KIND, DP, NB>;
   constexpr int PIECES = S::kPieces, KSTEPS = DP / 16;
   const int32_t side = SIDE ? c.side : 0;
@@ -252,7 +264,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   const uint32_t tiles_at = smem_of(room + warp * S::kRoom);
   const int32_t group = a.heads / c.heads, blocks = (group + S::kHeads - 1) / S::kHeads;
   const int32_t per_row = (c.heads >> side) * blocks;  // unit rows of a row
-  const int32_t part_of_side = warp & ((1 << side) - 1), rank = warp >> side;  // the warp's kv head and tokens of a unit
+  // the warp's kv head and tokens of a unit
+  const int32_t part_of_side = warp & ((1 << side) - 1), rank = warp >> side;
   const int32_t tile_log = S::kTileLog - side;
 
   // ---- this CTA's range of the units: a thread sums those of consecutive rows, the CTA scans the threads' sums.
@@ -261,7 +274,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   for (int32_t i0 = r0; i0 < r0 + each && i0 < a.n; i0 += 4) {
     Row r[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = row_at<WHOLE>(c, a, i0 + k < r0 + each ? i0 + k : a.n, blockIdx.x == 0 ? w.err : nullptr);
+    for (int k = 0; k < 4; ++k)
+      r[k] = row_at<WHOLE>(c, a, i0 + k < r0 + each ? i0 + k : a.n, blockIdx.x == 0 ? w.err : nullptr);
 #pragma unroll
     for (int k = 0; k < 4; ++k) mine += i0 + k < r0 + each && i0 + k < a.n ? r[k].tiles(tile_log) + kOver : 0;
   }
@@ -280,7 +294,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     all += sh.sums[k];
   }
   const int64_t total = all * per_row;
-  // Two units a CTA at least: fewer parts to join (one sequence of 3,000 tokens with 8 kv heads: 11.0 us with one, 10.0 with two).
+  // Two units a CTA at least: fewer parts to join (one sequence of 3,000 tokens with 8 kv heads: 11.0 us with one,
+  // 10.0 with two).
   const int64_t ctas = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
   if (blockIdx.x >= ctas) return;
   const int64_t x0 = total * blockIdx.x / ctas, x_end = total * (blockIdx.x + 1) / ctas;
@@ -320,7 +335,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     return to;
   };
   const int64_t across = c.v - c.k, layer_at = (int64_t)a.layer * c.layer_stride + part_of_side * c.head_stride;
-  // WHOLE: lane l has where the sixteens of tile near_t + l of row near_i lie (< 0: none); the kv heads of a row share them.
+  // WHOLE: lane l has where the sixteens of tile near_t + l of row near_i lie (< 0: none); the kv heads of a row
+  // share them.
   constexpr int SIXTEENS = S::kRows / 16;
   int64_t near[SIXTEENS];
   int32_t near_i = -1, near_t = 0;
@@ -344,7 +360,9 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
       }
       const uint32_t to = next_slot();
       const int64_t t0 = (int64_t)ahead.row.from + ((int64_t)ahead.t << tile_log) + rank * S::kRows;
-      const int32_t lo = (int32_t)max(ahead.row.begin - t0, (int64_t)0), n = (int32_t)(min(ahead.row.end - t0, (int64_t)S::kRows) - lo);  // rows lo .. lo + n - 1
+      // rows lo .. lo + n - 1
+      const int32_t lo = (int32_t)max(ahead.row.begin - t0, (int64_t)0);
+      const int32_t n = (int32_t)(min(ahead.row.end - t0, (int64_t)S::kRows) - lo);
 #pragma unroll
       for (int m = 0; m < SIXTEENS; ++m) {
         const int64_t o = __shfl_sync(~0u, near[m], ahead.t - near_t);
@@ -371,7 +389,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   const auto look_up = [&]() {
     Token k = {-1, 0};
     if (ahead.left > 0) {
-      const int64_t t = (int64_t)ahead.row.from + ((int64_t)ahead.t << tile_log) + rank * S::kRows + (lane & (S::kRows - 1));
+      const int64_t t = (int64_t)ahead.row.from + ((int64_t)ahead.t << tile_log) + rank * S::kRows +
+          (lane & (S::kRows - 1));
       if (t < ahead.row.end) {
         const uint32_t e = c.by_page.div((uint32_t)t);
         k.page = c.table[(int64_t)ahead.row.seq * c.max_pages + e];
@@ -420,7 +439,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
   uint32_t q[KSTEPS][NB][2];
   float mul[NB][2];  // logit (in log2) of a sum, for the heads 2 * (lane % 4) + {0, 1} of a block
   const auto load_queries = [&](const Cursor& u) {
-    const int32_t head0 = (u.h + part_of_side) * group + u.block * S::kHeads, heads = min(group - u.block * S::kHeads, S::kHeads);
+    const int32_t head0 = (u.h + part_of_side) * group + u.block * S::kHeads,
+        heads = min(group - u.block * S::kHeads, S::kHeads);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int32_t head = b * 8 + lane / 4;
@@ -431,7 +451,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         for (int y = 0; y < 2; ++y) {
           const int d = KIND == P2P_KV_E4M3 ? 16 * k + 4 * (lane % 4) + 2 * y : 16 * k + 8 * y + 2 * (lane % 4);
           uint32_t v = 0;
-          if (head < heads && d < c.dim) v = a.q_pairs ? *(const uint32_t*)(from + d) : from[d] | (uint32_t)from[d + 1] << 16;
+          if (head < heads && d < c.dim)
+            v = a.q_pairs ? *(const uint32_t*)(from + d) : from[d] | (uint32_t)from[d + 1] << 16;
           q[k][b][y] = v;
         }
     }
@@ -509,7 +530,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
             load4(r, keys16 + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, k + (lane >> 4)));
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              const uint32_t f[4] = {widen(r[2 * y]), widen(r[2 * y + 1]), widen_high(r[2 * y]), widen_high(r[2 * y + 1])};
+              const uint32_t f[4] = {widen(r[2 * y]), widen(r[2 * y + 1]), widen_high(r[2 * y]),
+                                     widen_high(r[2 * y + 1])};
 #pragma unroll
               for (int b = 0; b < NB; ++b) multiply<KIND>(s[m][b], f, q[k + y][b]);
             }
@@ -524,7 +546,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
           }
         }
       }
-      const int32_t left = (int32_t)((uint32_t)u.row.end - (first + ((uint32_t)j << tile_log)));  // tokens that are seen, if not all
+      // The tile's tokens that are seen, if not all, and those before them that are not.
+      const int32_t left = (int32_t)((uint32_t)u.row.end - (first + ((uint32_t)j << tile_log)));
       bool past = false;
 #pragma unroll
       for (int m = 0; m < MB; ++m)
@@ -532,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int y = 0; y < 4; ++y) s[m][b][y] *= mul[b][y & 1];
-      const int32_t lead = WHOLE ? u.row.begin - (int32_t)(first + ((uint32_t)j << tile_log)) : 0;  // and that are not, before them
+      const int32_t lead = WHOLE ? u.row.begin - (int32_t)(first + ((uint32_t)j << tile_log)) : 0;
       if (left < S::kRows || lead > 0) {
 #pragma unroll
         for (int m = 0; m < MB; ++m)
@@ -594,8 +617,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
             load4t(r, values16 + place<PIECES>((lane & 7) + (lane >> 3 & 1) * 8, k + (lane >> 4)));
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              // A lane's register: values 2 * (lane / 4) + {0, 1} of one token, then of the next; the product's rows 0-7
-              // are the even values, 8-15 the odd ones.
+              // A lane's register: values 2 * (lane / 4) + {0, 1} of one token, then of the next; the product's rows
+              // 0-7 are the even values, 8-15 the odd ones.
               const uint32_t lo = __byte_perm(r[2 * y], 0, 0x3120), hi = __byte_perm(r[2 * y + 1], 0, 0x3120);
               const uint32_t f[4] = {widen(lo), widen_high(lo), widen(hi), widen_high(hi)};
 #pragma unroll
@@ -613,7 +636,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         }
       }
     }
-    float* const sums = (float*)(room + warp * S::kRoom + (slot ? slot - 1 : S::kStages - 1) * S::kStage);  // (the last tile's room: it is not filled before the next step)
+    // (the last tile's room: it is not filled before the next step)
+    float* const sums = (float*)(room + warp * S::kRoom + (slot ? slot - 1 : S::kStages - 1) * S::kStage);
     here.advance<WHOLE>(count, c, a, blocks, side, tile_log);
     if (here.left > 0) load_queries(here);  // (on their way while this unit row's parts are joined)
 
@@ -659,7 +683,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
         for (int k = 0; k < kWarps; ++k)
           if ((k & ((1 << side) - 1)) == beside) {
             const float fade = exp2_fast(sh.top[k][head] - ref);
-            const float4 f = *(const float4*)(sums + (k - warp) * (S::kRoom / 4) + head * S::kSumPitch + (d ^ head * 4));
+            const float* const his = sums + (k - warp) * (S::kRoom / 4);
+            const float4 f = *(const float4*)(his + head * S::kSumPitch + (d ^ head * 4));
             z += fade * sh.sum[k][head];
             v.x += fade * f.x, v.y += fade * f.y, v.z += fade * f.z, v.w += fade * f.w;
           }
@@ -678,23 +703,23 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
     }
     if (whole) continue;
 
-    // The CTA that brings the last part of the unit row joins them; where there are many, that of each `near` of them joins
-    // those, and the one that brings the last of the results joins these.  Each thread has four values of a head, over the
-    // parts in their order, kJoin of which are on their way at a time; with few values, groups of threads take every so
-    // many parts, and the first group puts theirs together.
+    // The CTA that brings the last part of the unit row joins them; where there are many, that of each `bunch` of
+    // them joins those, and the one that brings the last of the results joins these.  Each thread has four values of
+    // a head, over the parts in their order, kJoin of which are on their way at a time; with few values, groups of
+    // threads take every so many parts, and the first group puts theirs together.
     const int32_t c0 = (int32_t)(((unit0 + 1) * ctas - 1) / total), c1 = (int32_t)(((unit0 + u.nt) * ctas - 1) / total);
     const int32_t parts = c1 - c0 + 1, all4 = (heads << side) * (DP / 4), turns = (all4 + kThreads - 1) / kThreads;
     const int32_t teams = max(1, kThreads / all4);
-    int32_t near = parts;
+    int32_t bunch = parts;
     if (parts * turns > 4 * kJoin * teams) {
-      near = kJoin * teams;
-      while (near * near < parts) near += kJoin * teams;
+      bunch = kJoin * teams;
+      while (bunch * bunch < parts) bunch += kJoin * teams;
     }
-    int32_t first_part = (blockIdx.x - c0) / near * near, members = min(near, parts - first_part);
+    int32_t first_part = (blockIdx.x - c0) / bunch * bunch, members = min(bunch, parts - first_part);
     for (int32_t level = 0;; ++level) {
       // Part k lies with its CTA: the first CTA's is its range's last unit row, the others' their first.
       const auto part_of = [&](int32_t k) { return w.parts + ((c0 + k) * 4 + (k == 0) + 2 * level) * part_size; };
-      const int32_t apart = level ? near : 1;
+      const int32_t apart = level ? bunch : 1;
       // (The count is read and raised after the barrier, in acquire and release order for all of the CTA's accesses.)
       __syncthreads();
       if (threadIdx.x == 0) {
@@ -707,8 +732,10 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
       const bool done = level == 1 || members == parts;
       float* const joined = w.parts + ((c0 + first_part) * 4 + (first_part == 0) + 2) * part_size;
       for (int y0 = 0; y0 < all4; y0 += kThreads) {
-        const int y = teams > 1 ? (int)threadIdx.x % all4 : y0 + (int)threadIdx.x, team = teams > 1 ? threadIdx.x / all4 : 0;
-        const int own = y / (DP / 4), beside = own / heads, head = own % heads, at = beside * S::kHeads + head, d = y % (DP / 4) * 4;
+        const int y = teams > 1 ? (int)threadIdx.x % all4 : y0 + (int)threadIdx.x;
+        const int team = teams > 1 ? (int)threadIdx.x / all4 : 0;
+        const int own = y / (DP / 4), beside = own / heads, head = own % heads, at = beside * S::kHeads + head;
+        const int d = y % (DP / 4) * 4;
         float t = -INFINITY, z = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (y < all4 && team < teams) {
@@ -774,10 +801,11 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas) attend_k
       }
       if (done) break;
       first_part = 0;
-      members = (parts + near - 1) / near;
+      members = (parts + bunch - 1) / bunch;
     }
     __syncthreads();
   }
+  wait<0>();  // (of copies past the end of the range, of nothing, into room that is given back now)
 }
 
 // With q = NULL the kernel is only made ready for launches.
@@ -786,17 +814,20 @@ cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, 
   using S = Shape<KIND, DP, NB>;
   const auto kernel = attend_kernel<KIND, DP, NB, SIDE, WHOLE>;
   if (!q) return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
-  // As many CTAs as are resident together (by shared memory: 227 KB an SM, of which each CTA takes 1 KB for the system).
+  // As many CTAs as are resident together (by shared memory: 227 KB an SM, of which each CTA takes 1 KB for the
+  // system).
   static_assert(S::kCtas <= KvAttendScratch::kCtasPerSm, "the scratch is for so many");
   return launch_early(kernel, dim3(S::kCtas * num_sms), kThreads, S::kBytes, st, c, *q, w);
 }
 
 template <int KIND, int DP, int NB, bool SIDE>
 cudaError_t launch_pages(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  return c.page % 16 == 0 ? launch<KIND, DP, NB, SIDE, true>(c, q, w, num_sms, st) : launch<KIND, DP, NB, SIDE, false>(c, q, w, num_sms, st);
+  return c.page % 16 == 0 ? launch<KIND, DP, NB, SIDE, true>(c, q, w, num_sms, st)
+                          : launch<KIND, DP, NB, SIDE, false>(c, q, w, num_sms, st);
 }
 
-// (Blocks of 16 query heads take 160 registers and more beyond DP = 128: blocks of eight, whose keys and values the second finds in L2.)
+// (Blocks of 16 query heads take 160 registers and more beyond DP = 128: blocks of eight, whose keys and values the
+// second finds in L2.)
 template <int KIND, int DP, bool SIDE>
 cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   if constexpr (DP > 128) {
@@ -806,7 +837,8 @@ cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratc
       const cudaError_t e = launch_pages<KIND, DP, 1, SIDE>(c, q, w, num_sms, st);
       return e == cudaSuccess ? launch_pages<KIND, DP, 2, SIDE>(c, q, w, num_sms, st) : e;
     }
-    return q->heads / c.heads <= 8 ? launch_pages<KIND, DP, 1, SIDE>(c, q, w, num_sms, st) : launch_pages<KIND, DP, 2, SIDE>(c, q, w, num_sms, st);
+    return q->heads / c.heads <= 8 ? launch_pages<KIND, DP, 1, SIDE>(c, q, w, num_sms, st)
+                                   : launch_pages<KIND, DP, 2, SIDE>(c, q, w, num_sms, st);
   }
 }
 

@@ -1,8 +1,8 @@
 // kv_cache.cpp -- host side of the paged key-value cache: the p2p_kv_* calls of p2p_router.h.
 //
-// The pages, the page table, the lengths and the reference counts are the caller's arrays.  The handle holds the scratch
-// of the calls, allocated once at its creation, so that no call allocates or waits (but p2p_kv_sync, _stats and
-// _set_stream): a decode loop can be captured in a CUDA graph.
+// The pages, the page table, the lengths and the reference counts are the caller's arrays.  The handle holds the
+// scratch of the calls, allocated once at its creation, so that no call allocates or waits (but p2p_kv_sync, _stats
+// and _set_stream): a decode loop can be captured in a CUDA graph.
 #include <algorithm>
 #include <cstdio>
 #include <cstring>
@@ -69,16 +69,18 @@ int esize(int32_t type) { return type == P2P_KV_E4M3 ? 1 : 2; }
 const char* check_layout(const p2p_kv_layout& a) {
   if (a.type != P2P_KV_BF16 && a.type != P2P_KV_F16 && a.type != P2P_KV_E4M3) return "type is none of P2P_KV_*";
   if (a.n_layers < 1 || a.n_layers > 65536 || a.n_pages < 1 || a.n_pages > (1 << 30) || a.page_tokens < 1 ||
-      a.page_tokens > 4096 || a.n_heads < 1 || a.n_heads > 1024 || a.n_seqs < 1 || a.n_seqs > (1 << 20) || a.max_pages < 1)
+      a.page_tokens > 4096 || a.n_heads < 1 || a.n_heads > 1024 || a.n_seqs < 1 || a.n_seqs > (1 << 20) ||
+      a.max_pages < 1)
     return "a size is out of range";
-  if (a.head_dim < 1 || a.head_dim > 256 || a.head_dim * esize(a.type) % 16) return "head_dim: at most 256, whole 16-byte pieces";
+  if (a.head_dim < 1 || a.head_dim > 256 || a.head_dim * esize(a.type) % 16)
+    return "head_dim: at most 256, whole 16-byte pieces";
   if ((int64_t)a.max_pages * a.page_tokens > INT32_MAX) return "max_pages * page_tokens exceeds 2^31 - 1";
   if (!a.k || !a.v || !a.table || !a.length || !a.refs) return "NULL device pointer";
   if ((a.type == P2P_KV_E4M3) != (a.k_scale != nullptr) || (a.type == P2P_KV_E4M3) != (a.v_scale != nullptr))
     return "k_scale and v_scale go with P2P_KV_E4M3 alone";
   if ((uintptr_t)a.k % 16 || (uintptr_t)a.v % 16) return "k and v must start on 16-byte boundaries";
-  std::pair<int64_t, int64_t> d[4] = {{a.layer_stride, a.n_layers}, {a.page_stride, a.n_pages}, {a.token_stride, a.page_tokens},
-                                      {a.head_stride, a.n_heads}};
+  std::pair<int64_t, int64_t> d[4] = {{a.layer_stride, a.n_layers}, {a.page_stride, a.n_pages},
+                                      {a.token_stride, a.page_tokens}, {a.head_stride, a.n_heads}};
   std::sort(d, d + 4);
   int64_t extent = a.head_dim;  // values that the dimensions so far reach over
   for (auto& [stride, n] : d) {
@@ -91,18 +93,21 @@ const char* check_layout(const p2p_kv_layout& a) {
   return nullptr;
 }
 
-// Where a token's heads lie together, the rows of one head are pieces of lines and of pages of memory that other heads share
-// (256 bytes and more are read as fast alone): the warps of a CTA of the attention take up to four neighbouring heads of
-// the same tokens instead of four times the tokens.  log2 of how many: with four, 191 x 1,000 tokens of 24 heads of 80 bf16
-// values take 236 us and with one 351.
+// Where a token's heads lie together, the rows of one head are pieces of lines and of pages of memory that other
+// heads share (256 bytes and more are read as fast alone): the warps of a CTA of the attention take up to four
+// neighbouring heads of the same tokens instead of four times the tokens.  log2 of how many: with four, 191 x 1,000
+// tokens of 24 heads of 80 bf16 values take 236 us and with one 351.
 int32_t heads_side_by_side(const p2p::KvView& c) {
   if (c.head_stride > c.token_stride || c.row16 % 16 == 0) return 0;
   return c.heads % 4 == 0 ? 2 : c.heads % 2 == 0 ? 1 : 0;
 }
 
-cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p::KvAttendScratch& w, int num_sms, cudaStream_t st) {
+cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p::KvAttendScratch& w, int num_sms,
+                          cudaStream_t st) {
   using namespace p2p;
-  const auto launch = c.side == 0 ? (c.type == P2P_KV_BF16 ? launch_kv_attend_bf16 : c.type == P2P_KV_F16 ? launch_kv_attend_f16 : launch_kv_attend_e4m3)
+  const auto launch = c.side == 0 ? (c.type == P2P_KV_BF16  ? launch_kv_attend_bf16
+                                     : c.type == P2P_KV_F16 ? launch_kv_attend_f16
+                                                            : launch_kv_attend_e4m3)
                                   : (c.type == P2P_KV_BF16  ? launch_kv_attend_bf16_side
                                      : c.type == P2P_KV_F16 ? launch_kv_attend_f16_side
                                                             : launch_kv_attend_e4m3_side);
@@ -159,19 +164,22 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   };
   const size_t S = (size_t)a.n_seqs, N = (size_t)a.n_pages;
   const size_t words = part(256), claim = part(4 * S),
-               arrived = part(sizeof(int32_t) * 4 * p2p::KvAttendScratch::kCtasPerSm * sms), zero = at, start = part(4 * (S + 1)), first = part(4 * S), cut = part(4 * S),
+               arrived = part(sizeof(int32_t) * 4 * p2p::KvAttendScratch::kCtasPerSm * sms), zero = at,
+               start = part(4 * (S + 1)), first = part(4 * S), cut = part(4 * S),
                list = part(4 * N), jobs = part(sizeof(p2p::KvJob) * std::max(S, N)),
                parts = part(sizeof(float) * p2p::kv_attend_parts(c, sms));
   cudaError_t e = cudaMalloc(&n->scratch, at);
   if (e == cudaSuccess) e = cudaMemset(n->scratch, 0, zero);
   if (e == cudaSuccess) e = p2p::prepare_kv_pages();
   if (e == cudaSuccess) e = launch_attend(c, nullptr, n->w, sms, nullptr);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);  // (calls may go to a stream that does not wait for this one)
+  // (calls may go to a stream that does not wait for this one)
+  if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     if (n->scratch) cudaFree(n->scratch);
     delete n;
-    return e == cudaErrorMemoryAllocation ? fail(h, P2P_E_NOMEM, "no device memory for the scratch") : cuda_fail(h, e, "the scratch");
+    return e == cudaErrorMemoryAllocation ? fail(h, P2P_E_NOMEM, "no device memory for the scratch")
+                                          : cuda_fail(h, e, "the scratch");
   }
   char* p = (char*)n->scratch;
   n->s.err = (int32_t*)(p + words);
@@ -221,10 +229,13 @@ int p2p_kv_sync(p2p_kv* h) {
   const int b = word[0];
   if (b == p2p::KV_NO_PAGES) return fail(h, P2P_E_NOMEM, "the pool has too few free pages");
   char m[256];
-  std::snprintf(m, sizeof(m), "device reported:%s%s%s%s%s%s", b & p2p::KV_BAD_SEQ ? " a sequence out of range or named twice;" : "",
-                b & p2p::KV_BAD_COUNT ? " a count or length out of range;" : "", b & p2p::KV_NO_PAGES ? " too few free pages;" : "",
-                b & p2p::KV_BAD_PAGE ? " a page table or reference count that does not hold together;" : "",
-                b & p2p::KV_SHARED ? " a write to a shared page;" : "", b & p2p::KV_BAD_OFFSETS ? " offsets out of range;" : "");
+  const auto say = [b](int bit, const char* what) { return b & bit ? what : ""; };
+  std::snprintf(m, sizeof(m), "device reported:%s%s%s%s%s%s",
+                say(p2p::KV_BAD_SEQ, " a sequence out of range or named twice;"),
+                say(p2p::KV_BAD_COUNT, " a count or length out of range;"),
+                say(p2p::KV_NO_PAGES, " too few free pages;"),
+                say(p2p::KV_BAD_PAGE, " a page table or reference count that does not hold together;"),
+                say(p2p::KV_SHARED, " a write to a shared page;"), say(p2p::KV_BAD_OFFSETS, " offsets out of range;"));
   return fail(h, P2P_E_DEVICE, m);
 }
 
@@ -290,10 +301,11 @@ int p2p_kv_compact(p2p_kv* h) {
 }
 
 int p2p_kv_write(p2p_kv* h, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq, const int64_t* offsets,
-                 int64_t n_tokens, const void* k, const void* v, int64_t layer_stride, int64_t token_stride, int64_t head_stride,
-                 int32_t type) {
+                 int64_t n_tokens, const void* k, const void* v, int64_t layer_stride, int64_t token_stride,
+                 int64_t head_stride, int32_t type) {
   if (int rc = check_list(h, n, seq, offsets)) return rc;
-  if (layer < 0 || n_layers < 0 || (int64_t)layer + n_layers > h->c.n_layers) return fail(h, P2P_E_INVAL, "layers out of range");
+  if (layer < 0 || n_layers < 0 || (int64_t)layer + n_layers > h->c.n_layers)
+    return fail(h, P2P_E_INVAL, "layers out of range");
   if (n_tokens < 0 || n_tokens > INT32_MAX) return fail(h, P2P_E_INVAL, "n_tokens out of range");
   if (h->c.type == P2P_KV_E4M3 ? type != P2P_KV_BF16 && type != P2P_KV_F16 : type != h->c.type)
     return fail(h, P2P_E_INVAL, "type of k and v: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
@@ -320,7 +332,8 @@ int p2p_kv_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const
   if (window < 0) return fail(h, P2P_E_INVAL, "negative window");
   if (n == 0) return P2P_OK;
   if (!q || !out) return fail(h, P2P_E_INVAL, "NULL device pointer");
-  if ((uintptr_t)q % 2 || (uintptr_t)out % 2 || (uintptr_t)lse % 4) return fail(h, P2P_E_INVAL, "a pointer is not aligned to its type");
+  if ((uintptr_t)q % 2 || (uintptr_t)out % 2 || (uintptr_t)lse % 4)
+    return fail(h, P2P_E_INVAL, "a pointer is not aligned to its type");
   DeviceGuard g(h->device);
   const p2p::KvQuery a = {q, out, lse, seq, q_row_stride, q_head_stride, out_row_stride, out_head_stride,
                           n, n_heads, type, window, layer, scale,

@@ -3,11 +3,11 @@
 // A call on the tables is one cluster of eight CTAs.  Each of them checks every item, counts the page entries that it
 // concerns and scans the counts in its own shared memory (for long lists the first CTA does, in scratch); the pool's
 // reference counts are scanned in eight parts.  The CTAs tell each other what they found through shared memory and
-// meet once; then, if every item was good, the entries are worked off as one flat range, so that one long sequence and
-// many short ones take the same time.  Nothing is changed before that.  What bounds these calls is the chain of loads
-// behind an item (its sequence, the length, the last page, its count), the cluster's meeting and the launch itself: 3.6 us
-// for a trim of 33 sequences, 4.3 for an extend (one CTA instead of eight: 33 us for a trim of 20,000 pages, 88 for an
-// extend by them and 200 for a compaction's plan; eight: 11, 13 and 15).
+// meet once; then, if every item was good, the entries are worked off as one flat range, so that one long sequence
+// and many short ones take the same time.  Nothing is changed before that.  What bounds these calls is the chain of
+// loads behind an item (its sequence, the length, the last page, its count), the cluster's meeting and the launch
+// itself: 3.6 us for a trim of 33 sequences, 4.3 for an extend (one CTA instead of eight: 33 us for a trim of 20,000
+// pages, 88 for an extend by them and 200 for a compaction's plan; eight: 11, 13 and 15).
 //
 // Pages are copied by a second launch over the whole GPU, from the list of copies that the plan leaves.
 #include <cooperative_groups.h>
@@ -17,8 +17,8 @@
 
 #include "kv.h"
 
-// (No load here goes past the coherent path, as __ldg or const __restrict__ would have it: the kernel before may still be
-// writing when this one starts, see launch_early.)
+// (No load here goes past the coherent path, as __ldg or const __restrict__ would have it: the kernel before may
+// still be writing when this one starts, see launch_early.)
 namespace p2p {
 namespace {
 
@@ -128,7 +128,8 @@ struct Part {
 __device__ __forceinline__ Part part_of(const KvView& c, int rank) {
   const int32_t each = ((c.n_pages + kCluster * kWarps - 1) / (kCluster * kWarps) + 31) / 32 * 32;
   const int64_t begin = (int64_t)(rank * kWarps + (threadIdx.x >> 5)) * each;
-  return {(int32_t)(begin < c.n_pages ? begin : c.n_pages), (int32_t)(begin + each < c.n_pages ? begin + each : c.n_pages)};
+  const int64_t n = c.n_pages;
+  return {(int32_t)min(begin, n), (int32_t)min(begin + each, n)};
 }
 // The reference counts of the warp's pages, the first of them read at construction.
 struct Counting {
@@ -152,7 +153,8 @@ struct Counting {
       n += page < r.end && what(page, v[k]);
     }
 #pragma unroll 8
-    for (int32_t page = r.begin + (threadIdx.x & 31) + 32 * kFirst; page < r.end; page += 32) n += what(page, __ldcg(c.refs + page));
+    for (int32_t page = r.begin + (threadIdx.x & 31) + 32 * kFirst; page < r.end; page += 32)
+      n += what(page, __ldcg(c.refs + page));
     return __reduce_add_sync(~0u, n);
   }
 };
@@ -198,16 +200,20 @@ __device__ void settle(const KvView& c, const KvScratch& s, int32_t n, const int
     *s.halt = 1;
   }
 }
-// (The first CTA alone marks the sequences: what it meets a second time was named twice.  The mark's old value is looked at
-// after the item's other loads are on their way.)
-__device__ __forceinline__ int32_t claim(const KvScratch& s, int32_t seq, bool first) { return first ? atomicExch(&s.claim[seq], 1) : 0; }
+// (The first CTA alone marks the sequences: what it meets a second time was named twice.  The mark's old value is
+// looked at after the item's other loads are on their way.)
+__device__ __forceinline__ int32_t claim(const KvScratch& s, int32_t seq, bool first) {
+  return first ? atomicExch(&s.claim[seq], 1) : 0;
+}
 
 // A length as the table can hold it, or -1.
 __device__ __forceinline__ int32_t length_of(const KvView& c, int32_t seq) {
   const int32_t n = c.length[seq];
   return n >= 0 && n <= c.max_pages * c.page ? n : -1;
 }
-__device__ __forceinline__ int32_t* row_of(const KvView& c, int32_t seq) { return c.table + (int64_t)seq * c.max_pages; }
+__device__ __forceinline__ int32_t* row_of(const KvView& c, int32_t seq) {
+  return c.table + (int64_t)seq * c.max_pages;
+}
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     extend_kernel(KvView c, KvScratch s, int32_t n, const int32_t* seq, const int32_t* count) {
@@ -270,7 +276,8 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
   if (p.found[0].count2) {
     cg::this_cluster().sync();  // (a page that all its sharers leave is free from here on, not for this call's entries)
     const int32_t jobs = __ldcg(s.njobs);
-    for (int32_t k = rank * kThreads + threadIdx.x; k < jobs; k += kCluster * kThreads) atomicSub(&c.refs[__ldcg(&s.jobs[k].from)], 1);
+    for (int32_t k = rank * kThreads + threadIdx.x; k < jobs; k += kCluster * kThreads)
+      atomicSub(&c.refs[__ldcg(&s.jobs[k].from)], 1);
   }
   if (rank == 0)
     for (int32_t i = threadIdx.x; i < n; i += kThreads) c.length[seq[i]] += count[i];
@@ -304,7 +311,8 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
   if (err) return;
   const int32_t total = it.start[n];
   for (int64_t r = rank * kThreads + threadIdx.x; r < total; r += kCluster * kThreads) {
-    const int32_t i = item_of(it.start, n, (int32_t)r), page = row_of(c, seq[i])[it.first[i] + (int32_t)r - it.start[i]];
+    const int32_t i = item_of(it.start, n, (int32_t)r);
+    const int32_t page = row_of(c, seq[i])[it.first[i] + (int32_t)r - it.start[i]];
     if ((uint32_t)page >= (uint32_t)c.n_pages)
       atomicOr(s.err, KV_BAD_PAGE);
     else if (atomicSub(&c.refs[page], 1) < 1)
@@ -388,7 +396,10 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) com
     m += k < rank ? p.found[k].count2 : 0;
   }
   each_page(c, mine, h, jobs, hole, [&](int32_t page, int64_t k) { s.jobs[k].to = page; });
-  each_page(c, mine, m, jobs, mover, [&](int32_t page, int64_t k) { s.jobs[k].from = page, s.jobs[k].tokens = c.page; });
+  each_page(c, mine, m, jobs, mover, [&](int32_t page, int64_t k) {
+    s.jobs[k].from = page;
+    s.jobs[k].tokens = c.page;
+  });
   cluster.sync();
   if (rank == 0 && threadIdx.x == 0) *s.njobs = (int32_t)jobs, *s.live = (int32_t)live;
   for (int64_t k = rank * kThreads + threadIdx.x; k < jobs; k += kCluster * kThreads) {
@@ -399,16 +410,17 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) com
   }
 }
 
-// The copies of the plan before it, in 16-byte pieces.  A warp takes 32 pieces of a page, one a lane, in 1 << PLANES_LOG of the
-// 2 * n_layers arrays (keys and values of each layer) and, where those are fewer than kCopies, further 32 pieces, so that
-// a lane has kCopies loads in flight whose places differ by strides alone.  Bound by the bytes read and written: 3.3 GB of
-// pages moved (6.7 GB in all) in 1.04 ms on one GB300, 94% of the copy bandwidth.
+// The copies of the plan before it, in 16-byte pieces.  A warp takes 32 pieces of a page, one a lane, in 1 <<
+// PLANES_LOG of the 2 * n_layers arrays (keys and values of each layer) and, where those are fewer than kCopies,
+// further 32 pieces, so that a lane has kCopies loads in flight whose places differ by strides alone.  Bound by the
+// bytes read and written: 3.3 GB of pages moved (6.7 GB in all) in 1.04 ms on one GB300, 94% of the copy bandwidth.
 constexpr int kCopies = 8, kCopyThreads = 256, kCopyCtas = 4;
 struct PageShape {
   FastDiv by_row, by_token;  // pieces of a head's values of a token, and of a token
 };
 template <int PLANES_LOG>
-__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvView c, KvScratch s, PageShape g, int32_t moved) {
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas)
+    copy_pages_kernel(KvView c, KvScratch s, PageShape g, int32_t moved) {
   begin_kernel();
   // (Loads past the first cache: this launch may have shared its SM with the plan's.)
   const int32_t njobs = __ldcg(s.njobs);
@@ -431,9 +443,11 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvV
   if (njobs == 0) return;
   constexpr int kPlanes = 1 << PLANES_LOG, kPieces = kCopies / kPlanes;
   const int lane = threadIdx.x & 31;
-  const int32_t chunks = (c.page * (int32_t)g.by_token.d + 32 * kPieces - 1) / (32 * kPieces), groups = (2 * c.n_layers + kPlanes - 1) / kPlanes;
+  const int32_t chunks = (c.page * (int32_t)g.by_token.d + 32 * kPieces - 1) / (32 * kPieces);
+  const int32_t groups = (2 * c.n_layers + kPlanes - 1) / kPlanes;
   const int64_t items = (int64_t)njobs * groups * chunks;
-  for (int64_t x = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); x < items; x += (int64_t)gridDim.x * (kCopyThreads / 32)) {
+  const int64_t all_warps = (int64_t)gridDim.x * (kCopyThreads / 32);
+  for (int64_t x = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); x < items; x += all_warps) {
     const int64_t job = x / ((int64_t)groups * chunks);
     const int32_t rest = (int32_t)(x - job * groups * chunks), group = rest / chunks;
     // (Turned from job to job: where pages are copied in part, no warp has their used beginnings alone.)
@@ -445,7 +459,8 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvV
     for (int y = 0; y < kPieces; ++y) {
       const int32_t z = (chunk * kPieces + y) * 32 + lane;
       const uint32_t t = g.by_token.div(z), in = z - t * g.by_token.d, h = g.by_row.div(in);
-      at[y] = (int32_t)t < j.z ? j.x * c.page_stride + t * c.token_stride + h * c.head_stride + (in - h * g.by_row.d) * 16 : -1;
+      const int64_t in_page = t * c.token_stride + h * c.head_stride + (in - h * g.by_row.d) * 16;
+      at[y] = (int32_t)t < j.z ? j.x * c.page_stride + in_page : -1;
     }
     const int32_t layer0 = group * (kPlanes / 2), layers = min(kPlanes / 2, c.n_layers - layer0);
     char *const k0 = c.k + layer0 * c.layer_stride, *const v0 = c.v + layer0 * c.layer_stride;
@@ -454,20 +469,23 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_pages_kernel(KvV
     for (int y = 0; y < kPieces; ++y)
 #pragma unroll
       for (int p = 0; p < kPlanes; ++p)
-        if (at[y] >= 0 && p / 2 < layers) v[y][p] = __ldcg((const uint4*)((p & 1 ? v0 : k0) + p / 2 * c.layer_stride + at[y]));
+        if (at[y] >= 0 && p / 2 < layers)
+          v[y][p] = __ldcg((const uint4*)((p & 1 ? v0 : k0) + p / 2 * c.layer_stride + at[y]));
 #pragma unroll
     for (int y = 0; y < kPieces; ++y)
 #pragma unroll
       for (int p = 0; p < kPlanes; ++p)
-        if (at[y] >= 0 && p / 2 < layers) __stcg((uint4*)((p & 1 ? v0 : k0) + p / 2 * c.layer_stride + at[y] + move), v[y][p]);
+        if (at[y] >= 0 && p / 2 < layers)
+          __stcg((uint4*)((p & 1 ? v0 : k0) + p / 2 * c.layer_stride + at[y] + move), v[y][p]);
   }
 }
 
 // ---- write ------------------------------------------------------------------------------------------------
 
-// Where the tokens of a block go is found once, a lane a token, and serves all their heads in the layers and arrays that
-// the CTA writes; the first values are read while it is found.  Bound by the bytes read and written: 61 prompts of 71,000
-// tokens, 2.3 GB of bf16 values in and 1.2 GB of 8-bit values out, in 0.56 ms on one GB300 (92% of the copy bandwidth).
+// Where the tokens of a block go is found once, a lane a token, and serves all their heads in the layers and arrays
+// that the CTA writes; the first values are read while it is found.  Bound by the bytes read and written: 61 prompts
+// of 71,000 tokens, 2.3 GB of bf16 values in and 1.2 GB of 8-bit values out, in 0.56 ms on one GB300 (92% of the copy
+// bandwidth).
 constexpr int kBlock = 32, kWriteThreads = 256;
 static_assert(kBlock == 32, "a warp finds the places, all its lanes together");
 
@@ -486,9 +504,9 @@ __device__ __forceinline__ int32_t find_item(const int64_t* offsets, int32_t n, 
   return lo;
 }
 
-// x / scale rounded to the nearest 32-bit value: the quotient by the rounded reciprocal, put right by its exact remainder
-// (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990), for scales of ordinary size; a
-// quotient that is above 448 by far stays as it is.
+// x / scale rounded to the nearest 32-bit value: the quotient by the rounded reciprocal, put right by its exact
+// remainder (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990), for
+// scales of ordinary size; a quotient that is above 448 by far stays as it is.
 __device__ __forceinline__ float divide(float x, float scale, float inverse) {
   const float y = x * inverse, z = fmaf(fmaf(-y, scale, x), inverse, y);
   return fabsf(y) < 65536.f ? z : y;
@@ -512,7 +530,8 @@ __device__ __forceinline__ uint4 narrow16(const uint4& a, const uint4& b, float 
       v.x = divide(v.x, scale, inverse), v.y = divide(v.y, scale, inverse);
       w.x = divide(w.x, scale, inverse), w.y = divide(w.y, scale, inverse);
     } else {
-      v.x = __fdiv_rn(v.x, scale), v.y = __fdiv_rn(v.y, scale), w.x = __fdiv_rn(w.x, scale), w.y = __fdiv_rn(w.y, scale);
+      v.x = __fdiv_rn(v.x, scale), v.y = __fdiv_rn(v.y, scale);
+      w.x = __fdiv_rn(w.x, scale), w.y = __fdiv_rn(w.y, scale);
     }
     out[i] = narrow(v) | narrow(w) << 16;
   }
@@ -524,7 +543,8 @@ template <bool WIDE, int N>
 __device__ __forceinline__ void read_values(uint4 (&v)[N], const uint16_t* p) {
   if constexpr (WIDE && N == 2) {
     asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y), "=r"(v[1].z), "=r"(v[1].w)
+                 : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y), "=r"(v[1].z),
+                   "=r"(v[1].w)
                  : "l"(p)
                  : "memory");
   } else if constexpr (WIDE) {
@@ -540,8 +560,9 @@ __device__ __forceinline__ void read_values(uint4 (&v)[N], const uint16_t* p) {
   }
 }
 
-// KIND: the cache's type, BF16: that of the values given.  A CTA takes a block of tokens and `share` of the 2 * n_layers
-// arrays (keys and values of each layer).  by_token: 16-byte pieces of a token in one array, by_row: of a head.
+// KIND: the cache's type, BF16: that of the values given.  A CTA takes a block of tokens and `share` of the 2 *
+// n_layers arrays (keys and values of each layer).  by_token: 16-byte pieces of a token in one array, by_row: of a
+// head.
 template <int KIND, bool BF16, bool WIDE>
 __global__ void __launch_bounds__(kWriteThreads)
     write_kernel(KvView c, KvScratch s, int32_t layer, int32_t n_layers, int32_t share, int32_t n, const int32_t* seq,
@@ -550,9 +571,11 @@ __global__ void __launch_bounds__(kWriteThreads)
   begin_kernel();
   const int32_t halt = *s.halt;
   const int64_t t0 = (int64_t)blockIdx.x * kBlock;
-  const int32_t tokens = (int32_t)min((int64_t)kBlock, n_tokens - t0), a0 = blockIdx.y * share, a1 = min(a0 + share, 2 * n_layers);
+  const int32_t tokens = (int32_t)min((int64_t)kBlock, n_tokens - t0);
+  const int32_t a0 = blockIdx.y * share, a1 = min(a0 + share, 2 * n_layers);
   const uint32_t all = tokens * by_token.d * (uint32_t)(a1 - a0);
-  constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8, kLoads = kValues / 8, kAhead = 4 / kLoads;  // pieces of a thread in flight
+  // Values and loads of a piece, and pieces of a thread in flight.
+  constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8, kLoads = kValues / 8, kAhead = 4 / kLoads;
   uint4 v[kAhead][kLoads];
   float scale[kAhead];
   char* to[kAhead];      // but for the token's place
@@ -564,9 +587,11 @@ __global__ void __launch_bounds__(kWriteThreads)
       token[k] = -1;
       if (y >= all) continue;
       const uint32_t token_of = by_token.div(y), over = tokens == kBlock ? token_of / kBlock : token_of / tokens;
-      const uint32_t t = token_of - over * tokens, array = a0 + over, z = y - token_of * by_token.d, h = by_row.div(z), piece = z - h * by_row.d;
+      const uint32_t t = token_of - over * tokens, array = a0 + over, z = y - token_of * by_token.d;
+      const uint32_t h = by_row.div(z), piece = z - h * by_row.d;
       const int32_t l = array >> 1;
-      const uint16_t* from = (const uint16_t*)(array & 1 ? in.v : in.k) + l * in.layer_stride + (t0 + t) * in.token_stride + h * in.head_stride + piece * kValues;
+      const uint16_t* from = (const uint16_t*)(array & 1 ? in.v : in.k) + l * in.layer_stride +
+          (t0 + t) * in.token_stride + h * in.head_stride + piece * kValues;
       read_values<WIDE>(v[k], from);
       if (KIND == P2P_KV_E4M3) scale[k] = (array & 1 ? c.v_scale : c.k_scale)[(layer + l) * c.heads + h];
       to[k] = (array & 1 ? c.v : c.k) + (int64_t)(layer + l) * c.layer_stride + h * c.head_stride + piece * 16;
@@ -652,27 +677,32 @@ cudaError_t launch_copies(const KvView& c, const KvScratch& s, bool moved, int n
   PageShape g;
   g.by_row = FastDiv((uint32_t)c.row16);
   g.by_token = FastDiv((uint32_t)(c.heads * c.row16));
-  const auto kernel = c.n_layers == 1 ? copy_pages_kernel<1> : c.n_layers == 2 ? copy_pages_kernel<2> : copy_pages_kernel<3>;
+  const auto kernel = c.n_layers == 1   ? copy_pages_kernel<1>
+                      : c.n_layers == 2 ? copy_pages_kernel<2>
+                                        : copy_pages_kernel<3>;
   return launch_early(kernel, dim3(kCopyCtas * num_sms), kCopyThreads, 0, st, c, s, g, (int32_t)moved);
 }
 
 template <int KIND, bool BF16, bool WIDE>
-cudaError_t write_launch(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq,
-                         const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms, cudaStream_t st) {
+cudaError_t write_launch(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n,
+                         const int32_t* seq, const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms,
+                         cudaStream_t st) {
   const int64_t blocks = (n_tokens + kBlock - 1) / kBlock;
   // All arrays of a block of tokens in one CTA where there are many blocks, else as few as fill the GPU.
   const int64_t want = (8LL * num_sms + blocks - 1) / blocks;
   // (A CTA's pieces are counted in 32 bits.)
   const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / (kBlock * c.heads * c.row16));
-  const int32_t share = (int32_t)std::min(most, std::max<int64_t>(1, 2 * n_layers / std::min<int64_t>(want, 2 * n_layers)));
+  const int64_t arrays = 2 * n_layers;
+  const int32_t share = (int32_t)std::min(most, std::max<int64_t>(1, arrays / std::min(want, arrays)));
   const dim3 grid((unsigned)blocks, (unsigned)((2 * n_layers + share - 1) / share));
-  return launch_early(write_kernel<KIND, BF16, WIDE>, grid, kWriteThreads, 0, st, c, s, layer, n_layers, share, n, seq, offsets, n_tokens,
-                      rows, FastDiv((uint32_t)(c.heads * c.row16)), FastDiv((uint32_t)c.row16));
+  return launch_early(write_kernel<KIND, BF16, WIDE>, grid, kWriteThreads, 0, st, c, s, layer, n_layers, share, n, seq,
+                      offsets, n_tokens, rows, FastDiv((uint32_t)(c.heads * c.row16)), FastDiv((uint32_t)c.row16));
 }
 
 template <int KIND, bool BF16>
-cudaError_t write_wide(bool wide, const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq,
-                       const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms, cudaStream_t st) {
+cudaError_t write_wide(bool wide, const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n,
+                       const int32_t* seq, const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms,
+                       cudaStream_t st) {
   return wide ? write_launch<KIND, BF16, true>(c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st)
               : write_launch<KIND, BF16, false>(c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st);
 }
@@ -687,13 +717,14 @@ cudaError_t prepare_kv_pages() {
   return e;
 }
 
-cudaError_t launch_kv_extend(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* count, int num_sms,
-                             cudaStream_t st) {
+cudaError_t launch_kv_extend(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* count,
+                             int num_sms, cudaStream_t st) {
   const cudaError_t e = launch_early(extend_kernel, dim3(kCluster), kThreads, item_bytes(n), st, c, s, n, seq, count);
   return e == cudaSuccess ? launch_copies(c, s, false, num_sms, st) : e;
 }
 
-cudaError_t launch_kv_trim(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* to, cudaStream_t st) {
+cudaError_t launch_kv_trim(const KvView& c, const KvScratch& s, int32_t n, const int32_t* seq, const int32_t* to,
+                           cudaStream_t st) {
   return launch_early(trim_kernel, dim3(kCluster), kThreads, item_bytes(n), st, c, s, n, seq, to);
 }
 
@@ -707,16 +738,19 @@ cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, 
   return e == cudaSuccess ? launch_copies(c, s, true, num_sms, st) : e;
 }
 
-cudaError_t launch_kv_write(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq,
-                            const int64_t* offsets, int64_t n_tokens, const KvRows& rows, int num_sms, cudaStream_t st) {
+cudaError_t launch_kv_write(const KvView& c, const KvScratch& s, int32_t layer, int32_t n_layers, int32_t n,
+                            const int32_t* seq, const int64_t* offsets, int64_t n_tokens, const KvRows& rows,
+                            int num_sms, cudaStream_t st) {
   const int64_t values = c.type == P2P_KV_E4M3 ? 16 : 8;  // that are read together
-  const bool wide = (uintptr_t)rows.k % (2 * values) == 0 && (uintptr_t)rows.v % (2 * values) == 0 && rows.layer_stride % values == 0 &&
+  const bool wide = (uintptr_t)rows.k % (2 * values) == 0 && (uintptr_t)rows.v % (2 * values) == 0 &&
+      rows.layer_stride % values == 0 &&
                     rows.token_stride % values == 0 && rows.head_stride % values == 0;
   if (c.type != P2P_KV_E4M3)  // (16-bit values are stored as they are)
     return write_wide<P2P_KV_BF16, true>(wide, c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st);
   return rows.type == P2P_KV_BF16
              ? write_wide<P2P_KV_E4M3, true>(wide, c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st)
-             : write_wide<P2P_KV_E4M3, false>(wide, c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms, st);
+             : write_wide<P2P_KV_E4M3, false>(wide, c, s, layer, n_layers, n, seq, offsets, n_tokens, rows, num_sms,
+                 st);
 }
 
 cudaError_t launch_kv_stats(const KvView& c, unsigned long long* out, int num_sms, cudaStream_t st) {
