@@ -116,6 +116,31 @@ def test_long_sequences(n, hq, hkv, dim, kind):
         assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])   # the same sums in the same order
 
 
+@pytest.mark.parametrize("hq,hkv,dim,kind,page", [(28, 4, 64, "bf16", 16), (64, 4, 80, "f16", 5), (96, 8, 64, "e4m3", 32),
+                                                  (6, 2, 96, "bf16", 1), (48, 4, 192, "e4m3", 16), (12, 12, 80, "bf16", 16)])
+def test_long_sequences_heads_inside_tokens(hq, hkv, dim, kind, page):
+    """The same where a token's heads lie together, with and without a window that starts inside a tile."""
+    lengths = [40003, 0, 9, 12345]
+    c = make(lengths, hkv, dim, page, kind, "lnth")
+    q = query(4, hq, dim, torch.float16 if kind == "f16" else torch.bfloat16)
+    for window in (0, 9001):
+        got = c.attend(0, q, window=window)
+        again = c.attend(0, q, window=window)
+        c.sync()
+        check(c, 0, q, dim ** -0.5, got, window=window)
+        assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_one_kv_head_and_many_parts(kind):
+    """One row of units over the whole GPU, whose parts are joined in two steps."""
+    c = make([150000], 1, 128, 16, kind)
+    q = query(1, 16, 128, torch.bfloat16)
+    got = c.attend(0, q)
+    c.sync()
+    check(c, 0, q, 128 ** -0.5, got)
+
+
 @pytest.mark.parametrize("n", [1, 2, 3, 150, 400, 1300])
 def test_many_sequences(n):
     rng = np.random.default_rng(n)

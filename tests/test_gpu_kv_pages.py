@@ -114,6 +114,34 @@ def test_large_tables():
     m.same(c)
 
 
+def test_lists_longer_than_shared_memory_holds():
+    """More than 8,192 items: planned in scratch by one CTA of the cluster."""
+    c, m = make(layers=1, pages=40000, page=2, heads=1, dim=16, n_seqs=20000, max_pages=6, seed=4)
+    rng = random.Random(6)
+    rows = rng.sample(range(20000), 20000)
+    first, second = rows[:9001], rows[9001:18002]
+    grow(c, m, first, [rng.randint(0, 4) for _ in first])
+    n = [rng.randint(0, int(m.length[s])) for s in first]
+    c.fork(i32(first), i32(second), i32(n))
+    m.fork(first, second, n)
+    grow(c, m, second, [rng.randint(0, 2) for _ in second], 5)   # thousands of shared pages are copied
+    c.sync()
+    m.same(c)
+    was = snapshot(c)
+    for seq, count in ((second + second[:1], [1] * 9002), (second, [1] * 9000 + [99])):
+        c.extend(i32(seq), i32(count))
+        with pytest.raises(g.P2PError) as e:
+            c.sync()
+        assert e.value.code == g.P2P_E_DEVICE and unchanged(c, was)
+    to = [rng.randint(0, int(m.length[s])) for s in first]
+    c.trim(i32(first), i32(to))
+    m.trim(first, to)
+    c.compact()
+    m.compact()
+    c.sync()
+    m.same(c)
+
+
 def test_every_page_taken_and_given_back():
     c, m = make(pages=20, page=4, n_seqs=4, max_pages=20)
     grow(c, m, [2, 0], [44, 36])          # 11 + 9 pages
