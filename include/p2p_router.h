@@ -398,7 +398,8 @@ typedef struct p2p_kv_layout {
  * handle. Errors: P2P_E_INVAL (message of p2p_kv_last_error(NULL)), P2P_E_NOMEM, P2P_E_CUDA. */
 int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out);
 
-/* Frees the handle and its scratch (after finishing its queued work).  NULL is a no-op. */
+/* Frees the handle (after finishing its queued work); the library keeps its scratch for handles made later.  NULL is a
+ * no-op. */
 void p2p_kv_destroy(p2p_kv* kv);
 
 /* Sets the CUDA stream of the calls that follow; waits for the work queued on the one before. */
