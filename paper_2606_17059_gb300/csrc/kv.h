@@ -124,10 +124,10 @@ struct KvAttendScratch {
   int32_t* arrived;  // [4 * kCtasPerSm * SMs]
   int32_t* err;
 };
-// Floats of `parts`: head_dim as the kernels pad it, at most, and blocks of 8 or 16 query heads of up to 4 kv heads.
+// Floats of `parts`: head_dim as the kernels pad it, at most, and blocks of up to 16 or 32 query heads of up to 4 kv heads.
 inline size_t kv_attend_parts(const KvView& c, int num_sms) {
   const int32_t dp = c.dim <= 64 ? 64 : c.dim <= 96 ? 96 : c.dim <= 128 ? 128 : c.dim <= 192 ? 192 : 256,
-      heads = dp > 128 ? 8 : 16;
+      heads = dp > 128 ? 16 : 32;
   return (size_t)4 * KvAttendScratch::kCtasPerSm * num_sms * (heads << c.side) * (dp + 2);
 }
 // With q = NULL they launch nothing, but make the cache's kernels ready for launches (at creation).
