@@ -82,8 +82,8 @@ struct Shape {
   static_assert(kWarps * kRows == 1 << kTileLog);
   static constexpr int kArray = kRows * kRowBytes;             // keys (or values) of a warp's tile
   static constexpr int kStage = 2 * kArray;
-  // Resident on an SM: three where three have room for more than two tiles a warp and registers enough (168 a thread), one
-  // where two have not.
+  // Resident on an SM: three where three have room for more than two tiles a warp and registers enough (168 a
+  // thread), one where two have not.
   static constexpr int kCtas = kRows * kRowBytes <= 3072 && DP * NB <= 256 ? 3 : kRowBytes <= 256 ? 2 : 1;
   static constexpr int kSumPitch = (DP + 31) / 32 * 32;        // of a head's sums, which lie in the room of a tile
   static_assert(8 * kSumPitch * 4 <= kStage);
@@ -821,17 +821,18 @@ cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, 
   return launch_early(kernel, dim3(S::kCtas * num_sms), kThreads, S::kBytes, st, c, *q, w);
 }
 
-// (Pages of 16 tokens taken token by token, as others are: 64 ragged 10.7 us, not 9.7, 256 sequences in 8 bits 109, not 104.)
+// (Pages of 16 tokens taken token by token, as others are: 64 ragged 10.7 us, not 9.7, 256 sequences in 8 bits 109,
+// not 104.)
 template <int KIND, int DP, int NB, bool SIDE>
 cudaError_t launch_pages(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   return c.page % 16 == 0 ? launch<KIND, DP, NB, SIDE, true>(c, q, w, num_sms, st)
                           : launch<KIND, DP, NB, SIDE, false>(c, q, w, num_sms, st);
 }
 
-// Blocks of 8, 16 or 32 query heads: the fewest that hold a kv head's, as each block reads the keys and values again (on the
-// 32 long sequences 40 heads on 8 take 282 us with blocks of 16 and 523 with 8; 128 heads of 256 values on 8 551 and 1,061;
-// 256 heads on 8 301 with blocks of 32 and 539 with 16).  Blocks of 32 beyond 128 values, or beside 8-bit values, do not fit
-// the registers (256 heads on 8 over the 8-bit case 286 us, and 234 with blocks of 16).
+// Blocks of 8, 16 or 32 query heads: the fewest that hold a kv head's, as each block reads the keys and values again
+// (on the 32 long sequences 40 heads on 8 take 282 us with blocks of 16 and 523 with 8; 128 heads of 256 values on 8
+// 551 and 1,061; 256 heads on 8 301 with blocks of 32 and 539 with 16).  Blocks of 32 beyond 128 values, or beside
+// 8-bit values, do not fit the registers (256 heads on 8 over the 8-bit case 286 us, and 234 with blocks of 16).
 template <int KIND, int DP, bool SIDE>
 cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   constexpr bool kWide = DP <= 128 && KIND != P2P_KV_E4M3;  // blocks of 32
