@@ -38,6 +38,8 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "kv.h"
 
 // (No load here goes past the coherent path, as __ldg or const __restrict__ would have it: the kernel before may
@@ -49,6 +51,10 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kOver = 3;                // units that a unit row counts for beyond its own
 constexpr int kJoin = 16;               // parts of a unit row that are read together
+// Heads side by side (see SIDE) with so many units a CTA at least and so many parts of a unit row at most, as joining
+// that many more heads' parts takes longer than the lines save: 4 rows with 8 heads of 192 8-bit values 50 us, not
+// 24; 21 of 20,000 tokens with 4 of 96 16-bit values 86 and 74 (29 parts); 40 of 1,000 with 24 of 80 60, not 86.
+constexpr int kSideUnits = 32, kSideParts = 16;
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -215,7 +221,7 @@ __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t
 }
 
 struct Shared {
-  int64_t sums[kWarps];
+  int64_t sums[2][kWarps];
   int64_t before;  // units of the rows before `row` (over the kv heads and blocks of one)
   int32_t row, last;
   float top[kWarps][8], sum[kWarps][8];  // of the warps' parts, by head of a block
@@ -249,50 +255,69 @@ struct Cursor {
   }
 };
 
-// SIDE: the warps of a CTA take 1 << c.side neighbouring kv heads (see heads_side_by_side in kv_cache.cpp), else
-// one.  WHOLE: pages are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly
+// SIDE: the warps of a CTA take 1 << c.side neighbouring kv heads (see heads_side_by_side in kv_cache.cpp) if there is
+// enough to read, else one.  WHOLE: pages are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly
 // apart.
 template <int KIND, int DP, int NB, bool SIDE, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
     attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
   using S = Shape<KIND, DP, NB>;
   constexpr int PIECES = S::kPieces, KSTEPS = DP / 16;
-  const int32_t side = SIDE ? c.side : 0;
   extern __shared__ __align__(128) char room[];
   __shared__ Shared sh;
   begin_kernel();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t tiles_at = smem_of(room + warp * S::kRoom);
   const int32_t group = a.heads / c.heads, blocks = (group + S::kHeads - 1) / S::kHeads;
-  const int32_t per_row = (c.heads >> side) * blocks;  // unit rows of a row
-  // the warp's kv head and tokens of a unit
-  const int32_t part_of_side = warp & ((1 << side) - 1), rank = warp >> side;
-  const int32_t tile_log = S::kTileLog - side;
 
   // ---- this CTA's range of the units: a thread sums those of consecutive rows, the CTA scans the threads' sums.
   const int32_t each = (a.n + kThreads - 1) / kThreads, r0 = threadIdx.x * each;
-  int64_t mine = 0;
+  int64_t mine[SIDE + 1] = {};  // with the heads side by side, and, last, without
   for (int32_t i0 = r0; i0 < r0 + each && i0 < a.n; i0 += 4) {
     Row r[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       r[k] = row_at<WHOLE>(c, a, i0 + k < r0 + each ? i0 + k : a.n, blockIdx.x == 0 ? w.err : nullptr);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) mine += i0 + k < r0 + each && i0 + k < a.n ? r[k].tiles(tile_log) + kOver : 0;
+    for (int k = 0; k < 4; ++k)
+      if (i0 + k < r0 + each && i0 + k < a.n) {
+        mine[SIDE] += r[k].tiles(S::kTileLog) + kOver;
+        if (SIDE) mine[0] += r[k].tiles(S::kTileLog - c.side) + kOver;
+      }
   }
-  int64_t scan = mine;
+  int64_t scan[SIDE + 1], before = 0, all = 0;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int64_t y = __shfl_up_sync(~0u, scan, d);
-    if (lane >= d) scan += y;
+  for (int x = 0; x <= SIDE; ++x) {
+    scan[x] = mine[x];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t y = __shfl_up_sync(~0u, scan[x], d);
+      if (lane >= d) scan[x] += y;
+    }
+    if (lane == 31) sh.sums[x][warp] = scan[x];
   }
-  if (lane == 31) sh.sums[warp] = scan;
   __syncthreads();
-  int64_t before = 0, all = 0;
+  int32_t side = 0;
+  if (SIDE) {
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) all += sh.sums[SIDE][k];
+    const int64_t unit_rows = (int64_t)a.n * (c.heads >> c.side) * blocks, grid = gridDim.x;
+    const bool enough = all * c.heads * blocks >= kSideUnits * grid & unit_rows * kSideParts >= grid;
+    // (Through a shuffle: taken directly, the registers spill, up to 1 KB, and the 256 sequences with 8 heads of 96
+    // 8-bit values take 147 us, not 107.)
+    side = __shfl_sync(~0u, enough ? c.side : 0, 0);
+    if (side == 0) mine[0] = mine[SIDE], scan[0] = scan[SIDE];
+    all = 0;
+  }
+  const int32_t per_row = (c.heads >> side) * blocks;  // unit rows of a row
+  // the warp's kv head and tokens of a unit
+  const int32_t part_of_side = warp & ((1 << side) - 1), rank = warp >> side;
+  const int32_t tile_log = S::kTileLog - side;
 #pragma unroll
   for (int k = 0; k < kWarps; ++k) {
-    before += k < warp ? sh.sums[k] : 0;
-    all += sh.sums[k];
+    const int64_t of_warp = SIDE && side == 0 ? sh.sums[SIDE][k] : sh.sums[0][k];
+    before += k < warp ? of_warp : 0;
+    all += of_warp;
   }
   const int64_t total = all * per_row;
   // Two units a CTA at least: fewer parts to join (one sequence of 3,000 tokens with 8 kv heads: 11.0 us with one,
@@ -300,9 +325,9 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
   const int64_t ctas = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
   if (blockIdx.x >= ctas) return;
   const int64_t x0 = total * blockIdx.x / ctas, x_end = total * (blockIdx.x + 1) / ctas;
-  before += scan - mine;
+  before += scan[0] - mine[0];
   const int64_t at = x0 / per_row;
-  if (at >= before && at < before + mine) {
+  if (at >= before && at < before + mine[0]) {
     int32_t i = r0;
     for (;; ++i) {
       const int32_t t = row_at<WHOLE>(c, a, i, nullptr).tiles(tile_log) + kOver;
@@ -706,8 +731,9 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
 
     // The CTA that brings the last part of the unit row joins them; where there are many, that of each `bunch` of
     // them joins those, and the one that brings the last of the results joins these.  Each thread has four values of
-    // a head, over the parts in their order, kJoin of which are on their way at a time; with few values, groups of
-    // threads take every so many parts, and the first group puts theirs together.
+    // a head, over the parts in their order, kJoin of which are on their way at a time, or, where there are few parts,
+    // 4 of 4 such values (34 short rows with 16 heads of 192 values to a kv head 13.7 us, not 16.6); with few values,
+    // groups of threads take every so many parts, and the first group puts theirs together.
     const int32_t c0 = (int32_t)(((unit0 + 1) * ctas - 1) / total), c1 = (int32_t)(((unit0 + u.nt) * ctas - 1) / total);
     const int32_t parts = c1 - c0 + 1, all4 = (heads << side) * (DP / 4), turns = (all4 + kThreads - 1) / kThreads;
     const int32_t teams = max(1, kThreads / all4);
@@ -732,74 +758,99 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
       if (!sh.last) break;
       const bool done = level == 1 || members == parts;
       float* const joined = w.parts + ((c0 + first_part) * 4 + (first_part == 0) + 2) * part_size;
-      for (int y0 = 0; y0 < all4; y0 += kThreads) {
-        const int y = teams > 1 ? (int)threadIdx.x % all4 : y0 + (int)threadIdx.x;
-        const int team = teams > 1 ? (int)threadIdx.x / all4 : 0;
-        const int own = y / (DP / 4), beside = own / heads, head = own % heads, at = beside * S::kHeads + head;
-        const int d = y % (DP / 4) * 4;
-        float t = -INFINITY, z = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (y < all4 && team < teams) {
-          for (int32_t k0 = team; k0 < members; k0 += teams * kJoin) {
-            float pt[kJoin], pz[kJoin];
-            float4 pv[kJoin];
+      // AT parts at a time, of ITEMS fours of values.
+      const auto join = [&](auto at_a_time, auto values) {
+        constexpr int AT = decltype(at_a_time)::value, ITEMS = decltype(values)::value;
+        for (int y0 = 0; y0 < all4; y0 += ITEMS * kThreads) {
+          const int y1 = teams > 1 ? (int)threadIdx.x % all4 : y0 + (int)threadIdx.x;
+          const int team = teams > 1 ? (int)threadIdx.x / all4 : 0;
+          float t[ITEMS], z[ITEMS];
+          float4 v[ITEMS];
+          int at[ITEMS], d[ITEMS];  // where each lies in a part; at < 0: nowhere
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) {
+          for (int i = 0; i < ITEMS; ++i) {
+            const int y = y1 + i * kThreads, own = y / (DP / 4), beside = own / heads;
+            t[i] = -INFINITY, z[i] = 0.f, v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            at[i] = y < all4 && team < teams ? beside * S::kHeads + (own - beside * heads) : -1;
+            d[i] = y % (DP / 4) * 4;
+          }
+          for (int32_t k0 = team; k0 < members; k0 += teams * AT) {
+            float pt[ITEMS][AT], pz[ITEMS][AT];
+            float4 pv[ITEMS][AT];
+#pragma unroll
+            for (int j = 0; j < AT; ++j) {
               const int32_t k = k0 + j * teams;
-              pt[j] = -INFINITY, pz[j] = 0.f, pv[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (k < members) {
-                const float* p = part_of(first_part + k * apart);
-                pt[j] = __ldcg(p + part_heads * DP + at);
-                pz[j] = __ldcg(p + part_heads * (DP + 1) + at);
-                pv[j] = __ldcg((const float4*)(p + at * DP + d));
+              const float* const p = part_of(first_part + min(k, members - 1) * apart);
+#pragma unroll
+              for (int i = 0; i < ITEMS; ++i) {
+                pt[i][j] = -INFINITY, pz[i][j] = 0.f, pv[i][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k < members && at[i] >= 0) {
+                  pt[i][j] = __ldcg(p + part_heads * DP + at[i]);
+                  pz[i][j] = __ldcg(p + part_heads * (DP + 1) + at[i]);
+                  pv[i][j] = __ldcg((const float4*)(p + at[i] * DP + d[i]));
+                }
               }
             }
-            float top1 = t;
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) top1 = fmaxf(top1, pt[j]);
-            const float ref = top1 == -INFINITY ? 0.f : top1;
-            const float fade = exp2_fast(t - ref);
-            t = top1;
-            z *= fade, v.x *= fade, v.y *= fade, v.z *= fade, v.w *= fade;
+            for (int i = 0; i < ITEMS; ++i) {
+              float top1 = t[i];
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) {
-              const float f = exp2_fast(pt[j] - ref);
-              z += f * pz[j], v.x += f * pv[j].x, v.y += f * pv[j].y, v.z += f * pv[j].z, v.w += f * pv[j].w;
+              for (int j = 0; j < AT; ++j) top1 = fmaxf(top1, pt[i][j]);
+              const float ref = top1 == -INFINITY ? 0.f : top1;
+              float fade = exp2_fast(t[i] - ref);
+              t[i] = top1;
+              z[i] *= fade, v[i].x *= fade, v[i].y *= fade, v[i].z *= fade, v[i].w *= fade;
+#pragma unroll
+              for (int j = 0; j < AT; ++j) {
+                fade = exp2_fast(pt[i][j] - ref);
+                z[i] += fade * pz[i][j];
+                v[i].x += fade * pv[i][j].x, v[i].y += fade * pv[i][j].y;
+                v[i].z += fade * pv[i][j].z, v[i].w += fade * pv[i][j].w;
+              }
+            }
+          }
+          if (ITEMS == 1 && teams > 1) {
+            const auto of_thread = [&](int x) { return sums + ((x >> 5) - warp) * (S::kRoom / 4) + (x & 31) * 8; };
+            float* const mine = of_thread(threadIdx.x);
+            mine[0] = t[0], mine[1] = z[0];
+            *(float4*)(mine + 4) = v[0];
+            __syncthreads();
+            if (team == 0) {
+              float top1 = t[0];
+              for (int k = 1; k < teams; ++k) top1 = fmaxf(top1, of_thread(threadIdx.x + k * all4)[0]);
+              const float ref = top1 == -INFINITY ? 0.f : top1;
+              float fade = exp2_fast(t[0] - ref);
+              t[0] = top1;
+              z[0] *= fade, v[0].x *= fade, v[0].y *= fade, v[0].z *= fade, v[0].w *= fade;
+              for (int k = 1; k < teams; ++k) {
+                const float* p = of_thread(threadIdx.x + k * all4);
+                fade = exp2_fast(p[0] - ref);
+                z[0] += fade * p[1], v[0].x += fade * p[4], v[0].y += fade * p[5], v[0].z += fade * p[6],
+                    v[0].w += fade * p[7];
+              }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < ITEMS; ++i) {
+            if (at[i] < 0 || team != 0) continue;
+            if (done) {
+              const int beside = at[i] / S::kHeads;
+              const int32_t q_head = head0 + beside * group + at[i] % S::kHeads;
+              const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
+              store4(c, a, u.i, q_head, d[i], v[i], __fdividef(v_scale, z[i]), false);
+              if (d[i] == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = (t[i] + __log2f(z[i])) * kLn2;
+            } else {
+              *(float4*)(joined + at[i] * DP + d[i]) = v[i];
+              if (d[i] == 0) joined[part_heads * DP + at[i]] = t[i], joined[part_heads * (DP + 1) + at[i]] = z[i];
             }
           }
         }
-        if (teams > 1) {
-          const auto of_thread = [&](int x) { return sums + ((x >> 5) - warp) * (S::kRoom / 4) + (x & 31) * 8; };
-          float* const mine = of_thread(threadIdx.x);
-          mine[0] = t, mine[1] = z;
-          *(float4*)(mine + 4) = v;
-          __syncthreads();
-          if (team == 0) {
-            float top1 = t;
-            for (int k = 1; k < teams; ++k) top1 = fmaxf(top1, of_thread(threadIdx.x + k * all4)[0]);
-            const float ref = top1 == -INFINITY ? 0.f : top1;
-            float fade = exp2_fast(t - ref);
-            t = top1;
-            z *= fade, v.x *= fade, v.y *= fade, v.z *= fade, v.w *= fade;
-            for (int k = 1; k < teams; ++k) {
-              const float* p = of_thread(threadIdx.x + k * all4);
-              fade = exp2_fast(p[0] - ref);
-              z += fade * p[1], v.x += fade * p[4], v.y += fade * p[5], v.z += fade * p[6], v.w += fade * p[7];
-            }
-          }
-        }
-        if (y < all4 && team == 0) {
-          if (done) {
-            const int32_t q_head = head0 + beside * group + head;
-            const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
-            store4(c, a, u.i, q_head, d, v, __fdividef(v_scale, z), false);
-            if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = (t + __log2f(z)) * kLn2;
-          } else {
-            *(float4*)(joined + at * DP + d) = v;
-            if (d == 0) joined[part_heads * DP + at] = t, joined[part_heads * (DP + 1) + at] = z;
-          }
-        }
-      }
+      };
+      using std::integral_constant;
+      if (members <= 4 && turns > 1)
+        join(integral_constant<int, 4>(), integral_constant<int, 4>());
+      else
+        join(integral_constant<int, kJoin>(), integral_constant<int, 1>());
       if (done) break;
       first_part = 0;
       members = (parts + bunch - 1) / bunch;

@@ -95,9 +95,11 @@ const char* check_layout(const p2p_kv_layout& a) {
 }
 
 // Where a token's heads lie together, the rows of one head are pieces of lines and of pages of memory that other
-// heads share (256 bytes and more are read as fast alone): the warps of a CTA of the attention take up to four
-// neighbouring heads of the same tokens instead of four times the tokens.  log2 of how many: with four, 191 x 1,000
-// tokens of 24 heads of 80 bf16 values take 236 us and with one 351.
+// heads share (rows of whole 256 bytes are read as fast alone): the warps of a CTA of the attention take up to four
+// neighbouring heads of the same tokens instead of four times the tokens, in calls with enough of them (the kernel
+// sees).  log2 of how many: with four, 191 x 1,000 tokens of 24 heads of 80 16-bit values take 236 us and with one
+// 365; 256 sequences with 8 heads of 96 8-bit values 107 and 191, of 128 8-bit values 127 and 143.  (Rows of whole
+// 128 bytes gain least: 192 16-bit values 240 us with pages of 16 tokens either way, 304 and 280 with pages of one.)
 int32_t heads_side_by_side(const p2p::KvView& c) {
   if (c.head_stride > c.token_stride || c.row16 % 16 == 0) return 0;
   return c.heads % 4 == 0 ? 2 : c.heads % 2 == 0 ? 1 : 0;

@@ -153,6 +153,25 @@ def test_many_sequences(n):
     check(c, 0, q, 0.125, got)
 
 
+@pytest.mark.parametrize("hq,hkv,dim,kind,page", [(8, 4, 80, "f16", 16), (4, 2, 64, "bf16", 5), (24, 4, 64, "e4m3", 32),
+                                                  (72, 4, 96, "bf16", 16), (6, 6, 192, "f16", 1), (48, 4, 176, "e4m3", 16),
+                                                  (36, 2, 240, "bf16", 16), (16, 8, 48, "e4m3", 3)])
+def test_many_sequences_heads_inside_tokens(hq, hkv, dim, kind, page):
+    """Enough of them that a CTA takes neighbouring heads together, and one so long that many CTAs share each of its heads."""
+    n = 2000
+    rng = np.random.default_rng(dim)
+    lengths = [int(x) for x in np.exp(rng.uniform(0, np.log(300), n))]
+    lengths[7], lengths[8], lengths[n // 2], lengths[n - 1] = 0, 3000, 40001, 0
+    c = make(lengths, hkv, dim, page, kind, "lnth")
+    q = query(n, hq, dim, torch.float16 if kind == "f16" else torch.bfloat16)
+    for window in (0, 30001):
+        got = c.attend(0, q, window=window)
+        again = c.attend(0, q, window=window)
+        c.sync()
+        check(c, 0, q, dim ** -0.5, got, window=window)
+        assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
 def test_sequences_in_any_order_and_again():
     c = make(LENGTHS, 2, 64, 16, "bf16")
     seq = torch.tensor([20, 3, 3, 0, 17, 20, 5] * 7, dtype=torch.int32, device="cuda")   # (more rows than sequences)
