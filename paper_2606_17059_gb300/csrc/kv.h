@@ -60,7 +60,8 @@ struct KvView {
   int64_t layer_stride, page_stride, token_stride, head_stride;
   FastDiv by_page;
   int32_t row16;  // 16-byte pieces of a head's values of one token
-  int32_t side;   // log2 of the kv heads that a unit of the attention takes side by side
+  int32_t side;   // log2 of the kv heads that a unit of the attention may take side by side
+  bool lines;     // whether heads share lines of memory (see shares_lines in kv_cache.cpp)
 };
 
 // Bits of the device error word.
@@ -124,7 +125,8 @@ struct KvAttendScratch {
   int32_t* arrived;  // [4 * kCtasPerSm * SMs]
   int32_t* err;
 };
-// Floats of `parts`: head_dim as the kernels pad it, at most, and blocks of up to 16 or 32 query heads of up to 4 kv heads.
+// Floats of `parts`: head_dim as the kernels pad it, at most, and blocks of up to 16 or 32 query heads of up to 4 kv
+// heads.
 inline size_t kv_attend_parts(const KvView& c, int num_sms) {
   const int32_t dp = c.dim <= 64 ? 64 : c.dim <= 96 ? 96 : c.dim <= 128 ? 128 : c.dim <= 192 ? 192 : 256,
       heads = dp > 128 ? 16 : 32;

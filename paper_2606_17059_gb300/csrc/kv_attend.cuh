@@ -51,10 +51,15 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kOver = 3;                // units that a unit row counts for beyond its own
 constexpr int kJoin = 16;               // parts of a unit row that are read together
-// Heads side by side (see SIDE) with so many units a CTA at least and so many parts of a unit row at most, as joining
-// that many more heads' parts takes longer than the lines save: 4 rows with 8 heads of 192 8-bit values 50 us, not
-// 24; 21 of 20,000 tokens with 4 of 96 16-bit values 86 and 74 (29 parts); 40 of 1,000 with 24 of 80 60, not 86.
-constexpr int kSideUnits = 32, kSideParts = 16;
+// Heads side by side (see SIDE), with so many units a CTA at least.  Where heads share lines of memory, with so many
+// parts of a unit row at most, as joining that many more heads' parts takes longer than the lines save: 4 rows with 8
+// heads of 192 8-bit values 50 us, not 24; 21 of 20,000 tokens with 4 of 96 16-bit values 86 and 74 (29 parts); 40 of
+// 1,000 with 24 of 80 60, not 86.  Elsewhere, with so many units a row's head on average at most (kOver of them for
+// starting it), as there are fewer unit rows to start and finish: 2,000 sequences of 1 to 200 tokens (half below 15)
+// with 8 heads of 128 16-bit values take 90 us, not 129, of 8-bit values 104, not 179; 512 of 1 to 800 (5.6 units) with
+// 24 heads of 80 16-bit values 82, not 104, though with 4 of 256 83, not 66.  Beyond, joins cost as much or more: 512 of
+// 1 to 1,600 with 8 heads of 64 50 us and 48, with 4 of 256 115 and 92.
+constexpr int kSideUnits = 32, kSideParts = 16, kSideShort = 6;
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -223,7 +228,7 @@ __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t
 struct Shared {
   int64_t sums[2][kWarps];
   int64_t before;  // units of the rows before `row` (over the kv heads and blocks of one)
-  int32_t row, last;
+  int32_t row, last, side;
   float top[kWarps][8], sum[kWarps][8];  // of the warps' parts, by head of a block
 };
 
@@ -255,9 +260,8 @@ struct Cursor {
   }
 };
 
-// SIDE: the warps of a CTA take 1 << c.side neighbouring kv heads (see heads_side_by_side in kv_cache.cpp) if there is
-// enough to read, else one.  WHOLE: pages are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly
-// apart.
+// SIDE: the warps of a CTA take 1 << c.side neighbouring kv heads where that pays (see kSideUnits), else one.  WHOLE:
+// pages are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly apart.
 template <int KIND, int DP, int NB, bool SIDE, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
     attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
@@ -299,15 +303,19 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
   __syncthreads();
   int32_t side = 0;
   if (SIDE) {
+    // (By one thread: where each decides for itself, the registers spill, up to 1 KB, and 256 sequences with 8 heads of
+    // 96 8-bit values take 147 us, not 107.)
+    if (threadIdx.x == 0) {
+      int64_t units = 0;
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) all += sh.sums[SIDE][k];
-    const int64_t unit_rows = (int64_t)a.n * (c.heads >> c.side) * blocks, grid = gridDim.x;
-    const bool enough = all * c.heads * blocks >= kSideUnits * grid & unit_rows * kSideParts >= grid;
-    // (Through a shuffle: taken directly, the registers spill, up to 1 KB, and the 256 sequences with 8 heads of 96
-    // 8-bit values take 147 us, not 107.)
-    side = __shfl_sync(~0u, enough ? c.side : 0, 0);
+      for (int k = 0; k < kWarps; ++k) units += sh.sums[SIDE][k];
+      const int64_t grid = gridDim.x, unit_rows = (int64_t)a.n * (c.heads >> c.side) * blocks;
+      const bool fit = c.lines ? unit_rows * kSideParts >= grid : units <= (int64_t)kSideShort * a.n;
+      sh.side = fit && units * c.heads * blocks >= kSideUnits * grid ? c.side : 0;
+    }
+    __syncthreads();
+    side = sh.side;
     if (side == 0) mine[0] = mine[SIDE], scan[0] = scan[SIDE];
-    all = 0;
   }
   const int32_t per_row = (c.heads >> side) * blocks;  // unit rows of a row
   // the warp's kv head and tokens of a unit

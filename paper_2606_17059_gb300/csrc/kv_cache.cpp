@@ -94,27 +94,30 @@ const char* check_layout(const p2p_kv_layout& a) {
   return nullptr;
 }
 
-// Where a token's heads lie together, the rows of one head are pieces of lines and of pages of memory that other
-// heads share (rows of whole 256 bytes are read as fast alone): the warps of a CTA of the attention take up to four
-// neighbouring heads of the same tokens instead of four times the tokens, in calls with enough of them (the kernel
-// sees).  log2 of how many: with four, 191 x 1,000 tokens of 24 heads of 80 16-bit values take 236 us and with one
-// 365; 256 sequences with 8 heads of 96 8-bit values 107 and 191, of 128 8-bit values 127 and 143.  (Rows of whole
-// 128 bytes gain least: 192 16-bit values 240 us with pages of 16 tokens either way, 304 and 280 with pages of one.)
-int32_t heads_side_by_side(const p2p::KvView& c) {
-  if (c.head_stride > c.token_stride || c.row16 % 16 == 0) return 0;
-  return c.heads % 4 == 0 ? 2 : c.heads % 2 == 0 ? 1 : 0;
-}
+// Whether the rows of one head are pieces of lines and of pages of memory that other heads share, as a token's heads
+// lie together (rows of whole 256 bytes are read as fast alone).  Then the warps of a CTA of the attention take up to
+// four neighbouring heads of the same tokens instead of four times the tokens, in calls with enough of them (the kernel
+// sees): 191 x 1,000 tokens of 24 heads of 80 16-bit values take 236 us and one head at a time 365; 256 sequences with
+// 8 heads of 96 8-bit values 107 and 191, of 128 8-bit values 127 and 143.  (Rows of whole 128 bytes gain least: 192
+// 16-bit values 240 us with pages of 16 tokens either way, 304 and 280 with pages of one.)
+bool shares_lines(const p2p::KvView& c) { return c.head_stride <= c.token_stride && c.row16 % 16 != 0; }
 
 cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p::KvAttendScratch& w, int num_sms,
                           cudaStream_t st) {
   using namespace p2p;
-  const auto launch = c.side == 0 ? (c.type == P2P_KV_BF16  ? launch_kv_attend_bf16
-                                     : c.type == P2P_KV_F16 ? launch_kv_attend_f16
-                                                            : launch_kv_attend_e4m3)
-                                  : (c.type == P2P_KV_BF16  ? launch_kv_attend_bf16_side
-                                     : c.type == P2P_KV_F16 ? launch_kv_attend_f16_side
-                                                            : launch_kv_attend_e4m3_side);
-  return launch(c, q, w, num_sms, st);
+  const auto alone = c.type == P2P_KV_BF16  ? launch_kv_attend_bf16
+                     : c.type == P2P_KV_F16 ? launch_kv_attend_f16
+                                            : launch_kv_attend_e4m3;
+  const auto side_by_side = c.type == P2P_KV_BF16  ? launch_kv_attend_bf16_side
+                            : c.type == P2P_KV_F16 ? launch_kv_attend_f16_side
+                                                   : launch_kv_attend_e4m3_side;
+  if (!q) {  // (both are made ready)
+    const cudaError_t e = alone(c, q, w, num_sms, st);
+    return e != cudaSuccess || c.side == 0 ? e : side_by_side(c, q, w, num_sms, st);
+  }
+  // Without shared lines it is many short rows that gain, see kSideShort: with fewer the kernel would find too little.
+  const bool many = (int64_t)q->n * c.heads >= (int64_t)4 * KvAttendScratch::kCtasPerSm * num_sms;
+  return (c.side != 0 && (c.lines || many) ? side_by_side : alone)(c, q, w, num_sms, st);
 }
 
 // Scratch comes from a memory pool of the library's for each device, which keeps what destroyed handles give back: a
@@ -182,7 +185,8 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   c.head_stride = a.head_stride * es;
   c.by_page = p2p::FastDiv((uint32_t)a.page_tokens);
   c.row16 = (int32_t)(a.head_dim * es / 16);
-  c.side = heads_side_by_side(c);
+  c.lines = shares_lines(c);
+  c.side = c.heads % 4 == 0 ? 2 : c.heads % 2 == 0 ? 1 : 0;
   // Scratch, each part on a 256-byte boundary.
   size_t at = 0;
   const auto part = [&at](size_t bytes) {

@@ -172,6 +172,28 @@ def test_many_sequences_heads_inside_tokens(hq, hkv, dim, kind, page):
         assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
 
 
+@pytest.mark.parametrize("hq,hkv,dim,kind,page", [(32, 8, 128, "bf16", 16), (28, 4, 64, "f16", 5), (64, 8, 128, "e4m3", 32),
+                                                  (80, 4, 128, "bf16", 48), (6, 6, 256, "f16", 1), (48, 4, 192, "e4m3", 16)])
+def test_many_short_sequences(hq, hkv, dim, kind, page):
+    """Heads apart: a CTA takes neighbouring ones together for short sequences, one among them long; half of them once more
+    in another order, where the long one has more weight."""
+    n = 2000
+    rng = np.random.default_rng(dim + hq)
+    lengths = [int(x) for x in np.exp(rng.uniform(0, np.log(200), n))]
+    lengths[7], lengths[8], lengths[n // 2], lengths[n - 1] = 0, 3000, 40001, 0
+    c = make(lengths, hkv, dim, page, kind, "lnht")
+    dtype = torch.float16 if kind == "f16" else torch.bfloat16
+    got = c.attend(0, q := query(n, hq, dim, dtype))
+    again = c.attend(0, q)
+    c.sync()
+    check(c, 0, q, dim ** -0.5, got)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+    seq = torch.from_numpy(rng.permutation(n)[:n // 2].astype(np.int32)).cuda()
+    got = c.attend(0, q := query(n // 2, hq, dim, dtype, 6), seq=seq)
+    c.sync()
+    check(c, 0, q, dim ** -0.5, got, seq)
+
+
 def test_sequences_in_any_order_and_again():
     c = make(LENGTHS, 2, 64, 16, "bf16")
     seq = torch.tensor([20, 3, 3, 0, 17, 20, 5] * 7, dtype=torch.int32, device="cuda")   # (more rows than sequences)
