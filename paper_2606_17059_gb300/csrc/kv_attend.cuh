@@ -56,9 +56,9 @@ constexpr int kJoin = 16;               // parts of a unit row that are read tog
 // heads of 192 8-bit values 50 us, not 24; 21 of 20,000 tokens with 4 of 96 16-bit values 86 and 74 (29 parts); 40 of
 // 1,000 with 24 of 80 60, not 86.  Elsewhere, with so many units a row's head on average at most (kOver of them for
 // starting it), as there are fewer unit rows to start and finish: 2,000 sequences of 1 to 200 tokens (half below 15)
-// with 8 heads of 128 16-bit values take 90 us, not 129, of 8-bit values 104, not 179; 512 of 1 to 800 (5.6 units) with
-// 24 heads of 80 16-bit values 82, not 104, though with 4 of 256 83, not 66.  Beyond, joins cost as much or more: 512 of
-// 1 to 1,600 with 8 heads of 64 50 us and 48, with 4 of 256 115 and 92.
+// with 8 heads of 128 16-bit values take 78 us, not 129, of 8-bit values 103, not 179; 512 of 1 to 800 (5.6 units)
+// with 24 heads of 80 16-bit values 80, not 104, though with 4 of 256 83, not 66.  Beyond, joins cost as much or more:
+// 512 of 1 to 1,600 with 8 heads of 64 50 us and 48, with 4 of 256 115 and 92 (and 87 in the kernel without SIDE).
 constexpr int kSideUnits = 32, kSideParts = 16, kSideShort = 6;
 constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -705,8 +705,10 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
         }
       }
       __syncthreads();
-      for (int y = threadIdx.x; y < 8 * DP / 4 << side; y += kThreads) {
-        const int beside = y / (8 * DP / 4), head = y / (DP / 4) % 8, d = y % (DP / 4) * 4, h8 = b * 8 + head;
+      // (only the block's heads: with 32 on 8 of 128, 2,000 sequences of 1 to 40 tokens take 58 us, with all 8 68)
+      for (int y = threadIdx.x; y < min(8, heads - b * 8) * (DP / 4) << side; y += kThreads) {
+        const int own = y / (DP / 4), beside = own & ((1 << side) - 1), head = own >> side, d = y % (DP / 4) * 4;
+        const int h8 = b * 8 + head;
         float t = -INFINITY, z = 0.f;
 #pragma unroll
         for (int k = 0; k < kWarps; ++k)  // the warps that had this kv head
@@ -726,7 +728,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
           const int at = beside * S::kHeads + h8;
           *(float4*)(part + at * DP + d) = v;
           if (d == 0) part[part_heads * DP + at] = t, part[part_heads * (DP + 1) + at] = z;
-        } else if (h8 < heads) {
+        } else {
           const int32_t q_head = head0 + beside * group + h8;
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
           store4(c, a, u.i, q_head, d, v, __fdividef(v_scale, z), empty);
