@@ -95,7 +95,7 @@ struct Shape {
   static constexpr int kStage = 2 * kArray;
   // Resident on an SM: three where three have room for more than two tiles a warp and registers enough (168 a
   // thread), one where two have not.
-  static constexpr int kCtas = kRows * kRowBytes <= 3072 && DP * NB <= 256 ? 3 : kRowBytes <= 256 ? 2 : 1;
+  static constexpr int kCtas = kRows * kRowBytes <= 3 * 1024 && DP * NB <= 256 ? 3 : kRowBytes <= 256 ? 2 : 1;
   static constexpr int kSumPitch = (DP + 31) / 32 * 32;        // of a head's sums, which lie in the room of a tile
   static_assert(8 * kSumPitch * 4 <= kStage);
   static constexpr int kFit = (232448 / kCtas - 1024 - 512) / kWarps / kStage;
