@@ -25,9 +25,12 @@
 // looked up two tiles ahead.  Sixteen tokens are multiplied transposed: S^T [tokens, heads] = K Q^T and O^T [dim,
 // heads] += V^T P^T, so that eight query heads fill a product's n and the tokens (or values) its m of 16.  P^T goes
 // from the first product's layout to the second's by two 8 x 8 transposes of registers.  exp(x - m) takes for m not
-// the running maximum but one that lags it by at most a factor of 2^8, so that a tile's maximum is only reduced, and
-// O rescaled, where it goes past that.  P is rounded to the values' type (f16 for 8 bits) for its product; sums,
-// maxima and O are held in 32 bits.
+// the running maximum but one that lags it by at most a factor of 2^8 (2^3 for f16 and 8 bits), so that a tile's maximum
+// is only reduced, and O rescaled, where it goes past that.  P is rounded to the values' type (f16 for 8 bits) for its
+// product; sums, maxima and O are held in 32 bits.  Of f16, whose range is small, P takes the upper end (kUp): what is
+// 2^26 times smaller than a warp's largest keeps all 11 bits, what is 2^37 times smaller is lost, 2^-37 of the largest
+// a token at most.  (P <= 1 loses bits from 2^-14 on and everything below 2^-25, and then, where one token that is far
+// ahead has values near zero, what the result consists of.)
 //
 // The products are warp-wide ones (mma): 9% of the tensor cores' time at the copy bandwidth (8 bits: 17%), and their
 // operands come out of shared memory by ldmatrix in any row size.  The tensor memory path (tcgen05) would free issue
@@ -60,22 +63,26 @@ constexpr int kJoin = 16;               // parts of a unit row that are read tog
 // with 24 heads of 80 16-bit values 80, not 104, though with 4 of 256 83, not 66.  Beyond, joins cost as much or more:
 // 512 of 1 to 1,600 with 8 heads of 64 50 us and 48, with 4 of 256 115 and 92 (and 87 in the kernel without SIDE).
 constexpr int kSideUnits = 32, kSideParts = 16, kSideShort = 6;
-constexpr float kLag = 8.f;             // how far (log2) a logit may pass the maximum in use
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// kUp: exp(x - m) is taken times 2^kUp (m is held less kUp, in log2).  kLag: how far (log2) a logit may pass the maximum
+// in use.  P is at most 2^(kUp + kLag), which f16 has to hold.
 template <int KIND>
 struct Type;
 template <>
 struct Type<P2P_KV_BF16> {
   static constexpr int kSize = 2;
+  static constexpr float kUp = 0.f, kLag = 8.f;
 };
 template <>
 struct Type<P2P_KV_F16> {
   static constexpr int kSize = 2;
+  static constexpr float kUp = 12.f, kLag = 3.f;
 };
 template <>
 struct Type<P2P_KV_E4M3> {
   static constexpr int kSize = 1;
+  static constexpr float kUp = 12.f, kLag = 3.f;
 };
 
 // Sizes of the kernel for values of KIND, head_dim padded to DP, NB blocks of eight query heads.
@@ -155,6 +162,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// ln of a sum of exp that was taken relative to t (in log2): near the largest term, where log2 is small.
+template <int KIND>
+__device__ __forceinline__ float log_sum(float t, float z) {
+  constexpr float kUp = Type<KIND>::kUp, kDown = 1.f / (1 << (int)kUp);
+  return (t + kUp + __log2f(z * kDown)) * kLn2;
 }
 template <int KIND>
 __device__ __forceinline__ uint32_t pack(float a, float b) {
@@ -604,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int y = 0; y < 4; ++y) past |= s[m][b][y] > top[b][y & 1] + kLag;
+          for (int y = 0; y < 4; ++y) past |= s[m][b][y] > top[b][y & 1] + (Type<KIND>::kUp + Type<KIND>::kLag);
       if (__any_sync(~0u, past)) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -616,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
             t = fmaxf(t, __shfl_xor_sync(~0u, t, 4));
             t = fmaxf(t, __shfl_xor_sync(~0u, t, 8));
             t = fmaxf(t, __shfl_xor_sync(~0u, t, 16));
-            t = fmaxf(t, top[b][y]);
+            t = fmaxf(t - Type<KIND>::kUp, top[b][y]);
             const float fade = t == -INFINITY ? 1.f : exp2_fast(top[b][y] - t);
             top[b][y] = t;
             sum[b][y] *= fade;
@@ -732,7 +745,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
           const int32_t q_head = head0 + beside * group + h8;
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
           store4(c, a, u.i, q_head, d, v, __fdividef(v_scale, z), empty);
-          if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = empty ? -INFINITY : (t + __log2f(z)) * kLn2;
+          if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = empty ? -INFINITY : log_sum<KIND>(t, z);
         }
       }
       if (whole || b + 1 < NB) __syncthreads();  // the sums' room is free again
@@ -848,7 +861,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
               const int32_t q_head = head0 + beside * group + at[i] % S::kHeads;
               const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
               store4(c, a, u.i, q_head, d[i], v[i], __fdividef(v_scale, z[i]), false);
-              if (d[i] == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = (t[i] + __log2f(z[i])) * kLn2;
+              if (d[i] == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = log_sum<KIND>(t[i], z[i]);
             } else {
               *(float4*)(joined + at[i] * DP + d[i]) = v[i];
               if (d[i] == 0) joined[part_heads * DP + at[i]] = t[i], joined[part_heads * (DP + 1) + at[i]] = z[i];
