@@ -484,9 +484,10 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyCtas)
 
 // Where the tokens of a block go is found once, a lane a token, and serves all their heads in the layers and arrays
 // that the CTA writes; the first values are read while it is found.  Bound by the bytes read and written: 61 prompts
-// of 71,000 tokens, 2.3 GB of bf16 values in and 1.2 GB of 8-bit values out, in 0.56 ms on one GB300 (92% of the copy
+// of 71,000 tokens, 2.3 GB of bf16 values in and 1.2 GB of 8-bit values out, in 0.53 ms on one GB300 (97% of the copy
 // bandwidth).
 constexpr int kBlock = 32, kWriteThreads = 256;
+constexpr int kFactors = 4096;  // scales of a CTA at most, with 8-bit values: 32 KB of shared memory
 static_assert(kBlock == 32, "a warp finds the places, all its lanes together");
 
 // The last item that starts at or before token t (items without tokens share a start): every lane gets it.
@@ -504,12 +505,40 @@ __device__ __forceinline__ int32_t find_item(const int64_t* offsets, int32_t n, 
   return lo;
 }
 
-// x / scale rounded to the nearest 32-bit value: the quotient by the rounded reciprocal, put right by its exact
-// remainder (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990), for
-// scales of ordinary size; a quotient that is above 448 by far stays as it is.
-__device__ __forceinline__ float divide(float x, float scale, float inverse) {
-  const float y = x * inverse, z = fmaf(fmaf(-y, scale, x), inverse, y);
-  return fabsf(y) < 65536.f ? z : y;
+// Rounding x / scale to 8 bits, x of at most 11 bits.  What must not happen is that a quotient close to the middle
+// between two 8-bit values (a tie: T, odd and below 32, times a power of two) is rounded to it, or across it, first.
+// It can for X / T alone that is next to the scale, X of 11 bits: two such ratios are 2^-16 apart, so that it is one
+// of them at most, and it says on which side of their ties all quotients lie that are close to one.  So a product with
+// a factor 2^-20 above the reciprocal (where the scale is above that ratio: below) rounds as the quotient does.  A
+// scale of up to 12 bits can be such a ratio exactly, and is 2^-17 away from all others: there 32 bits of the quotient
+// are enough, but for ties they have to be right, and the factor has two parts.  (By division and remainder for each
+// value, the 61 prompts below take 597 us, not 534; rounded twice, 574.)
+__device__ __forceinline__ bool ordinary(float scale) {
+  return fabsf(scale) > 0x1p-60f && fabsf(scale) < 0x1p60f;
+}
+// The factor for a scale (x: 0 where it is of an extreme size), by the 16 lanes of a half warp, one for each T; every
+// lane gets it.  Its second part, if not 0, has the sign of the first.
+__device__ __forceinline__ float2 factor_of(float scale) {
+  const uint32_t lane = threadIdx.x & 31, x = (__float_as_uint(scale) & 0x7fffff) | 0x800000;
+  const uint32_t p = x * (2 * (lane & 15) + 1), n = 31 - __clz(p);  // scale * T, of n + 1 bits
+  // beyond its first 11 bits, and 2^-18 of it
+  const uint32_t rest = p & ((1u << (n - 10)) - 1), close = 1u << (n - 18);
+  const uint32_t above = __ballot_sync(~0u, rest < close) >> (lane & 16) & 0xffff;
+  if (!ordinary(scale)) return make_float2(0.f, 0.f);
+  if ((x & 0xfff) == 0) {
+    const float most = __frcp_rz(scale);
+    return make_float2(most, fmaf(-scale, most, 1.f) * most);
+  }
+  const float inverse = __frcp_rn(scale);
+  return make_float2(fmaf(inverse, above ? -0x1p-20f : 0x1p-20f, inverse), 0.f);
+}
+// If the quotient rounded to 32 bits is a tie (its 19 lowest bits are zero) and the quotient is not: one step to its
+// side, as its exact remainder tells (of which nothing vanishes or overflows).  For scales of an extreme size.
+__device__ __forceinline__ float divide_extreme(float x, float scale) {
+  const float z = __fdiv_rn(x, scale), up = fabsf(scale) < 1.f ? 0x1p100f : 1.f, r = fmaf(-z, scale * up, x * up);
+  int32_t b = __float_as_int(z);
+  if ((b & 0x7ffff) == 0 && (r < 0.f || r > 0.f)) b += (r < 0.f) == (x < 0.f) ? 1 : -1;
+  return __int_as_float(b);
 }
 template <bool BF16>
 __device__ __forceinline__ float2 two_values(uint32_t x) {
@@ -519,21 +548,15 @@ __device__ __forceinline__ float2 two_values(uint32_t x) {
 __device__ __forceinline__ uint32_t narrow(float2 v) {
   return __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3);
 }
-template <bool BF16>
-__device__ __forceinline__ uint4 narrow16(const uint4& a, const uint4& b, float scale, float inverse, bool plain) {
+// 16 values, each by `divide`, to 8 bits.
+template <bool BF16, class F>
+__device__ __forceinline__ uint4 narrow16(const uint4& a, const uint4& b, F divide) {
   const uint32_t in[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
   uint32_t out[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float2 v = two_values<BF16>(in[2 * i]), w = two_values<BF16>(in[2 * i + 1]);
-    if (plain) {
-      v.x = divide(v.x, scale, inverse), v.y = divide(v.y, scale, inverse);
-      w.x = divide(w.x, scale, inverse), w.y = divide(w.y, scale, inverse);
-    } else {
-      v.x = __fdiv_rn(v.x, scale), v.y = __fdiv_rn(v.y, scale);
-      w.x = __fdiv_rn(w.x, scale), w.y = __fdiv_rn(w.y, scale);
-    }
-    out[i] = narrow(v) | narrow(w) << 16;
+    const float2 x = two_values<BF16>(in[2 * i]), y = two_values<BF16>(in[2 * i + 1]);
+    out[i] = narrow(make_float2(divide(x.x), divide(x.y))) | narrow(make_float2(divide(y.x), divide(y.y))) << 16;
   }
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
@@ -568,6 +591,7 @@ __global__ void __launch_bounds__(kWriteThreads)
     write_kernel(KvView c, KvScratch s, int32_t layer, int32_t n_layers, int32_t share, int32_t n, const int32_t* seq,
                  const int64_t* offsets, int64_t n_tokens, KvRows in, FastDiv by_token, FastDiv by_row) {
   __shared__ int64_t place[kBlock];  // of a token, within its layer; -1: it is not written
+  extern __shared__ float2 factor[];  // 8-bit values: for the scales of the CTA's arrays and heads (see factor_of)
   begin_kernel();
   const int32_t halt = *s.halt;
   const int64_t t0 = (int64_t)blockIdx.x * kBlock;
@@ -577,7 +601,7 @@ __global__ void __launch_bounds__(kWriteThreads)
   // Values and loads of a piece, and pieces of a thread in flight.
   constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8, kLoads = kValues / 8, kAhead = 4 / kLoads;
   uint4 v[kAhead][kLoads];
-  float scale[kAhead];
+  int32_t scaled[kAhead];  // the number of its scale among the CTA's
   char* to[kAhead];      // but for the token's place
   int32_t token[kAhead];  // of the block; -1: no piece
   const auto read = [&](uint32_t y0) {
@@ -593,10 +617,14 @@ __global__ void __launch_bounds__(kWriteThreads)
       const uint16_t* from = (const uint16_t*)(array & 1 ? in.v : in.k) + l * in.layer_stride +
           (t0 + t) * in.token_stride + h * in.head_stride + piece * kValues;
       read_values<WIDE>(v[k], from);
-      if (KIND == P2P_KV_E4M3) scale[k] = (array & 1 ? c.v_scale : c.k_scale)[(layer + l) * c.heads + h];
+      scaled[k] = over * c.heads + h;
       to[k] = (array & 1 ? c.v : c.k) + (int64_t)(layer + l) * c.layer_stride + h * c.head_stride + piece * 16;
       token[k] = t;
     }
+  };
+  const auto scale_at = [&](int32_t i) {
+    const int32_t over = i / c.heads, array = a0 + over;
+    return (array & 1 ? c.v_scale : c.k_scale)[(layer + (array >> 1)) * c.heads + i - over * c.heads];
   };
   read(threadIdx.x);  // (on their way while it is found where they go)
   if (blockIdx.x == 0 && blockIdx.y == 0)
@@ -632,6 +660,12 @@ __global__ void __launch_bounds__(kWriteThreads)
       if (bad) atomicOr(s.err, bad);
     }
     place[threadIdx.x] = at;
+  } else if (KIND == P2P_KV_E4M3) {  // (the other warps, a scale for each half of one)
+    const int32_t scales = (a1 - a0) * c.heads, half = threadIdx.x >> 4 & 1;
+    for (int32_t i0 = (threadIdx.x - kBlock) / 32 * 2; i0 < scales; i0 += (kWriteThreads - kBlock) / 16) {
+      const float2 f = factor_of(scale_at(min(i0 + half, scales - 1)));
+      if ((threadIdx.x & 15) == 0 && i0 + half < scales) factor[i0 + half] = f;
+    }
   }
   __syncthreads();
   const auto write = [&]() {
@@ -640,8 +674,16 @@ __global__ void __launch_bounds__(kWriteThreads)
       const int64_t at = token[k] < 0 ? -1 : place[token[k]];
       if (at < 0) continue;
       if (KIND == P2P_KV_E4M3) {
-        const bool plain = fabsf(scale[k]) > 0x1p-60f && fabsf(scale[k]) < 0x1p60f;
-        __stcs((uint4*)(to[k] + at), narrow16<BF16>(v[k][0], v[k][kLoads - 1], scale[k], __frcp_rn(scale[k]), plain));
+        uint4 x;
+        if (const float2 f = factor[scaled[k]]; f.x == 0.f) {
+          const float scale = scale_at(scaled[k]);
+          x = narrow16<BF16>(v[k][0], v[k][kLoads - 1], [&](float y) { return divide_extreme(y, scale); });
+        } else if (f.y == 0.f) {
+          x = narrow16<BF16>(v[k][0], v[k][kLoads - 1], [&](float y) { return y * f.x; });
+        } else {
+          x = narrow16<BF16>(v[k][0], v[k][kLoads - 1], [&](float y) { return fmaf(y, f.x, y * f.y); });
+        }
+        __stcs((uint4*)(to[k] + at), x);
       } else {
         __stcs((uint4*)(to[k] + at), v[k][0]);
       }
@@ -691,12 +733,16 @@ cudaError_t write_launch(const KvView& c, const KvScratch& s, int32_t layer, int
   // All arrays of a block of tokens in one CTA where there are many blocks, else as few as fill the GPU.
   const int64_t want = (8LL * num_sms + blocks - 1) / blocks;
   // (A CTA's pieces are counted in 32 bits.)
-  const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / (kBlock * c.heads * c.row16));
+  int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / (kBlock * c.heads * c.row16));
+  static_assert(kFactors >= 4 * 1024, "with all the heads there may be, those of all layers in a grid of 65,535");
+  if (KIND == P2P_KV_E4M3) most = std::min<int64_t>(most, kFactors / c.heads);
   const int64_t arrays = 2 * n_layers;
   const int32_t share = (int32_t)std::min(most, std::max<int64_t>(1, arrays / std::min(want, arrays)));
   const dim3 grid((unsigned)blocks, (unsigned)((2 * n_layers + share - 1) / share));
-  return launch_early(write_kernel<KIND, BF16, WIDE>, grid, kWriteThreads, 0, st, c, s, layer, n_layers, share, n, seq,
-                      offsets, n_tokens, rows, FastDiv((uint32_t)(c.heads * c.row16)), FastDiv((uint32_t)c.row16));
+  const size_t factors = KIND == P2P_KV_E4M3 ? sizeof(float2) * share * c.heads : 0;
+  return launch_early(write_kernel<KIND, BF16, WIDE>, grid, kWriteThreads, factors, st, c, s, layer, n_layers, share, n,
+                      seq, offsets, n_tokens, rows, FastDiv((uint32_t)(c.heads * c.row16)),
+                      FastDiv((uint32_t)c.row16));
 }
 
 template <int KIND, bool BF16>
