@@ -448,7 +448,8 @@ int p2p_kv_fork(p2p_kv* kv, int32_t n, const int32_t* src, const int32_t* dst, c
 int p2p_kv_trim(p2p_kv* kv, int32_t n, const int32_t* seq, const int32_t* n_tokens);
 
 /* Moves the pages in use to the front of the pool: with n of them, those numbered n and up go, in ascending order, to
- * the free ones below n, in ascending order; contents, table and refs follow. */
+ * the free ones below n, in ascending order; contents, table and refs follow.  Device-side errors (nothing changes): a
+ * sequence whose length is out of range, or an entry within it that names no page in use. */
 int p2p_kv_compact(p2p_kv* kv);
 
 /* Attention of one new token of each of n sequences seq[i] (NULL: sequences 0 .. n-1; one may be named again) over the

@@ -92,7 +92,7 @@ cudaError_t launch_kv_trim(const KvView& c, const KvScratch& s, int32_t n, const
                            cudaStream_t st);
 cudaError_t launch_kv_fork(const KvView& c, const KvScratch& s, int32_t n, const int32_t* src, const int32_t* dst,
                            const int32_t* tokens, cudaStream_t st);
-cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, cudaStream_t st, int* launches);
 // Keys and values to write; strides in elements.
 struct KvRows {
   const void *k, *v;

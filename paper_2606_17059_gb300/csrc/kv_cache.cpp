@@ -328,8 +328,9 @@ int p2p_kv_fork(p2p_kv* h, int32_t n, const int32_t* src, const int32_t* dst, co
 int p2p_kv_compact(p2p_kv* h) {
   if (!h) return fail(nullptr, P2P_E_INVAL, "cache is NULL");
   DeviceGuard g(h->device);
-  CK(p2p::launch_kv_compact(h->c, h->s, h->num_sms, h->stream));
-  h->launches += 2;
+  int launches = 0;
+  CK(p2p::launch_kv_compact(h->c, h->s, h->num_sms, h->stream, &launches));
+  h->launches += launches;
   return P2P_OK;
 }
 

@@ -361,9 +361,54 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     for (int32_t i = threadIdx.x; i < n; i += kThreads) c.length[dst[i]] = tokens[i];
 }
 
+// Before a compaction: every length is one that the table holds, and every entry within it names a page in use; else
+// an error's bits.  `warps` of them, of which this is number `warp`, share the sequences, `each` of them the entries
+// of one.
+constexpr int kChunk = 256;  // entries that a warp has on their way
+__device__ __forceinline__ int32_t check_rows(const KvView& c, int32_t warp, int32_t warps, int32_t each) {
+  const int lane = threadIdx.x & 31;
+  const int32_t per_turn = warps / each;
+  int32_t bad = 0;
+  if (warp >= per_turn * each) return 0;
+  for (int32_t q = warp / each; q < c.n_seqs; q += per_turn) {
+    const int32_t len = length_of(c, q), used = len < 0 ? 0 : (int32_t)c.by_page.ceil(len);
+    if (len < 0) bad |= KV_BAD_COUNT;
+    const int32_t* row = row_of(c, q);
+    for (int64_t e0 = (int64_t)(warp % each) * kChunk; e0 < used; e0 += (int64_t)each * kChunk) {
+      int32_t page[kChunk / 32];
+#pragma unroll
+      for (int k = 0; k < kChunk / 32; ++k) {
+        const int64_t e = e0 + 32 * k + lane;
+        page[k] = e < used ? __ldcg(row + e) : 0;
+      }
+#pragma unroll
+      for (int k = 0; k < kChunk / 32; ++k)
+        if (e0 + 32 * k + lane < used)
+          if ((uint32_t)page[k] >= (uint32_t)c.n_pages || __ldcg(c.refs + page[k]) < 1) bad |= KV_BAD_PAGE;
+    }
+  }
+  return bad;
+}
+// How many warps a sequence, of those there are.
+int32_t warps_each(const KvView& c, int32_t warps) {
+  return std::max(1, std::min(warps / c.n_seqs, (c.max_pages - 1) / kChunk + 1));
+}
+constexpr int kCheckThreads = 256, kCheckCtas = 4;
+__global__ void __launch_bounds__(kCheckThreads) check_kernel(KvView c, KvScratch s, int32_t each) {
+  begin_kernel();
+  const int32_t halt = *s.halt, warp = (int32_t)(blockIdx.x * kCheckThreads + threadIdx.x) >> 5;
+  const int32_t bad = check_rows(c, warp, (int32_t)(gridDim.x * (kCheckThreads / 32)), each);
+  if (bad && !halt) {
+    atomicOr(s.err, bad);
+    *s.halt = 1;
+  }
+}
+
 // `live` pages are in use: those numbered live and up go to the free ones below, both in ascending order.  The k-th of
-// either kind is job k's; list[page]: where a page goes (the tables follow in copy_pages_kernel).
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) compact_kernel(KvView c, KvScratch s) {
+// either kind is job k's; list[page]: where a page goes (the tables follow in copy_pages_kernel).  With `each` the
+// cluster checks the tables itself.
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+    compact_kernel(KvView c, KvScratch s, int32_t each) {
   __shared__ Plan p;
   begin_kernel();
   cg::cluster_group cluster = cg::this_cluster();
@@ -375,9 +420,15 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) com
   if (*s.halt) return;
   __syncthreads();
   const Part mine = part_of(c, rank);
+  if (each)
+    if (const int32_t bad = check_rows(c, rank * kWarps + (threadIdx.x >> 5), kCluster * kWarps, each))
+      atomicOr(&p.err, bad);
   int32_t used;
   scan_warps(p, count_pages(c, mine, [](int32_t, int32_t refs) { return refs > 0; }), used);
-  meet(p, used, 0);
+  if (const int32_t err = meet(p, used, 0)) {
+    if (rank == 0 && threadIdx.x == 0) atomicOr(s.err, err), *s.halt = 1;
+    return;
+  }
   int64_t live = 0;
 #pragma unroll
   for (int k = 0; k < kCluster; ++k) live += p.found[k].count;
@@ -424,20 +475,14 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyCtas)
   begin_kernel();
   // (Loads past the first cache: this launch may have shared its SM with the plan's.)
   const int32_t njobs = __ldcg(s.njobs);
-  if (moved && !__ldcg(s.halt)) {  // the tables of a compaction
+  if (moved && !__ldcg(s.halt)) {  // the tables of a compaction (which were found to hold together)
     const int32_t live = __ldcg(s.live);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int32_t q = blockIdx.x * (kCopyThreads / 32) + warp; q < c.n_seqs; q += gridDim.x * (kCopyThreads / 32)) {
-      const int32_t len = length_of(c, q), used = len < 0 ? 0 : (int32_t)c.by_page.ceil(len);
-      if (len < 0 && lane == 0) atomicOr(s.err, KV_BAD_COUNT);
+      const int32_t used = (int32_t)c.by_page.ceil(c.length[q]);
       int32_t* row = row_of(c, q);
-      for (int32_t e = lane; e < used; e += 32) {
-        const int32_t page = __ldcg(row + e);
-        if ((uint32_t)page >= (uint32_t)c.n_pages)
-          atomicOr(s.err, KV_BAD_PAGE);
-        else if (page >= live)
-          row[e] = __ldcg(s.list + page);
-      }
+      for (int32_t e = lane; e < used; e += 32)
+        if (const int32_t page = __ldcg(row + e); page >= live) row[e] = __ldcg(s.list + page);
     }
   }
   if (njobs == 0) return;
@@ -779,8 +824,21 @@ cudaError_t launch_kv_fork(const KvView& c, const KvScratch& s, int32_t n, const
   return launch_early(fork_kernel, dim3(kCluster), kThreads, item_bytes(n), st, c, s, n, src, dst, tokens);
 }
 
-cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, cudaStream_t st) {
-  const cudaError_t e = launch_early(compact_kernel, dim3(kCluster), kThreads, 0, st, c, s);
+cudaError_t launch_kv_compact(const KvView& c, const KvScratch& s, int num_sms, cudaStream_t st,
+                              int* launches) {
+  // Tables of as many chunks as the plan has warps are checked there, larger ones by a launch of their own over the
+  // whole GPU: a compaction that finds nothing to move takes, with 40 sequences of 72 pages, 9.5 us (10.3 with the
+  // launch, 7.6 without a check), with 600 of 136 14.0 (15.9 by the plan, 10.5), with 200,000 of 3 102 (658, 38).
+  int32_t each = warps_each(c, kCluster * kWarps);
+  cudaError_t e = cudaSuccess;
+  *launches = 2;
+  if ((int64_t)c.n_seqs * ((c.max_pages - 1) / kChunk + 1) > kCluster * kWarps) {
+    each = warps_each(c, kCheckCtas * num_sms * (kCheckThreads / 32));
+    e = launch_early(check_kernel, dim3(kCheckCtas * num_sms), kCheckThreads, 0, st, c, s, each);
+    each = 0;
+    *launches = 3;
+  }
+  if (e == cudaSuccess) e = launch_early(compact_kernel, dim3(kCluster), kThreads, 0, st, c, s, each);
   return e == cudaSuccess ? launch_copies(c, s, true, num_sms, st) : e;
 }
 
