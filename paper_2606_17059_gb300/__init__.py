@@ -453,6 +453,7 @@ def p2p_kv_create(layout: KvLayout):
     """Handle on the cache that `layout` describes (its device arrays must outlive the handle)."""
     h = _vp()
     _kv_check(_load().p2p_kv_create(ctypes.byref(layout), ctypes.byref(h)))
+    h.stream, h.stream_address = None, 0  # (the calls' stream, for KvCache: as p2p_kv_set_stream was last given it)
     return h
 
 
@@ -465,6 +466,8 @@ def p2p_kv_set_stream(kv, stream=None) -> None:
     if stream is not None:
         s = stream if isinstance(stream, int) else stream.cuda_stream
     _kv_check(_load().p2p_kv_set_stream(kv, s), kv)
+    if isinstance(kv, _vp):
+        kv.stream, kv.stream_address = stream, s or 0
 
 
 def p2p_kv_sync(kv) -> None:
@@ -530,9 +533,11 @@ class KvCache:
     table     int32 [sequences, pages a sequence]; length int32 [sequences]; refs int32 [pages]
     k_scale, v_scale   float32 [layers, heads], with float8_e4m3fn only
 
-    ``KvCache.empty`` allocates them.  Calls run on `stream` (torch's current one at construction) and return before their
-    work is done; tensors made or used on another stream are the caller's to order.  What the device finds wrong is
-    raised by ``sync``."""
+    ``KvCache.empty`` allocates them.  Calls run on `stream` (torch's current one at construction; ``set_stream`` gives them
+    another) and return before their work is done; tensors made or used on another stream are the caller's to order.  What
+    ``attend`` allocates itself is allocated on the calls' stream: a program on another one waits for that stream before it
+    reads the result, and keeps it (or calls its record_stream) until that is done.  A CUDA graph records the calls of a cache
+    whose stream is the one being captured.  No call records gradients.  What the device finds wrong is raised by ``sync``."""
 
     def __init__(self, k, v, table, length, refs, k_scale=None, v_scale=None, stream=None):
         import torch
@@ -563,11 +568,13 @@ class KvCache:
             lib.p2p_kv_extend, lib.p2p_kv_trim, lib.p2p_kv_fork, lib.p2p_kv_write, lib.p2p_kv_attend)
         a = KvLayout(self._types[k.dtype], layers, pages, page, heads, dim, table.shape[0], table.shape[1], *k.stride()[:4],
                      k.data_ptr(), v.data_ptr(), _addr(k_scale), _addr(v_scale), table.data_ptr(), length.data_ptr(), refs.data_ptr())
-        self.device = k.device
+        self.device, self._index = k.device, k.device.index
+        self._cuda, self._current = torch.cuda, torch._C._cuda_getCurrentRawStream
         with torch.cuda.device(k.device):
             self._h = p2p_kv_create(a)
-            self.stream = stream if stream is not None else torch.cuda.current_stream()
-        p2p_kv_set_stream(self._h, self.stream)
+            if stream is None:
+                stream = torch.cuda.current_stream()
+        p2p_kv_set_stream(self._h, stream)
 
     @classmethod
     def empty(cls, layers: int, pages: int, page: int, heads: int, dim: int, n_seqs: int, max_pages: int, dtype=None, k_scale=None,
@@ -590,6 +597,23 @@ class KvCache:
 
     def __del__(self):
         self.close()
+
+    @property
+    def stream(self):
+        """The calls' stream."""
+        return None if self._h is None else self._h.stream
+
+    def set_stream(self, stream) -> None:
+        """Gives the calls another stream (waits for the work queued on the one before)."""
+        p2p_kv_set_stream(self._h, stream)
+
+    def _empty_on_stream(self, shape, dtype, device):
+        """torch.empty, where torch's current stream is not the calls'."""
+        s = self._h.stream
+        if s is None or isinstance(s, int):
+            s = self._cuda.ExternalStream(s, device) if s else self._cuda.default_stream(device)
+        with self._cuda.stream(s):
+            return self._empty(shape, dtype=dtype, device=device)
 
     def _list(self, t, n: int, dtype) -> int:
         """Address of a list of n entries."""
@@ -648,15 +672,16 @@ class KvCache:
         kind = self._types.get(dtype)
         if dim != self.dim or kind is None or inner != 1 and dim > 1 or q.device != self.device:
             raise ValueError("q must be [n, query heads, head dim] on the cache's device, the last dimension contiguous")
+        empty = self._empty if self._current(self._index) == self._h.stream_address else self._empty_on_stream
         if out is None:
-            out = self._empty(shape, dtype=dtype, device=self.device)
+            out = empty(shape, dtype=dtype, device=self.device)
             out_row, out_head = heads * dim, dim
         else:
             if out.shape != shape or out.dtype is not dtype or out.device != self.device or out.stride(2) != 1 and dim > 1:
                 raise ValueError("out must be like q, the last dimension contiguous")
             out_row, out_head, _ = out.stride()
         if lse is None:
-            lse = self._empty((n, heads), dtype=self._float32, device=self.device)
+            lse = empty((n, heads), dtype=self._float32, device=self.device)
         elif (tuple(lse.shape) != (n, heads) or lse.dtype is not self._float32 or lse.device != self.device
               or not lse.is_contiguous()):
             raise ValueError("lse must be contiguous float32 [n, query heads]")
