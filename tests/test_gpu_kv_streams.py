@@ -1,4 +1,4 @@
-"""The paged cache's calls on streams: which one the results belong to, and a change of it."""
+"""The paged cache's calls on streams: which one the results belong to, a change of it, handles made after others, and that calls allocate nothing."""
 import pytest
 
 import paper_2606_17059_gb300 as g
@@ -7,7 +7,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 if torch.cuda.is_available():
-    from test_gpu_kv_attend import make, query
+    from test_gpu_kv_attend import check, make, query
 
 
 def test_results_belong_to_the_calls_stream():
@@ -58,3 +58,56 @@ def test_the_stream_is_changed():
     assert torch.equal(out, want) and torch.equal(lse, want_lse)
     c.close()
     assert c.stream is None
+
+
+def test_handles_after_handles():
+    """Scratch that a destroyed handle gave back is a later one's, whose calls find in it what a new one's would."""
+    st = torch.cuda.Stream()
+    for turn in range(6):
+        lengths = [[70001], [40, 0, 300], [5] * 2000][turn % 3]
+        c = make(lengths, 4, 128, 16, "bf16", seed=turn)
+        torch.cuda.synchronize()
+        if turn % 2:
+            c.set_stream(st)
+        q = query(len(lengths), 8, 128, torch.bfloat16, seed=turn)
+        got = c.attend(0, q)
+        c.sync()
+        check(c, 0, q, 128 ** -0.5, got)
+        if turn != 3:
+            c.close()                          # (with nothing queued; the others are closed with a call under way)
+        else:
+            c.attend(0, q)
+            c.close()
+            c.close()
+
+
+def test_calls_allocate_nothing():
+    """Once a handle is made, calls take no device memory from the driver, nor from torch beyond attend's own results."""
+    c = make([100, 9000, 5], 2, 64, 16, "bf16", spare=40)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q = query(3, 14, 64, torch.bfloat16)
+    out, lse = torch.empty_like(q), torch.empty((3, 14), device="cuda")
+    k = torch.zeros((1, 7, 2, 64), device="cuda", dtype=torch.bfloat16)
+    seq, other, count, less, off = i32(0), i32(2), i32(7), i32(90), torch.tensor([0, 7], device="cuda")
+    none, part = i32(0), i32(33)
+
+    def calls():
+        c.extend(seq, count)
+        c.write(0, seq, off, k, k)
+        c.attend(0, q, out=out, lse=lse)
+        c.trim(other, none)
+        c.fork(seq, other, part)
+        c.extend(other, count)
+        c.compact()
+        c.trim(seq, less)
+        c.sync()
+
+    c.trim(seq, less)
+    calls()
+    torch.cuda.synchronize()
+    free, held = torch.cuda.mem_get_info()[0], torch.cuda.memory_stats()["allocation.all.allocated"]
+    for _ in range(20):
+        calls()
+    torch.cuda.synchronize()
+    assert torch.cuda.mem_get_info()[0] == free
+    assert torch.cuda.memory_stats()["allocation.all.allocated"] == held
