@@ -102,6 +102,20 @@ const char* check_layout(const p2p_kv_layout& a) {
 // 16-bit values 240 us with pages of 16 tokens either way, 304 and 280 with pages of one.)
 bool shares_lines(const p2p::KvView& c) { return c.head_stride <= c.token_stride && c.row16 % 16 != 0; }
 
+// Whether two of the rows that a result is written to, `dim` values each at i * row + h * head (i < n, h < heads), share
+// a value.
+bool rows_overlap(int64_t n, int64_t heads, int64_t dim, int64_t row, int64_t head) {
+  using wide = __int128;
+  const wide r = row < 0 ? -(wide)row : row, g = head < 0 ? -(wide)head : head;
+  if ((n > 1 && r < dim) || (heads > 1 && g < dim)) return true;
+  if (n == 1 || heads == 1 || r >= (heads - 1) * g + dim || g >= (n - 1) * r + dim) return false;
+  for (int64_t h = 1; h < heads; ++h) {  // (neither dimension lies within the other's steps)
+    const wide i = h * g / r;
+    if ((i < n && h * g - i * r < dim) || (i + 1 < n && (i + 1) * r - h * g < dim)) return true;
+  }
+  return false;
+}
+
 cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p::KvAttendScratch& w, int num_sms,
                           cudaStream_t st) {
   using namespace p2p;
@@ -368,6 +382,8 @@ int p2p_kv_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const
   if (!q || !out) return fail(h, P2P_E_INVAL, "NULL device pointer");
   if ((uintptr_t)q % 2 || (uintptr_t)out % 2 || (uintptr_t)lse % 4)
     return fail(h, P2P_E_INVAL, "a pointer is not aligned to its type");
+  if (rows_overlap(n, n_heads, h->c.dim, out_row_stride, out_head_stride))
+    return fail(h, P2P_E_INVAL, "rows of out overlap");
   DeviceGuard g(h->device);
   const p2p::KvQuery a = {q, out, lse, seq, q_row_stride, q_head_stride, out_row_stride, out_head_stride,
                           n, n_heads, type, window, layer, scale,
