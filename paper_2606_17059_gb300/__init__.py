@@ -658,6 +658,8 @@ class KvCache:
                              "the last dimension contiguous")
         if k.device != self.device or v.device != self.device:
             raise ValueError("tensors must be on the cache's device")
+        if not 0 <= layer <= self.layers:
+            layer = -1  # (refused by the call, whose numbers are of 32 bits)
         rc = self._write(self._h, layer, shape[0], n, self._list(seq, n, self._int32), self._list(offsets, n + 1, self._int64),
                          shape[1], k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2], kind)
         if rc:
@@ -685,6 +687,10 @@ class KvCache:
         elif (tuple(lse.shape) != (n, heads) or lse.dtype is not self._float32 or lse.device != self.device
               or not lse.is_contiguous()):
             raise ValueError("lse must be contiguous float32 [n, query heads]")
+        if not 0 <= layer < self.layers:
+            layer = -1  # (refused by the call, whose numbers are of 32 bits, as is a negative window)
+        if not 0 <= window < 1 << 31:
+            window = -1 if window < 0 else (1 << 31) - 1
         rc = self._attend(self._h, layer, n, None if seq is None else self._list(seq, n, self._int32), q.data_ptr(), row, head, kind,
                           heads, dim ** -0.5 if scale is None else scale, window, out.data_ptr(), out_row, out_head, lse.data_ptr())
         if rc:
