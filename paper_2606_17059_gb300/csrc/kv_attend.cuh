@@ -510,8 +510,9 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
     for (int b = 0; b < NB; ++b) {
       float mine = unit;
       if (KIND == P2P_KV_E4M3) {
-        // The queries in f16, scaled by a power of two so that a row's largest is in [1, 2): exact but for what is
-        // below 2^-14 of it.
+        // The queries in f16, scaled by a power of two so that a row's largest is in [2^14, 2^15): exact but for what
+        // is below 2^-28 of it.  (In [1, 2) it would be 2^-14, and the upper half of f16's range of no use; sums of 256
+        // products with up to 448 are far from the end of 32 bits either way.)
         float largest = 0.f;
 #pragma unroll
         for (int k = 0; k < KSTEPS; ++k)
@@ -522,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
           }
         largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 1));
         largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 2));
-        const int e = largest > 0.f && largest < INFINITY ? max(ilogbf(largest), -126) : 0;
+        const int e = largest > 0.f && largest < INFINITY ? max(ilogbf(largest), -112) - 14 : 0;
         const float down = ldexpf(1.f, -e);
         mine = ldexpf(unit, e);
 #pragma unroll

@@ -47,3 +47,22 @@ def test_a_token_far_ahead_whose_values_are_zero(kind, hq, hkv, dim, order, ahea
         off = off + torch.tensor(lengths, device="cuda")[:, None, None] * 2.0 ** -37 * 2 * v
     assert far(out, want, off) <= 1
     assert far(lse, want_lse, off_lse) <= 1
+
+
+@pytest.mark.parametrize("dtype,outlier,rest", [("bfloat16", 2.0 ** 20, 3.0), ("bfloat16", 2.0 ** -90, 2.0 ** -108),
+                                                ("bfloat16", 2.0 ** 127, 2.0 ** 108), ("float16", 60000.0, 0.1)])
+def test_one_large_value_in_a_query_beside_8_bit_keys(dtype, outlier, rest):
+    """A query's value that is 2^18 times the others, where all keys are 0: the logits are the others'."""
+    dim = 128
+    c = make([1, 40, 3000], 2, dim, 16, "e4m3")
+    c.k[..., 5].copy_(torch.zeros(c.k.shape[:4], device="cuda").to(c.k.dtype))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q = (torch.randn((3, 8, dim), device="cuda", generator=gen) * rest).to(getattr(torch, dtype))
+    q[..., 5] = outlier
+    scale = 0.3 / rest
+    out, lse = c.attend(0, q, scale)
+    c.sync()
+    want, want_lse, spread, reach = km.attend(c, 0, q, scale)
+    off, off_lse = km.bounds(spread, reach, dim, "e4m3", "f16" if dtype == "float16" else "bf16")
+    assert far(out, want, off) <= 1
+    assert far(lse, want_lse, off_lse) <= 1
