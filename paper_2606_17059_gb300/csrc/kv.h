@@ -117,6 +117,37 @@ struct KvQuery {
   // Whether rows of q may be read by twos, and those of out written by fours, of their values.
   bool q_pairs, out_fours;
 };
+// The attention's kernel for values of a type, head_dim and `group` query heads a kv head: head_dim as it is padded,
+// blocks of eight query heads taken together, and CTAs resident on an SM.
+constexpr int attend_value_size(int type) { return type == P2P_KV_E4M3 ? 1 : 2; }
+constexpr int attend_dim(int type, int dim) {
+  // (80 values of 8 bits are five 16-byte pieces, not whole turns of a warp)
+  return dim <= 64    ? 64
+         : dim <= 80 && type != P2P_KV_E4M3 ? 80
+         : dim <= 96  ? 96
+         : dim <= 128 ? 128
+         : dim <= 192 ? 192
+                      : 256;
+}
+constexpr int attend_blocks(int type, int dp, int group) {
+  return group <= 8 ? 1 : group <= 16 || dp > 128 || type == P2P_KV_E4M3 ? 2 : 4;
+}
+// Tokens that a warp takes at a time (see Shape in kv_attend.cuh).
+constexpr int attend_rows(int type, int dp) { return type == P2P_KV_E4M3 && dp <= 128 ? 32 : 16; }
+// Three where three have room for more than two tiles a warp and registers enough (168 a thread), one where two have
+// not.
+constexpr int attend_ctas(int type, int dp, int blocks) {
+  const int row = dp * attend_value_size(type);
+  return attend_rows(type, dp) * row <= 3 * 1024 && dp * blocks <= 256 ? 3 : row <= 256 ? 2 : 1;
+}
+
+// Rows (of a sequence and kv head) a CTA, of two an SM at least, from which the attention's kernel that may take heads
+// together is used where they do not share lines: only the device knows how long they are.  Below, it is mostly the
+// slower one: 512 sequences of 1 to 800 tokens with 4 heads of 256 16-bit values 84 us, not 66 (of 1 to 40 40, not
+// 45), 608 of 1 to 300 with 4 of 64 22.4, not 20.9.  Above, short rows gain up to 2x (see kSideShort), those of some
+// hundred tokens lose up to 18% (608 of 1 to 800 with 4 of 256 90, not 77; 2,000 of them 236, not 225) and long ones
+// 1% (512 of 1,000 to 4,000 with 8 of 128 657, not 653).
+constexpr int kSideRows = 7;
 // Parts of rows that several CTAs share, four a CTA (see the kernel), and how many have arrived (zero between
 // launches).
 struct KvAttendScratch {

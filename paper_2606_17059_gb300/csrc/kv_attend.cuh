@@ -59,9 +59,11 @@ constexpr int kJoin = 16;               // parts of a unit row that are read tog
 // heads of 192 8-bit values 50 us, not 24; 21 of 20,000 tokens with 4 of 96 16-bit values 86 and 74 (29 parts); 40 of
 // 1,000 with 24 of 80 60, not 86.  Elsewhere, with so many units a row's head on average at most (kOver of them for
 // starting it), as there are fewer unit rows to start and finish: 2,000 sequences of 1 to 200 tokens (half below 15)
-// with 8 heads of 128 16-bit values take 78 us, not 129, of 8-bit values 103, not 179; 512 of 1 to 800 (5.6 units)
-// with 24 heads of 80 16-bit values 80, not 104, though with 4 of 256 83, not 66.  Beyond, joins cost as much or more:
-// 512 of 1 to 1,600 with 8 heads of 64 50 us and 48, with 4 of 256 115 and 92 (and 87 in the kernel without SIDE).
+// with 8 heads of 128 and 4 query heads to each take 78 us, with one head at a time 137, and 122 in the kernel without
+// SIDE; in 8 bits 81, 168 and 158.  More query heads gain less, as parts grow with them: 1,000 of 1 to 500 (5 units)
+// with 4 heads of 128 and 4, 8 or 16 query heads to each 41, 50 and 75, not 50, 56 and 80 (without SIDE 46, 50 and
+// 71); 512 of 1 to 800 (5.6 units) with 8 of 256 and 4 or 8 96 and 140, not 120 and 136 (112 and 119).  Beyond, the
+// parts cost as much or more: 512 of 1 to 1,200 with 8 of 256 and 8 171, not 153 (138).
 constexpr int kSideUnits = 32, kSideParts = 16, kSideShort = 6;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -71,38 +73,33 @@ template <int KIND>
 struct Type;
 template <>
 struct Type<P2P_KV_BF16> {
-  static constexpr int kSize = 2;
   static constexpr float kUp = 0.f, kLag = 8.f;
 };
 template <>
 struct Type<P2P_KV_F16> {
-  static constexpr int kSize = 2;
   static constexpr float kUp = 12.f, kLag = 3.f;
 };
 template <>
 struct Type<P2P_KV_E4M3> {
-  static constexpr int kSize = 1;
   static constexpr float kUp = 12.f, kLag = 3.f;
 };
 
 // Sizes of the kernel for values of KIND, head_dim padded to DP, NB blocks of eight query heads.
 template <int KIND, int DP, int NB>
 struct Shape {
-  static constexpr int kRowBytes = DP * Type<KIND>::kSize;
+  static constexpr int kRowBytes = DP * attend_value_size(KIND);
   static constexpr int kPieces = kRowBytes / 16;               // 16-byte pieces of a row
   static_assert(kPieces % 2 == 0, "a tile's pieces are whole turns of the warp");
   // Tokens that a warp takes at a time: 32 of small 8-bit rows, where a turn of the loop costs much beside the bytes
   // it takes (256 sequences of 8-bit values of 64: 83 us with 16, 65 with 32).  Of 16-bit values of 64, 131,071
   // tokens take 49.3 and 47.9 us, but 512 sequences of 10 to 300 tokens 13.6 and 14.8: there smaller tiles fit rows
   // better.
-  static constexpr int kRows = KIND == P2P_KV_E4M3 && kRowBytes <= 128 ? 32 : 16;
+  static constexpr int kRows = attend_rows(KIND, DP);
   static constexpr int kTileLog = kRows == 32 ? 7 : 6;         // (log2) that a CTA takes at a time, of one head
   static_assert(kWarps * kRows == 1 << kTileLog);
   static constexpr int kArray = kRows * kRowBytes;             // keys (or values) of a warp's tile
   static constexpr int kStage = 2 * kArray;
-  // Resident on an SM: three where three have room for more than two tiles a warp and registers enough (168 a
-  // thread), one where two have not.
-  static constexpr int kCtas = kRows * kRowBytes <= 3 * 1024 && DP * NB <= 256 ? 3 : kRowBytes <= 256 ? 2 : 1;
+  static constexpr int kCtas = attend_ctas(KIND, DP, NB);
   static constexpr int kSumPitch = (DP + 31) / 32 * 32;        // of a head's sums, which lie in the room of a tile
   static_assert(8 * kSumPitch * 4 <= kStage);
   static constexpr int kFit = (232448 / kCtas - 1024 - 512) / kWarps / kStage;
@@ -910,26 +907,25 @@ cudaError_t launch_pages(const KvView& c, const KvQuery* q, const KvAttendScratc
 // 8-bit values, do not fit the registers (256 heads on 8 over the 8-bit case 286 us, and 234 with blocks of 16).
 template <int KIND, int DP, bool SIDE>
 cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  constexpr bool kWide = DP <= 128 && KIND != P2P_KV_E4M3;  // blocks of 32
-  const int32_t group = q ? q->heads / c.heads : 0;
+  const int blocks = q ? attend_blocks(KIND, DP, q->heads / c.heads) : 0;
   cudaError_t e = cudaSuccess;
-  if (!q || group <= 8) e = launch_pages<KIND, DP, 1, SIDE>(c, q, w, num_sms, st);
-  if (e == cudaSuccess && (!q || (group > 8 && (group <= 16 || !kWide))))
-    e = launch_pages<KIND, DP, 2, SIDE>(c, q, w, num_sms, st);
-  if constexpr (kWide)
-    if (e == cudaSuccess && (!q || group > 16)) e = launch_pages<KIND, DP, 4, SIDE>(c, q, w, num_sms, st);
+  if (!q || blocks == 1) e = launch_pages<KIND, DP, 1, SIDE>(c, q, w, num_sms, st);
+  if (e == cudaSuccess && (!q || blocks == 2)) e = launch_pages<KIND, DP, 2, SIDE>(c, q, w, num_sms, st);
+  if constexpr (attend_blocks(KIND, DP, 32) == 4)
+    if (e == cudaSuccess && (!q || blocks == 4)) e = launch_pages<KIND, DP, 4, SIDE>(c, q, w, num_sms, st);
   return e;
 }
 
 template <int KIND, bool SIDE>
 cudaError_t launch_dim(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  constexpr int k80 = KIND == P2P_KV_E4M3 ? 96 : 80;  // (80 values of 8 bits are five pieces, not whole turns)
-  return c.dim <= 64    ? launch_heads<KIND, 64, SIDE>(c, q, w, num_sms, st)
-         : c.dim <= k80 ? launch_heads<KIND, k80, SIDE>(c, q, w, num_sms, st)
-         : c.dim <= 96  ? launch_heads<KIND, 96, SIDE>(c, q, w, num_sms, st)
-         : c.dim <= 128 ? launch_heads<KIND, 128, SIDE>(c, q, w, num_sms, st)
-         : c.dim <= 192 ? launch_heads<KIND, 192, SIDE>(c, q, w, num_sms, st)
-                        : launch_heads<KIND, 256, SIDE>(c, q, w, num_sms, st);
+  switch (attend_dim(KIND, c.dim)) {
+    case 64: return launch_heads<KIND, 64, SIDE>(c, q, w, num_sms, st);
+    case 80: return launch_heads<KIND, attend_dim(KIND, 80), SIDE>(c, q, w, num_sms, st);
+    case 96: return launch_heads<KIND, 96, SIDE>(c, q, w, num_sms, st);
+    case 128: return launch_heads<KIND, 128, SIDE>(c, q, w, num_sms, st);
+    case 192: return launch_heads<KIND, 192, SIDE>(c, q, w, num_sms, st);
+    default: return launch_heads<KIND, 256, SIDE>(c, q, w, num_sms, st);
+  }
 }
 
 }  // namespace

@@ -129,8 +129,11 @@ cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p
     const cudaError_t e = alone(c, q, w, num_sms, st);
     return e != cudaSuccess || c.side == 0 ? e : side_by_side(c, q, w, num_sms, st);
   }
-  // Without shared lines it is many short rows that gain, see kSideShort: with fewer the kernel would find too little.
-  const bool many = (int64_t)q->n * c.heads >= (int64_t)4 * KvAttendScratch::kCtasPerSm * num_sms;
+  // Without shared lines it is many short rows that gain (see kSideShort): with fewer the kernel finds too little to take
+  // heads together, and is then the slower of the two.
+  const int dp = attend_dim(c.type, c.dim), group = q->heads / c.heads;
+  const int ctas = attend_ctas(c.type, dp, attend_blocks(c.type, dp, group));
+  const bool many = (int64_t)q->n * c.heads >= (int64_t)kSideRows * std::max(2, ctas) * num_sms;
   return (c.side != 0 && (c.lines || many) ? side_by_side : alone)(c, q, w, num_sms, st);
 }
 
