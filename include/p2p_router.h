@@ -393,7 +393,7 @@ typedef struct p2p_kv_layout {
   int32_t *refs;        /* int32[n_pages] */
 } p2p_kv_layout;
 
-/* A handle on the cache `layout` describes, on the current CUDA device; its scratch (15 to 121 MB by head_dim and
+/* A handle on the cache `layout` describes, on the current CUDA device; its scratch (7 to 81 MB by type, head_dim and
  * heads, and up to 20 bytes a page and 32 a sequence) is allocated here.  The arrays stay the caller's and must outlive
  * the handle. Errors: P2P_E_INVAL (message of p2p_kv_last_error(NULL)), P2P_E_NOMEM, P2P_E_CUDA. */
 int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out);

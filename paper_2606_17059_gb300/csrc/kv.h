@@ -156,12 +156,16 @@ struct KvAttendScratch {
   int32_t* arrived;  // [4 * kCtasPerSm * SMs]
   int32_t* err;
 };
-// Floats of `parts`: head_dim as the kernels pad it, at most, and blocks of up to 16 or 32 query heads of up to 4 kv
-// heads.
+// Floats of `parts`: for the blocks of query heads that take most, each part with the sums, maximum and sum of exp of up
+// to 4 kv heads.
 inline size_t kv_attend_parts(const KvView& c, int num_sms) {
-  const int32_t dp = c.dim <= 64 ? 64 : c.dim <= 96 ? 96 : c.dim <= 128 ? 128 : c.dim <= 192 ? 192 : 256,
-      heads = dp > 128 ? 16 : 32;
-  return (size_t)4 * KvAttendScratch::kCtasPerSm * num_sms * (heads << c.side) * (dp + 2);
+  const int dp = attend_dim(c.type, c.dim);
+  size_t most = 0;
+  for (const int group : {8, 16, 32}) {
+    const int blocks = attend_blocks(c.type, dp, group);
+    most = std::max(most, (size_t)4 * attend_ctas(c.type, dp, blocks) * num_sms * (8 * blocks << c.side) * (dp + 2));
+  }
+  return most;
 }
 // With q = NULL they launch nothing, but make the cache's kernels ready for launches (at creation).
 cudaError_t launch_kv_attend_bf16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,

@@ -1,10 +1,17 @@
-"""The paged cache's calls on streams: which one the results belong to, a change of it, handles made after others, and that calls allocate nothing."""
+"""The paged cache's calls on streams: which one the results belong to, a change of it, handles made after others, and what
+handles and calls allocate."""
+import os
+import subprocess
+import sys
+
 import pytest
 
 import paper_2606_17059_gb300 as g
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 if torch.cuda.is_available():
     from test_gpu_kv_attend import check, make, query
@@ -111,3 +118,20 @@ def test_calls_allocate_nothing():
     torch.cuda.synchronize()
     assert torch.cuda.mem_get_info()[0] == free
     assert torch.cuda.memory_stats()["allocation.all.allocated"] == held
+
+
+def test_scratch_is_what_the_kernels_need():
+    """Of a handle's scratch the kernels for one size of rows use all; in a process of its own, as scratch is kept."""
+    code = """
+import torch, paper_2606_17059_gb300 as g
+first = g.KvCache.empty(1, 4, 16, 1, 16, 1, 1)     # (the library's kernels and its pool are there)
+torch.cuda.synchronize()
+made, free = [], torch.cuda.mem_get_info()[0]
+for _ in range(8):
+    made.append(g.KvCache.empty(1, 4, 16, 4, 256, 1, 1))
+torch.cuda.synchronize()
+print((free - torch.cuda.mem_get_info()[0]) / 8e6)
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT)
+    assert r.returncode == 0, r.stderr
+    assert float(r.stdout) < 46, r.stdout      # 40.2 MB of parts; the driver gives memory in blocks
