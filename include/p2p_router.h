@@ -458,8 +458,11 @@ int p2p_kv_compact(p2p_kv* kv);
  *   out[i * out_row_stride + h * out_head_stride + x] = sum_t p_t v_t[x],   p = softmax over t of scale * (q . k_t),
  *   lse[i * n_heads + h] (float, nullable) = ln sum_t exp(scale * (q . k_t)),
  * q[i * q_row_stride + h * q_head_stride + x] of `type` like out: the cache's, for P2P_KV_E4M3 P2P_KV_BF16 or
- * P2P_KV_F16.  No two rows of out may share values.  Sums are held in 32 bits.  A sequence without tokens gives 0 and -infinity.  Device-side errors: a
- * sequence or a page out of range. */
+ * P2P_KV_F16.  No two rows of out may share values.  Logits, maxima and sums are held in 32 bits.  Each p_t is rounded
+ * to the cache's type before its product with v_t (to f16 with P2P_KV_E4M3; of f16, what is 2^-26 of the largest or
+ * less has fewer bits, and what is less than 2^-37 of it is lost), and q, with P2P_KV_E4M3, to f16 after scaling by a
+ * power of two (what is 2^-28 of a row's largest value or less has fewer bits).  A sequence without tokens gives 0 and
+ * -infinity.  Device-side errors: a sequence or a page out of range. */
 int p2p_kv_attend(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, const void* q, int64_t q_row_stride,
                   int64_t q_head_stride, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
                   int64_t out_row_stride, int64_t out_head_stride, float* lse);

@@ -105,7 +105,7 @@ cudaError_t launch_kv_write(const KvView& c, const KvScratch& s, int32_t layer, 
 // out (zeroed by the launch): pages in use, pages shared, the highest page in use + 1, tokens held.
 cudaError_t launch_kv_stats(const KvView& c, unsigned long long* out, int num_sms, cudaStream_t st);
 
-// One token of each of n sequences (kv_attend.cu).
+// One token of each of n sequences (kv_attend.cuh).
 struct KvQuery {
   const void* q;
   void* out;
@@ -156,8 +156,8 @@ struct KvAttendScratch {
   int32_t* arrived;  // [4 * kCtasPerSm * SMs]
   int32_t* err;
 };
-// Floats of `parts`: for the blocks of query heads that take most, each part with the sums, maximum and sum of exp of up
-// to 4 kv heads.
+// Floats of `parts`: for the blocks of query heads that take most, each part with the sums, maximum and sum of exp of
+// up to 4 kv heads.
 inline size_t kv_attend_parts(const KvView& c, int num_sms) {
   const int dp = attend_dim(c.type, c.dim);
   size_t most = 0;

@@ -5,18 +5,18 @@
 //
 // Keys and values are read once, and that is what bounds it: with g query heads a kv head, 4 g dim operations go with
 // 4 dim bytes, g a byte (2 g with 8 bits), where the GPU has 277 operations of its tensor cores for a byte of memory.
-// Measured (one GB300, copy bandwidth 6.8 TB/s): 32 sequences of 4,352 to 33,792 tokens, 40 / 8 heads of 128 f16
-// values, 1.88 GB in 277 us (the copy bandwidth); one sequence of 131,071 tokens, 32 / 8 heads, 0.54 GB in 85 us
-// (93%); 256 sequences of 128 to 4,224 tokens in 8 bits, 64 / 8 heads, 0.61 GB in 105 us (87%: there the widening of
-// the values and the ends of the rows weigh); one of 540 tokens 7.0 us, a chain of a launch, four loads, a tile and
+// Measured on one GB300 (device time in a graph; copy bandwidth 6.8 TB/s): 32 sequences of 4,352 to 33,792 tokens, 40
+// / 8 heads of 128 f16 values, 1.88 GB in 282 us (98%); one sequence of 131,071 tokens, 32 / 8 heads, 0.54 GB in 86 us
+// (92%); 256 sequences of 128 to 4,224 tokens in 8 bits, 64 / 8 heads, 0.62 GB in 104 us (88%: there the widening of
+// the values and the ends of the rows weigh); one of 540 tokens 7.6 us, a chain of a launch, four loads, a tile and
 // the join.
 //
-// The work is cut into units of 64 or 128 tokens of a (sequence, kv head, block of its query heads), numbered in that
-// order, and every CTA takes an equal, contiguous range of them: one long sequence fills the GPU as a batch does.  A
-// range's parts of a unit row that it shares with other CTAs go to scratch (maximum, sum, unnormalised out), and the
-// CTA that finishes such a row last joins its parts, in their order: results do not depend on timing.  (The start of
-// a unit row counts as kOver units more, for what its end costs: with 1 instead of 3, the 256 sequences in 8 bits
-// take 115 us.)
+// The work is cut into units of 64 or 128 tokens (2^kTileLog) of a (sequence, kv head, block of its query heads), or,
+// where that pays (SIDE), of 2^side times fewer tokens of 2^side neighbouring kv heads, numbered in that order, and
+// every CTA takes an equal, contiguous range of them: one long sequence fills the GPU as a batch does.  A range's
+// parts of a unit row that it shares with other CTAs go to scratch (maximum, sum, unnormalised out), and the CTA that
+// finishes such a row last joins its parts, in their order: results do not depend on timing.  (The start of a unit row
+// counts as kOver units more, for what its end costs: with 1 instead of 3, the 256 sequences in 8 bits take 115 us.)
 //
 // Each warp streams 16 or 32 tokens at a time through shared memory of its own, up to seven tiles ahead (cp.async, 16
 // bytes a lane, 16-byte pieces turned so that ldmatrix meets no bank twice), with no barrier between warps inside a
@@ -25,14 +25,14 @@
 // looked up two tiles ahead.  Sixteen tokens are multiplied transposed: S^T [tokens, heads] = K Q^T and O^T [dim,
 // heads] += V^T P^T, so that eight query heads fill a product's n and the tokens (or values) its m of 16.  P^T goes
 // from the first product's layout to the second's by two 8 x 8 transposes of registers.  exp(x - m) takes for m not
-// the running maximum but one that lags it by at most a factor of 2^8 (2^3 for f16 and 8 bits), so that a tile's maximum
-// is only reduced, and O rescaled, where it goes past that.  P is rounded to the values' type (f16 for 8 bits) for its
-// product; sums, maxima and O are held in 32 bits.  Of f16, whose range is small, P takes the upper end (kUp): what is
-// 2^26 times smaller than a warp's largest keeps all 11 bits, what is 2^37 times smaller is lost, 2^-37 of the largest
-// a token at most.  (P <= 1 loses bits from 2^-14 on and everything below 2^-25, and then, where one token that is far
-// ahead has values near zero, what the result consists of.)
+// the running maximum but one that lags it by at most a factor of 2^8 (2^3 for f16 and 8 bits), so that a tile's
+// maximum is only reduced, and O rescaled, where it goes past that.  P is rounded to the values' type (f16 for 8 bits)
+// for its product; sums, maxima and O are held in 32 bits.  Of f16, whose range is small, P takes the upper end (kUp):
+// what is 2^26 times smaller than a warp's largest keeps all 11 bits, what is 2^37 times smaller is lost, 2^-37 of the
+// largest a token at most.  (P <= 1 loses bits from 2^-14 on and everything below 2^-25, and then, where one token
+// that is far ahead has values near zero, what the result consists of.)
 //
-// The products are warp-wide ones (mma): 9% of the tensor cores' time at the copy bandwidth (8 bits: 17%), and their
+// The products are warp-wide ones (mma): 9% of the tensor cores' time at the copy bandwidth (8 bits: 18%), and their
 // operands come out of shared memory by ldmatrix in any row size.  The tensor memory path (tcgen05) would free issue
 // slots that 16-bit values do not need and that 8-bit values, which have to be widened beside 16-bit queries, could
 // not use it for.
@@ -67,8 +67,8 @@ constexpr int kJoin = 16;               // parts of a unit row that are read tog
 constexpr int kSideUnits = 32, kSideParts = 16, kSideShort = 6;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// kUp: exp(x - m) is taken times 2^kUp (m is held less kUp, in log2).  kLag: how far (log2) a logit may pass the maximum
-// in use.  P is at most 2^(kUp + kLag), which f16 has to hold.
+// kUp: exp(x - m) is taken times 2^kUp (m is held less kUp, in log2).  kLag: how far (log2) a logit may pass the
+// maximum in use.  P is at most 2^(kUp + kLag), which f16 has to hold.
 template <int KIND>
 struct Type;
 template <>

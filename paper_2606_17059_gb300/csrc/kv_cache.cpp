@@ -102,8 +102,8 @@ const char* check_layout(const p2p_kv_layout& a) {
 // 16-bit values 240 us with pages of 16 tokens either way, 304 and 280 with pages of one.)
 bool shares_lines(const p2p::KvView& c) { return c.head_stride <= c.token_stride && c.row16 % 16 != 0; }
 
-// Whether two of the rows that a result is written to, `dim` values each at i * row + h * head (i < n, h < heads), share
-// a value.
+// Whether two of the rows that a result is written to, `dim` values each at i * row + h * head (i < n, h < heads),
+// share a value.
 bool rows_overlap(int64_t n, int64_t heads, int64_t dim, int64_t row, int64_t head) {
   using wide = __int128;
   const wide r = row < 0 ? -(wide)row : row, g = head < 0 ? -(wide)head : head;
@@ -129,8 +129,8 @@ cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p
     const cudaError_t e = alone(c, q, w, num_sms, st);
     return e != cudaSuccess || c.side == 0 ? e : side_by_side(c, q, w, num_sms, st);
   }
-  // Without shared lines it is many short rows that gain (see kSideShort): with fewer the kernel finds too little to take
-  // heads together, and is then the slower of the two.
+  // Without shared lines it is many short rows that gain (see kSideShort): with fewer the kernel finds too little to
+  // take heads together, and is then the slower of the two.
   const int dp = attend_dim(c.type, c.dim), group = q->heads / c.heads;
   const int ctas = attend_ctas(c.type, dp, attend_blocks(c.type, dp, group));
   const bool many = (int64_t)q->n * c.heads >= (int64_t)kSideRows * std::max(2, ctas) * num_sms;
