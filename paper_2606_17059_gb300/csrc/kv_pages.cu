@@ -557,7 +557,7 @@ __device__ __forceinline__ int32_t find_item(const int64_t* offsets, int32_t n, 
 // a factor 2^-20 above the reciprocal (where the scale is above that ratio: below) rounds as the quotient does.  A
 // scale of up to 12 bits can be such a ratio exactly, and is 2^-17 away from all others: there 32 bits of the quotient
 // are enough, but for ties they have to be right, and the factor has two parts.  (By division and remainder for each
-// value, the 61 prompts below take 597 us, not 534; rounded twice, 574.)
+// value, the 61 prompts above take 597 us, not 534; rounded twice, 574.)
 __device__ __forceinline__ bool ordinary(float scale) {
   return fabsf(scale) > 0x1p-60f && fabsf(scale) < 0x1p60f;
 }
