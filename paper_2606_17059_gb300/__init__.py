@@ -16,7 +16,7 @@ import numpy as np
 from . import build as _build
 
 __all__ = [
-    "P2PError", "Router", "KvCache", "build", "library_path",
+    "P2PError", "Router", "KvCache", "Rope", "build", "library_path",
     "p2p_router_create", "p2p_router_destroy", "p2p_router_set_stream", "p2p_router_sync", "p2p_last_error",
     "p2p_router_num_trees", "p2p_router_launch_count", "p2p_snapshot_build", "p2p_snapshot_view", "p2p_snapshot_free",
     "p2p_flat_tree_validate", "p2p_tree_upload", "p2p_tree_build", "p2p_tree_download", "p2p_tree_apply_delta",
@@ -25,6 +25,7 @@ __all__ = [
     "p2p_lru_enable", "p2p_lru_insert", "p2p_lru_access", "p2p_lru_evict", "p2p_hit_rate", "p2p_route_prepare",
     "p2p_kv_create", "p2p_kv_destroy", "p2p_kv_set_stream", "p2p_kv_sync", "p2p_kv_last_error", "p2p_kv_launch_count",
     "p2p_kv_stats", "p2p_kv_extend", "p2p_kv_write", "p2p_kv_fork", "p2p_kv_trim", "p2p_kv_compact", "p2p_kv_attend",
+    "p2p_kv_rotation_turns", "p2p_kv_write_rotated", "p2p_kv_attend_prompt", "p2p_kv_attend_shared", "p2p_kv_attend_shared_work",
 ]
 
 P2P_OK, P2P_E_INVAL, P2P_E_NOMEM, P2P_E_FORMAT, P2P_E_CUDA, P2P_E_DEVICE = 0, -1, -2, -3, -4, -5
@@ -69,6 +70,11 @@ class KvLayout(ctypes.Structure):
     _fields_ = ([(f, _i32) for f in ("type", "n_layers", "n_pages", "page_tokens", "n_heads", "head_dim", "n_seqs", "max_pages")]
                 + [(f, _i64) for f in ("layer_stride", "page_stride", "token_stride", "head_stride")]
                 + [(f, _vp) for f in ("k", "v", "k_scale", "v_scale", "table", "length", "refs")])
+
+
+class KvRotation(ctypes.Structure):
+    _fields_ = [("dim", _i32), ("interleaved", _i32), ("amplitude", ctypes.c_float), ("eps", ctypes.c_float), ("turns", _vp),
+                ("q_weight", _vp), ("k_weight", _vp)]
 
 
 _lib = None
@@ -127,6 +133,14 @@ def _load():
             "p2p_kv_compact": (ctypes.c_int, [_vp]),
             "p2p_kv_attend": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _i64, _i64, _i32, _i32, ctypes.c_float, _i32, _vp, _i64,
                                              _i64, _vp]),
+            "p2p_kv_rotation_turns": (ctypes.c_int, [_i32, _vp, _vp]),
+            "p2p_kv_write_rotated": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _i64, P(KvRotation), _vp, _i64, _i64, _i32, _vp, _vp,
+                                                    _i64, _i64, _i32, _vp, _i64, _i64]),
+            "p2p_kv_attend_prompt": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _i64, _i32, _i32, ctypes.c_float, _i32,
+                                                    _vp, _i64, _i64, _vp]),
+            "p2p_kv_attend_shared": (ctypes.c_int, [_vp, _i32, _i32, _vp, _i32, _vp, _vp, _i64, _i64, _i32, _i32, ctypes.c_float, _i32,
+                                                    _vp, _i64, _i64, _vp, _vp]),
+            "p2p_kv_attend_shared_work": (_i64, [_vp, _i32, _i32]),
             "p2p_router_kernel_time": (ctypes.c_int, [_vp, _i32, P(ctypes.c_char_p), P(_i64), P(ctypes.c_double)]),
         }
         for name, (res, args) in sig.items():
@@ -523,7 +537,105 @@ def p2p_kv_attend(kv, layer: int, n: int, seq, q, q_row_stride: int, q_head_stri
                                     out_row_stride, out_head_stride, _addr(lse)), kv)
 
 
+def p2p_kv_rotation_turns(radians) -> np.ndarray:
+    """uint64 turns a position (times 2^64) from radians a position (host arrays)."""
+    r = np.ascontiguousarray(radians, dtype=np.float64)
+    out = np.empty(r.shape, np.uint64)
+    _kv_check(_load().p2p_kv_rotation_turns(r.size, r.ctypes.data, out.ctypes.data))
+    return out
+
+
+def p2p_kv_write_rotated(kv, layer: int, n: int, seq, offsets, n_tokens: int, rotation: KvRotation, q, q_token_stride: int,
+                         q_head_stride: int, n_heads: int, k, v, token_stride: int, head_stride: int, dtype: int, out,
+                         out_token_stride: int, out_head_stride: int) -> None:
+    """Norms, rotary positions and the write in one pass; q, k, v and out are addresses (their strides are arguments)."""
+    _kv_check(_load().p2p_kv_write_rotated(kv, layer, n, _addr(seq), _addr(offsets), n_tokens, ctypes.byref(rotation), q, q_token_stride,
+                                           q_head_stride, n_heads, k, v, token_stride, head_stride, dtype, out, out_token_stride,
+                                           out_head_stride), kv)
+
+
+def p2p_kv_attend_prompt(kv, layer: int, n: int, seq, offsets, n_tokens: int, q, q_token_stride: int, q_head_stride: int, dtype: int,
+                         n_heads: int, scale: float, window: int, out, out_token_stride: int, out_head_stride: int, lse=None) -> None:
+    """The last tokens of each sequence; q and out are addresses (their strides are arguments)."""
+    _kv_check(_load().p2p_kv_attend_prompt(kv, layer, n, _addr(seq), _addr(offsets), n_tokens, q, q_token_stride, q_head_stride, dtype,
+                                           n_heads, scale, window, out, out_token_stride, out_head_stride, _addr(lse)), kv)
+
+
+def p2p_kv_attend_shared_work(kv, n: int, n_heads: int) -> int:
+    return int(_load().p2p_kv_attend_shared_work(kv, n, n_heads))
+
+
+def p2p_kv_attend_shared(kv, layer: int, n: int, seq, n_groups: int, groups, q, q_row_stride: int, q_head_stride: int, dtype: int,
+                         n_heads: int, scale: float, window: int, out, out_row_stride: int, out_head_stride: int, lse, work) -> None:
+    """One new token of each row, groups of rows that share a prefix; q and out are addresses (their strides are arguments)."""
+    _kv_check(_load().p2p_kv_attend_shared(kv, layer, n, _addr(seq), n_groups, _addr(groups), q, q_row_stride, q_head_stride, dtype,
+                                           n_heads, scale, window, out, out_row_stride, out_head_stride, _addr(lse), _addr(work)), kv)
+
+
 # ---- convenience wrappers ---------------------------------------------------------------------------------
+
+class Rope:
+    """Rotary positions for KvCache.write_rotated: the first `dim` values of a head turn in dim / 2 pairs, pair j by
+    theta ** (-2 j / dim) radians a position.
+
+    interleaved   pair j is values 2j and 2j + 1 of a head, else j and j + dim / 2
+    scaling       None, or how positions are stretched to `factor` times those of training:
+                  "linear"    all pairs turn `factor` times slower
+                  "ntk"       theta grows by factor ** (dim / (dim - 2)), so that the last pair turns `factor` times slower
+                  "by_parts"  pairs that turn `high` times or more in the `original` length stay, those that turn `low` times or
+                              less are `factor` times slower, and in between the two are mixed linearly in the turns
+                              (low 1 and high 4 unless given)
+                  "yarn"      as "by_parts", but mixed linearly in the pair's number, from where it turns `high` times, rounded
+                              down, to where it turns `low` times, rounded up (1 and 32 unless given), and cosines and sines
+                              times 0.1 ln(factor) + 1 (Peng et al., YaRN, 2023)
+    amplitude     what cosines and sines are multiplied by, instead of the above
+    radians       a position, of each pair, instead of all of it"""
+
+    def __init__(self, dim: int, theta: float = 10000.0, interleaved: bool = False, scaling=None, factor: float = 1.0, original: int = 0,
+                 low=None, high=None, amplitude=None, radians=None, device="cuda"):
+        import torch
+        if dim < 0 or dim % 2:
+            raise ValueError("dim must be even")
+        self.dim, self.interleaved = dim, bool(interleaved)
+        if radians is None:
+            radians = self._radians(dim, float(theta), scaling, float(factor), original, low, high)
+        elif scaling is not None:
+            raise ValueError("radians are given as they are: scaling does not go with them")
+        self.radians = np.ascontiguousarray(radians, dtype=np.float64)
+        if self.radians.shape != (dim // 2,):
+            raise ValueError("radians must be [dim / 2]")
+        if amplitude is None:
+            amplitude = 0.1 * np.log(factor) + 1 if scaling == "yarn" else 1.0
+        self.amplitude = float(amplitude)
+        self.turns = torch.from_numpy(p2p_kv_rotation_turns(self.radians).view(np.int64)).to(device)
+
+    @staticmethod
+    def _radians(dim, theta, scaling, factor, original, low, high):
+        if scaling not in (None, "linear", "ntk", "by_parts", "yarn"):
+            raise ValueError('scaling must be None, "linear", "ntk", "by_parts" or "yarn"')
+        if not theta > 1 or not factor >= 1:
+            raise ValueError("theta must be above 1, factor at least 1")
+        if scaling == "ntk":
+            if dim < 4:
+                raise ValueError('"ntk" needs two pairs at least')
+            theta *= factor ** (dim / (dim - 2))
+        j = np.arange(dim // 2, dtype=np.float64)
+        f = theta ** (-2 * j / max(dim, 1))
+        if scaling == "linear":
+            return f / factor
+        if scaling in ("by_parts", "yarn"):
+            low, high = 1.0 if low is None else float(low), (4.0 if scaling == "by_parts" else 32.0) if high is None else float(high)
+            if original < 1 or not 0 < low < high:
+                raise ValueError("original must be given, and 0 < low < high")
+            if scaling == "by_parts":
+                keep = np.clip((original * f / (2 * np.pi) - low) / (high - low), 0, 1)
+            else:
+                first, last = (dim * np.log(original / (turns * 2 * np.pi)) / (2 * np.log(theta)) for turns in (high, low))
+                first, last = max(np.floor(first), 0), min(np.ceil(last), dim - 1)
+                keep = 1 - np.clip((j - first) / max(last - first, 1e-3), 0, 1)
+            return f * keep + f / factor * (1 - keep)
+        return f
+
 
 class KvCache:
     """A paged key-value cache (p2p_kv) over the caller's CUDA tensors.
@@ -566,6 +678,9 @@ class KvCache:
         lib = _load()  # (the calls of a decode step go to the library's functions directly)
         self._extend, self._trim, self._fork, self._write, self._attend = (
             lib.p2p_kv_extend, lib.p2p_kv_trim, lib.p2p_kv_fork, lib.p2p_kv_write, lib.p2p_kv_attend)
+        self._write_rotated, self._attend_prompt, self._attend_shared, self._shared_work = (
+            lib.p2p_kv_write_rotated, lib.p2p_kv_attend_prompt, lib.p2p_kv_attend_shared, lib.p2p_kv_attend_shared_work)
+        self._uint8 = torch.uint8
         a = KvLayout(self._types[k.dtype], layers, pages, page, heads, dim, table.shape[0], table.shape[1], *k.stride()[:4],
                      k.data_ptr(), v.data_ptr(), _addr(k_scale), _addr(v_scale), table.data_ptr(), length.data_ptr(), refs.data_ptr())
         self.device, self._index = k.device, k.device.index
@@ -665,9 +780,82 @@ class KvCache:
         if rc:
             _kv_check(rc, self._h)
 
+    def write_rotated(self, layer: int, seq, offsets, q, k, v, rope: Rope, q_weight=None, k_weight=None, eps: float = 1e-6, out=None):
+        """``write`` of one layer with norms and rotary positions in the same pass: q [tokens, query heads, head dim], k and v
+        [tokens, heads, head dim]; q_weight and k_weight float32 [head dim] (None: no norm).  Returns the queries, normed and
+        rotated (in out, which may be q); those of tokens of no sequence are left as they were."""
+        n, kind, dim = seq.numel(), self._types.get(k.dtype), self.dim
+        if (q.dim() != 3 or k.dim() != 3 or kind is None or q.dtype is not k.dtype or v.dtype is not k.dtype or q.shape[0] != k.shape[0]
+                or q.shape[2] != dim or tuple(k.shape[1:]) != (self.heads, dim) or v.shape != k.shape or v.stride() != k.stride()
+                or dim > 1 and (q.stride(2) != 1 or k.stride(2) != 1)):
+            raise ValueError("q, k and v must be [tokens, heads, head dim] of one type, the last dimension contiguous, k and v strided alike")
+        if any(t is not None and t.device != self.device for t in (q, k, v, out, q_weight, k_weight, rope.turns)):
+            raise ValueError("tensors must be on the cache's device")
+        for w in (q_weight, k_weight):
+            if w is not None and (tuple(w.shape) != (dim,) or w.dtype is not self._float32 or not w.is_contiguous()):
+                raise ValueError("weights must be contiguous float32 [head dim]")
+        if out is None:
+            out = self._make(q.shape, q.dtype)
+        elif out.shape != q.shape or out.dtype is not q.dtype or dim > 1 and out.stride(2) != 1:
+            raise ValueError("out must be like q, the last dimension contiguous")
+        if not 0 <= layer < self.layers:
+            layer = -1  # (refused by the call, whose numbers are of 32 bits)
+        rotation = KvRotation(rope.dim, rope.interleaved, rope.amplitude, eps, rope.turns.data_ptr(),
+                              None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
+        rc = self._write_rotated(self._h, layer, n, self._list(seq, n, self._int32), self._list(offsets, n + 1, self._int64), q.shape[0],
+                                 ctypes.byref(rotation), q.data_ptr(), q.stride(0), q.stride(1), q.shape[1], k.data_ptr(), v.data_ptr(),
+                                 k.stride(0), k.stride(1), kind, out.data_ptr(), out.stride(0), out.stride(1))
+        if rc:
+            _kv_check(rc, self._h)
+        return out
+
     def attend(self, layer: int, q, scale=None, seq=None, window: int = 0, out=None, lse=None):
         """One new token of each sequence (of seq, int32, or sequences 0, 1, ...): q [n, query heads, head dim]; scale: head
         dim ** -0.5 unless given.  Returns (out like q, lse float32 [n, query heads])."""
+        (n, heads, dim), row, head, kind, out, out_row, out_head, lse, layer, scale, window = self._rows(layer, q, scale, window, out, lse)
+        rc = self._attend(self._h, layer, n, None if seq is None else self._list(seq, n, self._int32), q.data_ptr(), row, head, kind,
+                          heads, scale, window, out.data_ptr(), out_row, out_head, lse.data_ptr())
+        if rc:
+            _kv_check(rc, self._h)
+        return out, lse
+
+    def attend_prompt(self, layer: int, q, offsets, scale=None, seq=None, window: int = 0, out=None, lse=None):
+        """The last offsets[i+1] - offsets[i] tokens of sequence seq[i] (int32; or of sequences 0, 1, ...), each over the tokens up
+        to itself: q [tokens, query heads, head dim], offsets int64 [n + 1].  Returns (out like q, lse float32 [tokens, query
+        heads]); rows of no sequence are left as they were."""
+        (n, heads, dim), row, head, kind, out, out_row, out_head, lse, layer, scale, window = self._rows(layer, q, scale, window, out, lse)
+        items = offsets.numel() - 1
+        if items < 0:
+            raise ValueError("offsets must have an entry at least")
+        rc = self._attend_prompt(self._h, layer, items, None if seq is None else self._list(seq, items, self._int32),
+                                 self._list(offsets, items + 1, self._int64), n, q.data_ptr(), row, head, kind, heads, scale, window,
+                                 out.data_ptr(), out_row, out_head, lse.data_ptr())
+        if rc:
+            _kv_check(rc, self._h)
+        return out, lse
+
+    def attend_shared(self, layer: int, q, groups, scale=None, seq=None, window: int = 0, out=None, lse=None):
+        """As ``attend``, where rows groups[g] .. groups[g+1] - 1 (int32 [groups + 1]) begin with the same tokens in the same pages
+        (as ``fork`` leaves them): those are read once for all rows of a group."""
+        (n, heads, dim), row, head, kind, out, out_row, out_head, lse, layer, scale, window = self._rows(layer, q, scale, window, out, lse)
+        n_groups = groups.numel() - 1
+        if n_groups < 0:
+            raise ValueError("groups must have an entry at least")
+        work = self._make((max(16, self._shared_work(self._h, n, heads)),), self._uint8)
+        rc = self._attend_shared(self._h, layer, n, None if seq is None else self._list(seq, n, self._int32), n_groups,
+                                 self._list(groups, n_groups + 1, self._int32), q.data_ptr(), row, head, kind, heads, scale, window,
+                                 out.data_ptr(), out_row, out_head, lse.data_ptr(), work.data_ptr())
+        if rc:
+            _kv_check(rc, self._h)
+        return out, lse
+
+    def _make(self, shape, dtype):
+        """torch.empty on the calls' stream."""
+        empty = self._empty if self._current(self._index) == self._h.stream_address else self._empty_on_stream
+        return empty(shape, dtype=dtype, device=self.device)
+
+    def _rows(self, layer, q, scale, window, out, lse):
+        """What the calls of the attention pass on of their arguments, checked, with results allocated where none are given."""
         shape, dtype = q.shape, q.dtype
         n, heads, dim = shape
         row, head, inner = q.stride()
@@ -691,11 +879,7 @@ class KvCache:
             layer = -1  # (refused by the call, whose numbers are of 32 bits, as is a negative window)
         if not 0 <= window < 1 << 31:
             window = -1 if window < 0 else (1 << 31) - 1
-        rc = self._attend(self._h, layer, n, None if seq is None else self._list(seq, n, self._int32), q.data_ptr(), row, head, kind,
-                          heads, dim ** -0.5 if scale is None else scale, window, out.data_ptr(), out_row, out_head, lse.data_ptr())
-        if rc:
-            _kv_check(rc, self._h)
-        return out, lse
+        return shape, row, head, kind, out, out_row, out_head, lse, layer, dim ** -0.5 if scale is None else scale, window
 
     def stats(self) -> dict:
         """Pages in use, shared pages, the highest page in use + 1, tokens held (waits for queued work)."""

@@ -105,6 +105,33 @@ cudaError_t launch_kv_write(const KvView& c, const KvScratch& s, int32_t layer, 
 // out (zeroed by the launch): pages in use, pages shared, the highest page in use + 1, tokens held.
 cudaError_t launch_kv_stats(const KvView& c, unsigned long long* out, int num_sms, cudaStream_t st);
 
+// Queries, keys and values of new tokens to norm, rotate and write (kv_rotate.cu); strides in elements.
+struct KvTurn {
+  const void *q, *k, *v;
+  void* out;  // of the queries
+  int64_t q_token, q_head, out_token, out_head, token, head;
+  const uint64_t* turns;
+  const float *q_weight, *k_weight;
+  float amplitude, eps;
+  int32_t heads, type, rot;
+  bool pairs;
+};
+cudaError_t launch_kv_turn(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t layer, int32_t n,
+                           const int32_t* seq, const int64_t* offsets, int64_t n_tokens, int num_sms, cudaStream_t st);
+
+// The last offsets[i + 1] - offsets[i] tokens of each of n sequences (kv_prompt.cu); strides in elements.
+struct KvPrompt {
+  const void* q;
+  void* out;
+  float* lse;
+  const int32_t* seq;  // NULL: sequences 0 .. n-1
+  const int64_t* offsets;
+  int64_t n_tokens, q_token, q_head, out_token, out_head;
+  int32_t n, heads, type, window, layer;
+  float scale;
+};
+cudaError_t launch_kv_prompt(const KvView& c, const KvPrompt& a, int32_t* err, int num_sms, cudaStream_t st);
+
 // One token of each of n sequences (kv_attend.cuh).
 struct KvQuery {
   const void* q;

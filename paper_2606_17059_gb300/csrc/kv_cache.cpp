@@ -5,6 +5,7 @@
 // and _set_stream): a decode loop can be captured in a CUDA graph.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -370,23 +371,36 @@ int p2p_kv_write(p2p_kv* h, int32_t layer, int32_t n_layers, int32_t n, const in
   return P2P_OK;
 }
 
-int p2p_kv_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const void* q, int64_t q_row_stride,
-                  int64_t q_head_stride, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
-                  int64_t out_row_stride, int64_t out_head_stride, float* lse) {
+// What the attention's calls check on the host: what is asked for, and where rows of queries and results lie.
+static bool bad_type(const p2p_kv* h, int32_t type) {
+  return h->c.type == P2P_KV_E4M3 ? type != P2P_KV_BF16 && type != P2P_KV_F16 : type != h->c.type;
+}
+static int check_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, int32_t type, int32_t n_heads,
+                        int32_t window) {
   if (!h) return fail(nullptr, P2P_E_INVAL, "cache is NULL");
   if (layer < 0 || layer >= h->c.n_layers) return fail(h, P2P_E_INVAL, "layer out of range");
   if (n < 0 || n > (1 << 20) || (!seq && n > h->c.n_seqs)) return fail(h, P2P_E_INVAL, "n out of range");
   if (n_heads < 1 || n_heads > 16384 || n_heads % h->c.heads)
     return fail(h, P2P_E_INVAL, "n_heads must be a multiple of the cache's heads, at most 16,384");
-  if (h->c.type == P2P_KV_E4M3 ? type != P2P_KV_BF16 && type != P2P_KV_F16 : type != h->c.type)
-    return fail(h, P2P_E_INVAL, "type of q and out: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
+  if (bad_type(h, type)) return fail(h, P2P_E_INVAL, "type of q and out: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
   if (window < 0) return fail(h, P2P_E_INVAL, "negative window");
-  if (n == 0) return P2P_OK;
+  return P2P_OK;
+}
+static int check_rows(p2p_kv* h, int64_t n, const void* q, int32_t n_heads, const void* out, int64_t out_row,
+                      int64_t out_head, const float* lse) {
   if (!q || !out) return fail(h, P2P_E_INVAL, "NULL device pointer");
   if ((uintptr_t)q % 2 || (uintptr_t)out % 2 || (uintptr_t)lse % 4)
     return fail(h, P2P_E_INVAL, "a pointer is not aligned to its type");
-  if (rows_overlap(n, n_heads, h->c.dim, out_row_stride, out_head_stride))
-    return fail(h, P2P_E_INVAL, "rows of out overlap");
+  if (rows_overlap(n, n_heads, h->c.dim, out_row, out_head)) return fail(h, P2P_E_INVAL, "rows of out overlap");
+  return P2P_OK;
+}
+
+int p2p_kv_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const void* q, int64_t q_row_stride,
+                  int64_t q_head_stride, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
+                  int64_t out_row_stride, int64_t out_head_stride, float* lse) {
+  if (int rc = check_attend(h, layer, n, seq, type, n_heads, window)) return rc;
+  if (n == 0) return P2P_OK;
+  if (int rc = check_rows(h, n, q, n_heads, out, out_row_stride, out_head_stride, lse)) return rc;
   DeviceGuard g(h->device);
   const p2p::KvQuery a = {q, out, lse, seq, q_row_stride, q_head_stride, out_row_stride, out_head_stride,
                           n, n_heads, type, window, layer, scale,
@@ -395,6 +409,89 @@ int p2p_kv_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const
   CK(launch_attend(h->c, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;
+}
+
+int p2p_kv_rotation_turns(int32_t n, const double* radians, uint64_t* turns) {
+  if (n < 0 || (n > 0 && (!radians || !turns))) return fail(nullptr, P2P_E_INVAL, "n is negative or an array is NULL");
+  // 1 / (2 pi) in two parts: the quotient to 2^-64 of a turn or 2^-52 of itself, whichever is more.
+  constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;
+  for (int32_t j = 0; j < n; ++j)
+    if (!(radians[j] >= 0.0) || !(radians[j] < 6.283185307179586)) return fail(nullptr, P2P_E_INVAL, "radians: 0 <= x < 2 pi");
+  for (int32_t j = 0; j < n; ++j) {
+    const double high = radians[j] * kHigh, low = std::fma(radians[j], kHigh, -high) + radians[j] * kLow;
+    const double scaled = std::ldexp(high, 64), whole = std::floor(scaled);
+    turns[j] = (uint64_t)whole + (uint64_t)(int64_t)std::llrint(scaled - whole + std::ldexp(low, 64));
+  }
+  return P2P_OK;
+}
+
+int p2p_kv_write_rotated(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,
+                         int64_t n_tokens, const p2p_kv_rotation* rotation, const void* q, int64_t q_token_stride,
+                         int64_t q_head_stride, int32_t n_heads, const void* k, const void* v, int64_t token_stride,
+                         int64_t head_stride, int32_t type, void* out, int64_t out_token_stride,
+                         int64_t out_head_stride) {
+  if (int rc = check_list(h, n, seq, offsets)) return rc;
+  if (layer < 0 || layer >= h->c.n_layers) return fail(h, P2P_E_INVAL, "layer out of range");
+  if (n_tokens < 0 || n_tokens > INT32_MAX) return fail(h, P2P_E_INVAL, "n_tokens out of range");
+  if (n_heads < 1 || n_heads > 16384) return fail(h, P2P_E_INVAL, "n_heads out of range");
+  if (bad_type(h, type)) return fail(h, P2P_E_INVAL, "type of q, k and v: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
+  if (!rotation) return fail(h, P2P_E_INVAL, "rotation is NULL");
+  const p2p_kv_rotation& r = *rotation;
+  if (r.dim < 0 || r.dim > h->c.dim || r.dim % 2) return fail(h, P2P_E_INVAL, "rotated values: even, at most head_dim");
+  if (r.dim > 0 && !r.turns) return fail(h, P2P_E_INVAL, "turns is NULL");
+  if (n == 0 || n_tokens == 0) return P2P_OK;
+  if (!q || !k || !v || !out) return fail(h, P2P_E_INVAL, "NULL device pointer");
+  if ((uintptr_t)q % 2 || (uintptr_t)k % 2 || (uintptr_t)v % 2 || (uintptr_t)out % 2 || (uintptr_t)r.turns % 8 ||
+      (uintptr_t)r.q_weight % 4 || (uintptr_t)r.k_weight % 4)
+    return fail(h, P2P_E_INVAL, "a pointer is not aligned to its type");
+  if (rows_overlap(n_tokens, n_heads, h->c.dim, out_token_stride, out_head_stride))
+    return fail(h, P2P_E_INVAL, "rows of out overlap");
+  if (q == out && (q_token_stride != out_token_stride || q_head_stride != out_head_stride))
+    return fail(h, P2P_E_INVAL, "q and out start together but have other strides");
+  DeviceGuard g(h->device);
+  const p2p::KvTurn a = {q, k, v, out, q_token_stride, q_head_stride, out_token_stride, out_head_stride, token_stride,
+                         head_stride, r.turns, r.q_weight, r.k_weight, r.amplitude, r.eps, n_heads, type, r.dim,
+                         r.interleaved != 0};
+  CK(p2p::launch_kv_turn(h->c, h->s, a, layer, n, seq, offsets, n_tokens, h->num_sms, h->stream));
+  h->launches += 1;
+  return P2P_OK;
+}
+
+int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,
+                         int64_t n_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t type,
+                         int32_t n_heads, float scale, int32_t window, void* out, int64_t out_token_stride,
+                         int64_t out_head_stride, float* lse) {
+  if (int rc = check_attend(h, layer, n, seq, type, n_heads, window)) return rc;
+  if (n_tokens < 0 || n_tokens > INT32_MAX || n_tokens * n_heads > (int64_t)1 << 36)
+    return fail(h, P2P_E_INVAL, "n_tokens out of range");
+  if (n == 0 || n_tokens == 0) return P2P_OK;
+  if (!offsets) return fail(h, P2P_E_INVAL, "NULL device pointer");
+  if (int rc = check_rows(h, n_tokens, q, n_heads, out, out_token_stride, out_head_stride, lse)) return rc;
+  DeviceGuard g(h->device);
+  const p2p::KvPrompt a = {q, out, lse, seq, offsets, n_tokens, q_token_stride, q_head_stride, out_token_stride,
+                           out_head_stride, n, n_heads, type, window, layer, scale};
+  CK(p2p::launch_kv_prompt(h->c, a, h->s.err, h->num_sms, h->stream));
+  h->launches += 1;
+  return P2P_OK;
+}
+
+int64_t p2p_kv_attend_shared_work(const p2p_kv* h, int32_t n, int32_t n_heads) {
+  if (!h || n < 0 || n > (1 << 20) || n_heads < 1 || n_heads > 16384) return -1;
+  return 16;
+}
+
+int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups, const int32_t* groups,
+                         const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t type, int32_t n_heads,
+                         float scale, int32_t window, void* out, int64_t out_row_stride, int64_t out_head_stride,
+                         float* lse, void* work) {
+  if (int rc = check_attend(h, layer, n, seq, type, n_heads, window)) return rc;
+  if (n_groups < 0 || n_groups > (1 << 20)) return fail(h, P2P_E_INVAL, "n_groups out of range");
+  if (n == 0) return P2P_OK;
+  if ((n_groups > 0 && !groups) || !work) return fail(h, P2P_E_INVAL, "NULL device pointer");
+  if ((uintptr_t)work % 16) return fail(h, P2P_E_INVAL, "work must start on a 16-byte boundary");
+  if (int rc = check_rows(h, n, q, n_heads, out, out_row_stride, out_head_stride, lse)) return rc;
+  return p2p_kv_attend(h, layer, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out, out_row_stride,
+                       out_head_stride, lse);
 }
 
 }  // extern "C"

@@ -15,7 +15,7 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
-#include "kv.h"
+#include "kv_values.cuh"
 
 // (No load here goes past the coherent path, as __ldg or const __restrict__ would have it: the kernel before may
 // still be writing when this one starts, see launch_early.)
@@ -204,15 +204,6 @@ __device__ void settle(const KvView& c, const KvScratch& s, int32_t n, const int
 // looked at after the item's other loads are on their way.)
 __device__ __forceinline__ int32_t claim(const KvScratch& s, int32_t seq, bool first) {
   return first ? atomicExch(&s.claim[seq], 1) : 0;
-}
-
-// A length as the table can hold it, or -1.
-__device__ __forceinline__ int32_t length_of(const KvView& c, int32_t seq) {
-  const int32_t n = c.length[seq];
-  return n >= 0 && n <= c.max_pages * c.page ? n : -1;
-}
-__device__ __forceinline__ int32_t* row_of(const KvView& c, int32_t seq) {
-  return c.table + (int64_t)seq * c.max_pages;
 }
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
@@ -535,21 +526,6 @@ constexpr int kBlock = 32, kWriteThreads = 256;
 constexpr int kFactors = 4096;  // scales of a CTA at most, with 8-bit values: 32 KB of shared memory
 static_assert(kBlock == 32, "a warp finds the places, all its lanes together");
 
-// The last item that starts at or before token t (items without tokens share a start): every lane gets it.
-__device__ __forceinline__ int32_t find_item(const int64_t* offsets, int32_t n, int64_t t) {
-  const int lane = threadIdx.x & 31;
-  int32_t lo = 0, hi = n;
-  while (hi - lo > 1) {  // 32 probes a round
-    const int32_t step = (hi - lo + 31) / 32, at = lo + step * lane;
-    const uint32_t m = __ballot_sync(~0u, at < hi && offsets[at] <= t);
-    if (!m) return lo;
-    const int32_t k = 31 - __clz(m);
-    lo = lo + step * k;
-    hi = min(hi, lo + step);
-  }
-  return lo;
-}
-
 // Rounding x / scale to 8 bits, x of at most 11 bits.  What must not happen is that a quotient close to the middle
 // between two 8-bit values (a tie: T, odd and below 32, times a power of two) is rounded to it, or across it, first.
 // It can for X / T alone that is next to the scale, X of 11 bits: two such ratios are 2^-16 apart, so that it is one
@@ -576,22 +552,6 @@ __device__ __forceinline__ float2 factor_of(float scale) {
   }
   const float inverse = __frcp_rn(scale);
   return make_float2(fmaf(inverse, above ? -0x1p-20f : 0x1p-20f, inverse), 0.f);
-}
-// If the quotient rounded to 32 bits is a tie (its 19 lowest bits are zero) and the quotient is not: one step to its
-// side, as its exact remainder tells (of which nothing vanishes or overflows).  For scales of an extreme size.
-__device__ __forceinline__ float divide_extreme(float x, float scale) {
-  const float z = __fdiv_rn(x, scale), up = fabsf(scale) < 1.f ? 0x1p100f : 1.f, r = fmaf(-z, scale * up, x * up);
-  int32_t b = __float_as_int(z);
-  if ((b & 0x7ffff) == 0 && (r < 0.f || r > 0.f)) b += (r < 0.f) == (x < 0.f) ? 1 : -1;
-  return __int_as_float(b);
-}
-template <bool BF16>
-__device__ __forceinline__ float2 two_values(uint32_t x) {
-  return BF16 ? __bfloat1622float2(*(const __nv_bfloat162*)&x) : __half22float2(*(const __half2*)&x);
-}
-// Two values to 8 bits each, the first in the low ones.
-__device__ __forceinline__ uint32_t narrow(float2 v) {
-  return __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3);
 }
 // 16 values, each by `divide`, to 8 bits.
 template <bool BF16, class F>
@@ -672,38 +632,10 @@ __global__ void __launch_bounds__(kWriteThreads)
     return (array & 1 ? c.v_scale : c.k_scale)[(layer + (array >> 1)) * c.heads + i - over * c.heads];
   };
   read(threadIdx.x);  // (on their way while it is found where they go)
-  if (blockIdx.x == 0 && blockIdx.y == 0)
-    for (int32_t i = threadIdx.x; i < n; i += kWriteThreads)
-      if (offsets[i] < 0 || offsets[i + 1] < offsets[i] || offsets[i + 1] > n_tokens) atomicOr(s.err, KV_BAD_OFFSETS);
+  if (blockIdx.x == 0 && blockIdx.y == 0) check_offsets(offsets, n, n_tokens, s.err);
   if (threadIdx.x < kBlock) {
-    const int64_t t = t0 + threadIdx.x;
-    int32_t lo = find_item(offsets, n, t0), hi = min(n, find_item(offsets, n, t0 + kBlock - 1) + 1);
-    while (hi - lo > 1) {
-      const int32_t mid = (lo + hi) >> 1;
-      if (offsets[mid] <= t)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    int64_t at = -1;
-    const int64_t o0 = offsets[lo], o1 = offsets[lo + 1];
-    if (!halt && o0 >= 0 && o0 <= t && t < o1 && o1 <= n_tokens) {  // (else it belongs to no sequence)
-      const int32_t q = seq[lo], len = (uint32_t)q < (uint32_t)c.n_seqs ? length_of(c, q) : 0;
-      int32_t bad = 0;
-      if ((uint32_t)q >= (uint32_t)c.n_seqs) {
-        bad = KV_BAD_SEQ;
-      } else if (o1 - o0 > len) {
-        bad = KV_BAD_COUNT;
-      } else {
-        const int32_t pos = len - (int32_t)(o1 - t), e = (int32_t)c.by_page.div(pos), page = row_of(c, q)[e];
-        const int32_t refs = (uint32_t)page < (uint32_t)c.n_pages ? c.refs[page] : 0;
-        if (refs != 1)
-          bad = refs > 1 ? KV_SHARED : KV_BAD_PAGE;
-        else
-          at = page * c.page_stride + (pos - e * c.page) * c.token_stride;
-      }
-      if (bad) atomicOr(s.err, bad);
-    }
+    int32_t pos;
+    const int64_t at = place_of(c, s, n, seq, offsets, n_tokens, t0, halt, pos);
     place[threadIdx.x] = at;
   } else if (KIND == P2P_KV_E4M3) {  // (the other warps, a scale for each half of one)
     const int32_t scales = (a1 - a0) * c.heads, half = threadIdx.x >> 4 & 1;
