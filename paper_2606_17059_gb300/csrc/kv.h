@@ -65,7 +65,7 @@ struct KvView {
 };
 
 // Bits of the device error word.
-enum { KV_BAD_SEQ = 1, KV_BAD_COUNT = 2, KV_NO_PAGES = 4, KV_BAD_PAGE = 8, KV_SHARED = 16, KV_BAD_OFFSETS = 32 };
+enum { KV_BAD_SEQ = 1, KV_BAD_COUNT = 2, KV_NO_PAGES = 4, KV_BAD_PAGE = 8, KV_SHARED = 16, KV_BAD_OFFSETS = 32, KV_STUCK = 64 };
 
 struct __align__(16) KvJob {  // copy the first `tokens` tokens of page `from` to page `to`, in every layer
   int32_t from, to, tokens, pad_;
@@ -119,19 +119,6 @@ struct KvTurn {
 cudaError_t launch_kv_turn(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t layer, int32_t n,
                            const int32_t* seq, const int64_t* offsets, int64_t n_tokens, int num_sms, cudaStream_t st);
 
-// The last offsets[i + 1] - offsets[i] tokens of each of n sequences (kv_prompt.cu); strides in elements.
-struct KvPrompt {
-  const void* q;
-  void* out;
-  float* lse;
-  const int32_t* seq;  // NULL: sequences 0 .. n-1
-  const int64_t* offsets;
-  int64_t n_tokens, q_token, q_head, out_token, out_head;
-  int32_t n, heads, type, window, layer;
-  float scale;
-};
-cudaError_t launch_kv_prompt(const KvView& c, const KvPrompt& a, int32_t* err, int num_sms, cudaStream_t st);
-
 // One token of each of n sequences (kv_attend.cuh).
 struct KvQuery {
   const void* q;
@@ -143,6 +130,10 @@ struct KvQuery {
   float scale;
   // Whether rows of q may be read by twos, and those of out written by fours, of their values.
   bool q_pairs, out_fours;
+  // Row i is taken from token skip[i] on (NULL: all of it); where that is not 0, its result goes, in 32 bits, to
+  // own [row][head][value] and own_lse [row][head].
+  const int32_t* skip;
+  float *own, *own_lse;
 };
 // The attention's kernel for values of a type, head_dim and `group` query heads a kv head: head_dim as it is padded,
 // blocks of eight query heads taken together, and CTAs resident on an SM.
@@ -207,5 +198,43 @@ cudaError_t launch_kv_attend_e4m3(const KvView& c, const KvQuery* q, const KvAtt
                                   cudaStream_t st);
 cudaError_t launch_kv_attend_e4m3_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
                                        cudaStream_t st);
+
+
+// What the rows of each group share, into spans[n_groups] (x: leading entries that are the same; y, z: the first and the last
+// token that a row's window begins with), and the tokens of each row that its group works off, into skip[n].
+cudaError_t launch_kv_share(const KvView& c, int32_t* err, int32_t n, const int32_t* seq, int32_t n_groups,
+                            const int32_t* groups, int32_t window, int32_t* skip, int4* spans, cudaStream_t st);
+// Fewer shared tokens than these are read by each row for itself.
+constexpr int kSharedTokens = 64;
+
+// Many query rows over the same keys and values (kv_rows.cuh): the last offsets[i + 1] - offsets[i] tokens of each of n
+// sequences, or, with spans, what each of n groups of rows shares.  Strides in elements.
+struct KvRowsCall {
+  const void* q;
+  void* out;
+  float* lse;
+  const int32_t* seq;  // of a sequence, or of a row; NULL: its own number
+  const int64_t* offsets;
+  const int32_t* groups;    // [n + 1]
+  const int4* spans;        // [n]: see launch_kv_share
+  const float *own, *own_lse;  // [row][head][value] and [row][head]: the result over the other tokens of a row (NULL: there are none)
+  int64_t n_tokens, q_row, q_head, out_row, out_head;
+  int32_t n, heads, group, type, window, layer;  // group: query heads a kv head
+  FastDiv by_group;
+  float scale;
+  bool q16, out16;  // whether rows of q (of out) lie on 16-byte boundaries
+};
+// Floats of KvAttendScratch::parts: two parts a CTA, of 256 or (head_dim above 128) 128 rows.
+inline size_t kv_rows_parts(const KvView& c, int num_sms) {
+  const int dp = (c.dim + 63) / 64 * 64;
+  return (size_t)2 * num_sms * (dp <= 128 ? 256 : 128) * (dp + 2);
+}
+// With a = NULL they launch nothing, but make the cache's kernel ready for launches (at creation).
+cudaError_t launch_kv_rows_bf16(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+                                cudaStream_t st);
+cudaError_t launch_kv_rows_f16(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+                               cudaStream_t st);
+cudaError_t launch_kv_rows_e4m3(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+                                cudaStream_t st);
 
 }  // namespace p2p

@@ -37,16 +37,9 @@
 // slots that 16-bit values do not need and that 8-bit values, which have to be widened beside 16-bit queries, could
 // not use it for.
 #pragma once
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-#include <cuda_fp8.h>
-
 #include <type_traits>
 
-#include "kv.h"
-
-// (No load here goes past the coherent path, as __ldg or const __restrict__ would have it: the kernel before may
-// still be writing when this one starts, see launch_early.)
+#include "kv_math.cuh"
 
 namespace p2p {
 namespace {
@@ -65,24 +58,6 @@ constexpr int kJoin = 16;               // parts of a unit row that are read tog
 // 71); 512 of 1 to 800 (5.6 units) with 8 of 256 and 4 or 8 96 and 140, not 120 and 136 (112 and 119).  Beyond, the
 // parts cost as much or more: 512 of 1 to 1,200 with 8 of 256 and 8 171, not 153 (138).
 constexpr int kSideUnits = 32, kSideParts = 16, kSideShort = 6;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// kUp: exp(x - m) is taken times 2^kUp (m is held less kUp, in log2).  kLag: how far (log2) a logit may pass the
-// maximum in use.  P is at most 2^(kUp + kLag), which f16 has to hold.
-template <int KIND>
-struct Type;
-template <>
-struct Type<P2P_KV_BF16> {
-  static constexpr float kUp = 0.f, kLag = 8.f;
-};
-template <>
-struct Type<P2P_KV_F16> {
-  static constexpr float kUp = 12.f, kLag = 3.f;
-};
-template <>
-struct Type<P2P_KV_E4M3> {
-  static constexpr float kUp = 12.f, kLag = 3.f;
-};
 
 // Sizes of the kernel for values of KIND, head_dim padded to DP, NB blocks of eight query heads.
 template <int KIND, int DP, int NB>
@@ -110,15 +85,6 @@ struct Shape {
   static_assert(kStages >= 2, "a tile on its way");
 };
 
-__device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool in) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void load4(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -150,50 +116,15 @@ __device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
-__device__ __forceinline__ int32_t add_acq_rel(int32_t* p, int32_t x) {
-  int32_t y;
-  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(y) : "l"(p), "r"(x) : "memory");
-  return y;
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// ln of a sum of exp that was taken relative to t (in log2): near the largest term, where log2 is small.
-template <int KIND>
-__device__ __forceinline__ float log_sum(float t, float z) {
-  constexpr float kUp = Type<KIND>::kUp, kDown = 1.f / (1 << (int)kUp);
-  return (t + kUp + __log2f(z * kDown)) * kLn2;
-}
-template <int KIND>
-__device__ __forceinline__ uint32_t pack(float a, float b) {
-  if (KIND == P2P_KV_BF16) {
-    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
-    return *(const uint32_t*)&x;
-  }
-  const __half2 x = __floats2half2_rn(a, b);
-  return *(const uint32_t*)&x;
-}
-// Two 8-bit values (the low half of x) as two of 16.
-__device__ __forceinline__ uint32_t widen(uint32_t x) {
-  uint32_t y;
-  asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, lo; }" : "=r"(y) : "r"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t widen_high(uint32_t x) {
-  uint32_t y;
-  asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, hi; }" : "=r"(y) : "r"(x));
-  return y;
-}
-__device__ __forceinline__ float2 two_halves(uint32_t x, int32_t type) {
-  return type == P2P_KV_BF16 ? __bfloat1622float2(*(const __nv_bfloat162*)&x) : __half22float2(*(const __half2*)&x);
-}
 // Values d .. d + 3 of a head's result, times f; zero: 0 in their place.
 __device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_t i, int32_t head, int32_t d, float4 v,
                                        float f, bool zero) {
   if (d >= c.dim) return;  // (dim is a multiple of 8)
   if (zero) v = make_float4(0.f, 0.f, 0.f, 0.f), f = 0.f;
+  if (a.skip && a.skip[i] > 0) {
+    *(float4*)(a.own + ((int64_t)i * a.heads + head) * c.dim + d) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+    return;
+  }
   const uint32_t x = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.x * f, v.y * f) : pack<P2P_KV_F16>(v.x * f, v.y * f);
   const uint32_t y = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.z * f, v.w * f) : pack<P2P_KV_F16>(v.z * f, v.w * f);
   uint16_t* to = (uint16_t*)a.out + i * a.out_row + head * a.out_head + d;
@@ -203,6 +134,11 @@ __device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_
     to[0] = (uint16_t)x, to[1] = (uint16_t)(x >> 16);
     to[2] = (uint16_t)y, to[3] = (uint16_t)(y >> 16);
   }
+}
+
+__device__ __forceinline__ void store_lse(const KvQuery& a, int32_t i, int32_t head, float lse) {
+  float* const to = a.skip && a.skip[i] > 0 ? a.own_lse : a.lse;
+  if (to) to[(int64_t)i * a.heads + head] = lse;
 }
 
 // Byte offset in a warp's tile of piece `piece` of row `row`: the pieces of eight rows that ldmatrix reads together lie
@@ -231,6 +167,7 @@ __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t
   if (err && !(known && fits)) atomicOr(err, known ? KV_BAD_COUNT : KV_BAD_SEQ);
   Row r = {known ? seq : 0, 0, 0, fits ? len : 0};
   r.begin = a.window && r.end > a.window ? r.end - a.window : 0;
+  if (a.skip && there) r.begin = min(max(r.begin, a.skip[i]), r.end);
   r.from = WHOLE ? r.begin / 16 * 16 : r.begin;
   return r;
 }
@@ -743,7 +680,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
           const int32_t q_head = head0 + beside * group + h8;
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
           store4(c, a, u.i, q_head, d, v, __fdividef(v_scale, z), empty);
-          if (d == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = empty ? -INFINITY : log_sum<KIND>(t, z);
+          if (d == 0) store_lse(a, u.i, q_head, empty ? -INFINITY : log_sum<KIND>(t, z));
         }
       }
       if (whole || b + 1 < NB) __syncthreads();  // the sums' room is free again
@@ -859,7 +796,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
               const int32_t q_head = head0 + beside * group + at[i] % S::kHeads;
               const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
               store4(c, a, u.i, q_head, d[i], v[i], __fdividef(v_scale, z[i]), false);
-              if (d[i] == 0 && a.lse) a.lse[(int64_t)u.i * a.heads + q_head] = log_sum<KIND>(t[i], z[i]);
+              if (d[i] == 0) store_lse(a, u.i, q_head, log_sum<KIND>(t[i], z[i]));
             } else {
               *(float4*)(joined + at[i] * DP + d[i]) = v[i];
               if (d[i] == 0) joined[part_heads * DP + at[i]] = t[i], joined[part_heads * (DP + 1) + at[i]] = z[i];

@@ -138,6 +138,14 @@ cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p
   return (c.side != 0 && (c.lines || many) ? side_by_side : alone)(c, q, w, num_sms, st);
 }
 
+cudaError_t launch_rows(const p2p::KvView& c, const p2p::KvRowsCall* a, const p2p::KvAttendScratch& w, int num_sms,
+                        cudaStream_t st) {
+  using namespace p2p;
+  return (c.type == P2P_KV_BF16  ? launch_kv_rows_bf16
+          : c.type == P2P_KV_F16 ? launch_kv_rows_f16
+                                 : launch_kv_rows_e4m3)(c, a, w, num_sms, st);
+}
+
 // Scratch comes from a memory pool of the library's for each device, which keeps what destroyed handles give back: a
 // handle made after them takes 40 us, not 135.  NULL, with *e set, where there is none.
 cudaMemPool_t scratch_pool(int device, cudaError_t* e) {
@@ -217,12 +225,13 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
                arrived = part(sizeof(int32_t) * 4 * p2p::KvAttendScratch::kCtasPerSm * sms), zero = at,
                start = part(4 * (S + 1)), first = part(4 * S), cut = part(4 * S),
                list = part(4 * N), jobs = part(sizeof(p2p::KvJob) * std::max(S, N)),
-               parts = part(sizeof(float) * p2p::kv_attend_parts(c, sms));
+               parts = part(sizeof(float) * std::max(p2p::kv_attend_parts(c, sms), p2p::kv_rows_parts(c, sms)));
   cudaError_t e = cudaSuccess;
   if (const cudaMemPool_t pool = scratch_pool(dev, &e)) e = cudaMallocFromPoolAsync(&n->scratch, at, pool, nullptr);
   if (e == cudaSuccess) e = cudaMemsetAsync(n->scratch, 0, zero, nullptr);
   if (e == cudaSuccess) e = p2p::prepare_kv_pages();
   if (e == cudaSuccess) e = launch_attend(c, nullptr, n->w, sms, nullptr);
+  if (e == cudaSuccess) e = launch_rows(c, nullptr, n->w, sms, nullptr);
   // (calls may go to a stream that does not wait for this one)
   if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
   if (e != cudaSuccess) {
@@ -281,12 +290,13 @@ int p2p_kv_sync(p2p_kv* h) {
   if (b == p2p::KV_NO_PAGES) return fail(h, P2P_E_NOMEM, "the pool has too few free pages");
   char m[256];
   const auto say = [b](int bit, const char* what) { return b & bit ? what : ""; };
-  std::snprintf(m, sizeof(m), "device reported:%s%s%s%s%s%s",
+  std::snprintf(m, sizeof(m), "device reported:%s%s%s%s%s%s%s",
                 say(p2p::KV_BAD_SEQ, " a sequence out of range or named twice;"),
                 say(p2p::KV_BAD_COUNT, " a count or length out of range;"),
                 say(p2p::KV_NO_PAGES, " too few free pages;"),
                 say(p2p::KV_BAD_PAGE, " a page table or reference count that does not hold together;"),
-                say(p2p::KV_SHARED, " a write to a shared page;"), say(p2p::KV_BAD_OFFSETS, " offsets out of range;"));
+                say(p2p::KV_SHARED, " a write to a shared page;"), say(p2p::KV_BAD_OFFSETS, " offsets out of range;"),
+                say(p2p::KV_STUCK, " a kernel that gave up waiting for itself;"));
   return fail(h, P2P_E_DEVICE, m);
 }
 
@@ -395,6 +405,15 @@ static int check_rows(p2p_kv* h, int64_t n, const void* q, int32_t n_heads, cons
   return P2P_OK;
 }
 
+static p2p::KvQuery query_of(int32_t layer, int32_t n, const int32_t* seq, const void* q, int64_t q_row, int64_t q_head,
+                             int32_t type, int32_t n_heads, float scale, int32_t window, void* out, int64_t out_row,
+                             int64_t out_head, float* lse) {
+  return {q, out, lse, seq, q_row, q_head, out_row, out_head, n, n_heads, type, window, layer, scale,
+          (uintptr_t)q % 4 == 0 && q_row % 2 == 0 && q_head % 2 == 0,
+          (uintptr_t)out % 8 == 0 && out_row % 4 == 0 && out_head % 4 == 0,
+          nullptr, nullptr, nullptr};
+}
+
 int p2p_kv_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const void* q, int64_t q_row_stride,
                   int64_t q_head_stride, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
                   int64_t out_row_stride, int64_t out_head_stride, float* lse) {
@@ -402,10 +421,8 @@ int p2p_kv_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const
   if (n == 0) return P2P_OK;
   if (int rc = check_rows(h, n, q, n_heads, out, out_row_stride, out_head_stride, lse)) return rc;
   DeviceGuard g(h->device);
-  const p2p::KvQuery a = {q, out, lse, seq, q_row_stride, q_head_stride, out_row_stride, out_head_stride,
-                          n, n_heads, type, window, layer, scale,
-                          (uintptr_t)q % 4 == 0 && q_row_stride % 2 == 0 && q_head_stride % 2 == 0,
-                          (uintptr_t)out % 8 == 0 && out_row_stride % 4 == 0 && out_head_stride % 4 == 0};
+  const p2p::KvQuery a = query_of(layer, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out,
+                                  out_row_stride, out_head_stride, lse);
   CK(launch_attend(h->c, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;
@@ -457,27 +474,56 @@ int p2p_kv_write_rotated(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   return P2P_OK;
 }
 
+static p2p::KvRowsCall rows_call(const p2p_kv* h, int32_t layer, const int32_t* seq, const void* q, int64_t q_row,
+                                 int64_t q_head, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
+                                 int64_t out_row, int64_t out_head, float* lse) {
+  p2p::KvRowsCall a = {};
+  a.q = q, a.out = out, a.lse = lse, a.seq = seq;
+  a.q_row = q_row, a.q_head = q_head, a.out_row = out_row, a.out_head = out_head;
+  a.heads = n_heads, a.group = n_heads / h->c.heads, a.type = type, a.window = window, a.layer = layer, a.scale = scale;
+  a.by_group = p2p::FastDiv((uint32_t)a.group);
+  a.q16 = (uintptr_t)q % 16 == 0 && q_row % 8 == 0 && q_head % 8 == 0;
+  a.out16 = (uintptr_t)out % 16 == 0 && out_row % 8 == 0 && out_head % 8 == 0;
+  return a;
+}
+
 int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,
                          int64_t n_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t type,
                          int32_t n_heads, float scale, int32_t window, void* out, int64_t out_token_stride,
                          int64_t out_head_stride, float* lse) {
   if (int rc = check_attend(h, layer, n, seq, type, n_heads, window)) return rc;
-  if (n_tokens < 0 || n_tokens > INT32_MAX || n_tokens * n_heads > (int64_t)1 << 36)
+  if (n_tokens < 0 || n_tokens > INT32_MAX || n_tokens * n_heads > (int64_t)1 << 33)
     return fail(h, P2P_E_INVAL, "n_tokens out of range");
   if (n == 0 || n_tokens == 0) return P2P_OK;
   if (!offsets) return fail(h, P2P_E_INVAL, "NULL device pointer");
   if (int rc = check_rows(h, n_tokens, q, n_heads, out, out_token_stride, out_head_stride, lse)) return rc;
   DeviceGuard g(h->device);
-  const p2p::KvPrompt a = {q, out, lse, seq, offsets, n_tokens, q_token_stride, q_head_stride, out_token_stride,
-                           out_head_stride, n, n_heads, type, window, layer, scale};
-  CK(p2p::launch_kv_prompt(h->c, a, h->s.err, h->num_sms, h->stream));
+  p2p::KvRowsCall a = rows_call(h, layer, seq, q, q_token_stride, q_head_stride, type, n_heads, scale, window, out,
+                                out_token_stride, out_head_stride, lse);
+  a.offsets = offsets;
+  a.n_tokens = n_tokens;
+  a.n = n;
+  CK(launch_rows(h->c, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;
 }
 
+// Where the parts of attend_shared's work lie: each row's result over its own tokens, what the groups share, and what of a row
+// its group works off.
+struct SharedWork {
+  size_t lse, spans, skip, bytes;
+  SharedWork(const p2p::KvView& c, int32_t n, int32_t n_heads) {
+    const size_t rows = (size_t)n * n_heads;
+    lse = sizeof(float) * rows * c.dim;
+    spans = lse + sizeof(float) * ((rows + 3) / 4 * 4);
+    skip = spans + sizeof(int4) * n;
+    bytes = skip + sizeof(int32_t) * n + 16;
+  }
+};
+
 int64_t p2p_kv_attend_shared_work(const p2p_kv* h, int32_t n, int32_t n_heads) {
   if (!h || n < 0 || n > (1 << 20) || n_heads < 1 || n_heads > 16384) return -1;
-  return 16;
+  return (int64_t)SharedWork(h->c, n, n_heads).bytes;
 }
 
 int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups, const int32_t* groups,
@@ -485,13 +531,37 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
                          float scale, int32_t window, void* out, int64_t out_row_stride, int64_t out_head_stride,
                          float* lse, void* work) {
   if (int rc = check_attend(h, layer, n, seq, type, n_heads, window)) return rc;
-  if (n_groups < 0 || n_groups > (1 << 20)) return fail(h, P2P_E_INVAL, "n_groups out of range");
+  if (n_groups < 0 || n_groups > n) return fail(h, P2P_E_INVAL, "n_groups: at most n");
   if (n == 0) return P2P_OK;
   if ((n_groups > 0 && !groups) || !work) return fail(h, P2P_E_INVAL, "NULL device pointer");
   if ((uintptr_t)work % 16) return fail(h, P2P_E_INVAL, "work must start on a 16-byte boundary");
   if (int rc = check_rows(h, n, q, n_heads, out, out_row_stride, out_head_stride, lse)) return rc;
-  return p2p_kv_attend(h, layer, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out, out_row_stride,
-                       out_head_stride, lse);
+  DeviceGuard g(h->device);
+  const SharedWork at(h->c, n, n_heads);
+  float *own = (float*)work, *own_lse = (float*)((char*)work + at.lse);
+  int4* spans = (int4*)((char*)work + at.spans);
+  int32_t* skip = (int32_t*)((char*)work + at.skip);
+  // What the groups share; every row's other tokens; the shared ones and both together.
+  CK(p2p::launch_kv_share(h->c, h->s.err, n, seq, n_groups, groups, window, skip, spans, h->stream));
+  p2p::KvQuery rest = query_of(layer, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out,
+                               out_row_stride, out_head_stride, lse);
+  rest.skip = skip;
+  rest.own = own;
+  rest.own_lse = own_lse;
+  CK(launch_attend(h->c, &rest, h->w, h->num_sms, h->stream));
+  h->launches += 2;
+  if (n_groups == 0) return P2P_OK;
+  p2p::KvRowsCall a = rows_call(h, layer, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out,
+                                out_row_stride, out_head_stride, lse);
+  a.groups = groups;
+  a.spans = spans;
+  a.own = own;
+  a.own_lse = own_lse;
+  a.n_tokens = n;
+  a.n = n_groups;
+  CK(launch_rows(h->c, &a, h->w, h->num_sms, h->stream));
+  h->launches += 1;
+  return P2P_OK;
 }
 
 }  // extern "C"

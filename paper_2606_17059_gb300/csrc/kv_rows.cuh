@@ -1,0 +1,1000 @@
+// kv_rows.cuh -- attention of many query rows over the same keys and values of the paged cache: the new tokens of prompts
+// (p2p_kv_attend_prompt) and the shared part of rows that begin with the same pages (p2p_kv_attend_shared).
+//
+// For a query row and the tokens t that it sees: x_t = scale * q . k_t, m = max x_t, z = sum exp(x_t - m), out = sum
+// exp(x_t - m) v_t / z, lse = m + ln z.  Rows are (token, query head of one kv head) pairs, numbered with the heads inside
+// the tokens; a unit is a tile of kRowsMax consecutive ones of one sequence (or group) and kv head, with the tokens that
+// any of them sees, kBt at a time.
+//
+// Both products are the tensor cores' (tcgen05): S = Q K^T with Q and K in shared memory, O += P V with P in tensor memory
+// and V in shared memory as it lies in the pages, tokens by values, which the second product takes as its transposed operand.
+// S, P (in the place of S) and O stay in tensor memory; a thread owns a row, so maxima and sums need no shuffles.  Two tiles
+// of 128 rows take turns: while one's logits go through exp, the tensor cores work on the other's.  exp(x - m) takes for m a
+// maximum that lags the running one by at most 2^kLag (see Type), so that O is rarely rescaled.
+//
+// A CTA of the persistent grid takes an equal, contiguous share of all units' steps (a step: kBt tokens); a unit that several
+// CTAs share goes to scratch in parts, and the CTA that brings the last one joins them in their order, so results do not
+// depend on timing.  Warps: softmax (four a row tile), copies (four), and one each for the products and the schedule, two that
+// look for infinities and NaN among the values of tokens which not all rows see: 0 * NaN is NaN, so such values are taken
+// out before the product and added to the rows that do see them at the end.
+#pragma once
+#include "kv_math.cuh"
+#include "kv_values.cuh"
+
+namespace p2p {
+namespace {
+
+template <int KIND, int DP>
+struct RowsShape {
+  static constexpr int kTiles = DP <= 128 ? 2 : 1;     // row tiles of a unit
+  static constexpr int kRowsMax = 128 * kTiles;
+  static constexpr int kBt = DP <= 128 ? 128 : 64;     // tokens of a step
+  static constexpr int kBtLog = DP <= 128 ? 7 : 6;
+  static constexpr int kChunks = DP / 64;              // of 64 values: 128 bytes, a swizzled row
+  static constexpr int kQTile = 128 * DP * 2;
+  static constexpr int kStage = kBt * DP * 2;          // keys or values of a step, 16 bits each
+  static constexpr int kRaw = KIND == P2P_KV_E4M3 ? kBt * DP : 0;  // the same in 8 bits, on its way
+  static constexpr int kRaws = 0;
+  static constexpr int kMisc = 2048;
+  static constexpr int kFit = (232448 - 1024 - kMisc - kTiles * kQTile - kRaws * kRaw) / kStage;
+  static constexpr int kStages = kFit < 8 ? kFit : 8;
+  static_assert(kStages >= 3, "");
+  static constexpr int kBytes = 1024 + kMisc + kTiles * kQTile + kRaws * kRaw + kStages * kStage;
+  static constexpr int kSoft = 4 * kTiles;             // softmax warps
+  static constexpr int kThreads = (kSoft + 8) * 32;
+  static constexpr int kOCol = kTiles * kBt;           // columns of tensor memory: S of the tiles, then O of them
+  static_assert(kOCol + kTiles * DP <= 512);
+  static constexpr int kSet = 2;                       // steps that a unit counts for beyond its own
+};
+
+constexpr int kRing = 4;  // units that the schedule is ahead
+struct RowsUnit {
+  int64_t row;       // of q: the unit's first
+  int32_t rows;      // 0: no more units
+  int32_t g0;        // the first row's head among its kv head's
+  int32_t h, seq;
+  int32_t pos;       // prompts: position of the first row's token
+  int32_t begin, end;        // tokens that any row sees
+  int32_t all_begin, all_end;  // tokens that every row sees, or none
+  int32_t j0, j1;            // steps of this piece
+  int32_t t0[2], t1[2];      // of them, those of each row tile
+  int32_t parts, part, c0;   // of the unit, where it is shared: this piece's number and the first one's CTA
+};
+struct RowsShared {
+  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], team[2], drain;
+  RowsUnit unit[kRing];
+  int64_t sums[16];
+  int64_t before, total;
+  int32_t item, tmem, dead, last[2];
+  int32_t poison[kRing];     // whether values were taken out of the unit's steps
+};
+static_assert(sizeof(RowsShared) <= 2048);
+
+__device__ __forceinline__ void bar_init(const uint64_t& bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_of(&bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(const uint64_t& bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_of(&bar)) : "memory");
+}
+__device__ __forceinline__ bool bar_try(const uint64_t& bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.b32 %0, 1, 0, p; }"
+               : "=r"(ok)
+               : "r"(smem_of(&bar)), "r"(parity)
+               : "memory");
+  return ok;
+}
+// Waits for a phase; false where that takes seconds (which it never should: the kernel then ends and reports it).
+__device__ __forceinline__ bool bar_wait_long(const uint64_t& bar, uint32_t parity, RowsShared& sh) {
+  const long long from = clock64();
+  while (!bar_try(bar, parity)) {
+    if (*(volatile int32_t*)&sh.dead) return false;
+    if (clock64() - from > 4000000000ll) {
+      *(volatile int32_t*)&sh.dead = 1;
+      return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ bool bar_wait(const uint64_t& bar, uint32_t parity, RowsShared& sh) {
+  return bar_try(bar, parity) || bar_wait_long(bar, parity, sh);
+}
+__device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void mma_done(const uint64_t& bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_of(&bar))
+               : "memory");
+}
+// A matrix in shared memory, rows of 128 bytes turned within eights of them; lead: bytes between chunks of 64 values, for an
+// operand whose rows are the product's k.
+__device__ __forceinline__ uint64_t matrix(uint32_t at, uint32_t lead) {
+  return (uint64_t)((at & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
+               "l"(a), "l"(b), "r"(what), "r"((uint32_t)add)
+               : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
+               "r"(a), "l"(b), "r"(what), "r"((uint32_t)add)
+               : "memory");
+}
+#define P2P_R8(r, o) "=r"((r)[o]), "=r"((r)[o + 1]), "=r"((r)[o + 2]), "=r"((r)[o + 3]), "=r"((r)[o + 4]), "=r"((r)[o + 5]), \
+                     "=r"((r)[o + 6]), "=r"((r)[o + 7])
+#define P2P_I8(r, o) "r"((r)[o]), "r"((r)[o + 1]), "r"((r)[o + 2]), "r"((r)[o + 3]), "r"((r)[o + 4]), "r"((r)[o + 5]), \
+                     "r"((r)[o + 6]), "r"((r)[o + 7])
+// 32 columns of the warp's 32 rows, a row a lane.
+__device__ __forceinline__ void tmem_load(uint32_t* r, uint32_t at) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+               "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+               : P2P_R8(r, 0), P2P_R8(r, 8), P2P_R8(r, 16), P2P_R8(r, 24)
+               : "r"(at)
+               : "memory");
+}
+// The same for 16 columns.
+__device__ __forceinline__ void tmem_load16(uint32_t* r, uint32_t at) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+               "[%16];"
+               : P2P_R8(r, 0), P2P_R8(r, 8)
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+               "%16};" ::"r"(at),
+               P2P_I8(r, 0), P2P_I8(r, 8)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+  uint64_t x;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
+  return x;
+}
+__device__ __forceinline__ float2 parts_of(uint64_t x) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(x));
+  return f;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t x;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+  return x;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t x;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+  return x;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float x;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(b), "f"(c));
+  return x;
+}
+
+// An item of the call: a sequence with its new tokens, or a group with what it shares.  Its tiles of rows follow one another for
+// each kv head in turn.
+struct RowsItem {
+  int64_t row0;              // its first row of q
+  int64_t all;               // rows: tokens (or members) times heads of a kv head
+  int32_t seq, pos;          // the first token's position; of a group: where the last row's window begins
+  int32_t shared, first;     // of a group: tokens first .. shared - 1 are seen
+  int32_t tiles;
+};
+template <class S>
+__device__ __forceinline__ RowsItem rows_item(const KvView& c, const KvRowsCall& a, int32_t i, int32_t* err) {
+  RowsItem r = {0, 0, 0, 0, 0, 0, 0};
+  if (a.spans) {
+    const int4 span = a.spans[i];
+    if (span.x == 0) return r;  // (nothing is shared, or the groups do not hold)
+    const int32_t r0 = a.groups[i], r1 = a.groups[i + 1], shared = shared_tokens(c, span, r1 - r0);
+    if (shared == 0) return r;
+    r = {r0, (int64_t)(r1 - r0) * a.group, a.seq ? a.seq[r0] : r0, span.z, shared, span.y, 0};
+  } else {
+    const int64_t o0 = a.offsets[i], o1 = a.offsets[i + 1];
+    int32_t bad = o0 < 0 || o1 < o0 || o1 > a.n_tokens ? KV_BAD_OFFSETS : 0;
+    if (!bad && o1 > o0) {
+      const int32_t seq = a.seq ? a.seq[i] : i;
+      if ((uint32_t)seq >= (uint32_t)c.n_seqs) {
+        bad = KV_BAD_SEQ;
+      } else {
+        const int32_t len = length_of(c, seq);
+        if (len < o1 - o0)
+          bad = KV_BAD_COUNT;
+        else
+          r = {o0, (o1 - o0) * a.group, seq, len - (int32_t)(o1 - o0), 0, 0, 0};
+      }
+    }
+    if (bad && err) atomicOr(err, bad);
+  }
+  r.tiles = (int32_t)((r.all + S::kRowsMax - 1) / S::kRowsMax);
+  return r;
+}
+// Tokens that rows r0 .. r1 - 1 of an item see: any of them, and each of them.
+struct RowsSpan {
+  int32_t begin, end, all_begin, all_end;
+};
+__device__ __forceinline__ int32_t window_begin(const KvRowsCall& a, int32_t end) {
+  return a.window && end > a.window ? end - a.window : 0;
+}
+__device__ __forceinline__ RowsSpan rows_span(const KvRowsCall& a, const RowsItem& it, int64_t r0, int64_t r1) {
+  if (a.spans) {
+    return {it.first, it.shared, it.pos, it.shared};
+  }
+  const int32_t e0 = it.pos + (int32_t)(r0 / a.group) + 1, e1 = it.pos + (int32_t)((r1 - 1) / a.group) + 1;
+  return {window_begin(a, e0), e1, window_begin(a, e1), e0};
+}
+// What the first j tiles of an item count for, each kSet for itself and about its steps: any rising function would do, as
+// long as all CTAs take the same.
+template <class S>
+__device__ __forceinline__ int64_t rows_cost(const KvRowsCall& a, const RowsItem& it, int64_t j) {
+  if (a.spans) return j * (((it.shared - 1) >> S::kBtLog) - (it.first >> S::kBtLog) + 1 + S::kSet);
+  const int64_t per = (int64_t)a.group << S::kBtLog;  // a tile's rows are kRowsMax / per of a step
+  const int64_t base = (it.pos >> S::kBtLog) + 1 + S::kSet;
+  int64_t rising = j, most = 0;
+  if (a.window) {
+    most = a.window / S::kBt + S::kRowsMax / per + 2;
+    rising = max((int64_t)0, min(j, ((most + S::kSet - base) * per) / S::kRowsMax));
+  }
+  return rising * base + S::kRowsMax * rising * (rising + 1) / (2 * per) + (j - rising) * (most + S::kSet);
+}
+
+// Values 8 at a time of a row of queries, from anywhere.
+__device__ __forceinline__ uint4 query_piece(const KvRowsCall& a, const uint16_t* p) {
+  if (a.q16) return *(const uint4*)p;
+  uint32_t x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
+template <int KIND, int DP>
+__global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
+    rows_kernel(KvView c, KvRowsCall a, KvAttendScratch w) {
+  using S = RowsShape<KIND, DP>;
+  constexpr int kTiles = S::kTiles, kBt = S::kBt, kStages = S::kStages;
+  extern __shared__ char room_[];
+  begin_kernel();
+  char* const room = room_ + ((1024 - (smem_of(room_) & 1023)) & 1023);
+  char* const q_room = room;
+  char* const stages = q_room + kTiles * S::kQTile;
+  char* const raws = stages + kStages * S::kStage;
+  RowsShared& sh = *(RowsShared*)(raws + S::kRaws * S::kRaw);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  // ---- this CTA's share: a thread sums the costs of consecutive items, the CTA scans the threads' sums.
+  const int32_t each = (a.n + S::kThreads - 1) / S::kThreads, i0 = threadIdx.x * each;
+  int64_t mine = 0;
+  for (int32_t i = i0; i < i0 + each && i < a.n; ++i) {
+    const RowsItem it = rows_item<S>(c, a, i, blockIdx.x == 0 ? w.err : nullptr);
+    if (it.tiles) mine += c.heads * rows_cost<S>(a, it, it.tiles);
+  }
+  int64_t scan = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t y = __shfl_up_sync(~0u, scan, d);
+    if (lane >= d) scan += y;
+  }
+  if (lane == 31) sh.sums[warp] = scan;
+  __syncthreads();
+  int64_t before = scan - mine, total = 0;
+#pragma unroll
+  for (int k = 0; k < S::kThreads / 32; ++k) {
+    const int64_t y = sh.sums[k];
+    before += k < warp ? y : 0;
+    total += y;
+  }
+  // (Four at least, so that no two CTAs' shares begin at the same step inside a unit.)
+  const int64_t ctas = min((int64_t)gridDim.x, max((int64_t)1, total / 4));
+  if (total == 0 || blockIdx.x >= ctas) return;
+  const int64_t x0 = total * blockIdx.x / ctas, x1 = total * (blockIdx.x + 1) / ctas;
+  if (x0 >= before && x0 < before + mine) {
+    int32_t i = i0;
+    for (;; ++i) {
+      const RowsItem it = rows_item<S>(c, a, i, nullptr);
+      const int64_t t = it.tiles ? c.heads * rows_cost<S>(a, it, it.tiles) : 0;
+      if (x0 < before + t) break;
+      before += t;
+    }
+    sh.item = i;
+    sh.before = before;
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], 4), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
+    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], 4), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1), bar_init(sh.team[i], 4);
+    for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
+    bar_init(sh.drain, 1);
+    sh.dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == S::kSoft + 4) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(&sh.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    before_sync();
+  }
+  __syncthreads();
+  after_sync();
+  const uint32_t tmem = sh.tmem;
+  const int32_t dim16 = (c.dim + 15) / 16 * 16;
+  int32_t ring = 0;          // the unit's place, and the phase of its barriers
+  uint32_t ring_phase = 0;
+  const auto next_unit = [&]() {
+    if (++ring == kRing) ring = 0, ring_phase ^= 1;
+  };
+
+  if (warp < S::kSoft) {
+    // ================================ softmax: a thread a row
+    if (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    const int tile = warp / 4, r = (warp & 3) * 32 + lane;  // of the row tile
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;      // (tensor memory's lanes 32 * (warp % 4) .., from bit 16 on)
+    const uint32_t s_at = tmem + lanes + tile * kBt, o_at = tmem + lanes + S::kOCol + tile * DP;
+    char* const q_tile = q_room + tile * S::kQTile;
+    uint32_t s_phase = 0, o_phase = 0, team_phase = 0;
+    // The row tile's four warps meet (with the limit that all waits have).
+    const auto meet = [&]() {
+      __syncwarp();
+      if (lane == 0) bar_arrive(sh.team[tile]);
+      if (!bar_wait(sh.team[tile], team_phase, sh)) return false;
+      team_phase ^= 1;
+      return true;
+    };
+    float mul = 0.f;  // logit (in log2) of a sum of products
+    // Where row x of the unit's tile is.
+    const auto row_of_q = [&](const RowsUnit& u, int x, int64_t& row, int32_t& head) {
+      const uint32_t y = u.g0 + tile * 128 + x, t = a.by_group.div(y);
+      row = u.row + t;
+      head = u.h * a.group + (int32_t)(y - t * a.group);
+    };
+    // Queries into shared memory; a negative scale changes their signs instead, as exp's maximum is the products'.
+    const auto load_queries = [&](const RowsUnit& u) {
+      constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;  // lanes a row, rows at a time
+      const int piece = lane % kLanes;
+      float unit = fabsf(a.scale) * kLog2e * (KIND == P2P_KV_E4M3 ? fabsf(c.k_scale[a.layer * c.heads + u.h]) : 1.f);
+      const bool minus = (a.scale < 0.f) != (KIND == P2P_KV_E4M3 && c.k_scale[a.layer * c.heads + u.h] < 0.f);
+      unit = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
+      const uint32_t flip = minus ? 0x80008000u : 0;
+      mul = unit;
+      constexpr int kLoads = KIND == P2P_KV_E4M3 ? 4 : 8;
+#pragma unroll 1
+      for (int x0 = 0; x0 < 32; x0 += kAtOnce * kLoads) {
+        uint4 v[kLoads];
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+          const int x = (warp & 3) * 32 + x0 + k * kAtOnce + lane / kLanes;
+          v[k] = make_uint4(0, 0, 0, 0);
+          if (tile * 128 + x < u.rows && piece * 8 < c.dim) {
+            int64_t row;
+            int32_t head;
+            row_of_q(u, x, row, head);
+            v[k] = query_piece(a, (const uint16_t*)a.q + row * a.q_row + head * a.q_head + piece * 8);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+          const int first = x0 + k * kAtOnce, x = (warp & 3) * 32 + first + lane / kLanes;
+          uint32_t b[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+          if (KIND == P2P_KV_E4M3) {
+            // In f16, scaled by a power of two so that the row's largest is in [2^14, 2^15): exact but for what is below
+            // 2^-28 of it.
+            float f[8], largest = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 y = two_halves(b[i], a.type);
+              f[2 * i] = y.x, f[2 * i + 1] = y.y;
+              largest = fmaxf(largest, fmaxf(fabsf(y.x), fabsf(y.y)));
+            }
+#pragma unroll
+            for (int d = kLanes / 2; d; d >>= 1) largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, d));
+            const int e = largest > 0.f && largest < INFINITY ? max(ilogbf(largest), -112) - 14 : 0;
+            const float down = ldexpf(1.f, -e), of_row = ldexpf(unit, e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[i] = pack<KIND>(f[2 * i] * down, f[2 * i + 1] * down);
+            const float got = __shfl_sync(~0u, of_row, (lane - first) * kLanes & 31);
+            if (lane >= first && lane < first + kAtOnce) mul = fmaxf(got, 0x1p-120f);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) b[i] ^= flip;
+          if (piece * 8 < dim16)
+            *(uint4*)(q_tile + (piece / 8) * (128 * 128) + x * 128 + ((piece & 7) ^ (x & 7)) * 16) = make_uint4(b[0], b[1], b[2], b[3]);
+        }
+      }
+      async_fence();
+      __syncwarp();
+      if (lane == 0) bar_arrive(sh.q_full[tile]);
+    };
+    const auto run = [&]() {
+      if (!bar_wait(sh.unit_full[0], 0, sh)) return;
+      if (sh.unit[0].t1[tile] > sh.unit[0].t0[tile]) load_queries(sh.unit[0]);
+      for (;;) {
+        const RowsUnit& u = sh.unit[ring];
+        if (u.rows == 0) return;
+        const bool some = u.rows > tile * 128;
+        float top = -INFINITY;
+        uint64_t sum = 0;
+        int64_t row = 0;
+        int32_t head = 0, begin = 0, end = INT32_MAX;  // (rows past the last one mask nothing)
+        const int32_t from = u.t0[tile], to = u.t1[tile];
+        const float unit_mul = mul;
+        if (some) {
+          if (tile * 128 + r < u.rows) {
+            row_of_q(u, r, row, head);
+            if (a.spans) {
+              end = u.end;
+              if (a.window) begin = window_begin(a, length_of(c, a.seq ? a.seq[row] : (int32_t)row));
+            } else {
+              end = u.pos + (int32_t)(row - u.row) + 1;
+              begin = window_begin(a, end);
+            }
+          }
+          for (int32_t j = from; j < to; ++j) {
+            if (!bar_wait(sh.s_full[tile], s_phase, sh)) return;
+            s_phase ^= 1;
+            after_sync();
+            uint32_t x[kBt];
+#pragma unroll
+            for (int k = 0; k < kBt / 32; ++k) tmem_load(x + 32 * k, s_at + 32 * k);
+            tmem_loaded();
+            const int32_t t0 = j * kBt, lo = begin - t0, hi = end - t0;  // seen: lo .. hi - 1
+            if (__any_sync(~0u, lo > 0 || hi < kBt)) {
+#pragma unroll
+              for (int k = 0; k < kBt / 32; ++k) {
+                const int32_t l = min(max(lo - 32 * k, 0), 32), m = min(max(hi - 32 * k, 0), 32);
+                const uint32_t seen = (m >= 32 ? ~0u : (1u << m) - 1) & (l >= 32 ? 0u : ~0u << l);
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (!(seen >> i & 1)) x[32 * k + i] = 0xff800000u;
+              }
+            }
+            float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < kBt; i += 8)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) t[k] = max3(t[k], __uint_as_float(x[i + 2 * k]), __uint_as_float(x[i + 2 * k + 1]));
+            const float most = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * unit_mul;
+            if (__any_sync(~0u, most > top + (Type<KIND>::kUp + Type<KIND>::kLag))) {
+              const float now = fmaxf(most - Type<KIND>::kUp, top), fade = now == -INFINITY ? 1.f : exp2_fast(top - now);
+              top = now;
+              const float2 z = parts_of(sum);
+              sum = pair_of(z.x * fade, z.y * fade);
+              if (j > from) {
+#pragma unroll 1
+                for (int32_t d = 0; d < dim16; d += 16) {
+                  uint32_t o[16];
+                  tmem_load16(o, o_at + d);
+                  tmem_loaded();
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fade);
+                  tmem_store16(o_at + d, o);
+                }
+              }
+            }
+            const float less = top == -INFINITY ? 0.f : -top;
+            const uint64_t by = pair_of(unit_mul, unit_mul), plus = pair_of(less, less);
+#pragma unroll
+            for (int k = 0; k < kBt / 32; ++k) {
+              uint32_t p[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int y = 32 * k + 2 * i;
+                const float2 f = parts_of(fma2(pair_of(__uint_as_float(x[y]), __uint_as_float(x[y + 1])), by, plus));
+                const float e0 = exp2_fast(f.x), e1 = exp2_fast(f.y);
+                sum = add2(sum, pair_of(e0, e1));
+                p[i] = pack<KIND>(e0, e1);
+              }
+              tmem_store16(s_at + 16 * k, p);
+            }
+            tmem_stored();
+            before_sync();
+            __syncwarp();
+            if (lane == 0) bar_arrive(sh.p_full[tile]);
+          }
+        }
+        // The next unit's queries: the products with this one's are done.
+        const int32_t now = ring;
+        next_unit();
+        if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
+        if (sh.unit[ring].t1[tile] > sh.unit[ring].t0[tile]) load_queries(sh.unit[ring]);
+        if (some) {
+          if (to > from) {
+            if (!bar_wait(sh.o_full[tile], o_phase, sh)) return;
+            o_phase ^= 1;
+            after_sync();
+          }
+          const float2 z2 = parts_of(sum);
+          float z = z2.x + z2.y;
+          const bool valid = tile * 128 + r < u.rows;
+          // Values that were taken out for rows that do not see them: added to those that do.
+          const auto add_poison = [&](float* o, int32_t d) {
+            if (!sh.poison[now]) return;
+            for (int32_t p = max(begin, from * kBt); p < min(end, to * kBt); ++p) {
+              const int32_t j = p >> S::kBtLog;
+              if (!valid || !(j * kBt < u.all_begin || min((j + 1) * kBt, u.end) > u.all_end)) continue;
+              const uint32_t e = c.by_page.div(p);
+              const int32_t page = row_of(c, u.seq)[e];
+              if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
+              const char* at = c.v + a.layer * c.layer_stride + page * c.page_stride + (p - e * c.page) * c.token_stride + u.h * c.head_stride;
+              for (int i = 0; i < 32 && d + i < c.dim; ++i) {
+                const float v = KIND == P2P_KV_E4M3 ? __half2float(__nv_cvt_fp8_to_halfraw(((const uint8_t*)at)[d + i], __NV_E4M3))
+                                : KIND == P2P_KV_BF16 ? __bfloat162float(((const __nv_bfloat16*)at)[d + i])
+                                                      : __half2float(((const __half*)at)[d + i]);
+                if (!(fabsf(v) < INFINITY)) o[i] += v;
+              }
+            }
+          };
+          const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h] : 1.f;
+          // Values d .. d + 31 of the row's result: o, times f, and with the part of the row that is its own.
+          float other = 0.f, f = 0.f;
+          const auto finish = [&](float t, float sum_of) {
+            f = sum_of > 0.f || sum_of != sum_of ? v_scale / sum_of : 0.f;
+            float lse = sum_of == 0.f ? -INFINITY : log_sum<KIND>(t, sum_of);
+            if (a.own) {
+              const float his = a.own_lse[row * a.heads + head], high = fmaxf(lse, his);
+              const float p = exp2_fast((lse - high) * kLog2e), q = exp2_fast((his - high) * kLog2e);
+              const float by = __fdividef(1.f, p + q);
+              f *= p * by, other = q * by;
+              lse = high + __logf(p + q);
+            }
+            if (a.lse) a.lse[row * a.heads + head] = lse;
+          };
+          const auto put = [&](const float* o, int32_t d) {
+            uint16_t* const out = (uint16_t*)a.out + row * a.out_row + head * a.out_head + d;
+            const float* const own = a.own + (row * a.heads + head) * c.dim + d;
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              if (d + i >= c.dim) break;
+              float v[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) v[k] = o[i + k] * f;
+              if (a.own) {
+                const float4 x = *(const float4*)(own + i), y = *(const float4*)(own + i + 4);
+                v[0] = fmaf(x.x, other, v[0]), v[1] = fmaf(x.y, other, v[1]), v[2] = fmaf(x.z, other, v[2]), v[3] = fmaf(x.w, other, v[3]);
+                v[4] = fmaf(y.x, other, v[4]), v[5] = fmaf(y.y, other, v[5]), v[6] = fmaf(y.z, other, v[6]), v[7] = fmaf(y.w, other, v[7]);
+              }
+              uint32_t b[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                b[k] = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v[2 * k], v[2 * k + 1]) : pack<P2P_KV_F16>(v[2 * k], v[2 * k + 1]);
+              if (a.out16) {
+                *(uint4*)(out + i) = make_uint4(b[0], b[1], b[2], b[3]);
+              } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) out[i + k] = (uint16_t)(b[k / 2] >> (k & 1) * 16);
+              }
+            }
+          };
+          constexpr int kPart = 128 * (DP + 2);  // floats of a row tile's part: [value][row], then maxima and sums
+          if (u.parts == 1) {
+            if (valid) finish(top, z);
+#pragma unroll 1
+            for (int32_t d = 0; d < dim16; d += 32) {
+              uint32_t o[32];
+              if (to > from) {
+                tmem_load(o, o_at + d);
+                tmem_loaded();
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0;
+              }
+              add_poison((float*)o, d);
+              if (valid) put((const float*)o, d);
+            }
+          } else {
+            const auto part_of = [&](int32_t k) { return w.parts + (int64_t)((2 * (u.c0 + k) + (k == 0)) * kTiles + tile) * kPart + r; };
+            float* const part = part_of(u.part);
+#pragma unroll 1
+            for (int32_t d = 0; d < dim16; d += 32) {
+              uint32_t o[32];
+              if (to > from) {
+                tmem_load(o, o_at + d);
+                tmem_loaded();
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0;
+              }
+              add_poison((float*)o, d);
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (d + i < dim16) part[(d + i) * 128] = __uint_as_float(o[i]);
+            }
+            part[DP * 128] = top, part[(DP + 1) * 128] = z;
+            if (!meet()) return;
+            if (r == 0) {
+              int32_t* const arrived = w.arrived + u.c0 * kTiles + tile;
+              sh.last[tile] = add_acq_rel(arrived, 1) == u.parts - 1;
+              if (sh.last[tile]) *arrived = 0;  // for the next launch
+            }
+            if (!meet()) return;
+            if (sh.last[tile]) {
+              float high = -INFINITY, sums = 0.f;
+              for (int32_t k = 0; k < u.parts; ++k) high = fmaxf(high, __ldcg(part_of(k) + DP * 128));
+              const float ref = high == -INFINITY ? 0.f : high;
+              for (int32_t k = 0; k < u.parts; ++k)
+                sums += exp2_fast(__ldcg(part_of(k) + DP * 128) - ref) * __ldcg(part_of(k) + (DP + 1) * 128);
+              if (valid) finish(high, sums);
+#pragma unroll 1
+              for (int32_t d = 0; d < dim16; d += 32) {
+                float o[32] = {};
+#pragma unroll 1
+                for (int32_t k = 0; k < u.parts; ++k) {
+                  const float* const p = part_of(k);
+                  const float fade = exp2_fast(__ldcg(p + DP * 128) - ref);
+                  float v[32];
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) v[i] = d + i < dim16 ? __ldcg(p + (d + i) * 128) : 0.f;
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) o[i] = fmaf(v[i], fade, o[i]);
+                }
+                if (valid) put(o, d);
+              }
+            }
+            if (!meet()) return;  // (sh.last has been read)
+          }
+        }
+        // (Loads of tensor memory are done before the next products may write there: P of the next unit is announced later.)
+        before_sync();
+        __syncwarp();
+        if (lane == 0) bar_arrive(sh.unit_empty[now]);
+      }
+    };
+    run();
+  } else if (warp < S::kSoft + 4) {
+    // ================================ copies: a warp has a quarter of a step's tokens
+    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    constexpr int kOwn = kBt / 4;
+    const int own0 = (warp - S::kSoft) * kOwn;
+    const int64_t across = c.v - c.k;
+    int32_t stage = 0;
+    uint32_t phase = 1;   // (of `empty`: a fresh barrier's last phase counts as done)
+    int32_t told = 0;     // stages whose copies are issued and not yet announced
+    int32_t tell = 0;     // the first of them
+    const auto announce = [&]() {
+      async_fence();
+      __syncwarp();
+      if (lane == 0) bar_arrive(sh.full[tell]);
+      if (++tell == kStages) tell = 0;
+      --told;
+    };
+    // A free stage.  (What is on its way is announced first where that has to be waited for: the products may need it.)
+    const auto claim = [&]() {
+      if (!bar_try(sh.empty[stage], phase)) {
+        if (told) wait<0>();
+        while (told) announce();
+        if (!bar_wait(sh.empty[stage], phase, sh)) return false;
+      }
+      return true;
+    };
+    const auto run = [&]() {
+      for (;;) {
+        if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
+        const RowsUnit& u = sh.unit[ring];
+        if (u.rows == 0) return;
+        const int32_t j0 = u.j0, j1 = u.j1, begin = u.begin, end = u.end;
+        const char* const base = c.k + a.layer * c.layer_stride + u.h * c.head_stride;
+        const int32_t* const pages = row_of(c, u.seq);
+        // A lane has a token: where it lies (-1: nowhere, zeros).
+        const auto page_at = [&](int32_t j) {
+          const int32_t t = j * kBt + own0 + (lane & (kOwn - 1));
+          return j < j1 && t >= begin && t < end ? pages[c.by_page.div(t)] : -1;
+        };
+        int32_t page = page_at(j0);
+        for (int32_t j = j0; j < j1; ++j) {
+          const int32_t t = j * kBt + own0 + (lane & (kOwn - 1));
+          int64_t at = -1;
+          if (t >= begin && t < end) {
+            const uint32_t e = c.by_page.div(t);
+            if ((uint32_t)page < (uint32_t)c.n_pages)
+              at = page * c.page_stride + (int64_t)(t - (int32_t)e * c.page) * c.token_stride;
+            else
+              atomicOr(w.err, KV_BAD_PAGE);
+          }
+          page = page_at(j + 1);
+          if (KIND != P2P_KV_E4M3) {
+            constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;
+            const int piece = lane % kLanes;
+            for (int v = 0; v < 2; ++v) {
+              if (!claim()) return;
+              const uint32_t to = smem_of(stages) + stage * S::kStage + (piece / 8) * (kBt * 128);
+#pragma unroll
+              for (int x = 0; x < kOwn; x += kAtOnce) {
+                const int row = x + lane / kLanes;
+                const int64_t o = __shfl_sync(~0u, at, row);
+                const bool in = o >= 0 && piece < c.row16;
+                const char* from = in ? base + o + (v ? across : 0) + piece * 16 : c.k;
+                const int in_tile = own0 + row;
+                if (piece * 8 < dim16) copy16(to + in_tile * 128 + ((piece & 7) ^ (in_tile & 7)) * 16, from, in);
+              }
+              commit();
+              if (++told > 2) {
+                wait<2>();
+                announce();
+              }
+              if (++stage == kStages) stage = 0, phase ^= 1;
+            }
+          } else {
+            // 16 values a piece; widened on the way.
+            constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
+            const int piece = lane % kLanes;
+            for (int v = 0; v < 2; ++v) {
+              uint4 b[kOwn / kAtOnce];
+#pragma unroll
+              for (int x = 0; x < kOwn; x += kAtOnce) {
+                const int64_t o = __shfl_sync(~0u, at, x + lane / kLanes);
+                b[x / kAtOnce] = make_uint4(0, 0, 0, 0);
+                if (o >= 0 && piece < c.row16) b[x / kAtOnce] = __ldcg((const uint4*)(base + o + (v ? across : 0) + piece * 16));
+              }
+              if (!claim()) return;
+              char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128);
+#pragma unroll
+              for (int x = 0; x < kOwn; x += kAtOnce) {
+                const int row = own0 + x + lane / kLanes;
+                const uint4 y = b[x / kAtOnce];
+                if (piece < c.row16) {
+                  *(uint4*)(to + row * 128 + ((2 * piece & 7) ^ (row & 7)) * 16) =
+                      make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
+                  *(uint4*)(to + row * 128 + (((2 * piece & 7) + 1) ^ (row & 7)) * 16) =
+                      make_uint4(widen(y.z), widen_high(y.z), widen(y.w), widen_high(y.w));
+                }
+              }
+              ++told;
+              announce();
+              if (++stage == kStages) stage = 0, phase ^= 1;
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(sh.unit_empty[ring]);
+        next_unit();
+      }
+    };
+    run();
+    wait<0>();
+    while (told) announce();
+  } else if (warp == S::kSoft + 4) {
+    // ================================ products, by one thread
+    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (lane == 0) {
+      const uint32_t type = KIND == P2P_KV_BF16 ? 1u : 0u;
+      const uint32_t what = 1u << 4 | type << 7 | type << 10 | 8u << 24;  // sums in 32 bits, 128 rows
+      const uint32_t qk = what | (uint32_t)(kBt / 8) << 17, pv = what | 1u << 16 | (uint32_t)(dim16 / 8) << 17;
+      const uint32_t q_at = smem_of(q_room), stage_at = smem_of(stages);
+      int32_t stage = 0;
+      uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      const auto next_stage = [&]() {
+        if (++stage == kStages) stage = 0, phase ^= 1;
+      };
+      const auto logits = [&](int tile, int at_stage) {
+        const uint32_t k_at = stage_at + at_stage * S::kStage;
+        for (int k = 0; k < dim16 / 16; ++k)
+          mma_ss(tmem + tile * kBt, matrix(q_at + tile * S::kQTile + (k / 4) * (128 * 128) + (k & 3) * 32, 16),
+                 matrix(k_at + (k / 4) * (kBt * 128) + (k & 3) * 32, 16), qk, k > 0);
+        mma_done(sh.s_full[tile]);
+      };
+      const auto run = [&]() {
+        for (;;) {
+          if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
+          const RowsUnit& u = sh.unit[ring];
+          if (u.rows == 0) return;
+          const int32_t j0 = u.j0, j1 = u.j1, all_begin = u.all_begin, all_end = u.all_end, last = u.end;
+          int32_t t0[2], t1[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) t0[i] = u.t0[i], t1[i] = u.t1[i];
+          for (int i = 0; i < kTiles; ++i)
+            if (t1[i] > t0[i]) {
+              if (!bar_wait(sh.q_full[i], q_phase[i], sh)) return;
+              q_phase[i] ^= 1;
+            }
+          bar_arrive(sh.unit_empty[ring]);
+          next_unit();
+          // Stages come as K, V of each step.
+          if (!bar_wait(sh.full[stage], phase, sh)) return;
+          after_sync();
+          for (int i = 0; i < kTiles; ++i)
+            if (j0 >= t0[i] && j0 < t1[i]) logits(i, stage);
+          mma_done(sh.empty[stage]);
+          next_stage();
+          for (int32_t j = j0; j < j1; ++j) {
+            if (!bar_wait(sh.full[stage], phase, sh)) return;
+            if (j * kBt < all_begin || min((j + 1) * kBt, last) > all_end) {
+              if (!bar_wait(sh.checked[stage], phase, sh)) return;
+            }
+            const int v_stage = stage;
+            const uint32_t v_at = stage_at + v_stage * S::kStage;
+            next_stage();
+            bool next = j + 1 >= j1;  // the next step's keys are there (or there are none)
+            for (int i = 0; i < kTiles; ++i) {
+              if (j >= t0[i] && j < t1[i]) {
+                if (!bar_wait(sh.p_full[i], p_phase[i], sh)) return;
+                p_phase[i] ^= 1;
+                after_sync();
+                for (int k = 0; k < kBt / 16; ++k)
+                  mma_ts(tmem + S::kOCol + i * DP, tmem + i * kBt + 8 * k, matrix(v_at + k * 2048, kBt * 128), pv, j > t0[i] || k > 0);
+                if (j + 1 == t1[i]) mma_done(sh.o_full[i]);
+              }
+              if (j + 1 < j1 && j + 1 >= t0[i] && j + 1 < t1[i]) {
+                if (!next) {
+                  if (!bar_wait(sh.full[stage], phase, sh)) return;
+                  next = true;
+                }
+                after_sync();
+                logits(i, stage);
+              }
+            }
+            mma_done(sh.empty[v_stage]);
+            if (j + 1 < j1) {
+              if (!next && !bar_wait(sh.full[stage], phase, sh)) return;
+              mma_done(sh.empty[stage]);
+              next_stage();
+            }
+          }
+        }
+      };
+      run();
+      mma_done(sh.drain);
+      for (int i = 0; i < 1 << 20 && !bar_try(sh.drain, 0); ++i) {
+      }
+    }
+    __syncwarp();
+  } else if (warp == S::kSoft + 5) {
+    // ================================ schedule: the units of this CTA's share
+    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    int32_t i = sh.item, h = 0;
+    int64_t at = sh.before;  // where the item begins
+    RowsItem it = rows_item<S>(c, a, i, nullptr);
+    int64_t all = rows_cost<S>(a, it, it.tiles), in = x0 - at;
+    h = (int32_t)(in / all);
+    in -= h * all;
+    int64_t j = 0, past = it.tiles;  // the tile that `in` is in
+    while (past - j > 1) {
+      const int64_t mid = (j + past) >> 1;
+      if (rows_cost<S>(a, it, mid) <= in)
+        j = mid;
+      else
+        past = mid;
+    }
+    int64_t cost = rows_cost<S>(a, it, j), x = at + h * all + cost;
+    bool alive = true;
+    const auto emit = [&](const RowsUnit& u) {
+      if (!bar_wait(sh.unit_empty[ring], ring_phase ^ 1, sh)) return false;
+      if (lane == 0) {
+        sh.unit[ring] = u;
+        sh.poison[ring] = 0;
+        bar_arrive(sh.unit_full[ring]);
+      }
+      __syncwarp();
+      next_unit();
+      return true;
+    };
+    while (x < x1 && alive) {
+      const int64_t cost1 = rows_cost<S>(a, it, j + 1), width = cost1 - cost;
+      const int64_t r0 = j * S::kRowsMax, r1 = min(r0 + S::kRowsMax, it.all);
+      const RowsSpan span = rows_span(a, it, r0, r1);
+      const int32_t j0 = span.begin >> S::kBtLog, n = ((span.end - 1) >> S::kBtLog) + 1 - j0;
+      const int64_t inside = min(width, (int64_t)n + S::kSet);  // a share that begins here begins within the unit
+      const auto step = [&](int64_t y) {
+        return y <= x ? 0 : y - x >= inside ? n : (int32_t)max((int64_t)0, y - x - S::kSet);
+      };
+      const int32_t s0 = step(x0), s1 = step(x1);
+      if (s1 > s0) {
+        RowsUnit u;
+        u.row = it.row0 + r0 / a.group;
+        u.g0 = (int32_t)(r0 % a.group);
+        u.rows = (int32_t)(r1 - r0);
+        u.h = h;
+        u.seq = it.seq;
+        u.pos = it.pos + (int32_t)(r0 / a.group);
+        u.begin = span.begin, u.end = span.end, u.all_begin = span.all_begin, u.all_end = span.all_end;
+        u.j0 = j0 + s0, u.j1 = j0 + s1;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          u.t0[k] = u.t1[k] = u.j0;
+          if (k < kTiles && r0 + 128 * k < r1) {
+            const RowsSpan own = rows_span(a, it, r0 + 128 * k, min(r0 + 128 * (k + 1), r1));
+            u.t0[k] = max(u.j0, own.begin >> S::kBtLog);
+            u.t1[k] = max(u.t0[k], min(u.j1, ((own.end - 1) >> S::kBtLog) + 1));
+          }
+        }
+        u.parts = 1, u.part = 0, u.c0 = blockIdx.x;
+        if (s1 - s0 < n) {
+          // The shares that begin at x + kSet + 1 .. x + inside - 1 begin within the unit.
+          const int64_t first = ((x + S::kSet + 1) * ctas + total - 1) / total, end = ((x + inside) * ctas + total - 1) / total;
+          u.c0 = (int32_t)first - 1;
+          u.parts = (int32_t)(end - first) + 1;
+          u.part = blockIdx.x - u.c0;
+        }
+        alive = emit(u);
+      }
+      x += width;
+      cost = cost1;
+      if (++j < it.tiles) continue;
+      j = 0, cost = 0;
+      if (++h < c.heads) continue;
+      h = 0;
+      do {
+        if (++i >= a.n) break;
+        it = rows_item<S>(c, a, i, nullptr);
+      } while (it.tiles == 0);
+      if (i >= a.n) break;
+    }
+    if (alive) {
+      RowsUnit u = {};
+      emit(u);
+    }
+  } else {
+    // ================================ infinities and NaN among values that not all rows see
+    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    const int mine = (warp - S::kSoft - 6) * 32 + lane;
+    int32_t stage = 0;
+    uint32_t phase = 0;
+    const auto run = [&]() {
+      for (;;) {
+        if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
+        const RowsUnit& u = sh.unit[ring];
+        if (u.rows == 0) return;
+        for (int32_t y = 2 * u.j0; y < 2 * u.j1; ++y) {  // (keys, then values of each step)
+          const int32_t j = y >> 1;
+          if (!bar_wait(sh.full[stage], phase, sh)) return;
+          if ((y & 1) && (j * kBt < u.all_begin || min((j + 1) * kBt, u.end) > u.all_end)) {
+            constexpr uint32_t kEnd = KIND == P2P_KV_BF16 ? 0x7f80u : 0x7c00u;
+            bool found = false;
+            const int rows16 = dim16 / 8;
+            for (int z = mine; z < kBt * rows16; z += 64) {
+              const int row = z / rows16, piece = z - row * rows16;
+              uint4* const p = (uint4*)(stages + stage * S::kStage + (piece / 8) * (kBt * 128) + row * 128 + ((piece & 7) ^ (row & 7)) * 16);
+              const uint4 v = *p;
+              uint32_t b[4] = {v.x, v.y, v.z, v.w};
+              bool bad = false;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t lo = b[k] & kEnd, hi = b[k] >> 16 & kEnd;
+                if (lo == kEnd) b[k] &= 0xffff0000u, bad = true;
+                if (hi == kEnd) b[k] &= 0xffffu, bad = true;
+              }
+              if (bad) *p = make_uint4(b[0], b[1], b[2], b[3]), found = true;
+            }
+            if (found) sh.poison[ring] = 1;
+            async_fence();
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(sh.checked[stage]);
+          if (++stage == kStages) stage = 0, phase ^= 1;
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(sh.unit_empty[ring]);
+        next_unit();
+      }
+    };
+    run();
+  }
+  __syncthreads();
+  if (sh.dead && threadIdx.x == 0) atomicOr(w.err, KV_STUCK);
+  if (warp == S::kSoft + 4)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+// With a = NULL the kernel is only made ready for launches.
+template <int KIND, int DP>
+cudaError_t launch_rows(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+  using S = RowsShape<KIND, DP>;
+  const auto kernel = rows_kernel<KIND, DP>;
+  if (!a) {
+    cudaFuncAttributes got;
+    cudaError_t e = cudaFuncGetAttributes(&got, kernel);
+    // (The softmax warps take 72 registers a thread more, which the others give back: of 128 that each starts with.)
+    if (e == cudaSuccess && S::kTiles == 2 && got.numRegs != 128) e = cudaErrorInvalidDeviceFunction;
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+  }
+  return launch_early(kernel, dim3(num_sms), S::kThreads, S::kBytes, st, c, *a, w);
+}
+template <int KIND>
+cudaError_t launch_rows_dim(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+  return c.dim <= 64    ? launch_rows<KIND, 64>(c, a, w, num_sms, st)
+         : c.dim <= 128 ? launch_rows<KIND, 128>(c, a, w, num_sms, st)
+         : c.dim <= 192 ? launch_rows<KIND, 192>(c, a, w, num_sms, st)
+                        : launch_rows<KIND, 256>(c, a, w, num_sms, st);
+}
+
+}  // namespace
+}  // namespace p2p

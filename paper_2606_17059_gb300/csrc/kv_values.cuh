@@ -22,7 +22,8 @@ __device__ __forceinline__ int32_t* row_of(const KvView& c, int32_t seq) {
 }
 
 // The last item that starts at or before token t (items without tokens share a start): every lane gets it.
-__device__ __forceinline__ int32_t find_item(const int64_t* offsets, int32_t n, int64_t t) {
+template <class T>
+__device__ __forceinline__ int32_t find_item(const T* offsets, int32_t n, int64_t t) {
   const int lane = threadIdx.x & 31;
   int32_t lo = 0, hi = n;
   while (hi - lo > 1) {  // 32 probes a round
@@ -34,6 +35,13 @@ __device__ __forceinline__ int32_t find_item(const int64_t* offsets, int32_t n, 
     hi = min(hi, lo + step);
   }
   return lo;
+}
+
+// Tokens that a group of rows works off together, from what launch_kv_share found: x entries that are the same, tokens from y on
+// seen by some row.
+__device__ __forceinline__ int32_t shared_tokens(const KvView& c, int4 span, int32_t members) {
+  const int32_t tokens = span.x * c.page;
+  return members > 1 && tokens - span.y >= kSharedTokens ? tokens : 0;
 }
 
 // By all threads of a CTA: reports offsets that do not ascend or leave the batch.

@@ -192,7 +192,7 @@ def test_refusals_and_errors():
         b = {**a, **bad}
         assert lib.p2p_kv_attend_shared(c.handle, 0, 3, None, b["n_groups"], b["groups"], q.data_ptr(), 256, 64, 0, 4, 0.1, 0, q.data_ptr(), 256, 64, None,
                                         b["work"]) == g.P2P_E_INVAL
-    for bad in (dict(seq=i32([0, 99, 1])), dict(seq=i32([0, 1, -1]))):
+    for bad in (dict(seq=i32([0, 99, 1])), dict(seq=i32([0, 1, -1])), dict(groups=i32([0, 4])), dict(groups=i32([2, 1])), dict(groups=i32([-1, 2]))):
         got = c.attend_shared(0, q, bad.get("groups", groups), seq=bad.get("seq"))
         with pytest.raises(g.P2PError) as e:
             c.sync()
