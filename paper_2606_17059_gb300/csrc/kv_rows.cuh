@@ -102,8 +102,15 @@ __device__ __forceinline__ bool bar_wait(const uint64_t& bar, uint32_t parity, R
 __device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void mma_done(const uint64_t& bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_of(&bar))
+// (The products' warp runs together and one of its threads issues: operands stay in uniform registers that way.)
+__device__ __forceinline__ uint32_t elected() {
+  uint32_t x;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.b32 %0, 1, 0, p; }" : "=r"(x));
+  return x;
+}
+__device__ __forceinline__ void mma_done(const uint64_t& bar, uint32_t one) {
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %1, 0;\n"
+               "@p tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(smem_of(&bar)), "r"(one)
                : "memory");
 }
 // A matrix in shared memory, rows of 128 bytes turned within eights of them; lead: bytes between chunks of 64 values, for an
@@ -111,14 +118,14 @@ __device__ __forceinline__ void mma_done(const uint64_t& bar) {
 __device__ __forceinline__ uint64_t matrix(uint32_t at, uint32_t lead) {
   return (uint64_t)((at & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
-               "l"(a), "l"(b), "r"(what), "r"((uint32_t)add)
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, uint32_t add, uint32_t one) {
+  asm volatile("{ .reg .pred p, q; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %5, 0;\n"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(what), "r"(add), "r"(one)
                : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
-               "r"(a), "l"(b), "r"(what), "r"((uint32_t)add)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, uint32_t add, uint32_t one) {
+  asm volatile("{ .reg .pred p, q; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %5, 0;\n"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(what), "r"(add), "r"(one)
                : "memory");
 }
 #define P2P_R8(r, o) "=r"((r)[o]), "=r"((r)[o + 1]), "=r"((r)[o + 2]), "=r"((r)[o + 3]), "=r"((r)[o + 4]), "=r"((r)[o + 5]), \
@@ -303,7 +310,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     sh.before = before;
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], 4), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
+    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
     for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], 4), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1), bar_init(sh.team[i], 4);
     for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
     bar_init(sh.drain, 1);
@@ -648,24 +655,6 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     const int64_t across = c.v - c.k;
     int32_t stage = 0;
     uint32_t phase = 1;   // (of `empty`: a fresh barrier's last phase counts as done)
-    int32_t told = 0;     // stages whose copies are issued and not yet announced
-    int32_t tell = 0;     // the first of them
-    const auto announce = [&]() {
-      async_fence();
-      __syncwarp();
-      if (lane == 0) bar_arrive(sh.full[tell]);
-      if (++tell == kStages) tell = 0;
-      --told;
-    };
-    // A free stage.  (What is on its way is announced first where that has to be waited for: the products may need it.)
-    const auto claim = [&]() {
-      if (!bar_try(sh.empty[stage], phase)) {
-        if (told) wait<0>();
-        while (told) announce();
-        if (!bar_wait(sh.empty[stage], phase, sh)) return false;
-      }
-      return true;
-    };
     const auto run = [&]() {
       for (;;) {
         if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
@@ -695,7 +684,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;
             const int piece = lane % kLanes;
             for (int v = 0; v < 2; ++v) {
-              if (!claim()) return;
+              if (!bar_wait(sh.empty[stage], phase, sh)) return;
               const uint32_t to = smem_of(stages) + stage * S::kStage + (piece / 8) * (kBt * 128);
 #pragma unroll
               for (int x = 0; x < kOwn; x += kAtOnce) {
@@ -706,11 +695,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
                 const int in_tile = own0 + row;
                 if (piece * 8 < dim16) copy16(to + in_tile * 128 + ((piece & 7) ^ (in_tile & 7)) * 16, from, in);
               }
-              commit();
-              if (++told > 2) {
-                wait<2>();
-                announce();
-              }
+              // (Arrives when the thread's copies have; whoever reads them through another path fences after it has waited.)
+              asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_of(&sh.full[stage])) : "memory");
               if (++stage == kStages) stage = 0, phase ^= 1;
             }
           } else {
@@ -725,7 +711,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
                 b[x / kAtOnce] = make_uint4(0, 0, 0, 0);
                 if (o >= 0 && piece < c.row16) b[x / kAtOnce] = __ldcg((const uint4*)(base + o + (v ? across : 0) + piece * 16));
               }
-              if (!claim()) return;
+              if (!bar_wait(sh.empty[stage], phase, sh)) return;
               char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128);
 #pragma unroll
               for (int x = 0; x < kOwn; x += kAtOnce) {
@@ -738,8 +724,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
                       make_uint4(widen(y.z), widen_high(y.z), widen(y.w), widen_high(y.w));
                 }
               }
-              ++told;
-              announce();
+              async_fence();
+              bar_arrive(sh.full[stage]);
               if (++stage == kStages) stage = 0, phase ^= 1;
             }
           }
@@ -750,12 +736,12 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       }
     };
     run();
-    wait<0>();
-    while (told) announce();
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == S::kSoft + 4) {
-    // ================================ products, by one thread
+    // ================================ products
     if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (lane == 0) {
+    {
+      const uint32_t one = elected();
       const uint32_t type = KIND == P2P_KV_BF16 ? 1u : 0u;
       const uint32_t what = 1u << 4 | type << 7 | type << 10 | 8u << 24;  // sums in 32 bits, 128 rows
       const uint32_t qk = what | (uint32_t)(kBt / 8) << 17, pv = what | 1u << 16 | (uint32_t)(dim16 / 8) << 17;
@@ -766,11 +752,13 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         if (++stage == kStages) stage = 0, phase ^= 1;
       };
       const auto logits = [&](int tile, int at_stage) {
-        const uint32_t k_at = stage_at + at_stage * S::kStage;
-        for (int k = 0; k < dim16 / 16; ++k)
-          mma_ss(tmem + tile * kBt, matrix(q_at + tile * S::kQTile + (k / 4) * (128 * 128) + (k & 3) * 32, 16),
-                 matrix(k_at + (k / 4) * (kBt * 128) + (k & 3) * 32, 16), qk, k > 0);
-        mma_done(sh.s_full[tile]);
+        const uint64_t q0 = matrix(q_at + tile * S::kQTile, 16), k0 = matrix(stage_at + at_stage * S::kStage, 16);
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+          if (k * 16 < dim16)
+            mma_ss(tmem + tile * kBt, q0 + ((k / 4) * (128 * 128) + (k & 3) * 32) / 16,
+                   k0 + ((k / 4) * (kBt * 128) + (k & 3) * 32) / 16, qk, k > 0, one);
+        mma_done(sh.s_full[tile], one);
       };
       const auto run = [&]() {
         for (;;) {
@@ -781,58 +769,64 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           int32_t t0[2], t1[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) t0[i] = u.t0[i], t1[i] = u.t1[i];
+#pragma unroll
           for (int i = 0; i < kTiles; ++i)
             if (t1[i] > t0[i]) {
               if (!bar_wait(sh.q_full[i], q_phase[i], sh)) return;
               q_phase[i] ^= 1;
             }
-          bar_arrive(sh.unit_empty[ring]);
+          if (one) bar_arrive(sh.unit_empty[ring]);
           next_unit();
           // Stages come as K, V of each step.
           if (!bar_wait(sh.full[stage], phase, sh)) return;
-          after_sync();
+          async_fence();
+#pragma unroll
           for (int i = 0; i < kTiles; ++i)
             if (j0 >= t0[i] && j0 < t1[i]) logits(i, stage);
-          mma_done(sh.empty[stage]);
+          mma_done(sh.empty[stage], one);
           next_stage();
           for (int32_t j = j0; j < j1; ++j) {
             if (!bar_wait(sh.full[stage], phase, sh)) return;
             if (j * kBt < all_begin || min((j + 1) * kBt, last) > all_end) {
               if (!bar_wait(sh.checked[stage], phase, sh)) return;
             }
+            async_fence();
             const int v_stage = stage;
             const uint32_t v_at = stage_at + v_stage * S::kStage;
             next_stage();
             bool next = j + 1 >= j1;  // the next step's keys are there (or there are none)
-            for (int i = 0; i < kTiles; ++i) {
+  #pragma unroll
+          for (int i = 0; i < kTiles; ++i) {
               if (j >= t0[i] && j < t1[i]) {
                 if (!bar_wait(sh.p_full[i], p_phase[i], sh)) return;
                 p_phase[i] ^= 1;
                 after_sync();
+                const uint64_t v0 = matrix(v_at, kBt * 128);
+#pragma unroll
                 for (int k = 0; k < kBt / 16; ++k)
-                  mma_ts(tmem + S::kOCol + i * DP, tmem + i * kBt + 8 * k, matrix(v_at + k * 2048, kBt * 128), pv, j > t0[i] || k > 0);
-                if (j + 1 == t1[i]) mma_done(sh.o_full[i]);
+                  mma_ts(tmem + S::kOCol + i * DP, tmem + i * kBt + 8 * k, v0 + k * (2048 / 16), pv, j > t0[i] || k > 0, one);
+                if (j + 1 == t1[i]) mma_done(sh.o_full[i], one);
               }
               if (j + 1 < j1 && j + 1 >= t0[i] && j + 1 < t1[i]) {
                 if (!next) {
                   if (!bar_wait(sh.full[stage], phase, sh)) return;
+                  async_fence();
                   next = true;
                 }
-                after_sync();
                 logits(i, stage);
               }
             }
-            mma_done(sh.empty[v_stage]);
+            mma_done(sh.empty[v_stage], one);
             if (j + 1 < j1) {
               if (!next && !bar_wait(sh.full[stage], phase, sh)) return;
-              mma_done(sh.empty[stage]);
+              mma_done(sh.empty[stage], one);
               next_stage();
             }
           }
         }
       };
       run();
-      mma_done(sh.drain);
+      mma_done(sh.drain, one);
       for (int i = 0; i < 1 << 20 && !bar_try(sh.drain, 0); ++i) {
       }
     }
