@@ -1,5 +1,6 @@
 // kv.h -- the paged key-value cache (p2p_kv_* of p2p_router.h): what its host code and its kernels share.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -224,17 +225,24 @@ struct KvRowsCall {
   float scale;
   bool q16, out16;  // whether rows of q (of out) lie on 16-byte boundaries
 };
+// The pages as tensors [layer][page][head][token][value] for copies of `rows` tokens of one head and page at a time, 16-bit
+// values 64 at a time (128 bytes, turned as the tensor cores want them), 8-bit ones whole rows; rows 0: not to be had
+// (pages that are not whole eights of tokens).
+struct KvMaps {
+  CUtensorMap k, v;
+  int32_t rows;
+};
 // Floats of KvAttendScratch::parts: two parts a CTA, of 256 or (head_dim above 128) 128 rows.
 inline size_t kv_rows_parts(const KvView& c, int num_sms) {
   const int dp = (c.dim + 63) / 64 * 64;
   return (size_t)2 * num_sms * (dp <= 128 ? 256 : 128) * (dp + 2);
 }
 // With a = NULL they launch nothing, but make the cache's kernel ready for launches (at creation).
-cudaError_t launch_kv_rows_bf16(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+cudaError_t launch_kv_rows_bf16(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
                                 cudaStream_t st);
-cudaError_t launch_kv_rows_f16(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+cudaError_t launch_kv_rows_f16(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
                                cudaStream_t st);
-cudaError_t launch_kv_rows_e4m3(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+cudaError_t launch_kv_rows_e4m3(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
                                 cudaStream_t st);
 
 }  // namespace p2p

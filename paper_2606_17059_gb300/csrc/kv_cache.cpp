@@ -18,12 +18,13 @@ struct p2p_kv {
   p2p::KvView c = {};
   p2p::KvScratch s = {};
   p2p::KvAttendScratch w = {};
+  p2p::KvMaps maps = {};
   void* scratch = nullptr;             // one allocation: s's arrays and d_stats
   unsigned long long* d_stats = nullptr;
   int device = 0, num_sms = 0;
   cudaStream_t stream = nullptr;
   int64_t launches = 0;
-  char err[256] = {};
+  char err[320] = {};
 };
 
 namespace {
@@ -138,12 +139,45 @@ cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p
   return (c.side != 0 && (c.lines || many) ? side_by_side : alone)(c, q, w, num_sms, st);
 }
 
-cudaError_t launch_rows(const p2p::KvView& c, const p2p::KvRowsCall* a, const p2p::KvAttendScratch& w, int num_sms,
+// The pages as tensors for copies by the tensor memory accelerator, where they are to be had.
+void make_maps(const p2p::KvView& c, p2p::KvMaps& m) {
+  m.rows = 0;
+  const bool eight = c.type == P2P_KV_E4M3;
+  // Tokens of a copy: a power of two that divides a page (and so lies in one), at most what a warp, or a step, takes.
+  uint32_t rows = c.page & -c.page;
+  rows = std::min(rows, eight ? (c.dim > 128 ? 16u : 32u) : (c.dim > 128 ? 64u : 128u));
+  if (rows < 8) return;
+  void* entry = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+      found != cudaDriverEntryPointSuccess || !entry) {
+    (void)cudaGetLastError();
+    return;
+  }
+  const cuuint64_t size[5] = {(cuuint64_t)c.dim, (cuuint64_t)c.page, (cuuint64_t)c.heads, (cuuint64_t)c.n_pages,
+                              (cuuint64_t)c.n_layers};
+  cuuint64_t stride[4] = {(cuuint64_t)c.token_stride, (cuuint64_t)c.head_stride, (cuuint64_t)c.page_stride,
+                          (cuuint64_t)c.layer_stride};
+  for (int i = 0; i < 4; ++i) {
+    if (size[i + 1] == 1) stride[i] = 16;  // (whatever the caller gave: it is not used)
+    if (stride[i] >= (cuuint64_t)1 << 40) return;
+  }
+  const cuuint32_t box[5] = {eight ? (cuuint32_t)c.dim : 64, rows, 1, 1, 1}, step[5] = {1, 1, 1, 1, 1};
+  const auto make = [&](CUtensorMap* map, void* at) {
+    return ((decltype(&cuTensorMapEncodeTiled))entry)(
+               map, eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, at, size, stride, box, step,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, eight ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (make(&m.k, c.k) && make(&m.v, c.v)) m.rows = (int32_t)rows;
+}
+
+cudaError_t launch_rows(const p2p::KvView& c, const p2p::KvMaps& m, const p2p::KvRowsCall* a, const p2p::KvAttendScratch& w, int num_sms,
                         cudaStream_t st) {
   using namespace p2p;
   return (c.type == P2P_KV_BF16  ? launch_kv_rows_bf16
           : c.type == P2P_KV_F16 ? launch_kv_rows_f16
-                                 : launch_kv_rows_e4m3)(c, a, w, num_sms, st);
+                                 : launch_kv_rows_e4m3)(c, m, a, w, num_sms, st);
 }
 
 // Scratch comes from a memory pool of the library's for each device, which keeps what destroyed handles give back: a
@@ -231,7 +265,7 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   if (e == cudaSuccess) e = cudaMemsetAsync(n->scratch, 0, zero, nullptr);
   if (e == cudaSuccess) e = p2p::prepare_kv_pages();
   if (e == cudaSuccess) e = launch_attend(c, nullptr, n->w, sms, nullptr);
-  if (e == cudaSuccess) e = launch_rows(c, nullptr, n->w, sms, nullptr);
+  if (e == cudaSuccess) e = launch_rows(c, n->maps, nullptr, n->w, sms, nullptr);
   // (calls may go to a stream that does not wait for this one)
   if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
   if (e != cudaSuccess) {
@@ -256,6 +290,7 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   n->w.parts = (float*)(p + parts);
   n->w.arrived = (int32_t*)(p + arrived);
   n->w.err = n->s.err;
+  make_maps(c, n->maps);
   *out = n;
   return P2P_OK;
 }
@@ -288,7 +323,7 @@ int p2p_kv_sync(p2p_kv* h) {
   CK(cudaStreamSynchronize(h->stream));
   const int b = word[0];
   if (b == p2p::KV_NO_PAGES) return fail(h, P2P_E_NOMEM, "the pool has too few free pages");
-  char m[256];
+  char m[320];
   const auto say = [b](int bit, const char* what) { return b & bit ? what : ""; };
   std::snprintf(m, sizeof(m), "device reported:%s%s%s%s%s%s%s",
                 say(p2p::KV_BAD_SEQ, " a sequence out of range or named twice;"),
@@ -503,7 +538,7 @@ int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   a.offsets = offsets;
   a.n_tokens = n_tokens;
   a.n = n;
-  CK(launch_rows(h->c, &a, h->w, h->num_sms, h->stream));
+  CK(launch_rows(h->c, h->maps, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;
 }
@@ -559,7 +594,7 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   a.own_lse = own_lse;
   a.n_tokens = n;
   a.n = n_groups;
-  CK(launch_rows(h->c, &a, h->w, h->num_sms, h->stream));
+  CK(launch_rows(h->c, h->maps, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;
 }

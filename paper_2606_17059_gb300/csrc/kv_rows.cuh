@@ -34,7 +34,7 @@ struct RowsShape {
   static constexpr int kQTile = 128 * DP * 2;
   static constexpr int kStage = kBt * DP * 2;          // keys or values of a step, 16 bits each
   static constexpr int kRaw = KIND == P2P_KV_E4M3 ? kBt * DP : 0;  // the same in 8 bits, on its way
-  static constexpr int kRaws = 0;
+  static constexpr int kRaws = 2;
   static constexpr int kMisc = 2048;
   static constexpr int kFit = (232448 - 1024 - kMisc - kTiles * kQTile - kRaws * kRaw) / kStage;
   static constexpr int kStages = kFit < 8 ? kFit : 8;
@@ -61,7 +61,7 @@ struct RowsUnit {
   int32_t parts, part, c0;   // of the unit, where it is shared: this piece's number and the first one's CTA
 };
 struct RowsShared {
-  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], team[2], drain;
+  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], team[2], drain, raw[4][2];
   RowsUnit unit[kRing];
   int64_t sums[16];
   int64_t before, total;
@@ -98,6 +98,16 @@ __device__ __forceinline__ bool bar_wait_long(const uint64_t& bar, uint32_t pari
 }
 __device__ __forceinline__ bool bar_wait(const uint64_t& bar, uint32_t parity, RowsShared& sh) {
   return bar_try(bar, parity) || bar_wait_long(bar, parity, sh);
+}
+// The next phase also takes so many bytes of copies.
+__device__ __forceinline__ void bar_expect(const uint64_t& bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_of(&bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, int32_t x, int32_t token, int32_t head, int32_t page,
+                                         int32_t layer, const uint64_t& bar) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, "
+               "%6}], [%7];" ::"r"(to), "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(layer), "r"(smem_of(&bar))
+               : "memory");
 }
 __device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -260,7 +270,7 @@ __device__ __forceinline__ uint4 query_piece(const KvRowsCall& a, const uint16_t
 
 template <int KIND, int DP>
 __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
-    rows_kernel(KvView c, KvRowsCall a, KvAttendScratch w) {
+    rows_kernel(KvView c, const __grid_constant__ KvMaps maps, KvRowsCall a, KvAttendScratch w) {
   using S = RowsShape<KIND, DP>;
   constexpr int kTiles = S::kTiles, kBt = S::kBt, kStages = S::kStages;
   extern __shared__ char room_[];
@@ -310,9 +320,10 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     sh.before = before;
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
+    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 1 : 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
     for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], 4), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1), bar_init(sh.team[i], 4);
     for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
+    for (int i = 0; i < 8; ++i) bar_init(sh.raw[i / 2][i & 1], 1);
     bar_init(sh.drain, 1);
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -518,7 +529,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (!sh.poison[now]) return;
             for (int32_t p = max(begin, from * kBt); p < min(end, to * kBt); ++p) {
               const int32_t j = p >> S::kBtLog;
-              if (!valid || !(j * kBt < u.all_begin || min((j + 1) * kBt, u.end) > u.all_end)) continue;
+              if (!valid || !(j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) continue;
               const uint32_t e = c.by_page.div(p);
               const int32_t page = row_of(c, u.seq)[e];
               if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
@@ -655,6 +666,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     const int64_t across = c.v - c.k;
     int32_t stage = 0;
     uint32_t phase = 1;   // (of `empty`: a fresh barrier's last phase counts as done)
+    uint32_t raw_phase = 0;
     const auto run = [&]() {
       for (;;) {
         if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
@@ -663,6 +675,110 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         const int32_t j0 = u.j0, j1 = u.j1, begin = u.begin, end = u.end;
         const char* const base = c.k + a.layer * c.layer_stride + u.h * c.head_stride;
         const int32_t* const pages = row_of(c, u.seq);
+        if (KIND != P2P_KV_E4M3 && maps.rows) {
+          // By the tensor memory accelerator, from one warp: a lane has a box of tokens.
+          if (warp == S::kSoft) {
+            const int32_t size = maps.rows, boxes = kBt / size, chunks = (dim16 + 63) / 64;
+            const auto page_of = [&](int32_t j) {
+              const int32_t t = j * kBt + lane * size;
+              return lane < boxes && j < j1 && t < end && t + size > begin ? pages[c.by_page.div(t)] : -1;
+            };
+            int32_t page = page_of(j0);
+            for (int32_t j = j0; j < j1; ++j) {
+              const int32_t t = j * kBt + lane * size;
+              const bool needed = lane < boxes && t < end && t + size > begin, there = needed && (uint32_t)page < (uint32_t)c.n_pages;
+              if (needed && !there) atomicOr(w.err, KV_BAD_PAGE);
+              const uint32_t boxes_there = __popc(__ballot_sync(~0u, there)), holes = __ballot_sync(~0u, needed && !there);
+              const int32_t in_page = t - (int32_t)c.by_page.div(max(t, 0)) * c.page, this_page = page;
+              page = page_of(j + 1);
+#pragma unroll
+              for (int v = 0; v < 2; ++v) {
+                if (!bar_wait(sh.empty[stage], phase, sh)) return;
+                char* const to = stages + stage * S::kStage;
+                for (uint32_t left = holes; left; left &= left - 1) {  // zeros in the place of pages that are out of range
+                  const int box = __ffs(left) - 1;
+                  for (int y = lane; y < size * chunks * 8; y += 32)
+                    *(uint4*)(to + y / (size * 8) * (kBt * 128) + box * size * 128 + y % (size * 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                if (holes) async_fence();
+                __syncwarp();
+                if (lane == 0) bar_expect(sh.full[stage], boxes_there * size * 128 * chunks);
+                __syncwarp();
+                if (there)
+                  for (int x = 0; x < chunks; ++x)
+                    copy_box(smem_of(to) + x * (kBt * 128) + lane * size * 128, v ? &maps.v : &maps.k, x * 64, in_page, u.h, this_page,
+                             a.layer, sh.full[stage]);
+                if (++stage == kStages) stage = 0, phase ^= 1;
+              }
+            }
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(sh.unit_empty[ring]);
+          next_unit();
+          continue;
+        }
+        if (KIND == P2P_KV_E4M3 && maps.rows) {
+          // The same in 8 bits into room of the warp's own, a step ahead; widened from there.
+          constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
+          const int piece = lane % kLanes;
+          const int32_t size = maps.rows, boxes = kOwn / size;
+          char* const raw = raws + (warp - S::kSoft) * (S::kRaw / 4);
+          const auto page_of = [&](int32_t j) {
+            const int32_t t = j * kBt + own0 + lane * size;
+            return lane < boxes && j < j1 && t < end && t + size > begin ? pages[c.by_page.div(t)] : -1;
+          };
+          const auto fetch = [&](int32_t j, int32_t page, int v) {  // which boxes there are
+            const int32_t t = j * kBt + own0 + lane * size;
+            const bool needed = lane < boxes && j < j1 && t < end && t + size > begin, there = needed && (uint32_t)page < (uint32_t)c.n_pages;
+            if (needed && !there) atomicOr(w.err, KV_BAD_PAGE);
+            const uint32_t which = __ballot_sync(~0u, there);
+            if (j < j1) {
+              if (lane == 0) bar_expect(sh.raw[warp - S::kSoft][v], __popc(which) * size * c.dim);
+              __syncwarp();
+              if (there)
+                copy_box(smem_of(raw) + v * S::kRaw + lane * size * c.dim, v ? &maps.v : &maps.k, 0,
+                         t - (int32_t)c.by_page.div(t) * c.page, u.h, page, a.layer, sh.raw[warp - S::kSoft][v]);
+            }
+            return which;
+          };
+          int32_t page = page_of(j0);
+          uint32_t here = fetch(j0, page, 0);
+          fetch(j0, page, 1);
+          page = page_of(j0 + 1);
+          for (int32_t j = j0; j < j1; ++j) {
+            uint32_t later = 0;
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              if (!bar_wait(sh.raw[warp - S::kSoft][v], raw_phase, sh) || !bar_wait(sh.empty[stage], phase, sh)) return;
+              char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128);
+#pragma unroll
+              for (int x = 0; x < kOwn; x += kAtOnce) {
+                const int row = x + lane / kLanes, in_tile = own0 + row, t = j * kBt + in_tile;
+                uint4 y = make_uint4(0, 0, 0, 0);
+                if (piece < c.row16 && t >= begin && t < end && (here >> row / size & 1))
+                  y = *(const uint4*)(raw + v * S::kRaw + row * c.dim + piece * 16);
+                if (piece < c.row16) {
+                  *(uint4*)(to + in_tile * 128 + ((2 * piece & 7) ^ (in_tile & 7)) * 16) =
+                      make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
+                  *(uint4*)(to + in_tile * 128 + (((2 * piece & 7) + 1) ^ (in_tile & 7)) * 16) =
+                      make_uint4(widen(y.z), widen_high(y.z), widen(y.w), widen_high(y.w));
+                }
+              }
+              async_fence();
+              bar_arrive(sh.full[stage]);
+              if (++stage == kStages) stage = 0, phase ^= 1;
+              __syncwarp();
+              later = fetch(j + 1, page, v);
+            }
+            here = later;
+            page = page_of(j + 2);
+            raw_phase ^= 1;
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(sh.unit_empty[ring]);
+          next_unit();
+          continue;
+        }
         // A lane has a token: where it lies (-1: nowhere, zeros).
         const auto page_at = [&](int32_t j) {
           const int32_t t = j * kBt + own0 + (lane & (kOwn - 1));
@@ -737,6 +853,14 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     };
     run();
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (*(volatile int32_t*)&sh.dead) {  // (copies that are still on their way, waited for with a limit)
+      for (int i = 0; i < kStages; ++i)
+        for (int x = 0; x < 1 << 16 && !bar_try(sh.full[i], i < stage ? phase ^ 1 : phase); ++x) {
+        }
+      for (int v = 0; v < 2; ++v)
+        for (int x = 0; x < 1 << 16 && !bar_try(sh.raw[warp - S::kSoft][v], raw_phase); ++x) {
+        }
+    }
   } else if (warp == S::kSoft + 4) {
     // ================================ products
     if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -765,7 +889,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
           const RowsUnit& u = sh.unit[ring];
           if (u.rows == 0) return;
-          const int32_t j0 = u.j0, j1 = u.j1, all_begin = u.all_begin, all_end = u.all_end, last = u.end;
+          const int32_t j0 = u.j0, j1 = u.j1, all_begin = u.all_begin, all_end = u.all_end;
           int32_t t0[2], t1[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) t0[i] = u.t0[i], t1[i] = u.t1[i];
@@ -787,9 +911,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           next_stage();
           for (int32_t j = j0; j < j1; ++j) {
             if (!bar_wait(sh.full[stage], phase, sh)) return;
-            if (j * kBt < all_begin || min((j + 1) * kBt, last) > all_end) {
-              if (!bar_wait(sh.checked[stage], phase, sh)) return;
-            }
+            if ((j * kBt < all_begin || (j + 1) * kBt > all_end) && !bar_wait(sh.checked[stage], phase, sh)) return;
             async_fence();
             const int v_stage = stage;
             const uint32_t v_at = stage_at + v_stage * S::kStage;
@@ -930,13 +1052,17 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         for (int32_t y = 2 * u.j0; y < 2 * u.j1; ++y) {  // (keys, then values of each step)
           const int32_t j = y >> 1;
           if (!bar_wait(sh.full[stage], phase, sh)) return;
-          if ((y & 1) && (j * kBt < u.all_begin || min((j + 1) * kBt, u.end) > u.all_end)) {
+          if ((y & 1) && (j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) {
             constexpr uint32_t kEnd = KIND == P2P_KV_BF16 ? 0x7f80u : 0x7c00u;
             bool found = false;
             const int rows16 = dim16 / 8;
             for (int z = mine; z < kBt * rows16; z += 64) {
               const int row = z / rows16, piece = z - row * rows16;
               uint4* const p = (uint4*)(stages + stage * S::kStage + (piece / 8) * (kBt * 128) + row * 128 + ((piece & 7) ^ (row & 7)) * 16);
+              if (j * kBt + row < u.begin || j * kBt + row >= u.end) {  // (nobody's: whatever lies there)
+                *p = make_uint4(0, 0, 0, 0);
+                continue;
+              }
               const uint4 v = *p;
               uint32_t b[4] = {v.x, v.y, v.z, v.w};
               bool bad = false;
@@ -970,7 +1096,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 
 // With a = NULL the kernel is only made ready for launches.
 template <int KIND, int DP>
-cudaError_t launch_rows(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+cudaError_t launch_rows(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   using S = RowsShape<KIND, DP>;
   const auto kernel = rows_kernel<KIND, DP>;
   if (!a) {
@@ -980,14 +1106,15 @@ cudaError_t launch_rows(const KvView& c, const KvRowsCall* a, const KvAttendScra
     if (e == cudaSuccess && S::kTiles == 2 && got.numRegs != 128) e = cudaErrorInvalidDeviceFunction;
     return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
   }
-  return launch_early(kernel, dim3(num_sms), S::kThreads, S::kBytes, st, c, *a, w);
+  return launch_early(kernel, dim3(num_sms), S::kThreads, S::kBytes, st, c, m, *a, w);
 }
 template <int KIND>
-cudaError_t launch_rows_dim(const KvView& c, const KvRowsCall* a, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  return c.dim <= 64    ? launch_rows<KIND, 64>(c, a, w, num_sms, st)
-         : c.dim <= 128 ? launch_rows<KIND, 128>(c, a, w, num_sms, st)
-         : c.dim <= 192 ? launch_rows<KIND, 192>(c, a, w, num_sms, st)
-                        : launch_rows<KIND, 256>(c, a, w, num_sms, st);
+cudaError_t launch_rows_dim(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+                            cudaStream_t st) {
+  return c.dim <= 64    ? launch_rows<KIND, 64>(c, m, a, w, num_sms, st)
+         : c.dim <= 128 ? launch_rows<KIND, 128>(c, m, a, w, num_sms, st)
+         : c.dim <= 192 ? launch_rows<KIND, 192>(c, m, a, w, num_sms, st)
+                        : launch_rows<KIND, 256>(c, m, a, w, num_sms, st);
 }
 
 }  // namespace
