@@ -223,7 +223,7 @@ struct KvRowsCall {
   int32_t n, heads, group, type, window, layer;  // group: query heads a kv head
   FastDiv by_group;
   float scale;
-  bool q16, out16;  // whether rows of q (of out) lie on 16-byte boundaries
+  bool q16, out32;  // whether rows of q lie on 16-byte boundaries, and those of out on 32-byte ones
 };
 // The pages as tensors [layer][page][head][token][value] for copies of `rows` tokens of one head and page at a time, 16-bit
 // values 64 at a time (128 bytes, turned as the tensor cores want them), 8-bit ones whole rows; rows 0: not to be had

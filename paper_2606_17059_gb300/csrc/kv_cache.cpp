@@ -518,7 +518,7 @@ static p2p::KvRowsCall rows_call(const p2p_kv* h, int32_t layer, const int32_t* 
   a.heads = n_heads, a.group = n_heads / h->c.heads, a.type = type, a.window = window, a.layer = layer, a.scale = scale;
   a.by_group = p2p::FastDiv((uint32_t)a.group);
   a.q16 = (uintptr_t)q % 16 == 0 && q_row % 8 == 0 && q_head % 8 == 0;
-  a.out16 = (uintptr_t)out % 16 == 0 && out_row % 8 == 0 && out_head % 8 == 0;
+  a.out32 = (uintptr_t)out % 32 == 0 && out_row % 16 == 0 && out_head % 16 == 0;
   return a;
 }
 

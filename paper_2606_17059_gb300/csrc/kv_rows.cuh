@@ -230,33 +230,48 @@ __device__ __forceinline__ RowsItem rows_item(const KvView& c, const KvRowsCall&
   r.tiles = (int32_t)((r.all + S::kRowsMax - 1) / S::kRowsMax);
   return r;
 }
-// Tokens that rows r0 .. r1 - 1 of an item see: any of them, and each of them.
-struct RowsSpan {
-  int32_t begin, end, all_begin, all_end;
-};
 __device__ __forceinline__ int32_t window_begin(const KvRowsCall& a, int32_t end) {
   return a.window && end > a.window ? end - a.window : 0;
 }
-__device__ __forceinline__ RowsSpan rows_span(const KvRowsCall& a, const RowsItem& it, int64_t r0, int64_t r1) {
-  if (a.spans) {
-    return {it.first, it.shared, it.pos, it.shared};
-  }
-  const int32_t e0 = it.pos + (int32_t)(r0 / a.group) + 1, e1 = it.pos + (int32_t)((r1 - 1) / a.group) + 1;
+// Tokens that some rows of an item see, the first of which are of its member (token) t0, the last of t1: any of the rows,
+// and each of them.
+struct RowsSpan {
+  int32_t begin, end, all_begin, all_end;
+};
+__device__ __forceinline__ RowsSpan rows_span(const KvRowsCall& a, const RowsItem& it, int32_t t0, int32_t t1) {
+  if (a.spans) return {it.first, it.shared, it.pos, it.shared};
+  const int32_t e0 = it.pos + t0 + 1, e1 = it.pos + t1 + 1;
   return {window_begin(a, e0), e1, window_begin(a, e1), e0};
 }
 // What the first j tiles of an item count for, each kSet for itself and about its steps: any rising function would do, as
 // long as all CTAs take the same.
 template <class S>
-__device__ __forceinline__ int64_t rows_cost(const KvRowsCall& a, const RowsItem& it, int64_t j) {
-  if (a.spans) return j * (((it.shared - 1) >> S::kBtLog) - (it.first >> S::kBtLog) + 1 + S::kSet);
-  const int64_t per = (int64_t)a.group << S::kBtLog;  // a tile's rows are kRowsMax / per of a step
-  const int64_t base = (it.pos >> S::kBtLog) + 1 + S::kSet;
-  int64_t rising = j, most = 0;
-  if (a.window) {
-    most = a.window / S::kBt + S::kRowsMax / per + 2;
-    rising = max((int64_t)0, min(j, ((most + S::kSet - base) * per) / S::kRowsMax));
+struct RowsCost {
+  int64_t base, most;  // steps of the first tile, and at most (with a window)
+  int64_t slope;       // by how much (in 256ths) each tile has more than the one before
+  int64_t rising;      // tiles before those that have most
+  __device__ __forceinline__ RowsCost(const KvRowsCall& a, const RowsItem& it) {
+    most = 0, rising = INT64_MAX;
+    if (a.spans) {
+      base = ((it.shared - 1) >> S::kBtLog) - (it.first >> S::kBtLog) + 1 + S::kSet;
+      slope = 0;
+      return;
+    }
+    slope = max(1u, (256u * S::kRowsMax / S::kBt) / (uint32_t)a.group);
+    base = (it.pos >> S::kBtLog) + 1 + S::kSet;
+    if (a.window) {
+      most = (a.window >> S::kBtLog) + (slope >> 8) + 2 + S::kSet;
+      const int64_t room = max((int64_t)0, min(most - base, (int64_t)1 << 22));
+      rising = ((uint32_t)room << 8) / (uint32_t)slope;
+    }
   }
-  return rising * base + S::kRowsMax * rising * (rising + 1) / (2 * per) + (j - rising) * (most + S::kSet);
+  __device__ __forceinline__ int64_t operator()(int64_t j) const {
+    const int64_t r = min(j, rising);
+    return r * base + (slope * r * (r + 1) >> 9) + (j - r) * most;
+  }
+};
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t y) {  // (of numbers that are mostly small)
+  return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
 }
 
 // Values 8 at a time of a row of queries, from anywhere.
@@ -274,7 +289,6 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   using S = RowsShape<KIND, DP>;
   constexpr int kTiles = S::kTiles, kBt = S::kBt, kStages = S::kStages;
   extern __shared__ char room_[];
-  begin_kernel();
   char* const room = room_ + ((1024 - (smem_of(room_) & 1023)) & 1023);
   char* const q_room = room;
   char* const stages = q_room + kTiles * S::kQTile;
@@ -282,12 +296,29 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   RowsShared& sh = *(RowsShared*)(raws + S::kRaws * S::kRaw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+  // (Nothing so far touches memory: it runs beside the end of the kernel before.)
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 1 : 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
+    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], 4), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1), bar_init(sh.team[i], 4);
+    for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
+    for (int i = 0; i < 8; ++i) bar_init(sh.raw[i / 2][i & 1], 1);
+    bar_init(sh.drain, 1);
+    sh.dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == S::kSoft + 4) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(&sh.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    before_sync();
+  }
+  begin_kernel();
+
   // ---- this CTA's share: a thread sums the costs of consecutive items, the CTA scans the threads' sums.
   const int32_t each = (a.n + S::kThreads - 1) / S::kThreads, i0 = threadIdx.x * each;
   int64_t mine = 0;
   for (int32_t i = i0; i < i0 + each && i < a.n; ++i) {
     const RowsItem it = rows_item<S>(c, a, i, blockIdx.x == 0 ? w.err : nullptr);
-    if (it.tiles) mine += c.heads * rows_cost<S>(a, it, it.tiles);
+    if (it.tiles) mine += c.heads * RowsCost<S>(a, it)(it.tiles);
   }
   int64_t scan = mine;
 #pragma unroll
@@ -306,32 +337,21 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   }
   // (Four at least, so that no two CTAs' shares begin at the same step inside a unit.)
   const int64_t ctas = min((int64_t)gridDim.x, max((int64_t)1, total / 4));
-  if (total == 0 || blockIdx.x >= ctas) return;
-  const int64_t x0 = total * blockIdx.x / ctas, x1 = total * (blockIdx.x + 1) / ctas;
+  if (total == 0 || blockIdx.x >= ctas) {  // (the barrier above has ordered this after the allocation)
+    if (warp == S::kSoft + 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem));
+    return;
+  }
+  const int64_t x0 = divide(total * blockIdx.x, ctas), x1 = divide(total * (blockIdx.x + 1), ctas);
   if (x0 >= before && x0 < before + mine) {
     int32_t i = i0;
     for (;; ++i) {
       const RowsItem it = rows_item<S>(c, a, i, nullptr);
-      const int64_t t = it.tiles ? c.heads * rows_cost<S>(a, it, it.tiles) : 0;
+      const int64_t t = it.tiles ? c.heads * RowsCost<S>(a, it)(it.tiles) : 0;
       if (x0 < before + t) break;
       before += t;
     }
     sh.item = i;
     sh.before = before;
-  }
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 1 : 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
-    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], 4), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1), bar_init(sh.team[i], 4);
-    for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
-    for (int i = 0; i < 8; ++i) bar_init(sh.raw[i / 2][i & 1], 1);
-    bar_init(sh.drain, 1);
-    sh.dead = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == S::kSoft + 4) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(&sh.tmem)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    before_sync();
   }
   __syncthreads();
   after_sync();
@@ -375,7 +395,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       unit = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
       const uint32_t flip = minus ? 0x80008000u : 0;
       mul = unit;
-      constexpr int kLoads = KIND == P2P_KV_E4M3 ? 4 : 8;
+      constexpr int kLoads = DP == 64 ? 8 : 16;
 #pragma unroll 1
       for (int x0 = 0; x0 < 32; x0 += kAtOnce * kLoads) {
         uint4 v[kLoads];
@@ -561,25 +581,32 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             uint16_t* const out = (uint16_t*)a.out + row * a.out_row + head * a.out_head + d;
             const float* const own = a.own + (row * a.heads + head) * c.dim + d;
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
+            for (int i = 0; i < 32; i += 16) {
               if (d + i >= c.dim) break;
-              float v[8];
+              const bool half = d + i + 8 >= c.dim;  // (head_dim is a multiple of 8)
+              float v[16];
 #pragma unroll
-              for (int k = 0; k < 8; ++k) v[k] = o[i + k] * f;
+              for (int k = 0; k < 16; ++k) v[k] = o[i + k] * f;
               if (a.own) {
-                const float4 x = *(const float4*)(own + i), y = *(const float4*)(own + i + 4);
-                v[0] = fmaf(x.x, other, v[0]), v[1] = fmaf(x.y, other, v[1]), v[2] = fmaf(x.z, other, v[2]), v[3] = fmaf(x.w, other, v[3]);
-                v[4] = fmaf(y.x, other, v[4]), v[5] = fmaf(y.y, other, v[5]), v[6] = fmaf(y.z, other, v[6]), v[7] = fmaf(y.w, other, v[7]);
-              }
-              uint32_t b[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
+                for (int k = 0; k < 16; k += 4) {
+                  if (k >= 8 && half) break;
+                  const float4 x = *(const float4*)(own + i + k);
+                  v[k] = fmaf(x.x, other, v[k]), v[k + 1] = fmaf(x.y, other, v[k + 1]);
+                  v[k + 2] = fmaf(x.z, other, v[k + 2]), v[k + 3] = fmaf(x.w, other, v[k + 3]);
+                }
+              }
+              uint32_t b[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
                 b[k] = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v[2 * k], v[2 * k + 1]) : pack<P2P_KV_F16>(v[2 * k], v[2 * k + 1]);
-              if (a.out16) {
-                *(uint4*)(out + i) = make_uint4(b[0], b[1], b[2], b[3]);
+              if (a.out32 && !half) {
+                // (Whole sectors: the lanes' rows are apart.  As two stores of 16 bytes, a unit's end takes half as long again.)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + i), P2P_I8(b, 0) : "memory");
               } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) out[i + k] = (uint16_t)(b[k / 2] >> (k & 1) * 16);
+                for (int k = 0; k < 16; ++k)
+                  if (k < 8 || !half) out[i + k] = (uint16_t)(b[k / 2] >> (k & 1) * 16);
               }
             }
           };
@@ -664,6 +691,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     constexpr int kOwn = kBt / 4;
     const int own0 = (warp - S::kSoft) * kOwn;
     const int64_t across = c.v - c.k;
+    const int32_t chunks = (dim16 + 63) / 64;  // (all 64 values of the last one are filled)
     int32_t stage = 0;
     uint32_t phase = 1;   // (of `empty`: a fresh barrier's last phase counts as done)
     uint32_t raw_phase = 0;
@@ -678,7 +706,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         if (KIND != P2P_KV_E4M3 && maps.rows) {
           // By the tensor memory accelerator, from one warp: a lane has a box of tokens.
           if (warp == S::kSoft) {
-            const int32_t size = maps.rows, boxes = kBt / size, chunks = (dim16 + 63) / 64;
+            const int32_t size = maps.rows, boxes = kBt / size;
             const auto page_of = [&](int32_t j) {
               const int32_t t = j * kBt + lane * size;
               return lane < boxes && j < j1 && t < end && t + size > begin ? pages[c.by_page.div(t)] : -1;
@@ -757,7 +785,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
                 uint4 y = make_uint4(0, 0, 0, 0);
                 if (piece < c.row16 && t >= begin && t < end && (here >> row / size & 1))
                   y = *(const uint4*)(raw + v * S::kRaw + row * c.dim + piece * 16);
-                if (piece < c.row16) {
+                if (piece < 4 * chunks) {
                   *(uint4*)(to + in_tile * 128 + ((2 * piece & 7) ^ (in_tile & 7)) * 16) =
                       make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
                   *(uint4*)(to + in_tile * 128 + (((2 * piece & 7) + 1) ^ (in_tile & 7)) * 16) =
@@ -802,14 +830,19 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             for (int v = 0; v < 2; ++v) {
               if (!bar_wait(sh.empty[stage], phase, sh)) return;
               const uint32_t to = smem_of(stages) + stage * S::kStage + (piece / 8) * (kBt * 128);
+              // (Places four at a time: one by one, each copy waits for its exchange.)
 #pragma unroll
-              for (int x = 0; x < kOwn; x += kAtOnce) {
-                const int row = x + lane / kLanes;
-                const int64_t o = __shfl_sync(~0u, at, row);
-                const bool in = o >= 0 && piece < c.row16;
-                const char* from = in ? base + o + (v ? across : 0) + piece * 16 : c.k;
-                const int in_tile = own0 + row;
-                if (piece * 8 < dim16) copy16(to + in_tile * 128 + ((piece & 7) ^ (in_tile & 7)) * 16, from, in);
+              for (int x0 = 0; x0 < kOwn; x0 += 4 * kAtOnce) {
+                int64_t o[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[k] = __shfl_sync(~0u, at, (x0 + k * kAtOnce + lane / kLanes) & 31);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const int in_tile = own0 + x0 + k * kAtOnce + lane / kLanes;
+                  const bool in = o[k] >= 0 && piece < c.row16;
+                  const char* from = in ? base + o[k] + (v ? across : 0) + piece * 16 : c.k;
+                  if (piece < 8 * chunks && x0 + k * kAtOnce < kOwn) copy16(to + in_tile * 128 + ((piece & 7) ^ (in_tile & 7)) * 16, from, in);
+                }
               }
               // (Arrives when the thread's copies have; whoever reads them through another path fences after it has waited.)
               asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_of(&sh.full[stage])) : "memory");
@@ -833,7 +866,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               for (int x = 0; x < kOwn; x += kAtOnce) {
                 const int row = own0 + x + lane / kLanes;
                 const uint4 y = b[x / kAtOnce];
-                if (piece < c.row16) {
+                if (piece < 4 * chunks) {
                   *(uint4*)(to + row * 128 + ((2 * piece & 7) ^ (row & 7)) * 16) =
                       make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
                   *(uint4*)(to + row * 128 + (((2 * piece & 7) + 1) ^ (row & 7)) * 16) =
@@ -956,21 +989,29 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   } else if (warp == S::kSoft + 5) {
     // ================================ schedule: the units of this CTA's share
     if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    int32_t i = sh.item, h = 0;
-    int64_t at = sh.before;  // where the item begins
+    int32_t i = sh.item;
+    int64_t x = sh.before;  // where the item begins; then, the tile
     RowsItem it = rows_item<S>(c, a, i, nullptr);
-    int64_t all = rows_cost<S>(a, it, it.tiles), in = x0 - at;
-    h = (int32_t)(in / all);
+    RowsCost<S> costs(a, it);
+    int64_t in = x0 - x;
+    const int64_t all = costs(it.tiles);
+    int32_t h = (int32_t)divide(in, all);
     in -= h * all;
-    int64_t j = 0, past = it.tiles;  // the tile that `in` is in
+    int32_t j = 0, past = it.tiles;  // the tile that `in` is in
     while (past - j > 1) {
-      const int64_t mid = (j + past) >> 1;
-      if (rows_cost<S>(a, it, mid) <= in)
+      const int32_t mid = j + ((past - j) >> 1);
+      if (costs(mid) <= in)
         j = mid;
       else
         past = mid;
     }
-    int64_t cost = rows_cost<S>(a, it, j), x = at + h * all + cost;
+    int64_t cost = costs(j);
+    x += h * all + cost;
+    // The first row's member (token) and head; how far tiles are apart.
+    const int32_t tile_t = S::kRowsMax / a.group, tile_g = S::kRowsMax % a.group, half_t = 128 / a.group, half_g = 128 % a.group;
+    const int64_t r_first = (int64_t)j * S::kRowsMax;
+    int32_t t = (int32_t)divide(r_first, a.group), g0 = (int32_t)(r_first - (int64_t)t * a.group);
+    int32_t members = (int32_t)divide(it.all, a.group);
     bool alive = true;
     const auto emit = [&](const RowsUnit& u) {
       if (!bar_wait(sh.unit_empty[ring], ring_phase ^ 1, sh)) return false;
@@ -984,9 +1025,15 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       return true;
     };
     while (x < x1 && alive) {
-      const int64_t cost1 = rows_cost<S>(a, it, j + 1), width = cost1 - cost;
-      const int64_t r0 = j * S::kRowsMax, r1 = min(r0 + S::kRowsMax, it.all);
-      const RowsSpan span = rows_span(a, it, r0, r1);
+      const int64_t cost1 = costs(j + 1), width = cost1 - cost;
+      const int64_t r0 = (int64_t)j * S::kRowsMax;
+      const int32_t rows = (int32_t)min((int64_t)S::kRowsMax, it.all - r0);
+      // The next tile's first row, and the second half's.
+      int32_t t_next = t + tile_t, g_next = g0 + tile_g, t_half = t + half_t, g_half = g0 + half_g;
+      if (g_next >= a.group) g_next -= a.group, ++t_next;
+      if (g_half >= a.group) g_half -= a.group, ++t_half;
+      const int32_t t_last = min(g_next ? t_next : t_next - 1, members - 1);
+      const RowsSpan span = rows_span(a, it, t, t_last);
       const int32_t j0 = span.begin >> S::kBtLog, n = ((span.end - 1) >> S::kBtLog) + 1 - j0;
       const int64_t inside = min(width, (int64_t)n + S::kSet);  // a share that begins here begins within the unit
       const auto step = [&](int64_t y) {
@@ -995,19 +1042,19 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       const int32_t s0 = step(x0), s1 = step(x1);
       if (s1 > s0) {
         RowsUnit u;
-        u.row = it.row0 + r0 / a.group;
-        u.g0 = (int32_t)(r0 % a.group);
-        u.rows = (int32_t)(r1 - r0);
+        u.row = it.row0 + t;
+        u.g0 = g0;
+        u.rows = rows;
         u.h = h;
         u.seq = it.seq;
-        u.pos = it.pos + (int32_t)(r0 / a.group);
+        u.pos = it.pos + t;
         u.begin = span.begin, u.end = span.end, u.all_begin = span.all_begin, u.all_end = span.all_end;
         u.j0 = j0 + s0, u.j1 = j0 + s1;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           u.t0[k] = u.t1[k] = u.j0;
-          if (k < kTiles && r0 + 128 * k < r1) {
-            const RowsSpan own = rows_span(a, it, r0 + 128 * k, min(r0 + 128 * (k + 1), r1));
+          if (k < kTiles && 128 * k < rows) {
+            const RowsSpan own = rows_span(a, it, k ? t_half : t, k || rows <= 128 ? t_last : g_half ? t_half : t_half - 1);
             u.t0[k] = max(u.j0, own.begin >> S::kBtLog);
             u.t1[k] = max(u.t0[k], min(u.j1, ((own.end - 1) >> S::kBtLog) + 1));
           }
@@ -1015,7 +1062,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         u.parts = 1, u.part = 0, u.c0 = blockIdx.x;
         if (s1 - s0 < n) {
           // The shares that begin at x + kSet + 1 .. x + inside - 1 begin within the unit.
-          const int64_t first = ((x + S::kSet + 1) * ctas + total - 1) / total, end = ((x + inside) * ctas + total - 1) / total;
+          const int64_t first = divide((x + S::kSet + 1) * ctas + total - 1, total), end = divide((x + inside) * ctas + total - 1, total);
           u.c0 = (int32_t)first - 1;
           u.parts = (int32_t)(end - first) + 1;
           u.part = blockIdx.x - u.c0;
@@ -1024,8 +1071,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       }
       x += width;
       cost = cost1;
+      t = t_next, g0 = g_next;
       if (++j < it.tiles) continue;
-      j = 0, cost = 0;
+      j = 0, cost = 0, t = 0, g0 = 0;
       if (++h < c.heads) continue;
       h = 0;
       do {
@@ -1033,6 +1081,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         it = rows_item<S>(c, a, i, nullptr);
       } while (it.tiles == 0);
       if (i >= a.n) break;
+      costs = RowsCost<S>(a, it);
+      members = (int32_t)divide(it.all, a.group);
     }
     if (alive) {
       RowsUnit u = {};
@@ -1053,26 +1103,42 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           const int32_t j = y >> 1;
           if (!bar_wait(sh.full[stage], phase, sh)) return;
           if ((y & 1) && (j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) {
-            constexpr uint32_t kEnd = KIND == P2P_KV_BF16 ? 0x7f80u : 0x7c00u;
+            // An exponent of all ones carries into the sign's place.
+            constexpr uint32_t kExponent = KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = KIND == P2P_KV_BF16 ? 0x00800080u : 0x04000400u;
+            char* const tile = stages + stage * S::kStage;
+            const int32_t first = max(u.begin - j * kBt, 0), end = min(u.end - j * kBt, kBt);  // the rows that are somebody's
+            for (int x = mine; x < (kBt - (end - first)) * 8; x += 64) {  // (the others hold whatever lay there)
+              const int row = x / 8 < first ? x / 8 : x / 8 - first + end;
+              for (int k = 0; k < S::kChunks; ++k) *(uint4*)(tile + k * (kBt * 128) + row * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+            }
+            uint32_t ends = 0;
+#pragma unroll 1
+            for (int k = 0; k * 64 < dim16; ++k)
+#pragma unroll 8
+              for (int x = mine; x < kBt * 8; x += 64) {
+                const uint4 v = *(const uint4*)(tile + k * (kBt * 128) + x * 16);
+                const uint32_t some = ((v.x & kExponent) + kOne) | ((v.y & kExponent) + kOne) | ((v.z & kExponent) + kOne) |
+                                      ((v.w & kExponent) + kOne);
+                const int row = x >> 3;
+                if (row >= first && row < end) ends |= some;
+              }
             bool found = false;
-            const int rows16 = dim16 / 8;
-            for (int z = mine; z < kBt * rows16; z += 64) {
-              const int row = z / rows16, piece = z - row * rows16;
-              uint4* const p = (uint4*)(stages + stage * S::kStage + (piece / 8) * (kBt * 128) + row * 128 + ((piece & 7) ^ (row & 7)) * 16);
-              if (j * kBt + row < u.begin || j * kBt + row >= u.end) {  // (nobody's: whatever lies there)
-                *p = make_uint4(0, 0, 0, 0);
-                continue;
-              }
-              const uint4 v = *p;
-              uint32_t b[4] = {v.x, v.y, v.z, v.w};
-              bool bad = false;
+            if (ends & 0x80008000u) {
+              for (int k = 0; k * 64 < dim16; ++k)
+                for (int x = mine; x < kBt * 8; x += 64) {
+                  const int row = x >> 3;
+                  if (row < first || row >= end) continue;
+                  uint4* const p = (uint4*)(tile + k * (kBt * 128) + x * 16);
+                  const uint4 v = *p;
+                  uint32_t b[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const uint32_t lo = b[k] & kEnd, hi = b[k] >> 16 & kEnd;
-                if (lo == kEnd) b[k] &= 0xffff0000u, bad = true;
-                if (hi == kEnd) b[k] &= 0xffffu, bad = true;
-              }
-              if (bad) *p = make_uint4(b[0], b[1], b[2], b[3]), found = true;
+                  for (int y = 0; y < 4; ++y) {
+                    const uint32_t bad = ((b[y] & kExponent) + kOne) & 0x80008000u;
+                    b[y] &= ~((bad >> 15) * 0xffffu);
+                  }
+                  *p = make_uint4(b[0], b[1], b[2], b[3]);
+                }
+              found = true;
             }
             if (found) sh.poison[ring] = 1;
             async_fence();
