@@ -502,7 +502,7 @@ int p2p_kv_write_rotated(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* se
  * named again), its keys and values written, and attends over the tokens up to itself, the last `window` of them (0: all).
  * Other arguments, results and roundings as p2p_kv_attend, with one lse[t * n_heads + h] a row.  Rows of no sequence are
  * left as they were, as are those of a sequence out of range or with fewer tokens than rows (device-side errors, like offsets out of range).
- * n is at most 2^20, n_tokens * n_heads at most 2^33. */
+ * n is at most 2^20, n_tokens * n_heads at most 2^29. */
 int p2p_kv_attend_prompt(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,
                          int64_t n_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t type,
                          int32_t n_heads, float scale, int32_t window, void* out, int64_t out_token_stride,
@@ -516,7 +516,8 @@ int64_t p2p_kv_attend_shared_work(const p2p_kv* kv, int32_t n, int32_t n_heads);
  * here: the leading page entries that are the same in all of them, as p2p_kv_fork leaves them.  Sequences that share nothing, and rows
  * of no group, are worked off each by itself, so the results are p2p_kv_attend's, but for the order of sums,
  * whatever the groups.  work: p2p_kv_attend_shared_work bytes of DEVICE memory on a 16-byte boundary, not used by
- * anything else until the call's work is done.  n_groups is at most n.  Device-side errors: as p2p_kv_attend, and groups out of range or
+ * anything else until the call's work is done.  n_groups is at most n, n * n_heads at
+ * most 2^29.  Device-side errors: as p2p_kv_attend, and groups out of range or
  * descending (no row is then grouped). */
 int p2p_kv_attend_shared(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups, const int32_t* groups,
                          const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t type, int32_t n_heads,

@@ -222,6 +222,8 @@ struct KvRowsCall {
   int64_t n_tokens, q_row, q_head, out_row, out_head;
   int32_t n, heads, group, type, window, layer;  // group: query heads a kv head
   FastDiv by_group;
+  int32_t shift;   // see RowsCost in kv_rows.cuh: 2^shift steps are counted as one, and a tile's rows are slope / 256 steps of tokens
+  uint32_t slope;
   float scale;
   bool q16, out32;  // whether rows of q lie on 16-byte boundaries, and those of out on 32-byte ones
 };

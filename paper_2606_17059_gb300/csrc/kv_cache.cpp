@@ -509,14 +509,20 @@ int p2p_kv_write_rotated(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   return P2P_OK;
 }
 
-static p2p::KvRowsCall rows_call(const p2p_kv* h, int32_t layer, const int32_t* seq, const void* q, int64_t q_row,
+static p2p::KvRowsCall rows_call(const p2p_kv* h, int32_t layer, int32_t n, int64_t n_rows, const int32_t* seq, const void* q, int64_t q_row,
                                  int64_t q_head, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
                                  int64_t out_row, int64_t out_head, float* lse) {
   p2p::KvRowsCall a = {};
   a.q = q, a.out = out, a.lse = lse, a.seq = seq;
   a.q_row = q_row, a.q_head = q_head, a.out_row = out_row, a.out_head = out_head;
-  a.heads = n_heads, a.group = n_heads / h->c.heads, a.type = type, a.window = window, a.layer = layer, a.scale = scale;
+  a.n = n, a.heads = n_heads, a.group = n_heads / h->c.heads, a.type = type, a.window = window, a.layer = layer, a.scale = scale;
   a.by_group = p2p::FastDiv((uint32_t)a.group);
+  // Steps of 128 (64) tokens for tiles of 256 (128) rows are counted in 32 bits: coarser where there may be too many.
+  const int rows = h->c.dim <= 128 ? 256 : 128, step = rows / 2;
+  a.slope = std::max(1u, (uint32_t)(256 * rows / step / a.group));
+  const double tiles = (double)std::min<int64_t>(n, n_rows) * h->c.heads + (double)n_rows * n_heads / rows;
+  const double most = (double)h->c.max_pages * h->c.page / step + 4;
+  while (tiles * (4 + std::ldexp(most, -a.shift)) > 4e9) ++a.shift;
   a.q16 = (uintptr_t)q % 16 == 0 && q_row % 8 == 0 && q_head % 8 == 0;
   a.out32 = (uintptr_t)out % 32 == 0 && out_row % 16 == 0 && out_head % 16 == 0;
   return a;
@@ -527,17 +533,16 @@ int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
                          int32_t n_heads, float scale, int32_t window, void* out, int64_t out_token_stride,
                          int64_t out_head_stride, float* lse) {
   if (int rc = check_attend(h, layer, n, seq, type, n_heads, window)) return rc;
-  if (n_tokens < 0 || n_tokens > INT32_MAX || n_tokens * n_heads > (int64_t)1 << 33)
+  if (n_tokens < 0 || n_tokens > INT32_MAX || n_tokens * n_heads > (int64_t)1 << 29)
     return fail(h, P2P_E_INVAL, "n_tokens out of range");
   if (n == 0 || n_tokens == 0) return P2P_OK;
   if (!offsets) return fail(h, P2P_E_INVAL, "NULL device pointer");
   if (int rc = check_rows(h, n_tokens, q, n_heads, out, out_token_stride, out_head_stride, lse)) return rc;
   DeviceGuard g(h->device);
-  p2p::KvRowsCall a = rows_call(h, layer, seq, q, q_token_stride, q_head_stride, type, n_heads, scale, window, out,
+  p2p::KvRowsCall a = rows_call(h, layer, n, n_tokens, seq, q, q_token_stride, q_head_stride, type, n_heads, scale, window, out,
                                 out_token_stride, out_head_stride, lse);
   a.offsets = offsets;
   a.n_tokens = n_tokens;
-  a.n = n;
   CK(launch_rows(h->c, h->maps, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;
@@ -566,6 +571,7 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
                          float scale, int32_t window, void* out, int64_t out_row_stride, int64_t out_head_stride,
                          float* lse, void* work) {
   if (int rc = check_attend(h, layer, n, seq, type, n_heads, window)) return rc;
+  if ((int64_t)n * n_heads > (int64_t)1 << 29) return fail(h, P2P_E_INVAL, "n * n_heads exceeds 2^29");
   if (n_groups < 0 || n_groups > n) return fail(h, P2P_E_INVAL, "n_groups: at most n");
   if (n == 0) return P2P_OK;
   if ((n_groups > 0 && !groups) || !work) return fail(h, P2P_E_INVAL, "NULL device pointer");
@@ -586,14 +592,13 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   CK(launch_attend(h->c, &rest, h->w, h->num_sms, h->stream));
   h->launches += 2;
   if (n_groups == 0) return P2P_OK;
-  p2p::KvRowsCall a = rows_call(h, layer, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out,
+  p2p::KvRowsCall a = rows_call(h, layer, n_groups, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out,
                                 out_row_stride, out_head_stride, lse);
   a.groups = groups;
   a.spans = spans;
   a.own = own;
   a.own_lse = own_lse;
   a.n_tokens = n;
-  a.n = n_groups;
   CK(launch_rows(h->c, h->maps, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;

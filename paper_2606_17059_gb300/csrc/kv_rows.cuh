@@ -63,9 +63,8 @@ struct RowsUnit {
 struct RowsShared {
   uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], team[2], drain, raw[4][2];
   RowsUnit unit[kRing];
-  int64_t sums[16];
-  int64_t before, total;
-  int32_t item, tmem, dead, last[2];
+  uint32_t sums[16];
+  int32_t tmem, dead, last[2];
   int32_t poison[kRing];     // whether values were taken out of the unit's steps
 };
 static_assert(sizeof(RowsShared) <= 2048);
@@ -193,13 +192,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // An item of the call: a sequence with its new tokens, or a group with what it shares.  Its tiles of rows follow one another for
-// each kv head in turn.
+// each kv head in turn.  (Rows are counted in 31 bits and costs in 32: the host sees to both.)
 struct RowsItem {
-  int64_t row0;              // its first row of q
-  int64_t all;               // rows: tokens (or members) times heads of a kv head
-  int32_t seq, pos;          // the first token's position; of a group: where the last row's window begins
-  int32_t shared, first;     // of a group: tokens first .. shared - 1 are seen
-  int32_t tiles;
+  int64_t row0;             // its first row of q
+  int32_t members, tiles;   // tokens (rows of the group), and tiles of them times the heads of a kv head
+  int32_t seq, pos;         // pos: the first token's position; of a group: where the last row's window begins
+  int32_t shared, first;    // of a group: tokens first .. shared - 1 are seen
 };
 template <class S>
 __device__ __forceinline__ RowsItem rows_item(const KvView& c, const KvRowsCall& a, int32_t i, int32_t* err) {
@@ -209,32 +207,29 @@ __device__ __forceinline__ RowsItem rows_item(const KvView& c, const KvRowsCall&
     if (span.x == 0) return r;  // (nothing is shared, or the groups do not hold)
     const int32_t r0 = a.groups[i], r1 = a.groups[i + 1], shared = shared_tokens(c, span, r1 - r0);
     if (shared == 0) return r;
-    r = {r0, (int64_t)(r1 - r0) * a.group, a.seq ? a.seq[r0] : r0, span.z, shared, span.y, 0};
+    r = {r0, r1 - r0, 0, a.seq ? a.seq[r0] : r0, span.z, shared, span.y};
   } else {
     const int64_t o0 = a.offsets[i], o1 = a.offsets[i + 1];
+    const int32_t seq = a.seq ? a.seq[i] : i;
     int32_t bad = o0 < 0 || o1 < o0 || o1 > a.n_tokens ? KV_BAD_OFFSETS : 0;
     if (!bad && o1 > o0) {
-      const int32_t seq = a.seq ? a.seq[i] : i;
-      if ((uint32_t)seq >= (uint32_t)c.n_seqs) {
+      const int32_t len = (uint32_t)seq < (uint32_t)c.n_seqs ? length_of(c, seq) : -2;
+      if (len == -2)
         bad = KV_BAD_SEQ;
-      } else {
-        const int32_t len = length_of(c, seq);
-        if (len < o1 - o0)
-          bad = KV_BAD_COUNT;
-        else
-          r = {o0, (o1 - o0) * a.group, seq, len - (int32_t)(o1 - o0), 0, 0, 0};
-      }
+      else if (len < o1 - o0)
+        bad = KV_BAD_COUNT;
+      else
+        r = {o0, (int32_t)(o1 - o0), 0, seq, len - (int32_t)(o1 - o0), 0, 0};
     }
     if (bad && err) atomicOr(err, bad);
   }
-  r.tiles = (int32_t)((r.all + S::kRowsMax - 1) / S::kRowsMax);
+  r.tiles = (r.members * a.group + S::kRowsMax - 1) / S::kRowsMax;
   return r;
 }
 __device__ __forceinline__ int32_t window_begin(const KvRowsCall& a, int32_t end) {
   return a.window && end > a.window ? end - a.window : 0;
 }
-// Tokens that some rows of an item see, the first of which are of its member (token) t0, the last of t1: any of the rows,
-// and each of them.
+// Tokens that rows of an item's members (tokens) t0 to t1 see: any of the rows, and each of them.
 struct RowsSpan {
   int32_t begin, end, all_begin, all_end;
 };
@@ -243,44 +238,113 @@ __device__ __forceinline__ RowsSpan rows_span(const KvRowsCall& a, const RowsIte
   const int32_t e0 = it.pos + t0 + 1, e1 = it.pos + t1 + 1;
   return {window_begin(a, e0), e1, window_begin(a, e1), e0};
 }
-// What the first j tiles of an item count for, each kSet for itself and about its steps: any rising function would do, as
-// long as all CTAs take the same.
+// What the first j tiles of an item count for, in units of 2^shift steps: each kSet for itself and about its steps.  Any rising
+// function would do, as long as all CTAs take the same.
 template <class S>
 struct RowsCost {
-  int64_t base, most;  // steps of the first tile, and at most (with a window)
-  int64_t slope;       // by how much (in 256ths) each tile has more than the one before
-  int64_t rising;      // tiles before those that have most
+  uint32_t base, most, slope, rising;  // the first tile's; how much each has more (in 512ths of a step) until they have most
+  int32_t shift;
   __device__ __forceinline__ RowsCost(const KvRowsCall& a, const RowsItem& it) {
-    most = 0, rising = INT64_MAX;
+    most = 0, rising = ~0u, slope = 0, shift = a.shift;
     if (a.spans) {
-      base = ((it.shared - 1) >> S::kBtLog) - (it.first >> S::kBtLog) + 1 + S::kSet;
-      slope = 0;
+      base = ((((it.shared - 1) >> S::kBtLog) - (it.first >> S::kBtLog) + 1) >> shift) + S::kSet;
       return;
     }
-    slope = max(1u, (256u * S::kRowsMax / S::kBt) / (uint32_t)a.group);
-    base = (it.pos >> S::kBtLog) + 1 + S::kSet;
+    slope = a.slope;
+    base = (((it.pos >> S::kBtLog) + 1) >> shift) + S::kSet;
     if (a.window) {
-      most = (a.window >> S::kBtLog) + (slope >> 8) + 2 + S::kSet;
-      const int64_t room = max((int64_t)0, min(most - base, (int64_t)1 << 22));
-      rising = ((uint32_t)room << 8) / (uint32_t)slope;
+      most = (((a.window >> S::kBtLog) + (slope >> 8) + 2) >> shift) + S::kSet;
+      rising = most > base ? (min(most - base, 1u << 16) << shift << 8) / slope : 0;
     }
   }
-  __device__ __forceinline__ int64_t operator()(int64_t j) const {
-    const int64_t r = min(j, rising);
-    return r * base + (slope * r * (r + 1) >> 9) + (j - r) * most;
+  __device__ __forceinline__ uint32_t operator()(uint32_t j) const {
+    const uint32_t r = min(j, rising);
+    return r * base + (uint32_t)((uint64_t)r * (r + 1) * slope >> (9 + shift)) + (j - r) * most;
   }
 };
-__device__ __forceinline__ int64_t divide(int64_t x, int64_t y) {  // (of numbers that are mostly small)
-  return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+// floor(x * y / z), y at most 65,536 and the result at most y.
+__device__ __forceinline__ uint32_t share_of(uint32_t x, uint32_t y, uint32_t z) {
+  const uint64_t n = (uint64_t)x * y;
+  uint32_t q = (uint32_t)__fdividef((float)x * (float)y, (float)z);
+  while ((uint64_t)q * z > n) --q;
+  while ((uint64_t)(q + 1) * z <= n) ++q;
+  return q;
 }
 
-// Values 8 at a time of a row of queries, from anywhere.
-__device__ __forceinline__ uint4 query_piece(const KvRowsCall& a, const uint16_t* p) {
-  if (a.q16) return *(const uint4*)p;
-  uint32_t x[4];
+// Values d .. d + 15 of a row's result: o, times f, and the row's own part times `other`.
+__device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_t row, int32_t head, int32_t d, const float* o, float f,
+                                    float other) {
+  uint16_t* const out = (uint16_t*)a.out + row * a.out_row + head * a.out_head + d;
+  const bool half = d + 8 >= c.dim;  // (head_dim is a multiple of 8)
+  float v[16];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
-  return make_uint4(x[0], x[1], x[2], x[3]);
+  for (int k = 0; k < 16; ++k) v[k] = o[k] * f;
+  if (a.own) {
+    const float* const own = a.own + (row * a.heads + head) * c.dim + d;
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) {
+      if (k >= 8 && half) break;
+      const float4 x = *(const float4*)(own + k);
+      v[k] = fmaf(x.x, other, v[k]), v[k + 1] = fmaf(x.y, other, v[k + 1]);
+      v[k + 2] = fmaf(x.z, other, v[k + 2]), v[k + 3] = fmaf(x.w, other, v[k + 3]);
+    }
+  }
+  uint32_t b[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    b[k] = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v[2 * k], v[2 * k + 1]) : pack<P2P_KV_F16>(v[2 * k], v[2 * k + 1]);
+  if (a.out32 && !half) {
+    // (Whole sectors, as the lanes' rows are apart.)
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out), P2P_I8(b, 0) : "memory");
+  } else {
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (k < 8 || !half) out[k] = (uint16_t)(b[k / 2] >> (k & 1) * 16);
+  }
+}
+// Infinities and NaN that were taken out of the values of steps j0 .. j1 - 1 (of those that not all rows see): added to the sums of the
+// rows that see them, tokens begin .. end - 1.  By a warp, whose 32 rows of sums are at o_at.  Rarely needed, so it is small, not
+// fast.
+template <int KIND, int BT>
+__device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall& a, const RowsUnit& u, uint32_t o_at, int32_t j0, int32_t j1,
+                                              int32_t begin, int32_t end) {
+  const int lane = threadIdx.x & 31;
+  constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8;  // of a piece
+#pragma unroll 1
+  for (int32_t p = max(u.begin, j0 * BT); p < min(u.end, j1 * BT); ++p) {
+    const int32_t j = p / BT;
+    if (!(j * BT < u.all_begin || (j + 1) * BT > u.all_end)) continue;
+    const uint32_t e = c.by_page.div(p);
+    const int32_t page = row_of(c, u.seq)[e];
+    if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
+    const char* const at = c.v + a.layer * c.layer_stride + page * c.page_stride + (p - (int32_t)e * c.page) * c.token_stride + u.h * c.head_stride;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (lane < c.row16) v = *(const uint4*)(at + lane * 16);
+    const uint32_t b[4] = {v.x, v.y, v.z, v.w};
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      bad |= KIND == P2P_KV_E4M3 ? (((b[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0
+                                 : (((b[k] & (KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u)) + (KIND == P2P_KV_BF16 ? 0x00800080u : 0x04000400u)) & 0x80008000u) != 0;
+#pragma unroll 1
+    for (uint32_t pieces = __ballot_sync(~0u, bad); pieces; pieces &= pieces - 1) {
+      const int piece = __ffs(pieces) - 1;
+#pragma unroll 1
+      for (int k = 0; k < kValues; ++k) {
+        const char* const one = at + piece * 16 + k * (16 / kValues);
+        const float f = KIND == P2P_KV_E4M3   ? __half2float(__nv_cvt_fp8_to_halfraw(*(const uint8_t*)one, __NV_E4M3))
+                        : KIND == P2P_KV_BF16 ? __bfloat162float(*(const __nv_bfloat16*)one)
+                                              : __half2float(*(const __half*)one);
+        if (fabsf(f) < INFINITY) continue;
+        uint32_t o;
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(o) : "r"(o_at + piece * kValues + k) : "memory");
+        tmem_loaded();
+        if (p >= begin && p < end) o = __float_as_uint(__uint_as_float(o) + f);
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(o_at + piece * kValues + k), "r"(o) : "memory");
+        tmem_stored();
+      }
+    }
+  }
 }
 
 template <int KIND, int DP>
@@ -313,48 +377,27 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   }
   begin_kernel();
 
-  // ---- this CTA's share: a thread sums the costs of consecutive items, the CTA scans the threads' sums.
-  const int32_t each = (a.n + S::kThreads - 1) / S::kThreads, i0 = threadIdx.x * each;
-  int64_t mine = 0;
-  for (int32_t i = i0; i < i0 + each && i < a.n; ++i) {
+  // ---- what all items count for: a warp sums consecutive ones, 32 at a time.  (Code that runs once costs its way from memory, a
+  // microsecond every few hundred instructions: this and the schedule are kept short.)
+  constexpr int kAll = S::kThreads / 32;
+  const int32_t per_warp = ((a.n + kAll - 1) / kAll + 31) & ~31;
+  uint32_t sum_of = 0;
+#pragma unroll 1
+  for (int32_t i = warp * per_warp + lane; i < min(a.n, (warp + 1) * per_warp); i += 32) {
     const RowsItem it = rows_item<S>(c, a, i, blockIdx.x == 0 ? w.err : nullptr);
-    if (it.tiles) mine += c.heads * RowsCost<S>(a, it)(it.tiles);
+    if (it.tiles) sum_of += c.heads * RowsCost<S>(a, it)(it.tiles);
   }
-  int64_t scan = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int64_t y = __shfl_up_sync(~0u, scan, d);
-    if (lane >= d) scan += y;
-  }
-  if (lane == 31) sh.sums[warp] = scan;
+  sum_of = __reduce_add_sync(~0u, sum_of);
+  if (lane == 0) sh.sums[warp] = sum_of;
   __syncthreads();
-  int64_t before = scan - mine, total = 0;
-#pragma unroll
-  for (int k = 0; k < S::kThreads / 32; ++k) {
-    const int64_t y = sh.sums[k];
-    before += k < warp ? y : 0;
-    total += y;
-  }
+  after_sync();
+  const uint32_t of_warp = lane < kAll ? sh.sums[lane] : 0, total = __reduce_add_sync(~0u, of_warp);
   // (Four at least, so that no two CTAs' shares begin at the same step inside a unit.)
-  const int64_t ctas = min((int64_t)gridDim.x, max((int64_t)1, total / 4));
-  if (total == 0 || blockIdx.x >= ctas) {  // (the barrier above has ordered this after the allocation)
+  const uint32_t ctas = min(gridDim.x, max(1u, total / 4));
+  if (total == 0 || blockIdx.x >= ctas) {
     if (warp == S::kSoft + 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem));
     return;
   }
-  const int64_t x0 = divide(total * blockIdx.x, ctas), x1 = divide(total * (blockIdx.x + 1), ctas);
-  if (x0 >= before && x0 < before + mine) {
-    int32_t i = i0;
-    for (;; ++i) {
-      const RowsItem it = rows_item<S>(c, a, i, nullptr);
-      const int64_t t = it.tiles ? c.heads * RowsCost<S>(a, it)(it.tiles) : 0;
-      if (x0 < before + t) break;
-      before += t;
-    }
-    sh.item = i;
-    sh.before = before;
-  }
-  __syncthreads();
-  after_sync();
   const uint32_t tmem = sh.tmem;
   const int32_t dim16 = (c.dim + 15) / 16 * 16;
   int32_t ring = 0;          // the unit's place, and the phase of its barriers
@@ -389,54 +432,70 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     // Queries into shared memory; a negative scale changes their signs instead, as exp's maximum is the products'.
     const auto load_queries = [&](const RowsUnit& u) {
       constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;  // lanes a row, rows at a time
-      const int piece = lane % kLanes;
-      float unit = fabsf(a.scale) * kLog2e * (KIND == P2P_KV_E4M3 ? fabsf(c.k_scale[a.layer * c.heads + u.h]) : 1.f);
-      const bool minus = (a.scale < 0.f) != (KIND == P2P_KV_E4M3 && c.k_scale[a.layer * c.heads + u.h] < 0.f);
-      unit = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
+      const int piece = lane % kLanes, own = (warp & 3) * 32;
+      float unit = fabsf(a.scale) * kLog2e;
+      bool minus = a.scale < 0.f;
+      if (KIND == P2P_KV_E4M3) {
+        const float k_scale = c.k_scale[a.layer * c.heads + u.h];
+        unit *= fabsf(k_scale), minus ^= k_scale < 0.f;
+      }
+      mul = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
       const uint32_t flip = minus ? 0x80008000u : 0;
-      mul = unit;
-      constexpr int kLoads = DP == 64 ? 8 : 16;
-#pragma unroll 1
-      for (int x0 = 0; x0 < 32; x0 += kAtOnce * kLoads) {
-        uint4 v[kLoads];
+      const auto at = [&](int x) -> const uint16_t* {
+        int64_t row;
+        int32_t head;
+        row_of_q(u, own + x, row, head);
+        return tile * 128 + own + x < u.rows && piece * 8 < c.dim ? (const uint16_t*)a.q + row * a.q_row + head * a.q_head + piece * 8
+                                                                  : nullptr;
+      };
+      const auto place = [&](int first, uint4 v) {  // rows first .. of the warp's
+        uint32_t b[4] = {v.x, v.y, v.z, v.w};
+        if (KIND == P2P_KV_E4M3) {
+          // In f16, scaled by a power of two so that the row's largest is in [2^14, 2^15): exact but for what is below 2^-28 of
+          // it.
+          float largest = 0.f;
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-          const int x = (warp & 3) * 32 + x0 + k * kAtOnce + lane / kLanes;
-          v[k] = make_uint4(0, 0, 0, 0);
-          if (tile * 128 + x < u.rows && piece * 8 < c.dim) {
-            int64_t row;
-            int32_t head;
-            row_of_q(u, x, row, head);
-            v[k] = query_piece(a, (const uint16_t*)a.q + row * a.q_row + head * a.q_head + piece * 8);
+          for (int i = 0; i < 4; ++i) {
+            const float2 y = two_halves(b[i], a.type);
+            largest = fmaxf(largest, fmaxf(fabsf(y.x), fabsf(y.y)));
           }
+#pragma unroll
+          for (int d = kLanes / 2; d; d >>= 1) largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, d));
+          const int e = largest > 0.f && largest < INFINITY ? max(ilogbf(largest), -112) - 14 : 0;
+          const float down = ldexpf(1.f, -e), of_row = ldexpf(unit, e);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 y = two_halves(b[i], a.type);
+            b[i] = pack<KIND>(y.x * down, y.y * down);
+          }
+          const float got = __shfl_sync(~0u, of_row, (lane - first) * kLanes & 31);
+          if (lane >= first && lane < first + kAtOnce) mul = fmaxf(got, 0x1p-120f);
         }
+        const int x = own + first + lane / kLanes;
+        if (piece * 8 < dim16)
+          *(uint4*)(q_tile + (piece / 8) * (128 * 128) + x * 128 + ((piece & 7) ^ (x & 7)) * 16) =
+              make_uint4(b[0] ^ flip, b[1] ^ flip, b[2] ^ flip, b[3] ^ flip);
+      };
+      constexpr int kLoads = KIND == P2P_KV_E4M3 ? 4 : 8;
+      if (a.q16) {
+#pragma unroll 1
+        for (int x0 = 0; x0 < 32; x0 += kAtOnce * kLoads) {
+          uint4 v[kLoads];
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-          const int first = x0 + k * kAtOnce, x = (warp & 3) * 32 + first + lane / kLanes;
-          uint32_t b[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-          if (KIND == P2P_KV_E4M3) {
-            // In f16, scaled by a power of two so that the row's largest is in [2^14, 2^15): exact but for what is below
-            // 2^-28 of it.
-            float f[8], largest = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 y = two_halves(b[i], a.type);
-              f[2 * i] = y.x, f[2 * i + 1] = y.y;
-              largest = fmaxf(largest, fmaxf(fabsf(y.x), fabsf(y.y)));
-            }
-#pragma unroll
-            for (int d = kLanes / 2; d; d >>= 1) largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, d));
-            const int e = largest > 0.f && largest < INFINITY ? max(ilogbf(largest), -112) - 14 : 0;
-            const float down = ldexpf(1.f, -e), of_row = ldexpf(unit, e);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) b[i] = pack<KIND>(f[2 * i] * down, f[2 * i + 1] * down);
-            const float got = __shfl_sync(~0u, of_row, (lane - first) * kLanes & 31);
-            if (lane >= first && lane < first + kAtOnce) mul = fmaxf(got, 0x1p-120f);
+          for (int k = 0; k < kLoads; ++k) {
+            const uint16_t* const p = at(x0 + k * kAtOnce + lane / kLanes);
+            v[k] = p ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) b[i] ^= flip;
-          if (piece * 8 < dim16)
-            *(uint4*)(q_tile + (piece / 8) * (128 * 128) + x * 128 + ((piece & 7) ^ (x & 7)) * 16) = make_uint4(b[0], b[1], b[2], b[3]);
+          for (int k = 0; k < kLoads; ++k) place(x0 + k * kAtOnce, v[k]);
+        }
+      } else {
+#pragma unroll 1
+        for (int x = 0; x < 32; x += kAtOnce) {
+          const uint16_t* const p = at(x + lane / kLanes);
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (p) v = make_uint4(p[0] | p[1] << 16, p[2] | p[3] << 16, p[4] | p[5] << 16, p[6] | p[7] << 16);
+          place(x, v);
         }
       }
       async_fence();
@@ -444,244 +503,187 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       if (lane == 0) bar_arrive(sh.q_full[tile]);
     };
     const auto run = [&]() {
-      if (!bar_wait(sh.unit_full[0], 0, sh)) return;
-      if (sh.unit[0].t1[tile] > sh.unit[0].t0[tile]) load_queries(sh.unit[0]);
-      for (;;) {
-        const RowsUnit& u = sh.unit[ring];
-        if (u.rows == 0) return;
-        const bool some = u.rows > tile * 128;
-        float top = -INFINITY;
-        uint64_t sum = 0;
-        int64_t row = 0;
-        int32_t head = 0, begin = 0, end = INT32_MAX;  // (rows past the last one mask nothing)
-        const int32_t from = u.t0[tile], to = u.t1[tile];
-        const float unit_mul = mul;
-        if (some) {
-          if (tile * 128 + r < u.rows) {
-            row_of_q(u, r, row, head);
-            if (a.spans) {
-              end = u.end;
-              if (a.window) begin = window_begin(a, length_of(c, a.seq ? a.seq[row] : (int32_t)row));
-            } else {
-              end = u.pos + (int32_t)(row - u.row) + 1;
-              begin = window_begin(a, end);
-            }
-          }
-          for (int32_t j = from; j < to; ++j) {
-            if (!bar_wait(sh.s_full[tile], s_phase, sh)) return;
-            s_phase ^= 1;
-            after_sync();
-            uint32_t x[kBt];
-#pragma unroll
-            for (int k = 0; k < kBt / 32; ++k) tmem_load(x + 32 * k, s_at + 32 * k);
-            tmem_loaded();
-            const int32_t t0 = j * kBt, lo = begin - t0, hi = end - t0;  // seen: lo .. hi - 1
-            if (__any_sync(~0u, lo > 0 || hi < kBt)) {
-#pragma unroll
-              for (int k = 0; k < kBt / 32; ++k) {
-                const int32_t l = min(max(lo - 32 * k, 0), 32), m = min(max(hi - 32 * k, 0), 32);
-                const uint32_t seen = (m >= 32 ? ~0u : (1u << m) - 1) & (l >= 32 ? 0u : ~0u << l);
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                  if (!(seen >> i & 1)) x[32 * k + i] = 0xff800000u;
-              }
-            }
-            float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int i = 0; i < kBt; i += 8)
-#pragma unroll
-              for (int k = 0; k < 4; ++k) t[k] = max3(t[k], __uint_as_float(x[i + 2 * k]), __uint_as_float(x[i + 2 * k + 1]));
-            const float most = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * unit_mul;
-            if (__any_sync(~0u, most > top + (Type<KIND>::kUp + Type<KIND>::kLag))) {
-              const float now = fmaxf(most - Type<KIND>::kUp, top), fade = now == -INFINITY ? 1.f : exp2_fast(top - now);
-              top = now;
-              const float2 z = parts_of(sum);
-              sum = pair_of(z.x * fade, z.y * fade);
-              if (j > from) {
+      int32_t now = -1;  // the unit whose results are to be put away
+      bool some = false, valid = false;
+      float top = 0.f;
+      uint64_t sum = 0;
+      int64_t row = 0;
+      int32_t head = 0, begin = 0, end = 0, from = 0, to = 0;
 #pragma unroll 1
-                for (int32_t d = 0; d < dim16; d += 16) {
-                  uint32_t o[16];
-                  tmem_load16(o, o_at + d);
-                  tmem_loaded();
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fade);
-                  tmem_store16(o_at + d, o);
-                }
-              }
-            }
-            const float less = top == -INFINITY ? 0.f : -top;
-            const uint64_t by = pair_of(unit_mul, unit_mul), plus = pair_of(less, less);
-#pragma unroll
-            for (int k = 0; k < kBt / 32; ++k) {
-              uint32_t p[16];
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int y = 32 * k + 2 * i;
-                const float2 f = parts_of(fma2(pair_of(__uint_as_float(x[y]), __uint_as_float(x[y + 1])), by, plus));
-                const float e0 = exp2_fast(f.x), e1 = exp2_fast(f.y);
-                sum = add2(sum, pair_of(e0, e1));
-                p[i] = pack<KIND>(e0, e1);
-              }
-              tmem_store16(s_at + 16 * k, p);
-            }
-            tmem_stored();
-            before_sync();
-            __syncwarp();
-            if (lane == 0) bar_arrive(sh.p_full[tile]);
-          }
-        }
-        // The next unit's queries: the products with this one's are done.
-        const int32_t now = ring;
-        next_unit();
+      for (;;) {
         if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
-        if (sh.unit[ring].t1[tile] > sh.unit[ring].t0[tile]) load_queries(sh.unit[ring]);
+        // This unit's queries: the products with the last one's are done.
+        const bool more = sh.unit[ring].rows > 0;
+        if (more && sh.unit[ring].t1[tile] > sh.unit[ring].t0[tile]) load_queries(sh.unit[ring]);
+
+        // ---- the last unit's results
         if (some) {
+          const RowsUnit& u = sh.unit[now];
           if (to > from) {
             if (!bar_wait(sh.o_full[tile], o_phase, sh)) return;
             o_phase ^= 1;
             after_sync();
+            if (sh.poison[now]) add_poison_of<KIND, kBt>(c, a, u, o_at, from, to, valid ? begin : INT32_MAX, end);
           }
           const float2 z2 = parts_of(sum);
-          float z = z2.x + z2.y;
-          const bool valid = tile * 128 + r < u.rows;
-          // Values that were taken out for rows that do not see them: added to those that do.
-          const auto add_poison = [&](float* o, int32_t d) {
-            if (!sh.poison[now]) return;
-            for (int32_t p = max(begin, from * kBt); p < min(end, to * kBt); ++p) {
-              const int32_t j = p >> S::kBtLog;
-              if (!valid || !(j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) continue;
-              const uint32_t e = c.by_page.div(p);
-              const int32_t page = row_of(c, u.seq)[e];
-              if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
-              const char* at = c.v + a.layer * c.layer_stride + page * c.page_stride + (p - e * c.page) * c.token_stride + u.h * c.head_stride;
-              for (int i = 0; i < 32 && d + i < c.dim; ++i) {
-                const float v = KIND == P2P_KV_E4M3 ? __half2float(__nv_cvt_fp8_to_halfraw(((const uint8_t*)at)[d + i], __NV_E4M3))
-                                : KIND == P2P_KV_BF16 ? __bfloat162float(((const __nv_bfloat16*)at)[d + i])
-                                                      : __half2float(((const __half*)at)[d + i]);
-                if (!(fabsf(v) < INFINITY)) o[i] += v;
-              }
-            }
-          };
+          float high = top, z = z2.x + z2.y;
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h] : 1.f;
-          // Values d .. d + 31 of the row's result: o, times f, and with the part of the row that is its own.
-          float other = 0.f, f = 0.f;
-          const auto finish = [&](float t, float sum_of) {
-            f = sum_of > 0.f || sum_of != sum_of ? v_scale / sum_of : 0.f;
-            float lse = sum_of == 0.f ? -INFINITY : log_sum<KIND>(t, sum_of);
-            if (a.own) {
-              const float his = a.own_lse[row * a.heads + head], high = fmaxf(lse, his);
-              const float p = exp2_fast((lse - high) * kLog2e), q = exp2_fast((his - high) * kLog2e);
-              const float by = __fdividef(1.f, p + q);
-              f *= p * by, other = q * by;
-              lse = high + __logf(p + q);
-            }
-            if (a.lse) a.lse[row * a.heads + head] = lse;
-          };
-          const auto put = [&](const float* o, int32_t d) {
-            uint16_t* const out = (uint16_t*)a.out + row * a.out_row + head * a.out_head + d;
-            const float* const own = a.own + (row * a.heads + head) * c.dim + d;
-#pragma unroll
-            for (int i = 0; i < 32; i += 16) {
-              if (d + i >= c.dim) break;
-              const bool half = d + i + 8 >= c.dim;  // (head_dim is a multiple of 8)
-              float v[16];
-#pragma unroll
-              for (int k = 0; k < 16; ++k) v[k] = o[i + k] * f;
-              if (a.own) {
-#pragma unroll
-                for (int k = 0; k < 16; k += 4) {
-                  if (k >= 8 && half) break;
-                  const float4 x = *(const float4*)(own + i + k);
-                  v[k] = fmaf(x.x, other, v[k]), v[k + 1] = fmaf(x.y, other, v[k + 1]);
-                  v[k + 2] = fmaf(x.z, other, v[k + 2]), v[k + 3] = fmaf(x.w, other, v[k + 3]);
-                }
-              }
-              uint32_t b[8];
-#pragma unroll
-              for (int k = 0; k < 8; ++k)
-                b[k] = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v[2 * k], v[2 * k + 1]) : pack<P2P_KV_F16>(v[2 * k], v[2 * k + 1]);
-              if (a.out32 && !half) {
-                // (Whole sectors: the lanes' rows are apart.  As two stores of 16 bytes, a unit's end takes half as long again.)
-                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + i), P2P_I8(b, 0) : "memory");
-              } else {
-#pragma unroll
-                for (int k = 0; k < 16; ++k)
-                  if (k < 8 || !half) out[i + k] = (uint16_t)(b[k / 2] >> (k & 1) * 16);
-              }
-            }
-          };
           constexpr int kPart = 128 * (DP + 2);  // floats of a row tile's part: [value][row], then maxima and sums
-          if (u.parts == 1) {
-            if (valid) finish(top, z);
+          const auto part_of = [&](int32_t k) { return w.parts + (int64_t)((2 * (u.c0 + k) + (k == 0)) * kTiles + tile) * kPart + r; };
+          const int32_t parts = u.parts;
+          // First this piece's, to where it goes; then, by the CTA that comes last, all of them.
 #pragma unroll 1
-            for (int32_t d = 0; d < dim16; d += 32) {
-              uint32_t o[32];
-              if (to > from) {
-                tmem_load(o, o_at + d);
-                tmem_loaded();
-              } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = 0;
+          for (int turn = 0; turn < 2; ++turn) {
+            const bool keep = turn == 0 && parts > 1;
+            float* const mine = part_of(u.part);
+            float f = 0.f, other = 0.f;
+            if (keep) {
+              mine[DP * 128] = high, mine[(DP + 1) * 128] = z;
+            } else if (valid) {
+              f = z > 0.f || z != z ? v_scale / z : 0.f;
+              float lse = z == 0.f ? -INFINITY : log_sum<KIND>(high, z);
+              if (a.own) {  // with the row's own tokens
+                const float his = a.own_lse[row * a.heads + head], most = fmaxf(lse, his);
+                const float p = exp2_fast((lse - most) * kLog2e), q = exp2_fast((his - most) * kLog2e);
+                const float by = __fdividef(1.f, p + q);
+                f *= p * by, other = q * by;
+                lse = most + __logf(p + q);
               }
-              add_poison((float*)o, d);
-              if (valid) put((const float*)o, d);
+              if (a.lse) a.lse[row * a.heads + head] = lse;
             }
-          } else {
-            const auto part_of = [&](int32_t k) { return w.parts + (int64_t)((2 * (u.c0 + k) + (k == 0)) * kTiles + tile) * kPart + r; };
-            float* const part = part_of(u.part);
+            const float ref = high == -INFINITY ? 0.f : high;
 #pragma unroll 1
-            for (int32_t d = 0; d < dim16; d += 32) {
-              uint32_t o[32];
-              if (to > from) {
-                tmem_load(o, o_at + d);
+            for (int32_t d = 0; d < dim16; d += 16) {
+              float o[16] = {};
+              if (turn == 1) {
+#pragma unroll 1
+                for (int32_t k = 0; k < parts; ++k) {
+                  const float* const p = part_of(k) + d * 128;
+                  const float fade = exp2_fast(__ldcg(part_of(k) + DP * 128) - ref);
+                  float v[16];
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) v[i] = __ldcg(p + i * 128);
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) o[i] = fmaf(v[i], fade, o[i]);
+                }
+              } else if (to > from) {
+                tmem_load16((uint32_t*)o, o_at + d);
                 tmem_loaded();
-              } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = 0;
               }
-              add_poison((float*)o, d);
+              if (keep) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (d + i < dim16) part[(d + i) * 128] = __uint_as_float(o[i]);
+                for (int i = 0; i < 16; ++i) mine[(d + i) * 128] = o[i];
+              } else if (valid) {
+                put(c, a, row, head, d, o, f, other);
+              }
             }
-            part[DP * 128] = top, part[(DP + 1) * 128] = z;
+            if (!keep) break;
             if (!meet()) return;
             if (r == 0) {
               int32_t* const arrived = w.arrived + u.c0 * kTiles + tile;
-              sh.last[tile] = add_acq_rel(arrived, 1) == u.parts - 1;
+              sh.last[tile] = add_acq_rel(arrived, 1) == parts - 1;
               if (sh.last[tile]) *arrived = 0;  // for the next launch
             }
             if (!meet()) return;
-            if (sh.last[tile]) {
-              float high = -INFINITY, sums = 0.f;
-              for (int32_t k = 0; k < u.parts; ++k) high = fmaxf(high, __ldcg(part_of(k) + DP * 128));
-              const float ref = high == -INFINITY ? 0.f : high;
-              for (int32_t k = 0; k < u.parts; ++k)
-                sums += exp2_fast(__ldcg(part_of(k) + DP * 128) - ref) * __ldcg(part_of(k) + (DP + 1) * 128);
-              if (valid) finish(high, sums);
+            const bool last = sh.last[tile];
+            if (!meet()) return;
+            if (!last) break;
+            high = -INFINITY, z = 0.f;
 #pragma unroll 1
-              for (int32_t d = 0; d < dim16; d += 32) {
-                float o[32] = {};
+            for (int32_t k = 0; k < parts; ++k) high = fmaxf(high, __ldcg(part_of(k) + DP * 128));
 #pragma unroll 1
-                for (int32_t k = 0; k < u.parts; ++k) {
-                  const float* const p = part_of(k);
-                  const float fade = exp2_fast(__ldcg(p + DP * 128) - ref);
-                  float v[32];
-#pragma unroll
-                  for (int i = 0; i < 32; ++i) v[i] = d + i < dim16 ? __ldcg(p + (d + i) * 128) : 0.f;
-#pragma unroll
-                  for (int i = 0; i < 32; ++i) o[i] = fmaf(v[i], fade, o[i]);
-                }
-                if (valid) put(o, d);
-              }
-            }
-            if (!meet()) return;  // (sh.last has been read)
+            for (int32_t k = 0; k < parts; ++k)
+              z += exp2_fast(__ldcg(part_of(k) + DP * 128) - (high == -INFINITY ? 0.f : high)) * __ldcg(part_of(k) + (DP + 1) * 128);
           }
         }
-        // (Loads of tensor memory are done before the next products may write there: P of the next unit is announced later.)
+        // (Loads of tensor memory are done before the next products may write there: P of this unit is announced later.)
         before_sync();
         __syncwarp();
-        if (lane == 0) bar_arrive(sh.unit_empty[now]);
+        if (now >= 0 && lane == 0) bar_arrive(sh.unit_empty[now]);
+        if (!more) return;
+
+        // ---- this unit's steps
+        now = ring;
+        next_unit();
+        const RowsUnit& u = sh.unit[now];
+        some = u.rows > tile * 128, valid = tile * 128 + r < u.rows;
+        from = u.t0[tile], to = u.t1[tile];
+        top = -INFINITY, sum = 0;
+        begin = 0, end = INT32_MAX;  // (rows past the last one mask nothing)
+        if (valid) {
+          row_of_q(u, r, row, head);
+          if (a.spans) {
+            end = u.end;
+            if (a.window) begin = window_begin(a, length_of(c, a.seq ? a.seq[row] : (int32_t)row));
+          } else {
+            end = u.pos + (int32_t)(row - u.row) + 1;
+            begin = window_begin(a, end);
+          }
+        }
+        const float unit_mul = mul;
+#pragma unroll 1
+        for (int32_t j = from; j < to; ++j) {
+          if (!bar_wait(sh.s_full[tile], s_phase, sh)) return;
+          s_phase ^= 1;
+          after_sync();
+          uint32_t x[kBt];
+#pragma unroll
+          for (int k = 0; k < kBt / 32; ++k) tmem_load(x + 32 * k, s_at + 32 * k);
+          tmem_loaded();
+          const int32_t t0 = j * kBt, lo = begin - t0, hi = end - t0;  // seen: lo .. hi - 1
+          if (__any_sync(~0u, lo > 0 || hi < kBt)) {
+#pragma unroll
+            for (int k = 0; k < kBt / 32; ++k) {
+              const int32_t l = min(max(lo - 32 * k, 0), 32), m = min(max(hi - 32 * k, 0), 32);
+              const uint32_t seen = (m >= 32 ? ~0u : (1u << m) - 1) & (l >= 32 ? 0u : ~0u << l);
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!(seen >> i & 1)) x[32 * k + i] = 0xff800000u;
+            }
+          }
+          float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < kBt; i += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t[k] = max3(t[k], __uint_as_float(x[i + 2 * k]), __uint_as_float(x[i + 2 * k + 1]));
+          const float most = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * unit_mul;
+          if (__any_sync(~0u, most > top + (Type<KIND>::kUp + Type<KIND>::kLag))) {
+            const float next = fmaxf(most - Type<KIND>::kUp, top), fade = next == -INFINITY ? 1.f : exp2_fast(top - next);
+            top = next;
+            const float2 z = parts_of(sum);
+            sum = pair_of(z.x * fade, z.y * fade);
+            if (j > from) {
+#pragma unroll 1
+              for (int32_t d = 0; d < dim16; d += 16) {
+                uint32_t o[16];
+                tmem_load16(o, o_at + d);
+                tmem_loaded();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fade);
+                tmem_store16(o_at + d, o);
+              }
+            }
+          }
+          const float less = top == -INFINITY ? 0.f : -top;
+          const uint64_t by = pair_of(unit_mul, unit_mul), plus = pair_of(less, less);
+#pragma unroll
+          for (int k = 0; k < kBt / 32; ++k) {
+            uint32_t p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int y = 32 * k + 2 * i;
+              const float2 f = parts_of(fma2(pair_of(__uint_as_float(x[y]), __uint_as_float(x[y + 1])), by, plus));
+              const float e0 = exp2_fast(f.x), e1 = exp2_fast(f.y);
+              sum = add2(sum, pair_of(e0, e1));
+              p[i] = pack<KIND>(e0, e1);
+            }
+            tmem_store16(s_at + 16 * k, p);
+          }
+          tmem_stored();
+          before_sync();
+          __syncwarp();
+          if (lane == 0) bar_arrive(sh.p_full[tile]);
+        }
       }
     };
     run();
@@ -719,7 +721,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               const uint32_t boxes_there = __popc(__ballot_sync(~0u, there)), holes = __ballot_sync(~0u, needed && !there);
               const int32_t in_page = t - (int32_t)c.by_page.div(max(t, 0)) * c.page, this_page = page;
               page = page_of(j + 1);
-#pragma unroll
+#pragma unroll 1
               for (int v = 0; v < 2; ++v) {
                 if (!bar_wait(sh.empty[stage], phase, sh)) return;
                 char* const to = stages + stage * S::kStage;
@@ -775,7 +777,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           page = page_of(j0 + 1);
           for (int32_t j = j0; j < j1; ++j) {
             uint32_t later = 0;
-#pragma unroll
+#pragma unroll 1
             for (int v = 0; v < 2; ++v) {
               if (!bar_wait(sh.raw[warp - S::kSoft][v], raw_phase, sh) || !bar_wait(sh.empty[stage], phase, sh)) return;
               char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128);
@@ -827,11 +829,12 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           if (KIND != P2P_KV_E4M3) {
             constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;
             const int piece = lane % kLanes;
+#pragma unroll 1
             for (int v = 0; v < 2; ++v) {
               if (!bar_wait(sh.empty[stage], phase, sh)) return;
               const uint32_t to = smem_of(stages) + stage * S::kStage + (piece / 8) * (kBt * 128);
               // (Places four at a time: one by one, each copy waits for its exchange.)
-#pragma unroll
+#pragma unroll 1
               for (int x0 = 0; x0 < kOwn; x0 += 4 * kAtOnce) {
                 int64_t o[4];
 #pragma unroll
@@ -852,6 +855,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             // 16 values a piece; widened on the way.
             constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
             const int piece = lane % kLanes;
+#pragma unroll 1
             for (int v = 0; v < 2; ++v) {
               uint4 b[kOwn / kAtOnce];
 #pragma unroll
@@ -989,30 +993,6 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   } else if (warp == S::kSoft + 5) {
     // ================================ schedule: the units of this CTA's share
     if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    int32_t i = sh.item;
-    int64_t x = sh.before;  // where the item begins; then, the tile
-    RowsItem it = rows_item<S>(c, a, i, nullptr);
-    RowsCost<S> costs(a, it);
-    int64_t in = x0 - x;
-    const int64_t all = costs(it.tiles);
-    int32_t h = (int32_t)divide(in, all);
-    in -= h * all;
-    int32_t j = 0, past = it.tiles;  // the tile that `in` is in
-    while (past - j > 1) {
-      const int32_t mid = j + ((past - j) >> 1);
-      if (costs(mid) <= in)
-        j = mid;
-      else
-        past = mid;
-    }
-    int64_t cost = costs(j);
-    x += h * all + cost;
-    // The first row's member (token) and head; how far tiles are apart.
-    const int32_t tile_t = S::kRowsMax / a.group, tile_g = S::kRowsMax % a.group, half_t = 128 / a.group, half_g = 128 % a.group;
-    const int64_t r_first = (int64_t)j * S::kRowsMax;
-    int32_t t = (int32_t)divide(r_first, a.group), g0 = (int32_t)(r_first - (int64_t)t * a.group);
-    int32_t members = (int32_t)divide(it.all, a.group);
-    bool alive = true;
     const auto emit = [&](const RowsUnit& u) {
       if (!bar_wait(sh.unit_empty[ring], ring_phase ^ 1, sh)) return false;
       if (lane == 0) {
@@ -1024,65 +1004,131 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       next_unit();
       return true;
     };
-    while (x < x1 && alive) {
-      const int64_t cost1 = costs(j + 1), width = cost1 - cost;
-      const int64_t r0 = (int64_t)j * S::kRowsMax;
-      const int32_t rows = (int32_t)min((int64_t)S::kRowsMax, it.all - r0);
-      // The next tile's first row, and the second half's.
-      int32_t t_next = t + tile_t, g_next = g0 + tile_g, t_half = t + half_t, g_half = g0 + half_g;
-      if (g_next >= a.group) g_next -= a.group, ++t_next;
-      if (g_half >= a.group) g_half -= a.group, ++t_half;
-      const int32_t t_last = min(g_next ? t_next : t_next - 1, members - 1);
-      const RowsSpan span = rows_span(a, it, t, t_last);
-      const int32_t j0 = span.begin >> S::kBtLog, n = ((span.end - 1) >> S::kBtLog) + 1 - j0;
-      const int64_t inside = min(width, (int64_t)n + S::kSet);  // a share that begins here begins within the unit
-      const auto step = [&](int64_t y) {
-        return y <= x ? 0 : y - x >= inside ? n : (int32_t)max((int64_t)0, y - x - S::kSet);
-      };
-      const int32_t s0 = step(x0), s1 = step(x1);
-      if (s1 > s0) {
-        RowsUnit u;
-        u.row = it.row0 + t;
-        u.g0 = g0;
-        u.rows = rows;
-        u.h = h;
-        u.seq = it.seq;
-        u.pos = it.pos + t;
-        u.begin = span.begin, u.end = span.end, u.all_begin = span.all_begin, u.all_end = span.all_end;
-        u.j0 = j0 + s0, u.j1 = j0 + s1;
+    const uint32_t x0 = share_of(total, blockIdx.x, ctas), x1 = share_of(total, blockIdx.x + 1, ctas);
+    // The first row's member (token) and head move by these from tile to tile, and to a tile's second half.
+    const int32_t tile_t = a.by_group.div(S::kRowsMax), tile_g = S::kRowsMax - tile_t * a.group;
+    const int32_t half_t = a.by_group.div(128), half_g = 128 - half_t * a.group;
+    // The warp that summed the item where the share begins, and where its items begin.
+    uint32_t x = of_warp;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          u.t0[k] = u.t1[k] = u.j0;
-          if (k < kTiles && 128 * k < rows) {
-            const RowsSpan own = rows_span(a, it, k ? t_half : t, k || rows <= 128 ? t_last : g_half ? t_half : t_half - 1);
-            u.t0[k] = max(u.j0, own.begin >> S::kBtLog);
-            u.t1[k] = max(u.t0[k], min(u.j1, ((own.end - 1) >> S::kBtLog) + 1));
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t y = __shfl_up_sync(~0u, x, d);
+      if (lane >= d) x += y;
+    }
+    const int from = __ffs(__ballot_sync(~0u, x0 < x)) - 1;
+    x = __shfl_sync(~0u, x - of_warp, from);
+    bool alive = true, found = false;
+    // 32 items at a time, a lane each.
+#pragma unroll 1
+    for (int32_t i0 = from * per_warp; alive && x < x1 && i0 < a.n; i0 += 32) {
+      RowsItem own = {};
+      uint32_t own_cost = 0;
+      if (i0 + lane < a.n) {
+        own = rows_item<S>(c, a, i0 + lane, nullptr);
+        if (own.tiles) own_cost = RowsCost<S>(a, own)(own.tiles);
+      }
+#pragma unroll 1
+      for (uint32_t some = __ballot_sync(~0u, own.tiles > 0); some && alive && x < x1; some &= some - 1) {
+        const int l = __ffs(some) - 1;
+        const uint32_t all = __shfl_sync(~0u, own_cost, l);
+        if (!found && x0 - x >= c.heads * all) {
+          x += c.heads * all;
+          continue;
+        }
+        RowsItem it;
+        it.row0 = __shfl_sync(~0u, own.row0, l);
+        it.members = __shfl_sync(~0u, own.members, l), it.tiles = __shfl_sync(~0u, own.tiles, l);
+        it.seq = __shfl_sync(~0u, own.seq, l), it.pos = __shfl_sync(~0u, own.pos, l);
+        it.shared = __shfl_sync(~0u, own.shared, l), it.first = __shfl_sync(~0u, own.first, l);
+        const RowsCost<S> costs(a, it);
+        int32_t h = 0, j = 0;
+        uint32_t cost = 0;
+        if (!found) {  // the head and tile where the share begins
+          found = true;
+          uint32_t in = x0 - x;
+          h = (int32_t)(in / all);
+          in -= h * all;
+          int32_t past = it.tiles;
+#pragma unroll 1
+          while (past - j > 1) {
+            const int32_t mid = j + ((past - j) >> 1);
+            const uint32_t y = costs(mid);
+            if (y <= in)
+              j = mid, cost = y;
+            else
+              past = mid;
           }
         }
-        u.parts = 1, u.part = 0, u.c0 = blockIdx.x;
-        if (s1 - s0 < n) {
-          // The shares that begin at x + kSet + 1 .. x + inside - 1 begin within the unit.
-          const int64_t first = divide((x + S::kSet + 1) * ctas + total - 1, total), end = divide((x + inside) * ctas + total - 1, total);
-          u.c0 = (int32_t)first - 1;
-          u.parts = (int32_t)(end - first) + 1;
-          u.part = blockIdx.x - u.c0;
+        const uint32_t x_next = x + c.heads * all;
+        x += h * all + cost;
+        int32_t t = a.by_group.div(j * S::kRowsMax), g0 = j * S::kRowsMax - t * a.group;
+#pragma unroll 1
+        while (alive && x < x1) {
+          const uint32_t cost1 = costs(j + 1), width = cost1 - cost;
+          const int32_t rows = min(S::kRowsMax, it.members * a.group - j * S::kRowsMax);
+          // The next tile's first row, and the second half's.
+          int32_t t_next = t + tile_t, g_next = g0 + tile_g, t_half = t + half_t, g_half = g0 + half_g;
+          if (g_next >= a.group) g_next -= a.group, ++t_next;
+          if (g_half >= a.group) g_half -= a.group, ++t_half;
+          const int32_t t_last = min(g_next ? t_next : t_next - 1, it.members - 1);
+          const RowsSpan span = rows_span(a, it, t, t_last);
+          const int32_t j0 = span.begin >> S::kBtLog, n = ((span.end - 1) >> S::kBtLog) + 1 - j0;
+          // A share that begins at x + kSet + 1 .. x + inside - 1 begins within the unit, at this step of it:
+          const uint32_t inside = min(width, (uint32_t)((n - 1) >> a.shift) + 1 + S::kSet);
+          const auto step = [&](uint32_t y) {
+            return y <= x + S::kSet ? 0 : y - x >= inside ? n : (int32_t)((y - x - S::kSet) << a.shift);
+          };
+          const int32_t s0 = step(x0), s1 = step(x1);
+          if (s1 > s0) {
+            RowsUnit u;
+            u.row = it.row0 + t;
+            u.g0 = g0;
+            u.rows = rows;
+            u.h = h;
+            u.seq = it.seq;
+            u.pos = it.pos + t;
+            u.begin = span.begin, u.end = span.end, u.all_begin = span.all_begin, u.all_end = span.all_end;
+            u.j0 = j0 + s0, u.j1 = j0 + s1;
+            u.t0[0] = u.t1[0] = u.t0[1] = u.t1[1] = u.j0;
+            {
+              const RowsSpan its = rows_span(a, it, t, rows <= 128 ? t_last : g_half ? t_half : t_half - 1);
+              u.t0[0] = max(u.j0, its.begin >> S::kBtLog);
+              u.t1[0] = max(u.t0[0], min(u.j1, ((its.end - 1) >> S::kBtLog) + 1));
+            }
+            if (kTiles == 2 && rows > 128) {
+              const RowsSpan its = rows_span(a, it, t_half, t_last);
+              u.t0[1] = max(u.j0, its.begin >> S::kBtLog);
+              u.t1[1] = max(u.t0[1], min(u.j1, ((its.end - 1) >> S::kBtLog) + 1));
+            }
+            u.parts = 1, u.part = 0, u.c0 = blockIdx.x;
+            if (s1 - s0 < n) {
+              // The first shares that begin within the unit, and after it.
+              uint32_t first = 0, end = 0;
+#pragma unroll 1
+              for (int k = 0; k < 2; ++k) {
+                const uint32_t y = x + (k ? inside : S::kSet + 1);
+                uint32_t q = share_of(y, ctas, total);
+                while (share_of(total, q, ctas) < y) ++q;
+                if (k == 0)
+                  first = q;
+                else
+                  end = q;
+              }
+              u.c0 = (int32_t)first - 1;
+              u.parts = (int32_t)(end - first) + 1;
+              u.part = blockIdx.x - u.c0;
+            }
+            alive = emit(u);
+          }
+          x += width;
+          cost = cost1;
+          t = t_next, g0 = g_next;
+          if (++j < it.tiles) continue;
+          j = 0, cost = 0, t = 0, g0 = 0;
+          if (++h == c.heads) break;
         }
-        alive = emit(u);
+        if (x < x1) x = x_next;
       }
-      x += width;
-      cost = cost1;
-      t = t_next, g0 = g_next;
-      if (++j < it.tiles) continue;
-      j = 0, cost = 0, t = 0, g0 = 0;
-      if (++h < c.heads) continue;
-      h = 0;
-      do {
-        if (++i >= a.n) break;
-        it = rows_item<S>(c, a, i, nullptr);
-      } while (it.tiles == 0);
-      if (i >= a.n) break;
-      costs = RowsCost<S>(a, it);
-      members = (int32_t)divide(it.all, a.group);
     }
     if (alive) {
       RowsUnit u = {};
@@ -1114,7 +1160,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             uint32_t ends = 0;
 #pragma unroll 1
             for (int k = 0; k * 64 < dim16; ++k)
-#pragma unroll 8
+#pragma unroll 4
               for (int x = mine; x < kBt * 8; x += 64) {
                 const uint4 v = *(const uint4*)(tile + k * (kBt * 128) + x * 16);
                 const uint32_t some = ((v.x & kExponent) + kOne) | ((v.y & kExponent) + kOne) | ((v.z & kExponent) + kOne) |
