@@ -515,7 +515,7 @@ int64_t p2p_kv_attend_shared_work(const p2p_kv* kv, int32_t n, int32_t n_heads);
  * groups[g+1] - 1 (int32 groups[n_groups + 1], non-decreasing, within [0, n]) are a group.  What its sequences share is found
  * here: the leading page entries that are the same in all of them, as p2p_kv_fork leaves them.  Sequences that share nothing, and rows
  * of no group, are worked off each by itself, so the results are p2p_kv_attend's, but for the order of sums,
- * whatever the groups.  work: p2p_kv_attend_shared_work bytes of DEVICE memory on a 16-byte boundary, not used by
+ * whatever the groups.  work: p2p_kv_attend_shared_work bytes of DEVICE memory on a 32-byte boundary, not used by
  * anything else until the call's work is done.  n_groups is at most n, n * n_heads at
  * most 2^29.  Device-side errors: as p2p_kv_attend, and groups out of range or
  * descending (no row is then grouped). */

@@ -131,10 +131,10 @@ struct KvQuery {
   float scale;
   // Whether rows of q may be read by twos, and those of out written by fours, of their values.
   bool q_pairs, out_fours;
-  // Row i is taken from token skip[i] on (NULL: all of it); where that is not 0, its result goes, in 32 bits, to
-  // own [row][head][value] and own_lse [row][head].
+  // Row i is taken from token skip[i] on (NULL: all of it), and where that is not 0, put together with the result of those
+  // before: pre [row][head][value] and pre_lse [row][head].
   const int32_t* skip;
-  float *own, *own_lse;
+  const float *pre, *pre_lse;
 };
 // The attention's kernel for values of a type, head_dim and `group` query heads a kv head: head_dim as it is padded,
 // blocks of eight query heads taken together, and CTAs resident on an SM.
@@ -169,10 +169,15 @@ constexpr int attend_ctas(int type, int dp, int blocks) {
 constexpr int kSideRows = 7;
 // Parts of rows that several CTAs share, four a CTA (see the kernel), and how many have arrived (zero between
 // launches).
+struct KvJoin {        // a unit of kv_rows.cuh that CTA c0 begins and others go on with
+  int64_t row;         // its first row
+  int32_t rows, g0, h, parts;  // parts: 0 where there is none
+};
 struct KvAttendScratch {
   static constexpr int kCtasPerSm = 3;
-  float* parts;      // [kv_attend_parts()]
+  float* parts;      // [the more of kv_attend_parts() and kv_rows_parts()]
   int32_t* arrived;  // [4 * kCtasPerSm * SMs]
+  KvJoin* joins;     // [SMs]: of each CTA of kv_rows.cuh
   int32_t* err;
 };
 // Floats of `parts`: for the blocks of query heads that take most, each part with the sums, maximum and sum of exp of
@@ -218,7 +223,7 @@ struct KvRowsCall {
   const int64_t* offsets;
   const int32_t* groups;    // [n + 1]
   const int4* spans;        // [n]: see launch_kv_share
-  const float *own, *own_lse;  // [row][head][value] and [row][head]: the result over the other tokens of a row (NULL: there are none)
+  float *pre, *pre_lse;     // where results go, in 32 bits, [row][head][value] and [row][head] (NULL: to out and lse)
   int64_t n_tokens, q_row, q_head, out_row, out_head;
   int32_t n, heads, group, type, window, layer;  // group: query heads a kv head
   FastDiv by_group;
@@ -234,6 +239,13 @@ struct KvMaps {
   CUtensorMap k, v;
   int32_t rows;
 };
+// Where the part of CTA `cta` of a unit that it begins (else: goes on with) lies among the parts, in floats: for each row tile of 128
+// rows [fours of values][row][4], then maxima and sums.
+__host__ __device__ inline int64_t rows_part(int32_t cta, bool begins, int32_t tiles, int32_t tile, int32_t dp) {
+  return (int64_t)((2 * cta + begins) * tiles + tile) * 128 * (dp + 2);
+}
+// Joins the parts of units that several CTAs of the launch before shared.
+cudaError_t launch_kv_join(const KvView& c, const KvRowsCall& a, const KvAttendScratch& w, int num_sms, cudaStream_t st);
 // Floats of KvAttendScratch::parts: two parts a CTA, of 256 or (head_dim above 128) 128 rows.
 inline size_t kv_rows_parts(const KvView& c, int num_sms) {
   const int dp = (c.dim + 63) / 64 * 64;

@@ -116,17 +116,31 @@ __device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
-// Values d .. d + 3 of a head's result, times f; zero: 0 in their place.
+// Weights of a row's own result, whose lse is given, and of the one of the tokens before (q), and the lse of both.
+struct Both {
+  float own, before, lse;
+};
+__device__ __forceinline__ Both with_before(const KvQuery& a, int32_t i, int32_t head, float lse) {
+  const float his = a.pre_lse[(int64_t)i * a.heads + head], most = fmaxf(lse, his);
+  const float p = exp2_fast((lse - most) * kLog2e), q = exp2_fast((his - most) * kLog2e), by = __fdividef(1.f, p + q);
+  return {p * by, q * by, most + __logf(p + q)};
+}
+// Values d .. d + 3 of a head's result, times f; zero: 0 in their place.  t, z: what the row's sums are relative to, and its sum of
+// exp.
+template <int KIND>
 __device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_t i, int32_t head, int32_t d, float4 v,
-                                       float f, bool zero) {
+                                       float f, float t, float z, bool zero) {
   if (d >= c.dim) return;  // (dim is a multiple of 8)
   if (zero) v = make_float4(0.f, 0.f, 0.f, 0.f), f = 0.f;
+  v.x *= f, v.y *= f, v.z *= f, v.w *= f;
   if (a.skip && a.skip[i] > 0) {
-    *(float4*)(a.own + ((int64_t)i * a.heads + head) * c.dim + d) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-    return;
+    const Both b = with_before(a, i, head, zero ? -INFINITY : log_sum<KIND>(t, z));
+    const float4 x = *(const float4*)(a.pre + ((int64_t)i * a.heads + head) * c.dim + d);
+    v.x = fmaf(x.x, b.before, v.x * b.own), v.y = fmaf(x.y, b.before, v.y * b.own);
+    v.z = fmaf(x.z, b.before, v.z * b.own), v.w = fmaf(x.w, b.before, v.w * b.own);
   }
-  const uint32_t x = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.x * f, v.y * f) : pack<P2P_KV_F16>(v.x * f, v.y * f);
-  const uint32_t y = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.z * f, v.w * f) : pack<P2P_KV_F16>(v.z * f, v.w * f);
+  const uint32_t x = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.x, v.y) : pack<P2P_KV_F16>(v.x, v.y);
+  const uint32_t y = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.z, v.w) : pack<P2P_KV_F16>(v.z, v.w);
   uint16_t* to = (uint16_t*)a.out + i * a.out_row + head * a.out_head + d;
   if (a.out_fours) {
     *(uint2*)to = make_uint2(x, y);
@@ -135,10 +149,12 @@ __device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_
     to[2] = (uint16_t)y, to[3] = (uint16_t)(y >> 16);
   }
 }
-
-__device__ __forceinline__ void store_lse(const KvQuery& a, int32_t i, int32_t head, float lse) {
-  float* const to = a.skip && a.skip[i] > 0 ? a.own_lse : a.lse;
-  if (to) to[(int64_t)i * a.heads + head] = lse;
+template <int KIND>
+__device__ __forceinline__ void store_lse(const KvQuery& a, int32_t i, int32_t head, float t, float z, bool zero) {
+  if (!a.lse) return;
+  float lse = zero ? -INFINITY : log_sum<KIND>(t, z);
+  if (a.skip && a.skip[i] > 0) lse = with_before(a, i, head, lse).lse;
+  a.lse[(int64_t)i * a.heads + head] = lse;
 }
 
 // Byte offset in a warp's tile of piece `piece` of row `row`: the pieces of eight rows that ldmatrix reads together lie
@@ -679,8 +695,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
         } else {
           const int32_t q_head = head0 + beside * group + h8;
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
-          store4(c, a, u.i, q_head, d, v, __fdividef(v_scale, z), empty);
-          if (d == 0) store_lse(a, u.i, q_head, empty ? -INFINITY : log_sum<KIND>(t, z));
+          store4<KIND>(c, a, u.i, q_head, d, v, __fdividef(v_scale, z), t, z, empty);
+          if (d == 0) store_lse<KIND>(a, u.i, q_head, t, z, empty);
         }
       }
       if (whole || b + 1 < NB) __syncthreads();  // the sums' room is free again
@@ -795,8 +811,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
               const int beside = at[i] / S::kHeads;
               const int32_t q_head = head0 + beside * group + at[i] % S::kHeads;
               const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
-              store4(c, a, u.i, q_head, d[i], v[i], __fdividef(v_scale, z[i]), false);
-              if (d[i] == 0) store_lse(a, u.i, q_head, log_sum<KIND>(t[i], z[i]));
+              store4<KIND>(c, a, u.i, q_head, d[i], v[i], __fdividef(v_scale, z[i]), t[i], z[i], false);
+              if (d[i] == 0) store_lse<KIND>(a, u.i, q_head, t[i], z[i], false);
             } else {
               *(float4*)(joined + at[i] * DP + d[i]) = v[i];
               if (d[i] == 0) joined[part_heads * DP + at[i]] = t[i], joined[part_heads * (DP + 1) + at[i]] = z[i];

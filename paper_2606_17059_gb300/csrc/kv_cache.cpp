@@ -259,6 +259,7 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
                arrived = part(sizeof(int32_t) * 4 * p2p::KvAttendScratch::kCtasPerSm * sms), zero = at,
                start = part(4 * (S + 1)), first = part(4 * S), cut = part(4 * S),
                list = part(4 * N), jobs = part(sizeof(p2p::KvJob) * std::max(S, N)),
+               joins = part(sizeof(p2p::KvJoin) * sms),
                parts = part(sizeof(float) * std::max(p2p::kv_attend_parts(c, sms), p2p::kv_rows_parts(c, sms)));
   cudaError_t e = cudaSuccess;
   if (const cudaMemPool_t pool = scratch_pool(dev, &e)) e = cudaMallocFromPoolAsync(&n->scratch, at, pool, nullptr);
@@ -289,6 +290,7 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   n->s.jobs = (p2p::KvJob*)(p + jobs);
   n->w.parts = (float*)(p + parts);
   n->w.arrived = (int32_t*)(p + arrived);
+  n->w.joins = (p2p::KvJoin*)(p + joins);
   n->w.err = n->s.err;
   make_maps(c, n->maps);
   *out = n;
@@ -544,12 +546,13 @@ int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   a.offsets = offsets;
   a.n_tokens = n_tokens;
   CK(launch_rows(h->c, h->maps, &a, h->w, h->num_sms, h->stream));
-  h->launches += 1;
+  CK(p2p::launch_kv_join(h->c, a, h->w, h->num_sms, h->stream));
+  h->launches += 2;
   return P2P_OK;
 }
 
-// Where the parts of attend_shared's work lie: each row's result over its own tokens, what the groups share, and what of a row
-// its group works off.
+// Where the parts of attend_shared's work lie: each row's result over its group's tokens, what the groups share, and the tokens of
+// each row that its group works off.
 struct SharedWork {
   size_t lse, spans, skip, bytes;
   SharedWork(const p2p::KvView& c, int32_t n, int32_t n_heads) {
@@ -575,31 +578,33 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   if (n_groups < 0 || n_groups > n) return fail(h, P2P_E_INVAL, "n_groups: at most n");
   if (n == 0) return P2P_OK;
   if ((n_groups > 0 && !groups) || !work) return fail(h, P2P_E_INVAL, "NULL device pointer");
-  if ((uintptr_t)work % 16) return fail(h, P2P_E_INVAL, "work must start on a 16-byte boundary");
+  if ((uintptr_t)work % 32) return fail(h, P2P_E_INVAL, "work must start on a 32-byte boundary");
   if (int rc = check_rows(h, n, q, n_heads, out, out_row_stride, out_head_stride, lse)) return rc;
   DeviceGuard g(h->device);
   const SharedWork at(h->c, n, n_heads);
-  float *own = (float*)work, *own_lse = (float*)((char*)work + at.lse);
+  float *pre = (float*)work, *pre_lse = (float*)((char*)work + at.lse);
   int4* spans = (int4*)((char*)work + at.spans);
   int32_t* skip = (int32_t*)((char*)work + at.skip);
-  // What the groups share; every row's other tokens; the shared ones and both together.
-  CK(p2p::launch_kv_share(h->c, h->s.err, n, seq, n_groups, groups, window, skip, spans, h->stream));
   p2p::KvQuery rest = query_of(layer, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out,
                                out_row_stride, out_head_stride, lse);
-  rest.skip = skip;
-  rest.own = own;
-  rest.own_lse = own_lse;
+  if (n_groups > 0) {
+    // What the groups share, and the attention over it; then every row's other tokens, put together with that.
+    CK(p2p::launch_kv_share(h->c, h->s.err, n, seq, n_groups, groups, window, skip, spans, h->stream));
+    p2p::KvRowsCall a = rows_call(h, layer, n_groups, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window,
+                                  out, out_row_stride, out_head_stride, lse);
+    a.groups = groups;
+    a.spans = spans;
+    a.pre = pre;
+    a.pre_lse = pre_lse;
+    a.n_tokens = n;
+    CK(launch_rows(h->c, h->maps, &a, h->w, h->num_sms, h->stream));
+    CK(p2p::launch_kv_join(h->c, a, h->w, h->num_sms, h->stream));
+    h->launches += 3;
+    rest.skip = skip;
+    rest.pre = pre;
+    rest.pre_lse = pre_lse;
+  }
   CK(launch_attend(h->c, &rest, h->w, h->num_sms, h->stream));
-  h->launches += 2;
-  if (n_groups == 0) return P2P_OK;
-  p2p::KvRowsCall a = rows_call(h, layer, n_groups, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out,
-                                out_row_stride, out_head_stride, lse);
-  a.groups = groups;
-  a.spans = spans;
-  a.own = own;
-  a.own_lse = own_lse;
-  a.n_tokens = n;
-  CK(launch_rows(h->c, h->maps, &a, h->w, h->num_sms, h->stream));
   h->launches += 1;
   return P2P_OK;
 }

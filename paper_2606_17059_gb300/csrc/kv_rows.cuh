@@ -13,11 +13,12 @@
 // maximum that lags the running one by at most 2^kLag (see Type), so that O is rarely rescaled.
 //
 // A CTA of the persistent grid takes an equal, contiguous share of all units' steps (a step: kBt tokens); a unit that several
-// CTAs share goes to scratch in parts, and the CTA that brings the last one joins them in their order, so results do not
-// depend on timing.  Warps: softmax (four a row tile), copies (four), and one each for the products and the schedule, two that
+// CTAs share goes to scratch in parts, which a launch after this one joins in their order (kv_join.cu).  Warps: softmax (four a row tile), copies (four), and one each for the products and the schedule, two that
 // look for infinities and NaN among the values of tokens which not all rows see: 0 * NaN is NaN, so such values are taken
 // out before the product and added to the rows that do see them at the end.
 #pragma once
+#include <type_traits>
+
 #include "kv_math.cuh"
 #include "kv_values.cuh"
 
@@ -61,10 +62,10 @@ struct RowsUnit {
   int32_t parts, part, c0;   // of the unit, where it is shared: this piece's number and the first one's CTA
 };
 struct RowsShared {
-  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], team[2], drain, raw[4][2];
+  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], drain, raw[4][2];
   RowsUnit unit[kRing];
   uint32_t sums[16];
-  int32_t tmem, dead, last[2];
+  int32_t tmem, dead;
   int32_t poison[kRing];     // whether values were taken out of the unit's steps
 };
 static_assert(sizeof(RowsShared) <= 2048);
@@ -271,30 +272,24 @@ __device__ __forceinline__ uint32_t share_of(uint32_t x, uint32_t y, uint32_t z)
   return q;
 }
 
-// Values d .. d + 15 of a row's result: o, times f, and the row's own part times `other`.
-__device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_t row, int32_t head, int32_t d, const float* o, float f,
-                                    float other) {
-  uint16_t* const out = (uint16_t*)a.out + row * a.out_row + head * a.out_head + d;
+// Values d .. d + 15 of a row's result: o, times f.  (Whole sectors where that is to be had, as the lanes' rows are apart.)
+__device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_t row, int32_t head, int32_t d, const float* o, float f) {
   const bool half = d + 8 >= c.dim;  // (head_dim is a multiple of 8)
-  float v[16];
+  if (a.pre) {
+    uint32_t b[16];
 #pragma unroll
-  for (int k = 0; k < 16; ++k) v[k] = o[k] * f;
-  if (a.own) {
-    const float* const own = a.own + (row * a.heads + head) * c.dim + d;
-#pragma unroll
-    for (int k = 0; k < 16; k += 4) {
-      if (k >= 8 && half) break;
-      const float4 x = *(const float4*)(own + k);
-      v[k] = fmaf(x.x, other, v[k]), v[k + 1] = fmaf(x.y, other, v[k + 1]);
-      v[k + 2] = fmaf(x.z, other, v[k + 2]), v[k + 3] = fmaf(x.w, other, v[k + 3]);
-    }
+    for (int k = 0; k < 16; ++k) b[k] = __float_as_uint(o[k] * f);
+    float* const to = a.pre + (row * a.heads + head) * c.dim + d;
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), P2P_I8(b, 0) : "memory");
+    if (!half) asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 8), P2P_I8(b, 8) : "memory");
+    return;
   }
+  uint16_t* const out = (uint16_t*)a.out + row * a.out_row + head * a.out_head + d;
   uint32_t b[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    b[k] = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v[2 * k], v[2 * k + 1]) : pack<P2P_KV_F16>(v[2 * k], v[2 * k + 1]);
+    b[k] = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(o[2 * k] * f, o[2 * k + 1] * f) : pack<P2P_KV_F16>(o[2 * k] * f, o[2 * k + 1] * f);
   if (a.out32 && !half) {
-    // (Whole sectors, as the lanes' rows are apart.)
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out), P2P_I8(b, 0) : "memory");
   } else {
 #pragma unroll
@@ -363,7 +358,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   // (Nothing so far touches memory: it runs beside the end of the kernel before.)
   if (threadIdx.x == 0) {
     for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 1 : 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
-    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], 4), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1), bar_init(sh.team[i], 4);
+    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], 4), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1);
     for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
     for (int i = 0; i < 8; ++i) bar_init(sh.raw[i / 2][i & 1], 1);
     bar_init(sh.drain, 1);
@@ -395,6 +390,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   // (Four at least, so that no two CTAs' shares begin at the same step inside a unit.)
   const uint32_t ctas = min(gridDim.x, max(1u, total / 4));
   if (total == 0 || blockIdx.x >= ctas) {
+    if (threadIdx.x == 0) w.joins[blockIdx.x].parts = 0;
     if (warp == S::kSoft + 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem));
     return;
   }
@@ -413,15 +409,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;      // (tensor memory's lanes 32 * (warp % 4) .., from bit 16 on)
     const uint32_t s_at = tmem + lanes + tile * kBt, o_at = tmem + lanes + S::kOCol + tile * DP;
     char* const q_tile = q_room + tile * S::kQTile;
-    uint32_t s_phase = 0, o_phase = 0, team_phase = 0;
-    // The row tile's four warps meet (with the limit that all waits have).
-    const auto meet = [&]() {
-      __syncwarp();
-      if (lane == 0) bar_arrive(sh.team[tile]);
-      if (!bar_wait(sh.team[tile], team_phase, sh)) return false;
-      team_phase ^= 1;
-      return true;
-    };
+    uint32_t s_phase = 0, o_phase = 0;
     float mul = 0.f;  // logit (in log2) of a sum of products
     // Where row x of the unit's tile is.
     const auto row_of_q = [&](const RowsUnit& u, int x, int64_t& row, int32_t& head) {
@@ -441,42 +429,59 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       }
       mul = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
       const uint32_t flip = minus ? 0x80008000u : 0;
-      const auto at = [&](int x) -> const uint16_t* {
+      const uint16_t* of_lane = nullptr;  // a lane has where one of the warp's rows is
+      if (tile * 128 + own + lane < u.rows) {
         int64_t row;
         int32_t head;
-        row_of_q(u, own + x, row, head);
-        return tile * 128 + own + x < u.rows && piece * 8 < c.dim ? (const uint16_t*)a.q + row * a.q_row + head * a.q_head + piece * 8
-                                                                  : nullptr;
+        row_of_q(u, own + lane, row, head);
+        of_lane = (const uint16_t*)a.q + row * a.q_row + head * a.q_head;
+      }
+      const auto at = [&](int x) -> const uint16_t* {
+        const uint16_t* const p = (const uint16_t*)__shfl_sync(~0u, (unsigned long long)of_lane, x);
+        return p && piece * 8 < c.dim ? p + piece * 8 : nullptr;
       };
-      const auto place = [&](int first, uint4 v) {  // rows first .. of the warp's
-        uint32_t b[4] = {v.x, v.y, v.z, v.w};
+      // N times kAtOnce rows, from x0 of the warp's on.
+      const auto place = [&](int x0, auto& v, auto count) {
+        constexpr int N = decltype(count)::value;
         if (KIND == P2P_KV_E4M3) {
           // In f16, scaled by a power of two so that the row's largest is in [2^14, 2^15): exact but for what is below 2^-28 of
-          // it.
-          float largest = 0.f;
+          // it.  (Magnitudes compare as their bits do.  Exchanges of all rows together, as each waits for the one before.)
+          uint32_t most[N];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 y = two_halves(b[i], a.type);
-            largest = fmaxf(largest, fmaxf(fabsf(y.x), fabsf(y.y)));
+          for (int k = 0; k < N; ++k) {
+            const uint32_t m = __vmaxu2(__vmaxu2(v[k].x & 0x7fff7fffu, v[k].y & 0x7fff7fffu), __vmaxu2(v[k].z & 0x7fff7fffu, v[k].w & 0x7fff7fffu));
+            most[k] = max(m & 0xffffu, m >> 16);
           }
 #pragma unroll
-          for (int d = kLanes / 2; d; d >>= 1) largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, d));
-          const int e = largest > 0.f && largest < INFINITY ? max(ilogbf(largest), -112) - 14 : 0;
-          const float down = ldexpf(1.f, -e), of_row = ldexpf(unit, e);
+          for (int d = kLanes / 2; d; d >>= 1)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 y = two_halves(b[i], a.type);
-            b[i] = pack<KIND>(y.x * down, y.y * down);
+            for (int k = 0; k < N; ++k) most[k] = max(most[k], __shfl_xor_sync(~0u, most[k], d));
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            const float largest = two_halves(most[k], a.type).x;
+            // (Of 0, an infinity or NaN: as they are.)
+            const int e = largest > 0.f && largest < INFINITY ? max((int)(__float_as_uint(largest) >> 23) - 127, -112) - 14 : 0;
+            const float down = __uint_as_float((127 - e) << 23);
+            const int of_lane_row = lane - (x0 + k * kAtOnce), his = __shfl_sync(~0u, e, of_lane_row * kLanes & 31);
+            if (of_lane_row >= 0 && of_lane_row < kAtOnce) mul = fmaxf(unit * __uint_as_float((127 + his) << 23), 0x1p-120f);
+            uint32_t b[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 y = two_halves(b[i], a.type);
+              b[i] = pack<KIND>(y.x * down, y.y * down);
+            }
+            v[k] = make_uint4(b[0], b[1], b[2], b[3]);
           }
-          const float got = __shfl_sync(~0u, of_row, (lane - first) * kLanes & 31);
-          if (lane >= first && lane < first + kAtOnce) mul = fmaxf(got, 0x1p-120f);
         }
-        const int x = own + first + lane / kLanes;
-        if (piece * 8 < dim16)
-          *(uint4*)(q_tile + (piece / 8) * (128 * 128) + x * 128 + ((piece & 7) ^ (x & 7)) * 16) =
-              make_uint4(b[0] ^ flip, b[1] ^ flip, b[2] ^ flip, b[3] ^ flip);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const int x = own + x0 + k * kAtOnce + lane / kLanes;
+          if (piece * 8 < dim16)
+            *(uint4*)(q_tile + (piece / 8) * (128 * 128) + x * 128 + ((piece & 7) ^ (x & 7)) * 16) =
+                make_uint4(v[k].x ^ flip, v[k].y ^ flip, v[k].z ^ flip, v[k].w ^ flip);
+        }
       };
-      constexpr int kLoads = KIND == P2P_KV_E4M3 ? 4 : 8;
+      constexpr int kLoads = DP == 128 && KIND != P2P_KV_E4M3 ? 16 : 8;
       if (a.q16) {
 #pragma unroll 1
         for (int x0 = 0; x0 < 32; x0 += kAtOnce * kLoads) {
@@ -486,16 +491,15 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             const uint16_t* const p = at(x0 + k * kAtOnce + lane / kLanes);
             v[k] = p ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
           }
-#pragma unroll
-          for (int k = 0; k < kLoads; ++k) place(x0 + k * kAtOnce, v[k]);
+          place(x0, v, std::integral_constant<int, kLoads>());
         }
       } else {
 #pragma unroll 1
-        for (int x = 0; x < 32; x += kAtOnce) {
-          const uint16_t* const p = at(x + lane / kLanes);
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (p) v = make_uint4(p[0] | p[1] << 16, p[2] | p[3] << 16, p[4] | p[5] << 16, p[6] | p[7] << 16);
-          place(x, v);
+        for (int x0 = 0; x0 < 32; x0 += kAtOnce) {
+          const uint16_t* const p = at(x0 + lane / kLanes);
+          uint4 v[1] = {make_uint4(0, 0, 0, 0)};
+          if (p) v[0] = make_uint4(p[0] | p[1] << 16, p[2] | p[3] << 16, p[4] | p[5] << 16, p[6] | p[7] << 16);
+          place(x0, v, std::integral_constant<int, 1>());
         }
       }
       async_fence();
@@ -526,74 +530,33 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (sh.poison[now]) add_poison_of<KIND, kBt>(c, a, u, o_at, from, to, valid ? begin : INT32_MAX, end);
           }
           const float2 z2 = parts_of(sum);
-          float high = top, z = z2.x + z2.y;
+          const float z = z2.x + z2.y;
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h] : 1.f;
-          constexpr int kPart = 128 * (DP + 2);  // floats of a row tile's part: [value][row], then maxima and sums
-          const auto part_of = [&](int32_t k) { return w.parts + (int64_t)((2 * (u.c0 + k) + (k == 0)) * kTiles + tile) * kPart + r; };
-          const int32_t parts = u.parts;
-          // First this piece's, to where it goes; then, by the CTA that comes last, all of them.
+          float* const part = w.parts + rows_part(u.c0 + u.part, u.part == 0, kTiles, tile, DP);
+          const bool keep = u.parts > 1;
+          float f = 0.f;
+          if (keep) {
+            part[DP * 128 + r] = top, part[(DP + 1) * 128 + r] = z;
+          } else if (valid) {
+            f = z > 0.f || z != z ? v_scale / z : 0.f;
+            float* const lse = a.pre ? a.pre_lse : a.lse;
+            if (lse) lse[row * a.heads + head] = z == 0.f ? -INFINITY : log_sum<KIND>(top, z);
+          }
 #pragma unroll 1
-          for (int turn = 0; turn < 2; ++turn) {
-            const bool keep = turn == 0 && parts > 1;
-            float* const mine = part_of(u.part);
-            float f = 0.f, other = 0.f;
+          for (int32_t d = 0; d < dim16; d += 32) {
+            float o[32] = {};
+            if (to > from) {
+              tmem_load((uint32_t*)o, o_at + d);
+              tmem_loaded();
+            }
             if (keep) {
-              mine[DP * 128] = high, mine[(DP + 1) * 128] = z;
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                if (d + 4 * i < dim16) ((float4*)part)[r + (d / 4 + i) * 128] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             } else if (valid) {
-              f = z > 0.f || z != z ? v_scale / z : 0.f;
-              float lse = z == 0.f ? -INFINITY : log_sum<KIND>(high, z);
-              if (a.own) {  // with the row's own tokens
-                const float his = a.own_lse[row * a.heads + head], most = fmaxf(lse, his);
-                const float p = exp2_fast((lse - most) * kLog2e), q = exp2_fast((his - most) * kLog2e);
-                const float by = __fdividef(1.f, p + q);
-                f *= p * by, other = q * by;
-                lse = most + __logf(p + q);
-              }
-              if (a.lse) a.lse[row * a.heads + head] = lse;
+              put(c, a, row, head, d, o, f);
+              if (d + 16 < dim16) put(c, a, row, head, d + 16, o + 16, f);
             }
-            const float ref = high == -INFINITY ? 0.f : high;
-#pragma unroll 1
-            for (int32_t d = 0; d < dim16; d += 16) {
-              float o[16] = {};
-              if (turn == 1) {
-#pragma unroll 1
-                for (int32_t k = 0; k < parts; ++k) {
-                  const float* const p = part_of(k) + d * 128;
-                  const float fade = exp2_fast(__ldcg(part_of(k) + DP * 128) - ref);
-                  float v[16];
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) v[i] = __ldcg(p + i * 128);
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) o[i] = fmaf(v[i], fade, o[i]);
-                }
-              } else if (to > from) {
-                tmem_load16((uint32_t*)o, o_at + d);
-                tmem_loaded();
-              }
-              if (keep) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mine[(d + i) * 128] = o[i];
-              } else if (valid) {
-                put(c, a, row, head, d, o, f, other);
-              }
-            }
-            if (!keep) break;
-            if (!meet()) return;
-            if (r == 0) {
-              int32_t* const arrived = w.arrived + u.c0 * kTiles + tile;
-              sh.last[tile] = add_acq_rel(arrived, 1) == parts - 1;
-              if (sh.last[tile]) *arrived = 0;  // for the next launch
-            }
-            if (!meet()) return;
-            const bool last = sh.last[tile];
-            if (!meet()) return;
-            if (!last) break;
-            high = -INFINITY, z = 0.f;
-#pragma unroll 1
-            for (int32_t k = 0; k < parts; ++k) high = fmaxf(high, __ldcg(part_of(k) + DP * 128));
-#pragma unroll 1
-            for (int32_t k = 0; k < parts; ++k)
-              z += exp2_fast(__ldcg(part_of(k) + DP * 128) - (high == -INFINITY ? 0.f : high)) * __ldcg(part_of(k) + (DP + 1) * 128);
           }
         }
         // (Loads of tensor memory are done before the next products may write there: P of this unit is announced later.)
@@ -1018,6 +981,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     const int from = __ffs(__ballot_sync(~0u, x0 < x)) - 1;
     x = __shfl_sync(~0u, x - of_warp, from);
     bool alive = true, found = false;
+    KvJoin join = {};  // the unit that the next CTA goes on with
     // 32 items at a time, a lane each.
 #pragma unroll 1
     for (int32_t i0 = from * per_warp; alive && x < x1 && i0 < a.n; i0 += 32) {
@@ -1117,6 +1081,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               u.c0 = (int32_t)first - 1;
               u.parts = (int32_t)(end - first) + 1;
               u.part = blockIdx.x - u.c0;
+              if (u.part == 0) join = {u.row, u.rows, u.g0, u.h, u.parts};
             }
             alive = emit(u);
           }
@@ -1130,6 +1095,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         if (x < x1) x = x_next;
       }
     }
+    if (lane == 0) w.joins[blockIdx.x] = join;
     if (alive) {
       RowsUnit u = {};
       emit(u);
