@@ -143,10 +143,11 @@ cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p
 void make_maps(const p2p::KvView& c, p2p::KvMaps& m) {
   m.rows = 0;
   const bool eight = c.type == P2P_KV_E4M3;
-  // Tokens of a copy: a power of two that divides a page (and so lies in one), at most what a warp, or a step, takes.
+  // Tokens of a copy: a power of two that divides a page (and so lies in one), at most what a warp takes of a step; copies go to
+  // whole 128 bytes (1,024 where their pieces are turned).
   uint32_t rows = c.page & -c.page;
-  rows = std::min(rows, eight ? (c.dim > 128 ? 16u : 32u) : (c.dim > 128 ? 64u : 128u));
-  if (rows < 8) return;
+  rows = std::min(rows, c.dim > 128 ? 16u : 32u);
+  if (eight ? rows * c.dim % 128 != 0 : rows < 8) return;
   void* entry = nullptr;
   cudaDriverEntryPointQueryResult found;
   if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found) != cudaSuccess ||

@@ -9,19 +9,34 @@
 namespace p2p {
 namespace {
 
-constexpr int kThreads = 128, kRowsOfWarp = 4;
+constexpr int kThreads = 128, kRowsOfWarp = 4, kMostCtas = 1024;
 
-__global__ void __launch_bounds__(kThreads) join_kernel(KvView c, KvRowsCall a, KvAttendScratch w, int32_t dp, int32_t tiles) {
+__global__ void __launch_bounds__(kThreads)
+    join_kernel(KvView c, KvRowsCall a, KvAttendScratch w, int32_t ctas, int32_t dp, int32_t tiles) {
+  __shared__ int32_t units[kMostCtas];
+  __shared__ int32_t count;
   begin_kernel();
-  const KvJoin u = w.joins[blockIdx.x];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tile = blockIdx.y;
-  if (u.parts == 0 || u.rows <= tile * 128) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // The units that there are, in the same order in every CTA.
+  if (warp == 0) {
+    int32_t n = 0;
+    for (int i0 = 0; i0 < ctas; i0 += 32) {
+      const bool some = i0 + lane < ctas && w.joins[i0 + lane].parts > 0;
+      const uint32_t m = __ballot_sync(~0u, some);
+      if (some) units[n + __popc(m & ((1u << lane) - 1))] = i0 + lane;
+      n += __popc(m);
+    }
+    if (lane == 0) count = n;
+  }
+  __syncthreads();
   // (The maximum is held less 2^kUp, see Type.)
   const float up = c.type == P2P_KV_BF16 ? Type<P2P_KV_BF16>::kUp : Type<P2P_KV_F16>::kUp;
-  const float v_scale = c.type == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h] : 1.f;
-  const int columns = (c.dim + 31) / 32, items = 128 / kRowsOfWarp * columns;
-  const auto part_of = [&](int32_t k) { return w.parts + rows_part(blockIdx.x + k, k == 0, tiles, tile, dp); };
-  for (int x = blockIdx.z * (kThreads / 32) + warp; x < items; x += gridDim.z * (kThreads / 32)) {
+  const int columns = (c.dim + 31) / 32, each = tiles * (128 / kRowsOfWarp) * columns;  // of a unit
+  for (int y = blockIdx.x * (kThreads / 32) + warp; y < count * each; y += gridDim.x * (kThreads / 32)) {
+    const int c0 = units[y / each], x = y % (each / tiles), tile = y % each / (each / tiles);
+    const KvJoin u = w.joins[c0];
+    const float v_scale = c.type == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h] : 1.f;
+    const auto part_of = [&](int32_t k) { return w.parts + rows_part(c0 + k, k == 0, tiles, tile, dp); };
     const int r = x / columns * kRowsOfWarp + lane / 8, d = x % columns * 32 + lane % 8 * 4;
     if (tile * 128 + r >= u.rows || d >= c.dim) continue;
     float m = -INFINITY, z = 0.f;
@@ -53,9 +68,9 @@ __global__ void __launch_bounds__(kThreads) join_kernel(KvView c, KvRowsCall a, 
         o.z = fmaf(po[k].z, fade, o.z), o.w = fmaf(po[k].w, fade, o.w);
       }
     }
-    const uint32_t y = u.g0 + tile * 128 + r, t = a.by_group.div(y);
+    const uint32_t at = u.g0 + tile * 128 + r, t = a.by_group.div(at);
     const int64_t row = u.row + t;
-    const int32_t head = u.h * a.group + (int32_t)(y - t * a.group);
+    const int32_t head = u.h * a.group + (int32_t)(at - t * a.group);
     const float f = z > 0.f || z != z ? v_scale / z : 0.f;
     if (d == 0)
       if (float* const lse = a.pre ? a.pre_lse : a.lse)
@@ -81,8 +96,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(KvView c, KvRowsCall a, 
 
 cudaError_t launch_kv_join(const KvView& c, const KvRowsCall& a, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   const int dp = (c.dim + 63) / 64 * 64, tiles = dp <= 128 ? 2 : 1;
-  const dim3 grid((unsigned)num_sms, (unsigned)tiles, 8);
-  return launch_early(join_kernel, grid, kThreads, 0, st, c, a, w, (int32_t)dp, (int32_t)tiles);
+  if (num_sms > kMostCtas) return cudaErrorInvalidConfiguration;
+  return launch_early(join_kernel, dim3(8 * num_sms), kThreads, 0, st, c, a, w, (int32_t)num_sms, (int32_t)dp, (int32_t)tiles);
 }
 
 }  // namespace p2p

@@ -60,13 +60,15 @@ struct RowsUnit {
   int32_t j0, j1;            // steps of this piece
   int32_t t0[2], t1[2];      // of them, those of each row tile
   int32_t parts, part, c0;   // of the unit, where it is shared: this piece's number and the first one's CTA
+  int32_t split;             // 1: both row tiles have the same rows, and every other step
 };
 struct RowsShared {
-  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], drain, raw[4][2];
+  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], q_empty[2], pair, pair_done, drain, raw[4][2];
   RowsUnit unit[kRing];
   uint32_t sums[16];
   int32_t tmem, dead;
   int32_t poison[kRing];     // whether values were taken out of the unit's steps
+  float pair_top[128], pair_sum[128];  // of the second tile's rows, where both have the same
 };
 static_assert(sizeof(RowsShared) <= 2048);
 
@@ -263,15 +265,6 @@ struct RowsCost {
     return r * base + (uint32_t)((uint64_t)r * (r + 1) * slope >> (9 + shift)) + (j - r) * most;
   }
 };
-// floor(x * y / z), y at most 65,536 and the result at most y.
-__device__ __forceinline__ uint32_t share_of(uint32_t x, uint32_t y, uint32_t z) {
-  const uint64_t n = (uint64_t)x * y;
-  uint32_t q = (uint32_t)__fdividef((float)x * (float)y, (float)z);
-  while ((uint64_t)q * z > n) --q;
-  while ((uint64_t)(q + 1) * z <= n) ++q;
-  return q;
-}
-
 // Values d .. d + 15 of a row's result: o, times f.  (Whole sectors where that is to be had, as the lanes' rows are apart.)
 __device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_t row, int32_t head, int32_t d, const float* o, float f) {
   const bool half = d + 8 >= c.dim;  // (head_dim is a multiple of 8)
@@ -297,18 +290,18 @@ __device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_
       if (k < 8 || !half) out[k] = (uint16_t)(b[k / 2] >> (k & 1) * 16);
   }
 }
-// Infinities and NaN that were taken out of the values of steps j0 .. j1 - 1 (of those that not all rows see): added to the sums of the
+// Infinities and NaN that were taken out of the values of `every` step from j0 to j1 (of those that not all rows see): added to the sums of the
 // rows that see them, tokens begin .. end - 1.  By a warp, whose 32 rows of sums are at o_at.  Rarely needed, so it is small, not
 // fast.
 template <int KIND, int BT>
 __device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall& a, const RowsUnit& u, uint32_t o_at, int32_t j0, int32_t j1,
-                                              int32_t begin, int32_t end) {
+                                              int32_t every, int32_t begin, int32_t end) {
   const int lane = threadIdx.x & 31;
   constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8;  // of a piece
 #pragma unroll 1
   for (int32_t p = max(u.begin, j0 * BT); p < min(u.end, j1 * BT); ++p) {
     const int32_t j = p / BT;
-    if (!(j * BT < u.all_begin || (j + 1) * BT > u.all_end)) continue;
+    if (!(j * BT < u.all_begin || (j + 1) * BT > u.all_end) || (j - j0) % every) continue;
     const uint32_t e = c.by_page.div(p);
     const int32_t page = row_of(c, u.seq)[e];
     if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
@@ -355,12 +348,17 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   RowsShared& sh = *(RowsShared*)(raws + S::kRaws * S::kRaw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+  // Queries are copied into shared memory by the warps that look for infinities, where they need no change of type or sign and
+  // lie on 16-byte boundaries; else by the softmax warps.
+  const bool helped = KIND != P2P_KV_E4M3 && a.q16 && a.scale >= 0.f;
   // (Nothing so far touches memory: it runs beside the end of the kernel before.)
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 1 : 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
-    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], 4), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1);
+    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 4 : 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
+    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], helped ? 64 : 4), bar_init(sh.q_empty[i], 1), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1);
     for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
     for (int i = 0; i < 8; ++i) bar_init(sh.raw[i / 2][i & 1], 1);
+    bar_init(sh.pair, 4);
+    bar_init(sh.pair_done, 4);
     bar_init(sh.drain, 1);
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -377,13 +375,18 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   constexpr int kAll = S::kThreads / 32;
   const int32_t per_warp = ((a.n + kAll - 1) / kAll + 31) & ~31;
   uint32_t sum_of = 0;
+  // (The schedule's warp has the first items, and keeps them.)
+  const int turn = warp >= S::kSoft + 5 ? warp - (S::kSoft + 5) : warp + 3;
+  RowsItem own = {};
+  uint32_t own_cost = 0;
 #pragma unroll 1
-  for (int32_t i = warp * per_warp + lane; i < min(a.n, (warp + 1) * per_warp); i += 32) {
-    const RowsItem it = rows_item<S>(c, a, i, blockIdx.x == 0 ? w.err : nullptr);
-    if (it.tiles) sum_of += c.heads * RowsCost<S>(a, it)(it.tiles);
+  for (int32_t i = turn * per_warp + lane; i < min(a.n, (turn + 1) * per_warp); i += 32) {
+    own = rows_item<S>(c, a, i, blockIdx.x == 0 ? w.err : nullptr);
+    own_cost = own.tiles ? RowsCost<S>(a, own)(own.tiles) : 0;
+    sum_of += c.heads * own_cost;
   }
   sum_of = __reduce_add_sync(~0u, sum_of);
-  if (lane == 0) sh.sums[warp] = sum_of;
+  if (lane == 0) sh.sums[turn] = sum_of;
   __syncthreads();
   after_sync();
   const uint32_t of_warp = lane < kAll ? sh.sums[lane] : 0, total = __reduce_add_sync(~0u, of_warp);
@@ -413,7 +416,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     float mul = 0.f;  // logit (in log2) of a sum of products
     // Where row x of the unit's tile is.
     const auto row_of_q = [&](const RowsUnit& u, int x, int64_t& row, int32_t& head) {
-      const uint32_t y = u.g0 + tile * 128 + x, t = a.by_group.div(y);
+      const uint32_t y = u.g0 + (u.split ? 0 : tile * 128) + x, t = a.by_group.div(y);
       row = u.row + t;
       head = u.h * a.group + (int32_t)(y - t * a.group);
     };
@@ -430,7 +433,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       mul = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
       const uint32_t flip = minus ? 0x80008000u : 0;
       const uint16_t* of_lane = nullptr;  // a lane has where one of the warp's rows is
-      if (tile * 128 + own + lane < u.rows) {
+      if ((u.split ? 0 : tile * 128) + own + lane < u.rows) {
         int64_t row;
         int32_t head;
         row_of_q(u, own + lane, row, head);
@@ -513,12 +516,18 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       uint64_t sum = 0;
       int64_t row = 0;
       int32_t head = 0, begin = 0, end = 0, from = 0, to = 0;
+      uint32_t pair_phase = 0;
 #pragma unroll 1
       for (;;) {
         if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
         // This unit's queries: the products with the last one's are done.
         const bool more = sh.unit[ring].rows > 0;
-        if (more && sh.unit[ring].t1[tile] > sh.unit[ring].t0[tile]) load_queries(sh.unit[ring]);
+        if (more && sh.unit[ring].t1[tile] > sh.unit[ring].t0[tile]) {
+          if (helped)
+            mul = fmaxf(a.scale * kLog2e, 0x1p-120f);
+          else
+            load_queries(sh.unit[ring]);
+        }
 
         // ---- the last unit's results
         if (some) {
@@ -527,13 +536,34 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (!bar_wait(sh.o_full[tile], o_phase, sh)) return;
             o_phase ^= 1;
             after_sync();
-            if (sh.poison[now]) add_poison_of<KIND, kBt>(c, a, u, o_at, from, to, valid ? begin : INT32_MAX, end);
+            if (sh.poison[now]) add_poison_of<KIND, kBt>(c, a, u, o_at, from, to, u.split ? 2 : 1, valid ? begin : INT32_MAX, end);
           }
           const float2 z2 = parts_of(sum);
-          const float z = z2.x + z2.y;
+          float z = z2.x + z2.y, fade = 1.f, fade2 = 0.f;  // of this tile's sums, and of the second's
+          const bool paired = kTiles == 2 && u.split && u.t1[1] > u.t0[1];
+          if (paired) {
+            if (tile == 1) {  // the first tile's warps take over
+              sh.pair_top[r] = top, sh.pair_sum[r] = z;
+              before_sync();
+              __syncwarp();
+              if (lane == 0) bar_arrive(sh.pair);
+              if (!bar_wait(sh.pair_done, pair_phase, sh)) return;
+              pair_phase ^= 1;
+              after_sync();
+              valid = false;
+            } else {
+              if (!bar_wait(sh.pair, pair_phase, sh)) return;
+              pair_phase ^= 1;
+              after_sync();
+              const float other = sh.pair_top[r], high = fmaxf(top, other), ref = high == -INFINITY ? 0.f : high;
+              fade = exp2_fast(top - ref), fade2 = exp2_fast(other - ref);
+              z = z * fade + sh.pair_sum[r] * fade2;
+              top = high;
+            }
+          }
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h] : 1.f;
           float* const part = w.parts + rows_part(u.c0 + u.part, u.part == 0, kTiles, tile, DP);
-          const bool keep = u.parts > 1;
+          const bool keep = u.parts > 1 && !(paired && tile == 1);
           float f = 0.f;
           if (keep) {
             part[DP * 128 + r] = top, part[(DP + 1) * 128 + r] = z;
@@ -543,10 +573,17 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (lse) lse[row * a.heads + head] = z == 0.f ? -INFINITY : log_sum<KIND>(top, z);
           }
 #pragma unroll 1
-          for (int32_t d = 0; d < dim16; d += 32) {
+          for (int32_t d = 0; d < dim16 && !(paired && tile == 1); d += 32) {
             float o[32] = {};
             if (to > from) {
               tmem_load((uint32_t*)o, o_at + d);
+              if (paired && tile == 0) {
+                uint32_t o2[32];
+                tmem_load(o2, o_at + DP + d);
+                tmem_loaded();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = o[i] * fade + __uint_as_float(o2[i]) * fade2;
+              }
               tmem_loaded();
             }
             if (keep) {
@@ -557,6 +594,11 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               put(c, a, row, head, d, o, f);
               if (d + 16 < dim16) put(c, a, row, head, d + 16, o + 16, f);
             }
+          }
+          if (paired && tile == 0) {
+            before_sync();
+            __syncwarp();
+            if (lane == 0) bar_arrive(sh.pair_done);
           }
         }
         // (Loads of tensor memory are done before the next products may write there: P of this unit is announced later.)
@@ -569,7 +611,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         now = ring;
         next_unit();
         const RowsUnit& u = sh.unit[now];
-        some = u.rows > tile * 128, valid = tile * 128 + r < u.rows;
+        const int32_t every = u.split ? 2 : 1;
+        some = u.split ? u.t1[tile] > u.t0[tile] : u.rows > tile * 128;
+        valid = some && (u.split ? 0 : tile * 128) + r < u.rows;
         from = u.t0[tile], to = u.t1[tile];
         top = -INFINITY, sum = 0;
         begin = 0, end = INT32_MAX;  // (rows past the last one mask nothing)
@@ -585,7 +629,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         }
         const float unit_mul = mul;
 #pragma unroll 1
-        for (int32_t j = from; j < to; ++j) {
+        for (int32_t j = from; j < to; j += every) {
           if (!bar_wait(sh.s_full[tile], s_phase, sh)) return;
           s_phase ^= 1;
           after_sync();
@@ -661,189 +705,160 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     uint32_t phase = 1;   // (of `empty`: a fresh barrier's last phase counts as done)
     uint32_t raw_phase = 0;
     const auto run = [&]() {
+#pragma unroll 1
       for (;;) {
         if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
         const RowsUnit& u = sh.unit[ring];
         if (u.rows == 0) return;
-        const int32_t j0 = u.j0, j1 = u.j1, begin = u.begin, end = u.end;
+        const int32_t j0 = u.j0, n = u.j1 - j0, begin = u.begin, end = u.end;
         const char* const base = c.k + a.layer * c.layer_stride + u.h * c.head_stride;
         const int32_t* const pages = row_of(c, u.seq);
-        if (KIND != P2P_KV_E4M3 && maps.rows) {
-          // By the tensor memory accelerator, from one warp: a lane has a box of tokens.
-          if (warp == S::kSoft) {
-            const int32_t size = maps.rows, boxes = kBt / size;
-            const auto page_of = [&](int32_t j) {
-              const int32_t t = j * kBt + lane * size;
-              return lane < boxes && j < j1 && t < end && t + size > begin ? pages[c.by_page.div(t)] : -1;
-            };
-            int32_t page = page_of(j0);
-            for (int32_t j = j0; j < j1; ++j) {
-              const int32_t t = j * kBt + lane * size;
-              const bool needed = lane < boxes && t < end && t + size > begin, there = needed && (uint32_t)page < (uint32_t)c.n_pages;
-              if (needed && !there) atomicOr(w.err, KV_BAD_PAGE);
-              const uint32_t boxes_there = __popc(__ballot_sync(~0u, there)), holes = __ballot_sync(~0u, needed && !there);
-              const int32_t in_page = t - (int32_t)c.by_page.div(max(t, 0)) * c.page, this_page = page;
-              page = page_of(j + 1);
-#pragma unroll 1
-              for (int v = 0; v < 2; ++v) {
-                if (!bar_wait(sh.empty[stage], phase, sh)) return;
-                char* const to = stages + stage * S::kStage;
-                for (uint32_t left = holes; left; left &= left - 1) {  // zeros in the place of pages that are out of range
-                  const int box = __ffs(left) - 1;
-                  for (int y = lane; y < size * chunks * 8; y += 32)
-                    *(uint4*)(to + y / (size * 8) * (kBt * 128) + box * size * 128 + y % (size * 8) * 16) = make_uint4(0, 0, 0, 0);
-                }
-                if (holes) async_fence();
-                __syncwarp();
-                if (lane == 0) bar_expect(sh.full[stage], boxes_there * size * 128 * chunks);
-                __syncwarp();
-                if (there)
-                  for (int x = 0; x < chunks; ++x)
-                    copy_box(smem_of(to) + x * (kBt * 128) + lane * size * 128, v ? &maps.v : &maps.k, x * 64, in_page, u.h, this_page,
-                             a.layer, sh.full[stage]);
-                if (++stage == kStages) stage = 0, phase ^= 1;
-              }
-            }
-          }
-          __syncwarp();
-          if (lane == 0) bar_arrive(sh.unit_empty[ring]);
-          next_unit();
-          continue;
-        }
+        // A lane has a box of tokens of each step (a token, without maps): its first, and the page that it lies in, -1: it is not
+        // needed.
+        const int32_t size = maps.rows ? maps.rows : 1, boxes = kOwn / size;
+        const auto token_of = [&](int32_t step) { return (j0 + step) * kBt + own0 + lane * size; };
+        const auto find = [&](int32_t step) {
+          const int32_t t = token_of(step);
+          if (lane >= boxes || step >= n || t >= end || t + size <= begin) return -1;
+          const int32_t page = pages[c.by_page.div(t)];
+          return (uint32_t)page < (uint32_t)c.n_pages ? page : INT32_MAX;  // INT32_MAX: none such
+        };
+        int32_t before = -1, page = -1, next = find(0);
         if (KIND == P2P_KV_E4M3 && maps.rows) {
-          // The same in 8 bits into room of the warp's own, a step ahead; widened from there.
+          // In 8 bits into room of the warp's own by the tensor memory accelerator, a step ahead; widened from there.
           constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
           const int piece = lane % kLanes;
-          const int32_t size = maps.rows, boxes = kOwn / size;
           char* const raw = raws + (warp - S::kSoft) * (S::kRaw / 4);
-          const auto page_of = [&](int32_t j) {
-            const int32_t t = j * kBt + own0 + lane * size;
-            return lane < boxes && j < j1 && t < end && t + size > begin ? pages[c.by_page.div(t)] : -1;
-          };
-          const auto fetch = [&](int32_t j, int32_t page, int v) {  // which boxes there are
-            const int32_t t = j * kBt + own0 + lane * size;
-            const bool needed = lane < boxes && j < j1 && t < end && t + size > begin, there = needed && (uint32_t)page < (uint32_t)c.n_pages;
-            if (needed && !there) atomicOr(w.err, KV_BAD_PAGE);
+          const auto fetch = [&](int32_t step, int32_t from, int v) {  // which boxes there are
+            const bool there = from >= 0 && from != INT32_MAX;
+            if (from == INT32_MAX) atomicOr(w.err, KV_BAD_PAGE);
             const uint32_t which = __ballot_sync(~0u, there);
-            if (j < j1) {
+            if (step < n) {
               if (lane == 0) bar_expect(sh.raw[warp - S::kSoft][v], __popc(which) * size * c.dim);
               __syncwarp();
+              const int32_t t = token_of(step);
               if (there)
                 copy_box(smem_of(raw) + v * S::kRaw + lane * size * c.dim, v ? &maps.v : &maps.k, 0,
-                         t - (int32_t)c.by_page.div(t) * c.page, u.h, page, a.layer, sh.raw[warp - S::kSoft][v]);
+                         t - (int32_t)c.by_page.div(t) * c.page, u.h, from, a.layer, sh.raw[warp - S::kSoft][v]);
             }
             return which;
           };
-          int32_t page = page_of(j0);
-          uint32_t here = fetch(j0, page, 0);
-          fetch(j0, page, 1);
-          page = page_of(j0 + 1);
-          for (int32_t j = j0; j < j1; ++j) {
-            uint32_t later = 0;
+          page = next;
+          uint32_t of_k = fetch(0, page, 0), of_v = fetch(0, page, 1);
+          next = find(1);
 #pragma unroll 1
-            for (int v = 0; v < 2; ++v) {
-              if (!bar_wait(sh.raw[warp - S::kSoft][v], raw_phase, sh) || !bar_wait(sh.empty[stage], phase, sh)) return;
-              char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128);
-#pragma unroll
-              for (int x = 0; x < kOwn; x += kAtOnce) {
-                const int row = x + lane / kLanes, in_tile = own0 + row, t = j * kBt + in_tile;
-                uint4 y = make_uint4(0, 0, 0, 0);
-                if (piece < c.row16 && t >= begin && t < end && (here >> row / size & 1))
-                  y = *(const uint4*)(raw + v * S::kRaw + row * c.dim + piece * 16);
-                if (piece < 4 * chunks) {
-                  *(uint4*)(to + in_tile * 128 + ((2 * piece & 7) ^ (in_tile & 7)) * 16) =
-                      make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
-                  *(uint4*)(to + in_tile * 128 + (((2 * piece & 7) + 1) ^ (in_tile & 7)) * 16) =
-                      make_uint4(widen(y.z), widen_high(y.z), widen(y.w), widen_high(y.w));
-                }
+          for (int32_t q = 0; q < 2 * n; ++q) {
+            const int v = q == 2 * n - 1 || (q > 0 && !(q & 1));
+            const int32_t step = v ? (q == 2 * n - 1 ? n - 1 : q / 2 - 1) : (q + 1) / 2;
+            if (!bar_wait(sh.raw[warp - S::kSoft][v], v ? raw_phase >> 1 : raw_phase & 1, sh) || !bar_wait(sh.empty[stage], phase, sh)) return;
+            raw_phase ^= 1 << v;
+            const uint32_t here = v ? of_v : of_k;
+            char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128);
+#pragma unroll 4
+            for (int x = 0; x < kOwn; x += kAtOnce) {
+              const int row = x + lane / kLanes, in_tile = own0 + row, t = (j0 + step) * kBt + in_tile;
+              uint4 y = make_uint4(0, 0, 0, 0);
+              if (piece < c.row16 && t >= begin && t < end && (here >> row / size & 1))
+                y = *(const uint4*)(raw + v * S::kRaw + row * c.dim + piece * 16);
+              if (piece < 4 * chunks) {
+                *(uint4*)(to + in_tile * 128 + ((2 * piece & 7) ^ (in_tile & 7)) * 16) =
+                    make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
+                *(uint4*)(to + in_tile * 128 + (((2 * piece & 7) + 1) ^ (in_tile & 7)) * 16) =
+                    make_uint4(widen(y.z), widen_high(y.z), widen(y.w), widen_high(y.w));
               }
-              async_fence();
-              bar_arrive(sh.full[stage]);
-              if (++stage == kStages) stage = 0, phase ^= 1;
+            }
+            async_fence();
+            bar_arrive(sh.full[stage]);
+            if (++stage == kStages) stage = 0, phase ^= 1;
+            __syncwarp();
+            if (v) {
+              of_v = fetch(step + 1, before, 1);
+            } else {
+              before = page, page = next, next = find(step + 2);
+              of_k = fetch(step + 1, page, 0);
+            }
+          }
+        } else {
+#pragma unroll 1
+          for (int32_t q = 0; q < 2 * n; ++q) {
+            const int v = q == 2 * n - 1 || (q > 0 && !(q & 1));
+            const int32_t step = v ? (q == 2 * n - 1 ? n - 1 : q / 2 - 1) : (q + 1) / 2;
+            if (!v) before = page, page = next, next = find(step + 1);
+            const int32_t from = v && step < n - 1 ? before : page, t = token_of(step);
+            const bool there = from >= 0 && from != INT32_MAX;
+            if (from == INT32_MAX) atomicOr(w.err, KV_BAD_PAGE);
+            const int32_t in_page = there ? t - (int32_t)c.by_page.div(t) * c.page : 0;
+            if (!bar_wait(sh.empty[stage], phase, sh)) return;
+            char* const to = stages + stage * S::kStage;
+            if (KIND != P2P_KV_E4M3 && maps.rows) {
+              // By the tensor memory accelerator; zeros in the place of pages that are out of range.
+              const uint32_t holes = __ballot_sync(~0u, from == INT32_MAX), which = __ballot_sync(~0u, there);
+              for (uint32_t left = holes; left; left &= left - 1) {
+                const int first = (own0 + (__ffs(left) - 1) * size) * 128;
+                for (int y = lane; y < size * chunks * 8; y += 32)
+                  *(uint4*)(to + y / (size * 8) * (kBt * 128) + first + y % (size * 8) * 16) = make_uint4(0, 0, 0, 0);
+              }
+              if (holes) async_fence();
               __syncwarp();
-              later = fetch(j + 1, page, v);
-            }
-            here = later;
-            page = page_of(j + 2);
-            raw_phase ^= 1;
-          }
-          __syncwarp();
-          if (lane == 0) bar_arrive(sh.unit_empty[ring]);
-          next_unit();
-          continue;
-        }
-        // A lane has a token: where it lies (-1: nowhere, zeros).
-        const auto page_at = [&](int32_t j) {
-          const int32_t t = j * kBt + own0 + (lane & (kOwn - 1));
-          return j < j1 && t >= begin && t < end ? pages[c.by_page.div(t)] : -1;
-        };
-        int32_t page = page_at(j0);
-        for (int32_t j = j0; j < j1; ++j) {
-          const int32_t t = j * kBt + own0 + (lane & (kOwn - 1));
-          int64_t at = -1;
-          if (t >= begin && t < end) {
-            const uint32_t e = c.by_page.div(t);
-            if ((uint32_t)page < (uint32_t)c.n_pages)
-              at = page * c.page_stride + (int64_t)(t - (int32_t)e * c.page) * c.token_stride;
-            else
-              atomicOr(w.err, KV_BAD_PAGE);
-          }
-          page = page_at(j + 1);
-          if (KIND != P2P_KV_E4M3) {
-            constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;
-            const int piece = lane % kLanes;
+              if (lane == 0) bar_expect(sh.full[stage], __popc(which) * size * 128 * chunks);
+              __syncwarp();
+              if (there)
+                for (int x = 0; x < chunks; ++x)
+                  copy_box(smem_of(to) + x * (kBt * 128) + (own0 + lane * size) * 128, v ? &maps.v : &maps.k, x * 64, in_page, u.h, from,
+                           a.layer, sh.full[stage]);
+            } else {
+              const int64_t at = there && t >= begin ? (v ? across : 0) + from * c.page_stride + (int64_t)in_page * c.token_stride : -1;
+              const bool some = there && t >= begin;
+              if (KIND != P2P_KV_E4M3) {
+                constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;
+                const int piece = lane % kLanes;
+                const uint32_t rows_there = __ballot_sync(~0u, some), tile_at = smem_of(to) + (piece / 8) * (kBt * 128);
+                // (Places four at a time: one by one, each copy waits for its exchange.)
 #pragma unroll 1
-            for (int v = 0; v < 2; ++v) {
-              if (!bar_wait(sh.empty[stage], phase, sh)) return;
-              const uint32_t to = smem_of(stages) + stage * S::kStage + (piece / 8) * (kBt * 128);
-              // (Places four at a time: one by one, each copy waits for its exchange.)
-#pragma unroll 1
-              for (int x0 = 0; x0 < kOwn; x0 += 4 * kAtOnce) {
-                int64_t o[4];
+                for (int x0 = 0; x0 < kOwn; x0 += 4 * kAtOnce) {
+                  int64_t o[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[k] = __shfl_sync(~0u, at, (x0 + k * kAtOnce + lane / kLanes) & 31);
+                  for (int k = 0; k < 4; ++k) o[k] = __shfl_sync(~0u, at, (x0 + k * kAtOnce + lane / kLanes) & 31);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const int in_tile = own0 + x0 + k * kAtOnce + lane / kLanes;
-                  const bool in = o[k] >= 0 && piece < c.row16;
-                  const char* from = in ? base + o[k] + (v ? across : 0) + piece * 16 : c.k;
-                  if (piece < 8 * chunks && x0 + k * kAtOnce < kOwn) copy16(to + in_tile * 128 + ((piece & 7) ^ (in_tile & 7)) * 16, from, in);
+                  for (int k = 0; k < 4; ++k) {
+                    const int row = x0 + k * kAtOnce + lane / kLanes, in_tile = own0 + row;
+                    const bool in = row < kOwn && (rows_there >> row & 1) && piece < c.row16;
+                    const char* const his = in ? base + o[k] + piece * 16 : c.k;
+                    if (piece < 8 * chunks && row < kOwn) copy16(tile_at + in_tile * 128 + ((piece & 7) ^ (in_tile & 7)) * 16, his, in);
+                  }
                 }
-              }
-              // (Arrives when the thread's copies have; whoever reads them through another path fences after it has waited.)
-              asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_of(&sh.full[stage])) : "memory");
-              if (++stage == kStages) stage = 0, phase ^= 1;
-            }
-          } else {
-            // 16 values a piece; widened on the way.
-            constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
-            const int piece = lane % kLanes;
-#pragma unroll 1
-            for (int v = 0; v < 2; ++v) {
-              uint4 b[kOwn / kAtOnce];
+                // (Arrives when the thread's copies have; whoever reads them through another path fences after it has waited.)
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_of(&sh.full[stage])) : "memory");
+              } else {
+                // 16 values a piece; widened on the way.
+                constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
+                const int piece = lane % kLanes;
+                const uint32_t rows_there = __ballot_sync(~0u, some);
+                uint4 b[kOwn / kAtOnce];
 #pragma unroll
-              for (int x = 0; x < kOwn; x += kAtOnce) {
-                const int64_t o = __shfl_sync(~0u, at, x + lane / kLanes);
-                b[x / kAtOnce] = make_uint4(0, 0, 0, 0);
-                if (o >= 0 && piece < c.row16) b[x / kAtOnce] = __ldcg((const uint4*)(base + o + (v ? across : 0) + piece * 16));
-              }
-              if (!bar_wait(sh.empty[stage], phase, sh)) return;
-              char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128);
-#pragma unroll
-              for (int x = 0; x < kOwn; x += kAtOnce) {
-                const int row = own0 + x + lane / kLanes;
-                const uint4 y = b[x / kAtOnce];
-                if (piece < 4 * chunks) {
-                  *(uint4*)(to + row * 128 + ((2 * piece & 7) ^ (row & 7)) * 16) =
-                      make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
-                  *(uint4*)(to + row * 128 + (((2 * piece & 7) + 1) ^ (row & 7)) * 16) =
-                      make_uint4(widen(y.z), widen_high(y.z), widen(y.w), widen_high(y.w));
+                for (int x = 0; x < kOwn; x += kAtOnce) {
+                  const int row = x + lane / kLanes;
+                  const int64_t o = __shfl_sync(~0u, at, row);
+                  b[x / kAtOnce] = make_uint4(0, 0, 0, 0);
+                  if ((rows_there >> row & 1) && piece < c.row16) b[x / kAtOnce] = __ldcg((const uint4*)(base + o + piece * 16));
                 }
+                char* const tile_at = to + (piece / 4) * (kBt * 128);
+#pragma unroll
+                for (int x = 0; x < kOwn; x += kAtOnce) {
+                  const int row = own0 + x + lane / kLanes;
+                  const uint4 y = b[x / kAtOnce];
+                  if (piece < 4 * chunks) {
+                    *(uint4*)(tile_at + row * 128 + ((2 * piece & 7) ^ (row & 7)) * 16) =
+                        make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
+                    *(uint4*)(tile_at + row * 128 + (((2 * piece & 7) + 1) ^ (row & 7)) * 16) =
+                        make_uint4(widen(y.z), widen_high(y.z), widen(y.w), widen_high(y.w));
+                  }
+                }
+                async_fence();
+                bar_arrive(sh.full[stage]);
               }
-              async_fence();
-              bar_arrive(sh.full[stage]);
-              if (++stage == kStages) stage = 0, phase ^= 1;
             }
+            if (++stage == kStages) stage = 0, phase ^= 1;
           }
         }
         __syncwarp();
@@ -858,7 +873,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         for (int x = 0; x < 1 << 16 && !bar_try(sh.full[i], i < stage ? phase ^ 1 : phase); ++x) {
         }
       for (int v = 0; v < 2; ++v)
-        for (int x = 0; x < 1 << 16 && !bar_try(sh.raw[warp - S::kSoft][v], raw_phase); ++x) {
+        for (int x = 0; x < 1 << 16 && !bar_try(sh.raw[warp - S::kSoft][v], raw_phase >> v & 1); ++x) {
         }
     }
   } else if (warp == S::kSoft + 4) {
@@ -871,11 +886,11 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       const uint32_t qk = what | (uint32_t)(kBt / 8) << 17, pv = what | 1u << 16 | (uint32_t)(dim16 / 8) << 17;
       const uint32_t q_at = smem_of(q_room), stage_at = smem_of(stages);
       int32_t stage = 0;
-      uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase = 0;
       const auto next_stage = [&]() {
         if (++stage == kStages) stage = 0, phase ^= 1;
       };
-      const auto logits = [&](int tile, int at_stage) {
+      const auto logits = [&](int tile, int at_stage, bool last) {
         const uint64_t q0 = matrix(q_at + tile * S::kQTile, 16), k0 = matrix(stage_at + at_stage * S::kStage, 16);
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k)
@@ -883,13 +898,35 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             mma_ss(tmem + tile * kBt, q0 + ((k / 4) * (128 * 128) + (k & 3) * 32) / 16,
                    k0 + ((k / 4) * (kBt * 128) + (k & 3) * 32) / 16, qk, k > 0, one);
         mma_done(sh.s_full[tile], one);
+        if (last) mma_done(sh.q_empty[tile], one);
+      };
+      int32_t all_begin = 0, all_end = 0;
+      // The values of step j, at the current stage.
+      const auto values_there = [&](int32_t j) {
+        if (!bar_wait(sh.full[stage], phase, sh)) return false;
+        if ((j * kBt < all_begin || (j + 1) * kBt > all_end) && !bar_wait(sh.checked[stage], phase, sh)) return false;
+        async_fence();
+        return true;
+      };
+      const auto add_values = [&](int tile, bool add, bool last) {
+        if (!bar_wait(sh.p_full[tile], p_phase >> tile & 1, sh)) return false;
+        p_phase ^= 1u << tile;
+        after_sync();
+        const uint64_t v0 = matrix(stage_at + stage * S::kStage, kBt * 128);
+#pragma unroll
+        for (int k = 0; k < kBt / 16; ++k)
+          mma_ts(tmem + S::kOCol + tile * DP, tmem + tile * kBt + 8 * k, v0 + k * (2048 / 16), pv, add || k > 0, one);
+        if (last) mma_done(sh.o_full[tile], one);
+        return true;
       };
       const auto run = [&]() {
         for (;;) {
           if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
           const RowsUnit& u = sh.unit[ring];
           if (u.rows == 0) return;
-          const int32_t j0 = u.j0, j1 = u.j1, all_begin = u.all_begin, all_end = u.all_end;
+          const int32_t j0 = u.j0, j1 = u.j1;
+          const bool split = u.split;
+          all_begin = u.all_begin, all_end = u.all_end;
           int32_t t0[2], t1[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) t0[i] = u.t0[i], t1[i] = u.t1[i];
@@ -898,51 +935,72 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (t1[i] > t0[i]) {
               if (!bar_wait(sh.q_full[i], q_phase[i], sh)) return;
               q_phase[i] ^= 1;
+              async_fence();
             }
           if (one) bar_arrive(sh.unit_empty[ring]);
           next_unit();
-          // Stages come as K, V of each step.
+          // Stages come as K0, K1, V0, K2, V1, .. of the steps.
           if (!bar_wait(sh.full[stage], phase, sh)) return;
           async_fence();
+          if (!split) {
 #pragma unroll
-          for (int i = 0; i < kTiles; ++i)
-            if (j0 >= t0[i] && j0 < t1[i]) logits(i, stage);
-          mma_done(sh.empty[stage], one);
-          next_stage();
-          for (int32_t j = j0; j < j1; ++j) {
-            if (!bar_wait(sh.full[stage], phase, sh)) return;
-            if ((j * kBt < all_begin || (j + 1) * kBt > all_end) && !bar_wait(sh.checked[stage], phase, sh)) return;
-            async_fence();
-            const int v_stage = stage;
-            const uint32_t v_at = stage_at + v_stage * S::kStage;
+            for (int i = 0; i < kTiles; ++i)
+              if (j0 >= t0[i] && j0 < t1[i]) logits(i, stage, j0 + 1 == t1[i]);
+            mma_done(sh.empty[stage], one);
             next_stage();
-            bool next = j + 1 >= j1;  // the next step's keys are there (or there are none)
-  #pragma unroll
-          for (int i = 0; i < kTiles; ++i) {
-              if (j >= t0[i] && j < t1[i]) {
-                if (!bar_wait(sh.p_full[i], p_phase[i], sh)) return;
-                p_phase[i] ^= 1;
-                after_sync();
-                const uint64_t v0 = matrix(v_at, kBt * 128);
+#pragma unroll 1
+            for (int32_t j = j0; j < j1; ++j) {
+              const bool more = j + 1 < j1;
+              const int k_stage = stage;
+              const uint32_t k_phase = phase;
+              if (more) next_stage();
+              if (!values_there(j)) return;
+              bool keys = !more;  // the next step's are there (or there are none)
 #pragma unroll
-                for (int k = 0; k < kBt / 16; ++k)
-                  mma_ts(tmem + S::kOCol + i * DP, tmem + i * kBt + 8 * k, v0 + k * (2048 / 16), pv, j > t0[i] || k > 0, one);
-                if (j + 1 == t1[i]) mma_done(sh.o_full[i], one);
-              }
-              if (j + 1 < j1 && j + 1 >= t0[i] && j + 1 < t1[i]) {
-                if (!next) {
-                  if (!bar_wait(sh.full[stage], phase, sh)) return;
-                  async_fence();
-                  next = true;
+              for (int i = 0; i < kTiles; ++i) {
+                if (j >= t0[i] && j < t1[i] && !add_values(i, j > t0[i], j + 1 == t1[i])) return;
+                if (more && j + 1 >= t0[i] && j + 1 < t1[i]) {
+                  if (!keys) {
+                    if (!bar_wait(sh.full[k_stage], k_phase, sh)) return;
+                    async_fence();
+                    keys = true;
+                  }
+                  logits(i, k_stage, j + 2 == t1[i]);
                 }
-                logits(i, stage);
               }
+              mma_done(sh.empty[stage], one);
+              if (more) {
+                if (!keys && !bar_wait(sh.full[k_stage], k_phase, sh)) return;
+                mma_done(sh.empty[k_stage], one);
+              }
+              next_stage();
             }
-            mma_done(sh.empty[v_stage], one);
-            if (j + 1 < j1) {
-              if (!next && !bar_wait(sh.full[stage], phase, sh)) return;
+          } else if (kTiles == 2) {
+            // The tiles take turns with the steps.
+            const int32_t n = j1 - j0;
+            logits(0, stage, n <= 2);
+            mma_done(sh.empty[stage], one);
+            next_stage();
+            if (n > 1) {
+              if (!bar_wait(sh.full[stage], phase, sh)) return;
+              async_fence();
+              logits(1, stage, n <= 3);
               mma_done(sh.empty[stage], one);
               next_stage();
+            }
+#pragma unroll 1
+            for (int32_t x = 0; x < n; ++x) {
+              const int i = x & 1;
+              if (!values_there(j0 + x) || !add_values(i, x > 1, x + 2 >= n)) return;
+              mma_done(sh.empty[stage], one);
+              next_stage();
+              if (x + 2 < n) {
+                if (!bar_wait(sh.full[stage], phase, sh)) return;
+                async_fence();
+                logits(i, stage, x + 4 >= n);
+                mma_done(sh.empty[stage], one);
+                next_stage();
+              }
             }
           }
         }
@@ -967,7 +1025,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       next_unit();
       return true;
     };
-    const uint32_t x0 = share_of(total, blockIdx.x, ctas), x1 = share_of(total, blockIdx.x + 1, ctas);
+    // floor(total * k / ctas) for this CTA and the next.
+    const uint32_t whole = total / ctas, rest = total - whole * ctas;
+    const uint32_t x0 = whole * blockIdx.x + rest * blockIdx.x / ctas, x1 = whole * (blockIdx.x + 1) + rest * (blockIdx.x + 1) / ctas;
     // The first row's member (token) and head move by these from tile to tile, and to a tile's second half.
     const int32_t tile_t = a.by_group.div(S::kRowsMax), tile_g = S::kRowsMax - tile_t * a.group;
     const int32_t half_t = a.by_group.div(128), half_g = 128 - half_t * a.group;
@@ -985,10 +1045,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     // 32 items at a time, a lane each.
 #pragma unroll 1
     for (int32_t i0 = from * per_warp; alive && x < x1 && i0 < a.n; i0 += 32) {
-      RowsItem own = {};
-      uint32_t own_cost = 0;
-      if (i0 + lane < a.n) {
-        own = rows_item<S>(c, a, i0 + lane, nullptr);
+      if (i0 > 0 || per_warp > 32) {  // (else they are still there)
+        own = {}, own_cost = 0;
+        if (i0 + lane < a.n) own = rows_item<S>(c, a, i0 + lane, nullptr);
         if (own.tiles) own_cost = RowsCost<S>(a, own)(own.tiles);
       }
 #pragma unroll 1
@@ -1064,20 +1123,20 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               u.t0[1] = max(u.j0, its.begin >> S::kBtLog);
               u.t1[1] = max(u.t0[1], min(u.j1, ((its.end - 1) >> S::kBtLog) + 1));
             }
+            u.split = 0;
+            if (kTiles == 2 && rows <= 128 && s1 - s0 > 1) {
+              u.split = 1;
+              u.t0[0] = u.j0, u.t0[1] = u.j0 + 1;
+              u.t1[0] = u.t1[1] = u.j1;
+            }
             u.parts = 1, u.part = 0, u.c0 = blockIdx.x;
             if (s1 - s0 < n) {
-              // The first shares that begin within the unit, and after it.
-              uint32_t first = 0, end = 0;
-#pragma unroll 1
-              for (int k = 0; k < 2; ++k) {
-                const uint32_t y = x + (k ? inside : S::kSet + 1);
-                uint32_t q = share_of(y, ctas, total);
-                while (share_of(total, q, ctas) < y) ++q;
-                if (k == 0)
-                  first = q;
-                else
-                  end = q;
-              }
+              // The first shares that begin within the unit, and after it, by a lane each: the first k with total * k >= y * ctas.
+              const uint32_t y = x + (lane & 1 ? inside : S::kSet + 1);
+              uint32_t k = (uint32_t)__fdividef((float)y * (float)ctas, (float)total);
+              k = k > 1 ? k - 1 : 0;
+              while ((uint64_t)k * total < (uint64_t)y * ctas) ++k;
+              const uint32_t first = __shfl_sync(~0u, k, 0), end = __shfl_sync(~0u, k, 1);
               u.c0 = (int32_t)first - 1;
               u.parts = (int32_t)(end - first) + 1;
               u.part = blockIdx.x - u.c0;
@@ -1105,16 +1164,45 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     const int mine = (warp - S::kSoft - 6) * 32 + lane;
     int32_t stage = 0;
-    uint32_t phase = 0;
+    uint32_t phase = 0, q_phase = 3;  // (of fresh barriers: the last phases count as done)
     const auto run = [&]() {
       for (;;) {
         if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
         const RowsUnit& u = sh.unit[ring];
         if (u.rows == 0) return;
-        for (int32_t y = 2 * u.j0; y < 2 * u.j1; ++y) {  // (keys, then values of each step)
-          const int32_t j = y >> 1;
+        if (helped) {
+          // The unit's queries, as the products with the last one's are done: a lane finds a row, eight to 32 lanes copy it.
+          constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;
+          const int piece = lane % kLanes;
+#pragma unroll 1
+          for (int i = 0; i < kTiles; ++i) {
+            if (u.t1[i] <= u.t0[i]) continue;
+            if (!bar_wait(sh.q_empty[i], q_phase >> i & 1, sh)) return;
+            q_phase ^= 1u << i;
+#pragma unroll 1
+            for (int x0 = mine / 32 * 64; x0 < mine / 32 * 64 + 64; x0 += 32) {
+              const int x = (u.split ? 0 : 128 * i) + x0 + lane;
+              const uint32_t y = u.g0 + x, t = a.by_group.div(y);
+              const uint16_t* const of_lane = (const uint16_t*)a.q + (u.row + t) * a.q_row + (u.h * a.group + (int32_t)(y - t * a.group)) * a.q_head;
+              const uint32_t rows = __ballot_sync(~0u, x < u.rows), to = smem_of(q_room) + i * S::kQTile + (piece / 8) * (128 * 128);
+#pragma unroll 4
+              for (int k = 0; k < 32; k += kAtOnce) {
+                const int row = k + lane / kLanes;
+                const uint16_t* const p = (const uint16_t*)__shfl_sync(~0u, (unsigned long long)of_lane, row);
+                const bool in = (rows >> row & 1) && piece * 8 < c.dim;
+                if (piece * 8 < dim16) copy16(to + (x0 + row) * 128 + ((piece & 7) ^ (row & 7)) * 16, in ? p + piece * 8 : a.q, in);
+              }
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_of(&sh.q_full[i])) : "memory");
+          }
+        }
+        const int32_t n = u.j1 - u.j0;
+#pragma unroll 1
+        for (int32_t q = 0; q < 2 * n; ++q) {  // (stages as they come: K0, K1, V0, K2, V1, ..)
+          const bool values = q == 2 * n - 1 || (q > 0 && !(q & 1));
+          const int32_t j = u.j0 + (q == 2 * n - 1 ? n - 1 : q / 2 - 1);
           if (!bar_wait(sh.full[stage], phase, sh)) return;
-          if ((y & 1) && (j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) {
+          if (values && (j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) {
             // An exponent of all ones carries into the sign's place.
             constexpr uint32_t kExponent = KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = KIND == P2P_KV_BF16 ? 0x00800080u : 0x04000400u;
             char* const tile = stages + stage * S::kStage;
