@@ -230,7 +230,9 @@ struct KvRowsCall {
   int32_t shift;   // see RowsCost in kv_rows.cuh: 2^shift steps are counted as one, and a tile's rows are slope / 256 steps of tokens
   uint32_t slope;
   float scale;
-  bool q16, out32;  // whether rows of q lie on 16-byte boundaries, and those of out on 32-byte ones
+  bool boxes, out32;      // whether queries come by boxes of whole tokens, and rows of out lie on 32-byte boundaries
+  int32_t tile_rows;      // rows of a row tile: 128, or as many whole tokens as fit them
+  const CUtensorMap* q_map;  // (host)
 };
 // The pages as tensors [layer][page][head][token][value] for copies of `rows` tokens of one head and page at a time, 16-bit
 // values 64 at a time (128 bytes, turned as the tensor cores want them), 8-bit ones whole rows; rows 0: not to be had

@@ -19,6 +19,7 @@ struct p2p_kv {
   p2p::KvScratch s = {};
   p2p::KvAttendScratch w = {};
   p2p::KvMaps maps = {};
+  void* encode = nullptr;              // cuTensorMapEncodeTiled, or NULL
   void* scratch = nullptr;             // one allocation: s's arrays and d_stats
   unsigned long long* d_stats = nullptr;
   int device = 0, num_sms = 0;
@@ -139,22 +140,25 @@ cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p
   return (c.side != 0 && (c.lines || many) ? side_by_side : alone)(c, q, w, num_sms, st);
 }
 
+void* map_encoder() {
+  void* entry = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found) == cudaSuccess &&
+      found == cudaDriverEntryPointSuccess)
+    return entry;
+  (void)cudaGetLastError();
+  return nullptr;
+}
+
 // The pages as tensors for copies by the tensor memory accelerator, where they are to be had.
-void make_maps(const p2p::KvView& c, p2p::KvMaps& m) {
+void make_maps(const p2p::KvView& c, void* entry, p2p::KvMaps& m) {
   m.rows = 0;
   const bool eight = c.type == P2P_KV_E4M3;
   // Tokens of a copy: a power of two that divides a page (and so lies in one), at most what a warp takes of a step; copies go to
   // whole 128 bytes (1,024 where their pieces are turned).
   uint32_t rows = c.page & -c.page;
   rows = std::min(rows, c.dim > 128 ? 16u : 32u);
-  if (eight ? rows * c.dim % 128 != 0 : rows < 8) return;
-  void* entry = nullptr;
-  cudaDriverEntryPointQueryResult found;
-  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-      found != cudaDriverEntryPointSuccess || !entry) {
-    (void)cudaGetLastError();
-    return;
-  }
+  if (!entry || (eight ? rows * c.dim % 128 != 0 : rows < 8)) return;
   const cuuint64_t size[5] = {(cuuint64_t)c.dim, (cuuint64_t)c.page, (cuuint64_t)c.heads, (cuuint64_t)c.n_pages,
                               (cuuint64_t)c.n_layers};
   cuuint64_t stride[4] = {(cuuint64_t)c.token_stride, (cuuint64_t)c.head_stride, (cuuint64_t)c.page_stride,
@@ -293,7 +297,8 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   n->w.arrived = (int32_t*)(p + arrived);
   n->w.joins = (p2p::KvJoin*)(p + joins);
   n->w.err = n->s.err;
-  make_maps(c, n->maps);
+  n->encode = map_encoder();
+  make_maps(c, n->encode, n->maps);
   *out = n;
   return P2P_OK;
 }
@@ -512,7 +517,24 @@ int p2p_kv_write_rotated(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   return P2P_OK;
 }
 
-static p2p::KvRowsCall rows_call(const p2p_kv* h, int32_t layer, int32_t n, int64_t n_rows, const int32_t* seq, const void* q, int64_t q_row,
+// Queries as a tensor [row][kv head][query head of it][value], copied a row tile's whole rows at a time; false where they do not lie
+// as that takes, or half a tile or more might stay empty.
+static bool make_query_map(const p2p_kv* h, const p2p::KvRowsCall& a, int64_t n_rows, CUtensorMap& map) {
+  if (!h->encode || a.group > 32 || (uintptr_t)a.q % 16) return false;
+  const cuuint64_t size[4] = {(cuuint64_t)h->c.dim, (cuuint64_t)a.group, (cuuint64_t)h->c.heads, (cuuint64_t)n_rows};
+  const int64_t given[3] = {a.q_head, a.q_head * a.group, a.q_row};
+  cuuint64_t stride[3];
+  for (int i = 0; i < 3; ++i) {
+    if (size[i + 1] > 1 && (given[i] <= 0 || given[i] % 8 || given[i] >= (int64_t)1 << 39)) return false;
+    stride[i] = size[i + 1] > 1 ? given[i] * 2 : 16;
+  }
+  const cuuint32_t box[4] = {64, (cuuint32_t)a.group, 1, (cuuint32_t)(128 / a.group)}, step[4] = {1, 1, 1, 1};
+  return ((decltype(&cuTensorMapEncodeTiled))h->encode)(
+             &map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, (void*)a.q, size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static p2p::KvRowsCall rows_call(const p2p_kv* h, CUtensorMap& q_map, int32_t layer, int32_t n, int64_t n_rows, const int32_t* seq, const void* q, int64_t q_row,
                                  int64_t q_head, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
                                  int64_t out_row, int64_t out_head, float* lse) {
   p2p::KvRowsCall a = {};
@@ -520,13 +542,15 @@ static p2p::KvRowsCall rows_call(const p2p_kv* h, int32_t layer, int32_t n, int6
   a.q_row = q_row, a.q_head = q_head, a.out_row = out_row, a.out_head = out_head;
   a.n = n, a.heads = n_heads, a.group = n_heads / h->c.heads, a.type = type, a.window = window, a.layer = layer, a.scale = scale;
   a.by_group = p2p::FastDiv((uint32_t)a.group);
+  a.boxes = make_query_map(h, a, n_rows, q_map);
+  a.tile_rows = a.boxes ? 128 / a.group * a.group : 128;
+  a.q_map = a.boxes ? &q_map : nullptr;
   // Steps of 128 (64) tokens for tiles of 256 (128) rows are counted in 32 bits: coarser where there may be too many.
   const int rows = h->c.dim <= 128 ? 256 : 128, step = rows / 2;
   a.slope = std::max(1u, (uint32_t)(256 * rows / step / a.group));
-  const double tiles = (double)std::min<int64_t>(n, n_rows) * h->c.heads + (double)n_rows * n_heads / rows;
+  const double tiles = (double)std::min<int64_t>(n, n_rows) * h->c.heads + (double)n_rows * n_heads / (rows / 2);
   const double most = (double)h->c.max_pages * h->c.page / step + 4;
   while (tiles * (4 + std::ldexp(most, -a.shift)) > 4e9) ++a.shift;
-  a.q16 = (uintptr_t)q % 16 == 0 && q_row % 8 == 0 && q_head % 8 == 0;
   a.out32 = (uintptr_t)out % 32 == 0 && out_row % 16 == 0 && out_head % 16 == 0;
   return a;
 }
@@ -542,7 +566,8 @@ int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   if (!offsets) return fail(h, P2P_E_INVAL, "NULL device pointer");
   if (int rc = check_rows(h, n_tokens, q, n_heads, out, out_token_stride, out_head_stride, lse)) return rc;
   DeviceGuard g(h->device);
-  p2p::KvRowsCall a = rows_call(h, layer, n, n_tokens, seq, q, q_token_stride, q_head_stride, type, n_heads, scale, window, out,
+  CUtensorMap q_map;
+  p2p::KvRowsCall a = rows_call(h, q_map, layer, n, n_tokens, seq, q, q_token_stride, q_head_stride, type, n_heads, scale, window, out,
                                 out_token_stride, out_head_stride, lse);
   a.offsets = offsets;
   a.n_tokens = n_tokens;
@@ -591,7 +616,8 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   if (n_groups > 0) {
     // What the groups share, and the attention over it; then every row's other tokens, put together with that.
     CK(p2p::launch_kv_share(h->c, h->s.err, n, seq, n_groups, groups, window, skip, spans, h->stream));
-    p2p::KvRowsCall a = rows_call(h, layer, n_groups, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window,
+    CUtensorMap q_map;
+    p2p::KvRowsCall a = rows_call(h, q_map, layer, n_groups, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window,
                                   out, out_row_stride, out_head_stride, lse);
     a.groups = groups;
     a.spans = spans;

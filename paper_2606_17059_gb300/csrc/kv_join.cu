@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kThreads)
     const float v_scale = c.type == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h] : 1.f;
     const auto part_of = [&](int32_t k) { return w.parts + rows_part(c0 + k, k == 0, tiles, tile, dp); };
     const int r = x / columns * kRowsOfWarp + lane / 8, d = x % columns * 32 + lane % 8 * 4;
-    if (tile * 128 + r >= u.rows || d >= c.dim) continue;
+    if (r >= a.tile_rows || tile * a.tile_rows + r >= u.rows || d >= c.dim) continue;
     float m = -INFINITY, z = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     constexpr int kAhead = 8;
@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kThreads)
         o.z = fmaf(po[k].z, fade, o.z), o.w = fmaf(po[k].w, fade, o.w);
       }
     }
-    const uint32_t at = u.g0 + tile * 128 + r, t = a.by_group.div(at);
+    const uint32_t at = u.g0 + tile * a.tile_rows + r, t = a.by_group.div(at);
     const int64_t row = u.row + t;
     const int32_t head = u.h * a.group + (int32_t)(at - t * a.group);
     const float f = z > 0.f || z != z ? v_scale / z : 0.f;

@@ -3,8 +3,8 @@
 //
 // For a query row and the tokens t that it sees: x_t = scale * q . k_t, m = max x_t, z = sum exp(x_t - m), out = sum
 // exp(x_t - m) v_t / z, lse = m + ln z.  Rows are (token, query head of one kv head) pairs, numbered with the heads inside
-// the tokens; a unit is a tile of kRowsMax consecutive ones of one sequence (or group) and kv head, with the tokens that
-// any of them sees, kBt at a time.
+// the tokens; a unit is one or two tiles of up to 128 consecutive ones of one sequence (or group) and kv head, with the tokens that
+// any of them sees, kBt at a time.  (Where queries come by boxes, a row tile is as many whole tokens as fit 128 rows.)
 //
 // Both products are the tensor cores' (tcgen05): S = Q K^T with Q and K in shared memory, O += P V with P in tensor memory
 // and V in shared memory as it lies in the pages, tokens by values, which the second product takes as its transposed operand.
@@ -17,8 +17,6 @@
 // look for infinities and NaN among the values of tokens which not all rows see: 0 * NaN is NaN, so such values are taken
 // out before the product and added to the rows that do see them at the end.
 #pragma once
-#include <type_traits>
-
 #include "kv_math.cuh"
 #include "kv_values.cuh"
 
@@ -28,7 +26,6 @@ namespace {
 template <int KIND, int DP>
 struct RowsShape {
   static constexpr int kTiles = DP <= 128 ? 2 : 1;     // row tiles of a unit
-  static constexpr int kRowsMax = 128 * kTiles;
   static constexpr int kBt = DP <= 128 ? 128 : 64;     // tokens of a step
   static constexpr int kBtLog = DP <= 128 ? 7 : 6;
   static constexpr int kChunks = DP / 64;              // of 64 values: 128 bytes, a swizzled row
@@ -62,8 +59,19 @@ struct RowsUnit {
   int32_t parts, part, c0;   // of the unit, where it is shared: this piece's number and the first one's CTA
   int32_t split;             // 1: both row tiles have the same rows, and every other step
 };
+// The q-th stage of a unit's n steps, keys or values of one: K0, V0, K1, V1, .., or, where the row tiles take turns with the steps, K0,
+// K1, V0, K2, V1, .., as the products need them.
+struct RowsStage {
+  int32_t step;
+  bool values;
+};
+__device__ __forceinline__ RowsStage rows_stage(int32_t q, int32_t n, bool split) {
+  if (!split) return {q >> 1, (q & 1) != 0};
+  const bool values = q == 2 * n - 1 || (q > 0 && !(q & 1));
+  return {q == 2 * n - 1 ? n - 1 : values ? q / 2 - 1 : (q + 1) / 2, values};
+}
 struct RowsShared {
-  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], q_empty[2], pair, pair_done, drain, raw[4][2];
+  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], q_empty[2], q_raw[2], pair, pair_done, drain, raw[4][2];
   RowsUnit unit[kRing];
   uint32_t sums[16];
   int32_t tmem, dead;
@@ -109,6 +117,12 @@ __device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, in
                                          int32_t layer, const uint64_t& bar) {
   asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, "
                "%6}], [%7];" ::"r"(to), "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(layer), "r"(smem_of(&bar))
+               : "memory");
+}
+__device__ __forceinline__ void copy_query_box(uint32_t to, const CUtensorMap* map, int32_t x, int32_t head, int32_t row,
+                                               const uint64_t& bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, 0, %3, %4}], "
+               "[%5];" ::"r"(to), "l"(map), "r"(x), "r"(head), "r"(row), "r"(smem_of(&bar))
                : "memory");
 }
 __device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -226,7 +240,8 @@ __device__ __forceinline__ RowsItem rows_item(const KvView& c, const KvRowsCall&
     }
     if (bad && err) atomicOr(err, bad);
   }
-  r.tiles = (r.members * a.group + S::kRowsMax - 1) / S::kRowsMax;
+  const uint32_t unit = S::kTiles * a.tile_rows;
+  r.tiles = (r.members * a.group + unit - 1) / unit;
   return r;
 }
 __device__ __forceinline__ int32_t window_begin(const KvRowsCall& a, int32_t end) {
@@ -337,7 +352,8 @@ __device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall&
 
 template <int KIND, int DP>
 __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
-    rows_kernel(KvView c, const __grid_constant__ KvMaps maps, KvRowsCall a, KvAttendScratch w) {
+    rows_kernel(KvView c, const __grid_constant__ KvMaps maps, const __grid_constant__ CUtensorMap q_map, KvRowsCall a,
+                KvAttendScratch w) {
   using S = RowsShape<KIND, DP>;
   constexpr int kTiles = S::kTiles, kBt = S::kBt, kStages = S::kStages;
   extern __shared__ char room_[];
@@ -348,13 +364,12 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   RowsShared& sh = *(RowsShared*)(raws + S::kRaws * S::kRaw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  // Queries are copied into shared memory by the warps that look for infinities, where they need no change of type or sign and
-  // lie on 16-byte boundaries; else by the softmax warps.
-  const bool helped = KIND != P2P_KV_E4M3 && a.q16 && a.scale >= 0.f;
+  // Whether queries are multiplied as they are (see change_queries).
+  const bool direct = KIND != P2P_KV_E4M3 && a.scale >= 0.f;
   // (Nothing so far touches memory: it runs beside the end of the kernel before.)
   if (threadIdx.x == 0) {
     for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 4 : 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
-    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], helped ? 64 : 4), bar_init(sh.q_empty[i], 1), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1);
+    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], !direct ? 4 : a.boxes ? 1 : 64), bar_init(sh.q_raw[i], a.boxes ? 1 : 64), bar_init(sh.q_empty[i], 1), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1);
     for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
     for (int i = 0; i < 8; ++i) bar_init(sh.raw[i / 2][i & 1], 1);
     bar_init(sh.pair, 4);
@@ -398,7 +413,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     return;
   }
   const uint32_t tmem = sh.tmem;
-  const int32_t dim16 = (c.dim + 15) / 16 * 16;
+  const int32_t dim16 = (c.dim + 15) / 16 * 16, chunks = (dim16 + 63) / 64;  // (of 64 values, all of which are filled)
   int32_t ring = 0;          // the unit's place, and the phase of its barriers
   uint32_t ring_phase = 0;
   const auto next_unit = [&]() {
@@ -416,98 +431,61 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     float mul = 0.f;  // logit (in log2) of a sum of products
     // Where row x of the unit's tile is.
     const auto row_of_q = [&](const RowsUnit& u, int x, int64_t& row, int32_t& head) {
-      const uint32_t y = u.g0 + (u.split ? 0 : tile * 128) + x, t = a.by_group.div(y);
+      const uint32_t y = u.g0 + (u.split ? 0 : tile * a.tile_rows) + x, t = a.by_group.div(y);
       row = u.row + t;
       head = u.h * a.group + (int32_t)(y - t * a.group);
     };
-    // Queries into shared memory; a negative scale changes their signs instead, as exp's maximum is the products'.
-    const auto load_queries = [&](const RowsUnit& u) {
-      constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;  // lanes a row, rows at a time
-      const int piece = lane % kLanes, own = (warp & 3) * 32;
+    // Queries that are not multiplied as they are: a negative scale changes their signs, as exp's maximum is the products', and beside
+    // 8-bit keys bf16 ones become f16.  A thread has its row.
+    uint32_t raw_phase = 0;
+    const auto change_queries = [&](const RowsUnit& u) {
+      if (!bar_wait(sh.q_raw[tile], raw_phase, sh)) return false;
+      raw_phase ^= 1;
       float unit = fabsf(a.scale) * kLog2e;
       bool minus = a.scale < 0.f;
       if (KIND == P2P_KV_E4M3) {
         const float k_scale = c.k_scale[a.layer * c.heads + u.h];
         unit *= fabsf(k_scale), minus ^= k_scale < 0.f;
       }
-      mul = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
       const uint32_t flip = minus ? 0x80008000u : 0;
-      const uint16_t* of_lane = nullptr;  // a lane has where one of the warp's rows is
-      if ((u.split ? 0 : tile * 128) + own + lane < u.rows) {
-        int64_t row;
-        int32_t head;
-        row_of_q(u, own + lane, row, head);
-        of_lane = (const uint16_t*)a.q + row * a.q_row + head * a.q_head;
+      const auto piece_at = [&](int k) { return (uint4*)(q_tile + k / 8 * (128 * 128) + r * 128 + ((k & 7) ^ (r & 7)) * 16); };
+      const bool narrow = KIND == P2P_KV_E4M3 && a.type == P2P_KV_BF16;
+      float down = 1.f;
+      if (narrow) {
+        // In f16, scaled by a power of two so that the row's largest is in [2^14, 2^15): exact but for what is below 2^-28 of it.
+        // (Magnitudes compare as their bits do.)
+        uint32_t m = 0;
+#pragma unroll 4
+        for (int k = 0; k < dim16 / 8; ++k) {
+          const uint4 v = *piece_at(k);
+          m = __vmaxu2(m, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+        }
+        const float largest = __uint_as_float(max(m << 16, m & 0xffff0000u));
+        // (Of 0, an infinity or NaN: as they are.)
+        const int e = largest > 0.f && largest < INFINITY ? max((int)(__float_as_uint(largest) >> 23) - 127, -112) - 14 : 0;
+        down = __uint_as_float((127 - e) << 23), unit *= __uint_as_float((127 + e) << 23);
       }
-      const auto at = [&](int x) -> const uint16_t* {
-        const uint16_t* const p = (const uint16_t*)__shfl_sync(~0u, (unsigned long long)of_lane, x);
-        return p && piece * 8 < c.dim ? p + piece * 8 : nullptr;
-      };
-      // N times kAtOnce rows, from x0 of the warp's on.
-      const auto place = [&](int x0, auto& v, auto count) {
-        constexpr int N = decltype(count)::value;
-        if (KIND == P2P_KV_E4M3) {
-          // In f16, scaled by a power of two so that the row's largest is in [2^14, 2^15): exact but for what is below 2^-28 of
-          // it.  (Magnitudes compare as their bits do.  Exchanges of all rows together, as each waits for the one before.)
-          uint32_t most[N];
+      mul = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
+      if (narrow || flip) {
+#pragma unroll 4
+        for (int k = 0; k < dim16 / 8; ++k) {
+          const uint4 v = *piece_at(k);
+          uint32_t b[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int k = 0; k < N; ++k) {
-            const uint32_t m = __vmaxu2(__vmaxu2(v[k].x & 0x7fff7fffu, v[k].y & 0x7fff7fffu), __vmaxu2(v[k].z & 0x7fff7fffu, v[k].w & 0x7fff7fffu));
-            most[k] = max(m & 0xffffu, m >> 16);
-          }
-#pragma unroll
-          for (int d = kLanes / 2; d; d >>= 1)
-#pragma unroll
-            for (int k = 0; k < N; ++k) most[k] = max(most[k], __shfl_xor_sync(~0u, most[k], d));
-#pragma unroll
-          for (int k = 0; k < N; ++k) {
-            const float largest = two_halves(most[k], a.type).x;
-            // (Of 0, an infinity or NaN: as they are.)
-            const int e = largest > 0.f && largest < INFINITY ? max((int)(__float_as_uint(largest) >> 23) - 127, -112) - 14 : 0;
-            const float down = __uint_as_float((127 - e) << 23);
-            const int of_lane_row = lane - (x0 + k * kAtOnce), his = __shfl_sync(~0u, e, of_lane_row * kLanes & 31);
-            if (of_lane_row >= 0 && of_lane_row < kAtOnce) mul = fmaxf(unit * __uint_as_float((127 + his) << 23), 0x1p-120f);
-            uint32_t b[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 y = two_halves(b[i], a.type);
-              b[i] = pack<KIND>(y.x * down, y.y * down);
+          for (int i = 0; i < 4; ++i) {
+            if (narrow) {
+              const float2 y = two_halves(b[i], P2P_KV_BF16);
+              b[i] = pack<P2P_KV_F16>(y.x * down, y.y * down);
             }
-            v[k] = make_uint4(b[0], b[1], b[2], b[3]);
+            b[i] ^= flip;
           }
+          *piece_at(k) = make_uint4(b[0], b[1], b[2], b[3]);
         }
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-          const int x = own + x0 + k * kAtOnce + lane / kLanes;
-          if (piece * 8 < dim16)
-            *(uint4*)(q_tile + (piece / 8) * (128 * 128) + x * 128 + ((piece & 7) ^ (x & 7)) * 16) =
-                make_uint4(v[k].x ^ flip, v[k].y ^ flip, v[k].z ^ flip, v[k].w ^ flip);
-        }
-      };
-      constexpr int kLoads = DP == 128 && KIND != P2P_KV_E4M3 ? 16 : 8;
-      if (a.q16) {
-#pragma unroll 1
-        for (int x0 = 0; x0 < 32; x0 += kAtOnce * kLoads) {
-          uint4 v[kLoads];
-#pragma unroll
-          for (int k = 0; k < kLoads; ++k) {
-            const uint16_t* const p = at(x0 + k * kAtOnce + lane / kLanes);
-            v[k] = p ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
-          }
-          place(x0, v, std::integral_constant<int, kLoads>());
-        }
-      } else {
-#pragma unroll 1
-        for (int x0 = 0; x0 < 32; x0 += kAtOnce) {
-          const uint16_t* const p = at(x0 + lane / kLanes);
-          uint4 v[1] = {make_uint4(0, 0, 0, 0)};
-          if (p) v[0] = make_uint4(p[0] | p[1] << 16, p[2] | p[3] << 16, p[4] | p[5] << 16, p[6] | p[7] << 16);
-          place(x0, v, std::integral_constant<int, 1>());
-        }
+        async_fence();
       }
-      async_fence();
       __syncwarp();
       if (lane == 0) bar_arrive(sh.q_full[tile]);
+      return true;
     };
     const auto run = [&]() {
       int32_t now = -1;  // the unit whose results are to be put away
@@ -520,14 +498,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 #pragma unroll 1
       for (;;) {
         if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
-        // This unit's queries: the products with the last one's are done.
         const bool more = sh.unit[ring].rows > 0;
-        if (more && sh.unit[ring].t1[tile] > sh.unit[ring].t0[tile]) {
-          if (helped)
-            mul = fmaxf(a.scale * kLog2e, 0x1p-120f);
-          else
-            load_queries(sh.unit[ring]);
-        }
 
         // ---- the last unit's results
         if (some) {
@@ -612,8 +583,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         next_unit();
         const RowsUnit& u = sh.unit[now];
         const int32_t every = u.split ? 2 : 1;
-        some = u.split ? u.t1[tile] > u.t0[tile] : u.rows > tile * 128;
-        valid = some && (u.split ? 0 : tile * 128) + r < u.rows;
+        some = u.split ? u.t1[tile] > u.t0[tile] : u.rows > tile * a.tile_rows;
+        valid = some && r < a.tile_rows && (u.split ? 0 : tile * a.tile_rows) + r < u.rows;
         from = u.t0[tile], to = u.t1[tile];
         top = -INFINITY, sum = 0;
         begin = 0, end = INT32_MAX;  // (rows past the last one mask nothing)
@@ -627,6 +598,10 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             begin = window_begin(a, end);
           }
         }
+        if (direct)
+          mul = fmaxf(a.scale * kLog2e, 0x1p-120f);
+        else if (to > from && !change_queries(u))
+          return;
         const float unit_mul = mul;
 #pragma unroll 1
         for (int32_t j = from; j < to; j += every) {
@@ -654,7 +629,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 #pragma unroll
             for (int k = 0; k < 4; ++k) t[k] = max3(t[k], __uint_as_float(x[i + 2 * k]), __uint_as_float(x[i + 2 * k + 1]));
           const float most = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * unit_mul;
-          if (__any_sync(~0u, most > top + (Type<KIND>::kUp + Type<KIND>::kLag))) {
+          // (Rows past the last one, whatever they are, have no say: results would depend on it.)
+          if (__any_sync(~0u, valid && most > top + (Type<KIND>::kUp + Type<KIND>::kLag))) {
             const float next = fmaxf(most - Type<KIND>::kUp, top), fade = next == -INFINITY ? 1.f : exp2_fast(top - next);
             top = next;
             const float2 z = parts_of(sum);
@@ -673,6 +649,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           }
           const float less = top == -INFINITY ? 0.f : -top;
           const uint64_t by = pair_of(unit_mul, unit_mul), plus = pair_of(less, less);
+          uint64_t sum2 = 0;
 #pragma unroll
           for (int k = 0; k < kBt / 32; ++k) {
             uint32_t p[16];
@@ -681,11 +658,15 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               const int y = 32 * k + 2 * i;
               const float2 f = parts_of(fma2(pair_of(__uint_as_float(x[y]), __uint_as_float(x[y + 1])), by, plus));
               const float e0 = exp2_fast(f.x), e1 = exp2_fast(f.y);
-              sum = add2(sum, pair_of(e0, e1));
+              if (i & 1)
+                sum2 = add2(sum2, pair_of(e0, e1));
+              else
+                sum = add2(sum, pair_of(e0, e1));
               p[i] = pack<KIND>(e0, e1);
             }
             tmem_store16(s_at + 16 * k, p);
           }
+          sum = add2(sum, sum2);
           tmem_stored();
           before_sync();
           __syncwarp();
@@ -700,7 +681,6 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     constexpr int kOwn = kBt / 4;
     const int own0 = (warp - S::kSoft) * kOwn;
     const int64_t across = c.v - c.k;
-    const int32_t chunks = (dim16 + 63) / 64;  // (all 64 values of the last one are filled)
     int32_t stage = 0;
     uint32_t phase = 1;   // (of `empty`: a fresh barrier's last phase counts as done)
     uint32_t raw_phase = 0;
@@ -711,6 +691,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         const RowsUnit& u = sh.unit[ring];
         if (u.rows == 0) return;
         const int32_t j0 = u.j0, n = u.j1 - j0, begin = u.begin, end = u.end;
+        const bool split = u.split;
         const char* const base = c.k + a.layer * c.layer_stride + u.h * c.head_stride;
         const int32_t* const pages = row_of(c, u.seq);
         // A lane has a box of tokens of each step (a token, without maps): its first, and the page that it lies in, -1: it is not
@@ -748,8 +729,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           next = find(1);
 #pragma unroll 1
           for (int32_t q = 0; q < 2 * n; ++q) {
-            const int v = q == 2 * n - 1 || (q > 0 && !(q & 1));
-            const int32_t step = v ? (q == 2 * n - 1 ? n - 1 : q / 2 - 1) : (q + 1) / 2;
+            const RowsStage it = rows_stage(q, n, split);
+            const int v = it.values, step = it.step;
             if (!bar_wait(sh.raw[warp - S::kSoft][v], v ? raw_phase >> 1 : raw_phase & 1, sh) || !bar_wait(sh.empty[stage], phase, sh)) return;
             raw_phase ^= 1 << v;
             const uint32_t here = v ? of_v : of_k;
@@ -772,7 +753,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (++stage == kStages) stage = 0, phase ^= 1;
             __syncwarp();
             if (v) {
-              of_v = fetch(step + 1, before, 1);
+              of_v = fetch(step + 1, split ? before : page, 1);
             } else {
               before = page, page = next, next = find(step + 2);
               of_k = fetch(step + 1, page, 0);
@@ -781,10 +762,10 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         } else {
 #pragma unroll 1
           for (int32_t q = 0; q < 2 * n; ++q) {
-            const int v = q == 2 * n - 1 || (q > 0 && !(q & 1));
-            const int32_t step = v ? (q == 2 * n - 1 ? n - 1 : q / 2 - 1) : (q + 1) / 2;
+            const RowsStage it = rows_stage(q, n, split);
+            const int v = it.values, step = it.step;
             if (!v) before = page, page = next, next = find(step + 1);
-            const int32_t from = v && step < n - 1 ? before : page, t = token_of(step);
+            const int32_t from = v && split && step < n - 1 ? before : page, t = token_of(step);
             const bool there = from >= 0 && from != INT32_MAX;
             if (from == INT32_MAX) atomicOr(w.err, KV_BAD_PAGE);
             const int32_t in_page = there ? t - (int32_t)c.by_page.div(t) * c.page : 0;
@@ -908,11 +889,11 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         async_fence();
         return true;
       };
-      const auto add_values = [&](int tile, bool add, bool last) {
+      const auto add_values = [&](int tile, int at_stage, bool add, bool last) {
         if (!bar_wait(sh.p_full[tile], p_phase >> tile & 1, sh)) return false;
         p_phase ^= 1u << tile;
         after_sync();
-        const uint64_t v0 = matrix(stage_at + stage * S::kStage, kBt * 128);
+        const uint64_t v0 = matrix(stage_at + at_stage * S::kStage, kBt * 128);
 #pragma unroll
         for (int k = 0; k < kBt / 16; ++k)
           mma_ts(tmem + S::kOCol + tile * DP, tmem + tile * kBt + 8 * k, v0 + k * (2048 / 16), pv, add || k > 0, one);
@@ -939,7 +920,6 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             }
           if (one) bar_arrive(sh.unit_empty[ring]);
           next_unit();
-          // Stages come as K0, K1, V0, K2, V1, .. of the steps.
           if (!bar_wait(sh.full[stage], phase, sh)) return;
           async_fence();
           if (!split) {
@@ -950,30 +930,28 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             next_stage();
 #pragma unroll 1
             for (int32_t j = j0; j < j1; ++j) {
-              const bool more = j + 1 < j1;
-              const int k_stage = stage;
-              const uint32_t k_phase = phase;
-              if (more) next_stage();
               if (!values_there(j)) return;
-              bool keys = !more;  // the next step's are there (or there are none)
+              const int v_stage = stage;
+              next_stage();
+              bool keys = j + 1 == j1;  // the next step's are there (or there are none)
 #pragma unroll
               for (int i = 0; i < kTiles; ++i) {
-                if (j >= t0[i] && j < t1[i] && !add_values(i, j > t0[i], j + 1 == t1[i])) return;
-                if (more && j + 1 >= t0[i] && j + 1 < t1[i]) {
+                if (j >= t0[i] && j < t1[i] && !add_values(i, v_stage, j > t0[i], j + 1 == t1[i])) return;
+                if (j + 1 < j1 && j + 1 >= t0[i] && j + 1 < t1[i]) {
                   if (!keys) {
-                    if (!bar_wait(sh.full[k_stage], k_phase, sh)) return;
+                    if (!bar_wait(sh.full[stage], phase, sh)) return;
                     async_fence();
                     keys = true;
                   }
-                  logits(i, k_stage, j + 2 == t1[i]);
+                  logits(i, stage, j + 2 == t1[i]);
                 }
               }
-              mma_done(sh.empty[stage], one);
-              if (more) {
-                if (!keys && !bar_wait(sh.full[k_stage], k_phase, sh)) return;
-                mma_done(sh.empty[k_stage], one);
+              mma_done(sh.empty[v_stage], one);
+              if (j + 1 < j1) {
+                if (!keys && !bar_wait(sh.full[stage], phase, sh)) return;
+                mma_done(sh.empty[stage], one);
+                next_stage();
               }
-              next_stage();
             }
           } else if (kTiles == 2) {
             // The tiles take turns with the steps.
@@ -991,7 +969,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 #pragma unroll 1
             for (int32_t x = 0; x < n; ++x) {
               const int i = x & 1;
-              if (!values_there(j0 + x) || !add_values(i, x > 1, x + 2 >= n)) return;
+              if (!values_there(j0 + x) || !add_values(i, stage, x > 1, x + 2 >= n)) return;
               mma_done(sh.empty[stage], one);
               next_stage();
               if (x + 2 < n) {
@@ -1029,8 +1007,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     const uint32_t whole = total / ctas, rest = total - whole * ctas;
     const uint32_t x0 = whole * blockIdx.x + rest * blockIdx.x / ctas, x1 = whole * (blockIdx.x + 1) + rest * (blockIdx.x + 1) / ctas;
     // The first row's member (token) and head move by these from tile to tile, and to a tile's second half.
-    const int32_t tile_t = a.by_group.div(S::kRowsMax), tile_g = S::kRowsMax - tile_t * a.group;
-    const int32_t half_t = a.by_group.div(128), half_g = 128 - half_t * a.group;
+    const int32_t unit = kTiles * a.tile_rows, tile_t = a.by_group.div(unit), tile_g = unit - tile_t * a.group;
+    const int32_t half_t = a.by_group.div(a.tile_rows), half_g = a.tile_rows - half_t * a.group;
     // The warp that summed the item where the share begins, and where its items begin.
     uint32_t x = of_warp;
 #pragma unroll
@@ -1084,11 +1062,11 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         }
         const uint32_t x_next = x + c.heads * all;
         x += h * all + cost;
-        int32_t t = a.by_group.div(j * S::kRowsMax), g0 = j * S::kRowsMax - t * a.group;
+        int32_t t = a.by_group.div(j * unit), g0 = j * unit - t * a.group;
 #pragma unroll 1
         while (alive && x < x1) {
           const uint32_t cost1 = costs(j + 1), width = cost1 - cost;
-          const int32_t rows = min(S::kRowsMax, it.members * a.group - j * S::kRowsMax);
+          const int32_t rows = min(unit, it.members * a.group - j * unit);
           // The next tile's first row, and the second half's.
           int32_t t_next = t + tile_t, g_next = g0 + tile_g, t_half = t + half_t, g_half = g0 + half_g;
           if (g_next >= a.group) g_next -= a.group, ++t_next;
@@ -1114,17 +1092,17 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             u.j0 = j0 + s0, u.j1 = j0 + s1;
             u.t0[0] = u.t1[0] = u.t0[1] = u.t1[1] = u.j0;
             {
-              const RowsSpan its = rows_span(a, it, t, rows <= 128 ? t_last : g_half ? t_half : t_half - 1);
+              const RowsSpan its = rows_span(a, it, t, rows <= a.tile_rows ? t_last : g_half ? t_half : t_half - 1);
               u.t0[0] = max(u.j0, its.begin >> S::kBtLog);
               u.t1[0] = max(u.t0[0], min(u.j1, ((its.end - 1) >> S::kBtLog) + 1));
             }
-            if (kTiles == 2 && rows > 128) {
+            if (kTiles == 2 && rows > a.tile_rows) {
               const RowsSpan its = rows_span(a, it, t_half, t_last);
               u.t0[1] = max(u.j0, its.begin >> S::kBtLog);
               u.t1[1] = max(u.t0[1], min(u.j1, ((its.end - 1) >> S::kBtLog) + 1));
             }
             u.split = 0;
-            if (kTiles == 2 && rows <= 128 && s1 - s0 > 1) {
+            if (kTiles == 2 && rows <= a.tile_rows && s1 - s0 > 1) {
               u.split = 1;
               u.t0[0] = u.j0, u.t0[1] = u.j0 + 1;
               u.t1[0] = u.t1[1] = u.j1;
@@ -1170,39 +1148,47 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
         const RowsUnit& u = sh.unit[ring];
         if (u.rows == 0) return;
-        if (helped) {
-          // The unit's queries, as the products with the last one's are done: a lane finds a row, eight to 32 lanes copy it.
-          constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;
-          const int piece = lane % kLanes;
+        // The unit's queries, when the products with the last one's are done.
 #pragma unroll 1
-          for (int i = 0; i < kTiles; ++i) {
-            if (u.t1[i] <= u.t0[i]) continue;
-            if (!bar_wait(sh.q_empty[i], q_phase >> i & 1, sh)) return;
-            q_phase ^= 1u << i;
-#pragma unroll 1
-            for (int x0 = mine / 32 * 64; x0 < mine / 32 * 64 + 64; x0 += 32) {
-              const int x = (u.split ? 0 : 128 * i) + x0 + lane;
-              const uint32_t y = u.g0 + x, t = a.by_group.div(y);
-              const uint16_t* const of_lane = (const uint16_t*)a.q + (u.row + t) * a.q_row + (u.h * a.group + (int32_t)(y - t * a.group)) * a.q_head;
-              const uint32_t rows = __ballot_sync(~0u, x < u.rows), to = smem_of(q_room) + i * S::kQTile + (piece / 8) * (128 * 128);
-#pragma unroll 4
-              for (int k = 0; k < 32; k += kAtOnce) {
-                const int row = k + lane / kLanes;
-                const uint16_t* const p = (const uint16_t*)__shfl_sync(~0u, (unsigned long long)of_lane, row);
-                const bool in = (rows >> row & 1) && piece * 8 < c.dim;
-                if (piece * 8 < dim16) copy16(to + (x0 + row) * 128 + ((piece & 7) ^ (row & 7)) * 16, in ? p + piece * 8 : a.q, in);
-              }
+        for (int i = 0; i < kTiles; ++i) {
+          if (u.t1[i] <= u.t0[i]) continue;
+          if (!bar_wait(sh.q_empty[i], q_phase >> i & 1, sh)) return;
+          q_phase ^= 1u << i;
+          const uint64_t& there = direct ? sh.q_full[i] : sh.q_raw[i];
+          const int first = u.split ? 0 : i * a.tile_rows;
+          char* const to = q_room + i * S::kQTile;
+          if (a.boxes) {  // whole tokens
+            if (mine == 0) {
+              bar_expect(there, a.tile_rows * 128 * chunks);
+              for (int x = 0; x < chunks; ++x)
+                copy_query_box(smem_of(to) + x * (128 * 128), &q_map, x * 64, u.h, (int32_t)(u.row + a.by_group.div(first)), there);
             }
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_of(&sh.q_full[i])) : "memory");
+            continue;
           }
+          // From anywhere, a piece of 16 bytes a thread.
+          const int pieces = dim16 / 8;
+#pragma unroll 1
+          for (int y = mine; y < 128 * pieces; y += 64) {
+            const int x = y / pieces, piece = y - x * pieces;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (first + x < u.rows && x < a.tile_rows && piece * 8 < c.dim) {
+              const uint32_t z = u.g0 + first + x, t = a.by_group.div(z);
+              const uint16_t* const f =
+                  (const uint16_t*)a.q + (u.row + t) * a.q_row + (u.h * a.group + (int32_t)(z - t * a.group)) * a.q_head + piece * 8;
+              v = make_uint4(f[0] | f[1] << 16, f[2] | f[3] << 16, f[4] | f[5] << 16, f[6] | f[7] << 16);
+            }
+            *(uint4*)(to + piece / 8 * (128 * 128) + x * 128 + ((piece & 7) ^ (x & 7)) * 16) = v;
+          }
+          async_fence();
+          bar_arrive(there);
         }
         const int32_t n = u.j1 - u.j0;
 #pragma unroll 1
-        for (int32_t q = 0; q < 2 * n; ++q) {  // (stages as they come: K0, K1, V0, K2, V1, ..)
-          const bool values = q == 2 * n - 1 || (q > 0 && !(q & 1));
-          const int32_t j = u.j0 + (q == 2 * n - 1 ? n - 1 : q / 2 - 1);
+        for (int32_t q = 0; q < 2 * n; ++q) {
+          const RowsStage it = rows_stage(q, n, u.split);
+          const int32_t j = u.j0 + it.step;
           if (!bar_wait(sh.full[stage], phase, sh)) return;
-          if (values && (j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) {
+          if (it.values && (j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) {
             // An exponent of all ones carries into the sign's place.
             constexpr uint32_t kExponent = KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = KIND == P2P_KV_BF16 ? 0x00800080u : 0x04000400u;
             char* const tile = stages + stage * S::kStage;
@@ -1272,7 +1258,7 @@ cudaError_t launch_rows(const KvView& c, const KvMaps& m, const KvRowsCall* a, c
     if (e == cudaSuccess && S::kTiles == 2 && got.numRegs != 128) e = cudaErrorInvalidDeviceFunction;
     return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
   }
-  return launch_early(kernel, dim3(num_sms), S::kThreads, S::kBytes, st, c, m, *a, w);
+  return launch_early(kernel, dim3(num_sms), S::kThreads, S::kBytes, st, c, m, a->q_map ? *a->q_map : m.k, *a, w);
 }
 template <int KIND>
 cudaError_t launch_rows_dim(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
