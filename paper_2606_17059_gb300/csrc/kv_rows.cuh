@@ -45,6 +45,7 @@ struct RowsShape {
   static constexpr int kSet = 2;                       // steps that a unit counts for beyond its own
 };
 
+constexpr int kSplitSteps = 4;  // from which on
 constexpr int kRing = 4;  // units that the schedule is ahead
 struct RowsUnit {
   int64_t row;       // of q: the unit's first
@@ -422,7 +423,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 
   if (warp < S::kSoft) {
     // ================================ softmax: a thread a row
-    if (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    if (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     const int tile = warp / 4, r = (warp & 3) * 32 + lane;  // of the row tile
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;      // (tensor memory's lanes 32 * (warp % 4) .., from bit 16 on)
     const uint32_t s_at = tmem + lanes + tile * kBt, o_at = tmem + lanes + S::kOCol + tile * DP;
@@ -677,7 +678,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     run();
   } else if (warp < S::kSoft + 4) {
     // ================================ copies: a warp has a quarter of a step's tokens
-    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     constexpr int kOwn = kBt / 4;
     const int own0 = (warp - S::kSoft) * kOwn;
     const int64_t across = c.v - c.k;
@@ -769,11 +770,12 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             const bool there = from >= 0 && from != INT32_MAX;
             if (from == INT32_MAX) atomicOr(w.err, KV_BAD_PAGE);
             const int32_t in_page = there ? t - (int32_t)c.by_page.div(t) * c.page : 0;
-            if (!bar_wait(sh.empty[stage], phase, sh)) return;
+            const uint32_t holes = __ballot_sync(~0u, from == INT32_MAX);
+            const uint32_t bytes = __popc(__ballot_sync(~0u, there)) * size * 128 * chunks;
             char* const to = stages + stage * S::kStage;
+            if (!bar_wait(sh.empty[stage], phase, sh)) return;
             if (KIND != P2P_KV_E4M3 && maps.rows) {
               // By the tensor memory accelerator; zeros in the place of pages that are out of range.
-              const uint32_t holes = __ballot_sync(~0u, from == INT32_MAX), which = __ballot_sync(~0u, there);
               for (uint32_t left = holes; left; left &= left - 1) {
                 const int first = (own0 + (__ffs(left) - 1) * size) * 128;
                 for (int y = lane; y < size * chunks * 8; y += 32)
@@ -781,11 +783,12 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               }
               if (holes) async_fence();
               __syncwarp();
-              if (lane == 0) bar_expect(sh.full[stage], __popc(which) * size * 128 * chunks);
+              if (lane == 0) bar_expect(sh.full[stage], bytes);
               __syncwarp();
               if (there)
-                for (int x = 0; x < chunks; ++x)
-                  copy_box(smem_of(to) + x * (kBt * 128) + (own0 + lane * size) * 128, v ? &maps.v : &maps.k, x * 64, in_page, u.h, from,
+#pragma unroll
+                for (int x = 0; x < S::kChunks; ++x)
+                  if (x < chunks) copy_box(smem_of(to) + x * (kBt * 128) + (own0 + lane * size) * 128, v ? &maps.v : &maps.k, x * 64, in_page, u.h, from,
                            a.layer, sh.full[stage]);
             } else {
               const int64_t at = there && t >= begin ? (v ? across : 0) + from * c.page_stride + (int64_t)in_page * c.token_stride : -1;
@@ -859,7 +862,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     }
   } else if (warp == S::kSoft + 4) {
     // ================================ products
-    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     {
       const uint32_t one = elected();
       const uint32_t type = KIND == P2P_KV_BF16 ? 1u : 0u;
@@ -991,7 +994,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     __syncwarp();
   } else if (warp == S::kSoft + 5) {
     // ================================ schedule: the units of this CTA's share
-    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     const auto emit = [&](const RowsUnit& u) {
       if (!bar_wait(sh.unit_empty[ring], ring_phase ^ 1, sh)) return false;
       if (lane == 0) {
@@ -1102,7 +1105,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               u.t1[1] = max(u.t0[1], min(u.j1, ((its.end - 1) >> S::kBtLog) + 1));
             }
             u.split = 0;
-            if (kTiles == 2 && rows <= a.tile_rows && s1 - s0 > 1) {
+            if (kTiles == 2 && rows <= a.tile_rows && s1 - s0 >= kSplitSteps) {
               u.split = 1;
               u.t0[0] = u.j0, u.t0[1] = u.j0 + 1;
               u.t1[0] = u.t1[1] = u.j1;
@@ -1139,7 +1142,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     }
   } else {
     // ================================ infinities and NaN among values that not all rows see
-    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     const int mine = (warp - S::kSoft - 6) * 32 + lane;
     int32_t stage = 0;
     uint32_t phase = 0, q_phase = 3;  // (of fresh barriers: the last phases count as done)
@@ -1254,7 +1257,7 @@ cudaError_t launch_rows(const KvView& c, const KvMaps& m, const KvRowsCall* a, c
   if (!a) {
     cudaFuncAttributes got;
     cudaError_t e = cudaFuncGetAttributes(&got, kernel);
-    // (The softmax warps take 72 registers a thread more, which the others give back: of 128 that each starts with.)
+    // (The softmax warps take 56 registers a thread more, which the others give back: of 128 that each starts with.)
     if (e == cudaSuccess && S::kTiles == 2 && got.numRegs != 128) e = cudaErrorInvalidDeviceFunction;
     return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
   }
