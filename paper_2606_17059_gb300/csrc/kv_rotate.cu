@@ -47,12 +47,28 @@ __device__ __forceinline__ TurnRow turn_row(const KvView& c, const KvTurn& a, in
   return r < c.heads ? TurnRow{1, r} : TurnRow{2, r - c.heads};
 }
 
-// IN: the type of q, k and v; EIGHT: the cache holds 8 bits, else IN.  Rows lie on 16-byte boundaries and the rotated
-// halves are whole pieces; log_lanes: of a row.
-template <int IN, bool EIGHT, int BATCH>
-__global__ void __launch_bounds__(kTurnThreads)
+// x / scale rounded to 32 bits, and where that is a tie of 8 bits and the quotient is not, to its side of it (see divide_extreme); inverse:
+// 1 / scale, positive and of an ordinary size.
+__device__ __forceinline__ float divide(float x, float scale, float inverse) {
+  const float z0 = x * inverse;
+  float z = fmaf(fmaf(-z0, scale, x), inverse, z0);
+  if (!(fabsf(z) < INFINITY)) z = z0;  // (infinities and NaN)
+  int32_t b = __float_as_int(z);
+  if ((b & 0x7ffff) == 0) {
+    const float r = fmaf(-z, scale, x);
+    if (r < 0.f || r > 0.f) b += (r < 0.f) == (x < 0.f) ? 1 : -1;
+  }
+  return __int_as_float(b);
+}
+
+// IN: the type of q, k and v; EIGHT: the cache holds 8 bits, else IN; NORMED: there are weights; PAIRS: interleaved.  Rows lie on 16-byte boundaries and the
+// rotated halves are whole pieces; log_lanes: of a row.  Queries, then keys, then values: what a kind's rows need stays in
+// registers, and a batch of rows is read while the one before it is worked on.
+template <int IN, bool EIGHT, bool NORMED, bool PAIRS>
+__global__ void __launch_bounds__(kTurnThreads, 2)
     turn_kernel(KvView c, KvScratch s, KvTurn a, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,
                 int64_t n_tokens, int32_t tokens, int32_t log_lanes, int32_t share) {
+  constexpr int BATCH = 2;
   __shared__ int64_t place[kTurnTokens];
   __shared__ int32_t position[kTurnTokens];
   begin_kernel();
@@ -67,14 +83,15 @@ __global__ void __launch_bounds__(kTurnThreads)
   __syncthreads();
   // The lane's pieces, each eight values; -1: none.
   const int u = lane & ((1 << log_lanes) - 1), pieces = c.dim / 8, turned = a.rot / 16;
-  const bool whole = a.pairs || u < turned;  // (interleaved: decided pair by pair)
   int first = 2 * u, second = 2 * u + 1;
-  if (!a.pairs) first = u < turned ? u : 2 * u, second = u < turned ? u + turned : 2 * u + 1;
+  if (!PAIRS && u < turned) first = u, second = u + turned;
   if (first >= pieces) first = -1;
   if (second >= pieces) second = -1;
-  const int32_t rows = a.heads + 2 * c.heads, r1 = min(rows, (int32_t)(blockIdx.y + 1) * share);
-  const int step = 32 >> log_lanes;
-  const bool normed = a.q_weight || a.k_weight;
+  const int mine = first < 0 || (!PAIRS && u >= turned) ? 0 : min(8, a.rot / 2 - 8 * u);  // pairs of the lane that are rotated
+  const int step = 32 >> log_lanes, of_warp = lane >> log_lanes;
+  const int32_t rows = a.heads + 2 * c.heads, begin = blockIdx.y * share, end = min(rows, begin + share);
+  const float per_value = 1.f / c.dim;
+#pragma unroll 1
   for (int32_t i = warp; i < tokens && t0 + i < n_tokens; i += kTurnWarps) {
     const int64_t at = place[i], t = t0 + i;
     if (at < 0) continue;
@@ -82,99 +99,107 @@ __global__ void __launch_bounds__(kTurnThreads)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       cs[j] = 1.f, sn[j] = 0.f;
-      if (whole && 8 * u + j < a.rot / 2) {
+      if (j < mine) {
         sincospif(half_turns(a.turns[8 * u + j], position[i]), &sn[j], &cs[j]);
         cs[j] *= a.amplitude, sn[j] *= a.amplitude;
       }
     }
-    for (int32_t r0 = blockIdx.y * share; r0 < r1; r0 += BATCH * step) {
-      uint4 raw[BATCH][2];
+#pragma unroll 1
+    for (int kind = 0; kind < 3; ++kind) {
+      const int32_t r_first = kind == 0 ? 0 : a.heads + (kind - 1) * c.heads, heads = kind == 0 ? a.heads : c.heads;
+      const int32_t h0 = max(begin - r_first, 0), h1 = min(end - r_first, heads);
+      if (h0 >= h1) continue;
+      const uint16_t* const from = kind == 0 ? (const uint16_t*)a.q + t * a.q_token : (const uint16_t*)(kind == 1 ? a.k : a.v) + t * a.token;
+      const int64_t apart = kind == 0 ? a.q_head : a.head;
+      const float* const weight = !NORMED ? nullptr : kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr;
+      float of_value[NORMED ? 16 : 1];
+      if (NORMED && weight) {
 #pragma unroll
-      for (int k = 0; k < BATCH; ++k) {
-        const int32_t r = r0 + k * step + (lane >> log_lanes);
-        raw[k][0] = raw[k][1] = make_uint4(0, 0, 0, 0);
-        if (r >= r1) continue;
-        const TurnRow w = turn_row(c, a, r);
-        const uint16_t* from = w.kind == 0 ? (const uint16_t*)a.q + t * a.q_token + w.head * a.q_head
-                                           : (const uint16_t*)(w.kind == 1 ? a.k : a.v) + t * a.token + w.head * a.head;
-        if (first >= 0) raw[k][0] = *(const uint4*)(from + first * 8);
-        if (second >= 0) raw[k][1] = *(const uint4*)(from + second * 8);
+        for (int y = 0; y < 4; ++y) {
+          const int piece = y < 2 ? first : second;
+          const float4 f = piece >= 0 ? *(const float4*)(weight + piece * 8 + (y & 1) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+          of_value[4 * y] = f.x, of_value[4 * y + 1] = f.y, of_value[4 * y + 2] = f.z, of_value[4 * y + 3] = f.w;
+        }
       }
+      uint4 raw[BATCH][2];
+      const auto read = [&](int32_t h) {
 #pragma unroll
-      for (int k = 0; k < BATCH; ++k) {
-        const int32_t r = r0 + k * step + (lane >> log_lanes);
-        const TurnRow w = turn_row(c, a, min(r, rows - 1));
-        const uint32_t in[8] = {raw[k][0].x, raw[k][0].y, raw[k][0].z, raw[k][0].w,
-                                raw[k][1].x, raw[k][1].y, raw[k][1].z, raw[k][1].w};
-        float x[16];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float2 f = two_values<IN == P2P_KV_BF16>(in[j]);
-          x[2 * j] = f.x, x[2 * j + 1] = f.y;
+        for (int k = 0; k < BATCH; ++k) {
+          const uint16_t* const p = from + (h + k * step + of_warp) * apart;
+          const bool there = h + k * step + of_warp < h1;
+          raw[k][0] = there && first >= 0 ? __ldcs((const uint4*)(p + first * 8)) : make_uint4(0, 0, 0, 0);
+          raw[k][1] = there && second >= 0 ? __ldcs((const uint4*)(p + second * 8)) : make_uint4(0, 0, 0, 0);
         }
-        if (normed) {
-          float sum = 0.f;
+      };
+      read(h0);
+#pragma unroll 1
+      for (int32_t h = h0; h < h1; h += BATCH * step) {
+        uint4 now[BATCH][2];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) sum = fmaf(x[j], x[j], sum);
-          for (int d = 1 << log_lanes >> 1; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-          const float* weight = w.kind == 0 ? a.q_weight : w.kind == 1 ? a.k_weight : nullptr;
-          if (weight) {
-            const float by = 1.f / sqrtf(sum / c.dim + a.eps);
+        for (int k = 0; k < BATCH; ++k) now[k][0] = raw[k][0], now[k][1] = raw[k][1];
+        if (h + BATCH * step < h1) read(h + BATCH * step);
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const int piece = y ? second : first;
-              if (piece < 0) continue;
-              const float4 lo = *(const float4*)(weight + piece * 8), hi = *(const float4*)(weight + piece * 8 + 4);
-              const float f[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-              for (int j = 0; j < 8; ++j) x[8 * y + j] *= by * f[j];
-            }
-          }
-        }
-        if (r >= r1) continue;
-        if (w.kind != 2 && whole) {
+        for (int k = 0; k < BATCH; ++k) {
+          const int32_t head = h + k * step + of_warp;
+          const uint32_t in[8] = {now[k][0].x, now[k][0].y, now[k][0].z, now[k][0].w,
+                                  now[k][1].x, now[k][1].y, now[k][1].z, now[k][1].w};
+          float x[16];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            // (what is not rotated is left as it is: 0 times an infinity would not be)
-            if (8 * u + j < a.rot / 2) {
-              const float p = a.pairs ? x[2 * j] : x[j], q = a.pairs ? x[2 * j + 1] : x[8 + j];
-              const float p1 = p * cs[j] - q * sn[j], q1 = p * sn[j] + q * cs[j];
-              if (a.pairs)
-                x[2 * j] = p1, x[2 * j + 1] = q1;
-              else
-                x[j] = p1, x[8 + j] = q1;
+            const float2 f = two_values<IN == P2P_KV_BF16>(in[j]);
+            x[2 * j] = f.x, x[2 * j + 1] = f.y;
+          }
+          if (NORMED && weight) {
+            float sum = 0.f, sum2 = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(x[j], x[j], sum), sum2 = fmaf(x[8 + j], x[8 + j], sum2);
+            sum += sum2;
+            for (int d = 1 << log_lanes >> 1; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+            const float by = rsqrtf(fmaf(sum, per_value, a.eps));
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[j] *= by * of_value[j];
+          }
+          if (head >= h1) continue;
+          if (kind != 2 && mine > 0) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              // (what is not rotated is left as it is: 0 times an infinity would not be)
+              if (j < mine) {
+                constexpr int kStep = PAIRS ? 2 : 1, kApart = PAIRS ? 1 : 8;
+                const float p = x[kStep * j], q = x[kStep * j + kApart];
+                x[kStep * j] = p * cs[j] - q * sn[j];
+                x[kStep * j + kApart] = p * sn[j] + q * cs[j];
+              }
             }
           }
-        }
-        uint4 v[2];
+          if (EIGHT && kind != 0) {
+            char* const to = (kind == 2 ? c.v : c.k) + (int64_t)layer * c.layer_stride + head * c.head_stride + at;
+            const float scale = scale_of(c, layer, head, kind == 2), inverse = __frcp_rn(scale);
+            const bool usual = scale > 0x1p-60f && scale < 0x1p60f;
+            uint2 b[2];
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
-          v[y] = make_uint4(pack16<IN>(x[8 * y], x[8 * y + 1]), pack16<IN>(x[8 * y + 2], x[8 * y + 3]),
-                            pack16<IN>(x[8 * y + 4], x[8 * y + 5]), pack16<IN>(x[8 * y + 6], x[8 * y + 7]));
-        if (w.kind == 0) {
-          uint16_t* to = (uint16_t*)a.out + t * a.out_token + w.head * a.out_head;
-          if (first >= 0) *(uint4*)(to + first * 8) = v[0];
-          if (second >= 0) *(uint4*)(to + second * 8) = v[1];
-          continue;
-        }
-        char* to = (w.kind == 2 ? c.v : c.k) + (int64_t)layer * c.layer_stride + w.head * c.head_stride + at;
-        if (EIGHT) {
-          const float scale = scale_of(c, layer, w.head, w.kind == 2);
-          uint2 b[2];
+            for (int y = 0; y < 2; ++y) {
+              float z[8];
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float z[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = divide_extreme(x[8 * y + j], scale);
-            b[y].x = narrow(make_float2(z[0], z[1])) | narrow(make_float2(z[2], z[3])) << 16;
-            b[y].y = narrow(make_float2(z[4], z[5])) | narrow(make_float2(z[6], z[7])) << 16;
+              for (int j = 0; j < 8; ++j) z[j] = usual ? divide(x[8 * y + j], scale, inverse) : divide_extreme(x[8 * y + j], scale);
+              b[y].x = narrow(make_float2(z[0], z[1])) | narrow(make_float2(z[2], z[3])) << 16;
+              b[y].y = narrow(make_float2(z[4], z[5])) | narrow(make_float2(z[6], z[7])) << 16;
+            }
+            if (first >= 0) __stcs((uint2*)(to + first * 8), b[0]);
+            if (second >= 0) __stcs((uint2*)(to + second * 8), b[1]);
+            continue;
           }
-          if (first >= 0) *(uint2*)(to + first * 8) = b[0];
-          if (second >= 0) *(uint2*)(to + second * 8) = b[1];
-        } else {
-          if (w.kind == 2) v[0] = raw[k][0], v[1] = raw[k][1];
-          if (first >= 0) *(uint4*)(to + first * 16) = v[0];
-          if (second >= 0) *(uint4*)(to + second * 16) = v[1];
+          uint4 v[2] = {now[k][0], now[k][1]};  // (values of 16 bits are stored as they are)
+          if (kind != 2) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+              v[y] = make_uint4(pack16<IN>(x[8 * y], x[8 * y + 1]), pack16<IN>(x[8 * y + 2], x[8 * y + 3]),
+                                pack16<IN>(x[8 * y + 4], x[8 * y + 5]), pack16<IN>(x[8 * y + 6], x[8 * y + 7]));
+          }
+          uint16_t* const to = kind == 0 ? (uint16_t*)a.out + t * a.out_token + head * a.out_head
+                                         : (uint16_t*)((kind == 2 ? c.v : c.k) + (int64_t)layer * c.layer_stride + head * c.head_stride + at);
+          if (first >= 0) __stcs((uint4*)(to + first * 8), v[0]);
+          if (second >= 0) __stcs((uint4*)(to + second * 8), v[1]);
         }
       }
     }
@@ -238,7 +263,7 @@ __global__ void __launch_bounds__(kTurnThreads)
 #pragma unroll
       for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
       const float* weight = w.kind == 0 ? a.q_weight : w.kind == 1 ? a.k_weight : nullptr;
-      const float by = weight ? 1.f / sqrtf(sum / c.dim + a.eps) : 1.f;
+      const float by = weight ? rsqrtf(sum / c.dim + a.eps) : 1.f;
       char* to = (w.kind == 2 ? c.v : c.k) + (int64_t)layer * c.layer_stride + w.head * c.head_stride + at;
       uint16_t* out = w.kind == 0 ? (uint16_t*)a.out + t * a.out_token + w.head * a.out_head : (uint16_t*)to;
 #pragma unroll
@@ -267,7 +292,7 @@ __global__ void __launch_bounds__(kTurnThreads)
 template <int IN, bool EIGHT>
 cudaError_t launch(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t layer, int32_t n, const int32_t* seq,
                    const int64_t* offsets, int64_t n_tokens, bool wide, int num_sms, cudaStream_t st) {
-  constexpr int kBatch = 2;
+  constexpr int kBatch = 2;  // (as in turn_kernel)
   int log_lanes = 0;
   while ((16 << log_lanes) < c.dim) ++log_lanes;
   const int32_t step = wide ? kBatch * (32 >> log_lanes) : 1;  // rows that a warp takes at a time
@@ -278,8 +303,10 @@ cudaError_t launch(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t
   const int32_t parts = (int32_t)std::min<int64_t>(steps, std::max<int64_t>(1, want / n_tokens));
   const int32_t share = (steps + parts - 1) / parts * step;
   const dim3 grid((unsigned)((n_tokens + tokens - 1) / tokens), (unsigned)((rows + share - 1) / share));
+  const bool normed = a.q_weight || a.k_weight;
   if (wide)
-    return launch_early(turn_kernel<IN, EIGHT, kBatch>, grid, kTurnThreads, 0, st, c, s, a, layer, n, seq, offsets,
+    return launch_early(a.pairs ? (normed ? turn_kernel<IN, EIGHT, true, true> : turn_kernel<IN, EIGHT, false, true>)
+                                : (normed ? turn_kernel<IN, EIGHT, true, false> : turn_kernel<IN, EIGHT, false, false>), grid, kTurnThreads, 0, st, c, s, a, layer, n, seq, offsets,
                         n_tokens, tokens, log_lanes, share);
   return launch_early(turn_any_kernel<IN, EIGHT>, grid, kTurnThreads, 0, st, c, s, a, layer, n, seq, offsets, n_tokens,
                       tokens, share);
