@@ -784,27 +784,31 @@ class KvCache:
         """``write`` of one layer with norms and rotary positions in the same pass: q [tokens, query heads, head dim], k and v
         [tokens, heads, head dim]; q_weight and k_weight float32 [head dim] (None: no norm).  Returns the queries, normed and
         rotated (in out, which may be q); those of tokens of no sequence are left as they were."""
-        n, kind, dim = seq.numel(), self._types.get(k.dtype), self.dim
-        if (q.dim() != 3 or k.dim() != 3 or kind is None or q.dtype is not k.dtype or v.dtype is not k.dtype or q.shape[0] != k.shape[0]
-                or q.shape[2] != dim or tuple(k.shape[1:]) != (self.heads, dim) or v.shape != k.shape or v.stride() != k.stride()
-                or dim > 1 and (q.stride(2) != 1 or k.stride(2) != 1)):
+        n, kind, dim, dev = seq.numel(), self._types.get(k.dtype), self.dim, self.device
+        shape, of_k, strides, of_v = q.shape, k.shape, q.stride(), k.stride()
+        if (len(shape) != 3 or len(of_k) != 3 or kind is None or q.dtype is not k.dtype or v.dtype is not k.dtype or shape[0] != of_k[0]
+                or shape[2] != dim or of_k[1] != self.heads or of_k[2] != dim or v.shape != of_k or v.stride() != of_v
+                or dim > 1 and (strides[2] != 1 or of_v[2] != 1)):
             raise ValueError("q, k and v must be [tokens, heads, head dim] of one type, the last dimension contiguous, k and v strided alike")
-        if any(t is not None and t.device != self.device for t in (q, k, v, out, q_weight, k_weight, rope.turns)):
+        if q.device != dev or k.device != dev or v.device != dev or rope.turns.device != dev:
             raise ValueError("tensors must be on the cache's device")
         for w in (q_weight, k_weight):
-            if w is not None and (tuple(w.shape) != (dim,) or w.dtype is not self._float32 or not w.is_contiguous()):
-                raise ValueError("weights must be contiguous float32 [head dim]")
+            if w is not None and (tuple(w.shape) != (dim,) or w.dtype is not self._float32 or not w.is_contiguous() or w.device != dev):
+                raise ValueError("weights must be contiguous float32 [head dim] on the cache's device")
         if out is None:
-            out = self._make(q.shape, q.dtype)
-        elif out.shape != q.shape or out.dtype is not q.dtype or dim > 1 and out.stride(2) != 1:
-            raise ValueError("out must be like q, the last dimension contiguous")
+            out = self._make(shape, q.dtype)
+            out_row, out_head = shape[1] * dim, dim
+        else:
+            if out.shape != shape or out.dtype is not q.dtype or out.device != dev or dim > 1 and out.stride(2) != 1:
+                raise ValueError("out must be like q, the last dimension contiguous")
+            out_row, out_head, _ = out.stride()
         if not 0 <= layer < self.layers:
             layer = -1  # (refused by the call, whose numbers are of 32 bits)
         rotation = KvRotation(rope.dim, rope.interleaved, rope.amplitude, eps, rope.turns.data_ptr(),
                               None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
-        rc = self._write_rotated(self._h, layer, n, self._list(seq, n, self._int32), self._list(offsets, n + 1, self._int64), q.shape[0],
-                                 ctypes.byref(rotation), q.data_ptr(), q.stride(0), q.stride(1), q.shape[1], k.data_ptr(), v.data_ptr(),
-                                 k.stride(0), k.stride(1), kind, out.data_ptr(), out.stride(0), out.stride(1))
+        rc = self._write_rotated(self._h, layer, n, self._list(seq, n, self._int32), self._list(offsets, n + 1, self._int64), shape[0],
+                                 rotation, q.data_ptr(), strides[0], strides[1], shape[1], k.data_ptr(), v.data_ptr(), of_v[0], of_v[1],
+                                 kind, out.data_ptr(), out_row, out_head)
         if rc:
             _kv_check(rc, self._h)
         return out
