@@ -32,11 +32,11 @@ struct RowsShape {
   static constexpr int kQTile = 128 * DP * 2;
   static constexpr int kStage = kBt * DP * 2;          // keys or values of a step, 16 bits each
   static constexpr int kRaw = KIND == P2P_KV_E4M3 ? kBt * DP : 0;  // the same in 8 bits, on its way
-  static constexpr int kRaws = 2;
+  static constexpr int kRaws = 4;                      // two of keys, two of values
   static constexpr int kMisc = 2048;
   static constexpr int kFit = (232448 - 1024 - kMisc - kTiles * kQTile - kRaws * kRaw) / kStage;
   static constexpr int kStages = kFit < 8 ? kFit : 8;
-  static_assert(kStages >= 3, "");
+  static_assert(kStages >= 3, "keys and values of a step, and the next on their way");
   static constexpr int kBytes = 1024 + kMisc + kTiles * kQTile + kRaws * kRaw + kStages * kStage;
   static constexpr int kSoft = 4 * kTiles;             // softmax warps
   static constexpr int kThreads = (kSoft + 8) * 32;
@@ -72,7 +72,7 @@ __device__ __forceinline__ RowsStage rows_stage(int32_t q, int32_t n, bool split
   return {q == 2 * n - 1 ? n - 1 : values ? q / 2 - 1 : (q + 1) / 2, values};
 }
 struct RowsShared {
-  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], q_empty[2], q_raw[2], pair, pair_done, drain, raw[4][2];
+  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], q_empty[2], q_raw[2], pair, pair_done, drain, raw[4][4];
   RowsUnit unit[kRing];
   uint32_t sums[16];
   int32_t tmem, dead;
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 4 : 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
     for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], !direct ? 4 : a.boxes ? 1 : 64), bar_init(sh.q_raw[i], a.boxes ? 1 : 64), bar_init(sh.q_empty[i], 1), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1);
     for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
-    for (int i = 0; i < 8; ++i) bar_init(sh.raw[i / 2][i & 1], 1);
+    for (int i = 0; i < 16; ++i) bar_init(sh.raw[i / 4][i & 3], 1);
     bar_init(sh.pair, 4);
     bar_init(sh.pair_done, 4);
     bar_init(sh.drain, 1);
@@ -707,41 +707,44 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         };
         int32_t before = -1, page = -1, next = find(0);
         if (KIND == P2P_KV_E4M3 && maps.rows) {
-          // In 8 bits into room of the warp's own by the tensor memory accelerator, a step ahead; widened from there.
+          // In 8 bits into room of the warp's own by the tensor memory accelerator, two steps ahead; widened from there.
           constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
           const int piece = lane % kLanes;
           char* const raw = raws + (warp - S::kSoft) * (S::kRaw / 4);
-          const auto fetch = [&](int32_t step, int32_t from, int v) {  // which boxes there are
-            const bool there = from >= 0 && from != INT32_MAX;
-            if (from == INT32_MAX) atomicOr(w.err, KV_BAD_PAGE);
+          // Steps by turns into two places each of keys and of values; a lane keeps its box's pages of four steps.
+          const auto fetch = [&](int32_t step, int32_t from, int v) {
+            const bool there = step < n && from >= 0 && from != INT32_MAX;
+            if (step < n && from == INT32_MAX) atomicOr(w.err, KV_BAD_PAGE);
             const uint32_t which = __ballot_sync(~0u, there);
             if (step < n) {
-              if (lane == 0) bar_expect(sh.raw[warp - S::kSoft][v], __popc(which) * size * c.dim);
+              const int slot = 2 * v + (step & 1);
+              if (lane == 0) bar_expect(sh.raw[warp - S::kSoft][slot], __popc(which) * size * c.dim);
               __syncwarp();
               const int32_t t = token_of(step);
               if (there)
-                copy_box(smem_of(raw) + v * S::kRaw + lane * size * c.dim, v ? &maps.v : &maps.k, 0,
-                         t - (int32_t)c.by_page.div(t) * c.page, u.h, from, a.layer, sh.raw[warp - S::kSoft][v]);
+                copy_box(smem_of(raw) + slot * S::kRaw + lane * size * c.dim, v ? &maps.v : &maps.k, 0,
+                         t - (int32_t)c.by_page.div(t) * c.page, u.h, from, a.layer, sh.raw[warp - S::kSoft][slot]);
             }
-            return which;
           };
-          page = next;
-          uint32_t of_k = fetch(0, page, 0), of_v = fetch(0, page, 1);
-          next = find(1);
+          int32_t p0 = next, p1 = find(1), p2 = find(2), p3 = find(3);
+          const auto page_of = [&](int32_t step) { return step & 2 ? (step & 1 ? p3 : p2) : step & 1 ? p1 : p0; };
+#pragma unroll
+          for (int k = 0; k < 2; ++k) fetch(k, page_of(k), 0), fetch(k, page_of(k), 1);
 #pragma unroll 1
           for (int32_t q = 0; q < 2 * n; ++q) {
             const RowsStage it = rows_stage(q, n, split);
-            const int v = it.values, step = it.step;
-            if (!bar_wait(sh.raw[warp - S::kSoft][v], v ? raw_phase >> 1 : raw_phase & 1, sh) || !bar_wait(sh.empty[stage], phase, sh)) return;
-            raw_phase ^= 1 << v;
-            const uint32_t here = v ? of_v : of_k;
+            const int v = it.values, step = it.step, slot = 2 * v + (step & 1);
+            const int32_t his = page_of(step);
+            const uint32_t here = __ballot_sync(~0u, his >= 0 && his != INT32_MAX);
+            if (!bar_wait(sh.raw[warp - S::kSoft][slot], raw_phase >> slot & 1, sh) || !bar_wait(sh.empty[stage], phase, sh)) return;
+            raw_phase ^= 1u << slot;
             char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128);
 #pragma unroll 4
             for (int x = 0; x < kOwn; x += kAtOnce) {
               const int row = x + lane / kLanes, in_tile = own0 + row, t = (j0 + step) * kBt + in_tile;
               uint4 y = make_uint4(0, 0, 0, 0);
               if (piece < c.row16 && t >= begin && t < end && (here >> row / size & 1))
-                y = *(const uint4*)(raw + v * S::kRaw + row * c.dim + piece * 16);
+                y = *(const uint4*)(raw + slot * S::kRaw + row * c.dim + piece * 16);
               if (piece < 4 * chunks) {
                 *(uint4*)(to + in_tile * 128 + ((2 * piece & 7) ^ (in_tile & 7)) * 16) =
                     make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
@@ -753,11 +756,11 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             bar_arrive(sh.full[stage]);
             if (++stage == kStages) stage = 0, phase ^= 1;
             __syncwarp();
-            if (v) {
-              of_v = fetch(step + 1, split ? before : page, 1);
-            } else {
-              before = page, page = next, next = find(step + 2);
-              of_k = fetch(step + 1, page, 0);
+            fetch(step + 2, page_of(step + 2), v);
+            if (v) {  // (the values come last: the step's page is not needed any more)
+              const int32_t later = find(step + 4);
+              p0 = (step & 3) == 0 ? later : p0, p1 = (step & 3) == 1 ? later : p1;
+              p2 = (step & 3) == 2 ? later : p2, p3 = (step & 3) == 3 ? later : p3;
             }
           }
         } else {
@@ -856,7 +859,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       for (int i = 0; i < kStages; ++i)
         for (int x = 0; x < 1 << 16 && !bar_try(sh.full[i], i < stage ? phase ^ 1 : phase); ++x) {
         }
-      for (int v = 0; v < 2; ++v)
+      for (int v = 0; v < 4; ++v)
         for (int x = 0; x < 1 << 16 && !bar_try(sh.raw[warp - S::kSoft][v], raw_phase >> v & 1); ++x) {
         }
     }
