@@ -1,8 +1,8 @@
 """One node of the paper's cluster around its router: Algorithm 1 with the key-value cache behind the node's own trie.
 
 Requests arrive in batches and are routed.  Those that stay on the node (tree 0, its own LRU trie) are served from the
-paged cache: the matched tokens of a cached prompt are forked, the rest is appended, new tokens are decoded one by one with
-attention over the cache, and the finished prompt stays cached.  When the pages run short, the least recently used
+paged cache: the matched tokens of a cached prompt are forked, the rest is appended and attends over them and itself, new tokens are
+decoded one by one with attention over the cache, and the finished prompt stays cached.  When the pages run short, the least recently used
 tokens leave the trie (EvictLRUTrie) and the same tokens leave the cache (EvictKVCache); the pages are moved together at the
 end.  The language model is a stand-in without weights of its own: a token's queries, keys and values are fixed functions of
 its id, its position and the layer, and the next token is read off the last layer's attention.  It gives the cache real work
@@ -126,7 +126,13 @@ class Node:
         cache.extend(one, ints([len(prompt) - n]))
         rest = tokens[n:]
         pos = torch.arange(n, len(prompt), device="cuda")
-        cache.write(0, one, torch.tensor([0, len(rest)], device="cuda"), model.rows("k", rest, pos), model.rows("v", rest, pos))
+        new = torch.tensor([0, len(rest)], device="cuda")
+        cache.write(0, one, new, model.rows("k", rest, pos), model.rows("v", rest, pos))
+        # The rest of the prompt attends over the matched tokens and itself.
+        q = model.rows("q", rest, pos)
+        outs = [cache.attend_prompt(layer, q[layer], new, seq=one)[0] for layer in range(LAYERS)]
+        if check:
+            self.check(prompt, q, outs)
         self.hit_tokens += n
         self.prompt_tokens += len(prompt)
         seq = list(prompt)
@@ -148,14 +154,15 @@ class Node:
         self.lru_insert([seq])
 
     def check(self, seq, q, outs):
-        """The layers' attention again, from the tokens alone and without the cache."""
+        """The layers' attention of the sequence's last tokens again, from the tokens alone and without the cache."""
         tokens, pos = torch.tensor(seq, device="cuda"), torch.arange(len(seq), device="cuda")
         eight = self.cache.k_scale is not None
         for layer, out in enumerate(outs):
             k, v = (self.model.rows(w, tokens, pos)[layer].float().repeat_interleave(HEADS // KV_HEADS, 1) for w in "kv")
-            x = torch.einsum("hd,thd->ht", q[layer][0].float(), k) * DIM ** -0.5
-            want = torch.einsum("ht,thd->hd", torch.softmax(x, 1), v)
-            far = float((out[0].float() - want).norm() / want.norm())
+            x = torch.einsum("qhd,thd->hqt", q[layer].float(), k) * DIM ** -0.5
+            x = x.masked_fill(pos > pos[-len(out):, None], -torch.inf)   # (each of the last tokens up to itself)
+            want = torch.einsum("hqt,thd->qhd", torch.softmax(x, 2), v)
+            far = float((out.float() - want).norm() / want.norm())
             # (16 bits: the result's and the probabilities' rounding; 8 bits: of every key and value, 2^-4 at most.)
             assert far < (0.25 if eight else 0.02), (layer, far)
 

@@ -80,6 +80,34 @@ def test_work_that_several_ctas_share(cached, new, hq, hkv, dim, kind):
         assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
 
 
+@pytest.mark.parametrize("page,dim", [(1, 64), (1, 128), (7, 80), (4, 64), (100, 256), (8, 16), (2, 192), (64, 96), (3, 256)])
+@pytest.mark.parametrize("kind", ["f16", "e4m3"])
+def test_pages_of_every_type(page, dim, kind):
+    """Pages that boxes of whole tokens fit, and others; pages inside and across steps."""
+    c = make(LENGTHS, 2, dim, page, kind, "lnth")
+    q = query(sum(NEW), 10, dim, torch.float16)
+    got = c.attend_prompt(0, q, offsets_of(NEW))
+    c.sync()
+    rm.check(c, 0, q, offsets_of(NEW), dim ** -0.5, got)
+
+
+@pytest.mark.parametrize("kind,dtype", [("bf16", torch.bfloat16), ("f16", torch.float16), ("e4m3", torch.bfloat16), ("e4m3", torch.float16)])
+@pytest.mark.parametrize("hq", [6, 80])
+def test_scales_and_signs(kind, dtype, hq):
+    """Negative and zero scales, keys with negative ones, queries of very different sizes in one tile."""
+    c = make(LENGTHS, 2, 64, 16, kind)
+    if kind == "e4m3":
+        c.k_scale[0, 0] *= -1
+        c.v_scale[0, 1] *= -1
+    q = query(sum(NEW), hq, 64, dtype, size=1.0)
+    q[::3] *= 8
+    q[1::7] *= 2.0 ** -12
+    for scale in (0.125, -0.125, 0.0, 1e-30):
+        got = c.attend_prompt(0, q, offsets_of(NEW), scale)
+        c.sync()
+        rm.check(c, 0, q, offsets_of(NEW), scale, got)
+
+
 def test_as_the_call_for_one_token():
     """One new token of each sequence: attend's results, but for the order of sums."""
     lengths = [1, 2, 17, 500, 3000, 64]
