@@ -711,6 +711,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
           const int piece = lane % kLanes;
           char* const raw = raws + (warp - S::kSoft) * (S::kRaw / 4);
+          const int size_log = __ffs(size) - 1;
           // Steps by turns into two places each of keys and of values; a lane keeps its box's pages of four steps.
           const auto fetch = [&](int32_t step, int32_t from, int v) {
             const bool there = step < n && from >= 0 && from != INT32_MAX;
@@ -738,17 +739,20 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             const uint32_t here = __ballot_sync(~0u, his >= 0 && his != INT32_MAX);
             if (!bar_wait(sh.raw[warp - S::kSoft][slot], raw_phase >> slot & 1, sh) || !bar_wait(sh.empty[stage], phase, sh)) return;
             raw_phase ^= 1u << slot;
-            char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128);
-#pragma unroll 4
-            for (int x = 0; x < kOwn; x += kAtOnce) {
-              const int row = x + lane / kLanes, in_tile = own0 + row, t = (j0 + step) * kBt + in_tile;
-              uint4 y = make_uint4(0, 0, 0, 0);
-              if (piece < c.row16 && t >= begin && t < end && (here >> row / size & 1))
-                y = *(const uint4*)(raw + slot * S::kRaw + row * c.dim + piece * 16);
-              if (piece < 4 * chunks) {
-                *(uint4*)(to + in_tile * 128 + ((2 * piece & 7) ^ (in_tile & 7)) * 16) =
+            // The warp's tokens that are there.
+            const int32_t t = (j0 + step) * kBt + own0 + lane;
+            const uint32_t rows = __ballot_sync(~0u, lane < kOwn && t >= begin && t < end && (here >> (lane >> size_log) & 1));
+            char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128) + own0 * 128;
+            const char* const his_raw = raw + slot * S::kRaw + piece * 16;
+            if (piece < 4 * chunks) {
+#pragma unroll
+              for (int x = 0; x < kOwn; x += kAtOnce) {
+                const int row = x + lane / kLanes;
+                uint4 y = *(const uint4*)(his_raw + row * c.dim);
+                if (piece >= c.row16 || !(rows >> row & 1)) y = make_uint4(0, 0, 0, 0);
+                *(uint4*)(to + row * 128 + ((2 * piece & 7) ^ (row & 7)) * 16) =
                     make_uint4(widen(y.x), widen_high(y.x), widen(y.y), widen_high(y.y));
-                *(uint4*)(to + in_tile * 128 + (((2 * piece & 7) + 1) ^ (in_tile & 7)) * 16) =
+                *(uint4*)(to + row * 128 + (((2 * piece & 7) + 1) ^ (row & 7)) * 16) =
                     make_uint4(widen(y.z), widen_high(y.z), widen(y.w), widen_high(y.w));
               }
             }
