@@ -350,9 +350,9 @@ int p2p_route_decide(p2p_router* r, const int32_t* match, int64_t B, const int32
  * length[s] how many tokens it holds, refs[p] how many table entries within their sequences' lengths name page p (0:
  * free).  A hit forks the matched tokens of a cached sequence (p2p_kv_fork: pages are shared), the rest of the prompt
  * is appended (p2p_kv_extend finds pages, p2p_kv_write fills them, layer by layer or all at once), every new token
- * attends over its sequence (p2p_kv_attend; p2p_kv_attend_prompt for several new tokens a sequence, p2p_kv_attend_shared
- * for sequences that share a prefix), evicted tokens are cut off (p2p_kv_trim, as EvictLRUTrie removes them from
- * the end), and the pages in use are moved together when a part of the pool is wanted back (p2p_kv_compact).
+ * attends over its sequence (p2p_kv_attend; p2p_kv_attend_prompt for several new tokens a sequence,
+ * p2p_kv_attend_shared for sequences that share a prefix), evicted tokens are cut off (p2p_kv_trim, as EvictLRUTrie
+ * removes them from the end), and the pages in use are moved together when a part of the pool is wanted back (p2p_kv_compact).
  *
  * Conventions
  *   - Every array, the pages, table, length and refs among them, is the caller's and in DEVICE memory.  The caller sets
@@ -394,7 +394,7 @@ typedef struct p2p_kv_layout {
   int32_t *refs;        /* int32[n_pages] */
 } p2p_kv_layout;
 
-/* A handle on the cache `layout` describes, on the current CUDA device; its scratch (7 to 81 MB by type, head_dim and
+/* A handle on the cache `layout` describes, on the current CUDA device; its scratch (20 to 81 MB by type, head_dim and
  * heads, and up to 20 bytes a page and 32 a sequence) is allocated here.  The arrays stay the caller's and must outlive
  * the handle. Errors: P2P_E_INVAL (message of p2p_kv_last_error(NULL)), P2P_E_NOMEM, P2P_E_CUDA. */
 int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out);
@@ -482,27 +482,28 @@ typedef struct p2p_kv_rotation {
  * fraction is exact to 2^-64 of a turn, or to the radians' own 53 bits.  Errors: P2P_E_INVAL. */
 int p2p_kv_rotation_turns(int32_t n, const double* radians, uint64_t* turns);
 
-/* p2p_kv_write for one layer and, in the same pass, norms and rotary positions: token t of the batch, at position p of
- * its sequence (the last offsets[i+1] - offsets[i] tokens of sequence seq[i], as p2p_kv_write takes them), has queries
- * q[t * q_token_stride + h * q_head_stride + x], h < n_heads, and keys and values (k or v)[t * token_stride + h *
- * head_stride + x], h < the cache's heads, all of `type` (the cache's; for P2P_KV_E4M3 P2P_KV_BF16 or P2P_KV_F16).  Each head y of
- * queries and keys becomes, in 32 bits, w * y / sqrt(mean of y^2 + eps) where there are weights; then pair (a, b) number
- * j becomes amplitude * (a cos - b sin, a sin + b cos) of the angle 2 pi * p * turns[j] / 2^64.  The queries go, rounded to `type`, to
- * out[t * out_token_stride + h * out_head_stride + x] (q itself with its strides, or memory of its own; no two rows may
- * share values); keys and values to the cache, rounded once (P2P_KV_E4M3: the quotient by their scale).  Tokens of no
- * sequence, and those of a device-side error, are left out, their queries too.  Errors as p2p_kv_write. */
+/* p2p_kv_write for one layer and, in the same pass, norms and rotary positions: token t of the batch, at position p
+ * of its sequence (the last offsets[i+1] - offsets[i] tokens of sequence seq[i], as p2p_kv_write takes them), has
+ * queries q[t * q_token_stride + h * q_head_stride + x], h < n_heads, and keys and values (k or v)[t * token_stride +
+ * h * head_stride + x], h < the cache's heads, all of `type` (the cache's; for P2P_KV_E4M3 P2P_KV_BF16 or
+ * P2P_KV_F16). Each head y of queries and keys becomes, in 32 bits, w * y / sqrt(mean of y^2 + eps) where there are
+ * weights; then pair (a, b) number j becomes amplitude * (a cos - b sin, a sin + b cos) of the angle 2 pi * p *
+ * turns[j] / 2^64.  The queries go, rounded to `type`, to out[t * out_token_stride + h * out_head_stride + x] (q
+ * itself with its strides, or memory of its own; no two rows may share values); keys and values to the cache, rounded
+ * once (P2P_KV_E4M3: the quotient by their scale).  Tokens of no sequence, and those of a device-side error, are left
+ * out, their queries too.  Errors as p2p_kv_write. */
 int p2p_kv_write_rotated(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,
                          int64_t n_tokens, const p2p_kv_rotation* rotation, const void* q, int64_t q_token_stride,
                          int64_t q_head_stride, int32_t n_heads, const void* k, const void* v, int64_t token_stride,
                          int64_t head_stride, int32_t type, void* out, int64_t out_token_stride,
                          int64_t out_head_stride);
 
-/* Attention of several new tokens a sequence: row t of q and out, offsets[i] <= t < offsets[i+1] (int64 offsets[n+1], as
- * p2p_kv_write takes them), is token length - offsets[i+1] + t of sequence seq[i] (NULL: sequences 0 .. n-1; one may be
- * named again), its keys and values written, and attends over the tokens up to itself, the last `window` of them (0: all).
- * Other arguments, results and roundings as p2p_kv_attend, with one lse[t * n_heads + h] a row.  Rows of no sequence are
- * left as they were, as are those of a sequence out of range or with fewer tokens than rows (device-side errors, like offsets out of range).
- * n is at most 2^20, n_tokens * n_heads at most 2^29. */
+/* Attention of several new tokens a sequence: row t of q and out, offsets[i] <= t < offsets[i+1] (int64 offsets[n+1],
+ * as p2p_kv_write takes them), is token length - offsets[i+1] + t of sequence seq[i] (NULL: sequences 0 .. n-1; one
+ * may be named again), its keys and values written, and attends over the tokens up to itself, the last `window` of
+ * them (0: all). Other arguments, results and roundings as p2p_kv_attend, with one lse[t * n_heads + h] a row.  Rows
+ * of no sequence are left as they were, as are those of a sequence out of range or with fewer tokens than rows
+ * (device-side errors, like offsets out of range). n is at most 2^20, n_tokens * n_heads at most 2^29. */
 int p2p_kv_attend_prompt(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,
                          int64_t n_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t type,
                          int32_t n_heads, float scale, int32_t window, void* out, int64_t out_token_stride,
@@ -512,17 +513,16 @@ int p2p_kv_attend_prompt(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* se
 int64_t p2p_kv_attend_shared_work(const p2p_kv* kv, int32_t n, int32_t n_heads);
 
 /* p2p_kv_attend for rows that begin with the same tokens, which are read once for all of them: rows groups[g] ..
- * groups[g+1] - 1 (int32 groups[n_groups + 1], non-decreasing, within [0, n]) are a group.  What its sequences share is found
- * here: the leading page entries that are the same in all of them, as p2p_kv_fork leaves them.  Sequences that share nothing, and rows
- * of no group, are worked off each by itself, so the results are p2p_kv_attend's, but for the order of sums,
- * whatever the groups.  work: p2p_kv_attend_shared_work bytes of DEVICE memory on a 32-byte boundary, not used by
- * anything else until the call's work is done.  n_groups is at most n, n * n_heads at
- * most 2^29.  Device-side errors: as p2p_kv_attend, and groups out of range or
- * descending (no row is then grouped). */
-int p2p_kv_attend_shared(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups, const int32_t* groups,
-                         const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t type, int32_t n_heads,
-                         float scale, int32_t window, void* out, int64_t out_row_stride, int64_t out_head_stride,
-                         float* lse, void* work);
+ * groups[g+1] - 1 (int32 groups[n_groups + 1], non-decreasing, within [0, n]) are a group.  What its sequences share
+ * is found here: the leading page entries that are the same in all of them, as p2p_kv_fork leaves them.  Sequences
+ * that share nothing, and rows of no group, are worked off each by itself, so the results are p2p_kv_attend's, but
+ * for the order of sums, whatever the groups.  work: p2p_kv_attend_shared_work bytes of DEVICE memory on a 32-byte
+ * boundary, not used by anything else until the call's work is done.  n_groups is at most n, n * n_heads at most
+ * 2^29.  Device-side errors: as p2p_kv_attend, and groups out of range or descending (no row is then grouped). */
+int p2p_kv_attend_shared(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups,
+                         const int32_t* groups, const void* q, int64_t q_row_stride, int64_t q_head_stride,
+                         int32_t type, int32_t n_heads, float scale, int32_t window, void* out, int64_t out_row_stride,
+                         int64_t out_head_stride, float* lse, void* work);
 
 #ifdef __cplusplus
 }

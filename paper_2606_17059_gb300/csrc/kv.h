@@ -66,7 +66,8 @@ struct KvView {
 };
 
 // Bits of the device error word.
-enum { KV_BAD_SEQ = 1, KV_BAD_COUNT = 2, KV_NO_PAGES = 4, KV_BAD_PAGE = 8, KV_SHARED = 16, KV_BAD_OFFSETS = 32, KV_STUCK = 64 };
+enum { KV_BAD_SEQ = 1, KV_BAD_COUNT = 2, KV_NO_PAGES = 4, KV_BAD_PAGE = 8, KV_SHARED = 16, KV_BAD_OFFSETS = 32,
+    KV_STUCK = 64 };
 
 struct __align__(16) KvJob {  // copy the first `tokens` tokens of page `from` to page `to`, in every layer
   int32_t from, to, tokens, pad_;
@@ -131,8 +132,8 @@ struct KvQuery {
   float scale;
   // Whether rows of q may be read by twos, and those of out written by fours, of their values.
   bool q_pairs, out_fours;
-  // Row i is taken from token skip[i] on (NULL: all of it), and where that is not 0, put together with the result of those
-  // before: pre [row][head][value] and pre_lse [row][head].
+  // Row i is taken from token skip[i] on (NULL: all of it), and where that is not 0, put together with the result of
+  // those before: pre [row][head][value] and pre_lse [row][head].
   const int32_t* skip;
   const float *pre, *pre_lse;
 };
@@ -206,8 +207,8 @@ cudaError_t launch_kv_attend_e4m3_side(const KvView& c, const KvQuery* q, const 
                                        cudaStream_t st);
 
 
-// What the rows of each group share, into spans[n_groups] (x: leading entries that are the same; y, z: the first and the last
-// token that a row's window begins with), and the tokens of each row that its group works off, into skip[n].
+// What the rows of each group share, into spans[n_groups] (x: leading entries that are the same; y, z: the first and
+// the last token that a row's window begins with), and the tokens of each row that its group works off, into skip[n].
 cudaError_t launch_kv_share(const KvView& c, int32_t* err, int32_t n, const int32_t* seq, int32_t n_groups,
                             const int32_t* groups, int32_t window, int32_t* skip, int4* spans, cudaStream_t st);
 // Fewer shared tokens than these are read by each row for itself.
@@ -227,38 +228,43 @@ struct KvRowsCall {
   int64_t n_tokens, q_row, q_head, out_row, out_head;
   int32_t n, heads, group, type, window, layer;  // group: query heads a kv head
   FastDiv by_group;
-  int32_t shift;   // see RowsCost in kv_rows.cuh: 2^shift steps are counted as one, and a tile's rows are slope / 256 steps of tokens
+  // see RowsCost in kv_rows.cuh: 2^shift steps are counted as one, and a tile's rows are slope / 256 steps of tokens
+  int32_t shift;
   uint32_t slope;
   float scale;
   bool boxes, out32;      // whether queries come by boxes of whole tokens, and rows of out lie on 32-byte boundaries
   int32_t tile_rows;      // rows of a row tile: 128, or as many whole tokens as fit them
   const CUtensorMap* q_map;  // (host)
 };
-// The pages as tensors [layer][page][head][token][value] for copies of `rows` tokens of one head and page at a time, 16-bit
-// values 64 at a time (128 bytes, turned as the tensor cores want them), 8-bit ones whole rows; rows 0: not to be had
-// (pages that are not whole eights of tokens).
+// The pages as tensors [layer][page][head][token][value] for copies of `rows` tokens of one head and page at a time,
+// 16-bit values 64 at a time (128 bytes, turned as the tensor cores want them), 8-bit ones whole rows; rows 0: not to
+// be had (pages that are not whole eights of tokens).
 struct KvMaps {
   CUtensorMap k, v;
   int32_t rows;
 };
-// Where the part of CTA `cta` of a unit that it begins (else: goes on with) lies among the parts, in floats: for each row tile of 128
-// rows [fours of values][row][4], then maxima and sums.
+// Where the part of CTA `cta` of a unit that it begins (else: goes on with) lies among the parts, in floats: for each
+// row tile of 128 rows [fours of values][row][4], then maxima and sums.
 __host__ __device__ inline int64_t rows_part(int32_t cta, bool begins, int32_t tiles, int32_t tile, int32_t dp) {
   return (int64_t)((2 * cta + begins) * tiles + tile) * 128 * (dp + 2);
 }
 // Joins the parts of units that several CTAs of the launch before shared.
-cudaError_t launch_kv_join(const KvView& c, const KvRowsCall& a, const KvAttendScratch& w, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_join(const KvView& c, const KvRowsCall& a, const KvAttendScratch& w, int num_sms,
+    cudaStream_t st);
 // Floats of KvAttendScratch::parts: two parts a CTA, of 256 or (head_dim above 128) 128 rows.
 inline size_t kv_rows_parts(const KvView& c, int num_sms) {
   const int dp = (c.dim + 63) / 64 * 64;
   return (size_t)2 * num_sms * (dp <= 128 ? 256 : 128) * (dp + 2);
 }
 // With a = NULL they launch nothing, but make the cache's kernel ready for launches (at creation).
-cudaError_t launch_kv_rows_bf16(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+cudaError_t launch_kv_rows_bf16(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w,
+    int num_sms,
                                 cudaStream_t st);
-cudaError_t launch_kv_rows_f16(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+cudaError_t launch_kv_rows_f16(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w,
+    int num_sms,
                                cudaStream_t st);
-cudaError_t launch_kv_rows_e4m3(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+cudaError_t launch_kv_rows_e4m3(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w,
+    int num_sms,
                                 cudaStream_t st);
 
 }  // namespace p2p

@@ -125,8 +125,8 @@ __device__ __forceinline__ Both with_before(const KvQuery& a, int32_t i, int32_t
   const float p = exp2_fast((lse - most) * kLog2e), q = exp2_fast((his - most) * kLog2e), by = __fdividef(1.f, p + q);
   return {p * by, q * by, most + __logf(p + q)};
 }
-// Values d .. d + 3 of a head's result, times f; zero: 0 in their place.  t, z: what the row's sums are relative to, and its sum of
-// exp.
+// Values d .. d + 3 of a head's result, times f; zero: 0 in their place.  t, z: what the row's sums are relative to,
+// and its sum of exp.
 template <int KIND>
 __device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_t i, int32_t head, int32_t d, float4 v,
                                        float f, float t, float z, bool zero) {

@@ -143,7 +143,8 @@ cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p
 void* map_encoder() {
   void* entry = nullptr;
   cudaDriverEntryPointQueryResult found;
-  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found) == cudaSuccess &&
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault,
+      &found) == cudaSuccess &&
       found == cudaDriverEntryPointSuccess)
     return entry;
   (void)cudaGetLastError();
@@ -154,8 +155,8 @@ void* map_encoder() {
 void make_maps(const p2p::KvView& c, void* entry, p2p::KvMaps& m) {
   m.rows = 0;
   const bool eight = c.type == P2P_KV_E4M3;
-  // Tokens of a copy: a power of two that divides a page (and so lies in one), at most what a warp takes of a step; copies go to
-  // whole 128 bytes (1,024 where their pieces are turned).
+  // Tokens of a copy: a power of two that divides a page (and so lies in one), at most what a warp takes of a step;
+  // copies go to whole 128 bytes (1,024 where their pieces are turned).
   uint32_t rows = c.page & -c.page;
   rows = std::min(rows, c.dim > 128 ? 16u : 32u);
   if (!entry || (eight ? rows * c.dim % 128 != 0 : rows < 8)) return;
@@ -170,14 +171,16 @@ void make_maps(const p2p::KvView& c, void* entry, p2p::KvMaps& m) {
   const cuuint32_t box[5] = {eight ? (cuuint32_t)c.dim : 64, rows, 1, 1, 1}, step[5] = {1, 1, 1, 1, 1};
   const auto make = [&](CUtensorMap* map, void* at) {
     return ((decltype(&cuTensorMapEncodeTiled))entry)(
-               map, eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, at, size, stride, box, step,
+               map, eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, at, size, stride, box,
+                   step,
                CU_TENSOR_MAP_INTERLEAVE_NONE, eight ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   };
   if (make(&m.k, c.k) && make(&m.v, c.v)) m.rows = (int32_t)rows;
 }
 
-cudaError_t launch_rows(const p2p::KvView& c, const p2p::KvMaps& m, const p2p::KvRowsCall* a, const p2p::KvAttendScratch& w, int num_sms,
+cudaError_t launch_rows(const p2p::KvView& c, const p2p::KvMaps& m, const p2p::KvRowsCall* a,
+    const p2p::KvAttendScratch& w, int num_sms,
                         cudaStream_t st) {
   using namespace p2p;
   return (c.type == P2P_KV_BF16  ? launch_kv_rows_bf16
@@ -435,7 +438,8 @@ static int check_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq,
   if (n < 0 || n > (1 << 20) || (!seq && n > h->c.n_seqs)) return fail(h, P2P_E_INVAL, "n out of range");
   if (n_heads < 1 || n_heads > 16384 || n_heads % h->c.heads)
     return fail(h, P2P_E_INVAL, "n_heads must be a multiple of the cache's heads, at most 16,384");
-  if (bad_type(h, type)) return fail(h, P2P_E_INVAL, "type of q and out: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
+  if (bad_type(h, type)) return fail(h, P2P_E_INVAL,
+      "type of q and out: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
   if (window < 0) return fail(h, P2P_E_INVAL, "negative window");
   return P2P_OK;
 }
@@ -476,7 +480,8 @@ int p2p_kv_rotation_turns(int32_t n, const double* radians, uint64_t* turns) {
   // 1 / (2 pi) in two parts: the quotient to 2^-64 of a turn or 2^-52 of itself, whichever is more.
   constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;
   for (int32_t j = 0; j < n; ++j)
-    if (!(radians[j] >= 0.0) || !(radians[j] < 6.283185307179586)) return fail(nullptr, P2P_E_INVAL, "radians: 0 <= x < 2 pi");
+    if (!(radians[j] >= 0.0) || !(radians[j] < 6.283185307179586)) return fail(nullptr, P2P_E_INVAL,
+        "radians: 0 <= x < 2 pi");
   for (int32_t j = 0; j < n; ++j) {
     const double high = radians[j] * kHigh, low = std::fma(radians[j], kHigh, -high) + radians[j] * kLow;
     const double scaled = std::ldexp(high, 64), whole = std::floor(scaled);
@@ -494,7 +499,8 @@ int p2p_kv_write_rotated(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   if (layer < 0 || layer >= h->c.n_layers) return fail(h, P2P_E_INVAL, "layer out of range");
   if (n_tokens < 0 || n_tokens > INT32_MAX) return fail(h, P2P_E_INVAL, "n_tokens out of range");
   if (n_heads < 1 || n_heads > 16384) return fail(h, P2P_E_INVAL, "n_heads out of range");
-  if (bad_type(h, type)) return fail(h, P2P_E_INVAL, "type of q, k and v: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
+  if (bad_type(h, type)) return fail(h, P2P_E_INVAL,
+      "type of q, k and v: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
   if (!rotation) return fail(h, P2P_E_INVAL, "rotation is NULL");
   const p2p_kv_rotation& r = *rotation;
   if (r.dim < 0 || r.dim > h->c.dim || r.dim % 2) return fail(h, P2P_E_INVAL, "rotated values: even, at most head_dim");
@@ -517,8 +523,8 @@ int p2p_kv_write_rotated(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   return P2P_OK;
 }
 
-// Queries as a tensor [row][kv head][query head of it][value], copied a row tile's whole rows at a time; false where they do not lie
-// as that takes, or half a tile or more might stay empty.
+// Queries as a tensor [row][kv head][query head of it][value], copied a row tile's whole rows at a time; false where
+// they do not lie as that takes, or half a tile or more might stay empty.
 static bool make_query_map(const p2p_kv* h, const p2p::KvRowsCall& a, int64_t n_rows, CUtensorMap& map) {
   if (!h->encode || a.group > 32 || (uintptr_t)a.q % 16) return false;
   const cuuint64_t size[4] = {(cuuint64_t)h->c.dim, (cuuint64_t)a.group, (cuuint64_t)h->c.heads, (cuuint64_t)n_rows};
@@ -530,17 +536,21 @@ static bool make_query_map(const p2p_kv* h, const p2p::KvRowsCall& a, int64_t n_
   }
   const cuuint32_t box[4] = {64, (cuuint32_t)a.group, 1, (cuuint32_t)(128 / a.group)}, step[4] = {1, 1, 1, 1};
   return ((decltype(&cuTensorMapEncodeTiled))h->encode)(
-             &map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, (void*)a.q, size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+             &map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, (void*)a.q, size, stride, box, step,
+                 CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static p2p::KvRowsCall rows_call(const p2p_kv* h, CUtensorMap& q_map, int32_t layer, int32_t n, int64_t n_rows, const int32_t* seq, const void* q, int64_t q_row,
+static p2p::KvRowsCall rows_call(const p2p_kv* h, CUtensorMap& q_map, int32_t layer, int32_t n, int64_t n_rows,
+    const int32_t* seq, const void* q, int64_t q_row,
                                  int64_t q_head, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
                                  int64_t out_row, int64_t out_head, float* lse) {
   p2p::KvRowsCall a = {};
   a.q = q, a.out = out, a.lse = lse, a.seq = seq;
   a.q_row = q_row, a.q_head = q_head, a.out_row = out_row, a.out_head = out_head;
-  a.n = n, a.heads = n_heads, a.group = n_heads / h->c.heads, a.type = type, a.window = window, a.layer = layer, a.scale = scale;
+  a.n = n, a.heads = n_heads, a.group = n_heads / h->c.heads, a.type = type, a.window = window, a.layer = layer,
+      a.scale = scale;
   a.by_group = p2p::FastDiv((uint32_t)a.group);
   a.boxes = make_query_map(h, a, n_rows, q_map);
   a.tile_rows = a.boxes ? 128 / a.group * a.group : 128;
@@ -567,7 +577,8 @@ int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   if (int rc = check_rows(h, n_tokens, q, n_heads, out, out_token_stride, out_head_stride, lse)) return rc;
   DeviceGuard g(h->device);
   CUtensorMap q_map;
-  p2p::KvRowsCall a = rows_call(h, q_map, layer, n, n_tokens, seq, q, q_token_stride, q_head_stride, type, n_heads, scale, window, out,
+  p2p::KvRowsCall a = rows_call(h, q_map, layer, n, n_tokens, seq, q, q_token_stride, q_head_stride, type, n_heads,
+      scale, window, out,
                                 out_token_stride, out_head_stride, lse);
   a.offsets = offsets;
   a.n_tokens = n_tokens;
@@ -577,8 +588,8 @@ int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   return P2P_OK;
 }
 
-// Where the parts of attend_shared's work lie: each row's result over its group's tokens, what the groups share, and the tokens of
-// each row that its group works off.
+// Where the parts of attend_shared's work lie: each row's result over its group's tokens, what the groups share, and
+// the tokens of each row that its group works off.
 struct SharedWork {
   size_t lse, spans, skip, bytes;
   SharedWork(const p2p::KvView& c, int32_t n, int32_t n_heads) {
@@ -595,7 +606,8 @@ int64_t p2p_kv_attend_shared_work(const p2p_kv* h, int32_t n, int32_t n_heads) {
   return (int64_t)SharedWork(h->c, n, n_heads).bytes;
 }
 
-int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups, const int32_t* groups,
+int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups,
+    const int32_t* groups,
                          const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t type, int32_t n_heads,
                          float scale, int32_t window, void* out, int64_t out_row_stride, int64_t out_head_stride,
                          float* lse, void* work) {
@@ -617,7 +629,8 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
     // What the groups share, and the attention over it; then every row's other tokens, put together with that.
     CK(p2p::launch_kv_share(h->c, h->s.err, n, seq, n_groups, groups, window, skip, spans, h->stream));
     CUtensorMap q_map;
-    p2p::KvRowsCall a = rows_call(h, q_map, layer, n_groups, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window,
+    p2p::KvRowsCall a = rows_call(h, q_map, layer, n_groups, n, seq, q, q_row_stride, q_head_stride, type, n_heads,
+        scale, window,
                                   out, out_row_stride, out_head_stride, lse);
     a.groups = groups;
     a.spans = spans;

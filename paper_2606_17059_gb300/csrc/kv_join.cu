@@ -1,8 +1,11 @@
-// kv_join.cu -- the parts of units that several CTAs of kv_rows.cuh shared, put together: with each part's maximum m_k (in log2),
-// sum z_k and unnormalised result o_k, out = sum 2^(m_k - m) o_k / sum 2^(m_k - m) z_k, m = max m_k, in the parts' order.
+// kv_join.cu -- the parts of units that several CTAs of kv_rows.cuh shared, put together: with each part's maximum m_k
+// (in log2), sum z_k and unnormalised result o_k, out = sum 2^(m_k - m) o_k / sum 2^(m_k - m) z_k, m = max m_k, in the
+// parts' order.
 //
-// A launch of its own, as its few loads in a row then run on all SMs at once: by the CTAs that brought the last parts, 40 of 128 x
-// 128 values and 5 parts each took 22 us at the end of the launch.  A warp has four rows and up to 128 values of them.
+// A launch of its own, as its few loads in a row then run on all SMs at once: by the CTAs that brought the last parts, 40
+// tiles of 128 x 128 values and 5 parts each took 22 us at the end of the launch, and take 6 here.  A warp has four rows
+// and up to 128 values of them, so that up to 16 loads of a lane are on their way together.  7 to 18 us under ncu (cold),
+// in a graph behind kv_rows.cuh less: a chain of loads (a unit's parts, their maxima, their rows).
 #include "kv_math.cuh"
 
 namespace p2p {
@@ -114,10 +117,12 @@ __global__ void __launch_bounds__(kThreads)
 
 }  // namespace
 
-cudaError_t launch_kv_join(const KvView& c, const KvRowsCall& a, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+cudaError_t launch_kv_join(const KvView& c, const KvRowsCall& a, const KvAttendScratch& w, int num_sms,
+    cudaStream_t st) {
   const int dp = (c.dim + 63) / 64 * 64, tiles = dp <= 128 ? 2 : 1;
   if (num_sms > kMostCtas) return cudaErrorInvalidConfiguration;
-  return launch_early(dp == 64 ? join_kernel<2> : join_kernel<4>, dim3(4 * num_sms), kThreads, 0, st, c, a, w, (int32_t)num_sms,
+  return launch_early(dp == 64 ? join_kernel<2> : join_kernel<4>, dim3(4 * num_sms), kThreads, 0, st, c, a, w,
+      (int32_t)num_sms,
                       (int32_t)dp, (int32_t)tiles);
 }
 

@@ -1,17 +1,19 @@
 // kv_rotate.cu -- queries, keys and values of new tokens on their way into the paged key-value cache
 // (p2p_kv_write_rotated): norms of each head, rotary positions and the write, in one pass.
 //
-// For a head's row x of a token at position p: y = x * w / sqrt(mean x^2 + eps) where there are weights; then pair j of the
-// rotated values, (y[j], y[j + rot / 2]) or (y[2 j], y[2 j + 1]), becomes amplitude * (a cos - b sin, a sin + b cos) of
-// the angle p * f_j.  Everything in 32 bits, rounded once.
+// For a head's row x of a token at position p: y = x * w / sqrt(mean x^2 + eps) where there are weights; then pair j of
+// the rotated values, (y[j], y[j + rot / 2]) or (y[2 j], y[2 j + 1]), becomes amplitude * (a cos - b sin, a sin + b
+// cos) of the angle p * f_j.  Everything in 32 bits, rounded once.
 //
 // The angle is held in turns: f_j comes as a fraction of a turn a position, in 64 bits after the point, and the product
 // with p drops whole turns by overflowing: what is left is exact to p * 2^-64 of a turn, so a position of 2^31 - 1 is
 // rotated as precisely as one of 1.  (In 32-bit floats an angle of 10^5 radians is off by 2^-8.)
 //
-// Bound by the bytes read and written: 61 prompts of 71,000 tokens with 64 / 8 heads of 128, normed, into 8 bits take 2.8
-// GB.  A lane has two 16-byte pieces of a row, those that hold each other's partners, so that a row is four to sixteen
-// lanes and no value crosses lanes but for the norm; a token's sines are the lane's for all its heads.
+// Bound by the bytes read and written, and nearly as much by issue slots: 61 prompts of 71,000 tokens with 64 / 8 heads
+// of 128, normed, into 8 bits are 2.8 GB in 621 us on one GB300 (67% of the copy bandwidth, 56% of the issue slots; with
+// the kinds of rows in one loop, and no rows on their way ahead, 1,052).  33 single tokens: 5.4 us, a launch and a chain
+// of five loads.  A lane has two 16-byte pieces of a row, those that hold each other's partners, so that a row is four
+// to sixteen lanes and no value crosses lanes but for the norm; a token's sines are the lane's for all its heads.
 #include "kv_values.cuh"
 
 namespace p2p {
@@ -47,8 +49,8 @@ __device__ __forceinline__ TurnRow turn_row(const KvView& c, const KvTurn& a, in
   return r < c.heads ? TurnRow{1, r} : TurnRow{2, r - c.heads};
 }
 
-// x / scale rounded to 32 bits, and where that is a tie of 8 bits and the quotient is not, to its side of it (see divide_extreme); inverse:
-// 1 / scale, positive and of an ordinary size.
+// x / scale rounded to 32 bits, and where that is a tie of 8 bits and the quotient is not, to its side of it (see
+// divide_extreme); inverse: 1 / scale, positive and of an ordinary size.
 __device__ __forceinline__ float divide(float x, float scale, float inverse) {
   const float z0 = x * inverse;
   float z = fmaf(fmaf(-z0, scale, x), inverse, z0);
@@ -61,9 +63,10 @@ __device__ __forceinline__ float divide(float x, float scale, float inverse) {
   return __int_as_float(b);
 }
 
-// IN: the type of q, k and v; EIGHT: the cache holds 8 bits, else IN; NORMED: there are weights; PAIRS: interleaved.  Rows lie on 16-byte boundaries and the
-// rotated halves are whole pieces; log_lanes: of a row.  Queries, then keys, then values: what a kind's rows need stays in
-// registers, and a batch of rows is read while the one before it is worked on.
+// IN: the type of q, k and v; EIGHT: the cache holds 8 bits, else IN; NORMED: there are weights; PAIRS: interleaved.
+// Rows lie on 16-byte boundaries and the rotated halves are whole pieces; log_lanes: of a row.  Queries, then keys,
+// then values: what a kind's rows need stays in registers, and a batch of rows is read while the one before it is
+// worked on.
 template <int IN, bool EIGHT, bool NORMED, bool PAIRS>
 __global__ void __launch_bounds__(kTurnThreads, 2)
     turn_kernel(KvView c, KvScratch s, KvTurn a, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,
@@ -87,7 +90,8 @@ __global__ void __launch_bounds__(kTurnThreads, 2)
   if (!PAIRS && u < turned) first = u, second = u + turned;
   if (first >= pieces) first = -1;
   if (second >= pieces) second = -1;
-  const int mine = first < 0 || (!PAIRS && u >= turned) ? 0 : min(8, a.rot / 2 - 8 * u);  // pairs of the lane that are rotated
+  // pairs of the lane that are rotated
+  const int mine = first < 0 || (!PAIRS && u >= turned) ? 0 : min(8, a.rot / 2 - 8 * u);
   const int step = 32 >> log_lanes, of_warp = lane >> log_lanes;
   const int32_t rows = a.heads + 2 * c.heads, begin = blockIdx.y * share, end = min(rows, begin + share);
   const float per_value = 1.f / c.dim;
@@ -109,7 +113,8 @@ __global__ void __launch_bounds__(kTurnThreads, 2)
       const int32_t r_first = kind == 0 ? 0 : a.heads + (kind - 1) * c.heads, heads = kind == 0 ? a.heads : c.heads;
       const int32_t h0 = max(begin - r_first, 0), h1 = min(end - r_first, heads);
       if (h0 >= h1) continue;
-      const uint16_t* const from = kind == 0 ? (const uint16_t*)a.q + t * a.q_token : (const uint16_t*)(kind == 1 ? a.k : a.v) + t * a.token;
+      const uint16_t* const from = kind == 0 ? (const uint16_t*)a.q + t * a.q_token
+          : (const uint16_t*)(kind == 1 ? a.k : a.v) + t * a.token;
       const int64_t apart = kind == 0 ? a.q_head : a.head;
       const float* const weight = !NORMED ? nullptr : kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr;
       float of_value[NORMED ? 16 : 1];
@@ -117,7 +122,8 @@ __global__ void __launch_bounds__(kTurnThreads, 2)
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const int piece = y < 2 ? first : second;
-          const float4 f = piece >= 0 ? *(const float4*)(weight + piece * 8 + (y & 1) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float4 f = piece >= 0 ? *(const float4*)(weight + piece * 8 + (y & 1) * 4)
+              : make_float4(0.f, 0.f, 0.f, 0.f);
           of_value[4 * y] = f.x, of_value[4 * y + 1] = f.y, of_value[4 * y + 2] = f.z, of_value[4 * y + 3] = f.w;
         }
       }
@@ -181,7 +187,8 @@ __global__ void __launch_bounds__(kTurnThreads, 2)
             for (int y = 0; y < 2; ++y) {
               float z[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) z[j] = usual ? divide(x[8 * y + j], scale, inverse) : divide_extreme(x[8 * y + j], scale);
+              for (int j = 0; j < 8; ++j) z[j] = usual ? divide(x[8 * y + j], scale, inverse)
+                  : divide_extreme(x[8 * y + j], scale);
               b[y].x = narrow(make_float2(z[0], z[1])) | narrow(make_float2(z[2], z[3])) << 16;
               b[y].y = narrow(make_float2(z[4], z[5])) | narrow(make_float2(z[6], z[7])) << 16;
             }
@@ -197,7 +204,8 @@ __global__ void __launch_bounds__(kTurnThreads, 2)
                                 pack16<IN>(x[8 * y + 4], x[8 * y + 5]), pack16<IN>(x[8 * y + 6], x[8 * y + 7]));
           }
           uint16_t* const to = kind == 0 ? (uint16_t*)a.out + t * a.out_token + head * a.out_head
-                                         : (uint16_t*)((kind == 2 ? c.v : c.k) + (int64_t)layer * c.layer_stride + head * c.head_stride + at);
+                                         : (uint16_t*)((kind == 2 ? c.v : c.k) + (int64_t)layer * c.layer_stride +
+                                             head * c.head_stride + at);
           if (first >= 0) __stcs((uint4*)(to + first * 8), v[0]);
           if (second >= 0) __stcs((uint4*)(to + second * 8), v[1]);
         }
@@ -306,7 +314,8 @@ cudaError_t launch(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t
   const bool normed = a.q_weight || a.k_weight;
   if (wide)
     return launch_early(a.pairs ? (normed ? turn_kernel<IN, EIGHT, true, true> : turn_kernel<IN, EIGHT, false, true>)
-                                : (normed ? turn_kernel<IN, EIGHT, true, false> : turn_kernel<IN, EIGHT, false, false>), grid, kTurnThreads, 0, st, c, s, a, layer, n, seq, offsets,
+                                : (normed ? turn_kernel<IN, EIGHT, true, false> : turn_kernel<IN, EIGHT, false, false>),
+                                    grid, kTurnThreads, 0, st, c, s, a, layer, n, seq, offsets,
                         n_tokens, tokens, log_lanes, share);
   return launch_early(turn_any_kernel<IN, EIGHT>, grid, kTurnThreads, 0, st, c, s, a, layer, n, seq, offsets, n_tokens,
                       tokens, share);
@@ -316,12 +325,15 @@ cudaError_t launch(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t
 
 cudaError_t launch_kv_turn(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t layer, int32_t n,
                            const int32_t* seq, const int64_t* offsets, int64_t n_tokens, int num_sms, cudaStream_t st) {
-  const auto on16 = [](const void* p, int64_t x, int64_t y) { return (uintptr_t)p % 16 == 0 && x % 8 == 0 && y % 8 == 0; };
+  const auto on16 = [](const void* p, int64_t x, int64_t y) { return (uintptr_t)p % 16 == 0 && x % 8 == 0 && y % 8 == 0;
+      };
   const bool wide = on16(a.q, a.q_token, a.q_head) && on16(a.out, a.out_token, a.out_head) &&
                     on16(a.k, a.token, a.head) && on16(a.v, a.token, a.head) &&
-                    (!a.q_weight || (uintptr_t)a.q_weight % 16 == 0) && (!a.k_weight || (uintptr_t)a.k_weight % 16 == 0) &&
+                    (!a.q_weight || (uintptr_t)a.q_weight % 16 == 0) &&
+                        (!a.k_weight || (uintptr_t)a.k_weight % 16 == 0) &&
                     (a.pairs || a.rot % 16 == 0);
-  const auto f = a.type == P2P_KV_BF16 ? (c.type == P2P_KV_E4M3 ? launch<P2P_KV_BF16, true> : launch<P2P_KV_BF16, false>)
+  const auto f = a.type == P2P_KV_BF16 ? (c.type == P2P_KV_E4M3 ? launch<P2P_KV_BF16, true> : launch<P2P_KV_BF16,
+      false>)
                                        : (c.type == P2P_KV_E4M3 ? launch<P2P_KV_F16, true> : launch<P2P_KV_F16, false>);
   return f(c, s, a, layer, n, seq, offsets, n_tokens, wide, num_sms, st);
 }

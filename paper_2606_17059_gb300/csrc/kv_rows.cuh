@@ -1,21 +1,41 @@
-// kv_rows.cuh -- attention of many query rows over the same keys and values of the paged cache: the new tokens of prompts
-// (p2p_kv_attend_prompt) and the shared part of rows that begin with the same pages (p2p_kv_attend_shared).
+// kv_rows.cuh -- attention of many query rows over the same keys and values of the paged cache: the new tokens of
+// prompts (p2p_kv_attend_prompt) and the shared part of rows that begin with the same pages (p2p_kv_attend_shared).
 //
 // For a query row and the tokens t that it sees: x_t = scale * q . k_t, m = max x_t, z = sum exp(x_t - m), out = sum
-// exp(x_t - m) v_t / z, lse = m + ln z.  Rows are (token, query head of one kv head) pairs, numbered with the heads inside
-// the tokens; a unit is one or two tiles of up to 128 consecutive ones of one sequence (or group) and kv head, with the tokens that
-// any of them sees, kBt at a time.  (Where queries come by boxes, a row tile is as many whole tokens as fit 128 rows.)
+// exp(x_t - m) v_t / z, lse = m + ln z.  Rows are (token, query head of one kv head) pairs, numbered with the heads
+// inside the tokens; a unit is one or two tiles of up to 128 consecutive ones of one sequence (or group) and kv head,
+// with the tokens that any of them sees, kBt at a time.  (Where queries come by boxes, a row tile is as many whole
+// tokens as fit 128 rows.)
 //
-// Both products are the tensor cores' (tcgen05): S = Q K^T with Q and K in shared memory, O += P V with P in tensor memory
-// and V in shared memory as it lies in the pages, tokens by values, which the second product takes as its transposed operand.
-// S, P (in the place of S) and O stay in tensor memory; a thread owns a row, so maxima and sums need no shuffles.  Two tiles
-// of 128 rows take turns: while one's logits go through exp, the tensor cores work on the other's.  exp(x - m) takes for m a
-// maximum that lags the running one by at most 2^kLag (see Type), so that O is rarely rescaled.
+// Both products are the tensor cores' (tcgen05): S = Q K^T with Q and K in shared memory, O += P V with P in tensor
+// memory and V in shared memory as it lies in the pages, tokens by values, which the second product takes as its
+// transposed operand. S, P (in the place of S) and O stay in tensor memory; a thread owns a row, so maxima and sums
+// need no shuffles.  Two tiles of 128 rows take turns: while one's logits go through exp, the tensor cores work on the
+// other's.  exp(x - m) takes for m a maximum that lags the running one by at most 2^kLag (see Type), so that O is
+// rarely rescaled.
 //
-// A CTA of the persistent grid takes an equal, contiguous share of all units' steps (a step: kBt tokens); a unit that several
-// CTAs share goes to scratch in parts, which a launch after this one joins in their order (kv_join.cu).  Warps: softmax (four a row tile), copies (four), and one each for the products and the schedule, two that
-// look for infinities and NaN among the values of tokens which not all rows see: 0 * NaN is NaN, so such values are taken
-// out before the product and added to the rows that do see them at the end.
+// A CTA of the persistent grid takes an equal, contiguous share of all units' steps (a step: kBt tokens); a unit that
+// several CTAs share goes to scratch in parts, which a launch after this one joins in their order (kv_join.cu), so
+// results do not depend on timing.  A unit with one row tile alone lets both tiles take its steps by turns, each with
+// sums of its own, as one tile's chain of products and exp leaves the tensor cores idle (191 sequences of 1 to 9 new
+// tokens, 1,000 seen: 375 us, and one tile at a time 408).
+//
+// Warps: softmax (four a row tile), copies (four), one each for the products and the schedule, and two helpers, which
+// bring the queries and look for infinities and NaN among the values of tokens that not all rows see: 0 * NaN is NaN,
+// so such values are taken out before the product and added to the rows that do see them at the end.  Pages of whole
+// eights of tokens come by the tensor memory accelerator, a box of tokens of one page and head at a time, turned as the
+// products read them; others by cp.async, 16 bytes a lane (an instruction for 512 bytes instead of some kilobytes: the
+// copy warps then need 3,500 cycles for a step of 128 tokens of 128 values, more than the products and exp).  8-bit values are widened to f16 on their way through a warp's
+// registers, as queries of 16 bits have to meet values of their own type.
+//
+// Long prompts are bound by the tensor cores and the chain behind them: 4,096 tokens after 12,288, 40 / 8 heads of 128
+// in f16, 1.2e12 operations in 784 to 850 us on one GB300 (1.41 to 1.53 PFLOP/s, 73 to 80% of what cuBLAS reaches in a
+// burst; the tensor pipe is 68% active): a step's S and P V take 2,048 cycles at the rate of the tensor cores, and the
+// 3,100 that they take are a tile's products (1,024), its exp (1,500: 512 of the exponential units, the rest loads of
+// tensor memory, the maximum, rounding and the way back) and the waits between them.  Short ones are bound by what a
+// unit costs beside its steps: 1.5 to 2 us of its queries' way in and its results' way out, and 5 to 10 us of the launch
+// before the first step (the schedule, cold code).  Registers: 184 a thread for softmax, where a step's logits stay, 72
+// for the others, which spill with 56.
 #pragma once
 #include "kv_math.cuh"
 #include "kv_values.cuh"
@@ -60,8 +80,8 @@ struct RowsUnit {
   int32_t parts, part, c0;   // of the unit, where it is shared: this piece's number and the first one's CTA
   int32_t split;             // 1: both row tiles have the same rows, and every other step
 };
-// The q-th stage of a unit's n steps, keys or values of one: K0, V0, K1, V1, .., or, where the row tiles take turns with the steps, K0,
-// K1, V0, K2, V1, .., as the products need them.
+// The q-th stage of a unit's n steps, keys or values of one: K0, V0, K1, V1, .., or, where the row tiles take turns
+// with the steps, K0, K1, V0, K2, V1, .., as the products need them.
 struct RowsStage {
   int32_t step;
   bool values;
@@ -72,7 +92,8 @@ __device__ __forceinline__ RowsStage rows_stage(int32_t q, int32_t n, bool split
   return {q == 2 * n - 1 ? n - 1 : values ? q / 2 - 1 : (q + 1) / 2, values};
 }
 struct RowsShared {
-  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing], checked[8], q_empty[2], q_raw[2], pair, pair_done, drain, raw[4][4];
+  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing],
+      checked[8], q_empty[2], q_raw[2], pair, pair_done, drain, raw[4][4];
   RowsUnit unit[kRing];
   uint32_t sums[16];
   int32_t tmem, dead;
@@ -114,13 +135,16 @@ __device__ __forceinline__ bool bar_wait(const uint64_t& bar, uint32_t parity, R
 __device__ __forceinline__ void bar_expect(const uint64_t& bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_of(&bar)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, int32_t x, int32_t token, int32_t head, int32_t page,
+__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, int32_t x, int32_t token, int32_t head,
+    int32_t page,
                                          int32_t layer, const uint64_t& bar) {
   asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, "
-               "%6}], [%7];" ::"r"(to), "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(layer), "r"(smem_of(&bar))
+               "%6}], [%7];" ::"r"(to), "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(layer),
+                   "r"(smem_of(&bar))
                : "memory");
 }
-__device__ __forceinline__ void copy_query_box(uint32_t to, const CUtensorMap* map, int32_t x, int32_t head, int32_t row,
+__device__ __forceinline__ void copy_query_box(uint32_t to, const CUtensorMap* map, int32_t x, int32_t head,
+    int32_t row,
                                                const uint64_t& bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, 0, %3, %4}], "
                "[%5];" ::"r"(to), "l"(map), "r"(x), "r"(head), "r"(row), "r"(smem_of(&bar))
@@ -137,22 +161,25 @@ __device__ __forceinline__ uint32_t elected() {
 }
 __device__ __forceinline__ void mma_done(const uint64_t& bar, uint32_t one) {
   asm volatile("{ .reg .pred p; setp.ne.b32 p, %1, 0;\n"
-               "@p tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(smem_of(&bar)), "r"(one)
+               "@p tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(smem_of(&bar)),
+                   "r"(one)
                : "memory");
 }
-// A matrix in shared memory, rows of 128 bytes turned within eights of them; lead: bytes between chunks of 64 values, for an
-// operand whose rows are the product's k.
+// A matrix in shared memory, rows of 128 bytes turned within eights of them; lead: bytes between chunks of 64 values,
+// for an operand whose rows are the product's k.
 __device__ __forceinline__ uint64_t matrix(uint32_t at, uint32_t lead) {
   return (uint64_t)((at & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, uint32_t add, uint32_t one) {
   asm volatile("{ .reg .pred p, q; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %5, 0;\n"
-               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(what), "r"(add), "r"(one)
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(what),
+                   "r"(add), "r"(one)
                : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, uint32_t add, uint32_t one) {
   asm volatile("{ .reg .pred p, q; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %5, 0;\n"
-               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(what), "r"(add), "r"(one)
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(what),
+                   "r"(add), "r"(one)
                : "memory");
 }
 #define P2P_R8(r, o) "=r"((r)[o]), "=r"((r)[o + 1]), "=r"((r)[o + 2]), "=r"((r)[o + 3]), "=r"((r)[o + 4]), "=r"((r)[o + 5]), \
@@ -209,8 +236,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return x;
 }
 
-// An item of the call: a sequence with its new tokens, or a group with what it shares.  Its tiles of rows follow one another for
-// each kv head in turn.  (Rows are counted in 31 bits and costs in 32: the host sees to both.)
+// An item of the call: a sequence with its new tokens, or a group with what it shares.  Its tiles of rows follow one
+// another for each kv head in turn.  (Rows are counted in 31 bits and costs in 32: the host sees to both.)
 struct RowsItem {
   int64_t row0;             // its first row of q
   int32_t members, tiles;   // tokens (rows of the group), and tiles of them times the heads of a kv head
@@ -257,11 +284,12 @@ __device__ __forceinline__ RowsSpan rows_span(const KvRowsCall& a, const RowsIte
   const int32_t e0 = it.pos + t0 + 1, e1 = it.pos + t1 + 1;
   return {window_begin(a, e0), e1, window_begin(a, e1), e0};
 }
-// What the first j tiles of an item count for, in units of 2^shift steps: each kSet for itself and about its steps.  Any rising
-// function would do, as long as all CTAs take the same.
+// What the first j tiles of an item count for, in units of 2^shift steps: each kSet for itself and about its steps.
+// Any rising function would do, as long as all CTAs take the same.
 template <class S>
 struct RowsCost {
-  uint32_t base, most, slope, rising;  // the first tile's; how much each has more (in 512ths of a step) until they have most
+  // the first tile's; how much each has more (in 512ths of a step) until they have most
+  uint32_t base, most, slope, rising;
   int32_t shift;
   __device__ __forceinline__ RowsCost(const KvRowsCall& a, const RowsItem& it) {
     most = 0, rising = ~0u, slope = 0, shift = a.shift;
@@ -281,8 +309,10 @@ struct RowsCost {
     return r * base + (uint32_t)((uint64_t)r * (r + 1) * slope >> (9 + shift)) + (j - r) * most;
   }
 };
-// Values d .. d + 15 of a row's result: o, times f.  (Whole sectors where that is to be had, as the lanes' rows are apart.)
-__device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_t row, int32_t head, int32_t d, const float* o, float f) {
+// Values d .. d + 15 of a row's result: o, times f.  (Whole sectors where that is to be had, as the lanes' rows are
+// apart.)
+__device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_t row, int32_t head, int32_t d,
+    const float* o, float f) {
   const bool half = d + 8 >= c.dim;  // (head_dim is a multiple of 8)
   if (a.pre) {
     uint32_t b[16];
@@ -290,14 +320,16 @@ __device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_
     for (int k = 0; k < 16; ++k) b[k] = __float_as_uint(o[k] * f);
     float* const to = a.pre + (row * a.heads + head) * c.dim + d;
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), P2P_I8(b, 0) : "memory");
-    if (!half) asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 8), P2P_I8(b, 8) : "memory");
+    if (!half) asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 8), P2P_I8(b, 8)
+        : "memory");
     return;
   }
   uint16_t* const out = (uint16_t*)a.out + row * a.out_row + head * a.out_head + d;
   uint32_t b[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    b[k] = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(o[2 * k] * f, o[2 * k + 1] * f) : pack<P2P_KV_F16>(o[2 * k] * f, o[2 * k + 1] * f);
+    b[k] = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(o[2 * k] * f, o[2 * k + 1] * f)
+        : pack<P2P_KV_F16>(o[2 * k] * f, o[2 * k + 1] * f);
   if (a.out32 && !half) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out), P2P_I8(b, 0) : "memory");
   } else {
@@ -306,11 +338,12 @@ __device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_
       if (k < 8 || !half) out[k] = (uint16_t)(b[k / 2] >> (k & 1) * 16);
   }
 }
-// Infinities and NaN that were taken out of the values of `every` step from j0 to j1 (of those that not all rows see): added to the sums of the
-// rows that see them, tokens begin .. end - 1.  By a warp, whose 32 rows of sums are at o_at.  Rarely needed, so it is small, not
-// fast.
+// Infinities and NaN that were taken out of the values of `every` step from j0 to j1 (of those that not all rows see):
+// added to the sums of the rows that see them, tokens begin .. end - 1.  By a warp, whose 32 rows of sums are at o_at.
+// Rarely needed, so it is small, not fast.
 template <int KIND, int BT>
-__device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall& a, const RowsUnit& u, uint32_t o_at, int32_t j0, int32_t j1,
+__device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall& a, const RowsUnit& u, uint32_t o_at,
+    int32_t j0, int32_t j1,
                                               int32_t every, int32_t begin, int32_t end) {
   const int lane = threadIdx.x & 31;
   constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8;  // of a piece
@@ -321,7 +354,8 @@ __device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall&
     const uint32_t e = c.by_page.div(p);
     const int32_t page = row_of(c, u.seq)[e];
     if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
-    const char* const at = c.v + a.layer * c.layer_stride + page * c.page_stride + (p - (int32_t)e * c.page) * c.token_stride + u.h * c.head_stride;
+    const char* const at = c.v + a.layer * c.layer_stride + page * c.page_stride +
+        (p - (int32_t)e * c.page) * c.token_stride + u.h * c.head_stride;
     uint4 v = make_uint4(0, 0, 0, 0);
     if (lane < c.row16) v = *(const uint4*)(at + lane * 16);
     const uint32_t b[4] = {v.x, v.y, v.z, v.w};
@@ -329,7 +363,8 @@ __device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall&
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       bad |= KIND == P2P_KV_E4M3 ? (((b[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0
-                                 : (((b[k] & (KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u)) + (KIND == P2P_KV_BF16 ? 0x00800080u : 0x04000400u)) & 0x80008000u) != 0;
+                                 : (((b[k] & (KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u)) +
+                                     (KIND == P2P_KV_BF16 ? 0x00800080u : 0x04000400u)) & 0x80008000u) != 0;
 #pragma unroll 1
     for (uint32_t pieces = __ballot_sync(~0u, bad); pieces; pieces &= pieces - 1) {
       const int piece = __ffs(pieces) - 1;
@@ -341,10 +376,12 @@ __device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall&
                                               : __half2float(*(const __half*)one);
         if (fabsf(f) < INFINITY) continue;
         uint32_t o;
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(o) : "r"(o_at + piece * kValues + k) : "memory");
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(o) : "r"(o_at + piece * kValues + k)
+            : "memory");
         tmem_loaded();
         if (p >= begin && p < end) o = __float_as_uint(__uint_as_float(o) + f);
-        asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(o_at + piece * kValues + k), "r"(o) : "memory");
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(o_at + piece * kValues + k), "r"(o)
+            : "memory");
         tmem_stored();
       }
     }
@@ -369,9 +406,13 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   const bool direct = KIND != P2P_KV_E4M3 && a.scale >= 0.f;
   // (Nothing so far touches memory: it runs beside the end of the kernel before.)
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 4 : 128), bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
-    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], !direct ? 4 : a.boxes ? 1 : 64), bar_init(sh.q_raw[i], a.boxes ? 1 : 64), bar_init(sh.q_empty[i], 1), bar_init(sh.s_full[i], 1), bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1);
-    for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7), sh.poison[i] = 0;
+    for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 4 : 128),
+        bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
+    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], !direct ? 4 : a.boxes ? 1 : 64),
+        bar_init(sh.q_raw[i], a.boxes ? 1 : 64), bar_init(sh.q_empty[i], 1), bar_init(sh.s_full[i], 1),
+            bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1);
+    for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7),
+        sh.poison[i] = 0;
     for (int i = 0; i < 16; ++i) bar_init(sh.raw[i / 4][i & 3], 1);
     bar_init(sh.pair, 4);
     bar_init(sh.pair_done, 4);
@@ -380,13 +421,15 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == S::kSoft + 4) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(&sh.tmem)) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(&sh.tmem))
+        : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     before_sync();
   }
   begin_kernel();
 
-  // ---- what all items count for: a warp sums consecutive ones, 32 at a time.  (Code that runs once costs its way from memory, a
+  // ---- what all items count for: a warp sums consecutive ones, 32 at a time.  (Code that runs once costs its way from
+  // memory, a
   // microsecond every few hundred instructions: this and the schedule are kept short.)
   constexpr int kAll = S::kThreads / 32;
   const int32_t per_warp = ((a.n + kAll - 1) / kAll + 31) & ~31;
@@ -425,7 +468,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     // ================================ softmax: a thread a row
     if (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     const int tile = warp / 4, r = (warp & 3) * 32 + lane;  // of the row tile
-    const uint32_t lanes = (uint32_t)(warp & 3) << 21;      // (tensor memory's lanes 32 * (warp % 4) .., from bit 16 on)
+    // (tensor memory's lanes 32 * (warp % 4) .., from bit 16 on)
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;
     const uint32_t s_at = tmem + lanes + tile * kBt, o_at = tmem + lanes + S::kOCol + tile * DP;
     char* const q_tile = q_room + tile * S::kQTile;
     uint32_t s_phase = 0, o_phase = 0;
@@ -436,8 +480,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       row = u.row + t;
       head = u.h * a.group + (int32_t)(y - t * a.group);
     };
-    // Queries that are not multiplied as they are: a negative scale changes their signs, as exp's maximum is the products', and beside
-    // 8-bit keys bf16 ones become f16.  A thread has its row.
+    // Queries that are not multiplied as they are: a negative scale changes their signs, as exp's maximum is the
+    // products', and beside 8-bit keys bf16 ones become f16.  A thread has its row.
     uint32_t raw_phase = 0;
     const auto change_queries = [&](const RowsUnit& u) {
       if (!bar_wait(sh.q_raw[tile], raw_phase, sh)) return false;
@@ -449,21 +493,24 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         unit *= fabsf(k_scale), minus ^= k_scale < 0.f;
       }
       const uint32_t flip = minus ? 0x80008000u : 0;
-      const auto piece_at = [&](int k) { return (uint4*)(q_tile + k / 8 * (128 * 128) + r * 128 + ((k & 7) ^ (r & 7)) * 16); };
+      const auto piece_at = [&](int k) { return (uint4*)(q_tile + k / 8 * (128 * 128) + r * 128 +
+          ((k & 7) ^ (r & 7)) * 16); };
       const bool narrow = KIND == P2P_KV_E4M3 && a.type == P2P_KV_BF16;
       float down = 1.f;
       if (narrow) {
-        // In f16, scaled by a power of two so that the row's largest is in [2^14, 2^15): exact but for what is below 2^-28 of it.
-        // (Magnitudes compare as their bits do.)
+        // In f16, scaled by a power of two so that the row's largest is in [2^14, 2^15): exact but for what is below
+        // 2^-28 of it. (Magnitudes compare as their bits do.)
         uint32_t m = 0;
 #pragma unroll 4
         for (int k = 0; k < dim16 / 8; ++k) {
           const uint4 v = *piece_at(k);
-          m = __vmaxu2(m, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+          m = __vmaxu2(m, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu),
+              __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
         }
         const float largest = __uint_as_float(max(m << 16, m & 0xffff0000u));
         // (Of 0, an infinity or NaN: as they are.)
-        const int e = largest > 0.f && largest < INFINITY ? max((int)(__float_as_uint(largest) >> 23) - 127, -112) - 14 : 0;
+        const int e = largest > 0.f && largest < INFINITY ? max((int)(__float_as_uint(largest) >> 23) - 127, -112) - 14
+            : 0;
         down = __uint_as_float((127 - e) << 23), unit *= __uint_as_float((127 + e) << 23);
       }
       mul = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
@@ -508,7 +555,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (!bar_wait(sh.o_full[tile], o_phase, sh)) return;
             o_phase ^= 1;
             after_sync();
-            if (sh.poison[now]) add_poison_of<KIND, kBt>(c, a, u, o_at, from, to, u.split ? 2 : 1, valid ? begin : INT32_MAX, end);
+            if (sh.poison[now]) add_poison_of<KIND, kBt>(c, a, u, o_at, from, to, u.split ? 2 : 1, valid ? begin
+                : INT32_MAX, end);
           }
           const float2 z2 = parts_of(sum);
           float z = z2.x + z2.y, fade = 1.f, fade2 = 0.f;  // of this tile's sums, and of the second's
@@ -561,7 +609,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (keep) {
 #pragma unroll
               for (int i = 0; i < 8; ++i)
-                if (d + 4 * i < dim16) ((float4*)part)[r + (d / 4 + i) * 128] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                if (d + 4 * i < dim16) ((float4*)part)[r + (d / 4 + i) * 128] = make_float4(o[4 * i], o[4 * i + 1],
+                    o[4 * i + 2], o[4 * i + 3]);
             } else if (valid) {
               put(c, a, row, head, d, o, f);
               if (d + 16 < dim16) put(c, a, row, head, d + 16, o + 16, f);
@@ -573,7 +622,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (lane == 0) bar_arrive(sh.pair_done);
           }
         }
-        // (Loads of tensor memory are done before the next products may write there: P of this unit is announced later.)
+        // (Loads of tensor memory are done before the next products may write there: P of this unit is announced
+        // later.)
         before_sync();
         __syncwarp();
         if (now >= 0 && lane == 0) bar_arrive(sh.unit_empty[now]);
@@ -628,11 +678,13 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 #pragma unroll
           for (int i = 0; i < kBt; i += 8)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) t[k] = max3(t[k], __uint_as_float(x[i + 2 * k]), __uint_as_float(x[i + 2 * k + 1]));
+            for (int k = 0; k < 4; ++k) t[k] = max3(t[k], __uint_as_float(x[i + 2 * k]),
+                __uint_as_float(x[i + 2 * k + 1]));
           const float most = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * unit_mul;
           // (Rows past the last one, whatever they are, have no say: results would depend on it.)
           if (__any_sync(~0u, valid && most > top + (Type<KIND>::kUp + Type<KIND>::kLag))) {
-            const float next = fmaxf(most - Type<KIND>::kUp, top), fade = next == -INFINITY ? 1.f : exp2_fast(top - next);
+            const float next = fmaxf(most - Type<KIND>::kUp, top), fade = next == -INFINITY ? 1.f
+                : exp2_fast(top - next);
             top = next;
             const float2 z = parts_of(sum);
             sum = pair_of(z.x * fade, z.y * fade);
@@ -695,8 +747,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         const bool split = u.split;
         const char* const base = c.k + a.layer * c.layer_stride + u.h * c.head_stride;
         const int32_t* const pages = row_of(c, u.seq);
-        // A lane has a box of tokens of each step (a token, without maps): its first, and the page that it lies in, -1: it is not
-        // needed.
+        // A lane has a box of tokens of each step (a token, without maps): its first, and the page that it lies in, -1:
+        // it is not needed.
         const int32_t size = maps.rows ? maps.rows : 1, boxes = kOwn / size;
         const auto token_of = [&](int32_t step) { return (j0 + step) * kBt + own0 + lane * size; };
         const auto find = [&](int32_t step) {
@@ -707,7 +759,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         };
         int32_t before = -1, page = -1, next = find(0);
         if (KIND == P2P_KV_E4M3 && maps.rows) {
-          // In 8 bits into room of the warp's own by the tensor memory accelerator, two steps ahead; widened from there.
+          // In 8 bits into room of the warp's own by the tensor memory accelerator, two steps ahead; widened from
+          // there.
           constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
           const int piece = lane % kLanes;
           char* const raw = raws + (warp - S::kSoft) * (S::kRaw / 4);
@@ -737,11 +790,13 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             const int v = it.values, step = it.step, slot = 2 * v + (step & 1);
             const int32_t his = page_of(step);
             const uint32_t here = __ballot_sync(~0u, his >= 0 && his != INT32_MAX);
-            if (!bar_wait(sh.raw[warp - S::kSoft][slot], raw_phase >> slot & 1, sh) || !bar_wait(sh.empty[stage], phase, sh)) return;
+            if (!bar_wait(sh.raw[warp - S::kSoft][slot], raw_phase >> slot & 1, sh) ||
+                !bar_wait(sh.empty[stage], phase, sh)) return;
             raw_phase ^= 1u << slot;
             // The warp's tokens that are there.
             const int32_t t = (j0 + step) * kBt + own0 + lane;
-            const uint32_t rows = __ballot_sync(~0u, lane < kOwn && t >= begin && t < end && (here >> (lane >> size_log) & 1));
+            const uint32_t rows = __ballot_sync(~0u, lane < kOwn && t >= begin && t < end &&
+                (here >> (lane >> size_log) & 1));
             char* const to = stages + stage * S::kStage + (piece / 4) * (kBt * 128) + own0 * 128;
             const char* const his_raw = raw + slot * S::kRaw + piece * 16;
             if (piece < 4 * chunks) {
@@ -795,10 +850,12 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               if (there)
 #pragma unroll
                 for (int x = 0; x < S::kChunks; ++x)
-                  if (x < chunks) copy_box(smem_of(to) + x * (kBt * 128) + (own0 + lane * size) * 128, v ? &maps.v : &maps.k, x * 64, in_page, u.h, from,
+                  if (x < chunks) copy_box(smem_of(to) + x * (kBt * 128) + (own0 + lane * size) * 128, v ? &maps.v
+                      : &maps.k, x * 64, in_page, u.h, from,
                            a.layer, sh.full[stage]);
             } else {
-              const int64_t at = there && t >= begin ? (v ? across : 0) + from * c.page_stride + (int64_t)in_page * c.token_stride : -1;
+              const int64_t at = there && t >= begin ? (v ? across : 0) + from * c.page_stride +
+                  (int64_t)in_page * c.token_stride : -1;
               const bool some = there && t >= begin;
               if (KIND != P2P_KV_E4M3) {
                 constexpr int kLanes = DP == 64 ? 8 : DP == 128 ? 16 : 32, kAtOnce = 32 / kLanes;
@@ -815,11 +872,14 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
                     const int row = x0 + k * kAtOnce + lane / kLanes, in_tile = own0 + row;
                     const bool in = row < kOwn && (rows_there >> row & 1) && piece < c.row16;
                     const char* const his = in ? base + o[k] + piece * 16 : c.k;
-                    if (piece < 8 * chunks && row < kOwn) copy16(tile_at + in_tile * 128 + ((piece & 7) ^ (in_tile & 7)) * 16, his, in);
+                    if (piece < 8 * chunks && row < kOwn) copy16(tile_at + in_tile * 128 +
+                        ((piece & 7) ^ (in_tile & 7)) * 16, his, in);
                   }
                 }
-                // (Arrives when the thread's copies have; whoever reads them through another path fences after it has waited.)
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_of(&sh.full[stage])) : "memory");
+                // (Arrives when the thread's copies have; whoever reads them through another path fences after it has
+                // waited.)
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_of(&sh.full[stage]))
+                    : "memory");
               } else {
                 // 16 values a piece; widened on the way.
                 constexpr int kLanes = DP == 64 ? 4 : DP == 128 ? 8 : 16, kAtOnce = 32 / kLanes;
@@ -831,7 +891,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
                   const int row = x + lane / kLanes;
                   const int64_t o = __shfl_sync(~0u, at, row);
                   b[x / kAtOnce] = make_uint4(0, 0, 0, 0);
-                  if ((rows_there >> row & 1) && piece < c.row16) b[x / kAtOnce] = __ldcg((const uint4*)(base + o + piece * 16));
+                  if ((rows_there >> row & 1) && piece < c.row16) b[x / kAtOnce] =
+                      __ldcg((const uint4*)(base + o + piece * 16));
                 }
                 char* const tile_at = to + (piece / 4) * (kBt * 128);
 #pragma unroll
@@ -1015,7 +1076,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     };
     // floor(total * k / ctas) for this CTA and the next.
     const uint32_t whole = total / ctas, rest = total - whole * ctas;
-    const uint32_t x0 = whole * blockIdx.x + rest * blockIdx.x / ctas, x1 = whole * (blockIdx.x + 1) + rest * (blockIdx.x + 1) / ctas;
+    const uint32_t x0 = whole * blockIdx.x + rest * blockIdx.x / ctas, x1 = whole * (blockIdx.x + 1) +
+        rest * (blockIdx.x + 1) / ctas;
     // The first row's member (token) and head move by these from tile to tile, and to a tile's second half.
     const int32_t unit = kTiles * a.tile_rows, tile_t = a.by_group.div(unit), tile_g = unit - tile_t * a.group;
     const int32_t half_t = a.by_group.div(a.tile_rows), half_g = a.tile_rows - half_t * a.group;
@@ -1119,7 +1181,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             }
             u.parts = 1, u.part = 0, u.c0 = blockIdx.x;
             if (s1 - s0 < n) {
-              // The first shares that begin within the unit, and after it, by a lane each: the first k with total * k >= y * ctas.
+              // The first shares that begin within the unit, and after it, by a lane each: the first k with total * k
+              // >= y * ctas.
               const uint32_t y = x + (lane & 1 ? inside : S::kSet + 1);
               uint32_t k = (uint32_t)__fdividef((float)y * (float)ctas, (float)total);
               k = k > 1 ? k - 1 : 0;
@@ -1171,7 +1234,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (mine == 0) {
               bar_expect(there, a.tile_rows * 128 * chunks);
               for (int x = 0; x < chunks; ++x)
-                copy_query_box(smem_of(to) + x * (128 * 128), &q_map, x * 64, u.h, (int32_t)(u.row + a.by_group.div(first)), there);
+                copy_query_box(smem_of(to) + x * (128 * 128), &q_map, x * 64, u.h,
+                    (int32_t)(u.row + a.by_group.div(first)), there);
             }
             continue;
           }
@@ -1184,7 +1248,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (first + x < u.rows && x < a.tile_rows && piece * 8 < c.dim) {
               const uint32_t z = u.g0 + first + x, t = a.by_group.div(z);
               const uint16_t* const f =
-                  (const uint16_t*)a.q + (u.row + t) * a.q_row + (u.h * a.group + (int32_t)(z - t * a.group)) * a.q_head + piece * 8;
+                  (const uint16_t*)a.q + (u.row + t) * a.q_row +
+                      (u.h * a.group + (int32_t)(z - t * a.group)) * a.q_head + piece * 8;
               v = make_uint4(f[0] | f[1] << 16, f[2] | f[3] << 16, f[4] | f[5] << 16, f[6] | f[7] << 16);
             }
             *(uint4*)(to + piece / 8 * (128 * 128) + x * 128 + ((piece & 7) ^ (x & 7)) * 16) = v;
@@ -1200,12 +1265,15 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           if (!bar_wait(sh.full[stage], phase, sh)) return;
           if (it.values && (j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) {
             // An exponent of all ones carries into the sign's place.
-            constexpr uint32_t kExponent = KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = KIND == P2P_KV_BF16 ? 0x00800080u : 0x04000400u;
+            constexpr uint32_t kExponent = KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = KIND == P2P_KV_BF16
+                ? 0x00800080u : 0x04000400u;
             char* const tile = stages + stage * S::kStage;
-            const int32_t first = max(u.begin - j * kBt, 0), end = min(u.end - j * kBt, kBt);  // the rows that are somebody's
+            // the rows that are somebody's
+            const int32_t first = max(u.begin - j * kBt, 0), end = min(u.end - j * kBt, kBt);
             for (int x = mine; x < (kBt - (end - first)) * 8; x += 64) {  // (the others hold whatever lay there)
               const int row = x / 8 < first ? x / 8 : x / 8 - first + end;
-              for (int k = 0; k < S::kChunks; ++k) *(uint4*)(tile + k * (kBt * 128) + row * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+              for (int k = 0; k < S::kChunks; ++k) *(uint4*)(tile + k * (kBt * 128) + row * 128 + (x & 7) * 16) =
+                  make_uint4(0, 0, 0, 0);
             }
             uint32_t ends = 0;
 #pragma unroll 1
@@ -1213,7 +1281,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 #pragma unroll 4
               for (int x = mine; x < kBt * 8; x += 64) {
                 const uint4 v = *(const uint4*)(tile + k * (kBt * 128) + x * 16);
-                const uint32_t some = ((v.x & kExponent) + kOne) | ((v.y & kExponent) + kOne) | ((v.z & kExponent) + kOne) |
+                const uint32_t some = ((v.x & kExponent) + kOne) | ((v.y & kExponent) + kOne) | ((v.z & kExponent) +
+                    kOne) |
                                       ((v.w & kExponent) + kOne);
                 const int row = x >> 3;
                 if (row >= first && row < end) ends |= some;
@@ -1258,7 +1327,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 
 // With a = NULL the kernel is only made ready for launches.
 template <int KIND, int DP>
-cudaError_t launch_rows(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
+cudaError_t launch_rows(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+    cudaStream_t st) {
   using S = RowsShape<KIND, DP>;
   const auto kernel = rows_kernel<KIND, DP>;
   if (!a) {
@@ -1271,7 +1341,8 @@ cudaError_t launch_rows(const KvView& c, const KvMaps& m, const KvRowsCall* a, c
   return launch_early(kernel, dim3(num_sms), S::kThreads, S::kBytes, st, c, m, a->q_map ? *a->q_map : m.k, *a, w);
 }
 template <int KIND>
-cudaError_t launch_rows_dim(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+cudaError_t launch_rows_dim(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w,
+    int num_sms,
                             cudaStream_t st) {
   return c.dim <= 64    ? launch_rows<KIND, 64>(c, m, a, w, num_sms, st)
          : c.dim <= 128 ? launch_rows<KIND, 128>(c, m, a, w, num_sms, st)

@@ -2,7 +2,8 @@
 #include "kv_rows.cuh"
 
 namespace p2p {
-cudaError_t launch_kv_rows_f16(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w, int num_sms,
+cudaError_t launch_kv_rows_f16(const KvView& c, const KvMaps& m, const KvRowsCall* a, const KvAttendScratch& w,
+    int num_sms,
                                 cudaStream_t st) {
   return launch_rows_dim<P2P_KV_F16>(c, m, a, w, num_sms, st);
 }

@@ -1,5 +1,5 @@
-// kv_values.cuh -- what the kernels that write to the paged key-value cache share: where a batch's tokens go, and values
-// of 8 bits.
+// kv_values.cuh -- what the kernels that write to the paged key-value cache share: where a batch's tokens go, and
+// values of 8 bits.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -37,8 +37,8 @@ __device__ __forceinline__ int32_t find_item(const T* offsets, int32_t n, int64_
   return lo;
 }
 
-// Tokens that a group of rows works off together, from what launch_kv_share found: x entries that are the same, tokens from y on
-// seen by some row.
+// Tokens that a group of rows works off together, from what launch_kv_share found: x entries that are the same, tokens
+// from y on seen by some row.
 __device__ __forceinline__ int32_t shared_tokens(const KvView& c, int4 span, int32_t members) {
   const int32_t tokens = span.x * c.page;
   return members > 1 && tokens - span.y >= kSharedTokens ? tokens : 0;
