@@ -352,7 +352,8 @@ int p2p_route_decide(p2p_router* r, const int32_t* match, int64_t B, const int32
  * is appended (p2p_kv_extend finds pages, p2p_kv_write fills them, layer by layer or all at once), every new token
  * attends over its sequence (p2p_kv_attend; p2p_kv_attend_prompt for several new tokens a sequence,
  * p2p_kv_attend_shared for sequences that share a prefix), evicted tokens are cut off (p2p_kv_trim, as EvictLRUTrie
- * removes them from the end), and the pages in use are moved together when a part of the pool is wanted back (p2p_kv_compact).
+ * removes them from the end), and the pages in use are moved together when a part of the pool is wanted back
+ * (p2p_kv_compact).
  *
  * Conventions
  *   - Every array, the pages, table, length and refs among them, is the caller's and in DEVICE memory.  The caller sets
@@ -516,13 +517,16 @@ int64_t p2p_kv_attend_shared_work(const p2p_kv* kv, int32_t n, int32_t n_heads);
  * groups[g+1] - 1 (int32 groups[n_groups + 1], non-decreasing, within [0, n]) are a group.  What its sequences share
  * is found here: the leading page entries that are the same in all of them, as p2p_kv_fork leaves them.  Sequences
  * that share nothing, and rows of no group, are worked off each by itself, so the results are p2p_kv_attend's, but
- * for the order of sums, whatever the groups.  work: p2p_kv_attend_shared_work bytes of DEVICE memory on a 32-byte
- * boundary, not used by anything else until the call's work is done.  n_groups is at most n, n * n_heads at most
- * 2^29.  Device-side errors: as p2p_kv_attend, and groups out of range or descending (no row is then grouped). */
+ * for the order of sums, whatever the groups.  So are all rows where groups would save the reading of fewer than
+ * `least` bytes of keys and values in all, a group of m rows that share t tokens counted as m - 4 times t (0: groups
+ * are made use of in any case; negative: a number that measured well).  work: p2p_kv_attend_shared_work bytes of
+ * DEVICE memory on a 32-byte boundary, not used by anything else until the call's work is done.  n_groups is at most
+ * n, n * n_heads at most 2^29.  Device-side errors: as p2p_kv_attend, and groups out of range or descending (no row is
+ * then grouped). */
 int p2p_kv_attend_shared(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups,
-                         const int32_t* groups, const void* q, int64_t q_row_stride, int64_t q_head_stride,
-                         int32_t type, int32_t n_heads, float scale, int32_t window, void* out, int64_t out_row_stride,
-                         int64_t out_head_stride, float* lse, void* work);
+                         const int32_t* groups, int64_t least, const void* q, int64_t q_row_stride,
+                         int64_t q_head_stride, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
+                         int64_t out_row_stride, int64_t out_head_stride, float* lse, void* work);
 
 #ifdef __cplusplus
 }

@@ -138,7 +138,7 @@ def _load():
                                                     _i64, _i64, _i32, _vp, _i64, _i64]),
             "p2p_kv_attend_prompt": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _i64, _i32, _i32, ctypes.c_float, _i32,
                                                     _vp, _i64, _i64, _vp]),
-            "p2p_kv_attend_shared": (ctypes.c_int, [_vp, _i32, _i32, _vp, _i32, _vp, _vp, _i64, _i64, _i32, _i32, ctypes.c_float, _i32,
+            "p2p_kv_attend_shared": (ctypes.c_int, [_vp, _i32, _i32, _vp, _i32, _vp, _i64, _vp, _i64, _i64, _i32, _i32, ctypes.c_float, _i32,
                                                     _vp, _i64, _i64, _vp, _vp]),
             "p2p_kv_attend_shared_work": (_i64, [_vp, _i32, _i32]),
             "p2p_router_kernel_time": (ctypes.c_int, [_vp, _i32, P(ctypes.c_char_p), P(_i64), P(ctypes.c_double)]),
@@ -565,10 +565,10 @@ def p2p_kv_attend_shared_work(kv, n: int, n_heads: int) -> int:
     return int(_load().p2p_kv_attend_shared_work(kv, n, n_heads))
 
 
-def p2p_kv_attend_shared(kv, layer: int, n: int, seq, n_groups: int, groups, q, q_row_stride: int, q_head_stride: int, dtype: int,
-                         n_heads: int, scale: float, window: int, out, out_row_stride: int, out_head_stride: int, lse, work) -> None:
+def p2p_kv_attend_shared(kv, layer: int, n: int, seq, n_groups: int, groups, least: int, q, q_row_stride: int, q_head_stride: int,
+                         dtype: int, n_heads: int, scale: float, window: int, out, out_row_stride: int, out_head_stride: int, lse, work) -> None:
     """One new token of each row, groups of rows that share a prefix; q and out are addresses (their strides are arguments)."""
-    _kv_check(_load().p2p_kv_attend_shared(kv, layer, n, _addr(seq), n_groups, _addr(groups), q, q_row_stride, q_head_stride, dtype,
+    _kv_check(_load().p2p_kv_attend_shared(kv, layer, n, _addr(seq), n_groups, _addr(groups), least, q, q_row_stride, q_head_stride, dtype,
                                            n_heads, scale, window, out, out_row_stride, out_head_stride, _addr(lse), _addr(work)), kv)
 
 
@@ -838,17 +838,18 @@ class KvCache:
             _kv_check(rc, self._h)
         return out, lse
 
-    def attend_shared(self, layer: int, q, groups, scale=None, seq=None, window: int = 0, out=None, lse=None):
+    def attend_shared(self, layer: int, q, groups, scale=None, seq=None, window: int = 0, out=None, lse=None, least: int = -1):
         """As ``attend``, where rows groups[g] .. groups[g+1] - 1 (int32 [groups + 1]) begin with the same tokens in the same pages
-        (as ``fork`` leaves them): those are read once for all rows of a group."""
+        (as ``fork`` leaves them): those are read once for all rows of a group, if that saves the reading of `least` bytes of keys
+        and values in all, m - 4 times those of what m rows share (0: in any case; negative: as many as make up for it)."""
         (n, heads, dim), row, head, kind, out, out_row, out_head, lse, layer, scale, window = self._rows(layer, q, scale, window, out, lse)
         n_groups = groups.numel() - 1
         if n_groups < 0:
             raise ValueError("groups must have an entry at least")
         work = self._make((max(16, self._shared_work(self._h, n, heads)),), self._uint8)
         rc = self._attend_shared(self._h, layer, n, None if seq is None else self._list(seq, n, self._int32), n_groups,
-                                 self._list(groups, n_groups + 1, self._int32), q.data_ptr(), row, head, kind, heads, scale, window,
-                                 out.data_ptr(), out_row, out_head, lse.data_ptr(), work.data_ptr())
+                                 self._list(groups, n_groups + 1, self._int32), least, q.data_ptr(), row, head, kind, heads, scale,
+                                 window, out.data_ptr(), out_row, out_head, lse.data_ptr(), work.data_ptr())
         if rc:
             _kv_check(rc, self._h)
         return out, lse

@@ -66,6 +66,9 @@ struct KvView {
 };
 
 // Bits of the device error word.
+// What a group's rows cost together, in rows that are read alone.
+constexpr int kTogether = 4;
+
 enum { KV_BAD_SEQ = 1, KV_BAD_COUNT = 2, KV_NO_PAGES = 4, KV_BAD_PAGE = 8, KV_SHARED = 16, KV_BAD_OFFSETS = 32,
     KV_STUCK = 64 };
 
@@ -208,9 +211,13 @@ cudaError_t launch_kv_attend_e4m3_side(const KvView& c, const KvQuery* q, const 
 
 
 // What the rows of each group share, into spans[n_groups] (x: leading entries that are the same; y, z: the first and
-// the last token that a row's window begins with), and the tokens of each row that its group works off, into skip[n].
+// the last token that a row's window begins with), and the tokens of each row that its group works off, into skip[n]:
+// none, if that saves the reading of fewer than `least` tokens, a group of m rows counted as m - kTogether (0: any).
 cudaError_t launch_kv_share(const KvView& c, int32_t* err, int32_t n, const int32_t* seq, int32_t n_groups,
-                            const int32_t* groups, int32_t window, int32_t* skip, int4* spans, cudaStream_t st);
+                            const int32_t* groups, int32_t window, int64_t least, int32_t* skip, int4* spans,
+                            cudaStream_t st);
+// Reports groups that do not ascend or leave the batch.
+cudaError_t launch_kv_groups(int32_t* err, int32_t n, int32_t n_groups, const int32_t* groups, cudaStream_t st);
 // Fewer shared tokens than these are read by each row for itself.
 constexpr int kSharedTokens = 64;
 

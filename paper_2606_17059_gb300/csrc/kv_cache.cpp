@@ -606,11 +606,17 @@ int64_t p2p_kv_attend_shared_work(const p2p_kv* h, int32_t n, int32_t n_heads) {
   return (int64_t)SharedWork(h->c, n, n_heads).bytes;
 }
 
+// Bytes of keys and values whose reading has to be saved for groups to be worth three more launches.  Measured on one
+// GB300, prefixes read together and row by row: 256 MB saved (64 rows, 14 / 2 heads of 64, 8,320 tokens) 45 and 30 us;
+// 200 rows, 40 / 8 of 128, 320 tokens 48 and 38; 32 rows, 32 / 8 of 128, 2,112 tokens 32 and 26; 512 MB 59 and 51, 49
+// and 55, 36 and 43; 1,024 MB 69 and 91, 54 and 87, 46 and 75.  Few rows gain less, as what they read together is read
+// at a lower rate (kTogether): 8 rows, 64 / 8 of 128, 18,720 tokens (512 MB) 59 and 47, 37,440 (1,024 MB) 82 and 82.
+constexpr int64_t kWorthSharing = (int64_t)448 << 20;
+
 int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups,
-    const int32_t* groups,
-                         const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t type, int32_t n_heads,
-                         float scale, int32_t window, void* out, int64_t out_row_stride, int64_t out_head_stride,
-                         float* lse, void* work) {
+                         const int32_t* groups, int64_t least, const void* q, int64_t q_row_stride,
+                         int64_t q_head_stride, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
+                         int64_t out_row_stride, int64_t out_head_stride, float* lse, void* work) {
   if (int rc = check_attend(h, layer, n, seq, type, n_heads, window)) return rc;
   if ((int64_t)n * n_heads > (int64_t)1 << 29) return fail(h, P2P_E_INVAL, "n * n_heads exceeds 2^29");
   if (n_groups < 0 || n_groups > n) return fail(h, P2P_E_INVAL, "n_groups: at most n");
@@ -625,13 +631,19 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   int32_t* skip = (int32_t*)((char*)work + at.skip);
   p2p::KvQuery rest = query_of(layer, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out,
                                out_row_stride, out_head_stride, lse);
-  if (n_groups > 0) {
+  // In tokens of a row, of which no more can be saved than the tables hold and the windows let see.
+  const int64_t token = 2 * (int64_t)h->c.heads * h->c.dim * (h->c.type == P2P_KV_E4M3 ? 1 : 2);
+  const int64_t tokens = ((least < 0 ? kWorthSharing : least) + token - 1) / token;
+  const int64_t seen = (int64_t)h->c.max_pages * h->c.page;
+  if (n_groups > 0 && tokens > 0 && (n - p2p::kTogether) * (window ? std::min<int64_t>(window, seen) : seen) < tokens) {
+    CK(p2p::launch_kv_groups(h->s.err, n, n_groups, groups, h->stream));
+    h->launches += 1;
+  } else if (n_groups > 0) {
     // What the groups share, and the attention over it; then every row's other tokens, put together with that.
-    CK(p2p::launch_kv_share(h->c, h->s.err, n, seq, n_groups, groups, window, skip, spans, h->stream));
+    CK(p2p::launch_kv_share(h->c, h->s.err, n, seq, n_groups, groups, window, tokens, skip, spans, h->stream));
     CUtensorMap q_map;
     p2p::KvRowsCall a = rows_call(h, q_map, layer, n_groups, n, seq, q, q_row_stride, q_head_stride, type, n_heads,
-        scale, window,
-                                  out, out_row_stride, out_head_stride, lse);
+                                  scale, window, out, out_row_stride, out_head_stride, lse);
     a.groups = groups;
     a.spans = spans;
     a.pre = pre;

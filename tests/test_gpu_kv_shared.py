@@ -60,7 +60,7 @@ def test_against_64_bits(kind, hq, hkv, dim):
     page, order = {"bf16": (16, "lnht"), "f16": (7, "lnth"), "e4m3": (32, "hnlt")}[kind]
     c = shared_cache(PREFIXES, OWN, hkv, dim, page, kind, order)
     q = query(sum(SIZES), hq, dim, torch.float16 if kind == "f16" or (kind == "e4m3" and hq % 2) else torch.bfloat16)
-    got = c.attend_shared(0, q, groups_of(SIZES))
+    got = c.attend_shared(0, q, groups_of(SIZES), least=0)
     c.sync()
     check(c, 0, q, dim ** -0.5, got)
 
@@ -70,7 +70,7 @@ def test_against_64_bits(kind, hq, hkv, dim):
 def test_window(window, kind, dim):
     c = shared_cache(PREFIXES, OWN, 2, dim, 16, kind)
     q = query(sum(SIZES), 8, dim, torch.float16 if kind == "f16" else torch.bfloat16)
-    got = c.attend_shared(0, q, groups_of(SIZES), window=window)
+    got = c.attend_shared(0, q, groups_of(SIZES), window=window, least=0)
     c.sync()
     check(c, 0, q, dim ** -0.5, got, window=window)
 
@@ -82,7 +82,7 @@ def test_one_prefix(n, prefix, hq, hkv, dim, kind, page):
     rng = np.random.default_rng(1)
     c = shared_cache([prefix], [rng.integers(0, 70, n).tolist()], hkv, dim, page, kind, "lnth")
     q = query(n, hq, dim, torch.float16 if kind == "f16" else torch.bfloat16)
-    got, again = (c.attend_shared(0, q, groups_of([n])) for _ in "12")
+    got, again = (c.attend_shared(0, q, groups_of([n]), least=0) for _ in "12")
     c.sync()
     check(c, 0, q, dim ** -0.5, got)
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
@@ -98,7 +98,7 @@ def test_rows_of_any_order_and_groups_that_are_wrong():
                         (np.arange(n), i32([2, 2, 9, 9, 9, 60])), (np.arange(n)[::-1].copy(), groups_of(SIZES[::-1]))):
         q = query(len(seq), 6, 64, torch.bfloat16)
         for window in (0, 300):
-            got = c.attend_shared(0, q, groups, 0.2, i32(seq), window)
+            got = c.attend_shared(0, q, groups, 0.2, i32(seq), window, least=0)
             c.sync()
             check(c, 0, q, 0.2, got, i32(seq), window)
 
@@ -113,8 +113,8 @@ def test_places():
         at = room[:, 1:7, shift:shift + 64]
         at.copy_(q)
         out = torch.full((6, n, pitch + shift), 7.0, device="cuda").bfloat16().transpose(0, 1)[:, :, shift:shift + 64]
-        c.attend_shared(0, at, groups_of(SIZES), 0.2, out=out)
-        got = c.attend_shared(0, at, groups_of(SIZES), 0.2)
+        c.attend_shared(0, at, groups_of(SIZES), 0.2, out=out, least=0)
+        got = c.attend_shared(0, at, groups_of(SIZES), 0.2, least=0)
         c.sync()
         check(c, 0, q, 0.2, got)
         assert torch.equal(out, got[0])
@@ -127,7 +127,7 @@ def test_what_a_row_does_not_see():
     c.k[0, int(c.table[0, 600 // 16]), 600 % 16] = torch.nan
     c.v[0, int(c.table[0, 600 // 16]), 600 % 16] = torch.nan
     q = query(4, 4, 64, torch.bfloat16)
-    out, lse = c.attend_shared(0, q, groups_of([4]), window=200)
+    out, lse = c.attend_shared(0, q, groups_of([4]), window=200, least=0)
     c.sync()
     assert bool(torch.isnan(out[:2]).all()) and bool(torch.isfinite(out[2:]).all()) and bool(torch.isfinite(lse[2:]).all())
     a, la = c.attend(0, q, window=200)
@@ -156,7 +156,7 @@ def test_after_forks_and_in_graphs():
     def step():
         kv.extend(seq, one)
         kv.write(0, seq, o, k, v)
-        kv.attend_shared(0, q, groups, seq=seq, out=out, lse=lse)
+        kv.attend_shared(0, q, groups, seq=seq, out=out, lse=lse, least=0)
 
     with torch.cuda.stream(s):
         step()
@@ -171,6 +171,38 @@ def test_after_forks_and_in_graphs():
     kv.sync()
     check(kv, 0, q, 0.125, (out, lse), seq)
     assert kv.length[1:34].tolist() == [555 - 2 * r + 21 for r in rows]
+
+
+@pytest.mark.parametrize("window,saved", [(0, 2 * 640 + 320), (500, 2 * 640 + 320 - 2 * 200 - 20)])
+def test_groups_that_save_too_little(window, saved):
+    """Rows are worked off together from as many saved bytes on as the caller names (2 and 1 times what the groups share), and by
+    attend, bit for bit, below."""
+    c = shared_cache([640, 320, 64], [[10, 60, 110] * 2, [200] * 5, [5]], 2, 64, 16, "bf16")   # (windows begin at 150 to 250, and at 20)
+    q, groups = query(12, 6, 64, torch.bfloat16), groups_of([6, 5, 1])
+    want = c.attend(0, q, window=window)
+    for least, together in ((saved * 512, True), (saved * 512 + 1, False), (1, True), (0, True), (2 ** 62, False), (-1, False)):
+        got = c.attend_shared(0, q, groups, window=window, least=least)
+        c.sync()
+        check(c, 0, q, 0.125, got, window=window)
+        assert torch.equal(got[1], want[1]) != together
+        assert together or torch.equal(got[0], want[0])
+
+
+def test_much_that_is_saved():
+    """Without a number: what only a few hundred rows on a long prefix save is worth it, and less is not."""
+    c = shared_cache([4096], [[i % 50 for i in range(200)]], 8, 128, 64, "bf16")
+    q = query(200, 16, 128, torch.bfloat16)
+    for groups, launches in ((groups_of([200]), 4), (groups_of([2, 2]), 4)):   # (the tables may hold as much: found on the device)
+        before = c.launch_count()
+        got = c.attend_shared(0, q, groups)
+        assert c.launch_count() - before == launches
+        c.sync()
+        check(c, 0, q, 128 ** -0.5, got)
+    before = c.launch_count()
+    got = c.attend_shared(0, q[:20], groups_of([20]))
+    assert c.launch_count() - before == 2
+    c.sync()
+    check(c, 0, q[:20], 128 ** -0.5, got, i32(range(20)))
 
 
 def test_refusals_and_errors():
@@ -190,19 +222,20 @@ def test_refusals_and_errors():
     a = dict(seq=None, n_groups=1, groups=groups.data_ptr())
     for bad in (dict(work=None), dict(work=q.data_ptr() + 8), dict(groups=None, work=q.data_ptr()), dict(n_groups=-1, work=q.data_ptr())):
         b = {**a, **bad}
-        assert lib.p2p_kv_attend_shared(c.handle, 0, 3, None, b["n_groups"], b["groups"], q.data_ptr(), 256, 64, 0, 4, 0.1, 0, q.data_ptr(), 256, 64, None,
+        assert lib.p2p_kv_attend_shared(c.handle, 0, 3, None, b["n_groups"], b["groups"], 0, q.data_ptr(), 256, 64, 0, 4, 0.1, 0, q.data_ptr(), 256, 64, None,
                                         b["work"]) == g.P2P_E_INVAL
     for bad in (dict(seq=i32([0, 99, 1])), dict(seq=i32([0, 1, -1])), dict(groups=i32([0, 4])), dict(groups=i32([2, 1])), dict(groups=i32([-1, 2]))):
-        got = c.attend_shared(0, q, bad.get("groups", groups), seq=bad.get("seq"))
-        with pytest.raises(g.P2PError) as e:
-            c.sync()
-        assert e.value.code == g.P2P_E_DEVICE
-        if "groups" in bad:   # (what is left ungrouped is right all the same)
-            check(c, 0, q, 0.125, got)
-        else:
-            assert bool((got[0][1 if bad["seq"][1] == 99 else 2] == 0).all())
+        for least in (0, -1):
+            got = c.attend_shared(0, q, bad.get("groups", groups), seq=bad.get("seq"), least=least)
+            with pytest.raises(g.P2PError) as e:
+                c.sync()
+            assert e.value.code == g.P2P_E_DEVICE
+            if "groups" in bad:   # (what is left ungrouped is right all the same)
+                check(c, 0, q, 0.125, got)
+            else:
+                assert bool((got[0][1 if bad["seq"][1] == 99 else 2] == 0).all())
     c.table[1, 0] = 10 ** 6
-    c.attend_shared(0, q, groups)
+    c.attend_shared(0, q, groups, least=0)
     with pytest.raises(g.P2PError):
         c.sync()
     assert c.attend_shared(0, q[:0], groups_of([]))[0].shape == (0, 4, 64)

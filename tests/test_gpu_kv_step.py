@@ -94,7 +94,7 @@ def test_prompts_then_steps(kind, hq, hkv, dim, pairs):
         near(out[a:b], s, b - a)
     for _ in range(3):
         q, _ = new_tokens(seq, [1] * 5)
-        out, lse = kv.attend_shared(0, q, i32([0, 5]), scale, seq=i32(seq))
+        out, lse = kv.attend_shared(0, q, i32([0, 5]), scale, seq=i32(seq), least=0)
         alone, lse1 = kv.attend(0, q, scale, seq=i32(seq))
         kv.sync()
         for i, s in enumerate(seq):
@@ -110,7 +110,7 @@ def test_two_caches_at_once():
     queries = [query(1267, 14, c.dim, c.k.dtype) for c in caches]
     want = []
     for c, q in zip(caches, queries):
-        want.append((c.attend_prompt(0, q, o), c.attend_shared(0, q[:4].contiguous(), i32([0, 4]))))
+        want.append((c.attend_prompt(0, q, o), c.attend_shared(0, q[:4].contiguous(), i32([0, 4]), least=0)))
         c.sync()
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in caches]
@@ -120,7 +120,7 @@ def test_two_caches_at_once():
     for _ in range(20):
         for i, (c, q) in enumerate(zip(caches, queries)):
             with torch.cuda.stream(streams[i]):
-                got[i].append((c.attend_prompt(0, q, o), c.attend_shared(0, q[:4], i32([0, 4]))))
+                got[i].append((c.attend_prompt(0, q, o), c.attend_shared(0, q[:4], i32([0, 4]), least=0)))
     torch.cuda.synchronize()
     for c, results, w in zip(caches, got, want):
         c.sync()
@@ -147,7 +147,7 @@ def test_many_short_sequences_and_many_groups():
     rm.check(c, 0, q[rows], part, 0.125, (got[0][rows], got[1][rows]), i32(some))
     q = query(2 * n, 4, 64, torch.bfloat16)
     seq = i32(np.repeat(np.arange(n), 2))
-    out, lse = c.attend_shared(0, q, i32(range(0, 2 * n + 1, 2)), seq=seq)
+    out, lse = c.attend_shared(0, q, i32(range(0, 2 * n + 1, 2)), seq=seq, least=0)
     alone, lse1 = c.attend(0, q, seq=seq)
     c.sync()
     assert torch.allclose(out.float(), alone.float(), atol=2.0 ** -7, rtol=2.0 ** -6) and torch.allclose(lse, lse1, atol=1e-4)

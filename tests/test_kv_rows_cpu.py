@@ -66,7 +66,7 @@ def test_calls_without_a_handle():
     r = g.KvRotation()
     for rc in (lib.p2p_kv_write_rotated(None, 0, 1, None, None, 1, ctypes.byref(r), None, 0, 0, 1, None, None, 0, 0, 0, None, 0, 0),
                lib.p2p_kv_attend_prompt(None, 0, 1, None, None, 1, None, 0, 0, 0, 1, 1.0, 0, None, 0, 0, None),
-               lib.p2p_kv_attend_shared(None, 0, 1, None, 0, None, None, 0, 0, 0, 1, 1.0, 0, None, 0, 0, None, None)):
+               lib.p2p_kv_attend_shared(None, 0, 1, None, 0, None, 0, None, 0, 0, 0, 1, 1.0, 0, None, 0, 0, None, None)):
         assert rc == g.P2P_E_INVAL
     assert lib.p2p_kv_attend_shared_work(None, 1, 1) == -1
 
