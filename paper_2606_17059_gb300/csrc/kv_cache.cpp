@@ -143,8 +143,8 @@ cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p
 void* map_encoder() {
   void* entry = nullptr;
   cudaDriverEntryPointQueryResult found;
-  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault,
-      &found) == cudaSuccess &&
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found) ==
+          cudaSuccess &&
       found == cudaDriverEntryPointSuccess)
     return entry;
   (void)cudaGetLastError();
@@ -180,8 +180,7 @@ void make_maps(const p2p::KvView& c, void* entry, p2p::KvMaps& m) {
 }
 
 cudaError_t launch_rows(const p2p::KvView& c, const p2p::KvMaps& m, const p2p::KvRowsCall* a,
-    const p2p::KvAttendScratch& w, int num_sms,
-                        cudaStream_t st) {
+                        const p2p::KvAttendScratch& w, int num_sms, cudaStream_t st) {
   using namespace p2p;
   return (c.type == P2P_KV_BF16  ? launch_kv_rows_bf16
           : c.type == P2P_KV_F16 ? launch_kv_rows_f16
@@ -438,8 +437,8 @@ static int check_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq,
   if (n < 0 || n > (1 << 20) || (!seq && n > h->c.n_seqs)) return fail(h, P2P_E_INVAL, "n out of range");
   if (n_heads < 1 || n_heads > 16384 || n_heads % h->c.heads)
     return fail(h, P2P_E_INVAL, "n_heads must be a multiple of the cache's heads, at most 16,384");
-  if (bad_type(h, type)) return fail(h, P2P_E_INVAL,
-      "type of q and out: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
+  if (bad_type(h, type))
+    return fail(h, P2P_E_INVAL, "type of q and out: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
   if (window < 0) return fail(h, P2P_E_INVAL, "negative window");
   return P2P_OK;
 }
@@ -480,8 +479,8 @@ int p2p_kv_rotation_turns(int32_t n, const double* radians, uint64_t* turns) {
   // 1 / (2 pi) in two parts: the quotient to 2^-64 of a turn or 2^-52 of itself, whichever is more.
   constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;
   for (int32_t j = 0; j < n; ++j)
-    if (!(radians[j] >= 0.0) || !(radians[j] < 6.283185307179586)) return fail(nullptr, P2P_E_INVAL,
-        "radians: 0 <= x < 2 pi");
+    if (!(radians[j] >= 0.0) || !(radians[j] < 6.283185307179586))
+      return fail(nullptr, P2P_E_INVAL, "radians: 0 <= x < 2 pi");
   for (int32_t j = 0; j < n; ++j) {
     const double high = radians[j] * kHigh, low = std::fma(radians[j], kHigh, -high) + radians[j] * kLow;
     const double scaled = std::ldexp(high, 64), whole = std::floor(scaled);
@@ -499,8 +498,8 @@ int p2p_kv_write_rotated(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   if (layer < 0 || layer >= h->c.n_layers) return fail(h, P2P_E_INVAL, "layer out of range");
   if (n_tokens < 0 || n_tokens > INT32_MAX) return fail(h, P2P_E_INVAL, "n_tokens out of range");
   if (n_heads < 1 || n_heads > 16384) return fail(h, P2P_E_INVAL, "n_heads out of range");
-  if (bad_type(h, type)) return fail(h, P2P_E_INVAL,
-      "type of q, k and v: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
+  if (bad_type(h, type))
+    return fail(h, P2P_E_INVAL, "type of q, k and v: the cache's own (bf16 or f16 for P2P_KV_E4M3)");
   if (!rotation) return fail(h, P2P_E_INVAL, "rotation is NULL");
   const p2p_kv_rotation& r = *rotation;
   if (r.dim < 0 || r.dim > h->c.dim || r.dim % 2) return fail(h, P2P_E_INVAL, "rotated values: even, at most head_dim");
@@ -537,15 +536,14 @@ static bool make_query_map(const p2p_kv* h, const p2p::KvRowsCall& a, int64_t n_
   const cuuint32_t box[4] = {64, (cuuint32_t)a.group, 1, (cuuint32_t)(128 / a.group)}, step[4] = {1, 1, 1, 1};
   return ((decltype(&cuTensorMapEncodeTiled))h->encode)(
              &map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, (void*)a.q, size, stride, box, step,
-                 CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 static p2p::KvRowsCall rows_call(const p2p_kv* h, CUtensorMap& q_map, int32_t layer, int32_t n, int64_t n_rows,
-    const int32_t* seq, const void* q, int64_t q_row,
-                                 int64_t q_head, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
-                                 int64_t out_row, int64_t out_head, float* lse) {
+                                 const int32_t* seq, const void* q, int64_t q_row, int64_t q_head, int32_t type,
+                                 int32_t n_heads, float scale, int32_t window, void* out, int64_t out_row,
+                                 int64_t out_head, float* lse) {
   p2p::KvRowsCall a = {};
   a.q = q, a.out = out, a.lse = lse, a.seq = seq;
   a.q_row = q_row, a.q_head = q_head, a.out_row = out_row, a.out_head = out_head;
@@ -578,8 +576,7 @@ int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   DeviceGuard g(h->device);
   CUtensorMap q_map;
   p2p::KvRowsCall a = rows_call(h, q_map, layer, n, n_tokens, seq, q, q_token_stride, q_head_stride, type, n_heads,
-      scale, window, out,
-                                out_token_stride, out_head_stride, lse);
+                                scale, window, out, out_token_stride, out_head_stride, lse);
   a.offsets = offsets;
   a.n_tokens = n_tokens;
   CK(launch_rows(h->c, h->maps, &a, h->w, h->num_sms, h->stream));
@@ -633,7 +630,7 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
                                out_row_stride, out_head_stride, lse);
   // In tokens of a row, of which no more can be saved than the tables hold and the windows let see.
   const int64_t token = 2 * (int64_t)h->c.heads * h->c.dim * (h->c.type == P2P_KV_E4M3 ? 1 : 2);
-  const int64_t tokens = ((least < 0 ? kWorthSharing : least) + token - 1) / token;
+  const int64_t bytes = least < 0 ? kWorthSharing : least, tokens = bytes / token + (bytes % token > 0);
   const int64_t seen = (int64_t)h->c.max_pages * h->c.page;
   if (n_groups > 0 && tokens > 0 && (n - p2p::kTogether) * (window ? std::min<int64_t>(window, seen) : seen) < tokens) {
     CK(p2p::launch_kv_groups(h->s.err, n, n_groups, groups, h->stream));

@@ -118,12 +118,11 @@ __global__ void __launch_bounds__(kThreads)
 }  // namespace
 
 cudaError_t launch_kv_join(const KvView& c, const KvRowsCall& a, const KvAttendScratch& w, int num_sms,
-    cudaStream_t st) {
+                           cudaStream_t st) {
   const int dp = (c.dim + 63) / 64 * 64, tiles = dp <= 128 ? 2 : 1;
   if (num_sms > kMostCtas) return cudaErrorInvalidConfiguration;
   return launch_early(dp == 64 ? join_kernel<2> : join_kernel<4>, dim3(4 * num_sms), kThreads, 0, st, c, a, w,
-      (int32_t)num_sms,
-                      (int32_t)dp, (int32_t)tiles);
+                      (int32_t)num_sms, (int32_t)dp, (int32_t)tiles);
 }
 
 }  // namespace p2p

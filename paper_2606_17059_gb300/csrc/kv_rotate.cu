@@ -315,8 +315,7 @@ cudaError_t launch(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t
   if (wide)
     return launch_early(a.pairs ? (normed ? turn_kernel<IN, EIGHT, true, true> : turn_kernel<IN, EIGHT, false, true>)
                                 : (normed ? turn_kernel<IN, EIGHT, true, false> : turn_kernel<IN, EIGHT, false, false>),
-                                    grid, kTurnThreads, 0, st, c, s, a, layer, n, seq, offsets,
-                        n_tokens, tokens, log_lanes, share);
+                        grid, kTurnThreads, 0, st, c, s, a, layer, n, seq, offsets, n_tokens, tokens, log_lanes, share);
   return launch_early(turn_any_kernel<IN, EIGHT>, grid, kTurnThreads, 0, st, c, s, a, layer, n, seq, offsets, n_tokens,
                       tokens, share);
 }
@@ -325,8 +324,9 @@ cudaError_t launch(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t
 
 cudaError_t launch_kv_turn(const KvView& c, const KvScratch& s, const KvTurn& a, int32_t layer, int32_t n,
                            const int32_t* seq, const int64_t* offsets, int64_t n_tokens, int num_sms, cudaStream_t st) {
-  const auto on16 = [](const void* p, int64_t x, int64_t y) { return (uintptr_t)p % 16 == 0 && x % 8 == 0 && y % 8 == 0;
-      };
+  const auto on16 = [](const void* p, int64_t x, int64_t y) {
+    return (uintptr_t)p % 16 == 0 && x % 8 == 0 && y % 8 == 0;
+  };
   const bool wide = on16(a.q, a.q_token, a.q_head) && on16(a.out, a.out_token, a.out_head) &&
                     on16(a.k, a.token, a.head) && on16(a.v, a.token, a.head) &&
                     (!a.q_weight || (uintptr_t)a.q_weight % 16 == 0) &&

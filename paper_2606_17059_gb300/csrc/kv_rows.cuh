@@ -25,8 +25,9 @@
 // so such values are taken out before the product and added to the rows that do see them at the end.  Pages of whole
 // eights of tokens come by the tensor memory accelerator, a box of tokens of one page and head at a time, turned as the
 // products read them; others by cp.async, 16 bytes a lane (an instruction for 512 bytes instead of some kilobytes: the
-// copy warps then need 3,500 cycles for a step of 128 tokens of 128 values, more than the products and exp).  8-bit values are widened to f16 on their way through a warp's
-// registers, as queries of 16 bits have to meet values of their own type.
+// copy warps then need 3,500 cycles for a step of 128 tokens of 128 values, more than the products and exp).  8-bit
+// values are widened to f16 on their way through a warp's registers, as queries of 16 bits have to meet values of their
+// own type.
 //
 // Long prompts are bound by the tensor cores and the chain behind them: 4,096 tokens after 12,288, 40 / 8 heads of 128
 // in f16, 1.2e12 operations in 784 to 850 us on one GB300 (1.41 to 1.53 PFLOP/s, 73 to 80% of what cuBLAS reaches in a
@@ -429,8 +430,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   begin_kernel();
 
   // ---- what all items count for: a warp sums consecutive ones, 32 at a time.  (Code that runs once costs its way from
-  // memory, a
-  // microsecond every few hundred instructions: this and the schedule are kept short.)
+  // memory, a microsecond every few hundred instructions: this and the schedule are kept short.)
   constexpr int kAll = S::kThreads / 32;
   const int32_t per_warp = ((a.n + kAll - 1) / kAll + 31) & ~31;
   uint32_t sum_of = 0;

@@ -180,7 +180,7 @@ def test_groups_that_save_too_little(window, saved):
     c = shared_cache([640, 320, 64], [[10, 60, 110] * 2, [200] * 5, [5]], 2, 64, 16, "bf16")   # (windows begin at 150 to 250, and at 20)
     q, groups = query(12, 6, 64, torch.bfloat16), groups_of([6, 5, 1])
     want = c.attend(0, q, window=window)
-    for least, together in ((saved * 512, True), (saved * 512 + 1, False), (1, True), (0, True), (2 ** 62, False), (-1, False)):
+    for least, together in ((saved * 512, True), (saved * 512 + 1, False), (1, True), (0, True), (2 ** 63 - 1, False), (-1, False)):
         got = c.attend_shared(0, q, groups, window=window, least=least)
         c.sync()
         check(c, 0, q, 0.125, got, window=window)
