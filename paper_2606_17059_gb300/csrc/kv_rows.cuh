@@ -286,7 +286,8 @@ __device__ __forceinline__ RowsSpan rows_span(const KvRowsCall& a, const RowsIte
   return {window_begin(a, e0), e1, window_begin(a, e1), e0};
 }
 // What the first j tiles of an item count for, in units of 2^shift steps: each kSet for itself and about its steps.
-// Any rising function would do, as long as all CTAs take the same.
+// Any rising function would do, as long as all CTAs take the same and a tile counts for more than kSet: a share that
+// ends kSet after a unit's begin has none of its steps.
 template <class S>
 struct RowsCost {
   // the first tile's; how much each has more (in 512ths of a step) until they have most
@@ -295,13 +296,13 @@ struct RowsCost {
   __device__ __forceinline__ RowsCost(const KvRowsCall& a, const RowsItem& it) {
     most = 0, rising = ~0u, slope = 0, shift = a.shift;
     if (a.spans) {
-      base = ((((it.shared - 1) >> S::kBtLog) - (it.first >> S::kBtLog) + 1) >> shift) + S::kSet;
+      base = max((((it.shared - 1) >> S::kBtLog) - (it.first >> S::kBtLog) + 1) >> shift, 1) + S::kSet;
       return;
     }
     slope = a.slope;
-    base = (((it.pos >> S::kBtLog) + 1) >> shift) + S::kSet;
+    base = max(((it.pos >> S::kBtLog) + 1) >> shift, 1) + S::kSet;
     if (a.window) {
-      most = (((a.window >> S::kBtLog) + (slope >> 8) + 2) >> shift) + S::kSet;
+      most = max(((a.window >> S::kBtLog) + (slope >> 8) + 2) >> shift, 1u) + S::kSet;
       rising = most > base ? (min(most - base, 1u << 16) << shift << 8) / slope : 0;
     }
   }
@@ -449,8 +450,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   __syncthreads();
   after_sync();
   const uint32_t of_warp = lane < kAll ? sh.sums[lane] : 0, total = __reduce_add_sync(~0u, of_warp);
-  // (Four at least, so that no two CTAs' shares begin at the same step inside a unit.)
-  const uint32_t ctas = min(gridDim.x, max(1u, total / 4));
+  // (Shares of kSet at least, so that no two begin at the same step inside a unit.  One prompt of 540 tokens, 14 / 2
+  // heads of 64: 14.8 us, and with shares of four at least 16.5, of eight 20.7.)
+  const uint32_t ctas = min(gridDim.x, max(1u, total / S::kSet));
   if (total == 0 || blockIdx.x >= ctas) {
     if (threadIdx.x == 0) w.joins[blockIdx.x].parts = 0;
     if (warp == S::kSoft + 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem));

@@ -298,3 +298,19 @@ def test_refusals_and_errors():
     assert c.attend_prompt(0, q[:0], offsets_of([0, 0]))[0].shape == (0, 4, 64)
     c.attend_prompt(0, q, offsets_of([]))
     c.sync()
+
+
+@pytest.mark.parametrize("window", [0, 50])
+def test_tables_that_may_hold_the_longest_sequences(window):
+    """Tables for sequences of 2^31 tokens, whose work is counted in coarser steps: units that are less than one of them are not lost."""
+    lengths = [1 + (37 * i) % 300 for i in range(64)]
+    counts = [min(n, 5) for n in lengths]
+    c = make(lengths, 8, 16, 4096, "bf16")
+    table = torch.full((64, 2 ** 31 // 4096 - 1), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.table.shape[1]] = c.table
+    wide = g.KvCache(c.k, c.v, table, c.length, c.refs)
+    q = query(sum(counts), 8, 16, torch.bfloat16)
+    out, lse = torch.full_like(q, 7.0), torch.full((sum(counts), 8), 7.0, device="cuda")
+    wide.attend_prompt(0, q, offsets_of(counts), window=window, out=out, lse=lse)
+    wide.sync()
+    rm.check(c, 0, q, offsets_of(counts), 0.25, (out, lse), window=window)
