@@ -136,9 +136,11 @@ struct KvQuery {
   // Whether rows of q may be read by twos, and those of out written by fours, of their values.
   bool q_pairs, out_fours;
   // Row i is taken from token skip[i] on (NULL: all of it), and where that is not 0, put together with the result of
-  // those before: pre [row][head][value] and pre_lse [row][head].
+  // those before: pre [row][head][value], and their maximum (in log2, as it is held: see Type) and sum of exp, pre_sum
+  // [row][head].
   const int32_t* skip;
-  const float *pre, *pre_lse;
+  const float* pre;
+  const float2* pre_sum;
 };
 // The attention's kernel for values of a type, head_dim and `group` query heads a kv head: head_dim as it is padded,
 // blocks of eight query heads taken together, and CTAs resident on an SM.
@@ -231,7 +233,8 @@ struct KvRowsCall {
   const int64_t* offsets;
   const int32_t* groups;    // [n + 1]
   const int4* spans;        // [n]: see launch_kv_share
-  float *pre, *pre_lse;     // where results go, in 32 bits, [row][head][value] and [row][head] (NULL: to out and lse)
+  float* pre;               // where results go, in 32 bits, [row][head][value] (NULL: to out and lse)
+  float2* pre_sum;          // and their maxima and sums of exp, [row][head]
   int64_t n_tokens, q_row, q_head, out_row, out_head;
   int32_t n, heads, group, type, window, layer;  // group: query heads a kv head
   FastDiv by_group;

@@ -116,28 +116,33 @@ __device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
-// Weights of a row's own result, whose lse is given, and of the one of the tokens before (q), and the lse of both.
+// A row's own tokens and those before them together: the weights of its own sums (unnormalised, with their maximum t and
+// sum of exp z) and of the result before, and both parts' maximum and sum of exp.  (A part whose logits are all
+// -infinity counts for nothing; where both are, weights are NaN, as attention over such tokens alone gives NaN.)
 struct Both {
-  float own, before, lse;
+  float own, before, t, z;
 };
-__device__ __forceinline__ Both with_before(const KvQuery& a, int32_t i, int32_t head, float lse) {
-  const float his = a.pre_lse[(int64_t)i * a.heads + head], most = fmaxf(lse, his);
-  const float p = exp2_fast((lse - most) * kLog2e), q = exp2_fast((his - most) * kLog2e), by = __fdividef(1.f, p + q);
-  return {p * by, q * by, most + __logf(p + q)};
+__device__ __forceinline__ Both with_before(const KvQuery& a, int32_t i, int32_t head, float t, float z) {
+  const float2 his = a.pre_sum[(int64_t)i * a.heads + head];
+  const float most = fmaxf(t, his.x), ref = most == -INFINITY ? 0.f : most;
+  const float p = exp2_fast(t - ref), q = his.y * exp2_fast(his.x - ref), sum = fmaf(z, p, q), by = __fdividef(1.f, sum);
+  return {p * by, q * by, most, sum};
 }
-// Values d .. d + 3 of a head's result, times f; zero: 0 in their place.  t, z: what the row's sums are relative to,
-// and its sum of exp.
+// Values d .. d + 3 of a head's result, unnormalised; t, z: what the row's sums are relative to, and its sum of exp;
+// empty: it has no tokens of its own.
 template <int KIND>
 __device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_t i, int32_t head, int32_t d, float4 v,
-                                       float f, float t, float z, bool zero) {
+                                       float v_scale, float t, float z, bool empty) {
   if (d >= c.dim) return;  // (dim is a multiple of 8)
-  if (zero) v = make_float4(0.f, 0.f, 0.f, 0.f), f = 0.f;
-  v.x *= f, v.y *= f, v.z *= f, v.w *= f;
   if (a.skip && a.skip[i] > 0) {
-    const Both b = with_before(a, i, head, zero ? -INFINITY : log_sum<KIND>(t, z));
+    const Both b = with_before(a, i, head, t, z);
     const float4 x = *(const float4*)(a.pre + ((int64_t)i * a.heads + head) * c.dim + d);
-    v.x = fmaf(x.x, b.before, v.x * b.own), v.y = fmaf(x.y, b.before, v.y * b.own);
-    v.z = fmaf(x.z, b.before, v.z * b.own), v.w = fmaf(x.w, b.before, v.w * b.own);
+    const float f = v_scale * b.own;
+    v.x = fmaf(x.x, b.before, v.x * f), v.y = fmaf(x.y, b.before, v.y * f);
+    v.z = fmaf(x.z, b.before, v.z * f), v.w = fmaf(x.w, b.before, v.w * f);
+  } else {
+    const float f = empty ? 0.f : __fdividef(v_scale, z);
+    v.x *= f, v.y *= f, v.z *= f, v.w *= f;
   }
   const uint32_t x = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.x, v.y) : pack<P2P_KV_F16>(v.x, v.y);
   const uint32_t y = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.z, v.w) : pack<P2P_KV_F16>(v.z, v.w);
@@ -150,11 +155,13 @@ __device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_
   }
 }
 template <int KIND>
-__device__ __forceinline__ void store_lse(const KvQuery& a, int32_t i, int32_t head, float t, float z, bool zero) {
+__device__ __forceinline__ void store_lse(const KvQuery& a, int32_t i, int32_t head, float t, float z) {
   if (!a.lse) return;
-  float lse = zero ? -INFINITY : log_sum<KIND>(t, z);
-  if (a.skip && a.skip[i] > 0) lse = with_before(a, i, head, lse).lse;
-  a.lse[(int64_t)i * a.heads + head] = lse;
+  if (a.skip && a.skip[i] > 0) {
+    const Both b = with_before(a, i, head, t, z);
+    t = b.t, z = b.z;
+  }
+  a.lse[(int64_t)i * a.heads + head] = z == 0.f ? -INFINITY : log_sum<KIND>(t, z);
 }
 
 // Byte offset in a warp's tile of piece `piece` of row `row`: the pieces of eight rows that ldmatrix reads together lie
@@ -695,8 +702,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
         } else {
           const int32_t q_head = head0 + beside * group + h8;
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
-          store4<KIND>(c, a, u.i, q_head, d, v, __fdividef(v_scale, z), t, z, empty);
-          if (d == 0) store_lse<KIND>(a, u.i, q_head, t, z, empty);
+          store4<KIND>(c, a, u.i, q_head, d, v, v_scale, t, z, empty);
+          if (d == 0) store_lse<KIND>(a, u.i, q_head, t, z);
         }
       }
       if (whole || b + 1 < NB) __syncthreads();  // the sums' room is free again
@@ -811,8 +818,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
               const int beside = at[i] / S::kHeads;
               const int32_t q_head = head0 + beside * group + at[i] % S::kHeads;
               const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
-              store4<KIND>(c, a, u.i, q_head, d[i], v[i], __fdividef(v_scale, z[i]), t[i], z[i], false);
-              if (d[i] == 0) store_lse<KIND>(a, u.i, q_head, t[i], z[i], false);
+              store4<KIND>(c, a, u.i, q_head, d[i], v[i], v_scale, t[i], z[i], false);
+              if (d[i] == 0) store_lse<KIND>(a, u.i, q_head, t[i], z[i]);
             } else {
               *(float4*)(joined + at[i] * DP + d[i]) = v[i];
               if (d[i] == 0) joined[part_heads * DP + at[i]] = t[i], joined[part_heads * (DP + 1) + at[i]] = z[i];

@@ -585,14 +585,14 @@ int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   return P2P_OK;
 }
 
-// Where the parts of attend_shared's work lie: each row's result over its group's tokens, what the groups share, and
-// the tokens of each row that its group works off.
+// Where the parts of attend_shared's work lie: each row's result over its group's tokens, its maximum and sum of exp,
+// what the groups share, and the tokens of each row that its group works off.
 struct SharedWork {
-  size_t lse, spans, skip, bytes;
+  size_t sum, spans, skip, bytes;
   SharedWork(const p2p::KvView& c, int32_t n, int32_t n_heads) {
     const size_t rows = (size_t)n * n_heads;
-    lse = sizeof(float) * rows * c.dim;
-    spans = lse + sizeof(float) * ((rows + 3) / 4 * 4);
+    sum = sizeof(float) * rows * c.dim;
+    spans = sum + sizeof(float2) * ((rows + 1) / 2 * 2);
     skip = spans + sizeof(int4) * n;
     bytes = skip + sizeof(int32_t) * n + 16;
   }
@@ -623,7 +623,8 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   if (int rc = check_rows(h, n, q, n_heads, out, out_row_stride, out_head_stride, lse)) return rc;
   DeviceGuard g(h->device);
   const SharedWork at(h->c, n, n_heads);
-  float *pre = (float*)work, *pre_lse = (float*)((char*)work + at.lse);
+  float* pre = (float*)work;
+  float2* pre_sum = (float2*)((char*)work + at.sum);
   int4* spans = (int4*)((char*)work + at.spans);
   int32_t* skip = (int32_t*)((char*)work + at.skip);
   p2p::KvQuery rest = query_of(layer, n, seq, q, q_row_stride, q_head_stride, type, n_heads, scale, window, out,
@@ -644,14 +645,14 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
     a.groups = groups;
     a.spans = spans;
     a.pre = pre;
-    a.pre_lse = pre_lse;
+    a.pre_sum = pre_sum;
     a.n_tokens = n;
     CK(launch_rows(h->c, h->maps, &a, h->w, h->num_sms, h->stream));
     CK(p2p::launch_kv_join(h->c, a, h->w, h->num_sms, h->stream));
     h->launches += 3;
     rest.skip = skip;
     rest.pre = pre;
-    rest.pre_lse = pre_lse;
+    rest.pre_sum = pre_sum;
   }
   CK(launch_attend(h->c, &rest, h->w, h->num_sms, h->stream));
   h->launches += 1;

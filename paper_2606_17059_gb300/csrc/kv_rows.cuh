@@ -591,8 +591,10 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             part[DP * 128 + r] = top, part[(DP + 1) * 128 + r] = z;
           } else if (valid) {
             f = z > 0.f || z != z ? v_scale / z : 0.f;
-            float* const lse = a.pre ? a.pre_lse : a.lse;
-            if (lse) lse[row * a.heads + head] = z == 0.f ? -INFINITY : log_sum<KIND>(top, z);
+            if (a.pre)
+              a.pre_sum[row * a.heads + head] = make_float2(top, z);
+            else if (a.lse)
+              a.lse[row * a.heads + head] = z == 0.f ? -INFINITY : log_sum<KIND>(top, z);
           }
 #pragma unroll 1
           for (int32_t d = 0; d < dim16 && !(paired && tile == 1); d += 32) {
