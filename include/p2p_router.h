@@ -464,7 +464,8 @@ int p2p_kv_compact(p2p_kv* kv);
  * to the cache's type before its product with v_t (to f16 with P2P_KV_E4M3; of f16, what is 2^-26 of the largest or
  * less has fewer bits, and what is less than 2^-37 of it is lost), and q, with P2P_KV_E4M3, to f16 after scaling by a
  * power of two (what is 2^-28 of a row's largest value or less has fewer bits).  A sequence without tokens gives 0 and
- * -infinity.  Device-side errors: a sequence or a page out of range. */
+ * -infinity, one whose logits are all -infinity NaN and -infinity.  Device-side errors: a sequence or a page out of
+ * range. */
 int p2p_kv_attend(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, const void* q, int64_t q_row_stride,
                   int64_t q_head_stride, int32_t type, int32_t n_heads, float scale, int32_t window, void* out,
                   int64_t out_row_stride, int64_t out_head_stride, float* lse);

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kThreads)
     const int64_t row = u.row + t;
     const int32_t head = u.h * a.group + (int32_t)(at - t * a.group);
     const float v_scale = c.type == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h] : 1.f;
-    const float f = z > 0.f || z != z ? v_scale / z : 0.f;
+    const float f = z == 0.f && a.pre ? 0.f : v_scale / z;  // (as in kv_rows.cuh)
     if (d0 == 0 && a.pre) a.pre_sum[row * a.heads + head] = make_float2(m, z);
     if (d0 == 0 && !a.pre && a.lse)
       a.lse[row * a.heads + head] = z == 0.f ? -INFINITY : (m + up + __log2f(z * exp2f(-up))) * kLn2;

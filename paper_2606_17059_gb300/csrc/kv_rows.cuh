@@ -590,7 +590,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           if (keep) {
             part[DP * 128 + r] = top, part[(DP + 1) * 128 + r] = z;
           } else if (valid) {
-            f = z > 0.f || z != z ? v_scale / z : 0.f;
+            // (A part without a finite logit counts for nothing; a row has a token at least, and is then NaN.)
+            f = z == 0.f && a.pre ? 0.f : v_scale / z;
             if (a.pre)
               a.pre_sum[row * a.heads + head] = make_float2(top, z);
             else if (a.lse)

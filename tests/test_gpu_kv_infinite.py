@@ -8,7 +8,7 @@ pytestmark = pytest.mark.gpu
 
 if torch.cuda.is_available():
     import kv_model as km
-    from test_gpu_kv_attend import query
+    from test_gpu_kv_attend import make, query
     from test_gpu_kv_shared import groups_of, i32, shared_cache
 
 TYPE = {"bf16": torch.bfloat16, "f16": torch.float16}
@@ -79,3 +79,21 @@ def test_rows_without_a_finite_logit(kind, hq, hkv, dim):
         c.sync()
         assert bool(torch.isnan(out[:3]).all()) and bool((lse[:3] == -torch.inf).all())
         assert bool(torch.isfinite(out[3:]).all()) and bool(torch.isfinite(lse[3:]).all())
+
+
+@pytest.mark.parametrize("kind,hq,hkv,dim", SHAPES)
+@pytest.mark.parametrize("cached", [0, 900, 20000])
+def test_prompts_without_a_finite_logit(kind, hq, hkv, dim, cached):
+    """Rows of prompts that see no finite logit, whole or split over the GPU: as from attend."""
+    c = make([cached + 5, cached + 5], hkv, dim, 16, kind)
+    sink(c, 0, range(cached + 3))
+    q = rising(10, hq, dim, kind)
+    out, lse = c.attend_prompt(0, q, torch.tensor([0, 5, 10], device="cuda"))
+    c.sync()
+    assert bool(torch.isnan(out[:3]).all()) and bool((lse[:3] == -torch.inf).all())
+    assert bool(torch.isfinite(out[3:]).all()) and bool(torch.isfinite(lse[3:]).all())
+    for t in range(5):
+        c.length.copy_(i32([cached + 1 + t] * 2))
+        a, la = c.attend(0, q[[t, 5 + t]].contiguous())
+        c.sync()
+        assert torch.equal(torch.isnan(a), torch.isnan(out[[t, 5 + t]])) and torch.equal(torch.isneginf(la), torch.isneginf(lse[[t, 5 + t]]))
