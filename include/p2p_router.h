@@ -505,7 +505,8 @@ int p2p_kv_write_rotated(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* se
  * may be named again), its keys and values written, and attends over the tokens up to itself, the last `window` of
  * them (0: all). Other arguments, results and roundings as p2p_kv_attend, with one lse[t * n_heads + h] a row.  Rows
  * of no sequence are left as they were, as are those of a sequence out of range or with fewer tokens than rows
- * (device-side errors, like offsets out of range). n is at most 2^20, n_tokens * n_heads at most 2^29. */
+ * (device-side errors), and all rows where offsets descend or leave the batch (one too).  n is at most 2^20, n_tokens *
+ * n_heads at most 2^29. */
 int p2p_kv_attend_prompt(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,
                          int64_t n_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t type,
                          int32_t n_heads, float scale, int32_t window, void* out, int64_t out_token_stride,

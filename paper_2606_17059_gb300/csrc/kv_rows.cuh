@@ -245,8 +245,11 @@ struct RowsItem {
   int32_t seq, pos;         // pos: the first token's position; of a group: where the last row's window begins
   int32_t shared, first;    // of a group: tokens first .. shared - 1 are seen
 };
+// broken: set where offsets descend or leave the batch.  (No item is then taken: rows that several items name would be
+// counted beyond what the host allows for.)
 template <class S>
-__device__ __forceinline__ RowsItem rows_item(const KvView& c, const KvRowsCall& a, int32_t i, int32_t* err) {
+__device__ __forceinline__ RowsItem rows_item(const KvView& c, const KvRowsCall& a, int32_t i, int32_t* err,
+                                              bool& broken) {
   RowsItem r = {0, 0, 0, 0, 0, 0, 0};
   if (a.spans) {
     const int4 span = a.spans[i];
@@ -258,6 +261,7 @@ __device__ __forceinline__ RowsItem rows_item(const KvView& c, const KvRowsCall&
     const int64_t o0 = a.offsets[i], o1 = a.offsets[i + 1];
     const int32_t seq = a.seq ? a.seq[i] : i;
     int32_t bad = o0 < 0 || o1 < o0 || o1 > a.n_tokens ? KV_BAD_OFFSETS : 0;
+    broken |= bad != 0;
     if (!bad && o1 > o0) {
       const int32_t len = (uint32_t)seq < (uint32_t)c.n_seqs ? length_of(c, seq) : -2;
       if (len == -2)
@@ -439,17 +443,19 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   const int turn = warp >= S::kSoft + 5 ? warp - (S::kSoft + 5) : warp + 3;
   RowsItem own = {};
   uint32_t own_cost = 0;
+  bool broken = false;
 #pragma unroll 1
   for (int32_t i = turn * per_warp + lane; i < min(a.n, (turn + 1) * per_warp); i += 32) {
-    own = rows_item<S>(c, a, i, blockIdx.x == 0 ? w.err : nullptr);
+    own = rows_item<S>(c, a, i, blockIdx.x == 0 ? w.err : nullptr, broken);
     own_cost = own.tiles ? RowsCost<S>(a, own)(own.tiles) : 0;
     sum_of += c.heads * own_cost;
   }
   sum_of = __reduce_add_sync(~0u, sum_of);
-  if (lane == 0) sh.sums[turn] = sum_of;
+  broken = __any_sync(~0u, broken);
+  if (lane == 0) sh.sums[turn] = broken ? ~0u : sum_of;
   __syncthreads();
   after_sync();
-  const uint32_t of_warp = lane < kAll ? sh.sums[lane] : 0, total = __reduce_add_sync(~0u, of_warp);
+  const uint32_t of_warp = lane < kAll ? sh.sums[lane] : 0, total = __any_sync(~0u, of_warp == ~0u) ? 0 : __reduce_add_sync(~0u, of_warp);
   // (Shares of kSet at least, so that no two begin at the same step inside a unit.  One prompt of 540 tokens, 14 / 2
   // heads of 64: 14.8 us, and with shares of four at least 16.5, of eight 20.7.)
   const uint32_t ctas = min(gridDim.x, max(1u, total / S::kSet));
@@ -1102,7 +1108,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     for (int32_t i0 = from * per_warp; alive && x < x1 && i0 < a.n; i0 += 32) {
       if (i0 > 0 || per_warp > 32) {  // (else they are still there)
         own = {}, own_cost = 0;
-        if (i0 + lane < a.n) own = rows_item<S>(c, a, i0 + lane, nullptr);
+        bool unused = false;
+        if (i0 + lane < a.n) own = rows_item<S>(c, a, i0 + lane, nullptr, unused);
         if (own.tiles) own_cost = RowsCost<S>(a, own)(own.tiles);
       }
 #pragma unroll 1
