@@ -7,6 +7,7 @@
 
 #include <algorithm>
 
+#include "kv_rows_cost.h"
 #include "p2p_router.h"
 
 namespace p2p {
@@ -238,9 +239,7 @@ struct KvRowsCall {
   int64_t n_tokens, q_row, q_head, out_row, out_head;
   int32_t n, heads, group, type, window, layer;  // group: query heads a kv head
   FastDiv by_group;
-  // see RowsCost in kv_rows.cuh: 2^shift steps are counted as one, and a tile's rows are slope / 256 steps of tokens
-  int32_t shift;
-  uint32_t slope;
+  RowsScale count;  // how work is counted
   float scale;
   bool boxes, out32;      // whether queries come by boxes of whole tokens, and rows of out lie on 32-byte boundaries
   int32_t tile_rows;      // rows of a row tile: 128, or as many whole tokens as fit them

@@ -553,12 +553,10 @@ static p2p::KvRowsCall rows_call(const p2p_kv* h, CUtensorMap& q_map, int32_t la
   a.boxes = make_query_map(h, a, n_rows, q_map);
   a.tile_rows = a.boxes ? 128 / a.group * a.group : 128;
   a.q_map = a.boxes ? &q_map : nullptr;
-  // Steps of 128 (64) tokens for tiles of 256 (128) rows are counted in 32 bits: coarser where there may be too many.
-  const int rows = h->c.dim <= 128 ? 256 : 128, step = rows / 2;
-  a.slope = std::max(1u, (uint32_t)(256 * rows / step / a.group));
-  const double tiles = (double)std::min<int64_t>(n, n_rows) * h->c.heads + (double)n_rows * n_heads / (rows / 2);
-  const double most = (double)h->c.max_pages * h->c.page / step + 4;
-  while (tiles * (4 + std::ldexp(most, -a.shift)) > 4e9) ++a.shift;
+  const int64_t tokens = (int64_t)h->c.max_pages * h->c.page;
+  if (window >= tokens) a.window = 0;  // (which is as much as a sequence can have)
+  const bool wide = h->c.dim > 128;    // (as RowsShape has it)
+  a.count = p2p::rows_scale(n, n_rows, n_heads, h->c.heads, wide ? 1 : 2, a.tile_rows, wide ? 6 : 7, tokens);
   a.out32 = (uintptr_t)out % 32 == 0 && out_row % 16 == 0 && out_head % 16 == 0;
   return a;
 }

@@ -63,7 +63,6 @@ struct RowsShape {
   static constexpr int kThreads = (kSoft + 8) * 32;
   static constexpr int kOCol = kTiles * kBt;           // columns of tensor memory: S of the tiles, then O of them
   static_assert(kOCol + kTiles * DP <= 512);
-  static constexpr int kSet = 2;                       // steps that a unit counts for beyond its own
 };
 
 constexpr int kSplitSteps = 4;  // from which on
@@ -289,32 +288,11 @@ __device__ __forceinline__ RowsSpan rows_span(const KvRowsCall& a, const RowsIte
   const int32_t e0 = it.pos + t0 + 1, e1 = it.pos + t1 + 1;
   return {window_begin(a, e0), e1, window_begin(a, e1), e0};
 }
-// What the first j tiles of an item count for, in units of 2^shift steps: each kSet for itself and about its steps.
-// Any rising function would do, as long as all CTAs take the same and a tile counts for more than kSet: a share that
-// ends kSet after a unit's begin has none of its steps.
 template <class S>
-struct RowsCost {
-  // the first tile's; how much each has more (in 512ths of a step) until they have most
-  uint32_t base, most, slope, rising;
-  int32_t shift;
-  __device__ __forceinline__ RowsCost(const KvRowsCall& a, const RowsItem& it) {
-    most = 0, rising = ~0u, slope = 0, shift = a.shift;
-    if (a.spans) {
-      base = max((((it.shared - 1) >> S::kBtLog) - (it.first >> S::kBtLog) + 1) >> shift, 1) + S::kSet;
-      return;
-    }
-    slope = a.slope;
-    base = max(((it.pos >> S::kBtLog) + 1) >> shift, 1) + S::kSet;
-    if (a.window) {
-      most = max(((a.window >> S::kBtLog) + (slope >> 8) + 2) >> shift, 1u) + S::kSet;
-      rising = most > base ? (min(most - base, 1u << 16) << shift << 8) / slope : 0;
-    }
-  }
-  __device__ __forceinline__ uint32_t operator()(uint32_t j) const {
-    const uint32_t r = min(j, rising);
-    return r * base + (uint32_t)((uint64_t)r * (r + 1) * slope >> (9 + shift)) + (j - r) * most;
-  }
-};
+__device__ __forceinline__ RowsCost rows_cost(const KvRowsCall& a, const RowsItem& it) {
+  return a.spans ? RowsCost::of_prefix(it.first, it.shared, a.count, S::kBtLog)
+                 : RowsCost::of_prompt(it.pos, a.window, a.count, S::kBtLog);
+}
 // Values d .. d + 15 of a row's result: o, times f.  (Whole sectors where that is to be had, as the lanes' rows are
 // apart.)
 __device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_t row, int32_t head, int32_t d,
@@ -447,7 +425,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 #pragma unroll 1
   for (int32_t i = turn * per_warp + lane; i < min(a.n, (turn + 1) * per_warp); i += 32) {
     own = rows_item<S>(c, a, i, blockIdx.x == 0 ? w.err : nullptr, broken);
-    own_cost = own.tiles ? RowsCost<S>(a, own)(own.tiles) : 0;
+    own_cost = own.tiles ? rows_cost<S>(a, own).of(own.tiles) : 0;
     sum_of += c.heads * own_cost;
   }
   sum_of = __reduce_add_sync(~0u, sum_of);
@@ -456,9 +434,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   __syncthreads();
   after_sync();
   const uint32_t of_warp = lane < kAll ? sh.sums[lane] : 0, total = __any_sync(~0u, of_warp == ~0u) ? 0 : __reduce_add_sync(~0u, of_warp);
-  // (Shares of kSet at least, so that no two begin at the same step inside a unit.  One prompt of 540 tokens, 14 / 2
+  // (Shares of kRowsSet at least, so that no two begin at the same step inside a unit.  One prompt of 540 tokens, 14 / 2
   // heads of 64: 14.8 us, and with shares of four at least 16.5, of eight 20.7.)
-  const uint32_t ctas = min(gridDim.x, max(1u, total / S::kSet));
+  const uint32_t ctas = min(gridDim.x, max(1u, total / kRowsSet));
   if (total == 0 || blockIdx.x >= ctas) {
     if (threadIdx.x == 0) w.joins[blockIdx.x].parts = 0;
     if (warp == S::kSoft + 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem));
@@ -1110,7 +1088,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         own = {}, own_cost = 0;
         bool unused = false;
         if (i0 + lane < a.n) own = rows_item<S>(c, a, i0 + lane, nullptr, unused);
-        if (own.tiles) own_cost = RowsCost<S>(a, own)(own.tiles);
+        if (own.tiles) own_cost = rows_cost<S>(a, own).of(own.tiles);
       }
 #pragma unroll 1
       for (uint32_t some = __ballot_sync(~0u, own.tiles > 0); some && alive && x < x1; some &= some - 1) {
@@ -1125,7 +1103,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         it.members = __shfl_sync(~0u, own.members, l), it.tiles = __shfl_sync(~0u, own.tiles, l);
         it.seq = __shfl_sync(~0u, own.seq, l), it.pos = __shfl_sync(~0u, own.pos, l);
         it.shared = __shfl_sync(~0u, own.shared, l), it.first = __shfl_sync(~0u, own.first, l);
-        const RowsCost<S> costs(a, it);
+        const RowsCost costs = rows_cost<S>(a, it);
         int32_t h = 0, j = 0;
         uint32_t cost = 0;
         if (!found) {  // the head and tile where the share begins
@@ -1137,7 +1115,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 #pragma unroll 1
           while (past - j > 1) {
             const int32_t mid = j + ((past - j) >> 1);
-            const uint32_t y = costs(mid);
+            const uint32_t y = costs.of(mid);
             if (y <= in)
               j = mid, cost = y;
             else
@@ -1149,7 +1127,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         int32_t t = a.by_group.div(j * unit), g0 = j * unit - t * a.group;
 #pragma unroll 1
         while (alive && x < x1) {
-          const uint32_t cost1 = costs(j + 1), width = cost1 - cost;
+          const uint32_t cost1 = costs.of(j + 1), width = cost1 - cost;
           const int32_t rows = min(unit, it.members * a.group - j * unit);
           // The next tile's first row, and the second half's.
           int32_t t_next = t + tile_t, g_next = g0 + tile_g, t_half = t + half_t, g_half = g0 + half_g;
@@ -1158,10 +1136,10 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           const int32_t t_last = min(g_next ? t_next : t_next - 1, it.members - 1);
           const RowsSpan span = rows_span(a, it, t, t_last);
           const int32_t j0 = span.begin >> S::kBtLog, n = ((span.end - 1) >> S::kBtLog) + 1 - j0;
-          // A share that begins at x + kSet + 1 .. x + inside - 1 begins within the unit, at this step of it:
-          const uint32_t inside = min(width, (uint32_t)((n - 1) >> a.shift) + 1 + S::kSet);
+          // A share that begins at x + kRowsSet + 1 .. x + inside - 1 begins within the unit, at this step of it:
+          const uint32_t inside = min(width, (uint32_t)((n - 1) >> a.count.shift) + 1 + kRowsSet);
           const auto step = [&](uint32_t y) {
-            return y <= x + S::kSet ? 0 : y - x >= inside ? n : (int32_t)((y - x - S::kSet) << a.shift);
+            return y <= x + kRowsSet ? 0 : y - x >= inside ? n : (int32_t)((y - x - kRowsSet) << a.count.shift);
           };
           const int32_t s0 = step(x0), s1 = step(x1);
           if (s1 > s0) {
@@ -1195,7 +1173,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (s1 - s0 < n) {
               // The first shares that begin within the unit, and after it, by a lane each: the first k with total * k
               // >= y * ctas.
-              const uint32_t y = x + (lane & 1 ? inside : S::kSet + 1);
+              const uint32_t y = x + (lane & 1 ? inside : kRowsSet + 1);
               uint32_t k = (uint32_t)__fdividef((float)y * (float)ctas, (float)total);
               k = k > 1 ? k - 1 : 0;
               while ((uint64_t)k * total < (uint64_t)y * ctas) ++k;
