@@ -391,9 +391,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
   // (Nothing so far touches memory: it runs beside the end of the kernel before.)
   if (threadIdx.x == 0) {
     for (int i = 0; i < 8; ++i) bar_init(sh.full[i], KIND != P2P_KV_E4M3 && maps.rows ? 4 : 128),
-        bar_init(sh.empty[i], 1), bar_init(sh.checked[i], 2);
-    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], !direct ? 4 : a.boxes ? 1 : 64),
-        bar_init(sh.q_raw[i], a.boxes ? 1 : 64), bar_init(sh.q_empty[i], 1), bar_init(sh.s_full[i], 1),
+        bar_init(sh.empty[i], 3), bar_init(sh.checked[i], 2);
+    for (int i = 0; i < 2; ++i) bar_init(sh.q_full[i], !direct ? 4 : a.boxes ? 2 : 64),
+        bar_init(sh.q_raw[i], a.boxes ? 2 : 64), bar_init(sh.q_empty[i], 1), bar_init(sh.s_full[i], 1),
             bar_init(sh.p_full[i], 4), bar_init(sh.o_full[i], 1);
     for (int i = 0; i < kRing; ++i) bar_init(sh.unit_full[i], 1), bar_init(sh.unit_empty[i], S::kSoft + 7),
         sh.poison[i] = 0;
@@ -1220,7 +1220,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           const uint64_t& there = direct ? sh.q_full[i] : sh.q_raw[i];
           const int first = u.split ? 0 : i * a.tile_rows;
           char* const to = q_room + i * S::kQTile;
+          // (Where one helper brings all, the other arrives as well, so that neither misses a phase of q_empty.)
           if (a.boxes) {  // whole tokens
+            if (mine == 32) bar_arrive(there);
             if (mine == 0) {
               bar_expect(there, a.tile_rows * 128 * chunks);
               for (int x = 0; x < chunks; ++x)
@@ -1299,7 +1301,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             async_fence();
           }
           __syncwarp();
-          if (lane == 0) bar_arrive(sh.checked[stage]);
+          // (A stage is free when the products and both helpers are done with it: one that fell a turn behind would take
+          // phases for one another.)
+          if (lane == 0) bar_arrive(sh.checked[stage]), bar_arrive(sh.empty[stage]);
           if (++stage == kStages) stage = 0, phase ^= 1;
         }
         __syncwarp();
