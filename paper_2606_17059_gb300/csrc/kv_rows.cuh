@@ -460,6 +460,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     char* const q_tile = q_room + tile * S::kQTile;
     uint32_t s_phase = 0, o_phase = 0;
     float mul = 0.f;  // logit (in log2) of a sum of products
+    // (0 times a masked -infinity would be NaN.  The least number instead makes of the largest sum 2^-21; NaN stays NaN.)
+    const auto not_zero = [](float x) { return x == 0.f ? 0x1p-149f : x; };
     // Where row x of the unit's tile is.
     const auto row_of_q = [&](const RowsUnit& u, int x, int64_t& row, int32_t& head) {
       const uint32_t y = u.g0 + (u.split ? 0 : tile * a.tile_rows) + x, t = a.by_group.div(y);
@@ -499,7 +501,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             : 0;
         down = __uint_as_float((127 - e) << 23), unit *= __uint_as_float((127 + e) << 23);
       }
-      mul = fmaxf(unit, 0x1p-120f);  // (0 times a masked -infinity would be NaN)
+      mul = not_zero(unit);
       if (narrow || flip) {
 #pragma unroll 4
         for (int k = 0; k < dim16 / 8; ++k) {
@@ -639,7 +641,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           }
         }
         if (direct)
-          mul = fmaxf(a.scale * kLog2e, 0x1p-120f);
+          mul = not_zero(a.scale * kLog2e);
         else if (to > from && !change_queries(u))
           return;
         const float unit_mul = mul;
