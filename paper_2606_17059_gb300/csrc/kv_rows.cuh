@@ -322,6 +322,11 @@ __device__ __forceinline__ void put(const KvView& c, const KvRowsCall& a, int64_
       if (k < 8 || !half) out[k] = (uint16_t)(b[k / 2] >> (k & 1) * 16);
   }
 }
+// Whether every row sees all of step j's tokens.  (Its end may be 2^31, which 32 bits do not hold.)
+template <int BT>
+__device__ __forceinline__ bool seen_by_all(int32_t j, int32_t all_begin, int32_t all_end) {
+  return j * BT >= all_begin && all_end - j * BT >= BT;
+}
 // Infinities and NaN that were taken out of the values of `every` step from j0 to j1 (of those that not all rows see):
 // added to the sums of the rows that see them, tokens begin .. end - 1.  By a warp, whose 32 rows of sums are at o_at.
 // Rarely needed, so it is small, not fast.
@@ -332,41 +337,44 @@ __device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall&
   const int lane = threadIdx.x & 31;
   constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8;  // of a piece
 #pragma unroll 1
-  for (int32_t p = max(u.begin, j0 * BT); p < min(u.end, j1 * BT); ++p) {
-    const int32_t j = p / BT;
-    if (!(j * BT < u.all_begin || (j + 1) * BT > u.all_end) || (j - j0) % every) continue;
-    const uint32_t e = c.by_page.div(p);
-    const int32_t page = row_of(c, u.seq)[e];
-    if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
-    const char* const at = c.v + a.layer * c.layer_stride + page * c.page_stride +
-        (p - (int32_t)e * c.page) * c.token_stride + u.h * c.head_stride;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (lane < c.row16) v = *(const uint4*)(at + lane * 16);
-    const uint32_t b[4] = {v.x, v.y, v.z, v.w};
-    bool bad = false;
+  for (int32_t j = j0; j < j1; j += every) {
+    if (seen_by_all<BT>(j, u.all_begin, u.all_end)) continue;
+    const int32_t last = j * BT + min(BT, u.end - j * BT);
+#pragma unroll 1
+    for (int32_t p = max(u.begin, j * BT); p < last; ++p) {
+      const uint32_t e = c.by_page.div(p);
+      const int32_t page = row_of(c, u.seq)[e];
+      if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
+      const char* const at = c.v + a.layer * c.layer_stride + page * c.page_stride +
+          (p - (int32_t)e * c.page) * c.token_stride + u.h * c.head_stride;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (lane < c.row16) v = *(const uint4*)(at + lane * 16);
+      const uint32_t b[4] = {v.x, v.y, v.z, v.w};
+      bool bad = false;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      bad |= KIND == P2P_KV_E4M3 ? (((b[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0
-                                 : (((b[k] & (KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u)) +
-                                     (KIND == P2P_KV_BF16 ? 0x00800080u : 0x04000400u)) & 0x80008000u) != 0;
+      for (int k = 0; k < 4; ++k)
+        bad |= KIND == P2P_KV_E4M3 ? (((b[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0
+                                   : (((b[k] & (KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u)) +
+                                       (KIND == P2P_KV_BF16 ? 0x00800080u : 0x04000400u)) & 0x80008000u) != 0;
 #pragma unroll 1
-    for (uint32_t pieces = __ballot_sync(~0u, bad); pieces; pieces &= pieces - 1) {
-      const int piece = __ffs(pieces) - 1;
+      for (uint32_t pieces = __ballot_sync(~0u, bad); pieces; pieces &= pieces - 1) {
+        const int piece = __ffs(pieces) - 1;
 #pragma unroll 1
-      for (int k = 0; k < kValues; ++k) {
-        const char* const one = at + piece * 16 + k * (16 / kValues);
-        const float f = KIND == P2P_KV_E4M3   ? __half2float(__nv_cvt_fp8_to_halfraw(*(const uint8_t*)one, __NV_E4M3))
-                        : KIND == P2P_KV_BF16 ? __bfloat162float(*(const __nv_bfloat16*)one)
-                                              : __half2float(*(const __half*)one);
-        if (fabsf(f) < INFINITY) continue;
-        uint32_t o;
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(o) : "r"(o_at + piece * kValues + k)
-            : "memory");
-        tmem_loaded();
-        if (p >= begin && p < end) o = __float_as_uint(__uint_as_float(o) + f);
-        asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(o_at + piece * kValues + k), "r"(o)
-            : "memory");
-        tmem_stored();
+        for (int k = 0; k < kValues; ++k) {
+          const char* const one = at + piece * 16 + k * (16 / kValues);
+          const float f = KIND == P2P_KV_E4M3   ? __half2float(__nv_cvt_fp8_to_halfraw(*(const uint8_t*)one, __NV_E4M3))
+                          : KIND == P2P_KV_BF16 ? __bfloat162float(*(const __nv_bfloat16*)one)
+                                                : __half2float(*(const __half*)one);
+          if (fabsf(f) < INFINITY) continue;
+          uint32_t o;
+          asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(o) : "r"(o_at + piece * kValues + k)
+              : "memory");
+          tmem_loaded();
+          if (p >= begin && p < end) o = __float_as_uint(__uint_as_float(o) + f);
+          asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(o_at + piece * kValues + k), "r"(o)
+              : "memory");
+          tmem_stored();
+        }
       }
     }
   }
@@ -741,7 +749,10 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         // A lane has a box of tokens of each step (a token, without maps): its first, and the page that it lies in, -1:
         // it is not needed.
         const int32_t size = maps.rows ? maps.rows : 1, boxes = kOwn / size;
-        const auto token_of = [&](int32_t step) { return (j0 + step) * kBt + own0 + lane * size; };
+        // (of a step past the last one: any number)
+        const auto token_of = [&](int32_t step) {
+          return (int32_t)((uint32_t)(j0 + step) * kBt + own0 + lane * size);
+        };
         const auto find = [&](int32_t step) {
           const int32_t t = token_of(step);
           if (lane >= boxes || step >= n || t >= end || t + size <= begin) return -1;
@@ -947,7 +958,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       // The values of step j, at the current stage.
       const auto values_there = [&](int32_t j) {
         if (!bar_wait(sh.full[stage], phase, sh)) return false;
-        if ((j * kBt < all_begin || (j + 1) * kBt > all_end) && !bar_wait(sh.checked[stage], phase, sh)) return false;
+        if (!seen_by_all<kBt>(j, all_begin, all_end) && !bar_wait(sh.checked[stage], phase, sh)) return false;
         async_fence();
         return true;
       };
@@ -1257,7 +1268,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           const RowsStage it = rows_stage(q, n, u.split);
           const int32_t j = u.j0 + it.step;
           if (!bar_wait(sh.full[stage], phase, sh)) return;
-          if (it.values && (j * kBt < u.all_begin || (j + 1) * kBt > u.all_end)) {
+          if (it.values && !seen_by_all<kBt>(j, u.all_begin, u.all_end)) {
             // An exponent of all ones carries into the sign's place.
             constexpr uint32_t kExponent = KIND == P2P_KV_BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = KIND == P2P_KV_BF16
                 ? 0x00800080u : 0x04000400u;
