@@ -21,7 +21,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["route_kernel.cu", "group_kernel.cu", "delta_kernel.cu", "delta_bulk.cu", "delta_static.cu", "update_kernel.cu",
            "lru_kernel.cu", "router.cu", "snapshot.cpp", "kv_pages.cu", "kv_rotate.cu", "kv_shared.cu", "kv_join.cu",
            "kv_cache.cpp",
-           *(f"kv_attend_{t}{w}.cu" for t in ("bf16", "f16", "e4m3") for w in ("", "_side")),
+           *(f"kv_attend_{t}{w}.cu" for t in ("bf16", "f16", "e4m3") for w in ("", "_side", "_after", "_side_after")),
            *(f"kv_rows_{t}.cu" for t in ("bf16", "f16", "e4m3"))]
 
 

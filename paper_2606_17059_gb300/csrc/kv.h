@@ -201,16 +201,28 @@ inline size_t kv_attend_parts(const KvView& c, int num_sms) {
 // With q = NULL they launch nothing, but make the cache's kernels ready for launches (at creation).
 cudaError_t launch_kv_attend_bf16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
                                   cudaStream_t st);
+cudaError_t launch_kv_attend_bf16_after(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                        cudaStream_t st);
 cudaError_t launch_kv_attend_bf16_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
                                        cudaStream_t st);
+cudaError_t launch_kv_attend_bf16_side_after(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                             cudaStream_t st);
 cudaError_t launch_kv_attend_f16(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
                                  cudaStream_t st);
+cudaError_t launch_kv_attend_f16_after(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                       cudaStream_t st);
 cudaError_t launch_kv_attend_f16_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
                                       cudaStream_t st);
+cudaError_t launch_kv_attend_f16_side_after(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                            cudaStream_t st);
 cudaError_t launch_kv_attend_e4m3(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
                                   cudaStream_t st);
+cudaError_t launch_kv_attend_e4m3_after(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                        cudaStream_t st);
 cudaError_t launch_kv_attend_e4m3_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
                                        cudaStream_t st);
+cudaError_t launch_kv_attend_e4m3_side_after(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
+                                             cudaStream_t st);
 
 
 // What the rows of each group share, into spans[n_groups] (x: leading entries that are the same; y, z: the first and

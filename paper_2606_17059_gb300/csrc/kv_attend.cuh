@@ -129,39 +129,42 @@ __device__ __forceinline__ Both with_before(const KvQuery& a, int32_t i, int32_t
   return {p * by, q * by, most, sum};
 }
 // Values d .. d + 3 of a head's result, unnormalised; t, z: what the row's sums are relative to, and its sum of exp;
-// empty: it has no tokens of its own.
-template <int KIND>
+// empty: it has no tokens of its own.  (AFTER: see attend_kernel.)
+template <int KIND, bool AFTER>
 __device__ __forceinline__ void store4(const KvView& c, const KvQuery& a, int32_t i, int32_t head, int32_t d, float4 v,
                                        float v_scale, float t, float z, bool empty) {
   if (d >= c.dim) return;  // (dim is a multiple of 8)
-  if (a.skip && a.skip[i] > 0) {
-    const Both b = with_before(a, i, head, t, z);
-    const float4 x = *(const float4*)(a.pre + ((int64_t)i * a.heads + head) * c.dim + d);
-    const float f = v_scale * b.own;
-    v.x = fmaf(x.x, b.before, v.x * f), v.y = fmaf(x.y, b.before, v.y * f);
-    v.z = fmaf(x.z, b.before, v.z * f), v.w = fmaf(x.w, b.before, v.w * f);
-  } else {
-    const float f = empty ? 0.f : __fdividef(v_scale, z);
-    v.x *= f, v.y *= f, v.z *= f, v.w *= f;
+  float f = __fdividef(v_scale, z);
+  if (empty) v = make_float4(0.f, 0.f, 0.f, 0.f), f = 0.f;
+  if constexpr (AFTER) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.skip[i] > 0) {
+      const Both b = with_before(a, i, head, t, z);
+      f = v_scale * b.own;
+      x = *(const float4*)(a.pre + ((int64_t)i * a.heads + head) * c.dim + d);
+      x.x *= b.before, x.y *= b.before, x.z *= b.before, x.w *= b.before;
+    }
+    v.x = fmaf(v.x, f, x.x), v.y = fmaf(v.y, f, x.y), v.z = fmaf(v.z, f, x.z), v.w = fmaf(v.w, f, x.w);
+    f = 1.f;
   }
-  const uint32_t x = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.x, v.y) : pack<P2P_KV_F16>(v.x, v.y);
-  const uint32_t y = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.z, v.w) : pack<P2P_KV_F16>(v.z, v.w);
+  const uint32_t lo = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.x * f, v.y * f) : pack<P2P_KV_F16>(v.x * f, v.y * f);
+  const uint32_t hi = a.type == P2P_KV_BF16 ? pack<P2P_KV_BF16>(v.z * f, v.w * f) : pack<P2P_KV_F16>(v.z * f, v.w * f);
   uint16_t* to = (uint16_t*)a.out + i * a.out_row + head * a.out_head + d;
   if (a.out_fours) {
-    *(uint2*)to = make_uint2(x, y);
+    *(uint2*)to = make_uint2(lo, hi);
   } else {
-    to[0] = (uint16_t)x, to[1] = (uint16_t)(x >> 16);
-    to[2] = (uint16_t)y, to[3] = (uint16_t)(y >> 16);
+    to[0] = (uint16_t)lo, to[1] = (uint16_t)(lo >> 16);
+    to[2] = (uint16_t)hi, to[3] = (uint16_t)(hi >> 16);
   }
 }
-template <int KIND>
-__device__ __forceinline__ void store_lse(const KvQuery& a, int32_t i, int32_t head, float t, float z) {
+template <int KIND, bool AFTER>
+__device__ __forceinline__ void store_lse(const KvQuery& a, int32_t i, int32_t head, float t, float z, bool empty) {
   if (!a.lse) return;
-  if (a.skip && a.skip[i] > 0) {
+  if (AFTER && a.skip[i] > 0) {
     const Both b = with_before(a, i, head, t, z);
-    t = b.t, z = b.z;
+    t = b.t, z = b.z, empty = false;
   }
-  a.lse[(int64_t)i * a.heads + head] = z == 0.f ? -INFINITY : log_sum<KIND>(t, z);
+  a.lse[(int64_t)i * a.heads + head] = empty ? -INFINITY : log_sum<KIND>(t, z);
 }
 
 // Byte offset in a warp's tile of piece `piece` of row `row`: the pieces of eight rows that ldmatrix reads together lie
@@ -180,7 +183,7 @@ struct Row {
     return end > begin ? ((end - from - 1) >> tile_log) + 1 : 1;
   }
 };
-template <bool WHOLE>
+template <bool WHOLE, bool AFTER>
 __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t i, int32_t* err) {
   const bool there = i < a.n;
   const int32_t seq = there && a.seq ? a.seq[i] : there ? i : 0;
@@ -190,7 +193,7 @@ __device__ __forceinline__ Row row_at(const KvView& c, const KvQuery& a, int32_t
   if (err && !(known && fits)) atomicOr(err, known ? KV_BAD_COUNT : KV_BAD_SEQ);
   Row r = {known ? seq : 0, 0, 0, fits ? len : 0};
   r.begin = a.window && r.end > a.window ? r.end - a.window : 0;
-  if (a.skip && there) r.begin = min(max(r.begin, a.skip[i]), r.end);
+  if (AFTER && there) r.begin = min(max(r.begin, a.skip[i]), r.end);
   r.from = WHOLE ? r.begin / 16 * 16 : r.begin;
   return r;
 }
@@ -210,7 +213,7 @@ struct Cursor {
   int32_t i, h, block, t, nt;  // (h: the first of the unit's kv heads)
   int64_t left;  // units of the range from here on; none: at its end
   // k tiles on, none past the unit row's end.
-  template <bool WHOLE>
+  template <bool WHOLE, bool AFTER>
   __device__ __forceinline__ void advance(int32_t k, const KvView& c, const KvQuery& a, int32_t blocks, int32_t side,
                                           int32_t tile_log) {
     t += k;
@@ -226,13 +229,16 @@ struct Cursor {
     ++i;
     row = next;
     nt = row.tiles(tile_log);
-    next = row_at<WHOLE>(c, a, i + 1, nullptr);
+    next = row_at<WHOLE, AFTER>(c, a, i + 1, nullptr);
   }
 };
 
 // SIDE: the warps of a CTA take 1 << c.side neighbouring kv heads where that pays (see kSideUnits), else one.  WHOLE:
-// pages are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly apart.
-template <int KIND, int DP, int NB, bool SIDE, bool WHOLE>
+// pages are whole sixteens of tokens, and tiles are counted from one: 16 tokens lie in one page, evenly apart.  AFTER:
+// rows begin with their token a.skip, and what comes before is put together with the rest (kernels of their own, as the
+// one-token attention of rows that share nothing takes up to 7% longer where it carries that: 600 sequences of 1 to 200
+// tokens, 64 / 2 heads of 64 in 16 bits, 37.1 us and 34.7).
+template <int KIND, int DP, int NB, bool SIDE, bool WHOLE, bool AFTER>
 __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
     attend_kernel(KvView c, KvQuery a, KvAttendScratch w) {
   using S = Shape<KIND, DP, NB>;
@@ -251,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
     Row r[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      r[k] = row_at<WHOLE>(c, a, i0 + k < r0 + each ? i0 + k : a.n, blockIdx.x == 0 ? w.err : nullptr);
+      r[k] = row_at<WHOLE, AFTER>(c, a, i0 + k < r0 + each ? i0 + k : a.n, blockIdx.x == 0 ? w.err : nullptr);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (i0 + k < r0 + each && i0 + k < a.n) {
@@ -308,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
   if (at >= before && at < before + mine[0]) {
     int32_t i = r0;
     for (;; ++i) {
-      const int32_t t = row_at<WHOLE>(c, a, i, nullptr).tiles(tile_log) + kOver;
+      const int32_t t = row_at<WHOLE, AFTER>(c, a, i, nullptr).tiles(tile_log) + kOver;
       if (at < before + t) break;
       before += t;
     }
@@ -318,8 +324,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
   __syncthreads();
   Cursor here;  // what is computed
   here.i = sh.row;
-  here.row = row_at<WHOLE>(c, a, here.i, nullptr);
-  here.next = row_at<WHOLE>(c, a, here.i + 1, nullptr);
+  here.row = row_at<WHOLE, AFTER>(c, a, here.i, nullptr);
+  here.next = row_at<WHOLE, AFTER>(c, a, here.i + 1, nullptr);
   here.nt = here.row.tiles(tile_log);
   {
     const int64_t in = x0 - sh.before * per_row;
@@ -381,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
           copy16(d + S::kArray, from + across, in);
         }
       }
-      ahead.advance<WHOLE>(1, c, a, blocks, side, tile_log);
+      ahead.advance<WHOLE, AFTER>(1, c, a, blocks, side, tile_log);
     }
     commit();
   };
@@ -401,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
         k.at = layer_at + ahead.h * c.head_stride + (int64_t)((uint32_t)t - e * (uint32_t)c.page) * c.token_stride;
         if (k.page < 0) k.page = INT32_MAX;
       }
-      ahead.advance<WHOLE>(1, c, a, blocks, side, tile_log);
+      ahead.advance<WHOLE, AFTER>(1, c, a, blocks, side, tile_log);
     }
     return k;
   };
@@ -643,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
     }
     // (the last tile's room: it is not filled before the next step)
     float* const sums = (float*)(room + warp * S::kRoom + (slot ? slot - 1 : S::kStages - 1) * S::kStage);
-    here.advance<WHOLE>(count, c, a, blocks, side, tile_log);
+    here.advance<WHOLE, AFTER>(count, c, a, blocks, side, tile_log);
     if (here.left > 0) load_queries(here);  // (on their way while this unit row's parts are joined)
 
     __syncwarp();  // every lane is done with the last tile
@@ -702,8 +708,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
         } else {
           const int32_t q_head = head0 + beside * group + h8;
           const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
-          store4<KIND>(c, a, u.i, q_head, d, v, v_scale, t, z, empty);
-          if (d == 0) store_lse<KIND>(a, u.i, q_head, t, z);
+          store4<KIND, AFTER>(c, a, u.i, q_head, d, v, v_scale, t, z, empty);
+          if (d == 0) store_lse<KIND, AFTER>(a, u.i, q_head, t, z, empty);
         }
       }
       if (whole || b + 1 < NB) __syncthreads();  // the sums' room is free again
@@ -818,8 +824,8 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
               const int beside = at[i] / S::kHeads;
               const int32_t q_head = head0 + beside * group + at[i] % S::kHeads;
               const float v_scale = KIND == P2P_KV_E4M3 ? c.v_scale[a.layer * c.heads + u.h + beside] : 1.f;
-              store4<KIND>(c, a, u.i, q_head, d[i], v[i], v_scale, t[i], z[i], false);
-              if (d[i] == 0) store_lse<KIND>(a, u.i, q_head, t[i], z[i]);
+              store4<KIND, AFTER>(c, a, u.i, q_head, d[i], v[i], v_scale, t[i], z[i], false);
+              if (d[i] == 0) store_lse<KIND, AFTER>(a, u.i, q_head, t[i], z[i], false);
             } else {
               *(float4*)(joined + at[i] * DP + d[i]) = v[i];
               if (d[i] == 0) joined[part_heads * DP + at[i]] = t[i], joined[part_heads * (DP + 1) + at[i]] = z[i];
@@ -842,10 +848,10 @@ __global__ void __launch_bounds__(kThreads, Shape<KIND, DP, NB>::kCtas)
 }
 
 // With q = NULL the kernel is only made ready for launches.
-template <int KIND, int DP, int NB, bool SIDE, bool WHOLE>
+template <int KIND, int DP, int NB, bool SIDE, bool WHOLE, bool AFTER>
 cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   using S = Shape<KIND, DP, NB>;
-  const auto kernel = attend_kernel<KIND, DP, NB, SIDE, WHOLE>;
+  const auto kernel = attend_kernel<KIND, DP, NB, SIDE, WHOLE, AFTER>;
   if (!q) return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
   // As many CTAs as are resident together (by shared memory: 227 KB an SM, of which each CTA takes 1 KB for the
   // system).
@@ -855,36 +861,36 @@ cudaError_t launch(const KvView& c, const KvQuery* q, const KvAttendScratch& w, 
 
 // (Pages of 16 tokens taken token by token, as others are: 64 ragged 10.7 us, not 9.7, 256 sequences in 8 bits 109,
 // not 104.)
-template <int KIND, int DP, int NB, bool SIDE>
+template <int KIND, int DP, int NB, bool SIDE, bool AFTER>
 cudaError_t launch_pages(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
-  return c.page % 16 == 0 ? launch<KIND, DP, NB, SIDE, true>(c, q, w, num_sms, st)
-                          : launch<KIND, DP, NB, SIDE, false>(c, q, w, num_sms, st);
+  return c.page % 16 == 0 ? launch<KIND, DP, NB, SIDE, true, AFTER>(c, q, w, num_sms, st)
+                          : launch<KIND, DP, NB, SIDE, false, AFTER>(c, q, w, num_sms, st);
 }
 
 // Blocks of 8, 16 or 32 query heads: the fewest that hold a kv head's, as each block reads the keys and values again
 // (on the 32 long sequences 40 heads on 8 take 282 us with blocks of 16 and 523 with 8; 128 heads of 256 values on 8
 // 551 and 1,061; 256 heads on 8 301 with blocks of 32 and 539 with 16).  Blocks of 32 beyond 128 values, or beside
 // 8-bit values, do not fit the registers (256 heads on 8 over the 8-bit case 286 us, and 234 with blocks of 16).
-template <int KIND, int DP, bool SIDE>
+template <int KIND, int DP, bool SIDE, bool AFTER>
 cudaError_t launch_heads(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   const int blocks = q ? attend_blocks(KIND, DP, q->heads / c.heads) : 0;
   cudaError_t e = cudaSuccess;
-  if (!q || blocks == 1) e = launch_pages<KIND, DP, 1, SIDE>(c, q, w, num_sms, st);
-  if (e == cudaSuccess && (!q || blocks == 2)) e = launch_pages<KIND, DP, 2, SIDE>(c, q, w, num_sms, st);
+  if (!q || blocks == 1) e = launch_pages<KIND, DP, 1, SIDE, AFTER>(c, q, w, num_sms, st);
+  if (e == cudaSuccess && (!q || blocks == 2)) e = launch_pages<KIND, DP, 2, SIDE, AFTER>(c, q, w, num_sms, st);
   if constexpr (attend_blocks(KIND, DP, 32) == 4)
-    if (e == cudaSuccess && (!q || blocks == 4)) e = launch_pages<KIND, DP, 4, SIDE>(c, q, w, num_sms, st);
+    if (e == cudaSuccess && (!q || blocks == 4)) e = launch_pages<KIND, DP, 4, SIDE, AFTER>(c, q, w, num_sms, st);
   return e;
 }
 
-template <int KIND, bool SIDE>
+template <int KIND, bool SIDE, bool AFTER>
 cudaError_t launch_dim(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms, cudaStream_t st) {
   switch (attend_dim(KIND, c.dim)) {
-    case 64: return launch_heads<KIND, 64, SIDE>(c, q, w, num_sms, st);
-    case 80: return launch_heads<KIND, attend_dim(KIND, 80), SIDE>(c, q, w, num_sms, st);
-    case 96: return launch_heads<KIND, 96, SIDE>(c, q, w, num_sms, st);
-    case 128: return launch_heads<KIND, 128, SIDE>(c, q, w, num_sms, st);
-    case 192: return launch_heads<KIND, 192, SIDE>(c, q, w, num_sms, st);
-    default: return launch_heads<KIND, 256, SIDE>(c, q, w, num_sms, st);
+    case 64: return launch_heads<KIND, 64, SIDE, AFTER>(c, q, w, num_sms, st);
+    case 80: return launch_heads<KIND, attend_dim(KIND, 80), SIDE, AFTER>(c, q, w, num_sms, st);
+    case 96: return launch_heads<KIND, 96, SIDE, AFTER>(c, q, w, num_sms, st);
+    case 128: return launch_heads<KIND, 128, SIDE, AFTER>(c, q, w, num_sms, st);
+    case 192: return launch_heads<KIND, 192, SIDE, AFTER>(c, q, w, num_sms, st);
+    default: return launch_heads<KIND, 256, SIDE, AFTER>(c, q, w, num_sms, st);
   }
 }
 

@@ -5,6 +5,6 @@
 namespace p2p {
 cudaError_t launch_kv_attend_f16_side(const KvView& c, const KvQuery* q, const KvAttendScratch& w, int num_sms,
                                       cudaStream_t st) {
-  return launch_dim<P2P_KV_F16, true>(c, q, w, num_sms, st);
+  return launch_dim<P2P_KV_F16, true, false>(c, q, w, num_sms, st);
 }
 }  // namespace p2p

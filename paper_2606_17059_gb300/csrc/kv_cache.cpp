@@ -122,22 +122,28 @@ bool rows_overlap(int64_t n, int64_t heads, int64_t dim, int64_t row, int64_t he
 cudaError_t launch_attend(const p2p::KvView& c, const p2p::KvQuery* q, const p2p::KvAttendScratch& w, int num_sms,
                           cudaStream_t st) {
   using namespace p2p;
-  const auto alone = c.type == P2P_KV_BF16  ? launch_kv_attend_bf16
-                     : c.type == P2P_KV_F16 ? launch_kv_attend_f16
-                                            : launch_kv_attend_e4m3;
-  const auto side_by_side = c.type == P2P_KV_BF16  ? launch_kv_attend_bf16_side
-                            : c.type == P2P_KV_F16 ? launch_kv_attend_f16_side
-                                                   : launch_kv_attend_e4m3_side;
-  if (!q) {  // (both are made ready)
-    const cudaError_t e = alone(c, q, w, num_sms, st);
-    return e != cudaSuccess || c.side == 0 ? e : side_by_side(c, q, w, num_sms, st);
+  using Launch = cudaError_t (*)(const KvView&, const KvQuery*, const KvAttendScratch&, int, cudaStream_t);
+  constexpr Launch kBf16[4] = {launch_kv_attend_bf16, launch_kv_attend_bf16_side, launch_kv_attend_bf16_after,
+                               launch_kv_attend_bf16_side_after};
+  constexpr Launch kF16[4] = {launch_kv_attend_f16, launch_kv_attend_f16_side, launch_kv_attend_f16_after,
+                              launch_kv_attend_f16_side_after};
+  constexpr Launch kE4m3[4] = {launch_kv_attend_e4m3, launch_kv_attend_e4m3_side, launch_kv_attend_e4m3_after,
+                               launch_kv_attend_e4m3_side_after};
+  const Launch* const of_type = c.type == P2P_KV_BF16 ? kBf16 : c.type == P2P_KV_F16 ? kF16 : kE4m3;
+  if (!q) {  // (all are made ready)
+    for (int i = 0; i < 4; ++i) {
+      if (i % 2 == 1 && c.side == 0) continue;
+      const cudaError_t e = of_type[i](c, q, w, num_sms, st);
+      if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
   }
   // Without shared lines it is many short rows that gain (see kSideShort): with fewer the kernel finds too little to
   // take heads together, and is then the slower of the two.
   const int dp = attend_dim(c.type, c.dim), group = q->heads / c.heads;
   const int ctas = attend_ctas(c.type, dp, attend_blocks(c.type, dp, group));
   const bool many = (int64_t)q->n * c.heads >= (int64_t)kSideRows * std::max(2, ctas) * num_sms;
-  return (c.side != 0 && (c.lines || many) ? side_by_side : alone)(c, q, w, num_sms, st);
+  return of_type[(c.side != 0 && (c.lines || many) ? 1 : 0) + (q->skip ? 2 : 0)](c, q, w, num_sms, st);
 }
 
 void* map_encoder() {
