@@ -491,7 +491,8 @@ int p2p_kv_rotation_turns(int32_t n, const double* radians, uint64_t* turns);
  * P2P_KV_F16). Each head y of queries and keys becomes, in 32 bits, w * y / sqrt(mean of y^2 + eps) where there are
  * weights; then pair (a, b) number j becomes amplitude * (a cos - b sin, a sin + b cos) of the angle 2 pi * p *
  * turns[j] / 2^64.  The queries go, rounded to `type`, to out[t * out_token_stride + h * out_head_stride + x] (q
- * itself with its strides, or memory of its own; no two rows may share values); keys and values to the cache, rounded
+ * itself with its strides, or rows that share no value with those of q, k and v; no two rows may share values; refused
+ * as well: rows among those of q, k or v, at other distances from token to token); keys and values to the cache, rounded
  * once (P2P_KV_E4M3: the quotient by their scale).  Tokens of no sequence, and those of a device-side error, are left
  * out, their queries too.  Errors as p2p_kv_write. */
 int p2p_kv_write_rotated(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* seq, const int64_t* offsets,

@@ -13,6 +13,7 @@
 
 #include "internal.h"
 #include "kv.h"
+#include "kv_strides.h"
 
 struct p2p_kv {
   p2p::KvView c = {};
@@ -517,8 +518,16 @@ int p2p_kv_write_rotated(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
     return fail(h, P2P_E_INVAL, "a pointer is not aligned to its type");
   if (rows_overlap(n_tokens, n_heads, h->c.dim, out_token_stride, out_head_stride))
     return fail(h, P2P_E_INVAL, "rows of out overlap");
-  if (q == out && (q_token_stride != out_token_stride || q_head_stride != out_head_stride))
-    return fail(h, P2P_E_INVAL, "q and out start together but have other strides");
+  // (A row is read whole before it is written, but rows of others are read at any time.)
+  using p2p::rows_meet;
+  const p2p::RowsAt to = {out, out_token_stride, out_head_stride, n_heads};
+  const bool same = q == out && (n_tokens == 1 || q_token_stride == out_token_stride) &&
+                    (n_heads == 1 || q_head_stride == out_head_stride);
+  if (!same && rows_meet({q, q_token_stride, q_head_stride, n_heads}, to, n_tokens, h->c.dim))
+    return fail(h, P2P_E_INVAL, "out overlaps q without being it");
+  if (rows_meet({k, token_stride, head_stride, h->c.heads}, to, n_tokens, h->c.dim) ||
+      rows_meet({v, token_stride, head_stride, h->c.heads}, to, n_tokens, h->c.dim))
+    return fail(h, P2P_E_INVAL, "out overlaps k or v");
   DeviceGuard g(h->device);
   const p2p::KvTurn a = {q, k, v, out, q_token_stride, q_head_stride, out_token_stride, out_head_stride, token_stride,
                          head_stride, r.turns, r.q_weight, r.k_weight, r.amplitude, r.eps, n_heads, type, r.dim,
