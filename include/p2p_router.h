@@ -513,6 +513,12 @@ int p2p_kv_attend_prompt(p2p_kv* kv, int32_t layer, int32_t n, const int32_t* se
                          int32_t n_heads, float scale, int32_t window, void* out, int64_t out_token_stride,
                          int64_t out_head_stride, float* lse);
 
+/* The kernel of p2p_kv_attend_prompt and p2p_kv_attend_shared waits for parts of itself.  Where nothing moves in it for
+ * more than `cycles` clock cycles (4e9 unless set here), which should never be, it ends with a device-side error, and
+ * what it wrote to out and lse is not to be used; later calls are not affected.  (-cycles, to see that happen: the kernel
+ * then never says that its work is done, and gives up waiting for that.)  Errors: P2P_E_INVAL. */
+int p2p_kv_set_patience(p2p_kv* kv, int64_t cycles);
+
 /* Bytes of `work` that p2p_kv_attend_shared needs for n rows of n_heads query heads; -1 for arguments out of range. */
 int64_t p2p_kv_attend_shared_work(const p2p_kv* kv, int32_t n, int32_t n_heads);
 

@@ -26,6 +26,7 @@ __all__ = [
     "p2p_kv_create", "p2p_kv_destroy", "p2p_kv_set_stream", "p2p_kv_sync", "p2p_kv_last_error", "p2p_kv_launch_count",
     "p2p_kv_stats", "p2p_kv_extend", "p2p_kv_write", "p2p_kv_fork", "p2p_kv_trim", "p2p_kv_compact", "p2p_kv_attend",
     "p2p_kv_rotation_turns", "p2p_kv_write_rotated", "p2p_kv_attend_prompt", "p2p_kv_attend_shared", "p2p_kv_attend_shared_work",
+    "p2p_kv_set_patience",
 ]
 
 P2P_OK, P2P_E_INVAL, P2P_E_NOMEM, P2P_E_FORMAT, P2P_E_CUDA, P2P_E_DEVICE = 0, -1, -2, -3, -4, -5
@@ -141,6 +142,7 @@ def _load():
             "p2p_kv_attend_shared": (ctypes.c_int, [_vp, _i32, _i32, _vp, _i32, _vp, _i64, _vp, _i64, _i64, _i32, _i32, ctypes.c_float, _i32,
                                                     _vp, _i64, _i64, _vp, _vp]),
             "p2p_kv_attend_shared_work": (_i64, [_vp, _i32, _i32]),
+            "p2p_kv_set_patience": (ctypes.c_int, [_vp, _i64]),
             "p2p_router_kernel_time": (ctypes.c_int, [_vp, _i32, P(ctypes.c_char_p), P(_i64), P(ctypes.c_double)]),
         }
         for name, (res, args) in sig.items():
@@ -559,6 +561,11 @@ def p2p_kv_attend_prompt(kv, layer: int, n: int, seq, offsets, n_tokens: int, q,
     """The last tokens of each sequence; q and out are addresses (their strides are arguments)."""
     _kv_check(_load().p2p_kv_attend_prompt(kv, layer, n, _addr(seq), _addr(offsets), n_tokens, q, q_token_stride, q_head_stride, dtype,
                                            n_heads, scale, window, out, out_token_stride, out_head_stride, _addr(lse)), kv)
+
+
+def p2p_kv_set_patience(kv, cycles: int) -> None:
+    """Clock cycles after which a wait within the kernel of several new tokens and shared prefixes counts as stuck."""
+    _kv_check(_load().p2p_kv_set_patience(kv, cycles), kv)
 
 
 def p2p_kv_attend_shared_work(kv, n: int, n_heads: int) -> int:

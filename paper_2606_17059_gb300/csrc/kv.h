@@ -251,7 +251,8 @@ struct KvRowsCall {
   int64_t n_tokens, q_row, q_head, out_row, out_head;
   int32_t n, heads, group, type, window, layer;  // group: query heads a kv head
   FastDiv by_group;
-  RowsScale count;  // how work is counted
+  RowsScale count;   // how work is counted
+  int64_t patience;  // clock cycles without a sign of work after which the kernel gives up; negative: it is made to
   float scale;
   bool boxes, out32;      // whether queries come by boxes of whole tokens, and rows of out lie on 32-byte boundaries
   int32_t tile_rows;      // rows of a row tile: 128, or as many whole tokens as fit them

@@ -26,6 +26,7 @@ struct p2p_kv {
   int device = 0, num_sms = 0;
   cudaStream_t stream = nullptr;
   int64_t launches = 0;
+  int64_t patience = 4000000000;  // (some two seconds)
   char err[320] = {};
 };
 
@@ -352,6 +353,13 @@ int p2p_kv_sync(p2p_kv* h) {
   return fail(h, P2P_E_DEVICE, m);
 }
 
+int p2p_kv_set_patience(p2p_kv* h, int64_t cycles) {
+  if (!h) return fail(nullptr, P2P_E_INVAL, "cache is NULL");
+  if (cycles == 0 || cycles == INT64_MIN) return fail(h, P2P_E_INVAL, "no patience at all");
+  h->patience = cycles;
+  return P2P_OK;
+}
+
 const char* p2p_kv_last_error(const p2p_kv* h) { return h ? h->err : p2p::global_error(); }
 
 int64_t p2p_kv_launch_count(const p2p_kv* h) { return h ? h->launches : 0; }
@@ -571,6 +579,7 @@ static p2p::KvRowsCall rows_call(const p2p_kv* h, CUtensorMap& q_map, int32_t la
   const int64_t tokens = (int64_t)h->c.max_pages * h->c.page;
   if (window >= tokens) a.window = 0;  // (which is as much as a sequence can have)
   const bool wide = h->c.dim > 128;    // (as RowsShape has it)
+  a.patience = h->patience;
   a.count = p2p::rows_scale(n, n_rows, n_heads, h->c.heads, wide ? 1 : 2, a.tile_rows, wide ? 6 : 7, tokens);
   a.out32 = (uintptr_t)out % 32 == 0 && out_row % 16 == 0 && out_head % 16 == 0;
   return a;

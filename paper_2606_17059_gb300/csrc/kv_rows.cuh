@@ -38,6 +38,8 @@
 // before the first step (the schedule, cold code).  Registers: 184 a thread for softmax, where a step's logits stay, 72
 // for the others, which spill with 56.
 #pragma once
+#include <limits.h>
+
 #include "kv_math.cuh"
 #include "kv_values.cuh"
 
@@ -93,10 +95,11 @@ __device__ __forceinline__ RowsStage rows_stage(int32_t q, int32_t n, bool split
 }
 struct RowsShared {
   uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], o_full[2], unit_full[kRing], unit_empty[kRing],
-      checked[8], q_empty[2], q_raw[2], pair, pair_done, drain, raw[4][4];
+      checked[8], q_empty[2], q_raw[2], pair, pair_done, drain, done, raw[4][4];
   RowsUnit unit[kRing];
   uint32_t sums[16];
   int32_t tmem, dead;
+  int32_t signs;             // of work: not negative; changes with every stage, and within add_poison_of
   int32_t poison[kRing];     // whether values were taken out of the unit's steps
   float pair_top[128], pair_sum[128];  // of the second tile's rows, where both have the same
 };
@@ -108,28 +111,52 @@ __device__ __forceinline__ void bar_init(const uint64_t& bar, uint32_t count) {
 __device__ __forceinline__ void bar_arrive(const uint64_t& bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_of(&bar)) : "memory");
 }
+// Whether a phase is over; the thread may sleep for up to 10 ms.
 __device__ __forceinline__ bool bar_try(const uint64_t& bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.b32 %0, 1, 0, p; }"
+  asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3; selp.b32 %0, 1, 0, p; }"
                : "=r"(ok)
-               : "r"(smem_of(&bar)), "r"(parity)
+               : "r"(smem_of(&bar)), "r"(parity), "r"(10000000)
                : "memory");
   return ok;
 }
-// Waits for a phase; false where that takes seconds (which it never should: the kernel then ends and reports it).
-__device__ __forceinline__ bool bar_wait_long(const uint64_t& bar, uint32_t parity, RowsShared& sh) {
-  const long long from = clock64();
-  while (!bar_try(bar, parity)) {
+// Waits for a phase; false where the watch (bar_watch) gave up meanwhile.  Of a warp's lanes some may go on and others
+// not.  (Every wait has this in place, so it is small: with a limit of its own in each, 191 sequences of 1 to 9 new
+// tokens take 429 us, not 377.)
+__device__ __forceinline__ bool bar_wait_lane(const uint64_t& bar, uint32_t parity, RowsShared& sh) {
+  while (!bar_try(bar, parity))
     if (*(volatile int32_t*)&sh.dead) return false;
-    if (clock64() - from > 4000000000ll) {
+  return true;
+}
+// The same for a whole warp, whose lanes go on or give up together: what follows takes all of them.
+__device__ __forceinline__ bool bar_wait(const uint64_t& bar, uint32_t parity, RowsShared& sh) {
+  while (!__all_sync(~0u, bar_try(bar, parity)))
+    if (__any_sync(~0u, *(volatile int32_t*)&sh.dead)) return false;
+  return true;
+}
+// The same for the one warp that watches while it waits: where it sees no sign of work in the CTA for as long as the
+// call has patience (which should never be), all give up, and the kernel ends and reports it.
+__device__ __forceinline__ bool bar_watch(const uint64_t& bar, uint32_t parity, RowsShared& sh, long long patience) {
+  long long from = clock64();
+  int32_t signs = -1;
+  while (!__all_sync(~0u, bar_try(bar, parity))) {
+    const int32_t now = *(volatile int32_t*)&sh.signs;
+    if (now != signs) signs = now, from = clock64();
+    if (__any_sync(~0u, clock64() - from > patience)) {
       *(volatile int32_t*)&sh.dead = 1;
       return false;
     }
   }
   return true;
 }
-__device__ __forceinline__ bool bar_wait(const uint64_t& bar, uint32_t parity, RowsShared& sh) {
-  return bar_try(bar, parity) || bar_wait_long(bar, parity, sh);
+// What is still on its way when a kernel gives up, waited for with a limit (a phase may never come).
+__device__ __forceinline__ void bar_drain(const uint64_t& bar, uint32_t parity) {
+  const long long from = clock64();
+  for (uint32_t ok = 0; !ok && clock64() - from < 1 << 22;)
+    asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.b32 %0, 1, 0, p; }"
+                 : "=r"(ok)
+                 : "r"(smem_of(&bar)), "r"(parity)
+                 : "memory");
 }
 // The next phase also takes so many bytes of copies.
 __device__ __forceinline__ void bar_expect(const uint64_t& bar, uint32_t bytes) {
@@ -333,7 +360,7 @@ __device__ __forceinline__ bool seen_by_all(int32_t j, int32_t all_begin, int32_
 template <int KIND, int BT>
 __device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall& a, const RowsUnit& u, uint32_t o_at,
     int32_t j0, int32_t j1,
-                                              int32_t every, int32_t begin, int32_t end) {
+                                              int32_t every, int32_t begin, int32_t end, int32_t& signs) {
   const int lane = threadIdx.x & 31;
   constexpr int kValues = KIND == P2P_KV_E4M3 ? 16 : 8;  // of a piece
 #pragma unroll 1
@@ -342,6 +369,7 @@ __device__ __forceinline__ void add_poison_of(const KvView& c, const KvRowsCall&
     const int32_t last = j * BT + min(BT, u.end - j * BT);
 #pragma unroll 1
     for (int32_t p = max(u.begin, j * BT); p < last; ++p) {
+      if (lane == 0) *(volatile int32_t*)&signs = p;  // (the next token's number is another)
       const uint32_t e = c.by_page.div(p);
       const int32_t page = row_of(c, u.seq)[e];
       if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
@@ -409,7 +437,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     bar_init(sh.pair, 4);
     bar_init(sh.pair_done, 4);
     bar_init(sh.drain, 1);
-    sh.dead = 0;
+    bar_init(sh.done, S::kSoft + 7);
+    sh.dead = 0, sh.signs = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == S::kSoft + 4) {
@@ -437,11 +466,12 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     sum_of += c.heads * own_cost;
   }
   sum_of = __reduce_add_sync(~0u, sum_of);
-  broken = __any_sync(~0u, broken);
+  broken = __any_sync(~0u, broken);  // (~0 in the place of a sum, which is less)
   if (lane == 0) sh.sums[turn] = broken ? ~0u : sum_of;
   __syncthreads();
   after_sync();
-  const uint32_t of_warp = lane < kAll ? sh.sums[lane] : 0, total = __any_sync(~0u, of_warp == ~0u) ? 0 : __reduce_add_sync(~0u, of_warp);
+  const uint32_t of_warp = lane < kAll ? sh.sums[lane] : 0,
+      total = __any_sync(~0u, of_warp == ~0u) ? 0 : __reduce_add_sync(~0u, of_warp);
   // (Shares of kRowsSet at least, so that no two begin at the same step inside a unit.  One prompt of 540 tokens, 14 / 2
   // heads of 64: 14.8 us, and with shares of four at least 16.5, of eight 20.7.)
   const uint32_t ctas = min(gridDim.x, max(1u, total / kRowsSet));
@@ -551,8 +581,8 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             if (!bar_wait(sh.o_full[tile], o_phase, sh)) return;
             o_phase ^= 1;
             after_sync();
-            if (sh.poison[now]) add_poison_of<KIND, kBt>(c, a, u, o_at, from, to, u.split ? 2 : 1, valid ? begin
-                : INT32_MAX, end);
+            if (sh.poison[now])
+              add_poison_of<KIND, kBt>(c, a, u, o_at, from, to, u.split ? 2 : 1, valid ? begin : INT32_MAX, end, sh.signs);
           }
           const float2 z2 = parts_of(sum);
           float z = z2.x + z2.y, fade = 1.f, fade2 = 0.f;  // of this tile's sums, and of the second's
@@ -922,13 +952,9 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
     };
     run();
     asm volatile("cp.async.wait_all;" ::: "memory");
-    if (*(volatile int32_t*)&sh.dead) {  // (copies that are still on their way, waited for with a limit)
-      for (int i = 0; i < kStages; ++i)
-        for (int x = 0; x < 1 << 16 && !bar_try(sh.full[i], i < stage ? phase ^ 1 : phase); ++x) {
-        }
-      for (int v = 0; v < 4; ++v)
-        for (int x = 0; x < 1 << 16 && !bar_try(sh.raw[warp - S::kSoft][v], raw_phase >> v & 1); ++x) {
-        }
+    if (*(volatile int32_t*)&sh.dead) {  // (copies that are still on their way)
+      for (int i = 0; i < kStages; ++i) bar_drain(sh.full[i], i < stage ? phase ^ 1 : phase);
+      for (int v = 0; v < 4; ++v) bar_drain(sh.raw[warp - S::kSoft][v], raw_phase >> v & 1);
     }
   } else if (warp == S::kSoft + 4) {
     // ================================ products
@@ -957,13 +983,13 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       int32_t all_begin = 0, all_end = 0;
       // The values of step j, at the current stage.
       const auto values_there = [&](int32_t j) {
-        if (!bar_wait(sh.full[stage], phase, sh)) return false;
-        if (!seen_by_all<kBt>(j, all_begin, all_end) && !bar_wait(sh.checked[stage], phase, sh)) return false;
+        if (!bar_wait_lane(sh.full[stage], phase, sh)) return false;
+        if (!seen_by_all<kBt>(j, all_begin, all_end) && !bar_wait_lane(sh.checked[stage], phase, sh)) return false;
         async_fence();
         return true;
       };
       const auto add_values = [&](int tile, int at_stage, bool add, bool last) {
-        if (!bar_wait(sh.p_full[tile], p_phase >> tile & 1, sh)) return false;
+        if (!bar_wait_lane(sh.p_full[tile], p_phase >> tile & 1, sh)) return false;
         p_phase ^= 1u << tile;
         after_sync();
         const uint64_t v0 = matrix(stage_at + at_stage * S::kStage, kBt * 128);
@@ -973,9 +999,11 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
         if (last) mma_done(sh.o_full[tile], one);
         return true;
       };
+      // (Its lanes wait each for itself, without a vote: nothing here needs them all, and the one that issues drains at
+      // the end.)
       const auto run = [&]() {
         for (;;) {
-          if (!bar_wait(sh.unit_full[ring], ring_phase, sh)) return;
+          if (!bar_wait_lane(sh.unit_full[ring], ring_phase, sh)) return;
           const RowsUnit& u = sh.unit[ring];
           if (u.rows == 0) return;
           const int32_t j0 = u.j0, j1 = u.j1;
@@ -987,13 +1015,13 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
 #pragma unroll
           for (int i = 0; i < kTiles; ++i)
             if (t1[i] > t0[i]) {
-              if (!bar_wait(sh.q_full[i], q_phase[i], sh)) return;
+              if (!bar_wait_lane(sh.q_full[i], q_phase[i], sh)) return;
               q_phase[i] ^= 1;
               async_fence();
             }
           if (one) bar_arrive(sh.unit_empty[ring]);
           next_unit();
-          if (!bar_wait(sh.full[stage], phase, sh)) return;
+          if (!bar_wait_lane(sh.full[stage], phase, sh)) return;
           async_fence();
           if (!split) {
 #pragma unroll
@@ -1012,7 +1040,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
                 if (j >= t0[i] && j < t1[i] && !add_values(i, v_stage, j > t0[i], j + 1 == t1[i])) return;
                 if (j + 1 < j1 && j + 1 >= t0[i] && j + 1 < t1[i]) {
                   if (!keys) {
-                    if (!bar_wait(sh.full[stage], phase, sh)) return;
+                    if (!bar_wait_lane(sh.full[stage], phase, sh)) return;
                     async_fence();
                     keys = true;
                   }
@@ -1021,7 +1049,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               }
               mma_done(sh.empty[v_stage], one);
               if (j + 1 < j1) {
-                if (!keys && !bar_wait(sh.full[stage], phase, sh)) return;
+                if (!keys && !bar_wait_lane(sh.full[stage], phase, sh)) return;
                 mma_done(sh.empty[stage], one);
                 next_stage();
               }
@@ -1033,7 +1061,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
             mma_done(sh.empty[stage], one);
             next_stage();
             if (n > 1) {
-              if (!bar_wait(sh.full[stage], phase, sh)) return;
+              if (!bar_wait_lane(sh.full[stage], phase, sh)) return;
               async_fence();
               logits(1, stage, n <= 3);
               mma_done(sh.empty[stage], one);
@@ -1046,7 +1074,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
               mma_done(sh.empty[stage], one);
               next_stage();
               if (x + 2 < n) {
-                if (!bar_wait(sh.full[stage], phase, sh)) return;
+                if (!bar_wait_lane(sh.full[stage], phase, sh)) return;
                 async_fence();
                 logits(i, stage, x + 4 >= n);
                 mma_done(sh.empty[stage], one);
@@ -1058,15 +1086,15 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       };
       run();
       mma_done(sh.drain, one);
-      for (int i = 0; i < 1 << 20 && !bar_try(sh.drain, 0); ++i) {
-      }
+      bar_drain(sh.drain, 0);
     }
     __syncwarp();
   } else if (warp == S::kSoft + 5) {
     // ================================ schedule: the units of this CTA's share
     if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    const long long patience = a.patience < 0 ? -a.patience : a.patience;
     const auto emit = [&](const RowsUnit& u) {
-      if (!bar_wait(sh.unit_empty[ring], ring_phase ^ 1, sh)) return false;
+      if (!bar_watch(sh.unit_empty[ring], ring_phase ^ 1, sh, patience)) return false;
       if (lane == 0) {
         sh.unit[ring] = u;
         sh.poison[ring] = 0;
@@ -1209,10 +1237,11 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       }
     }
     if (lane == 0) w.joins[blockIdx.x] = join;
-    if (alive) {
+    if (alive && a.patience >= 0) {  // (else the others wait for a word that never comes: see p2p_kv_set_patience)
       RowsUnit u = {};
-      emit(u);
+      alive = emit(u);
     }
+    if (alive) bar_watch(sh.done, 0, sh, patience);
   } else {
     // ================================ infinities and NaN among values that not all rows see
     if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -1316,7 +1345,7 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
           __syncwarp();
           // (A stage is free when the products and both helpers are done with it: one that fell a turn behind would take
           // phases for one another.)
-          if (lane == 0) bar_arrive(sh.checked[stage]), bar_arrive(sh.empty[stage]);
+          if (lane == 0) bar_arrive(sh.checked[stage]), bar_arrive(sh.empty[stage]), ++*(volatile int32_t*)&sh.signs;
           if (++stage == kStages) stage = 0, phase ^= 1;
         }
         __syncwarp();
@@ -1325,7 +1354,11 @@ __global__ void __launch_bounds__(RowsShape<KIND, DP>::kThreads, 1)
       }
     };
     run();
+    if (*(volatile int32_t*)&sh.dead)  // (queries that are still on their way)
+      for (int i = 0; i < kTiles; ++i) bar_drain(direct ? sh.q_full[i] : sh.q_raw[i], q_phase >> i & 1);
   }
+  __syncwarp();
+  if (warp != S::kSoft + 5 && lane == 0) bar_arrive(sh.done);
   __syncthreads();
   if (sh.dead && threadIdx.x == 0) atomicOr(w.err, KV_STUCK);
   if (warp == S::kSoft + 4)
