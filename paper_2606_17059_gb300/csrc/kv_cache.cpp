@@ -26,7 +26,8 @@ struct p2p_kv {
   int device = 0, num_sms = 0;
   cudaStream_t stream = nullptr;
   int64_t launches = 0;
-  int64_t patience = 4000000000;  // (some two seconds)
+  int64_t patience = 4000000000;      // (some two seconds)
+  bool many_rows = true;              // whether the kernel for many rows can be launched
   char err[320] = {};
 };
 
@@ -281,7 +282,11 @@ int p2p_kv_create(const p2p_kv_layout* layout, p2p_kv** out) {
   if (e == cudaSuccess) e = cudaMemsetAsync(n->scratch, 0, zero, nullptr);
   if (e == cudaSuccess) e = p2p::prepare_kv_pages();
   if (e == cudaSuccess) e = launch_attend(c, nullptr, n->w, sms, nullptr);
-  if (e == cudaSuccess) e = launch_rows(c, n->maps, nullptr, n->w, sms, nullptr);
+  if (e == cudaSuccess) {
+    e = launch_rows(c, n->maps, nullptr, n->w, sms, nullptr);
+    // (Compiled to other registers than it shares out: the calls that need it refuse, the cache is there.)
+    if (e == cudaErrorInvalidDeviceFunction) n->many_rows = false, e = cudaSuccess, (void)cudaGetLastError();
+  }
   // (calls may go to a stream that does not wait for this one)
   if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
   if (e != cudaSuccess) {
@@ -457,6 +462,9 @@ static int check_attend(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq,
   if (window < 0) return fail(h, P2P_E_INVAL, "negative window");
   return P2P_OK;
 }
+static int check_kernel(p2p_kv* h) {
+  return h->many_rows ? P2P_OK : fail(h, P2P_E_CUDA, "the attention of many rows was not compiled to 128 registers a thread");
+}
 static int check_rows(p2p_kv* h, int64_t n, const void* q, int32_t n_heads, const void* out, int64_t out_row,
                       int64_t out_head, const float* lse) {
   if (!q || !out) return fail(h, P2P_E_INVAL, "NULL device pointer");
@@ -595,6 +603,7 @@ int p2p_kv_attend_prompt(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   if (n == 0 || n_tokens == 0) return P2P_OK;
   if (!offsets) return fail(h, P2P_E_INVAL, "NULL device pointer");
   if (int rc = check_rows(h, n_tokens, q, n_heads, out, out_token_stride, out_head_stride, lse)) return rc;
+  if (int rc = check_kernel(h)) return rc;
   DeviceGuard g(h->device);
   CUtensorMap q_map;
   p2p::KvRowsCall a = rows_call(h, q_map, layer, n, n_tokens, seq, q, q_token_stride, q_head_stride, type, n_heads,
@@ -643,6 +652,7 @@ int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq
   if ((n_groups > 0 && !groups) || !work) return fail(h, P2P_E_INVAL, "NULL device pointer");
   if ((uintptr_t)work % 32) return fail(h, P2P_E_INVAL, "work must start on a 32-byte boundary");
   if (int rc = check_rows(h, n, q, n_heads, out, out_row_stride, out_head_stride, lse)) return rc;
+  if (int rc = check_kernel(h)) return rc;
   DeviceGuard g(h->device);
   const SharedWork at(h->c, n, n_heads);
   float* pre = (float*)work;
