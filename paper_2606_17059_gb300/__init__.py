@@ -874,7 +874,8 @@ class KvCache:
         kind = self._types.get(dtype)
         if dim != self.dim or kind is None or inner != 1 and dim > 1 or q.device != self.device:
             raise ValueError("q must be [n, query heads, head dim] on the cache's device, the last dimension contiguous")
-        empty = self._empty if self._current(self._index) == self._h.stream_address else self._empty_on_stream
+        if out is None or lse is None:
+            empty = self._empty if self._current(self._index) == self._h.stream_address else self._empty_on_stream
         if out is None:
             out = empty(shape, dtype=dtype, device=self.device)
             out_row, out_head = heads * dim, dim
