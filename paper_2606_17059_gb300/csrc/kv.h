@@ -67,9 +67,6 @@ struct KvView {
 };
 
 // Bits of the device error word.
-// What a group's rows cost together, in rows that are read alone.
-constexpr int kTogether = 4;
-
 enum { KV_BAD_SEQ = 1, KV_BAD_COUNT = 2, KV_NO_PAGES = 4, KV_BAD_PAGE = 8, KV_SHARED = 16, KV_BAD_OFFSETS = 32,
     KV_STUCK = 64 };
 
@@ -174,12 +171,12 @@ constexpr int attend_ctas(int type, int dp, int blocks) {
 // hundred tokens lose up to 18% (608 of 1 to 800 with 4 of 256 90, not 77; 2,000 of them 236, not 225) and long ones
 // 1% (512 of 1,000 to 4,000 with 8 of 128 657, not 653).
 constexpr int kSideRows = 7;
-// Parts of rows that several CTAs share, four a CTA (see the kernel), and how many have arrived (zero between
-// launches).
 struct KvJoin {        // a unit of kv_rows.cuh that CTA c0 begins and others go on with
   int64_t row;         // its first row
   int32_t rows, g0, h, parts;  // parts: 0 where there is none
 };
+// Parts of rows that several CTAs share, four a CTA (see the kernel), and how many have arrived (zero between
+// launches).
 struct KvAttendScratch {
   static constexpr int kCtasPerSm = 3;
   float* parts;      // [the more of kv_attend_parts() and kv_rows_parts()]
@@ -235,6 +232,8 @@ cudaError_t launch_kv_share(const KvView& c, int32_t* err, int32_t n, const int3
 cudaError_t launch_kv_groups(int32_t* err, int32_t n, int32_t n_groups, const int32_t* groups, cudaStream_t st);
 // Fewer shared tokens than these are read by each row for itself.
 constexpr int kSharedTokens = 64;
+// What a group's rows cost together, in rows that are read alone.
+constexpr int kTogether = 4;
 
 // Many query rows over the same keys and values (kv_rows.cuh): the last offsets[i + 1] - offsets[i] tokens of each of n
 // sequences, or, with spans, what each of n groups of rows shares.  Strides in elements.

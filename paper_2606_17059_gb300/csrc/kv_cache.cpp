@@ -635,10 +635,11 @@ int64_t p2p_kv_attend_shared_work(const p2p_kv* h, int32_t n, int32_t n_heads) {
 }
 
 // Bytes of keys and values whose reading has to be saved for groups to be worth three more launches.  Measured on one
-// GB300, prefixes read together and row by row: 256 MB saved (64 rows, 14 / 2 heads of 64, 8,320 tokens) 45 and 30 us;
-// 200 rows, 40 / 8 of 128, 320 tokens 48 and 38; 32 rows, 32 / 8 of 128, 2,112 tokens 32 and 26; 512 MB 59 and 51, 49
-// and 55, 36 and 43; 1,024 MB 69 and 91, 54 and 87, 46 and 75.  Few rows gain less, as what they read together is read
-// at a lower rate (kTogether): 8 rows, 64 / 8 of 128, 18,720 tokens (512 MB) 59 and 47, 37,440 (1,024 MB) 82 and 82.
+// GB300, prefixes read together and row by row, in us: with 256 MB saved 55 and 31 (64 rows, 14 / 2 heads of 64), 43 and
+// 36 (200 rows, 40 / 8 of 128), 35 and 29 (32 rows, 32 / 8 of 128), 56 and 43 (8 rows, 64 / 8 of 128); 448 MB 61 and 47,
+// 46 and 48, 42 and 42, 73 and 67; 640 MB 63 and 62, 46 and 61, 46 and 56, 82 and 90; 1,024 MB 67 and 94, 49 and 85, 49
+// and 83, 104 and 138.  (Few rows gain less, as what they read together is read at a lower rate: kTogether.)  One number
+// for all of them: just above it few kv heads lose up to 14 us, and many rows would gain from 384 MB on.
 constexpr int64_t kWorthSharing = (int64_t)448 << 20;
 
 int p2p_kv_attend_shared(p2p_kv* h, int32_t layer, int32_t n, const int32_t* seq, int32_t n_groups,

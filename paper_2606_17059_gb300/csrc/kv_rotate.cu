@@ -50,7 +50,8 @@ __device__ __forceinline__ TurnRow turn_row(const KvView& c, const KvTurn& a, in
 }
 
 // x / scale rounded to 32 bits, and where that is a tie of 8 bits and the quotient is not, to its side of it (see
-// divide_extreme); inverse: 1 / scale, positive and of an ordinary size.
+// divide_extreme); inverse: 1 / scale, positive and of an ordinary size.  (The product with the inverse, corrected once by
+// its exact remainder: Markstein, Computation of Elementary Functions on the IBM RISC System/6000 Processor, 1990.)
 __device__ __forceinline__ float divide(float x, float scale, float inverse) {
   const float z0 = x * inverse;
   float z = fmaf(fmaf(-z0, scale, x), inverse, z0);

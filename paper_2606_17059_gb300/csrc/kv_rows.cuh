@@ -12,7 +12,9 @@
 // transposed operand. S, P (in the place of S) and O stay in tensor memory; a thread owns a row, so maxima and sums
 // need no shuffles.  Two tiles of 128 rows take turns: while one's logits go through exp, the tensor cores work on the
 // other's.  exp(x - m) takes for m a maximum that lags the running one by at most 2^kLag (see Type), so that O is
-// rarely rescaled.
+// rarely rescaled.  P is rounded to the values' type (beside 8-bit ones to f16), as the tensor cores take both operands
+// in 16 bits: each term is off by half a step at most, 2^-8 of it in bf16 and 2^-11 in f16, to either side; z is summed
+// from what was not rounded.  Maxima, sums, S, O and parts have 32 bits.
 //
 // A CTA of the persistent grid takes an equal, contiguous share of all units' steps (a step: kBt tokens); a unit that
 // several CTAs share goes to scratch in parts, which a launch after this one joins in their order (kv_join.cu), so
@@ -36,10 +38,9 @@
 // tensor memory, the maximum, rounding and the way back) and the waits between them.  Short ones are bound by what a
 // unit costs beside its steps: 1.5 to 2 us of its queries' way in and its results' way out, and 5 to 10 us of the launch
 // before the first step (the schedule, cold code).  Registers: 184 a thread for softmax, where a step's logits stay, 72
-// for the others, which spill with 56.
+// for the others, which spill more with 56 (of the kernels for heads of up to 128, 32 to 112 bytes a thread are spilled,
+// none beyond).
 #pragma once
-#include <limits.h>
-
 #include "kv_math.cuh"
 #include "kv_values.cuh"
 

@@ -14,7 +14,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 1024, kWarps = kThreads / 32, kCluster = 8, kAhead = 8;
+constexpr int kThreads = 1024, kCluster = 8, kAhead = 8;
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     share_kernel(KvView c, int32_t* err, int32_t n, const int32_t* seq, int32_t n_groups, const int32_t* groups,
